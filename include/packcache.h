@@ -371,6 +371,99 @@ pc_status pc_window_cache(pc_window *w, pc_cache *out);
  * the accumulated temporal shift, and which buffer (0 = hist_a, 1 = hist_b) is active. */
 pc_status pc_window_state(pc_window *w, int32_t *n_frames, int32_t *counts, int64_t *t_shift, int32_t *active);
 
+/* ---- Cache in four bits.
+ *
+ * A pc_q4_segment holds keys and values at five bits a value: codes of four bits, and per 32 channels of a row a step and a
+ * low in half precision.  A group x of 32 channels becomes
+ *     low = fp16(min x), step = fp16((max x - low) / 15), code = clamp(rint((x - low) * (1 / step)), 0, 15)  (step 0: code 0)
+ * in fp32 from the inputs, and stands for low + step * code.  Values beyond +-65504 are held as +-65504 and NaN as 0, with
+ * PC_ERR_INVALID_ARG in the status word; steps are multiples of 2^-24, so a group whose values differ by less than 15 * 2^-25 is
+ * held as its low.
+ *
+ * Keys are held rotated, at (t + t_shift, h, w) of their position: a single token's attention then rotates its queries only.
+ * The rebase of Eq. 9 shifts t of a whole segment, so it moves the stored t and t_shift in opposite directions and leaves the
+ * codes as they are; queries that meet the segment are rotated at t + t_shift.  t + t_shift of every token and query has to
+ * lie inside the rotary table (pc_layer_desc.max_pos[0]).
+ *
+ * A token's row, for each KV head: the key's record, then the value's, each of 5 d / 8 bytes:
+ *     d / 2 bytes of codes, d / 32 steps (fp16), d / 32 lows (fp16).
+ * Codes of a key: 32-bit word number t * (d / 32) + g (t = 0 .. 3) holds channels 32 g + 8 t .. + 7, the first in its lowest bits.
+ * Codes of a value: 16-bit word number n * (d / 32) + g (n = 0 .. 7) holds channels 32 g + 4 n .. + 3, the first in its lowest bits.
+ * (The parts of a channel group that one thread of the attention kernel multiplies lie side by side.) */
+typedef struct {
+    void *rows;       /* device [capacity][Hkv][2][5 d / 8] bytes, 16-byte aligned */
+    int32_t *pos;     /* device [capacity][4], as in pc_segment */
+    float *weight;    /* device [capacity] fp32: attention weight a token has received (see pc_q4_attend); NULL: not kept */
+    int32_t n_tokens; /* tokens in use */
+    int32_t capacity; /* tokens allocated */
+    int32_t t_shift;  /* what rebases have taken from t since the keys were rotated; >= 0 */
+} pc_q4_segment;
+
+typedef struct {
+    pc_q4_segment anchors; /* never evicted; its weight is not used */
+    pc_q4_segment history;
+} pc_q4_cache;
+
+/* Write the rows of src into dst's rows at, at + 1, ...: keys rotated and held in four bits, values likewise, positions copied,
+ * weights (if kept) set to zero.  at <= dst->n_tokens; dst->n_tokens becomes at + src->n_tokens where that is more (the frame that
+ * is being generated can be written to one place pass after pass).
+ * Errors: PC_ERR_INVALID_ARG, PC_ERR_CAPACITY (at + src->n_tokens > dst->capacity). */
+pc_status pc_q4_store(pc_ctx *ctx, const pc_segment *src, pc_q4_segment *dst, int32_t at, void *stream);
+
+/* The way back: tokens first .. first + n - 1 of src as rows 0 .. n - 1 of dst in the context's element type, keys turned back by
+ * the rotation they are held with, positions copied.  dst->n_tokens becomes n.
+ * Errors: PC_ERR_INVALID_ARG, PC_ERR_CAPACITY (n > dst->capacity). */
+pc_status pc_q4_load(pc_ctx *ctx, const pc_q4_segment *src, int32_t first, int32_t n, pc_segment *dst, void *stream);
+
+/* Workspaces of pc_q4_attend for caches of up to max_tokens tokens (anchors and history) and calls of up to the context's max_q
+ * queries.  parts: PC_Q4_FRAMES adds room for the values of the whole cache in 16 bits, with which calls of many queries run on the
+ * context's tensor-core attention kernel; PC_Q4_WEIGH adds room for the logits of at least one query and is needed for weights.
+ * Errors: PC_ERR_INVALID_ARG, PC_ERR_CUDA. */
+typedef struct pc_q4 pc_q4;
+enum { PC_Q4_FRAMES = 1, PC_Q4_WEIGH = 2 };
+pc_status pc_q4_create(pc_ctx *ctx, int32_t max_tokens, int32_t parts, pc_q4 **out);
+pc_status pc_q4_destroy(pc_q4 *w);
+
+/* Attention of n_q queries (a single token, a few, or a whole frame) over anchors ++ history:
+ *   out[i][h] = softmax_j((R q_ih).(R k_j,g) / sqrt(d)) v_j,g,  g = h / (Hq/Hkv), k and v what the codes stand for.
+ *   valid device [history tokens] bytes or NULL: 0 = masked (Eq. 1), whatever its row, its step and its low hold.  A call whose keys are
+ *   all masked gives out 0 and lse -infinity.
+ *   weigh host or NULL: the weights of the history are brought up to date in the same call,
+ *     weight_j <- decay * weight_j + gain * (mean over queries and heads of the probability of token j).
+ *   out device [n_q][Hq][d]; lse device [n_q][Hq] fp32 or NULL.
+ * Sums and softmax statistics are fp32.  Queries go to the multiply-adds as two fp16 parts (22 bits), probabilities times steps as one
+ * (bf16 contexts) or two (fp32).  Calls of many queries without mask and weights, on a context with tensor-core attention and a
+ * workspace with PC_Q4_FRAMES, instead turn the cache into 16 bits once and run pc_attend_frame's kernel (its roundings: rotated queries,
+ * keys, values and probabilities in bf16); they use the context's rotated-key scratch as pc_attend_frame does, and what
+ * pc_attend_prepare fixed is dropped.  Calls that share a workspace have to be ordered on the GPU.
+ * Errors: PC_ERR_INVALID_ARG (no keys at all, weigh without PC_Q4_WEIGH or without weights), PC_ERR_CAPACITY, PC_ERR_CUDA. */
+typedef struct {
+    float decay, gain;
+} pc_q4_weigh;
+pc_status pc_q4_attend(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, const void *q, const int32_t *q_pos, int32_t n_q,
+                       void *out, float *lse, const pc_q4_weigh *weigh, void *stream);
+
+/* ---- Eviction by accumulated attention weight.
+ *
+ * Keeps `keep` tokens of src (all, if it has no more): the `recent` newest, and of the older ones those with the largest weight, equal
+ * weights by lower index (-0 == +0).  A token with valid == 0 is taken only after all others among the older ones.  Kept rows go to dst in
+ * their order; K, V or 4-bit rows, (h, w, tag) and weights are bit copies, delta_t is subtracted from t (and added to the 4-bit
+ * segment's t_shift, so that its keys stay as they are; delta_t >= -t_shift).  A NaN weight is recorded in the status word.
+ *   weight device [n_tokens]; valid device bytes or NULL; dst and src must not overlap; dst->n_tokens is set;
+ *   sel_idx device out [min(keep, n_tokens)]: the source index of every kept token, ascending.
+ * Errors: PC_ERR_INVALID_ARG (recent > keep, overlapping buffers, no weights), PC_ERR_CAPACITY. */
+typedef struct {
+    int32_t keep, recent, delta_t;
+} pc_evict_params;
+pc_status pc_q4_evict(pc_ctx *ctx, const pc_q4_segment *src, const pc_evict_params *params, const uint8_t *valid, pc_q4_segment *dst,
+                      int32_t *sel_idx, void *stream);
+pc_status pc_evict(pc_ctx *ctx, const pc_segment *src, const float *weight, const pc_evict_params *params, const uint8_t *valid,
+                   pc_segment *dst, float *dst_weight, int32_t *sel_idx, void *stream);
+
+/* weight_j <- decay * weight_j + gain * mass_j for n tokens: accumulates what pc_attend_mass gives, for pc_evict.
+ * Both device fp32, 4-byte alignment is enough.  Errors: PC_ERR_INVALID_ARG. */
+pc_status pc_accumulate(pc_ctx *ctx, const float *mass, int32_t n, float decay, float gain, float *weight, void *stream);
+
 /* Wait for the stream, then return and clear the first device-side event
  * recorded since the last poll (PC_OK if none). */
 pc_status pc_poll_status(pc_ctx *ctx, void *stream);

@@ -28,7 +28,8 @@ EXPORTS = ["pc_create", "pc_destroy", "pc_plan_budget", "pc_score", "pc_compact"
            "pc_window_create", "pc_window_destroy", "pc_window_append", "pc_window_append_masked", "pc_window_update", "pc_window_cache",
            "pc_window_state", "pc_attend_prepare", "pc_attend_prepared", "pc_attend_mass", "pc_frame_step",
            "pc_forget_anchors", "pc_set_wait_limit_us", "pc_test_expect_extra_bytes", "pc_test_leave_parts", "pc_window_step", "pc_window_step_host", "pc_set_timing_skip",
-           "pc_get_span", "pc_probe_stream_read", "pc_probe_mma_rate"]
+           "pc_get_span", "pc_probe_stream_read", "pc_probe_mma_rate", "pc_q4_store", "pc_q4_load", "pc_q4_create", "pc_q4_destroy",
+           "pc_q4_attend", "pc_q4_evict", "pc_evict", "pc_accumulate"]
 
 
 class pc_layer_desc(C.Structure):
@@ -160,6 +161,9 @@ def load() -> C.CDLL:
     lib.pc_window_cache.argtypes = [C.c_void_p, C.POINTER(pc_cache)]
     lib.pc_window_state.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int64),
                                     C.POINTER(C.c_int32)]
+    lib.pc_q4_create.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
+    lib.pc_q4_destroy.argtypes = [C.c_void_p]
+    lib.pc_accumulate.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
     _lib = lib
     return lib
 
@@ -527,3 +531,119 @@ class Window:
             self.close()
         except Exception:
             pass
+
+
+# ---- cache in four bits, and eviction by accumulated attention weight
+PC_Q4_FRAMES, PC_Q4_WEIGH = 1, 2
+
+
+@dataclass
+class Q4Segment:
+    """A run of tokens held in four bits: rows [capacity][Hkv][2][5 d / 8] bytes, pos [capacity][4] int32, weight [capacity] fp32
+    or None; t_shift is what rebases have taken from t since the keys were rotated."""
+    rows: Optional[torch.Tensor]
+    pos: Optional[torch.Tensor]
+    weight: Optional[torch.Tensor]
+    n_tokens: int
+    t_shift: int = 0
+
+    @staticmethod
+    def empty(ctx: Context, capacity: int, t_shift: int = 0, weight: bool = False) -> "Q4Segment":
+        """Room for ``capacity`` tokens of the context's heads, with weights on request; capacity 0: nothing at all."""
+        if capacity == 0:
+            return Q4Segment(None, None, None, 0, t_shift)
+        d = ctx.desc
+        rows = torch.empty(capacity, d.n_kv_heads, 2, 5 * d.head_dim // 8, dtype=torch.uint8, device="cuda")
+        pos = torch.empty(capacity, 4, dtype=torch.int32, device="cuda")
+        return Q4Segment(rows, pos, torch.zeros(capacity, device="cuda") if weight else None, 0, t_shift)
+
+    @property
+    def capacity(self) -> int:
+        return 0 if self.rows is None else self.rows.shape[0]
+
+
+@dataclass
+class Q4Cache:
+    """Anchors held apart from the history, both in four bits."""
+    anchors: Q4Segment
+    history: Q4Segment
+
+
+class Q4Work:
+    """Workspaces of pc_q4_attend for caches of up to max_tokens tokens; frames: room for calls of many queries on the tensor-core
+    kernel; weigh: room for weights."""
+
+    def __init__(self, ctx: Context, max_tokens: int, frames: bool = False, weigh: bool = False):
+        self.ctx = ctx                                   # the context outlives its workspaces
+        h = C.c_void_p()
+        parts = (PC_Q4_FRAMES if frames else 0) | (PC_Q4_WEIGH if weigh else 0)
+        _check(load().pc_q4_create(ctx.handle, max_tokens, parts, C.byref(h)), "pc_q4_create")
+        self.handle = h
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            load().pc_q4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def pc_q4_store(ctx: Context, src: Segment, dst: Q4Segment, at: Optional[int] = None, stream=None) -> None:
+    """Write src's rows to dst's rows from ``at`` on (default: behind the tokens in use)."""
+    if at is None:
+        at = dst.n_tokens
+    _check(_native().q4_store(ctx.handle, src, dst, at, _stream(stream)), "pc_q4_store")
+    dst.n_tokens = max(dst.n_tokens, at + src.n_tokens)
+
+
+def pc_q4_load(ctx: Context, src: Q4Segment, first: int, n: int, dst: Segment, stream=None) -> None:
+    """Tokens first .. first + n - 1 of src as dst's rows, keys turned back to how they came in."""
+    _check(_native().q4_load(ctx.handle, src, first, n, dst, _stream(stream)), "pc_q4_load")
+    dst.n_tokens = n
+
+
+def pc_q4_attend(work: Q4Work, cache: Q4Cache, q: torch.Tensor, q_pos: torch.Tensor, valid: Optional[torch.Tensor] = None,
+                 weigh: Optional[tuple] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 want_lse: bool = False, stream=None):
+    """Attention over a cache in four bits; weigh = (decay, gain): bring cache.history.weight up to date in the same call."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+    decay, gain = weigh if weigh is not None else (None, None)
+    _check(_native().q4_attend(work.handle, cache, valid, q, q_pos, out, lse, decay, gain, _stream(stream)), "pc_q4_attend")
+    return (out, lse) if want_lse else out
+
+
+def pc_q4_evict(ctx: Context, src: Q4Segment, keep: int, recent: int, dst: Q4Segment, delta_t: int = 0,
+                valid: Optional[torch.Tensor] = None, sel_idx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Keep the ``recent`` newest tokens and the heaviest of the others, ``keep`` in all, in dst; returns sel_idx."""
+    kept = min(keep, src.n_tokens)
+    if sel_idx is None:
+        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=src.rows.device)
+    _check(_native().q4_evict(ctx.handle, src, keep, recent, delta_t, valid, dst, sel_idx, _stream(stream)), "pc_q4_evict")
+    dst.n_tokens = kept
+    dst.t_shift = src.t_shift + delta_t
+    return sel_idx
+
+
+def pc_evict(ctx: Context, src: Segment, weight: torch.Tensor, keep: int, recent: int, dst: Segment,
+             dst_weight: Optional[torch.Tensor] = None, delta_t: int = 0, valid: Optional[torch.Tensor] = None,
+             sel_idx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The same for rows in the context's element type."""
+    kept = min(keep, src.n_tokens)
+    if sel_idx is None:
+        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=weight.device)
+    _check(_native().evict(ctx.handle, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel_idx, _stream(stream)), "pc_evict")
+    dst.n_tokens = kept
+    return sel_idx
+
+
+def pc_accumulate(ctx: Context, mass: torch.Tensor, weight: torch.Tensor, decay: float, gain: float, stream=None) -> None:
+    """weight <- decay * weight + gain * mass, over mass's tokens."""
+    assert weight.numel() >= mass.numel(), "fewer weights than masses"
+    _check(load().pc_accumulate(ctx.handle, _ptr(mass), mass.numel(), decay, gain, _ptr(weight), _stream(stream)), "pc_accumulate")

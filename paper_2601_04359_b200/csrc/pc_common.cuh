@@ -31,6 +31,10 @@ enum {
     PC_WHERE_SCORE_WAIT = 8,
     PC_WHERE_MASK_COUNT = 9,
     PC_WHERE_MASS_WAIT = 10,
+    PC_WHERE_Q4_RANGE = 11,
+    PC_WHERE_Q4_POS = 12,
+    PC_WHERE_Q4_WAIT = 13,
+    PC_WHERE_EVICT_NAN = 14,
 };
 
 constexpr int PC_MAX_SEGMENTS = 3;

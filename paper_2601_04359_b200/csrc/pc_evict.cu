@@ -1,0 +1,320 @@
+// Eviction by accumulated attention weight: of a history's older tokens the ones with the largest weight, behind them the newest tokens.
+//
+// Two launches.  k_evict_select finds the kept tokens: weights become 32-bit keys whose unsigned order is the weights' (score_key); three
+// passes over digits of 11, 11 and 10 bits narrow the range in which the want-th largest key lies, and an ordered sweep writes the
+// indices of all larger keys and of the first equal ones.  One CTA for short histories; for longer ones a cluster of CTAs that
+// each hold a piece of the history in shared memory, count it, and read one another's counts through distributed shared memory: one
+// barrier of the cluster a pass.  k_evict_move copies the kept rows.
+#include <algorithm>
+
+#include "pc_q4.cuh"
+#include "pc_select.cuh"
+
+namespace {
+
+constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
+constexpr int DIGIT_BINS = 2048;
+constexpr int MAX_CLUSTER = 8;
+constexpr int CACHED = 36 * 1024;                  // keys of a CTA's piece kept in shared memory; the rest is read again
+
+struct SelectParams {
+    const float *weight;
+    const uint8_t *valid;
+    int n_old, want, recent;                       // older tokens, how many of them stay (0 < want < n_old), newest tokens
+    int piece;                                     // tokens of a CTA, a multiple of 4
+    int32_t *sel_idx;
+    int32_t *status;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm("mov.u32 %0, %cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int remote_int(uint32_t addr, uint32_t rank) {
+    uint32_t there;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+    return v;
+}
+
+// Sum of v over the threads before this one, and over all
+__device__ __forceinline__ int scan_block(int v, int *warp_sums, int &all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += x;
+    }
+    __syncthreads();                               // the sums of the call before have been read
+    if (lane == 31) warp_sums[warp] = inc;
+    __syncthreads();
+    const int w = warp_sums[lane];                 // SEL_WARPS == 32
+    all = __reduce_add_sync(0xffffffffu, w);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + inc - v;
+}
+
+__global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectParams P) {
+    extern __shared__ uint32_t keys[];             // [min(piece, CACHED)]
+    __shared__ int hist[2][DIGIT_BINS];
+    __shared__ int warp_sums[SEL_WARPS];
+    __shared__ int found[2], counts[2];
+    static_assert(SEL_WARPS == 32 && DIGIT_BINS == 2 * SEL_THREADS, "a lane reads a warp's total, a thread owns two bins");
+    pc_grid_dep_launch();
+    const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
+    const int first = rank * P.piece, n = max(0, min(P.piece, P.n_old - first));
+    for (int b = threadIdx.x; b < 2 * DIGIT_BINS; b += SEL_THREADS) (&hist[0][0])[b] = 0;
+    pc_grid_dep_wait();
+    const auto key_of = [&](int j) {
+        const float w = P.weight[first + j];
+        if (P.valid && P.valid[first + j] == 0) return 0u;           // after every other token
+        return max(score_key(w), 1u);
+    };
+    bool nan = false;
+    for (int j = threadIdx.x; j < n; j += SEL_THREADS) {
+        const uint32_t k = key_of(j);
+        if (j < CACHED) keys[j] = k;
+        const float w = P.weight[first + j];
+        nan |= w != w && k != 0u;
+    }
+    if (nan) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_EVICT_NAN);
+    const auto key_at = [&](int j) { return j < CACHED ? keys[j] : key_of(j); };
+
+    // digits from the top: `prefix` holds those of the want-th largest key so far
+    uint32_t prefix = 0;
+    int want = P.want;
+    __syncthreads();
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), above = pass == 0 ? 32 : (pass == 1 ? 21 : 10);
+        const uint32_t mask = (1u << (above - shift)) - 1u;
+        int *h = hist[pass & 1];
+        for (int j = threadIdx.x; j < n; j += SEL_THREADS) {
+            const uint32_t k = key_at(j);
+            if (pass == 0 || ((k ^ prefix) >> above) == 0) atomicAdd(&h[(k >> shift) & mask], 1);
+        }
+        if (ctas > 1) cluster_sync();
+        else __syncthreads();
+        // thread t owns the bins 2047 - 2 t and 2046 - 2 t: counts from the top bin down
+        const int b0 = DIGIT_BINS - 1 - 2 * threadIdx.x;
+        int c0 = 0, c1 = 0;
+        if (ctas > 1) {
+            const uint32_t at = pc_smem_u32(h + b0);
+            for (int r = 0; r < ctas; ++r) {
+                c0 += remote_int(at, r);
+                c1 += remote_int(at - 4, r);
+            }
+        } else {
+            c0 = h[b0];
+            c1 = h[b0 - 1];
+        }
+        int all;
+        const int before = scan_block(c0 + c1, warp_sums, all);
+        if (before < want && want <= before + c0 + c1) {
+            const bool second = before + c0 < want;
+            found[0] = b0 - (second ? 1 : 0);
+            found[1] = want - before - (second ? c0 : 0);
+        }
+        // the other buffer was read by all before this pass's barrier of the cluster: cleared for the next pass
+        if (pass == 1)
+            for (int b = threadIdx.x; b < DIGIT_BINS; b += SEL_THREADS) hist[0][b] = 0;
+        __syncthreads();
+        prefix |= (uint32_t)found[0] << shift;
+        want = found[1];
+    }
+    // keys above `prefix` stay, and the first `want` equal to it
+    const int per = (n + SEL_THREADS - 1) / SEL_THREADS, j0 = min(n, (int)threadIdx.x * per), j1 = min(n, j0 + per);
+    int gt = 0, eq = 0;
+    for (int j = j0; j < j1; ++j) {
+        const uint32_t k = key_at(j);
+        gt += k > prefix;
+        eq += k == prefix;
+    }
+    int all_gt, all_eq;
+    const int gt0 = scan_block(gt, warp_sums, all_gt), eq0 = scan_block(eq, warp_sums, all_eq);
+    int gt_before = gt0, eq_before = eq0;
+    if (ctas > 1) {
+        if (threadIdx.x == 0) {
+            counts[0] = all_gt;
+            counts[1] = all_eq;
+        }
+        cluster_sync();
+        for (int r = 0; r < rank; ++r) {
+            gt_before += remote_int(pc_smem_u32(&counts[0]), r);
+            eq_before += remote_int(pc_smem_u32(&counts[1]), r);
+        }
+    }
+    for (int j = j0; j < j1; ++j) {
+        const uint32_t k = key_at(j);
+        const bool keep = k > prefix || (k == prefix && eq_before < want);
+        if (keep) P.sel_idx[gt_before + min(eq_before, want)] = first + j;
+        gt_before += k > prefix;
+        eq_before += k == prefix;
+    }
+    for (int j = rank * SEL_THREADS + threadIdx.x; j < P.recent; j += ctas * SEL_THREADS) P.sel_idx[P.want + j] = P.n_old + j;
+    if (ctas > 1) cluster_sync();                  // nobody leaves while others read its counts
+}
+
+// Nothing to choose: the tokens from `first` on are kept
+__global__ void __launch_bounds__(256) k_evict_tail(int32_t *sel_idx, int first, int n) {
+    pc_grid_dep_launch();
+    pc_grid_dep_wait();
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < n) sel_idx[j] = first + j;
+}
+
+struct MoveParams {
+    const char *a, *b;                             // rows: K and V, or the 4-bit rows and nothing
+    char *to_a, *to_b;
+    const int32_t *pos;
+    int32_t *to_pos;
+    const float *weight;
+    float *to_weight;
+    const int32_t *sel_idx;
+    int n, chunks, delta_t;                        // tokens kept, 16-byte pieces of a row
+};
+
+// A warp per kept token
+__global__ void __launch_bounds__(256) k_evict_move(const MoveParams P) {
+    pc_grid_dep_launch();
+    const int r = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+    pc_grid_dep_wait();
+    if (r >= P.n) return;
+    const int s = __ldg(P.sel_idx + r);
+    const size_t from = (size_t)s * P.chunks * 16, to = (size_t)r * P.chunks * 16;
+#pragma unroll 4
+    for (int c = lane; c < P.chunks; c += 32) pc_stg_stream(P.to_a + to + c * 16, pc_ldg_stream(P.a + from + c * 16));
+    if (P.b)
+#pragma unroll 4
+        for (int c = lane; c < P.chunks; c += 32) pc_stg_stream(P.to_b + to + c * 16, pc_ldg_stream(P.b + from + c * 16));
+    if (lane == 0) {
+        int4 p = __ldg(reinterpret_cast<const int4 *>(P.pos) + s);
+        p.x -= P.delta_t;
+        reinterpret_cast<int4 *>(P.to_pos)[r] = p;
+        if (P.to_weight) P.to_weight[r] = __ldg(P.weight + s);
+    }
+}
+
+pc_status check_params(const pc_evict_params *p) {
+    if (!p || p->keep < 0 || p->recent < 0 || p->recent > p->keep) return PC_ERR_INVALID_ARG;
+    return PC_OK;
+}
+
+pc_status select_and_move(pc_ctx *ctx, const float *weight, const pc_evict_params *p, const uint8_t *valid, int n, int32_t *sel_idx, MoveParams M,
+                          cudaStream_t stream) {
+    const int kept = std::min(p->keep, n), recent = std::min(p->recent, kept), n_old = n - recent, want = kept - recent;
+    if (kept == 0) return PC_OK;
+    if (want > 0 && want < n_old) {
+        SelectParams S{weight, valid, n_old, want, recent, 0, sel_idx, ctx->status};
+        const int ctas = n_old > 8192 ? MAX_CLUSTER : 1;
+        S.piece = ((n_old + ctas - 1) / ctas + 3) / 4 * 4;
+        const size_t smem = (size_t)std::min(S.piece, CACHED) * sizeof(uint32_t);
+        static bool attr_set[PC_MAX_DEVICES] = {};
+        if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
+        if (!attr_set[ctx->device]) {
+            PC_CUDA_TRY(cudaFuncSetAttribute(k_evict_select, cudaFuncAttributeMaxDynamicSharedMemorySize, CACHED * (int)sizeof(uint32_t)));
+            attr_set[ctx->device] = true;
+        }
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(SEL_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = ctas;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        PC_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_evict_select, S));
+    } else {
+        PC_LAUNCH(k_evict_tail, dim3((kept + 255) / 256), dim3(256), 0, stream, sel_idx, n - kept, kept);
+    }
+    M.sel_idx = sel_idx;
+    M.n = kept;
+    M.delta_t = p->delta_t;
+    PC_LAUNCH(k_evict_move, dim3((unsigned)(((long long)kept * 32 + 255) / 256)), dim3(256), 0, stream, M);
+    return PC_OK;
+}
+
+}  // namespace
+
+extern "C" pc_status pc_q4_evict(pc_ctx *ctx, const pc_q4_segment *src, const pc_evict_params *params, const uint8_t *valid, pc_q4_segment *dst,
+                                 int32_t *sel_idx, void *stream) {
+    if (!ctx || !src || !dst) return PC_ERR_INVALID_ARG;
+    pc_status st = q4_check_segment(src, true);
+    if (st == PC_OK) st = check_params(params);
+    if (st != PC_OK) return st;
+    const int64_t shift = (int64_t)src->t_shift + params->delta_t;
+    if (shift < 0 || shift > INT32_MAX) return PC_ERR_INVALID_ARG;
+    const int n = src->n_tokens, kept = std::min(params->keep, n);
+    pc_q4_segment made = *dst;
+    made.n_tokens = kept;
+    made.t_shift = (int32_t)shift;
+    if (kept > dst->capacity) return PC_ERR_CAPACITY;
+    st = q4_check_segment(&made, true);
+    if (st != PC_OK) return st;
+    if (n > 0 && !src->weight) return PC_ERR_INVALID_ARG;
+    if (kept > 0) {
+        if (!sel_idx || !pc_aligned16(sel_idx)) return PC_ERR_INVALID_ARG;
+        const size_t row = q4_row(ctx->desc);
+        if (pc_overlaps(src->rows, n * row, dst->rows, kept * row) || pc_overlaps(src->pos, (size_t)n * 16, dst->pos, (size_t)kept * 16) ||
+            pc_overlaps(src->weight, (size_t)n * 4, dst->weight, (size_t)kept * 4)) return PC_ERR_INVALID_ARG;
+        MoveParams M{};
+        M.a = static_cast<const char *>(src->rows);
+        M.to_a = static_cast<char *>(dst->rows);
+        M.pos = src->pos;
+        M.to_pos = dst->pos;
+        M.weight = src->weight;
+        M.to_weight = dst->weight;
+        M.chunks = (int)(row / 16);
+        st = select_and_move(ctx, src->weight, params, valid, n, sel_idx, M, static_cast<cudaStream_t>(stream));
+        if (st != PC_OK) return st;
+    }
+    *dst = made;
+    return PC_OK;
+}
+
+extern "C" pc_status pc_evict(pc_ctx *ctx, const pc_segment *src, const float *weight, const pc_evict_params *params, const uint8_t *valid,
+                              pc_segment *dst, float *dst_weight, int32_t *sel_idx, void *stream) {
+    if (!ctx || !src || !dst) return PC_ERR_INVALID_ARG;
+    pc_status st = pc_check_segment(src, true);
+    if (st == PC_OK) st = check_params(params);
+    if (st != PC_OK) return st;
+    const int n = src->n_tokens, kept = std::min(params->keep, n);
+    if (kept > dst->capacity) return PC_ERR_CAPACITY;
+    pc_segment made = *dst;
+    made.n_tokens = kept;
+    st = pc_check_segment(&made, true);
+    if (st != PC_OK) return st;
+    if ((n > 0 && !weight) || ((reinterpret_cast<uintptr_t>(weight) | reinterpret_cast<uintptr_t>(dst_weight)) & 3u)) return PC_ERR_INVALID_ARG;
+    if (kept > 0) {
+        if (!sel_idx || !pc_aligned16(sel_idx)) return PC_ERR_INVALID_ARG;
+        const size_t row = (size_t)ctx->desc.n_kv_heads * ctx->desc.head_dim * ctx->elem_size;
+        const void *from[2] = {src->k, src->v}, *to[2] = {dst->k, dst->v};
+        for (const void *f : from)
+            for (const void *t : to)
+                if (pc_overlaps(f, n * row, t, kept * row)) return PC_ERR_INVALID_ARG;
+        if (pc_overlaps(src->pos, (size_t)n * 16, dst->pos, (size_t)kept * 16) || pc_overlaps(weight, (size_t)n * 4, dst_weight, (size_t)kept * 4))
+            return PC_ERR_INVALID_ARG;
+        MoveParams M{};
+        M.a = static_cast<const char *>(src->k);
+        M.b = static_cast<const char *>(src->v);
+        M.to_a = static_cast<char *>(dst->k);
+        M.to_b = static_cast<char *>(dst->v);
+        M.pos = src->pos;
+        M.to_pos = dst->pos;
+        M.weight = weight;
+        M.to_weight = dst_weight;
+        M.chunks = (int)(row / 16);
+        st = select_and_move(ctx, weight, params, valid, n, sel_idx, M, static_cast<cudaStream_t>(stream));
+        if (st != PC_OK) return st;
+    }
+    *dst = made;
+    return PC_OK;
+}

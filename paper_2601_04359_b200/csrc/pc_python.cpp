@@ -17,7 +17,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value;
+PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift;
 PyObject *g_as_i32;       // numpy.ascontiguousarray(x, dtype=int32), for anything that is not an int32 array already
 
 bool failed() { return PyErr_Occurred() != nullptr; }
@@ -136,6 +136,23 @@ bool segment_of(PyObject *o, pc_segment *out) {
     Py_XDECREF(k);
     Py_XDECREF(v);
     Py_XDECREF(pos);
+    return !failed();
+}
+
+bool q4_segment_of(PyObject *o, pc_q4_segment *out) {
+    *out = pc_q4_segment{};
+    PyObject *rows = PyObject_GetAttr(o, s_rows), *pos = PyObject_GetAttr(o, s_pos), *weight = PyObject_GetAttr(o, s_weight);
+    if (rows && pos && weight) {
+        out->rows = tensor_ptr(rows);
+        if (!failed()) out->pos = static_cast<int32_t *>(tensor_ptr(pos));
+        if (!failed()) out->weight = static_cast<float *>(tensor_ptr(weight));
+        if (!failed()) out->n_tokens = int_attr(o, s_n_tokens);
+        if (!failed()) out->t_shift = int_attr(o, s_t_shift);
+        if (!failed() && rows != Py_None) out->capacity = rows_of(rows);
+    }
+    Py_XDECREF(rows);
+    Py_XDECREF(pos);
+    Py_XDECREF(weight);
     return !failed();
 }
 
@@ -323,6 +340,77 @@ PyObject *window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {       // w
     return Py_BuildValue("ii", (int)st, (int)regime);
 }
 
+PyObject *q4_store(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, src, dst, at, stream
+    if (!arity(n, 5)) return nullptr;
+    pc_segment src{};
+    pc_q4_segment dst{};
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[4]);
+    const int32_t at = int_of(a[3]);
+    if (failed() || !segment_of(a[1], &src) || !q4_segment_of(a[2], &dst)) return nullptr;
+    return call([&] { return pc_q4_store(static_cast<pc_ctx *>(ctx), &src, &dst, at, stream); });
+}
+
+PyObject *q4_load(PyObject *, PyObject *const *a, Py_ssize_t n) {           // ctx, src, first, n, dst, stream
+    if (!arity(n, 6)) return nullptr;
+    pc_q4_segment src{};
+    pc_segment dst{};
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[5]);
+    const int32_t first = int_of(a[2]), count = int_of(a[3]);
+    if (failed() || !q4_segment_of(a[1], &src) || !segment_of(a[4], &dst)) return nullptr;
+    return call([&] { return pc_q4_load(static_cast<pc_ctx *>(ctx), &src, first, count, &dst, stream); });
+}
+
+PyObject *q4_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {         // work, cache, valid, q, q_pos, out, lse, decay, gain (None: no weights), stream
+    if (!arity(n, 10)) return nullptr;
+    pc_q4_cache cache{};
+    Tensors<5> t;
+    pc_q4_weigh weigh{};
+    void *work = handle_of(a[0]), *stream = stream_of(a[9]);
+    const bool weighs = a[7] != Py_None;
+    if (weighs) {
+        weigh.decay = (float)PyFloat_AsDouble(a[7]);
+        weigh.gain = (float)PyFloat_AsDouble(a[8]);
+    }
+    if (failed()) return nullptr;
+    PyObject *anchors = PyObject_GetAttr(a[1], s_anchors), *history = PyObject_GetAttr(a[1], s_history);
+    const bool ok = anchors && history && q4_segment_of(anchors, &cache.anchors) && q4_segment_of(history, &cache.history);
+    Py_XDECREF(anchors);
+    Py_XDECREF(history);
+    if (!ok || !t.take(a + 2)) return nullptr;
+    const int32_t n_q = rows_of(a[3]);
+    if (failed()) return nullptr;
+    return call([&] {
+        return pc_q4_attend(static_cast<pc_q4 *>(work), &cache, static_cast<uint8_t *>(t.p[0]), t.p[1], static_cast<int32_t *>(t.p[2]), n_q, t.p[3],
+                            static_cast<float *>(t.p[4]), weighs ? &weigh : nullptr, stream);
+    });
+}
+
+PyObject *q4_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, src, keep, recent, delta_t, valid, dst, sel, stream
+    if (!arity(n, 9)) return nullptr;
+    pc_q4_segment src{}, dst{};
+    Tensors<1> valid, sel;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[8]);
+    const pc_evict_params p{int_of(a[2]), int_of(a[3]), int_of(a[4])};
+    if (failed() || !q4_segment_of(a[1], &src) || !valid.take(a + 5) || !q4_segment_of(a[6], &dst) || !sel.take(a + 7)) return nullptr;
+    return call([&] {
+        return pc_q4_evict(static_cast<pc_ctx *>(ctx), &src, &p, static_cast<uint8_t *>(valid.p[0]), &dst, static_cast<int32_t *>(sel.p[0]), stream);
+    });
+}
+
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {             // ctx, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel, stream
+    if (!arity(n, 11)) return nullptr;
+    pc_segment src{}, dst{};
+    Tensors<1> weight, valid;
+    Tensors<2> to;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[10]);
+    const pc_evict_params p{int_of(a[3]), int_of(a[4]), int_of(a[5])};
+    if (failed() || !segment_of(a[1], &src) || !weight.take(a + 2) || !valid.take(a + 6) || !segment_of(a[7], &dst) || !to.take(a + 8)) return nullptr;
+    return call([&] {
+        return pc_evict(static_cast<pc_ctx *>(ctx), &src, static_cast<float *>(weight.p[0]), &p, static_cast<uint8_t *>(valid.p[0]), &dst,
+                        static_cast<float *>(to.p[0]), static_cast<int32_t *>(to.p[1]), stream);
+    });
+}
+
 PyObject *set_i32_converter(PyObject *, PyObject *f) {
     Py_INCREF(f);
     Py_XSETREF(g_as_i32, f);
@@ -332,6 +420,7 @@ PyObject *set_i32_converter(PyObject *, PyObject *f) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(plan_budget), FAST(total), FAST(score), FAST(compact), FAST(attend_frame), FAST(attend_prepare), FAST(attend_prepared),
                          FAST(attend_mass), FAST(frame_step), FAST(window_append), FAST(window_step),
+                         FAST(q4_store), FAST(q4_load), FAST(q4_attend), FAST(q4_evict), FAST(evict),
                          {"set_i32_converter", set_i32_converter, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackcache.so on the binding's objects.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -340,7 +429,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackc
 PyMODINIT_FUNC PyInit__packcache_py(void) {
     struct { PyObject **at; const char *name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_is_contiguous, "is_contiguous"}, {&s_shape, "shape"},
         {&s_k, "k"}, {&s_v, "v"}, {&s_pos, "pos"}, {&s_n_tokens, "n_tokens"}, {&s_anchors, "anchors"}, {&s_history, "history"},
-        {&s_frame_count, "frame_count"}, {&s_value, "value"}};
+        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"}};
     for (auto &x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;
     return PyModule_Create(&module);

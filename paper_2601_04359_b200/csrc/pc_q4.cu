@@ -1,0 +1,310 @@
+// Rows of the 4-bit cache: written from, and read back into, rows of the context's element type.
+//
+// Both directions are bound by memory: a token of 8 KV heads x 128 channels is 4,096 bytes in bf16 and 1,280 in four bits.  A thread owns
+// eight channels of a row, so a group of 32 channels is four neighbouring lanes (two shuffles give its range) and the d / 8 lanes of a
+// token go through up to HEADS of its heads: the four rotary table entries of a thread's channels are looked up once for all of them,
+// and the loads of all heads are in flight together.
+#include "pc_q4.cuh"
+
+namespace {
+
+constexpr int ROW_THREADS = 256;
+constexpr int HEADS = 4;                           // heads of a token that one group of lanes takes
+
+template <bool F32> struct Eight { uint4 a; };
+template <> struct Eight<true> { uint4 a, b; };
+
+template <bool F32> __device__ __forceinline__ Eight<F32> load8(const void *base, size_t elem) {
+    Eight<F32> e;
+    if constexpr (F32) {
+        const char *p = static_cast<const char *>(base) + elem * 4;
+        e.a = pc_ldg_stream(p);
+        e.b = pc_ldg_stream(p + 16);
+    } else {
+        e.a = pc_ldg_stream(static_cast<const char *>(base) + elem * 2);
+    }
+    return e;
+}
+template <bool F32> __device__ __forceinline__ void unpack8(const Eight<F32> &e, float (&x)[8]) {
+    const uint32_t w[4] = {e.a.x, e.a.y, e.a.z, e.a.w};
+    if constexpr (F32) {
+        const uint32_t u[4] = {e.b.x, e.b.y, e.b.z, e.b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[i] = __uint_as_float(w[i]); x[4 + i] = __uint_as_float(u[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = pc_bf16_lo(w[i]); x[2 * i + 1] = pc_bf16_hi(w[i]); }
+    }
+}
+template <bool F32> __device__ __forceinline__ void store8(void *base, size_t elem, const float (&x)[8]) {
+    if constexpr (F32) {
+        uint4 *p = reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 4);
+        p[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        p[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+    } else {
+        *reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2) =
+            make_uint4(pc_pack_bf16(x[0], x[1]), pc_pack_bf16(x[2], x[3]), pc_pack_bf16(x[4], x[5]), pc_pack_bf16(x[6], x[7]));
+    }
+}
+
+// A pair turned by (cos, sin) with every product and sum rounded by itself, so that the codes follow from plain fp32 arithmetic
+__device__ __forceinline__ void turn(float &x0, float &x1, float2 cs) {
+    const float a = __fsub_rn(__fmul_rn(x0, cs.x), __fmul_rn(x1, cs.y)), b = __fadd_rn(__fmul_rn(x0, cs.y), __fmul_rn(x1, cs.x));
+    x0 = a;
+    x1 = b;
+}
+
+// Codes, step and low of this thread's eight channels; all four lanes of a group get the same step and low.
+__device__ __forceinline__ uint32_t quantise8(float (&x)[8], __half &step, __half &low, bool &bad) {
+    float lo = 0.f, hi = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        bad |= !(fabsf(x[i]) <= Q4_MAX);
+        x[i] = x[i] != x[i] ? 0.f : fminf(fmaxf(x[i], -Q4_MAX), Q4_MAX);
+        lo = i ? fminf(lo, x[i]) : x[i];
+        hi = i ? fmaxf(hi, x[i]) : x[i];
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    low = __float2half_rn(lo);
+    const float l = __half2float(low);
+    step = __float2half_rn(__fmul_rn(__fsub_rn(hi, l), 1.0f / 15.0f));
+    const float s = __half2float(step), inv = s > 0.f ? __frcp_rn(s) : 0.f;
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = fminf(fmaxf(rintf(__fmul_rn(__fsub_rn(x[i], l), inv)), 0.f), 15.f);
+        word |= (uint32_t)c << (4 * i);
+    }
+    return word;
+}
+
+struct RowsArgs {
+    const void *k, *v;          // rows in the element type (store: source; load: destination, written through the non-const copies)
+    void *k_out, *v_out;
+    const int32_t *pos_in;
+    int32_t *pos_out;
+    char *q4;                   // row 0 of the 4-bit rows of the call
+    float *weight;
+    int n, n_kv, slices;        // tokens, KV heads, slices of HEADS heads
+    int t_shift;
+    int32_t *status;
+};
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_rope_dev rope) {
+    constexpr int LANES = D / 8, NG = D / Q4_GROUP, REC = q4_record(D);
+    pc_grid_dep_launch();
+    const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
+    const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
+    const bool live = token < A.n;                 // lanes of a warp stay together for the shuffles
+    const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
+    const int g = u >> 2, t = u & 3;
+    pc_grid_dep_wait();
+    Eight<F32> kr[HEADS], vr[HEADS];
+    const size_t at = ((size_t)token * A.n_kv + h0) * D + u * 8;
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+        if (h < heads) {
+            kr[h] = load8<F32>(A.k, at + h * D);
+            vr[h] = load8<F32>(A.v, at + h * D);
+        } else {
+            kr[h] = Eight<F32>{};
+            vr[h] = Eight<F32>{};
+        }
+    float2 cs[4] = {};
+    bool bad_pos = false, bad = false;
+    if (live) {
+        const int4 p = __ldg(reinterpret_cast<const int4 *>(A.pos_in) + token);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cs[i] = pc_rope_cs_clamped(rope, u * 4 + i, p.x + A.t_shift, p.y, p.z, bad_pos);
+        if (h0 == 0 && u == 0) {
+            reinterpret_cast<int4 *>(A.pos_out)[token] = p;
+            if (A.weight) A.weight[token] = 0.f;
+        }
+    }
+    if (bad_pos) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
+    char *row = A.q4 + ((size_t)token * A.n_kv + h0) * (2 * REC);
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+        float x[8];
+        __half ks, kl, vs, vl;
+        unpack8<F32>(kr[h], x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], cs[i]);
+        const uint32_t kc = quantise8(x, ks, kl, bad);
+        unpack8<F32>(vr[h], x);
+        const uint32_t vc = quantise8(x, vs, vl, bad);
+        // 16-bit words n = 2t (channels 0-3) and 2t + 1 (4-7) of group g: the even group's lane writes the former for both groups of a
+        // pair, the odd one's the latter
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, (g & 1) ? vc & 0xFFFFu : vc >> 16, 4);
+        if (h < heads) {
+            char *k = row + h * (2 * REC), *v = k + REC;
+            reinterpret_cast<uint32_t *>(k)[t * NG + g] = kc;
+            reinterpret_cast<uint32_t *>(v)[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)] =
+                (g & 1) ? other | (vc & 0xFFFF0000u) : (vc & 0xFFFFu) | (other << 16);
+            __half *sk = reinterpret_cast<__half *>(k + D / 2), *sv = reinterpret_cast<__half *>(v + D / 2);
+            if (t == 0) sk[g] = ks;
+            if (t == 1) sk[NG + g] = kl;
+            if (t == 2) sv[g] = vs;
+            if (t == 3) sv[NG + g] = vl;
+        }
+    }
+    if (bad) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_RANGE);
+}
+
+// FROM_POS: keys turned back from (t + t_shift, h, w) to how they came in; else from t_shift alone (they stay rotated at their positions)
+template <int D, bool F32, bool FROM_POS>
+__global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_rope_dev rope) {
+    constexpr int LANES = D / 8, NG = D / Q4_GROUP, REC = q4_record(D);
+    pc_grid_dep_launch();
+    const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
+    const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
+    const bool live = token < A.n;
+    const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
+    const int g = u >> 2, t = u & 3;
+    pc_grid_dep_wait();
+    const char *row = A.q4 + ((size_t)token * A.n_kv + h0) * (2 * REC);
+    uint32_t kc[HEADS], vc[HEADS], kq[HEADS], vq[HEADS];       // codes; step and low of the thread's group
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+        kc[h] = vc[h] = kq[h] = vq[h] = 0;
+        if (h < heads) {
+            const char *k = row + h * (2 * REC), *v = k + REC;
+            const uint16_t *sk = reinterpret_cast<const uint16_t *>(k + D / 2), *sv = reinterpret_cast<const uint16_t *>(v + D / 2);
+            kc[h] = reinterpret_cast<const uint32_t *>(k)[t * NG + g];
+            vc[h] = reinterpret_cast<const uint32_t *>(v)[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)];
+            kq[h] = sk[g] | (uint32_t)sk[NG + g] << 16;
+            vq[h] = sv[g] | (uint32_t)sv[NG + g] << 16;
+        }
+    }
+    float2 cs[4] = {};
+    bool bad_pos = false;
+    const bool turned = FROM_POS || A.t_shift != 0;
+    if (live && turned) {
+        int4 p = make_int4(0, 0, 0, 0);
+        if constexpr (FROM_POS) p = __ldg(reinterpret_cast<const int4 *>(A.pos_in) + token);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cs[i] = pc_rope_cs_clamped(rope, u * 4 + i, p.x + A.t_shift, p.y, p.z, bad_pos);
+            cs[i].y = -cs[i].y;
+        }
+        if constexpr (FROM_POS)
+            if (h0 == 0 && u == 0) reinterpret_cast<int4 *>(A.pos_out)[token] = p;
+    }
+    if (bad_pos) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
+    const size_t at = ((size_t)token * A.n_kv + h0) * D + u * 8;
+    const auto value = [](uint32_t word, int i, float step, float low) { return __fmaf_rn(step, (float)((word >> (4 * i)) & 15u), low); };
+    const auto half_of = [](uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu))); };
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, (g & 1) ? vc[h] & 0xFFFFu : vc[h] >> 16, 4);
+        const uint32_t vw = (g & 1) ? (vc[h] & 0xFFFF0000u) | other : (vc[h] & 0xFFFFu) | (other << 16);
+        if (h < heads) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = value(kc[h], i, half_of(kq[h]), half_of(kq[h] >> 16));
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], cs[i]);
+            }
+            store8<F32>(A.k_out, at + h * D, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = value(vw, i, half_of(vq[h]), half_of(vq[h] >> 16));
+            store8<F32>(A.v_out, at + h * D, x);
+        }
+    }
+}
+
+unsigned row_blocks(const pc_layer_desc &D, int n, int slices) {
+    const long long threads = (long long)n * slices * (D.head_dim / 8);
+    return (unsigned)((threads + ROW_THREADS - 1) / ROW_THREADS);
+}
+
+#define Q4_ROWS_CASES(KERNEL, ...)                                                                                                \
+    do {                                                                                                                          \
+        const dim3 grid(row_blocks(ctx->desc, A.n, A.slices)), block(ROW_THREADS);                                                \
+        const bool f32 = ctx->desc.dtype == PC_F32;                                                                               \
+        if (ctx->desc.head_dim == 128 && f32) PC_LAUNCH((KERNEL<128, true __VA_ARGS__>), grid, block, 0, stream, A, ctx->rope);        \
+        else if (ctx->desc.head_dim == 128) PC_LAUNCH((KERNEL<128, false __VA_ARGS__>), grid, block, 0, stream, A, ctx->rope);         \
+        else if (f32) PC_LAUNCH((KERNEL<64, true __VA_ARGS__>), grid, block, 0, stream, A, ctx->rope);                                 \
+        else PC_LAUNCH((KERNEL<64, false __VA_ARGS__>), grid, block, 0, stream, A, ctx->rope);                                         \
+    } while (0)
+
+}  // namespace
+
+extern "C" pc_status pc_q4_store(pc_ctx *ctx, const pc_segment *src, pc_q4_segment *dst, int32_t at, void *stream_) {
+    if (!ctx || !src || !dst) return PC_ERR_INVALID_ARG;
+    pc_status st = pc_check_segment(src, true);
+    if (st != PC_OK) return st;
+    if (at < 0 || at > dst->n_tokens || dst->n_tokens > dst->capacity || dst->t_shift < 0) return PC_ERR_INVALID_ARG;
+    if (src->n_tokens > dst->capacity - at) return PC_ERR_CAPACITY;
+    if (src->n_tokens == 0) return PC_OK;
+    pc_q4_segment whole = *dst;
+    whole.n_tokens = whole.n_tokens > at + src->n_tokens ? whole.n_tokens : at + src->n_tokens;
+    st = q4_check_segment(&whole, false);
+    if (st != PC_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    RowsArgs A{};
+    A.k = src->k;
+    A.v = src->v;
+    A.pos_in = src->pos;
+    A.pos_out = dst->pos + (size_t)at * 4;
+    A.q4 = static_cast<char *>(dst->rows) + (size_t)at * q4_row(ctx->desc);
+    A.weight = dst->weight ? dst->weight + at : nullptr;
+    A.n = src->n_tokens;
+    A.n_kv = ctx->desc.n_kv_heads;
+    A.slices = (A.n_kv + HEADS - 1) / HEADS;
+    A.t_shift = dst->t_shift;
+    A.status = ctx->status;
+    Q4_ROWS_CASES(k_q4_store);
+    *dst = whole;
+    return PC_OK;
+}
+
+extern "C" pc_status pc_q4_load(pc_ctx *ctx, const pc_q4_segment *src, int32_t first, int32_t n, pc_segment *dst, void *stream_) {
+    if (!ctx || !src || !dst) return PC_ERR_INVALID_ARG;
+    pc_status st = q4_check_segment(src, true);
+    if (st != PC_OK) return st;
+    if (first < 0 || n < 0 || n > src->n_tokens - first) return PC_ERR_INVALID_ARG;
+    if (n > dst->capacity) return PC_ERR_CAPACITY;
+    pc_segment filled = *dst;
+    filled.n_tokens = n;
+    st = pc_check_segment(&filled, true);
+    if (st != PC_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n > 0) {
+        RowsArgs A{};
+        A.k_out = dst->k;
+        A.v_out = dst->v;
+        A.pos_in = src->pos + (size_t)first * 4;
+        A.pos_out = dst->pos;
+        A.q4 = static_cast<char *>(src->rows) + (size_t)first * q4_row(ctx->desc);
+        A.n = n;
+        A.n_kv = ctx->desc.n_kv_heads;
+        A.slices = (A.n_kv + HEADS - 1) / HEADS;
+        A.t_shift = src->t_shift;
+        A.status = ctx->status;
+#define Q4_COMMA ,
+        Q4_ROWS_CASES(k_q4_load, Q4_COMMA true);
+    }
+    dst->n_tokens = n;
+    return PC_OK;
+}
+
+pc_status pc_q4_launch_thaw(pc_ctx *ctx, const pc_q4_segment *src, void *k_rot, void *v, cudaStream_t stream) {
+    RowsArgs A{};
+    A.k_out = k_rot;
+    A.v_out = v;
+    A.q4 = static_cast<char *>(src->rows);
+    A.n = src->n_tokens;
+    A.n_kv = ctx->desc.n_kv_heads;
+    A.slices = (A.n_kv + HEADS - 1) / HEADS;
+    A.t_shift = src->t_shift;
+    A.status = ctx->status;
+    Q4_ROWS_CASES(k_q4_load, Q4_COMMA false);
+    return PC_OK;
+}

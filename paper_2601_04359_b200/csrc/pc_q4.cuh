@@ -1,0 +1,29 @@
+// What the kernels of the 4-bit cache share: the layout of a row and the checks of a segment.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "pc_common.cuh"
+
+constexpr int Q4_GROUP = 32;                       // channels that share a step and a low
+constexpr int Q4_STEP = 16;                        // keys that a warp of the attention kernel takes at a time
+constexpr float Q4_MAX = 65504.f;                  // largest value of half precision
+
+__host__ __device__ constexpr int q4_record(int d) { return d / 2 + d / 8; }       // bytes of a key or a value
+inline size_t q4_row(const pc_layer_desc &D) { return (size_t)D.n_kv_heads * 2 * q4_record(D.head_dim); }
+
+inline pc_status q4_check_segment(const pc_q4_segment *s, bool allow_empty) {
+    if (!s) return PC_ERR_INVALID_ARG;
+    if (s->n_tokens < 0 || s->capacity < s->n_tokens || s->t_shift < 0) return PC_ERR_INVALID_ARG;
+    if (s->n_tokens == 0) return allow_empty ? PC_OK : PC_ERR_INVALID_ARG;
+    if (!s->rows || !s->pos || !pc_aligned16(s->rows) || !pc_aligned16(s->pos)) return PC_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(s->weight) & 3u) return PC_ERR_INVALID_ARG;
+    return PC_OK;
+}
+
+inline bool pc_overlaps(const void *a, size_t na, const void *b, size_t nb) {
+    const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+    return a && b && x < y + nb && y < x + na;
+}
+
+// Rows of a segment in bf16 for the tensor-core attention kernel: keys turned back by t_shift only (they stay rotated at their positions)
+pc_status pc_q4_launch_thaw(pc_ctx *ctx, const pc_q4_segment *src, void *k_rot, void *v, cudaStream_t stream);

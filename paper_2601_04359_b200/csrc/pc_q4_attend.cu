@@ -1,0 +1,765 @@
+// Attention of few queries over the 4-bit cache, and the weights that tokens receive from it.
+//
+// Mathematics.  With codes c, steps s and lows l of a key's channel groups g,
+//     q . k = sum_g s_g (q_g . c_g) + sum_g l_g sum(q_g),          out = sum_j p_j v_j = sum_g (sum_j (p_j s_jg) c_jg + sum_j p_j l_jg),
+// so no value is ever decoded: the codes go to the tensor cores as they are, the step scales a sum over 32 channels (keys) or a
+// probability (values), and the lows take one multiply-add instruction per 16 keys each.  A code becomes an fp16 number with one AND: the low four bits
+// of a 16-bit half are the subnormal c 2^-24, the next four c 2^-20; the powers of two come off at the end.  Queries are scaled by a power of two
+// per row and split into two fp16 parts (22 bits).  Softmax runs in base 2 with the running maximum and sum in fp32.
+//
+// Shape.  m16n8k16 instructions with 16 keys (channels, for the values) as rows and 8 query rows of one KV head as columns: a warp
+// takes one KV head and 8 query rows and goes through the keys 16 at a time; the warps of a CTA cover the KV heads (and several
+// blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  Rows come by one bulk copy per token into a ring of
+// tiles that the warps fill in turn; a pad between rows in shared memory keeps the lanes' reads on different banks.  CTAs split
+// the keys evenly; k_q4_join merges their parts, k_q4_weigh turns the logits that the history left into weights.
+#include <algorithm>
+#include <new>
+
+#include "pc_q4.cuh"
+
+struct pc_q4 {
+    pc_ctx *ctx;
+    int max_tokens, parts;
+    float *part_o, *part_ml, *lse;     // partial sums, (maximum, sum), and lse of a call (device)
+    size_t part_rows;
+    float *logits;                     // [history token][rows of a pass]
+    size_t logit_floats;
+    void *v;                           // values of the whole cache in bf16 (PC_Q4_FRAMES)
+    size_t v_rows;
+};
+
+namespace {
+
+constexpr int ROWS = 8;                // query rows of a warp
+constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
+constexpr int MAX_STAGES = 8;
+constexpr int RING_AT = 256;           // barriers and flags before it
+constexpr int RING_BYTES = 210 * 1024;
+constexpr float P_SCALE = 4.f;         // probabilities times steps stay below fp16's largest: 4 * 2 * 65504 / 15
+
+struct Q4Params {
+    const char *rows[2];               // anchors, history
+    int n[2], shift[2];
+    const uint8_t *valid;              // of the history, or NULL
+    const void *q;
+    const int32_t *q_pos;
+    int n_q, n_q_heads, n_kv, group, n_rows;      // n_rows = n_q * group: query rows of a KV head
+    int row_bytes;                     // of a token
+    int heads, blocks, subs;           // of a CTA: KV heads, blocks of 8 query rows, parts of the keys
+    int block_groups;                  // CTAs that share a set of heads
+    int steps0, steps;                 // steps of 16 keys: the anchors', all
+    int stages, stride, stage_bytes;   // ring of tiles of `subs` steps; bytes from row to row
+    float *part_o, *part_ml;           // [split][KV head * n_rows + row]
+    float *logits;                     // [history token][n_kv * n_rows] or NULL
+    float scale;                       // log2(e) / sqrt(d)
+    int32_t *status;
+    uint32_t wait_us;
+};
+
+struct JoinParams {
+    const float *part_o, *part_ml;
+    int splits, rows, n_rows, group, n_q_heads;
+    void *out;
+    float *lse, *lse_rows;             // the caller's [query][head] and the workspace's [row], either may be NULL
+};
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
+__device__ __forceinline__ uint32_t lds16(uint32_t a) { uint16_t v; asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a)); return v; }
+// N 32-bit words of shared memory (2 or 4; N = 1 for the values of d = 64)
+template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N]) {
+    if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
+    else w[0] = lds32(a);
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {         // an 8 x 8 matrix of 16-bit values, two a lane
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t mul_half(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// Key of a step that is row i (0 .. 7) of the instruction's upper half.  With rows of shared memory 32 bytes past a multiple of 128 apart, lanes that are
+// served together read different banks: key codes (16 bytes a lane, rows i and i + 1 of an even i together) and value codes (8 bytes
+// a lane, four even or four odd rows together).
+__device__ __forceinline__ int key_of_row(int i) { return (0x57463120u >> (4 * i)) & 7; }
+
+template <int D> struct Queries {      // the B operand of Q K^T: column = query row lane / 4
+    static constexpr int NG = D / Q4_GROUP;
+    uint32_t hi[2 * NG][2], lo[2 * NG][2];
+    uint32_t sum0, sum1;               // sums over the channel groups, in fp16 parts
+    float f0, f1;                      // what the sums of columns 2 (lane % 4) and + 1 are to be multiplied by
+};
+
+// Query rows of a block, rotated at (t + shift, h, w), times log2(e) / sqrt(d): channels 32 g + 8 (lane % 4) .. + 7 of row lane / 4
+template <int D, bool F32>
+__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, int kv_head, int block, int shift, Queries<D> &Q) {
+    constexpr int NG = D / Q4_GROUP;
+    const int lane = threadIdx.x & 31, t = lane & 3, r = block * ROWS + (lane >> 2);
+    float x[NG][8];
+    float most = 0.f;
+    if (r < P.n_rows) {
+        const int i = r / P.group, head = kv_head * P.group + r % P.group;
+        const size_t at = ((size_t)i * P.n_q_heads + head) * D + 8 * t;
+        const int4 p = __ldg(reinterpret_cast<const int4 *>(P.q_pos) + i);
+        bool bad = false;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            if constexpr (F32) {
+                const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(P.q) + at + g * Q4_GROUP);
+                const float4 a = __ldg(q), b = __ldg(q + 1);
+                x[g][0] = a.x; x[g][1] = a.y; x[g][2] = a.z; x[g][3] = a.w;
+                x[g][4] = b.x; x[g][5] = b.y; x[g][6] = b.z; x[g][7] = b.w;
+            } else {
+                const uint4 a = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(P.q) + at + g * Q4_GROUP));
+                const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { x[g][2 * k] = pc_bf16_lo(w[k]); x[g][2 * k + 1] = pc_bf16_hi(w[k]); }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 cs = pc_rope_cs_clamped(rope, 16 * g + 4 * t + k, p.x + shift, p.y, p.z, bad);
+                const float2 y = pc_rotate(x[g][2 * k], x[g][2 * k + 1], cs);
+                x[g][2 * k] = y.x * P.scale;
+                x[g][2 * k + 1] = y.y * P.scale;
+                most = fmaxf(most, fmaxf(fabsf(x[g][2 * k]), fabsf(x[g][2 * k + 1])));
+            }
+        }
+        if (bad) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
+    } else {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[g][k] = 0.f;
+    }
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
+    const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
+    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+    float total[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        total[g] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            x[g][k] *= up;
+            total[g] += x[g][k];
+        }
+        total[g] += __shfl_xor_sync(0xffffffffu, total[g], 1);
+        total[g] += __shfl_xor_sync(0xffffffffu, total[g], 2);
+        // channels of the code words' 16-bit halves: (0, 4) (2, 6) in bits 0-3 and 8-11, (1, 5) (3, 7) in bits 4-7 and 12-15, 2^4 larger
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const float m = s ? 0.0625f : 1.f, y0 = x[g][s + 2 * b] * m, y1 = x[g][s + 2 * b + 4] * m;
+                const uint32_t h = pack_half(y0, y1);
+                const float2 back = halves(h);
+                Q.hi[2 * g + s][b] = h;
+                Q.lo[2 * g + s][b] = pack_half(y0 - back.x, y1 - back.y);
+            }
+    }
+    // sums of the groups against the lows: k index (2 t, 2 t + 1) of the instruction = groups, a further fp16 part every NG indices
+    const auto part = [](float v, int n) {
+        float h = __half2float(__float2half_rn(v));
+        for (int i = 0; i < n; ++i) { v -= h; h = __half2float(__float2half_rn(v)); }
+        return h;
+    };
+    if constexpr (NG == 4) {
+        const float a = (t & 1) ? total[2] : total[0], b = (t & 1) ? total[3] : total[1];
+        Q.sum0 = pack_half(part(a, t >> 1), part(b, t >> 1));
+        Q.sum1 = t < 2 ? pack_half(part(a, 2), part(b, 2)) : 0u;
+    } else {
+        Q.sum0 = t < 3 ? pack_half(part(total[0], t), part(total[1], t)) : 0u;
+        Q.sum1 = 0u;
+    }
+    const float f = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
+    Q.f0 = __shfl_sync(0xffffffffu, f, t * 8);
+    Q.f1 = __shfl_sync(0xffffffffu, f, t * 8 + 4);
+}
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_constant__ Q4Params P, const pc_rope_dev rope) {
+    constexpr int NG = D / Q4_GROUP, REC = q4_record(D);
+    extern __shared__ __align__(128) char smem[];
+    pc_grid_dep_launch();
+    const uint32_t base = pc_smem_u32(smem), ring = base + RING_AT;
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 16 * MAX_STAGES);
+    const auto full = [&](int s) { return base + 8 * s; };
+    const auto empty = [&](int s) { return base + 8 * (MAX_STAGES + s); };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_warps = P.heads * P.blocks * P.subs;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < P.stages; ++s) {
+            pc_mbar_init(full(s), 1);
+            pc_mbar_init(empty(s), n_warps);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const int first_head = blockIdx.y / P.block_groups * P.heads, n_heads = min(P.heads, P.n_kv - first_head);
+    const int s_begin = (int)((long long)P.steps * blockIdx.x / gridDim.x), s_end = (int)((long long)P.steps * (blockIdx.x + 1) / gridDim.x);
+    const int n_tiles = (s_end - s_begin + P.subs - 1) / P.subs;
+    // a step's segment, first token and tokens
+    const auto step_at = [&](int s, int &seg, int &first) {
+        seg = s >= P.steps0;
+        first = (seg ? s - P.steps0 : s) * Q4_STEP;
+        return min(Q4_STEP, P.n[seg] - first);
+    };
+    pc_grid_dep_wait();
+
+    // A tile's rows into its stage, a bulk copy per token, by one warp
+    const uint32_t bytes = (uint32_t)n_heads * 2 * REC;
+    const size_t head_at = (size_t)first_head * 2 * REC;
+    const auto fetch = [&](int tile) {
+        const int st = tile % P.stages, s0 = s_begin + tile * P.subs, steps = min(P.subs, s_end - s0);
+        int tokens = 0;
+        for (int i = 0; i < steps; ++i) {
+            int seg, first;
+            tokens += step_at(s0 + i, seg, first);
+        }
+        if (lane == 0) pc_mbar_expect_tx(full(st), bytes * tokens);
+        __syncwarp();
+        for (int i = lane; i < steps * Q4_STEP; i += 32) {
+            int seg, first;
+            const int n = step_at(s0 + i / Q4_STEP, seg, first), k = i % Q4_STEP;
+            if (k < n) pc_bulk_g2s(ring + st * P.stage_bytes + i * P.stride, P.rows[seg] + (size_t)(first + k) * P.row_bytes + head_at, bytes, full(st));
+        }
+    };
+    // The warps take turns at refilling: before tile i one of them fetches the tile that follows in the stage of tile i - 1
+    const auto ready = [&](int tile) {
+        if (tile > 0 && warp == tile % n_warps && tile - 1 + P.stages < n_tiles) {
+            const int st = (tile - 1) % P.stages;
+            if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(st), ((tile - 1) / P.stages) & 1, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) return false;
+            fetch(tile - 1 + P.stages);
+        }
+        return __all_sync(0xffffffffu, pc_mbar_wait(full(tile % P.stages), (tile / P.stages) & 1, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us)) != 0;
+    };
+    for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile);
+
+    const int task = warp % (P.heads * P.blocks), sub = warp / (P.heads * P.blocks);
+    const int head = task % P.heads, block = (blockIdx.y % P.block_groups) * P.blocks + task / P.heads;
+    const int t = lane & 3, row = lane >> 2;
+    float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group `row`
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) O[i][j] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) L[j] = 0.f;
+    if (head < n_heads && block * ROWS < P.n_rows) {
+        Queries<D> Q;
+        int have = -1;                 // segment that Q is rotated for
+        const int k0 = key_of_row(row), va = key_of_row(2 * t), vb = key_of_row(2 * t + 1);
+        const int R = P.n_kv * P.n_rows;
+        const int r0 = block * ROWS + 2 * t;
+        for (int tile = 0; tile < n_tiles; ++tile) {
+            const int st = tile % P.stages;
+            const int s = s_begin + tile * P.subs + sub;
+            int seg = 0, first = 0, n = 0;
+            bool ok0 = false, ok1 = false;
+            if (s < s_end) {
+                n = step_at(s, seg, first);
+                ok0 = k0 < n;
+                ok1 = k0 + 8 < n;
+                if (seg == 1 && P.valid) {
+                    if (ok0) ok0 = __ldg(P.valid + first + k0) != 0;
+                    if (ok1) ok1 = __ldg(P.valid + first + k0 + 8) != 0;
+                }
+                if (seg != have) {
+                    take_queries<D, F32>(P, rope, first_head + head, block, P.shift[seg], Q);
+                    have = seg;
+                }
+            }
+            if (!ready(tile)) break;
+            if (s < s_end) {
+                const uint32_t rows = ring + st * P.stage_bytes + sub * Q4_STEP * P.stride + head * 2 * REC;
+                const uint32_t ka = rows + k0 * P.stride, kb = ka + 8 * P.stride;
+                const uint32_t b0 = __ballot_sync(0xffffffffu, ok0), b1 = __ballot_sync(0xffffffffu, ok1);
+                // ---- logits
+                uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2];
+                lds(ka + t * NG * 4, wa);
+                lds(kb + t * NG * 4, wb);
+                lds(ka + D / 2, sa);
+                lds(kb + D / 2, sb);
+                float S[4] = {0.f, 0.f, 0.f, 0.f};
+                {
+                    const uint32_t off = D / 2 + 2 * NG + (NG == 4 ? (t & 1) * 4 : 0);
+                    const uint32_t la = lds32(ka + off), lb = lds32(kb + off);
+                    mma(S, la, lb, la, lb, Q.sum0, Q.sum1);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[j] *= 1.f / 16777216.f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float C[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint32_t xa = wa[g] >> 8, xb = wb[g] >> 8;
+                    const uint32_t a0 = wa[g] & 0x000F000Fu, a1 = wb[g] & 0x000F000Fu, a2 = xa & 0x000F000Fu, a3 = xb & 0x000F000Fu;
+                    const uint32_t c0 = wa[g] & 0x00F000F0u, c1 = wb[g] & 0x00F000F0u, c2 = xa & 0x00F000F0u, c3 = xb & 0x00F000F0u;
+                    mma(C, a0, a1, a2, a3, Q.lo[2 * g][0], Q.lo[2 * g][1]);
+                    mma(C, c0, c1, c2, c3, Q.lo[2 * g + 1][0], Q.lo[2 * g + 1][1]);
+                    mma(C, a0, a1, a2, a3, Q.hi[2 * g][0], Q.hi[2 * g][1]);
+                    mma(C, c0, c1, c2, c3, Q.hi[2 * g + 1][0], Q.hi[2 * g + 1][1]);
+                    const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
+                    const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
+                    S[0] = fmaf(fa, C[0], S[0]);
+                    S[1] = fmaf(fa, C[1], S[1]);
+                    S[2] = fmaf(fb, C[2], S[2]);
+                    S[3] = fmaf(fb, C[3], S[3]);
+                }
+                S[0] = ok0 ? S[0] * Q.f0 : -INFINITY;
+                S[1] = ok0 ? S[1] * Q.f1 : -INFINITY;
+                S[2] = ok1 ? S[2] * Q.f0 : -INFINITY;
+                S[3] = ok1 ? S[3] * Q.f1 : -INFINITY;
+                if (P.logits && seg == 1) {
+                    float *at = P.logits + (size_t)(first + k0) * R + (size_t)(first_head + head) * P.n_rows + r0;
+                    if (k0 < n) {
+                        if (r0 < P.n_rows) at[0] = S[0];
+                        if (r0 + 1 < P.n_rows) at[1] = S[1];
+                    }
+                    if (k0 + 8 < n) {
+                        at += (size_t)8 * R;
+                        if (r0 < P.n_rows) at[0] = S[2];
+                        if (r0 + 1 < P.n_rows) at[1] = S[3];
+                    }
+                }
+                // ---- softmax: maximum of the 16 keys of each column
+                float x0 = fmaxf(S[0], S[2]), x1 = fmaxf(S[1], S[3]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
+                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
+                }
+                if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
+                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+                    const float c0 = n0 == -INFINITY ? 1.f : exp2_fast(m0 - n0), c1 = n1 == -INFINITY ? 1.f : exp2_fast(m1 - n1);
+                    m0 = n0;
+                    m1 = n1;
+                    l0 *= c0;
+                    l1 *= c1;
+#pragma unroll
+                    for (int i = 0; i < 2 * NG; ++i) { O[i][0] *= c0; O[i][1] *= c1; O[i][2] *= c0; O[i][3] *= c1; }
+                    L[0] *= c0;
+                    L[1] *= c1;
+                }
+                const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
+                const float p0 = exp2_fast(S[0] - z0), p1 = exp2_fast(S[1] - z1), p2 = exp2_fast(S[2] - z0), p3 = exp2_fast(S[3] - z1);
+                l0 += p0 + p2;
+                l1 += p1 + p3;
+                // ---- values: keys of rows 2 t, 2 t + 1 (and + 8) of the instruction
+                uint32_t u[4], steps[4][NG / 2], codes[4][NG / 2];
+                const uint32_t vrow[4] = {rows + REC + va * P.stride, rows + REC + vb * P.stride, rows + REC + (va + 8) * P.stride, rows + REC + (vb + 8) * P.stride};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    lds(vrow[j] + row * NG * 2, codes[j]);
+                    lds(vrow[j] + D / 2, steps[j]);
+                    u[j] = row < NG ? lds16(vrow[j] + D / 2 + 2 * NG + 2 * row) : 0u;
+                }
+                if ((b0 & b1) != 0xffffffffu) {      // what lies in the place of a masked key may be anything
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (!(((j < 2 ? b0 : b1) >> (4 * (2 * t + (j & 1)))) & 1u)) {
+                            u[j] = 0u;
+#pragma unroll
+                            for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
+                        }
+                }
+                uint32_t pl[2], ph[2];               // probabilities as the B operand: column = query row lane / 4
+                ph[0] = pack_half(p0 * P_SCALE, p1 * P_SCALE);
+                ph[1] = pack_half(p2 * P_SCALE, p3 * P_SCALE);
+                if constexpr (F32) {
+                    const float2 a = halves(ph[0]), b = halves(ph[1]);
+                    pl[0] = transpose8(pack_half(p0 * P_SCALE - a.x, p1 * P_SCALE - a.y));
+                    pl[1] = transpose8(pack_half(p2 * P_SCALE - b.x, p3 * P_SCALE - b.y));
+                }
+                ph[0] = transpose8(ph[0]);
+                ph[1] = transpose8(ph[1]);
+                const uint32_t ua = u[0] | u[1] << 16, ub = u[2] | u[3] << 16;
+                mma(L, ua, 0u, ub, 0u, ph[0], ph[1]);
+                if constexpr (F32) mma(L, ua, 0u, ub, 0u, pl[0], pl[1]);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
+                    const uint32_t ta = __byte_perm(codes[0][g / 2], codes[1][g / 2], pick), tb = __byte_perm(codes[2][g / 2], codes[3][g / 2], pick);
+                    const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
+                    const uint32_t ya = ta >> 8, yb = tb >> 8;
+                    const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
+                    const uint32_t c0 = ya & 0x000F000Fu, c1 = ya & 0x00F000F0u, c2 = yb & 0x000F000Fu, c3 = yb & 0x00F000F0u;
+                    if constexpr (F32) {
+                        // probability times step in fp32 from the two parts, split again
+                        const float2 sa2 = halves(qa), sb2 = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
+                        const float e0 = (xh.x + xl.x) * sa2.x, e1 = (xh.y + xl.y) * sa2.y, e2 = (yh.x + yl.x) * sb2.x, e3 = (yh.y + yl.y) * sb2.y;
+                        const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
+                        const float2 g0 = halves(h0), g1 = halves(h1);
+                        const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
+                        mma(O[2 * g], a0, a1, a2, a3, w0, w1);
+                        mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
+                        mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                        mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                    } else {
+                        const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
+                        mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                        mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) pc_mbar_arrive(empty(st));
+        }
+    } else {                           // no head or no rows for this warp: the ring still goes round
+        for (int tile = 0; tile < n_tiles && ready(tile); ++tile)
+            if (lane == 0) pc_mbar_arrive(empty(tile % P.stages));
+    }
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) pc_let_copies_land();
+        return;
+    }
+
+    // ---- the parts of the keys that the CTA's warps took, merged in shared memory (the ring is done with)
+    constexpr int PITCH = D + 4;
+    float *parts = reinterpret_cast<float *>(smem + RING_AT);        // [warp][8][PITCH], then [warp][8] maxima, sums
+    float *ms = parts + n_warps * ROWS * PITCH, *ls = ms + n_warps * ROWS;
+    {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+        }
+        if (row == 0) {
+            ms[warp * ROWS + 2 * t] = m0;
+            ms[warp * ROWS + 2 * t + 1] = m1;
+            ls[warp * ROWS + 2 * t] = l0;
+            ls[warp * ROWS + 2 * t + 1] = l1;
+        }
+        float *mine = parts + (warp * ROWS + 2 * t) * PITCH + 4 * row;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const float w0 = __shfl_sync(0xffffffffu, L[0], g * 4 + t), w1 = __shfl_sync(0xffffffffu, L[1], g * 4 + t);
+            constexpr float A = 16777216.f / P_SCALE, B = 1048576.f / P_SCALE, C = 1.f / P_SCALE;
+            *reinterpret_cast<float4 *>(mine + g * Q4_GROUP) =
+                make_float4(fmaf(O[2 * g][0], A, w0 * C), fmaf(O[2 * g][2], B, w0 * C), fmaf(O[2 * g + 1][0], A, w0 * C), fmaf(O[2 * g + 1][2], B, w0 * C));
+            *reinterpret_cast<float4 *>(mine + PITCH + g * Q4_GROUP) =
+                make_float4(fmaf(O[2 * g][1], A, w1 * C), fmaf(O[2 * g][3], B, w1 * C), fmaf(O[2 * g + 1][1], A, w1 * C), fmaf(O[2 * g + 1][3], B, w1 * C));
+        }
+    }
+    __syncthreads();
+    const int tasks = P.heads * P.blocks, rows_all = P.n_kv * P.n_rows;
+    for (int e = threadIdx.x; e < tasks * ROWS * (D / 4); e += blockDim.x) {
+        const int c = e % (D / 4), r = e / (D / 4) % ROWS, k = e / (D / 4) / ROWS;
+        const int h = k % P.heads, in_head = ((blockIdx.y % P.block_groups) * P.blocks + k / P.heads) * ROWS + r;
+        if (h >= n_heads || in_head >= P.n_rows) continue;
+        float M = -INFINITY, l = 0.f;
+        for (int b = 0; b < P.subs; ++b) M = fmaxf(M, ms[(b * tasks + k) * ROWS + r]);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (M != -INFINITY)
+            for (int b = 0; b < P.subs; ++b) {
+                const float f = exp2_fast(ms[(b * tasks + k) * ROWS + r] - M);
+                const float4 x = *reinterpret_cast<const float4 *>(parts + ((b * tasks + k) * ROWS + r) * PITCH + 4 * c);
+                l = fmaf(f, ls[(b * tasks + k) * ROWS + r], l);
+                o.x = fmaf(f, x.x, o.x);
+                o.y = fmaf(f, x.y, o.y);
+                o.z = fmaf(f, x.z, o.z);
+                o.w = fmaf(f, x.w, o.w);
+            }
+        const size_t at = (size_t)blockIdx.x * rows_all + (size_t)(first_head + h) * P.n_rows + in_head;
+        reinterpret_cast<float4 *>(P.part_o)[at * (D / 4) + c] = o;
+        if (c == 0) reinterpret_cast<float2 *>(P.part_ml)[at] = make_float2(M, l);
+    }
+}
+
+// Parts of a row merged: a block per row, warps take every (JOIN_THREADS / D)-th part
+constexpr int JOIN_THREADS = 512;
+template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_join(const JoinParams J) {
+    constexpr int LANES = D / 4, SETS = JOIN_THREADS / LANES;
+    __shared__ float4 sums[SETS][LANES];
+    pc_grid_dep_launch();
+    pc_grid_dep_wait();
+    const int row = blockIdx.x, lane = threadIdx.x & 31;
+    const float2 *ml = reinterpret_cast<const float2 *>(J.part_ml) + row;
+    float M = -INFINITY, l = 0.f;
+    for (int s = lane; s < J.splits; s += 32) M = fmaxf(M, ml[(size_t)s * J.rows].x);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    const float z = M == -INFINITY ? 0.f : M;
+    for (int s = lane; s < J.splits; s += 32) {
+        const float2 x = ml[(size_t)s * J.rows];
+        l = fmaf(exp2_fast(x.x - z), x.y, l);
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const int c = threadIdx.x % LANES, set = threadIdx.x / LANES;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = set; s < J.splits; s += SETS) {
+        const float f = exp2_fast(ml[(size_t)s * J.rows].x - z);
+        const float4 x = reinterpret_cast<const float4 *>(J.part_o)[((size_t)s * J.rows + row) * LANES + c];
+        sum.x = fmaf(f, x.x, sum.x);
+        sum.y = fmaf(f, x.y, sum.y);
+        sum.z = fmaf(f, x.z, sum.z);
+        sum.w = fmaf(f, x.w, sum.w);
+    }
+    sums[set][c] = sum;
+    __syncthreads();
+    const int r = row % J.n_rows, h = row / J.n_rows * J.group + r % J.group;
+    const size_t to = (size_t)(r / J.group) * J.n_q_heads + h;
+    if (threadIdx.x < LANES) {
+        for (int i = 1; i < SETS; ++i) {
+            const float4 x = sums[i][c];
+            sum.x += x.x;
+            sum.y += x.y;
+            sum.z += x.z;
+            sum.w += x.w;
+        }
+        const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);      // no key left: 0; NaN stays
+        if constexpr (F32) reinterpret_cast<float4 *>(J.out)[to * LANES + c] = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+        else reinterpret_cast<uint2 *>(J.out)[to * LANES + c] = make_uint2(pc_pack_bf16(sum.x * inv, sum.y * inv), pc_pack_bf16(sum.z * inv, sum.w * inv));
+    }
+    if (threadIdx.x == 0) {
+        const float lse2 = M + log2f(l);             // base 2; -infinity where no key is left
+        if (J.lse_rows) J.lse_rows[row] = lse2;
+        if (J.lse) J.lse[to] = lse2 * 0.6931471805599453f;
+    }
+}
+
+// weight_j <- decay weight_j + gain sum over rows of 2^(logit - lse): eight lanes a token, which take its rows in turn
+constexpr int WEIGH_THREADS = 256, WEIGH_LANES = 8;
+__global__ void __launch_bounds__(WEIGH_THREADS) k_q4_weigh(const float *__restrict__ logits, const float *__restrict__ lse, int n, int rows,
+                                                            float decay, float gain, float *__restrict__ weight) {
+    pc_grid_dep_launch();
+    const int lane = threadIdx.x % WEIGH_LANES, j = (int)(((long long)blockIdx.x * WEIGH_THREADS + threadIdx.x) / WEIGH_LANES);
+    pc_grid_dep_wait();
+    float sum = 0.f;
+    if (j < n)
+        for (int r = lane; r < rows; r += WEIGH_LANES) {
+            const float z = lse[r];
+            sum += z == -INFINITY ? 0.f : exp2_fast(logits[(size_t)j * rows + r] - z);
+        }
+#pragma unroll
+    for (int o = 1; o < WEIGH_LANES; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (j < n && lane == 0) weight[j] = fmaf(decay, weight[j], gain * sum);
+}
+
+__global__ void __launch_bounds__(256) k_accumulate(const float *__restrict__ mass, int n, float decay, float gain, float *__restrict__ weight) {
+    pc_grid_dep_launch();
+    pc_grid_dep_wait();
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < n) weight[j] = fmaf(decay, weight[j], gain * mass[j]);
+}
+
+int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// Queries i0 .. i0 + n_q - 1 through the kernels above
+pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, const void *q, const int32_t *q_pos, int n_q, void *out,
+                      float *lse, const pc_q4_weigh *weigh, float gain, cudaStream_t stream) {
+    pc_ctx *ctx = w->ctx;
+    const pc_layer_desc &D = ctx->desc;
+    const int rec2 = 2 * q4_record(D.head_dim);
+    Q4Params P{};
+    const pc_q4_segment *segs[2] = {&cache->anchors, &cache->history};
+    for (int i = 0; i < 2; ++i) {
+        P.rows[i] = static_cast<const char *>(segs[i]->rows);
+        P.n[i] = segs[i]->n_tokens;
+        P.shift[i] = segs[i]->t_shift;
+    }
+    P.valid = valid;
+    P.q = q;
+    P.q_pos = q_pos;
+    P.n_q = n_q;
+    P.n_q_heads = D.n_q_heads;
+    P.n_kv = D.n_kv_heads;
+    P.group = ctx->group;
+    P.n_rows = n_q * ctx->group;
+    P.row_bytes = (int)q4_row(D);
+    // KV heads of a CTA: up to eight, shared out evenly; then as many blocks of query rows as there are warps for; the warps left over
+    // take further parts of the keys
+    const int head_sets = div_up(P.n_kv, 8);
+    P.heads = div_up(P.n_kv, head_sets);
+    const int n_blocks = div_up(P.n_rows, ROWS);
+    P.block_groups = div_up(n_blocks, MAX_WARPS / P.heads);
+    P.blocks = div_up(n_blocks, P.block_groups);
+    P.subs = MAX_WARPS / (P.heads * P.blocks);
+    P.steps0 = div_up(P.n[0], Q4_STEP);
+    P.steps = P.steps0 + div_up(P.n[1], Q4_STEP);
+    const int piece = P.heads * rec2;
+    P.stride = piece + (32 + 128 - piece % 128) % 128;
+    P.stage_bytes = P.subs * Q4_STEP * P.stride;
+    P.stages = std::min(MAX_STAGES, RING_BYTES / P.stage_bytes);
+    P.scale = pc_q_rot_scale(D.head_dim);
+    P.status = ctx->status;
+    P.wait_us = ctx->wait_limit_us;
+    P.part_o = w->part_o;
+    P.part_ml = w->part_ml;
+    P.logits = weigh && P.n[1] > 0 ? w->logits : nullptr;
+    // parts of the keys: the count with which the CTAs' waves over the SMs take the fewest steps in all
+    const int rows = P.n_kv * P.n_rows, ctas = head_sets * P.block_groups;
+    const int most = (int)std::min<long long>({(long long)div_up(P.steps, P.subs), (long long)(w->part_rows / rows), (long long)std::max(1, 2 * ctx->sm_count / ctas)});
+    int splits = 1;
+    long long best = -1;
+    for (int s = 1; s <= most; ++s) {
+        const long long cost = (long long)div_up(ctas * s, ctx->sm_count) * (div_up(div_up(P.steps, s), P.subs) + 2);
+        if (best < 0 || cost < best) { best = cost; splits = s; }
+    }
+    const int n_warps = P.heads * P.blocks * P.subs;
+    const size_t ring = std::max<size_t>((size_t)P.stages * P.stage_bytes, (size_t)n_warps * ROWS * (D.head_dim + 4 + 2) * sizeof(float));
+    const size_t smem = RING_AT + ring;
+    const bool f32 = D.dtype == PC_F32;
+    const dim3 grid(splits, ctas), block(n_warps * 32);
+    static bool attr_set[PC_MAX_DEVICES] = {};
+    if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
+    if (!attr_set[ctx->device]) {
+        for (const auto kernel : {k_q4_attend<128, false>, k_q4_attend<128, true>, k_q4_attend<64, false>, k_q4_attend<64, true>})
+            PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+        attr_set[ctx->device] = true;
+    }
+    if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_attend<128, true>), grid, block, smem, stream, P, ctx->rope);
+    else if (D.head_dim == 128) PC_LAUNCH((k_q4_attend<128, false>), grid, block, smem, stream, P, ctx->rope);
+    else if (f32) PC_LAUNCH((k_q4_attend<64, true>), grid, block, smem, stream, P, ctx->rope);
+    else PC_LAUNCH((k_q4_attend<64, false>), grid, block, smem, stream, P, ctx->rope);
+    JoinParams J{w->part_o, w->part_ml, splits, rows, P.n_rows, P.group, P.n_q_heads, out, lse, P.logits ? w->lse : nullptr};
+    if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_join<128, true>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
+    else if (D.head_dim == 128) PC_LAUNCH((k_q4_join<128, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
+    else if (f32) PC_LAUNCH((k_q4_join<64, true>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
+    else PC_LAUNCH((k_q4_join<64, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
+    if (P.logits)
+        PC_LAUNCH(k_q4_weigh, dim3((unsigned)(((long long)P.n[1] * WEIGH_LANES + WEIGH_THREADS - 1) / WEIGH_THREADS)), dim3(WEIGH_THREADS), 0, stream,
+                  w->logits, w->lse, P.n[1], rows, weigh->decay, gain, cache->history.weight);
+    return PC_OK;
+}
+
+// The whole cache in 16 bits, then the context's tensor-core attention
+pc_status attend_frame(pc_q4 *w, const pc_q4_cache *cache, const void *q, const int32_t *q_pos, int n_q, void *out, float *lse, cudaStream_t stream) {
+    pc_ctx *ctx = w->ctx;
+    const size_t row = (size_t)ctx->desc.n_kv_heads * ctx->desc.head_dim * sizeof(__nv_bfloat16);
+    ctx->prepared_n_seg = 0;                       // the rotated-key scratch is about to be overwritten
+    ctx->anchor_rot_n = 0;
+    ctx->last_n_q = 0;
+    pc_segment segs[2];
+    int n_seg = 0;
+    size_t at = 0;                                 // rows; segments start on tile boundaries
+    for (const pc_q4_segment *s : {&cache->anchors, &cache->history}) {
+        if (s->n_tokens == 0) continue;
+        char *v = static_cast<char *>(w->v) + at * row;
+        const pc_status st = pc_q4_launch_thaw(ctx, s, static_cast<char *>(ctx->k_rot) + at * row, v, stream);
+        if (st != PC_OK) return st;
+        segs[n_seg++] = pc_segment{nullptr, v, s->pos, s->n_tokens, s->n_tokens};
+        at += (size_t)div_up(s->n_tokens, 128) * 128;
+    }
+    const pc_status st = pc_launch_attend_tc(ctx, n_seg, segs, q, q_pos, n_q, out, lse, stream, PC_TC_ROPE_Q | PC_TC_ATTEND);
+    ctx->last_n_q = 0;                             // the masses of this call's queries are not offered
+    return st;
+}
+
+}  // namespace
+
+extern "C" pc_status pc_q4_create(pc_ctx *ctx, int32_t max_tokens, int32_t parts, pc_q4 **out) {
+    if (!ctx || !out) return PC_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (max_tokens <= 0 || (parts & ~(PC_Q4_FRAMES | PC_Q4_WEIGH))) return PC_ERR_INVALID_ARG;
+    pc_q4 *w = new (std::nothrow) pc_q4();
+    if (!w) return PC_ERR_CUDA;
+    w->ctx = ctx;
+    w->max_tokens = max_tokens;
+    w->parts = parts;
+    const pc_layer_desc &D = ctx->desc;
+    // every row of the largest call once, and what two CTAs an SM leave in any split
+    w->part_rows = std::max((size_t)D.max_q * D.n_q_heads, (size_t)2 * ctx->sm_count * MAX_WARPS * ROWS);
+    const auto fill = [&]() -> pc_status {
+        PC_CUDA_TRY(cudaMalloc(&w->part_o, w->part_rows * D.head_dim * sizeof(float)));
+        PC_CUDA_TRY(cudaMalloc(&w->part_ml, w->part_rows * 2 * sizeof(float)));
+        PC_CUDA_TRY(cudaMalloc(&w->lse, (size_t)D.max_q * D.n_q_heads * sizeof(float)));
+        if (parts & PC_Q4_WEIGH) {
+            // a call's queries go in passes that fit: one at least, up to 64 MB (half of L2) of logits
+            const size_t one = (size_t)max_tokens * D.n_q_heads;
+            w->logit_floats = std::max(one, std::min(one * (size_t)D.max_q, (size_t)16 << 20));
+            PC_CUDA_TRY(cudaMalloc(&w->logits, w->logit_floats * sizeof(float)));
+        }
+        if ((parts & PC_Q4_FRAMES) && pc_tensor_core_shape(ctx)) {
+            w->v_rows = (size_t)(div_up(max_tokens, 128) + 1) * 128;
+            PC_CUDA_TRY(cudaMalloc(&w->v, w->v_rows * D.n_kv_heads * D.head_dim * sizeof(__nv_bfloat16)));
+        }
+        return PC_OK;
+    };
+    const pc_status st = fill();
+    if (st != PC_OK) {
+        pc_q4_destroy(w);
+        return st;
+    }
+    *out = w;
+    return PC_OK;
+}
+
+extern "C" pc_status pc_q4_destroy(pc_q4 *w) {
+    if (!w) return PC_ERR_INVALID_ARG;
+    cudaFree(w->part_o);
+    cudaFree(w->part_ml);
+    cudaFree(w->lse);
+    cudaFree(w->logits);
+    cudaFree(w->v);
+    delete w;
+    return PC_OK;
+}
+
+extern "C" pc_status pc_q4_attend(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, const void *q, const int32_t *q_pos, int32_t n_q,
+                                  void *out, float *lse, const pc_q4_weigh *weigh, void *stream_) {
+    if (!w || !cache) return PC_ERR_INVALID_ARG;
+    pc_ctx *ctx = w->ctx;
+    const pc_layer_desc &D = ctx->desc;
+    if (!q || !q_pos || !out || n_q <= 0) return PC_ERR_INVALID_ARG;
+    if (!pc_aligned16(q) || !pc_aligned16(q_pos) || !pc_aligned16(out) || (lse && !pc_aligned16(lse))) return PC_ERR_INVALID_ARG;
+    if (n_q > D.max_q) return PC_ERR_CAPACITY;
+    for (const pc_q4_segment *s : {&cache->anchors, &cache->history}) {
+        const pc_status st = q4_check_segment(s, true);
+        if (st != PC_OK) return st;
+    }
+    const int64_t keys = (int64_t)cache->anchors.n_tokens + cache->history.n_tokens;
+    if (keys == 0) return PC_ERR_INVALID_ARG;
+    if (keys > w->max_tokens) return PC_ERR_CAPACITY;
+    if (weigh && (!(w->parts & PC_Q4_WEIGH) || (!cache->history.weight && cache->history.n_tokens > 0))) return PC_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    // Many queries: the tensor-core kernel's rows of 128 are full, and the pass that turns the cache into 16 bits is paid once for all.
+    const size_t tile_rows = (size_t)(div_up(cache->anchors.n_tokens, 128) + div_up(cache->history.n_tokens, 128)) * 128;
+    if (n_q * ctx->group >= 128 && !valid && !weigh && w->v && ctx->attend_impl != 1 && tile_rows <= w->v_rows && tile_rows <= ctx->k_rot_rows)
+        return attend_frame(w, cache, q, q_pos, n_q, out, lse, stream);
+    int pass = n_q;
+    if (weigh && cache->history.n_tokens > 0) {
+        const size_t fit = w->logit_floats / ((size_t)cache->history.n_tokens * D.n_q_heads);
+        const int passes = div_up(n_q, (int)std::min<size_t>(fit, n_q));
+        pass = div_up(n_q, passes);
+    }
+    const size_t row = (size_t)D.n_q_heads * D.head_dim * ctx->elem_size;
+    pc_q4_weigh now{};
+    if (weigh) now = *weigh;
+    for (int i = 0; i < n_q; i += pass) {
+        const int n = std::min(pass, n_q - i);
+        const pc_status st = attend_rows(w, cache, valid, static_cast<const char *>(q) + i * row, q_pos + (size_t)i * 4, n, static_cast<char *>(out) + i * row,
+                                         lse ? lse + (size_t)i * D.n_q_heads : nullptr, weigh ? &now : nullptr,
+                                         now.gain / ((float)n_q * D.n_q_heads), stream);
+        if (st != PC_OK) return st;
+        now.decay = 1.f;                           // the first pass has taken it
+    }
+    return PC_OK;
+}
+
+extern "C" pc_status pc_accumulate(pc_ctx *ctx, const float *mass, int32_t n, float decay, float gain, float *weight, void *stream_) {
+    if (!ctx || n < 0 || (n > 0 && (!mass || !weight))) return PC_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(mass) | reinterpret_cast<uintptr_t>(weight)) & 3u) return PC_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n > 0) PC_LAUNCH(k_accumulate, dim3(div_up(n, 256)), dim3(256), 0, stream, mass, n, decay, gain, weight);
+    return PC_OK;
+}
