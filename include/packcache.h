@@ -385,13 +385,13 @@ pc_status pc_window_state(pc_window *w, int32_t *n_frames, int32_t *counts, int6
  * codes as they are; queries that meet the segment are rotated at t + t_shift.  t + t_shift of every token and query has to
  * lie inside the rotary table (pc_layer_desc.max_pos[0]).
  *
- * A token's row, for each KV head: the key's record, then the value's, each of 5 d / 8 bytes:
- *     d / 2 bytes of codes, d / 32 steps (fp16), d / 32 lows (fp16).
+ * A token's row is Hkv * 5 d / 4 bytes: the codes of the keys [Hkv][d / 2], the codes of the values [Hkv][d / 2], then for each KV head four runs of
+ * d / 32 fp16 numbers, steps and lows of the key and steps and lows of the value.
  * Codes of a key: 32-bit word number t * (d / 32) + g (t = 0 .. 3) holds channels 32 g + 8 t .. + 7, the first in its lowest bits.
  * Codes of a value: 16-bit word number n * (d / 32) + g (n = 0 .. 7) holds channels 32 g + 4 n .. + 3, the first in its lowest bits.
  * (The parts of a channel group that one thread of the attention kernel multiplies lie side by side.) */
 typedef struct {
-    void *rows;       /* device [capacity][Hkv][2][5 d / 8] bytes, 16-byte aligned */
+    void *rows;       /* device [capacity][Hkv * 5 d / 4] bytes, 16-byte aligned */
     int32_t *pos;     /* device [capacity][4], as in pc_segment */
     float *weight;    /* device [capacity] fp32: attention weight a token has received (see pc_q4_attend); NULL: not kept */
     int32_t n_tokens; /* tokens in use */

@@ -539,7 +539,7 @@ PC_Q4_FRAMES, PC_Q4_WEIGH = 1, 2
 
 @dataclass
 class Q4Segment:
-    """A run of tokens held in four bits: rows [capacity][Hkv][2][5 d / 8] bytes, pos [capacity][4] int32, weight [capacity] fp32
+    """A run of tokens held in four bits: rows [capacity][Hkv * 5 d / 4] bytes, pos [capacity][4] int32, weight [capacity] fp32
     or None; t_shift is what rebases have taken from t since the keys were rotated."""
     rows: Optional[torch.Tensor]
     pos: Optional[torch.Tensor]
@@ -553,7 +553,7 @@ class Q4Segment:
         if capacity == 0:
             return Q4Segment(None, None, None, 0, t_shift)
         d = ctx.desc
-        rows = torch.empty(capacity, d.n_kv_heads, 2, 5 * d.head_dim // 8, dtype=torch.uint8, device="cuda")
+        rows = torch.empty(capacity, d.n_kv_heads * 5 * d.head_dim // 4, dtype=torch.uint8, device="cuda")
         pos = torch.empty(capacity, 4, dtype=torch.int32, device="cuda")
         return Q4Segment(rows, pos, torch.zeros(capacity, device="cuda") if weight else None, 0, t_shift)
 

@@ -96,7 +96,7 @@ struct RowsArgs {
 
 template <int D, bool F32>
 __global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_rope_dev rope) {
-    constexpr int LANES = D / 8, NG = D / Q4_GROUP, REC = q4_record(D);
+    constexpr int LANES = D / 8, NG = D / Q4_GROUP;
     pc_grid_dep_launch();
     const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
     const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_r
         }
     }
     if (bad_pos) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
-    char *row = A.q4 + ((size_t)token * A.n_kv + h0) * (2 * REC);
+    char *row = A.q4 + (size_t)token * A.n_kv * (D + D / 4);
+    char *kc_at = row + h0 * (D / 2), *vc_at = kc_at + A.n_kv * (D / 2), *sl_at = row + A.n_kv * D + h0 * (D / 4);
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
         float x[8];
@@ -142,15 +143,10 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_r
         // pair, the odd one's the latter
         const uint32_t other = __shfl_xor_sync(0xffffffffu, (g & 1) ? vc & 0xFFFFu : vc >> 16, 4);
         if (h < heads) {
-            char *k = row + h * (2 * REC), *v = k + REC;
-            reinterpret_cast<uint32_t *>(k)[t * NG + g] = kc;
-            reinterpret_cast<uint32_t *>(v)[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)] =
+            reinterpret_cast<uint32_t *>(kc_at + h * (D / 2))[t * NG + g] = kc;
+            reinterpret_cast<uint32_t *>(vc_at + h * (D / 2))[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)] =
                 (g & 1) ? other | (vc & 0xFFFF0000u) : (vc & 0xFFFFu) | (other << 16);
-            __half *sk = reinterpret_cast<__half *>(k + D / 2), *sv = reinterpret_cast<__half *>(v + D / 2);
-            if (t == 0) sk[g] = ks;
-            if (t == 1) sk[NG + g] = kl;
-            if (t == 2) sv[g] = vs;
-            if (t == 3) sv[NG + g] = vl;
+            reinterpret_cast<__half *>(sl_at + h * (D / 4))[t * NG + g] = t == 0 ? ks : (t == 1 ? kl : (t == 2 ? vs : vl));
         }
     }
     if (bad) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_RANGE);
@@ -159,7 +155,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_r
 // FROM_POS: keys turned back from (t + t_shift, h, w) to how they came in; else from t_shift alone (they stay rotated at their positions)
 template <int D, bool F32, bool FROM_POS>
 __global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_rope_dev rope) {
-    constexpr int LANES = D / 8, NG = D / Q4_GROUP, REC = q4_record(D);
+    constexpr int LANES = D / 8, NG = D / Q4_GROUP;
     pc_grid_dep_launch();
     const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
     const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
@@ -167,18 +163,18 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_ro
     const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
     const int g = u >> 2, t = u & 3;
     pc_grid_dep_wait();
-    const char *row = A.q4 + ((size_t)token * A.n_kv + h0) * (2 * REC);
+    const char *row = A.q4 + (size_t)token * A.n_kv * (D + D / 4);
+    const char *kc_at = row + h0 * (D / 2), *vc_at = kc_at + A.n_kv * (D / 2), *sl_at = row + A.n_kv * D + h0 * (D / 4);
     uint32_t kc[HEADS], vc[HEADS], kq[HEADS], vq[HEADS];       // codes; step and low of the thread's group
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
         kc[h] = vc[h] = kq[h] = vq[h] = 0;
         if (h < heads) {
-            const char *k = row + h * (2 * REC), *v = k + REC;
-            const uint16_t *sk = reinterpret_cast<const uint16_t *>(k + D / 2), *sv = reinterpret_cast<const uint16_t *>(v + D / 2);
-            kc[h] = reinterpret_cast<const uint32_t *>(k)[t * NG + g];
-            vc[h] = reinterpret_cast<const uint32_t *>(v)[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)];
-            kq[h] = sk[g] | (uint32_t)sk[NG + g] << 16;
-            vq[h] = sv[g] | (uint32_t)sv[NG + g] << 16;
+            const uint16_t *sl = reinterpret_cast<const uint16_t *>(sl_at + h * (D / 4));
+            kc[h] = reinterpret_cast<const uint32_t *>(kc_at + h * (D / 2))[t * NG + g];
+            vc[h] = reinterpret_cast<const uint32_t *>(vc_at + h * (D / 2))[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)];
+            kq[h] = sl[g] | (uint32_t)sl[NG + g] << 16;
+            vq[h] = sl[2 * NG + g] | (uint32_t)sl[3 * NG + g] << 16;
         }
     }
     float2 cs[4] = {};

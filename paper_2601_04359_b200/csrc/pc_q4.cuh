@@ -8,8 +8,8 @@ constexpr int Q4_GROUP = 32;                       // channels that share a step
 constexpr int Q4_STEP = 16;                        // keys that a warp of the attention kernel takes at a time
 constexpr float Q4_MAX = 65504.f;                  // largest value of half precision
 
-__host__ __device__ constexpr int q4_record(int d) { return d / 2 + d / 8; }       // bytes of a key or a value
-inline size_t q4_row(const pc_layer_desc &D) { return (size_t)D.n_kv_heads * 2 * q4_record(D.head_dim); }
+// A token's row: key codes [Hkv][d / 2], value codes [Hkv][d / 2], then per head the steps and lows of its key and of its value (d / 4 bytes)
+inline size_t q4_row(const pc_layer_desc &D) { return (size_t)D.n_kv_heads * (D.head_dim + D.head_dim / 4); }
 
 inline pc_status q4_check_segment(const pc_q4_segment *s, bool allow_empty) {
     if (!s) return PC_ERR_INVALID_ARG;

@@ -9,13 +9,14 @@
 //
 // Shape.  m16n8k16 instructions with 16 keys (channels, for the values) as rows and 8 query rows of one KV head as columns: a warp
 // takes one KV head and 8 query rows and goes through the keys 16 at a time; the warps of a CTA cover the KV heads (and several
-// blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  Rows come by one bulk copy per token into a ring of
-// tiles that the warps fill in turn; a pad between rows in shared memory keeps the lanes' reads on different banks.  CTAs split
-// the keys evenly; k_q4_join merges their parts, k_q4_weigh turns the logits that the history left into weights.
+// blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  TMA brings them, boxes of 16 tokens x 128 bytes with the 128-byte
+// swizzle, into a ring of tiles that the warps refill in turn.  CTAs split the keys evenly; k_q4_join merges their parts, k_q4_weigh
+// turns the logits that the history left into weights.
 #include <algorithm>
 #include <new>
 
 #include "pc_q4.cuh"
+#include "pc_tc.cuh"
 
 struct pc_q4 {
     pc_ctx *ctx;
@@ -33,22 +34,27 @@ namespace {
 constexpr int ROWS = 8;                // query rows of a warp
 constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
 constexpr int MAX_STAGES = 8;
-constexpr int RING_AT = 256;           // barriers and flags before it
-constexpr int RING_BYTES = 210 * 1024;
+constexpr int BOX = 128, BOX_BYTES = Q4_STEP * BOX;        // a box of the rows: 16 tokens x 128 bytes
+constexpr int BAR_BYTES = 256;         // barriers and flags
+constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
 constexpr float P_SCALE = 4.f;         // probabilities times steps stay below fp16's largest: 4 * 2 * 65504 / 15
 
+// Queries as the B operand in shared memory, of a task (KV head, block of 8 rows): words [hi and lo parts 8 NG][sums 2] of 32 lanes, then 8 factors
+constexpr int query_words(int d) { return 8 * (d / Q4_GROUP) + 2; }
+constexpr int query_bytes(int d) { return query_words(d) * 128 + ROWS * 4; }
+
 struct Q4Params {
-    const char *rows[2];               // anchors, history
-    int n[2], shift[2];
+    int n[2], shift[2];                // tokens of anchors, history; what their keys are shifted by
     const uint8_t *valid;              // of the history, or NULL
     const void *q;
     const int32_t *q_pos;
     int n_q, n_q_heads, n_kv, group, n_rows;      // n_rows = n_q * group: query rows of a KV head
-    int row_bytes;                     // of a token
     int heads, blocks, subs;           // of a CTA: KV heads, blocks of 8 query rows, parts of the keys
     int block_groups;                  // CTAs that share a set of heads
     int steps0, steps;                 // steps of 16 keys: the anchors', all
-    int stages, stride, stage_bytes;   // ring of tiles of `subs` steps; bytes from row to row
+    int boxes_k, boxes;                // boxes of a step: of the key codes (as many for the values), all
+    int step_bytes, stages;            // of the ring; a stage holds `subs` steps
+    int ring_at, queries_at;           // places in shared memory
     float *part_o, *part_ml;           // [split][KV head * n_rows + row]
     float *logits;                     // [history token][n_kv * n_rows] or NULL
     float scale;                       // log2(e) / sqrt(d)
@@ -72,12 +78,12 @@ template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N
     else w[0] = lds32(a);
 }
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {         // an 8 x 8 matrix of 16-bit values, two a lane
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -91,117 +97,108 @@ __device__ __forceinline__ uint32_t mul_half(uint32_t a, uint32_t b) {
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// Key of a step that is row i (0 .. 7) of the instruction's upper half.  With rows of shared memory 32 bytes past a multiple of 128 apart, lanes that are
-// served together read different banks: key codes (16 bytes a lane, rows i and i + 1 of an even i together) and value codes (8 bytes
-// a lane, four even or four odd rows together).
-__device__ __forceinline__ int key_of_row(int i) { return (0x57463120u >> (4 * i)) & 7; }
+// Key of a step that is row i (0 .. 7) of the instruction's upper half.  The swizzle moves the 16-byte units of a token's 128 bytes by
+// exclusive-or with the token's number; lanes that are served together then read different banks: key codes (16 bytes a lane, rows i and
+// i + 1 of an even i together: tokens that differ in bit 2) and value codes (8 bytes a lane, four even or four odd rows together: tokens that
+// differ in bits 1 and 2).
+__device__ __forceinline__ int key_of_row(int i) { return (0x36147250u >> (4 * i)) & 7; }
 
-template <int D> struct Queries {      // the B operand of Q K^T: column = query row lane / 4
-    static constexpr int NG = D / Q4_GROUP;
-    uint32_t hi[2 * NG][2], lo[2 * NG][2];
-    uint32_t sum0, sum1;               // sums over the channel groups, in fp16 parts
-    float f0, f1;                      // what the sums of columns 2 (lane % 4) and + 1 are to be multiplied by
-};
+// Byte `b` of a section (its first box at `box0`) of token `key` (0 .. 7) in a step
+__device__ __forceinline__ uint32_t place(int box0, int b, int key) {
+    return (uint32_t)((box0 + (b >> 7)) * BOX_BYTES + key * BOX + ((((b >> 4) & 7) ^ key) << 4) + (b & 15));
+}
 
-// Query rows of a block, rotated at (t + shift, h, w), times log2(e) / sqrt(d): channels 32 g + 8 (lane % 4) .. + 7 of row lane / 4
+// The queries of a CTA's tasks, rotated at (t + shift, h, w), times log2(e) / sqrt(d), as the B operand of Q K^T in shared memory: a warp per row, D / 32
+// consecutive channels a lane.  Called by all threads; rows that there are none of are zero.
 template <int D, bool F32>
-__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, int kv_head, int block, int shift, Queries<D> &Q) {
-    constexpr int NG = D / Q4_GROUP;
-    const int lane = threadIdx.x & 31, t = lane & 3, r = block * ROWS + (lane >> 2);
-    float x[NG][8];
-    float most = 0.f;
-    if (r < P.n_rows) {
-        const int i = r / P.group, head = kv_head * P.group + r % P.group;
-        const size_t at = ((size_t)i * P.n_q_heads + head) * D + 8 * t;
-        const int4 p = __ldg(reinterpret_cast<const int4 *>(P.q_pos) + i);
+__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int first_head, int n_heads, int first_block, int shift) {
+    constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D), BYTES = query_bytes(D);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+    const int row0 = first_block * ROWS, count = min(P.n_rows - row0, P.blocks * ROWS);
+    __syncthreads();                               // the queries of the segment before are in registers
+    for (int i = threadIdx.x; i < P.heads * P.blocks * (BYTES / 16); i += blockDim.x) reinterpret_cast<uint4 *>(to)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    // channel 32 g + 8 t + k of a row: 16-bit half k / 4 of word (2 g + k % 2) * 2 + (k / 2) % 2 of lane 4 row + t.  The code words give
+    // channels (k, k + 4) as one register: k even in the low four bits of their bytes, k odd in the high four, 2^4 larger
+    const int g = lane * CH / Q4_GROUP, t = lane * CH % Q4_GROUP / 8, k0 = lane * CH % 8;
+    for (int i = warp; i < n_heads * count; i += n_warps) {
+        const int h = i / count, r = i % count, task = r / ROWS * P.heads + h, col = r % ROWS;
+        const int query = (row0 + r) / P.group, head = (first_head + h) * P.group + (row0 + r) % P.group;
+        const size_t at = ((size_t)query * P.n_q_heads + head) * D + lane * CH;
+        const int4 p = __ldg(reinterpret_cast<const int4 *>(P.q_pos) + query);
+        float x[CH];
+        if constexpr (F32) {
+#pragma unroll
+            for (int c = 0; c < CH; c += 2) {
+                const float2 v = __ldg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + at + c));
+                x[c] = v.x;
+                x[c + 1] = v.y;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; c += 2) {
+                const uint32_t v = __ldg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + at + c));
+                x[c] = pc_bf16_lo(v);
+                x[c + 1] = pc_bf16_hi(v);
+            }
+        }
         bool bad = false;
+        float most = 0.f, total = 0.f;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            if constexpr (F32) {
-                const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(P.q) + at + g * Q4_GROUP);
-                const float4 a = __ldg(q), b = __ldg(q + 1);
-                x[g][0] = a.x; x[g][1] = a.y; x[g][2] = a.z; x[g][3] = a.w;
-                x[g][4] = b.x; x[g][5] = b.y; x[g][6] = b.z; x[g][7] = b.w;
-            } else {
-                const uint4 a = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(P.q) + at + g * Q4_GROUP));
-                const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) { x[g][2 * k] = pc_bf16_lo(w[k]); x[g][2 * k + 1] = pc_bf16_hi(w[k]); }
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 cs = pc_rope_cs_clamped(rope, 16 * g + 4 * t + k, p.x + shift, p.y, p.z, bad);
-                const float2 y = pc_rotate(x[g][2 * k], x[g][2 * k + 1], cs);
-                x[g][2 * k] = y.x * P.scale;
-                x[g][2 * k + 1] = y.y * P.scale;
-                most = fmaxf(most, fmaxf(fabsf(x[g][2 * k]), fabsf(x[g][2 * k + 1])));
-            }
+        for (int c = 0; c < CH; c += 2) {
+            const float2 y = pc_rotate(x[c], x[c + 1], pc_rope_cs_clamped(rope, (lane * CH + c) / 2, p.x + shift, p.y, p.z, bad));
+            x[c] = y.x * P.scale;
+            x[c + 1] = y.y * P.scale;
+            most = fmaxf(most, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
         }
         if (bad) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
-    } else {
+        // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
+        most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+        const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
+        const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+        char *mine = to + task * BYTES;
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[g][k] = 0.f;
-    }
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
-    const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
-    const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-    float total[NG];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-        total[g] = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            x[g][k] *= up;
-            total[g] += x[g][k];
+        for (int c = 0; c < CH; ++c) {
+            const int k = k0 + c;
+            x[c] *= up;
+            total += x[c];
+            const float y = (c & 1) ? x[c] * 0.0625f : x[c];         // k0 is even
+            const __half hi = __float2half_rn(y);
+            const int word = (2 * g + (k & 1)) * 2 + ((k >> 1) & 1);
+            __half *at16 = reinterpret_cast<__half *>(mine + (word * 32 + col * 4 + t) * 4) + (k >> 2);
+            at16[0] = hi;
+            at16[4 * NG * 64] = __float2half_rn(y - __half2float(hi));
         }
-        total[g] += __shfl_xor_sync(0xffffffffu, total[g], 1);
-        total[g] += __shfl_xor_sync(0xffffffffu, total[g], 2);
-        // channels of the code words' 16-bit halves: (0, 4) (2, 6) in bits 0-3 and 8-11, (1, 5) (3, 7) in bits 4-7 and 12-15, 2^4 larger
+        // sums over the groups against the lows: index 2 t, 2 t + 1 of the instruction = groups, a further fp16 part every NG indices
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const float m = s ? 0.0625f : 1.f, y0 = x[g][s + 2 * b] * m, y1 = x[g][s + 2 * b + 4] * m;
-                const uint32_t h = pack_half(y0, y1);
-                const float2 back = halves(h);
-                Q.hi[2 * g + s][b] = h;
-                Q.lo[2 * g + s][b] = pack_half(y0 - back.x, y1 - back.y);
+        for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (lane % (Q4_GROUP / CH) == 0) {
+            char *sums = mine + 8 * NG * 128;
+            for (int part = 0; part < 3; ++part) {
+                const __half v = __float2half_rn(total);
+                const int index = part * NG + g;                     // 0 .. 15
+                reinterpret_cast<__half *>(sums + ((index / 8) * 32 + col * 4 + index % 8 / 2) * 4)[index & 1] = v;
+                total -= __half2float(v);
             }
+        }
+        if (lane == 0) reinterpret_cast<float *>(mine + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
     }
-    // sums of the groups against the lows: k index (2 t, 2 t + 1) of the instruction = groups, a further fp16 part every NG indices
-    const auto part = [](float v, int n) {
-        float h = __half2float(__float2half_rn(v));
-        for (int i = 0; i < n; ++i) { v -= h; h = __half2float(__float2half_rn(v)); }
-        return h;
-    };
-    if constexpr (NG == 4) {
-        const float a = (t & 1) ? total[2] : total[0], b = (t & 1) ? total[3] : total[1];
-        Q.sum0 = pack_half(part(a, t >> 1), part(b, t >> 1));
-        Q.sum1 = t < 2 ? pack_half(part(a, 2), part(b, 2)) : 0u;
-    } else {
-        Q.sum0 = t < 3 ? pack_half(part(total[0], t), part(total[1], t)) : 0u;
-        Q.sum1 = 0u;
-    }
-    const float f = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
-    Q.f0 = __shfl_sync(0xffffffffu, f, t * 8);
-    Q.f1 = __shfl_sync(0xffffffffu, f, t * 8 + 4);
+    __syncthreads();
 }
 
 template <int D, bool F32>
-__global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_constant__ Q4Params P, const pc_rope_dev rope) {
-    constexpr int NG = D / Q4_GROUP, REC = q4_record(D);
-    extern __shared__ __align__(128) char smem[];
+__global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_constant__ CUtensorMap map0, const __grid_constant__ CUtensorMap map1,
+                                                                  const __grid_constant__ Q4Params P, const pc_rope_dev rope) {
+    constexpr int NG = D / Q4_GROUP;
+    extern __shared__ char smem_raw[];
     pc_grid_dep_launch();
-    const uint32_t base = pc_smem_u32(smem), ring = base + RING_AT;
+    const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + P.ring_at;
+    char *smem = smem_raw + (base - pc_smem_u32(smem_raw));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 16 * MAX_STAGES);
     const auto full = [&](int s) { return base + 8 * s; };
     const auto empty = [&](int s) { return base + 8 * (MAX_STAGES + s); };
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n_warps = P.heads * P.blocks * P.subs;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int tasks = P.heads * P.blocks, n_warps = tasks * P.subs;
     if (threadIdx.x == 0) {
         for (int s = 0; s < P.stages; ++s) {
             pc_mbar_init(full(s), 1);
@@ -209,50 +206,62 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    const int first_head = blockIdx.y / P.block_groups * P.heads, n_heads = min(P.heads, P.n_kv - first_head);
-    const int s_begin = (int)((long long)P.steps * blockIdx.x / gridDim.x), s_end = (int)((long long)P.steps * (blockIdx.x + 1) / gridDim.x);
-    const int n_tiles = (s_end - s_begin + P.subs - 1) / P.subs;
-    // a step's segment, first token and tokens
-    const auto step_at = [&](int s, int &seg, int &first) {
-        seg = s >= P.steps0;
-        first = (seg ? s - P.steps0 : s) * Q4_STEP;
-        return min(Q4_STEP, P.n[seg] - first);
-    };
+    const int set = blockIdx.y / P.block_groups, first_block = (blockIdx.y - set * P.block_groups) * P.blocks;
+    const int first_head = set * P.heads, n_heads = min(P.heads, P.n_kv - first_head);
+    // This CTA's steps of the two segments; a tile is `subs` steps of one segment
+    const int s0 = (int)((long long)P.steps * blockIdx.x / gridDim.x), s1 = (int)((long long)P.steps * (blockIdx.x + 1) / gridDim.x);
+    const int begin0 = min(s0, P.steps0), end0 = min(s1, P.steps0), begin1 = max(s0 - P.steps0, 0), end1 = max(s1 - P.steps0, 0);
+    const int tiles0 = (end0 - begin0 + P.subs - 1) / P.subs, n_tiles = tiles0 + (end1 - begin1 + P.subs - 1) / P.subs;
     pc_grid_dep_wait();
 
-    // A tile's rows into its stage, a bulk copy per token, by one warp
-    const uint32_t bytes = (uint32_t)n_heads * 2 * REC;
-    const size_t head_at = (size_t)first_head * 2 * REC;
-    const auto fetch = [&](int tile) {
-        const int st = tile % P.stages, s0 = s_begin + tile * P.subs, steps = min(P.subs, s_end - s0);
-        int tokens = 0;
-        for (int i = 0; i < steps; ++i) {
-            int seg, first;
-            tokens += step_at(s0 + i, seg, first);
-        }
-        if (lane == 0) pc_mbar_expect_tx(full(st), bytes * tokens);
+    // A tile into stage st, by one warp: boxes of the key codes, of the value codes, of the steps and lows
+    const auto fetch = [&](int tile, int st) {
+        const bool hist = tile >= tiles0;
+        const int first = hist ? begin1 + (tile - tiles0) * P.subs : begin0 + tile * P.subs;
+        const int n = min(P.subs, (hist ? end1 : end0) - first) * P.boxes;
+        const CUtensorMap *map = hist ? &map1 : &map0;
+        const uint32_t dst = ring + st * P.subs * P.step_bytes;
+        if (lane == 0) pc_mbar_expect_tx(full(st), n * BOX_BYTES);
         __syncwarp();
-        for (int i = lane; i < steps * Q4_STEP; i += 32) {
-            int seg, first;
-            const int n = step_at(s0 + i / Q4_STEP, seg, first), k = i % Q4_STEP;
-            if (k < n) pc_bulk_g2s(ring + st * P.stage_bytes + i * P.stride, P.rows[seg] + (size_t)(first + k) * P.row_bytes + head_at, bytes, full(st));
+        for (int i = lane; i < n; i += 32) {
+            const int step = i / P.boxes, box = i - step * P.boxes;
+            const int in_v = box - P.boxes_k, in_s = in_v - P.boxes_k;
+            const int x = in_v < 0 ? first_head * (D / 2) + box * BOX
+                                   : (in_s < 0 ? (P.n_kv + first_head) * (D / 2) + in_v * BOX : P.n_kv * D + first_head * (D / 4) + in_s * BOX);
+            pc_tc::tma_load_2d(dst + i * BOX_BYTES, map, x, (first + step) * Q4_STEP, full(st));
         }
     };
-    // The warps take turns at refilling: before tile i one of them fetches the tile that follows in the stage of tile i - 1
-    const auto ready = [&](int tile) {
-        if (tile > 0 && warp == tile % n_warps && tile - 1 + P.stages < n_tiles) {
-            const int st = (tile - 1) % P.stages;
-            if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(st), ((tile - 1) / P.stages) & 1, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) return false;
-            fetch(tile - 1 + P.stages);
+    // Where the warp is in the ring, and whose turn it is to refill: before a tile one of the warps fetches the tile that follows in
+    // the stage of the tile before it
+    int st = 0, at = 0, turn = 0;
+    uint32_t phase = 0;
+    const auto ready = [&]() {
+        if (at > 0 && at - 1 + P.stages < n_tiles) {
+            if (warp == turn) {
+                const int before = st == 0 ? P.stages - 1 : st - 1;
+                if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(before), st == 0 ? phase ^ 1u : phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) return false;
+                fetch(at - 1 + P.stages, before);
+            }
+            if (++turn == n_warps) turn = 0;
         }
-        return __all_sync(0xffffffffu, pc_mbar_wait(full(tile % P.stages), (tile / P.stages) & 1, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us)) != 0;
+        return __all_sync(0xffffffffu, pc_mbar_wait(full(st), phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us)) != 0;
     };
-    for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile);
+    const auto done = [&]() {
+        __syncwarp();
+        if (lane == 0) pc_mbar_arrive(empty(st));
+        ++at;
+        if (++st == P.stages) {
+            st = 0;
+            phase ^= 1u;
+        }
+    };
+    for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile, tile);
 
-    const int task = warp % (P.heads * P.blocks), sub = warp / (P.heads * P.blocks);
-    const int head = task % P.heads, block = (blockIdx.y % P.block_groups) * P.blocks + task / P.heads;
+    const int task = warp % tasks, sub = warp / tasks, head = task % P.heads, block = first_block + task / P.heads;
+    const bool works = head < n_heads && block * ROWS < P.n_rows;      // else the ring still goes round
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group `row`
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
@@ -262,80 +271,110 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         for (int j = 0; j < 4; ++j) O[i][j] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) L[j] = 0.f;
-    if (head < n_heads && block * ROWS < P.n_rows) {
-        Queries<D> Q;
-        int have = -1;                 // segment that Q is rotated for
-        const int k0 = key_of_row(row), va = key_of_row(2 * t), vb = key_of_row(2 * t + 1);
-        const int R = P.n_kv * P.n_rows;
-        const int r0 = block * ROWS + 2 * t;
-        for (int tile = 0; tile < n_tiles; ++tile) {
-            const int st = tile % P.stages;
-            const int s = s_begin + tile * P.subs + sub;
-            int seg = 0, first = 0, n = 0;
-            bool ok0 = false, ok1 = false;
-            if (s < s_end) {
-                n = step_at(s, seg, first);
-                ok0 = k0 < n;
-                ok1 = k0 + 8 < n;
-                if (seg == 1 && P.valid) {
-                    if (ok0) ok0 = __ldg(P.valid + first + k0) != 0;
-                    if (ok1) ok1 = __ldg(P.valid + first + k0 + 8) != 0;
-                }
-                if (seg != have) {
-                    take_queries<D, F32>(P, rope, first_head + head, block, P.shift[seg], Q);
-                    have = seg;
-                }
+    // places of the lane's keys in a step: codes, steps and lows of its two keys, and of the four whose values it takes (rows 2 t, 2 t + 1
+    // of the instruction; the second half lies 8 tokens on)
+    const int k0 = key_of_row(row), kva = key_of_row(2 * t), kvb = key_of_row(2 * t + 1);
+    constexpr uint32_t EIGHT = 8 * BOX;
+    const int box_s = 2 * P.boxes_k;
+    const uint32_t at_k = place(0, head * (D / 2) + t * NG * 4, k0), at_ks = place(box_s, head * (D / 4), k0);
+    const uint32_t at_va = place(P.boxes_k, head * (D / 2) + row * NG * 2, kva), at_vb = place(P.boxes_k, head * (D / 2) + row * NG * 2, kvb);
+    const uint32_t at_vsa = place(box_s, head * (D / 4) + 4 * NG, kva), at_vsb = place(box_s, head * (D / 4) + 4 * NG, kvb);
+    const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;
+    bool alive = true;
+#pragma unroll 1
+    for (int seg = 0; seg < 2; ++seg) {
+        const int seg_begin = seg ? begin1 : begin0, seg_end = seg ? end1 : end0;
+        if (seg_begin == seg_end) continue;
+        char *queries = smem + P.queries_at;
+        take_queries<D, F32>(P, rope, queries, first_head, n_heads, first_block, seg ? P.shift[1] : P.shift[0]);
+        uint32_t q_hi[2 * NG][2], q_lo[2 * NG][2], q_sum[2];
+        const uint32_t my_q = pc_smem_u32(queries) + task * query_bytes(D) + lane * 4;
+#pragma unroll
+        for (int i = 0; i < 4 * NG; ++i) {
+            q_hi[i / 2][i & 1] = lds32(my_q + i * 128);
+            q_lo[i / 2][i & 1] = lds32(my_q + (4 * NG + i) * 128);
+        }
+        q_sum[0] = lds32(my_q + 8 * NG * 128);
+        q_sum[1] = lds32(my_q + (8 * NG + 1) * 128);
+        const float *factor = reinterpret_cast<const float *>(queries + task * query_bytes(D) + query_words(D) * 128);
+        const float f0 = factor[2 * t], f1 = factor[2 * t + 1];
+        const uint8_t *valid = seg == 1 ? P.valid : nullptr;
+        float *logits = seg == 1 ? P.logits : nullptr;
+        if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
+        const int n_seg = seg ? P.n[1] : P.n[0];
+#pragma unroll 1
+        for (int s = seg_begin + sub; alive && s - sub < seg_end; s += P.subs) {
+            if (!ready()) {
+                alive = false;
+                break;
             }
-            if (!ready(tile)) break;
-            if (s < s_end) {
-                const uint32_t rows = ring + st * P.stage_bytes + sub * Q4_STEP * P.stride + head * 2 * REC;
-                const uint32_t ka = rows + k0 * P.stride, kb = ka + 8 * P.stride;
-                const uint32_t b0 = __ballot_sync(0xffffffffu, ok0), b1 = __ballot_sync(0xffffffffu, ok1);
+            if (works && s < seg_end) {
+                const uint32_t rows = ring + (st * P.subs + sub) * P.step_bytes;
+                const int first = s * Q4_STEP, n = n_seg - first;
+                bool ok0 = true, ok1 = true;
+                uint32_t b0 = 0xffffffffu, b1 = 0xffffffffu;
+                if (n < Q4_STEP || valid) {
+                    ok0 = k0 < n;
+                    ok1 = k0 + 8 < n;
+                    if (valid) {
+                        if (ok0) ok0 = __ldg(valid + first + k0) != 0;
+                        if (ok1) ok1 = __ldg(valid + first + k0 + 8) != 0;
+                    }
+                    b0 = __ballot_sync(0xffffffffu, ok0);
+                    b1 = __ballot_sync(0xffffffffu, ok1);
+                }
                 // ---- logits
+                const uint32_t ka = rows + at_k, kb = ka + EIGHT, ks = rows + at_ks;
                 uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2];
-                lds(ka + t * NG * 4, wa);
-                lds(kb + t * NG * 4, wb);
-                lds(ka + D / 2, sa);
-                lds(kb + D / 2, sb);
-                float S[4] = {0.f, 0.f, 0.f, 0.f};
+                lds(ka, wa);
+                lds(kb, wb);
+                lds(ks, sa);
+                lds(ks + EIGHT, sb);
+                float S[4] = {0.f, 0.f, 0.f, 0.f}, C[NG][4];
                 {
-                    const uint32_t off = D / 2 + 2 * NG + (NG == 4 ? (t & 1) * 4 : 0);
-                    const uint32_t la = lds32(ka + off), lb = lds32(kb + off);
-                    mma(S, la, lb, la, lb, Q.sum0, Q.sum1);
+                    const uint32_t off = 2 * NG + (NG == 4 ? (t & 1) * 4 : 0);
+                    const uint32_t la = lds32(ks + off), lb = lds32(ks + EIGHT + off);
+                    mma(S, la, lb, la, lb, q_sum[0], q_sum[1]);
+                }
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) C[g][j] = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {        // channels in the low four bits of the code words' bytes, then in the high four
+                    const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+                        mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+                        mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_hi[2 * g + h][0], q_hi[2 * g + h][1]);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) S[j] *= 1.f / 16777216.f;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    float C[4] = {0.f, 0.f, 0.f, 0.f};
-                    const uint32_t xa = wa[g] >> 8, xb = wb[g] >> 8;
-                    const uint32_t a0 = wa[g] & 0x000F000Fu, a1 = wb[g] & 0x000F000Fu, a2 = xa & 0x000F000Fu, a3 = xb & 0x000F000Fu;
-                    const uint32_t c0 = wa[g] & 0x00F000F0u, c1 = wb[g] & 0x00F000F0u, c2 = xa & 0x00F000F0u, c3 = xb & 0x00F000F0u;
-                    mma(C, a0, a1, a2, a3, Q.lo[2 * g][0], Q.lo[2 * g][1]);
-                    mma(C, c0, c1, c2, c3, Q.lo[2 * g + 1][0], Q.lo[2 * g + 1][1]);
-                    mma(C, a0, a1, a2, a3, Q.hi[2 * g][0], Q.hi[2 * g][1]);
-                    mma(C, c0, c1, c2, c3, Q.hi[2 * g + 1][0], Q.hi[2 * g + 1][1]);
                     const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
                     const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
-                    S[0] = fmaf(fa, C[0], S[0]);
-                    S[1] = fmaf(fa, C[1], S[1]);
-                    S[2] = fmaf(fb, C[2], S[2]);
-                    S[3] = fmaf(fb, C[3], S[3]);
+                    S[0] = fmaf(fa, C[g][0], S[0]);
+                    S[1] = fmaf(fa, C[g][1], S[1]);
+                    S[2] = fmaf(fb, C[g][2], S[2]);
+                    S[3] = fmaf(fb, C[g][3], S[3]);
                 }
-                S[0] = ok0 ? S[0] * Q.f0 : -INFINITY;
-                S[1] = ok0 ? S[1] * Q.f1 : -INFINITY;
-                S[2] = ok1 ? S[2] * Q.f0 : -INFINITY;
-                S[3] = ok1 ? S[3] * Q.f1 : -INFINITY;
-                if (P.logits && seg == 1) {
-                    float *at = P.logits + (size_t)(first + k0) * R + (size_t)(first_head + head) * P.n_rows + r0;
+                S[0] = ok0 ? S[0] * f0 : -INFINITY;
+                S[1] = ok0 ? S[1] * f1 : -INFINITY;
+                S[2] = ok1 ? S[2] * f0 : -INFINITY;
+                S[3] = ok1 ? S[3] * f1 : -INFINITY;
+                if (logits) {
+                    float *to = logits + (size_t)(first + k0) * R;
                     if (k0 < n) {
-                        if (r0 < P.n_rows) at[0] = S[0];
-                        if (r0 + 1 < P.n_rows) at[1] = S[1];
+                        if (r0 < P.n_rows) to[0] = S[0];
+                        if (r0 + 1 < P.n_rows) to[1] = S[1];
                     }
                     if (k0 + 8 < n) {
-                        at += (size_t)8 * R;
-                        if (r0 < P.n_rows) at[0] = S[2];
-                        if (r0 + 1 < P.n_rows) at[1] = S[3];
+                        to += (size_t)8 * R;
+                        if (r0 < P.n_rows) to[0] = S[2];
+                        if (r0 + 1 < P.n_rows) to[1] = S[3];
                     }
                 }
                 // ---- softmax: maximum of the 16 keys of each column
@@ -363,12 +402,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 l1 += p1 + p3;
                 // ---- values: keys of rows 2 t, 2 t + 1 (and + 8) of the instruction
                 uint32_t u[4], steps[4][NG / 2], codes[4][NG / 2];
-                const uint32_t vrow[4] = {rows + REC + va * P.stride, rows + REC + vb * P.stride, rows + REC + (va + 8) * P.stride, rows + REC + (vb + 8) * P.stride};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    lds(vrow[j] + row * NG * 2, codes[j]);
-                    lds(vrow[j] + D / 2, steps[j]);
-                    u[j] = row < NG ? lds16(vrow[j] + D / 2 + 2 * NG + 2 * row) : 0u;
+                    const uint32_t sl = rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT;
+                    lds(rows + (j & 1 ? at_vb : at_va) + (j >> 1) * EIGHT, codes[j]);
+                    lds(sl, steps[j]);
+                    u[j] = row < NG ? lds16(sl + 2 * NG + 2 * row) : 0u;
                 }
                 if ((b0 & b1) != 0xffffffffu) {      // what lies in the place of a masked key may be anything
 #pragma unroll
@@ -418,12 +457,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                     }
                 }
             }
-            __syncwarp();
-            if (lane == 0) pc_mbar_arrive(empty(st));
+            done();
         }
-    } else {                           // no head or no rows for this warp: the ring still goes round
-        for (int tile = 0; tile < n_tiles && ready(tile); ++tile)
-            if (lane == 0) pc_mbar_arrive(empty(tile % P.stages));
     }
     __syncthreads();
     if (*abort_flag) {
@@ -433,7 +468,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
 
     // ---- the parts of the keys that the CTA's warps took, merged in shared memory (the ring is done with)
     constexpr int PITCH = D + 4;
-    float *parts = reinterpret_cast<float *>(smem + RING_AT);        // [warp][8][PITCH], then [warp][8] maxima, sums
+    float *parts = reinterpret_cast<float *>(smem + P.ring_at);      // [warp][8][PITCH], then [warp][8] maxima, sums
     float *ms = parts + n_warps * ROWS * PITCH, *ls = ms + n_warps * ROWS;
     {
 #pragma unroll
@@ -459,11 +494,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         }
     }
     __syncthreads();
-    const int tasks = P.heads * P.blocks, rows_all = P.n_kv * P.n_rows;
-    for (int e = threadIdx.x; e < tasks * ROWS * (D / 4); e += blockDim.x) {
-        const int c = e % (D / 4), r = e / (D / 4) % ROWS, k = e / (D / 4) / ROWS;
-        const int h = k % P.heads, in_head = ((blockIdx.y % P.block_groups) * P.blocks + k / P.heads) * ROWS + r;
-        if (h >= n_heads || in_head >= P.n_rows) continue;
+    const int rows_all = P.n_kv * P.n_rows, count = min(P.n_rows - first_block * ROWS, P.blocks * ROWS);
+    for (int e = threadIdx.x; e < n_heads * count * (D / 4); e += blockDim.x) {
+        const int c = e % (D / 4), i = e / (D / 4), h = i / count, in_head = first_block * ROWS + i % count;
+        const int k = i % count / ROWS * P.heads + h, r = i % count % ROWS;
         float M = -INFINITY, l = 0.f;
         for (int b = 0; b < P.subs; ++b) M = fmaxf(M, ms[(b * tasks + k) * ROWS + r]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -483,55 +517,75 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     }
 }
 
-// Parts of a row merged: a block per row, warps take every (JOIN_THREADS / D)-th part
+// Parts of a row merged: a block per row, D / 4 lanes a part.  The parts' sums are fetched before their maxima are compared, eight at a time.
 constexpr int JOIN_THREADS = 512;
 template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_join(const JoinParams J) {
-    constexpr int LANES = D / 4, SETS = JOIN_THREADS / LANES;
+    constexpr int LANES = D / 4, SETS = JOIN_THREADS / LANES, BATCH = 8;
     __shared__ float4 sums[SETS][LANES];
+    __shared__ float2 mls[SETS];
     pc_grid_dep_launch();
     pc_grid_dep_wait();
-    const int row = blockIdx.x, lane = threadIdx.x & 31;
+    const int row = blockIdx.x, c = threadIdx.x % LANES, set = threadIdx.x / LANES;
     const float2 *ml = reinterpret_cast<const float2 *>(J.part_ml) + row;
+    const float4 *po = reinterpret_cast<const float4 *>(J.part_o) + (size_t)row * LANES + c;
     float M = -INFINITY, l = 0.f;
-    for (int s = lane; s < J.splits; s += 32) M = fmaxf(M, ml[(size_t)s * J.rows].x);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    const float z = M == -INFINITY ? 0.f : M;
-    for (int s = lane; s < J.splits; s += 32) {
-        const float2 x = ml[(size_t)s * J.rows];
-        l = fmaf(exp2_fast(x.x - z), x.y, l);
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    const int c = threadIdx.x % LANES, set = threadIdx.x / LANES;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int s = set; s < J.splits; s += SETS) {
-        const float f = exp2_fast(ml[(size_t)s * J.rows].x - z);
-        const float4 x = reinterpret_cast<const float4 *>(J.part_o)[((size_t)s * J.rows + row) * LANES + c];
+    for (int s0 = set; s0 < J.splits; s0 += SETS * BATCH) {
+        float4 x[BATCH];
+        float2 y[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int s = s0 + i * SETS;
+            y[i] = make_float2(-INFINITY, 0.f);
+            x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s < J.splits) {
+                y[i] = __ldg(ml + (size_t)s * J.rows);
+                x[i] = __ldg(po + (size_t)s * J.rows * LANES);
+            }
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) top = fmaxf(top, y[i].x);
+        const float z = top == -INFINITY ? 0.f : top, f0 = exp2_fast(M - z);
+        l *= f0;
+        sum = make_float4(sum.x * f0, sum.y * f0, sum.z * f0, sum.w * f0);
+        M = top;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float f = exp2_fast(y[i].x - z);
+            l = fmaf(f, y[i].y, l);
+            sum.x = fmaf(f, x[i].x, sum.x);
+            sum.y = fmaf(f, x[i].y, sum.y);
+            sum.z = fmaf(f, x[i].z, sum.z);
+            sum.w = fmaf(f, x[i].w, sum.w);
+        }
+    }
+    sums[set][c] = sum;
+    if (c == 0) mls[set] = make_float2(M, l);
+    __syncthreads();
+    const int r = row % J.n_rows, h = row / J.n_rows * J.group + r % J.group;
+    const size_t to = (size_t)(r / J.group) * J.n_q_heads + h;
+    if (threadIdx.x >= LANES) return;
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) M = fmaxf(M, mls[i].x);
+    const float z = M == -INFINITY ? 0.f : M;
+    l = 0.f;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+        const float f = exp2_fast(mls[i].x - z);
+        const float4 x = sums[i][c];
+        l = fmaf(f, mls[i].y, l);
         sum.x = fmaf(f, x.x, sum.x);
         sum.y = fmaf(f, x.y, sum.y);
         sum.z = fmaf(f, x.z, sum.z);
         sum.w = fmaf(f, x.w, sum.w);
     }
-    sums[set][c] = sum;
-    __syncthreads();
-    const int r = row % J.n_rows, h = row / J.n_rows * J.group + r % J.group;
-    const size_t to = (size_t)(r / J.group) * J.n_q_heads + h;
-    if (threadIdx.x < LANES) {
-        for (int i = 1; i < SETS; ++i) {
-            const float4 x = sums[i][c];
-            sum.x += x.x;
-            sum.y += x.y;
-            sum.z += x.z;
-            sum.w += x.w;
-        }
-        const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);      // no key left: 0; NaN stays
-        if constexpr (F32) reinterpret_cast<float4 *>(J.out)[to * LANES + c] = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-        else reinterpret_cast<uint2 *>(J.out)[to * LANES + c] = make_uint2(pc_pack_bf16(sum.x * inv, sum.y * inv), pc_pack_bf16(sum.z * inv, sum.w * inv));
-    }
-    if (threadIdx.x == 0) {
-        const float lse2 = M + log2f(l);             // base 2; -infinity where no key is left
+    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);          // no key left: 0; NaN stays
+    if constexpr (F32) reinterpret_cast<float4 *>(J.out)[to * LANES + c] = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+    else reinterpret_cast<uint2 *>(J.out)[to * LANES + c] = make_uint2(pc_pack_bf16(sum.x * inv, sum.y * inv), pc_pack_bf16(sum.z * inv, sum.w * inv));
+    if (c == 0) {
+        const float lse2 = M + log2f(l);                                // base 2; -infinity where no key is left
         if (J.lse_rows) J.lse_rows[row] = lse2;
         if (J.lse) J.lse[to] = lse2 * 0.6931471805599453f;
     }
@@ -564,18 +618,32 @@ __global__ void __launch_bounds__(256) k_accumulate(const float *__restrict__ ma
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
+// Rows as bytes, boxes of 16 tokens x 128 bytes; what lies outside reads as zero
+bool make_row_map(CUtensorMap *m, const void *rows, uint64_t n, uint64_t row_bytes) {
+    const pc_tc::EncodeTiledFn fn = pc_tc::encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {row_bytes, n}, strides[1] = {row_bytes};
+    const cuuint32_t box[2] = {BOX, Q4_STEP}, estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(rows), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Queries i0 .. i0 + n_q - 1 through the kernels above
 pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, const void *q, const int32_t *q_pos, int n_q, void *out,
                       float *lse, const pc_q4_weigh *weigh, float gain, cudaStream_t stream) {
     pc_ctx *ctx = w->ctx;
     const pc_layer_desc &D = ctx->desc;
-    const int rec2 = 2 * q4_record(D.head_dim);
     Q4Params P{};
     const pc_q4_segment *segs[2] = {&cache->anchors, &cache->history};
+    CUtensorMap maps[2];
     for (int i = 0; i < 2; ++i) {
-        P.rows[i] = static_cast<const char *>(segs[i]->rows);
         P.n[i] = segs[i]->n_tokens;
         P.shift[i] = segs[i]->t_shift;
+        const pc_q4_segment *s = P.n[i] > 0 ? segs[i] : segs[1 - i];          // an empty segment is never asked for
+        if (!make_row_map(&maps[i], s->rows, (uint64_t)s->n_tokens, q4_row(D))) {
+            fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
+            return PC_ERR_CUDA;
+        }
     }
     P.valid = valid;
     P.q = q;
@@ -585,7 +653,6 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
     P.n_rows = n_q * ctx->group;
-    P.row_bytes = (int)q4_row(D);
     // KV heads of a CTA: up to eight, shared out evenly; then as many blocks of query rows as there are warps for; the warps left over
     // take further parts of the keys
     const int head_sets = div_up(P.n_kv, 8);
@@ -596,10 +663,14 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.subs = MAX_WARPS / (P.heads * P.blocks);
     P.steps0 = div_up(P.n[0], Q4_STEP);
     P.steps = P.steps0 + div_up(P.n[1], Q4_STEP);
-    const int piece = P.heads * rec2;
-    P.stride = piece + (32 + 128 - piece % 128) % 128;
-    P.stage_bytes = P.subs * Q4_STEP * P.stride;
-    P.stages = std::min(MAX_STAGES, RING_BYTES / P.stage_bytes);
+    P.boxes_k = div_up(P.heads * D.head_dim / 2, BOX);
+    P.boxes = 2 * P.boxes_k + div_up(P.heads * D.head_dim / 4, BOX);
+    P.step_bytes = P.boxes * BOX_BYTES;
+    const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
+    P.queries_at = BAR_BYTES;
+    P.ring_at = div_up(BAR_BYTES + P.heads * P.blocks * query_bytes(D.head_dim), 1024) * 1024;
+    P.stages = std::min(MAX_STAGES, (SMEM_MOST - 1024 - P.ring_at) / (P.subs * P.step_bytes));
+    const size_t smem = 1024 + P.ring_at + std::max(P.stages * P.subs * P.step_bytes, merge_bytes);
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
@@ -615,9 +686,6 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
         const long long cost = (long long)div_up(ctas * s, ctx->sm_count) * (div_up(div_up(P.steps, s), P.subs) + 2);
         if (best < 0 || cost < best) { best = cost; splits = s; }
     }
-    const int n_warps = P.heads * P.blocks * P.subs;
-    const size_t ring = std::max<size_t>((size_t)P.stages * P.stage_bytes, (size_t)n_warps * ROWS * (D.head_dim + 4 + 2) * sizeof(float));
-    const size_t smem = RING_AT + ring;
     const bool f32 = D.dtype == PC_F32;
     const dim3 grid(splits, ctas), block(n_warps * 32);
     static bool attr_set[PC_MAX_DEVICES] = {};
@@ -627,10 +695,10 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
             PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
         attr_set[ctx->device] = true;
     }
-    if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_attend<128, true>), grid, block, smem, stream, P, ctx->rope);
-    else if (D.head_dim == 128) PC_LAUNCH((k_q4_attend<128, false>), grid, block, smem, stream, P, ctx->rope);
-    else if (f32) PC_LAUNCH((k_q4_attend<64, true>), grid, block, smem, stream, P, ctx->rope);
-    else PC_LAUNCH((k_q4_attend<64, false>), grid, block, smem, stream, P, ctx->rope);
+    if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_attend<128, true>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
+    else if (D.head_dim == 128) PC_LAUNCH((k_q4_attend<128, false>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
+    else if (f32) PC_LAUNCH((k_q4_attend<64, true>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
+    else PC_LAUNCH((k_q4_attend<64, false>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
     JoinParams J{w->part_o, w->part_ml, splits, rows, P.n_rows, P.group, P.n_q_heads, out, lse, P.logits ? w->lse : nullptr};
     if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_join<128, true>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
     else if (D.head_dim == 128) PC_LAUNCH((k_q4_join<128, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);

@@ -36,36 +36,22 @@ def quantise(x):
 
 
 def decode(rows, d):
-    """Rows as they lie in memory, [n][Hkv][2][5 d / 8] bytes -> two (codes, steps, lows), of keys and of values"""
+    """Rows as they lie in memory, [n][Hkv * 5 d / 4] bytes -> two (codes, steps, lows), of keys and of values"""
     rows = np.ascontiguousarray(rows)
-    n, hkv = rows.shape[:2]
-    ng = d // GROUP
+    n = len(rows)
+    hkv, ng = rows.shape[1] * 4 // (5 * d), d // GROUP
+    sl = np.ascontiguousarray(rows[:, hkv * d:]).view(np.float16).astype(np.float64).reshape(n, hkv, 4, ng)
     out = []
     for kv in range(2):
-        rec = rows[:, :, kv]
+        byte = rows[:, kv * hkv * d // 2:(kv + 1) * hkv * d // 2].reshape(n, hkv, d // 2)
         nib = np.empty((n, hkv, d), np.uint8)
-        nib[..., 0::2], nib[..., 1::2] = rec[..., : d // 2] & 15, rec[..., : d // 2] >> 4     # nibbles in memory order
+        nib[..., 0::2], nib[..., 1::2] = byte & 15, byte >> 4                                     # nibbles in memory order
         if kv == 0:
             codes = nib.reshape(n, hkv, 4, ng, 8).transpose(0, 1, 3, 2, 4)                    # word (t, g) = channels 32 g + 8 t ..
         else:
             codes = nib.reshape(n, hkv, 8, ng, 4).transpose(0, 1, 3, 2, 4)                    # half (n, g) = channels 32 g + 4 n ..
-        sl = np.ascontiguousarray(rec[..., d // 2:]).view(np.float16).astype(np.float64)
-        out.append((codes.reshape(n, hkv, d).astype(np.float64), sl[..., :ng], sl[..., ng:]))
+        out.append((codes.reshape(n, hkv, d).astype(np.float64), sl[:, :, 2 * kv], sl[:, :, 2 * kv + 1]))
     return out
-
-
-def encode(kq, vq, d):
-    """The way back: (codes, steps, lows) of keys and of values -> rows in memory"""
-    n, hkv = kq[0].shape[:2]
-    ng = d // GROUP
-    rows = np.empty((n, hkv, 2, 5 * d // 8), np.uint8)
-    for kv, (c, s, l) in enumerate((kq, vq)):
-        c = c.astype(np.uint8).reshape(n, hkv, ng, 4, 8) if kv == 0 else c.astype(np.uint8).reshape(n, hkv, ng, 8, 4)
-        nib = np.ascontiguousarray(c.transpose(0, 1, 3, 2, 4)).reshape(n, hkv, d)
-        rows[:, :, kv, : d // 2] = nib[..., 0::2] | (nib[..., 1::2] << 4)
-        sl = np.ascontiguousarray(np.concatenate([s, l], -1).astype(np.float16))
-        rows[:, :, kv, d // 2:] = sl.view(np.uint8).reshape(n, hkv, -1)
-    return rows
 
 
 def values(q):

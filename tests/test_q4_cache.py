@@ -145,7 +145,7 @@ class Case:
     def parts(self):
         out = []
         for seg in (self.anchors, self.hist):
-            rows = seg.rows[:seg.n_tokens].cpu().numpy() if seg.rows is not None else np.zeros((0, SHAPES[self.shape][1], 2, 5 * self.d // 8), np.uint8)
+            rows = seg.rows[:seg.n_tokens].cpu().numpy() if seg.rows is not None else np.zeros((0, SHAPES[self.shape][1] * 5 * self.d // 4), np.uint8)
             kq, vq = ref.decode(rows, self.d)
             out.append((kq, vq, seg.t_shift))
         return out
@@ -213,7 +213,7 @@ def test_masked_rows_may_hold_anything(shape, byte):
     parts = c.parts()
     c.hist.rows[torch.from_numpy(~valid).cuda()] = byte
     if byte == 0x7C:
-        c.hist.rows[torch.from_numpy(~valid).cuda(), :, :, 1::2] = 0          # 0x007c and the like in turn
+        c.hist.rows[torch.from_numpy(~valid).cuda(), 0::2] = 0          # 0x7c00: infinity
     c.check(valid, weigh=(1.0, 1.0), parts=parts)
 
 
@@ -353,7 +353,7 @@ def test_refusals():
     _refused(pc.PC_ERR_CAPACITY, pc.pc_q4_store, ctx, src, small)
     _refused(pc.PC_ERR_INVALID_ARG, pc.pc_q4_store, ctx, src, small, 1)                   # a gap
     _refused(pc.PC_ERR_INVALID_ARG, pc.pc_q4_store, ctx, src, pc.Q4Segment.empty(ctx, 8, t_shift=-1))
-    bad = pc.Q4Segment(torch.empty(8 * 1280 + 1, dtype=torch.uint8, device="cuda")[1:].view(8, 8, 2, 80), small.pos, None, 0)
+    bad = pc.Q4Segment(torch.empty(8 * 1280 + 1, dtype=torch.uint8, device="cuda")[1:].view(8, 1280), small.pos, None, 0)
     _refused(pc.PC_ERR_INVALID_ARG, pc.pc_q4_store, ctx, src, bad)
     back = pc.Segment(src.k, src.v, src.pos, 0)
     _refused(pc.PC_ERR_INVALID_ARG, pc.pc_q4_load, ctx, c.hist, 38, 3, back)
