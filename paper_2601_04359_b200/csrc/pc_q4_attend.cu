@@ -9,7 +9,7 @@
 //
 // Shape.  m16n8k16 instructions with 16 keys (channels, for the values) as rows and 8 query rows of one KV head as columns: a warp
 // takes one KV head and 8 query rows and goes through the keys 16 at a time; the warps of a CTA cover the KV heads (and several
-// blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  TMA brings them, boxes of 16 tokens x 128 bytes with the 128-byte
+// blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  TMA brings them, boxes of 32 tokens x 128 bytes with the 128-byte
 // swizzle, into a ring of tiles that the warps refill in turn.  CTAs split the keys evenly; k_q4_join merges their parts, k_q4_weigh
 // turns the logits that the history left into weights.
 #include <algorithm>
@@ -34,10 +34,13 @@ namespace {
 constexpr int ROWS = 8;                // query rows of a warp
 constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
 constexpr int MAX_STAGES = 8;
-constexpr int BOX = 128, BOX_BYTES = Q4_STEP * BOX;        // a box of the rows: 16 tokens x 128 bytes
 constexpr int BAR_BYTES = 256;         // barriers and flags
 constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
-constexpr float P_SCALE = 4.f;         // probabilities times steps stay below fp16's largest: 4 * 2 * 65504 / 15
+constexpr int UNIT = 2, UNIT_KEYS = UNIT * Q4_STEP;        // steps that a warp takes together
+constexpr int BOX = 128, BOX_BYTES = UNIT_KEYS * BOX;      // a box of the rows: a unit's tokens x 128 bytes
+// Probabilities are scaled by 2^P_LOG (the sums with them, so that it cancels): times a step they stay below fp16's largest, 4 * 2 * 65504 / 15
+constexpr float P_LOG = 2.f;
+constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, so that a masked logit (-infinity) gives probability 0
 
 // Queries as the B operand in shared memory, of a task (KV head, block of 8 rows): words [hi and lo parts 8 NG][sums 2] of 32 lanes, then 8 factors
 constexpr int query_words(int d) { return 8 * (d / Q4_GROUP) + 2; }
@@ -52,8 +55,8 @@ struct Q4Params {
     int heads, blocks, subs;           // of a CTA: KV heads, blocks of 8 query rows, parts of the keys
     int block_groups;                  // CTAs that share a set of heads
     int steps0, steps;                 // steps of 16 keys: the anchors', all
-    int boxes_k, boxes;                // boxes of a step: of the key codes (as many for the values), all
-    int step_bytes, stages;            // of the ring; a stage holds `subs` steps
+    int boxes_k, boxes;                // boxes of a unit: of the key codes (as many for the values), all
+    int unit_bytes, stages;            // of the ring; a stage holds a unit for each of `subs`
     int ring_at, queries_at;           // places in shared memory
     float *part_o, *part_ml;           // [split][KV head * n_rows + row]
     float *logits;                     // [history token][n_kv * n_rows] or NULL
@@ -70,7 +73,6 @@ struct JoinParams {
 };
 
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
-__device__ __forceinline__ uint32_t lds16(uint32_t a) { uint16_t v; asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a)); return v; }
 // N 32-bit words of shared memory (2 or 4; N = 1 for the values of d = 64)
 template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N]) {
     if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
@@ -80,6 +82,15 @@ template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// Two 8 x 8 matrices of 16-bit values, a row at the address of each of the first sixteen lanes; TRANS: transposed
+template <bool TRANS> __device__ __forceinline__ void load_matrices(uint32_t a, uint32_t &x, uint32_t &y) {
+    if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
+    else asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {         // an 8 x 8 matrix of 16-bit values, two a lane
     uint32_t y;
@@ -103,7 +114,7 @@ __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.f
 // differ in bits 1 and 2).
 __device__ __forceinline__ int key_of_row(int i) { return (0x36147250u >> (4 * i)) & 7; }
 
-// Byte `b` of a section (its first box at `box0`) of token `key` (0 .. 7) in a step
+// Byte `b` of a section (its first box at `box0`) of token `key` (0 .. 7) in a unit
 __device__ __forceinline__ uint32_t place(int box0, int b, int key) {
     return (uint32_t)((box0 + (b >> 7)) * BOX_BYTES + key * BOX + ((((b >> 4) & 7) ^ key) << 4) + (b & 15));
 }
@@ -169,17 +180,14 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
             at16[0] = hi;
             at16[4 * NG * 64] = __float2half_rn(y - __half2float(hi));
         }
-        // sums over the groups against the lows: index 2 t, 2 t + 1 of the instruction = groups, a further fp16 part every NG indices
+        // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps and stay
+        // zero), a second fp16 part at the same places of the other eight
 #pragma unroll
         for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         if (lane % (Q4_GROUP / CH) == 0) {
-            char *sums = mine + 8 * NG * 128;
-            for (int part = 0; part < 3; ++part) {
-                const __half v = __float2half_rn(total);
-                const int index = part * NG + g;                     // 0 .. 15
-                reinterpret_cast<__half *>(sums + ((index / 8) * 32 + col * 4 + index % 8 / 2) * 4)[index & 1] = v;
-                total -= __half2float(v);
-            }
+            __half *sum = reinterpret_cast<__half *>(mine + (8 * NG * 32 + col * 4 + (NG + g) / 2) * 4) + (g & 1);
+            sum[0] = __float2half_rn(total);
+            sum[64] = __float2half_rn(total - __half2float(sum[0]));
         }
         if (lane == 0) reinterpret_cast<float *>(mine + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
     }
@@ -211,28 +219,41 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     __syncthreads();
     const int set = blockIdx.y / P.block_groups, first_block = (blockIdx.y - set * P.block_groups) * P.blocks;
     const int first_head = set * P.heads, n_heads = min(P.heads, P.n_kv - first_head);
-    // This CTA's steps of the two segments; a tile is `subs` steps of one segment
+    // This CTA's steps of the two segments; a tile is UNIT * subs steps of one segment
     const int s0 = (int)((long long)P.steps * blockIdx.x / gridDim.x), s1 = (int)((long long)P.steps * (blockIdx.x + 1) / gridDim.x);
     const int begin0 = min(s0, P.steps0), end0 = min(s1, P.steps0), begin1 = max(s0 - P.steps0, 0), end1 = max(s1 - P.steps0, 0);
-    const int tiles0 = (end0 - begin0 + P.subs - 1) / P.subs, n_tiles = tiles0 + (end1 - begin1 + P.subs - 1) / P.subs;
+    const int tile_steps = UNIT * P.subs;
+    const int tiles0 = (end0 - begin0 + tile_steps - 1) / tile_steps, n_tiles = tiles0 + (end1 - begin1 + tile_steps - 1) / tile_steps;
     pc_grid_dep_wait();
 
-    // A tile into stage st, by one warp: boxes of the key codes, of the value codes, of the steps and lows
+    // A tile into stage st, by one warp: boxes of the key codes, of the value codes, of the steps and lows.  One elected lane issues them (about 20
+    // cycles each; spread over the lanes of a warp they took 90).
+    const bool lead = pc_tc::elect_one();
     const auto fetch = [&](int tile, int st) {
         const bool hist = tile >= tiles0;
-        const int first = hist ? begin1 + (tile - tiles0) * P.subs : begin0 + tile * P.subs;
-        const int n = min(P.subs, (hist ? end1 : end0) - first) * P.boxes;
+        const int first = hist ? begin1 + (tile - tiles0) * tile_steps : begin0 + tile * tile_steps;
+        const int units = (min(tile_steps, (hist ? end1 : end0) - first) + UNIT - 1) / UNIT;
         const CUtensorMap *map = hist ? &map1 : &map0;
-        const uint32_t dst = ring + st * P.subs * P.step_bytes;
-        if (lane == 0) pc_mbar_expect_tx(full(st), n * BOX_BYTES);
-        __syncwarp();
-        for (int i = lane; i < n; i += 32) {
-            const int step = i / P.boxes, box = i - step * P.boxes;
-            const int in_v = box - P.boxes_k, in_s = in_v - P.boxes_k;
-            const int x = in_v < 0 ? first_head * (D / 2) + box * BOX
-                                   : (in_s < 0 ? (P.n_kv + first_head) * (D / 2) + in_v * BOX : P.n_kv * D + first_head * (D / 4) + in_s * BOX);
-            pc_tc::tma_load_2d(dst + i * BOX_BYTES, map, x, (first + step) * Q4_STEP, full(st));
+        const uint32_t bar = full(st);
+        uint32_t dst = ring + st * P.subs * P.unit_bytes;
+        if (lead) {
+            pc_mbar_expect_tx(bar, units * P.unit_bytes);
+#pragma unroll 1
+            for (int u = 0; u < units; ++u) {
+                const int y = (first + u * UNIT) * Q4_STEP;
+                int x = first_head * (D / 2);
+#pragma unroll 1
+                for (int i = 0; i < P.boxes_k; ++i, x += BOX, dst += BOX_BYTES) {
+                    pc_tc::tma_load_2d(dst, map, x, y, bar);
+                    pc_tc::tma_load_2d(dst + P.boxes_k * BOX_BYTES, map, x + P.n_kv * (D / 2), y, bar);
+                }
+                dst += P.boxes_k * BOX_BYTES;
+                x = P.n_kv * D + first_head * (D / 4);
+#pragma unroll 1
+                for (int i = 2 * P.boxes_k; i < P.boxes; ++i, x += BOX, dst += BOX_BYTES) pc_tc::tma_load_2d(dst, map, x, y, bar);
+            }
         }
+        __syncwarp();
     };
     // Where the warp is in the ring, and whose turn it is to refill: before a tile one of the warps fetches the tile that follows in
     // the stage of the tile before it
@@ -258,13 +279,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             phase ^= 1u;
         }
     };
-    for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile, tile);
+    if (warp == 0) fetch(0, 0);
 
     const int task = warp % tasks, sub = warp / tasks, head = task % P.heads, block = first_block + task / P.heads;
     const bool works = head < n_heads && block * ROWS < P.n_rows;      // else the ring still goes round
     const int t = lane & 3, row = lane >> 2;
-    float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group `row`
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
+    float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * NG; ++i)
 #pragma unroll
@@ -279,6 +300,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const uint32_t at_k = place(0, head * (D / 2) + t * NG * 4, k0), at_ks = place(box_s, head * (D / 4), k0);
     const uint32_t at_va = place(P.boxes_k, head * (D / 2) + row * NG * 2, kva), at_vb = place(P.boxes_k, head * (D / 2) + row * NG * 2, kvb);
     const uint32_t at_vsa = place(box_s, head * (D / 4) + 4 * NG, kva), at_vsb = place(box_s, head * (D / 4) + 4 * NG, kvb);
+    // steps and lows as matrices, eight numbers of a token a row
+    const int km = key_of_row(lane & 7);
+    const uint32_t at_mk = place(box_s, head * (D / 4), km) + ((lane >> 3) & 1) * EIGHT;
+    const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + ((lane >> 3) & 1) * EIGHT;
     const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;
     bool alive = true;
 #pragma unroll 1
@@ -287,6 +312,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         if (seg_begin == seg_end) continue;
         char *queries = smem + P.queries_at;
         take_queries<D, F32>(P, rope, queries, first_head, n_heads, first_block, seg ? P.shift[1] : P.shift[0]);
+        if (at == 0)                   // the ring's other stages: behind the queries, whose few loads would wait behind them
+            for (int tile = 1 + warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile, tile);
         uint32_t q_hi[2 * NG][2], q_lo[2 * NG][2], q_sum[2];
         const uint32_t my_q = pc_smem_u32(queries) + task * query_bytes(D) + lane * 4;
 #pragma unroll
@@ -302,91 +329,157 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         float *logits = seg == 1 ? P.logits : nullptr;
         if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
         const int n_seg = seg ? P.n[1] : P.n[0];
+        // Raw logits of a step's keys k0, k0 + 8 against columns 2 t, 2 t + 1: to be multiplied by f0, f1
+        const auto logits_of = [&](uint32_t rows, float (&S)[4]) {
+            uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la, lb;
+            lds(rows + at_k, wa);
+            lds(rows + at_k + EIGHT, wb);
+            lds(rows + at_ks, sa);
+            lds(rows + at_ks + EIGHT, sb);
+            load_matrices<false>(rows + at_mk, la, lb);
+            float E[4], C[NG][4];
+            mma_first(E, la, lb, la, lb, q_sum[0], q_sum[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {            // channels in the low four bits of the code words' bytes, then in the high four
+                const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    if (h == 0) mma_first(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g][0], q_lo[2 * g][1]);
+                    else mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g + 1][0], q_lo[2 * g + 1][1]);
+                }
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_hi[2 * g + h][0], q_hi[2 * g + h][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[j] = E[j] * (1.f / 16777216.f);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
+                const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
+                S[0] = fmaf(fa, C[g][0], S[0]);
+                S[1] = fmaf(fa, C[g][1], S[1]);
+                S[2] = fmaf(fb, C[g][2], S[2]);
+                S[3] = fmaf(fb, C[g][3], S[3]);
+            }
+        };
+        // Keys of a step that are there and not masked: a bit per row of the instruction
+        const auto look_at_mask = [&](int first, float (&S)[4]) {
+            const int n = n_seg - first;
+            bool ok0 = k0 < n, ok1 = k0 + 8 < n;
+            if (valid) {
+                if (ok0) ok0 = __ldg(valid + first + k0) != 0;
+                if (ok1) ok1 = __ldg(valid + first + k0 + 8) != 0;
+            }
+            if (!ok0) S[0] = S[1] = -INFINITY;
+            if (!ok1) S[2] = S[3] = -INFINITY;
+            // lane 4 i speaks for row i, lane 4 i + 1 for row i + 8
+            return __ballot_sync(0xffffffffu, t == 0 ? ok0 : ok1);
+        };
+        const auto leave_logits = [&](int first, const float (&S)[4]) {
+            const int n = n_seg - first;
+            float *to = logits + (size_t)(first + k0) * R;
+            if (k0 < n) {
+                if (r0 < P.n_rows) to[0] = S[0] * f0;
+                if (r0 + 1 < P.n_rows) to[1] = S[1] * f1;
+            }
+            if (k0 + 8 < n) {
+                to += (size_t)8 * R;
+                if (r0 < P.n_rows) to[0] = S[2] * f0;
+                if (r0 + 1 < P.n_rows) to[1] = S[3] * f1;
+            }
+        };
+        // O += P V of a step, p = the probabilities of S's keys and columns
+        const auto add_values = [&](uint32_t rows, const float (&p)[4], bool all, uint32_t seen) {
+            uint32_t steps[4][NG / 2], codes[4][NG / 2], ua, ub;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lds(rows + (j & 1 ? at_vb : at_va) + (j >> 1) * EIGHT, codes[j]);
+                lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
+            }
+            load_matrices<true>(rows + at_mv, ua, ub);
+            if (!all) {                              // what lies in the place of a masked key may be anything
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!((seen >> (4 * (2 * t + (j & 1)) + (j >> 1))) & 1u)) {
+                        (j < 2 ? ua : ub) &= (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+                        for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
+                    }
+            }
+            uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
+            ph[0] = pack_half(p[0], p[1]);
+            ph[1] = pack_half(p[2], p[3]);
+            if constexpr (F32) {
+                const float2 a = halves(ph[0]), b = halves(ph[1]);
+                pl[0] = transpose8(pack_half(p[0] - a.x, p[1] - a.y));
+                pl[1] = transpose8(pack_half(p[2] - b.x, p[3] - b.y));
+            }
+            ph[0] = transpose8(ph[0]);
+            ph[1] = transpose8(ph[1]);
+            mma(L, ua, 0u, ub, 0u, ph[0], ph[1]);
+            if constexpr (F32) mma(L, ua, 0u, ub, 0u, pl[0], pl[1]);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
+                const uint32_t ta = __byte_perm(codes[0][g / 2], codes[1][g / 2], pick), tb = __byte_perm(codes[2][g / 2], codes[3][g / 2], pick);
+                const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
+                const uint32_t ya = ta >> 8, yb = tb >> 8;
+                const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
+                const uint32_t c0 = ya & 0x000F000Fu, c1 = ya & 0x00F000F0u, c2 = yb & 0x000F000Fu, c3 = yb & 0x00F000F0u;
+                if constexpr (F32) {
+                    // probability times step in fp32 from the two parts, split again
+                    const float2 sa = halves(qa), sb = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
+                    const float e0 = (xh.x + xl.x) * sa.x, e1 = (xh.y + xl.y) * sa.y, e2 = (yh.x + yl.x) * sb.x, e3 = (yh.y + yl.y) * sb.y;
+                    const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
+                    const float2 g0 = halves(h0), g1 = halves(h1);
+                    const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
+                    mma(O[2 * g], a0, a1, a2, a3, w0, w1);
+                    mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
+                    mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                    mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                } else {
+                    const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
+                    mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                    mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                }
+            }
+        };
 #pragma unroll 1
-        for (int s = seg_begin + sub; alive && s - sub < seg_end; s += P.subs) {
+        for (int tile_first = seg_begin; alive && tile_first < seg_end; tile_first += tile_steps) {
             if (!ready()) {
                 alive = false;
                 break;
             }
+            const int s = tile_first + UNIT * sub;
             if (works && s < seg_end) {
-                const uint32_t rows = ring + (st * P.subs + sub) * P.step_bytes;
-                const int first = s * Q4_STEP, n = n_seg - first;
-                bool ok0 = true, ok1 = true;
-                uint32_t b0 = 0xffffffffu, b1 = 0xffffffffu;
-                if (n < Q4_STEP || valid) {
-                    ok0 = k0 < n;
-                    ok1 = k0 + 8 < n;
-                    if (valid) {
-                        if (ok0) ok0 = __ldg(valid + first + k0) != 0;
-                        if (ok1) ok1 = __ldg(valid + first + k0 + 8) != 0;
-                    }
-                    b0 = __ballot_sync(0xffffffffu, ok0);
-                    b1 = __ballot_sync(0xffffffffu, ok1);
+                const uint32_t rows = ring + (st * P.subs + sub) * P.unit_bytes, rows1 = rows + Q4_STEP * BOX;
+                const bool two = s + 1 < seg_end;
+                float S0[4], S1[4];
+                logits_of(rows, S0);
+                if (two) logits_of(rows1, S1);
+                else S1[0] = S1[1] = S1[2] = S1[3] = -INFINITY;
+                uint32_t seen0 = 0xffffffffu, seen1 = 0xffffffffu;
+                const bool all = !valid && (s + UNIT) * Q4_STEP <= n_seg;
+                if (!all) {
+                    seen0 = look_at_mask(s * Q4_STEP, S0);
+                    if (two) seen1 = look_at_mask((s + 1) * Q4_STEP, S1);
                 }
-                // ---- logits
-                const uint32_t ka = rows + at_k, kb = ka + EIGHT, ks = rows + at_ks;
-                uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2];
-                lds(ka, wa);
-                lds(kb, wb);
-                lds(ks, sa);
-                lds(ks + EIGHT, sb);
-                float S[4] = {0.f, 0.f, 0.f, 0.f}, C[NG][4];
-                {
-                    const uint32_t off = 2 * NG + (NG == 4 ? (t & 1) * 4 : 0);
-                    const uint32_t la = lds32(ks + off), lb = lds32(ks + EIGHT + off);
-                    mma(S, la, lb, la, lb, q_sum[0], q_sum[1]);
-                }
-#pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) C[g][j] = 0.f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {        // channels in the low four bits of the code words' bytes, then in the high four
-                    const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
-#pragma unroll
-                    for (int g = 0; g < NG; ++g)
-                        mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
-#pragma unroll
-                    for (int g = 0; g < NG; ++g)
-                        mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_hi[2 * g + h][0], q_hi[2 * g + h][1]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) S[j] *= 1.f / 16777216.f;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
-                    const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
-                    S[0] = fmaf(fa, C[g][0], S[0]);
-                    S[1] = fmaf(fa, C[g][1], S[1]);
-                    S[2] = fmaf(fb, C[g][2], S[2]);
-                    S[3] = fmaf(fb, C[g][3], S[3]);
-                }
-                S[0] = ok0 ? S[0] * f0 : -INFINITY;
-                S[1] = ok0 ? S[1] * f1 : -INFINITY;
-                S[2] = ok1 ? S[2] * f0 : -INFINITY;
-                S[3] = ok1 ? S[3] * f1 : -INFINITY;
                 if (logits) {
-                    float *to = logits + (size_t)(first + k0) * R;
-                    if (k0 < n) {
-                        if (r0 < P.n_rows) to[0] = S[0];
-                        if (r0 + 1 < P.n_rows) to[1] = S[1];
-                    }
-                    if (k0 + 8 < n) {
-                        to += (size_t)8 * R;
-                        if (r0 < P.n_rows) to[0] = S[2];
-                        if (r0 + 1 < P.n_rows) to[1] = S[3];
-                    }
+                    leave_logits(s * Q4_STEP, S0);
+                    if (two) leave_logits((s + 1) * Q4_STEP, S1);
                 }
-                // ---- softmax: maximum of the 16 keys of each column
-                float x0 = fmaxf(S[0], S[2]), x1 = fmaxf(S[1], S[3]);
+                // ---- softmax: maximum of the keys of each column
+                float x0 = fmaxf(fmaxf(S0[0], S0[2]), fmaxf(S1[0], S1[2])), x1 = fmaxf(fmaxf(S0[1], S0[3]), fmaxf(S1[1], S1[3]));
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) {
                     x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
                     x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
                 }
+                x0 = fmaf(x0, f0, -P_LOG);
+                x1 = fmaf(x1, f1, -P_LOG);
                 if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
-                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-                    const float c0 = n0 == -INFINITY ? 1.f : exp2_fast(m0 - n0), c1 = n1 == -INFINITY ? 1.f : exp2_fast(m1 - n1);
+                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1), c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1);
                     m0 = n0;
                     m1 = n1;
                     l0 *= c0;
@@ -396,66 +489,15 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                     L[0] *= c0;
                     L[1] *= c1;
                 }
-                const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
-                const float p0 = exp2_fast(S[0] - z0), p1 = exp2_fast(S[1] - z1), p2 = exp2_fast(S[2] - z0), p3 = exp2_fast(S[3] - z1);
-                l0 += p0 + p2;
-                l1 += p1 + p3;
-                // ---- values: keys of rows 2 t, 2 t + 1 (and + 8) of the instruction
-                uint32_t u[4], steps[4][NG / 2], codes[4][NG / 2];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t sl = rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT;
-                    lds(rows + (j & 1 ? at_vb : at_va) + (j >> 1) * EIGHT, codes[j]);
-                    lds(sl, steps[j]);
-                    u[j] = row < NG ? lds16(sl + 2 * NG + 2 * row) : 0u;
+                    S0[j] = exp2_fast(fmaf(S0[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
+                    S1[j] = exp2_fast(fmaf(S1[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
                 }
-                if ((b0 & b1) != 0xffffffffu) {      // what lies in the place of a masked key may be anything
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (!(((j < 2 ? b0 : b1) >> (4 * (2 * t + (j & 1)))) & 1u)) {
-                            u[j] = 0u;
-#pragma unroll
-                            for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
-                        }
-                }
-                uint32_t pl[2], ph[2];               // probabilities as the B operand: column = query row lane / 4
-                ph[0] = pack_half(p0 * P_SCALE, p1 * P_SCALE);
-                ph[1] = pack_half(p2 * P_SCALE, p3 * P_SCALE);
-                if constexpr (F32) {
-                    const float2 a = halves(ph[0]), b = halves(ph[1]);
-                    pl[0] = transpose8(pack_half(p0 * P_SCALE - a.x, p1 * P_SCALE - a.y));
-                    pl[1] = transpose8(pack_half(p2 * P_SCALE - b.x, p3 * P_SCALE - b.y));
-                }
-                ph[0] = transpose8(ph[0]);
-                ph[1] = transpose8(ph[1]);
-                const uint32_t ua = u[0] | u[1] << 16, ub = u[2] | u[3] << 16;
-                mma(L, ua, 0u, ub, 0u, ph[0], ph[1]);
-                if constexpr (F32) mma(L, ua, 0u, ub, 0u, pl[0], pl[1]);
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
-                    const uint32_t ta = __byte_perm(codes[0][g / 2], codes[1][g / 2], pick), tb = __byte_perm(codes[2][g / 2], codes[3][g / 2], pick);
-                    const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
-                    const uint32_t ya = ta >> 8, yb = tb >> 8;
-                    const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
-                    const uint32_t c0 = ya & 0x000F000Fu, c1 = ya & 0x00F000F0u, c2 = yb & 0x000F000Fu, c3 = yb & 0x00F000F0u;
-                    if constexpr (F32) {
-                        // probability times step in fp32 from the two parts, split again
-                        const float2 sa2 = halves(qa), sb2 = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
-                        const float e0 = (xh.x + xl.x) * sa2.x, e1 = (xh.y + xl.y) * sa2.y, e2 = (yh.x + yl.x) * sb2.x, e3 = (yh.y + yl.y) * sb2.y;
-                        const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
-                        const float2 g0 = halves(h0), g1 = halves(h1);
-                        const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
-                        mma(O[2 * g], a0, a1, a2, a3, w0, w1);
-                        mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
-                        mma(O[2 * g], a0, a1, a2, a3, h0, h1);
-                        mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
-                    } else {
-                        const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
-                        mma(O[2 * g], a0, a1, a2, a3, h0, h1);
-                        mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
-                    }
-                }
+                l0 += (S0[0] + S0[2]) + (S1[0] + S1[2]);
+                l1 += (S0[1] + S0[3]) + (S1[1] + S1[3]);
+                add_values(rows, S0, all, seen0);
+                if (two) add_values(rows1, S1, all, seen1);
             }
             done();
         }
@@ -485,12 +527,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         float *mine = parts + (warp * ROWS + 2 * t) * PITCH + 4 * row;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const float w0 = __shfl_sync(0xffffffffu, L[0], g * 4 + t), w1 = __shfl_sync(0xffffffffu, L[1], g * 4 + t);
-            constexpr float A = 16777216.f / P_SCALE, B = 1048576.f / P_SCALE, C = 1.f / P_SCALE;
+            const float w0 = __shfl_sync(0xffffffffu, L[0], (8 - NG + g) * 4 + t), w1 = __shfl_sync(0xffffffffu, L[1], (8 - NG + g) * 4 + t);
+            constexpr float A = 16777216.f, B = 1048576.f;      // the codes' powers of two
             *reinterpret_cast<float4 *>(mine + g * Q4_GROUP) =
-                make_float4(fmaf(O[2 * g][0], A, w0 * C), fmaf(O[2 * g][2], B, w0 * C), fmaf(O[2 * g + 1][0], A, w0 * C), fmaf(O[2 * g + 1][2], B, w0 * C));
+                make_float4(fmaf(O[2 * g][0], A, w0), fmaf(O[2 * g][2], B, w0), fmaf(O[2 * g + 1][0], A, w0), fmaf(O[2 * g + 1][2], B, w0));
             *reinterpret_cast<float4 *>(mine + PITCH + g * Q4_GROUP) =
-                make_float4(fmaf(O[2 * g][1], A, w1 * C), fmaf(O[2 * g][3], B, w1 * C), fmaf(O[2 * g + 1][1], A, w1 * C), fmaf(O[2 * g + 1][3], B, w1 * C));
+                make_float4(fmaf(O[2 * g][1], A, w1), fmaf(O[2 * g][3], B, w1), fmaf(O[2 * g + 1][1], A, w1), fmaf(O[2 * g + 1][3], B, w1));
         }
     }
     __syncthreads();
@@ -498,19 +540,18 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     for (int e = threadIdx.x; e < n_heads * count * (D / 4); e += blockDim.x) {
         const int c = e % (D / 4), i = e / (D / 4), h = i / count, in_head = first_block * ROWS + i % count;
         const int k = i % count / ROWS * P.heads + h, r = i % count % ROWS;
-        float M = -INFINITY, l = 0.f;
+        float M = NO_MAX, l = 0.f;
         for (int b = 0; b < P.subs; ++b) M = fmaxf(M, ms[(b * tasks + k) * ROWS + r]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (M != -INFINITY)
-            for (int b = 0; b < P.subs; ++b) {
-                const float f = exp2_fast(ms[(b * tasks + k) * ROWS + r] - M);
-                const float4 x = *reinterpret_cast<const float4 *>(parts + ((b * tasks + k) * ROWS + r) * PITCH + 4 * c);
-                l = fmaf(f, ls[(b * tasks + k) * ROWS + r], l);
-                o.x = fmaf(f, x.x, o.x);
-                o.y = fmaf(f, x.y, o.y);
-                o.z = fmaf(f, x.z, o.z);
-                o.w = fmaf(f, x.w, o.w);
-            }
+        for (int b = 0; b < P.subs; ++b) {
+            const float f = exp2_fast(ms[(b * tasks + k) * ROWS + r] - M);
+            const float4 x = *reinterpret_cast<const float4 *>(parts + ((b * tasks + k) * ROWS + r) * PITCH + 4 * c);
+            l = fmaf(f, ls[(b * tasks + k) * ROWS + r], l);
+            o.x = fmaf(f, x.x, o.x);
+            o.y = fmaf(f, x.y, o.y);
+            o.z = fmaf(f, x.z, o.z);
+            o.w = fmaf(f, x.w, o.w);
+        }
         const size_t at = (size_t)blockIdx.x * rows_all + (size_t)(first_head + h) * P.n_rows + in_head;
         reinterpret_cast<float4 *>(P.part_o)[at * (D / 4) + c] = o;
         if (c == 0) reinterpret_cast<float2 *>(P.part_ml)[at] = make_float2(M, l);
@@ -528,7 +569,7 @@ template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_
     const int row = blockIdx.x, c = threadIdx.x % LANES, set = threadIdx.x / LANES;
     const float2 *ml = reinterpret_cast<const float2 *>(J.part_ml) + row;
     const float4 *po = reinterpret_cast<const float4 *>(J.part_o) + (size_t)row * LANES + c;
-    float M = -INFINITY, l = 0.f;
+    float M = NO_MAX, l = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s0 = set; s0 < J.splits; s0 += SETS * BATCH) {
         float4 x[BATCH];
@@ -536,7 +577,7 @@ template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const int s = s0 + i * SETS;
-            y[i] = make_float2(-INFINITY, 0.f);
+            y[i] = make_float2(NO_MAX, 0.f);
             x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (s < J.splits) {
                 y[i] = __ldg(ml + (size_t)s * J.rows);
@@ -546,13 +587,13 @@ template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_
         float top = M;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) top = fmaxf(top, y[i].x);
-        const float z = top == -INFINITY ? 0.f : top, f0 = exp2_fast(M - z);
+        const float f0 = exp2_fast(M - top);
         l *= f0;
         sum = make_float4(sum.x * f0, sum.y * f0, sum.z * f0, sum.w * f0);
         M = top;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const float f = exp2_fast(y[i].x - z);
+            const float f = exp2_fast(y[i].x - top);
             l = fmaf(f, y[i].y, l);
             sum.x = fmaf(f, x[i].x, sum.x);
             sum.y = fmaf(f, x[i].y, sum.y);
@@ -568,12 +609,11 @@ template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_
     if (threadIdx.x >= LANES) return;
 #pragma unroll
     for (int i = 0; i < SETS; ++i) M = fmaxf(M, mls[i].x);
-    const float z = M == -INFINITY ? 0.f : M;
     l = 0.f;
     sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < SETS; ++i) {
-        const float f = exp2_fast(mls[i].x - z);
+        const float f = exp2_fast(mls[i].x - M);
         const float4 x = sums[i][c];
         l = fmaf(f, mls[i].y, l);
         sum.x = fmaf(f, x.x, sum.x);
@@ -618,12 +658,12 @@ __global__ void __launch_bounds__(256) k_accumulate(const float *__restrict__ ma
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// Rows as bytes, boxes of 16 tokens x 128 bytes; what lies outside reads as zero
+// Rows as bytes, boxes of 32 tokens x 128 bytes; what lies outside reads as zero
 bool make_row_map(CUtensorMap *m, const void *rows, uint64_t n, uint64_t row_bytes) {
     const pc_tc::EncodeTiledFn fn = pc_tc::encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {row_bytes, n}, strides[1] = {row_bytes};
-    const cuuint32_t box[2] = {BOX, Q4_STEP}, estr[2] = {1, 1};
+    const cuuint32_t box[2] = {BOX, UNIT_KEYS}, estr[2] = {1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(rows), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -660,17 +700,18 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     const int n_blocks = div_up(P.n_rows, ROWS);
     P.block_groups = div_up(n_blocks, MAX_WARPS / P.heads);
     P.blocks = div_up(n_blocks, P.block_groups);
-    P.subs = MAX_WARPS / (P.heads * P.blocks);
     P.steps0 = div_up(P.n[0], Q4_STEP);
     P.steps = P.steps0 + div_up(P.n[1], Q4_STEP);
     P.boxes_k = div_up(P.heads * D.head_dim / 2, BOX);
     P.boxes = 2 * P.boxes_k + div_up(P.heads * D.head_dim / 4, BOX);
-    P.step_bytes = P.boxes * BOX_BYTES;
-    const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
+    P.unit_bytes = P.boxes * BOX_BYTES;
     P.queries_at = BAR_BYTES;
     P.ring_at = div_up(BAR_BYTES + P.heads * P.blocks * query_bytes(D.head_dim), 1024) * 1024;
-    P.stages = std::min(MAX_STAGES, (SMEM_MOST - 1024 - P.ring_at) / (P.subs * P.step_bytes));
-    const size_t smem = 1024 + P.ring_at + std::max(P.stages * P.subs * P.step_bytes, merge_bytes);
+    const int room = SMEM_MOST - 1024 - P.ring_at;
+    P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), room / (2 * P.unit_bytes));          // of one or two heads a unit holds more than it needs
+    const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
+    P.stages = std::min(MAX_STAGES, room / (P.subs * P.unit_bytes));
+    const size_t smem = 1024 + P.ring_at + std::max(P.stages * P.subs * P.unit_bytes, merge_bytes);
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
