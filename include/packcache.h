@@ -388,8 +388,8 @@ pc_status pc_window_state(pc_window *w, int32_t *n_frames, int32_t *counts, int6
  * A token's row is Hkv * 5 d / 4 bytes: the codes of the keys [Hkv][d / 2], the codes of the values [Hkv][d / 2], then for each KV head four runs of
  * d / 32 fp16 numbers, steps and lows of the key and steps and lows of the value.
  * Codes of a key: 32-bit word number t * (d / 32) + g (t = 0 .. 3) holds channels 32 g + 8 t .. + 7, the first in its lowest bits.
- * Codes of a value: 16-bit word number n * (d / 32) + g (n = 0 .. 7) holds channels 32 g + 4 n .. + 3, the first in its lowest bits.
- * (The parts of a channel group that one thread of the attention kernel multiplies lie side by side.) */
+ * Codes of a value: channel c in half c % 2 of byte c / 2, even channels in the low half.
+ * (The parts of a key that one thread of the attention kernel multiplies lie side by side.) */
 typedef struct {
     void *rows;       /* device [capacity][Hkv * 5 d / 4] bytes, 16-byte aligned */
     int32_t *pos;     /* device [capacity][4], as in pc_segment */

@@ -139,13 +139,9 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_store(const RowsArgs A, pc_r
         const uint32_t kc = quantise8(x, ks, kl, bad);
         unpack8<F32>(vr[h], x);
         const uint32_t vc = quantise8(x, vs, vl, bad);
-        // 16-bit words n = 2t (channels 0-3) and 2t + 1 (4-7) of group g: the even group's lane writes the former for both groups of a
-        // pair, the odd one's the latter
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, (g & 1) ? vc & 0xFFFFu : vc >> 16, 4);
         if (h < heads) {
             reinterpret_cast<uint32_t *>(kc_at + h * (D / 2))[t * NG + g] = kc;
-            reinterpret_cast<uint32_t *>(vc_at + h * (D / 2))[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)] =
-                (g & 1) ? other | (vc & 0xFFFF0000u) : (vc & 0xFFFFu) | (other << 16);
+            reinterpret_cast<uint32_t *>(vc_at + h * (D / 2))[u] = vc;
             reinterpret_cast<__half *>(sl_at + h * (D / 4))[t * NG + g] = t == 0 ? ks : (t == 1 ? kl : (t == 2 ? vs : vl));
         }
     }
@@ -172,7 +168,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_ro
         if (h < heads) {
             const uint16_t *sl = reinterpret_cast<const uint16_t *>(sl_at + h * (D / 4));
             kc[h] = reinterpret_cast<const uint32_t *>(kc_at + h * (D / 2))[t * NG + g];
-            vc[h] = reinterpret_cast<const uint32_t *>(vc_at + h * (D / 2))[(2 * t + (g & 1)) * (NG / 2) + (g >> 1)];
+            vc[h] = reinterpret_cast<const uint32_t *>(vc_at + h * (D / 2))[u];
             kq[h] = sl[g] | (uint32_t)sl[NG + g] << 16;
             vq[h] = sl[2 * NG + g] | (uint32_t)sl[3 * NG + g] << 16;
         }
@@ -197,8 +193,6 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_ro
     const auto half_of = [](uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu))); };
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, (g & 1) ? vc[h] & 0xFFFFu : vc[h] >> 16, 4);
-        const uint32_t vw = (g & 1) ? (vc[h] & 0xFFFF0000u) | other : (vc[h] & 0xFFFFu) | (other << 16);
         if (h < heads) {
             float x[8];
 #pragma unroll
@@ -209,7 +203,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_q4_load(const RowsArgs A, pc_ro
             }
             store8<F32>(A.k_out, at + h * D, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = value(vw, i, half_of(vq[h]), half_of(vq[h] >> 16));
+            for (int i = 0; i < 8; ++i) x[i] = value(vc[h], i, half_of(vq[h]), half_of(vq[h] >> 16));
             store8<F32>(A.v_out, at + h * D, x);
         }
     }

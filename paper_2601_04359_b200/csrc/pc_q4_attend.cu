@@ -53,8 +53,10 @@ struct Q4Params {
     const int32_t *q_pos;
     int n_q, n_q_heads, n_kv, group, n_rows;      // n_rows = n_q * group: query rows of a KV head
     int heads, blocks, subs;           // of a CTA: KV heads, blocks of 8 query rows, parts of the keys
-    int block_groups;                  // CTAs that share a set of heads
-    int steps0, steps;                 // steps of 16 keys: the anchors', all
+    uint32_t inv_tasks, inv_heads;     // 65536 / (heads * blocks) + 1, 65536 / heads + 1: a warp's number (below 16) is divided by multiplying
+    float inv_group;
+    int steps0;                        // steps of 16 keys of the anchors
+    int steps_cta, steps_more;         // steps of a CTA, and how many CTAs take one more
     int boxes_k, boxes;                // boxes of a unit: of the key codes (as many for the values), all
     int unit_bytes, stages;            // of the ring; a stage holds a unit for each of `subs`
     int ring_at, queries_at;           // places in shared memory
@@ -92,6 +94,9 @@ template <bool TRANS> __device__ __forceinline__ void load_matrices(uint32_t a, 
     if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
     else asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
 }
+__device__ __forceinline__ void load_codes(uint32_t a, uint32_t &x0, uint32_t &x1, uint32_t &x2, uint32_t &x3) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x0), "=r"(x1), "=r"(x2), "=r"(x3) : "r"(a));
+}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {         // an 8 x 8 matrix of 16-bit values, two a lane
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -119,77 +124,123 @@ __device__ __forceinline__ uint32_t place(int box0, int b, int key) {
     return (uint32_t)((box0 + (b >> 7)) * BOX_BYTES + key * BOX + ((((b >> 4) & 7) ^ key) << 4) + (b & 15));
 }
 
-// The queries of a CTA's tasks, rotated at (t + shift, h, w), times log2(e) / sqrt(d), as the B operand of Q K^T in shared memory: a warp per row, D / 32
-// consecutive channels a lane.  Called by all threads; rows that there are none of are zero.
-template <int D, bool F32>
-__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int first_head, int n_heads, int first_block, int shift) {
-    constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D), BYTES = query_bytes(D);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    const int row0 = first_block * ROWS, count = min(P.n_rows - row0, P.blocks * ROWS);
-    __syncthreads();                               // the queries of the segment before are in registers
-    for (int i = threadIdx.x; i < P.heads * P.blocks * (BYTES / 16); i += blockDim.x) reinterpret_cast<uint4 *>(to)[i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
+__device__ __forceinline__ int4 ldg_int4(const int32_t *p) {        // in program order, ahead of the copies that are issued behind it
+    int4 v;
+    asm volatile("ld.global.nc.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float2 ldg_float2(const float2 *p) {
+    float2 v;
+    asm volatile("ld.global.nc.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+
+// The queries of a task, rotated at (t + shift, h, w), times log2(e) / sqrt(d), as the B operand of Q K^T in shared memory.  The warps of a task (one for
+// each part of the keys) take its rows in turn, D / 32 consecutive channels a lane; columns without a row are zero.  Positions and queries
+// of up to PER rows are requested first, then the first tile (between()), then the table entries that the positions name, then the
+// other tiles (behind()): these few loads, one behind the other, would take 7,500 cycles behind the whole ring's.
+template <int D, bool F32, typename Between, typename Behind>
+__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int kv_head, int block, int sub, int shift,
+                                             Between between, Behind behind) {
+    constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D), PER = 2;
+    const int lane = threadIdx.x & 31;
+    const int count = min(P.n_rows - block * ROWS, ROWS);            // none or fewer for a warp that has no head or no rows
     // channel 32 g + 8 t + k of a row: 16-bit half k / 4 of word (2 g + k % 2) * 2 + (k / 2) % 2 of lane 4 row + t.  The code words give
     // channels (k, k + 4) as one register: k even in the low four bits of their bytes, k odd in the high four, 2^4 larger
     const int g = lane * CH / Q4_GROUP, t = lane * CH % Q4_GROUP / 8, k0 = lane * CH % 8;
-    for (int i = warp; i < n_heads * count; i += n_warps) {
-        const int h = i / count, r = i % count, task = r / ROWS * P.heads + h, col = r % ROWS;
-        const int query = (row0 + r) / P.group, head = (first_head + h) * P.group + (row0 + r) % P.group;
-        const size_t at = ((size_t)query * P.n_q_heads + head) * D + lane * CH;
-        const int4 p = __ldg(reinterpret_cast<const int4 *>(P.q_pos) + query);
-        float x[CH];
-        if constexpr (F32) {
+#pragma unroll 1
+    for (int base = sub;; base += PER * P.subs) {
+        const bool first = base == sub;
+        if (!first && base >= count) break;
+        int4 p[PER];
+        uint32_t raw[PER][CH];
 #pragma unroll
-            for (int c = 0; c < CH; c += 2) {
-                const float2 v = __ldg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + at + c));
-                x[c] = v.x;
-                x[c + 1] = v.y;
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < CH; c += 2) {
-                const uint32_t v = __ldg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + at + c));
-                x[c] = pc_bf16_lo(v);
-                x[c + 1] = pc_bf16_hi(v);
+        for (int u = 0; u < PER; ++u) {
+            const int r = block * ROWS + base + u * P.subs;
+            p[u] = make_int4(0, 0, 0, 0);
+            if (base + u * P.subs < count) {
+                const int query = (int)(((float)r + 0.5f) * P.inv_group), head = kv_head * P.group + r - query * P.group;
+                p[u] = ldg_int4(P.q_pos + (size_t)query * 4);
+                const char *src = static_cast<const char *>(P.q) + (((size_t)query * P.n_q_heads + head) * D + lane * CH) * (F32 ? 4 : 2);
+                constexpr int N = CH * (F32 ? 4 : 2) / 4;
+                if constexpr (N == 4) asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(raw[u][0]), "=r"(raw[u][1]), "=r"(raw[u][2]), "=r"(raw[u][3]) : "l"(src));
+                else if constexpr (N == 2) asm volatile("ld.global.nc.v2.u32 {%0,%1}, [%2];" : "=r"(raw[u][0]), "=r"(raw[u][1]) : "l"(src));
+                else asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(raw[u][0]) : "l"(src));
             }
         }
+        if (first) {
+            between();
+            __syncthreads();                       // the queries of the segment before are in registers
+            if ((lane >> 2) >= count) {
+                for (int w = sub; w < WORDS; w += P.subs) reinterpret_cast<uint32_t *>(to)[w * 32 + lane] = 0u;
+                if ((lane & 3) == 0) reinterpret_cast<float *>(to + WORDS * 128)[lane >> 2] = 0.f;
+            }
+        }
+        float2 cs[PER][CH / 2];
         bool bad = false;
-        float most = 0.f, total = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; c += 2) {
-            const float2 y = pc_rotate(x[c], x[c + 1], pc_rope_cs_clamped(rope, (lane * CH + c) / 2, p.x + shift, p.y, p.z, bad));
-            x[c] = y.x * P.scale;
-            x[c + 1] = y.y * P.scale;
-            most = fmaxf(most, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
+        for (int c = 0; c < CH / 2; ++c) {
+            const int pair = lane * (CH / 2) + c, a = pair % 3;
+            const int most = a == 0 ? rope.max_pos[0] : (a == 1 ? rope.max_pos[1] : rope.max_pos[2]);
+            const int off = (a == 0 ? rope.off[0] : (a == 1 ? rope.off[1] : rope.off[2])) + pair / 3;
+            const int n = a == 0 ? rope.n_axis[0] : (a == 1 ? rope.n_axis[1] : rope.n_axis[2]);
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int at = a == 0 ? p[u].x + shift : (a == 1 ? p[u].y : p[u].z);
+                bad |= base + u * P.subs < count && (unsigned)at >= (unsigned)most;
+                cs[u][c] = ldg_float2(rope.tab + off + (size_t)min(max(at, 0), most - 1) * n);
+            }
         }
+        if (first) behind();
         if (bad) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
-        // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
-        most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-        const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
-        const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-        char *mine = to + task * BYTES;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int k = k0 + c;
-            x[c] *= up;
-            total += x[c];
-            const float y = (c & 1) ? x[c] * 0.0625f : x[c];         // k0 is even
-            const __half hi = __float2half_rn(y);
-            const int word = (2 * g + (k & 1)) * 2 + ((k >> 1) & 1);
-            __half *at16 = reinterpret_cast<__half *>(mine + (word * 32 + col * 4 + t) * 4) + (k >> 2);
-            at16[0] = hi;
-            at16[4 * NG * 64] = __float2half_rn(y - __half2float(hi));
-        }
-        // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps and stay
-        // zero), a second fp16 part at the same places of the other eight
+        for (int u = 0; u < PER; ++u) {
+            const int col = base + u * P.subs;
+            if (col >= count) break;
+            float x[CH], most = 0.f, total = 0.f;
 #pragma unroll
-        for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        if (lane % (Q4_GROUP / CH) == 0) {
-            __half *sum = reinterpret_cast<__half *>(mine + (8 * NG * 32 + col * 4 + (NG + g) / 2) * 4) + (g & 1);
-            sum[0] = __float2half_rn(total);
-            sum[64] = __float2half_rn(total - __half2float(sum[0]));
+            for (int c = 0; c < CH; c += 2) {
+                const float x0 = F32 ? __uint_as_float(raw[u][c]) : pc_bf16_lo(raw[u][c / 2]);
+                const float x1 = F32 ? __uint_as_float(raw[u][c + 1]) : pc_bf16_hi(raw[u][c / 2]);
+                const float2 y = pc_rotate(x0, x1, cs[u][c / 2]);
+                x[c] = y.x * P.scale;
+                x[c + 1] = y.y * P.scale;
+                most = fmaxf(most, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
+            }
+            // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
+            most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+            const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
+            const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int k = k0 + c;
+                const float v = x[c] * up, y = (c & 1) ? v * 0.0625f : v;             // k0 is even
+                total += v;
+                const __half hi = __float2half_rn(y);
+                const int word = (2 * g + (c & 1)) * 2 + ((k >> 1) & 1);
+                __half *at16 = reinterpret_cast<__half *>(to + (word * 32 + col * 4 + t) * 4) + (k >> 2);
+                at16[0] = hi;
+                at16[4 * NG * 64] = __float2half_rn(y - __half2float(hi));
+            }
+            // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps and
+            // are zero), a second fp16 part at the same places of the other eight
+#pragma unroll
+            for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            uint32_t *sums = reinterpret_cast<uint32_t *>(to) + 8 * NG * 32 + col * 4;
+            const float next = __shfl_down_sync(0xffffffffu, total, Q4_GROUP / CH);   // of the group behind
+            if (lane < 4) {                        // a word of two groups a lane, zero where the steps are
+                sums[lane] = 0u;
+                sums[32 + lane] = 0u;
+            }
+            __syncwarp();
+            if (lane % (2 * Q4_GROUP / CH) == 0) {
+                const uint32_t h = pack_half(total, next);
+                const float2 back = halves(h);
+                sums[NG / 2 + g / 2] = h;
+                sums[32 + NG / 2 + g / 2] = pack_half(total - back.x, next - back.y);
+            }
+            if (lane == 0) reinterpret_cast<float *>(to + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
         }
-        if (lane == 0) reinterpret_cast<float *>(mine + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
     }
     __syncthreads();
 }
@@ -217,10 +268,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    const int set = blockIdx.y / P.block_groups, first_block = (blockIdx.y - set * P.block_groups) * P.blocks;
-    const int first_head = set * P.heads, n_heads = min(P.heads, P.n_kv - first_head);
+    const int first_head = blockIdx.z * P.heads, first_block = blockIdx.y * P.blocks, n_heads = min(P.heads, P.n_kv - first_head);
+    const int sub = (int)(warp * P.inv_tasks >> 16), task = warp - sub * tasks;
+    const int head = task - (int)(task * P.inv_heads >> 16) * P.heads, block = first_block + (int)(task * P.inv_heads >> 16);
+    const bool works = head < n_heads && block * ROWS < P.n_rows;      // else the ring still goes round
     // This CTA's steps of the two segments; a tile is UNIT * subs steps of one segment
-    const int s0 = (int)((long long)P.steps * blockIdx.x / gridDim.x), s1 = (int)((long long)P.steps * (blockIdx.x + 1) / gridDim.x);
+    const int bx = (int)blockIdx.x, s0 = bx * P.steps_cta + min(bx, P.steps_more), s1 = s0 + P.steps_cta + (bx < P.steps_more ? 1 : 0);
     const int begin0 = min(s0, P.steps0), end0 = min(s1, P.steps0), begin1 = max(s0 - P.steps0, 0), end1 = max(s1 - P.steps0, 0);
     const int tile_steps = UNIT * P.subs;
     const int tiles0 = (end0 - begin0 + tile_steps - 1) / tile_steps, n_tiles = tiles0 + (end1 - begin1 + tile_steps - 1) / tile_steps;
@@ -279,10 +332,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             phase ^= 1u;
         }
     };
-    if (warp == 0) fetch(0, 0);
 
-    const int task = warp % tasks, sub = warp / tasks, head = task % P.heads, block = first_block + task / P.heads;
-    const bool works = head < n_heads && block * ROWS < P.n_rows;      // else the ring still goes round
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
     float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
@@ -298,11 +348,14 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     constexpr uint32_t EIGHT = 8 * BOX;
     const int box_s = 2 * P.boxes_k;
     const uint32_t at_k = place(0, head * (D / 2) + t * NG * 4, k0), at_ks = place(box_s, head * (D / 4), k0);
-    const uint32_t at_va = place(P.boxes_k, head * (D / 2) + row * NG * 2, kva), at_vb = place(P.boxes_k, head * (D / 2) + row * NG * 2, kvb);
     const uint32_t at_vsa = place(box_s, head * (D / 4) + 4 * NG, kva), at_vsb = place(box_s, head * (D / 4) + 4 * NG, kvb);
     // steps and lows as matrices, eight numbers of a token a row
     const int km = key_of_row(lane & 7);
     const uint32_t at_mk = place(box_s, head * (D / 4), km) + ((lane >> 3) & 1) * EIGHT;
+    // value codes likewise: a group's 16 bytes of a token a row; lanes 0-15 give the rows of the even group of a pair, lanes 16-31 of the odd
+    uint32_t at_v[NG / 2];
+#pragma unroll
+    for (int g = 0; g < NG; g += 2) at_v[g / 2] = place(P.boxes_k, head * (D / 2) + (g + (lane >> 4)) * 16, km) + ((lane >> 3) & 1) * EIGHT;
     const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + ((lane >> 3) & 1) * EIGHT;
     const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;
     bool alive = true;
@@ -310,12 +363,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     for (int seg = 0; seg < 2; ++seg) {
         const int seg_begin = seg ? begin1 : begin0, seg_end = seg ? end1 : end0;
         if (seg_begin == seg_end) continue;
-        char *queries = smem + P.queries_at;
-        take_queries<D, F32>(P, rope, queries, first_head, n_heads, first_block, seg ? P.shift[1] : P.shift[0]);
-        if (at == 0)                   // the ring's other stages: behind the queries, whose few loads would wait behind them
-            for (int tile = 1 + warp; tile < min(P.stages, n_tiles); tile += n_warps) fetch(tile, tile);
+        char *queries = smem + P.queries_at + task * query_bytes(D);
+        const bool starts = at == 0;
+        take_queries<D, F32>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, seg ? P.shift[1] : P.shift[0],
+                             [&] { if (starts && warp == 0) fetch(0, 0); },
+                             [&] { if (starts) for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) if (tile > 0) fetch(tile, tile); });
         uint32_t q_hi[2 * NG][2], q_lo[2 * NG][2], q_sum[2];
-        const uint32_t my_q = pc_smem_u32(queries) + task * query_bytes(D) + lane * 4;
+        const uint32_t my_q = pc_smem_u32(queries) + lane * 4;
 #pragma unroll
         for (int i = 0; i < 4 * NG; ++i) {
             q_hi[i / 2][i & 1] = lds32(my_q + i * 128);
@@ -323,7 +377,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         }
         q_sum[0] = lds32(my_q + 8 * NG * 128);
         q_sum[1] = lds32(my_q + (8 * NG + 1) * 128);
-        const float *factor = reinterpret_cast<const float *>(queries + task * query_bytes(D) + query_words(D) * 128);
+        const float *factor = reinterpret_cast<const float *>(queries + query_words(D) * 128);
         const float f0 = factor[2 * t], f1 = factor[2 * t + 1];
         const uint8_t *valid = seg == 1 ? P.valid : nullptr;
         float *logits = seg == 1 ? P.logits : nullptr;
@@ -391,12 +445,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         };
         // O += P V of a step, p = the probabilities of S's keys and columns
         const auto add_values = [&](uint32_t rows, const float (&p)[4], bool all, uint32_t seen) {
-            uint32_t steps[4][NG / 2], codes[4][NG / 2], ua, ub;
+            uint32_t steps[4][NG / 2], ca[NG], cb[NG], ua, ub;         // codes: a group's four of each key, of two keys a word
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                lds(rows + (j & 1 ? at_vb : at_va) + (j >> 1) * EIGHT, codes[j]);
-                lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
-            }
+            for (int j = 0; j < 4; ++j) lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
+#pragma unroll
+            for (int g = 0; g < NG; g += 2) load_codes(rows + at_v[g / 2], ca[g], cb[g], ca[g + 1], cb[g + 1]);
             load_matrices<true>(rows + at_mv, ua, ub);
             if (!all) {                              // what lies in the place of a masked key may be anything
 #pragma unroll
@@ -422,7 +475,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
-                const uint32_t ta = __byte_perm(codes[0][g / 2], codes[1][g / 2], pick), tb = __byte_perm(codes[2][g / 2], codes[3][g / 2], pick);
+                const uint32_t ta = ca[g], tb = cb[g];
                 const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
                 const uint32_t ya = ta >> 8, yb = tb >> 8;
                 const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
@@ -536,25 +589,27 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         }
     }
     __syncthreads();
-    const int rows_all = P.n_kv * P.n_rows, count = min(P.n_rows - first_block * ROWS, P.blocks * ROWS);
-    for (int e = threadIdx.x; e < n_heads * count * (D / 4); e += blockDim.x) {
-        const int c = e % (D / 4), i = e / (D / 4), h = i / count, in_head = first_block * ROWS + i % count;
-        const int k = i % count / ROWS * P.heads + h, r = i % count % ROWS;
+    if (!works) return;
+    // the warps of a task take its rows in turn
+    const int rows_all = P.n_kv * P.n_rows, count = min(P.n_rows - block * ROWS, ROWS), step = P.subs * (32 / (D / 4));
+    for (int r = sub * (32 / (D / 4)) + lane / (D / 4); r < count; r += step) {
+        const int c = lane % (D / 4);
         float M = NO_MAX, l = 0.f;
-        for (int b = 0; b < P.subs; ++b) M = fmaxf(M, ms[(b * tasks + k) * ROWS + r]);
+        for (int b = 0; b < P.subs; ++b) M = fmaxf(M, ms[(b * tasks + task) * ROWS + r]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int b = 0; b < P.subs; ++b) {
-            const float f = exp2_fast(ms[(b * tasks + k) * ROWS + r] - M);
-            const float4 x = *reinterpret_cast<const float4 *>(parts + ((b * tasks + k) * ROWS + r) * PITCH + 4 * c);
-            l = fmaf(f, ls[(b * tasks + k) * ROWS + r], l);
+            const int at = (b * tasks + task) * ROWS + r;
+            const float f = exp2_fast(ms[at] - M);
+            const float4 x = *reinterpret_cast<const float4 *>(parts + at * PITCH + 4 * c);
+            l = fmaf(f, ls[at], l);
             o.x = fmaf(f, x.x, o.x);
             o.y = fmaf(f, x.y, o.y);
             o.z = fmaf(f, x.z, o.z);
             o.w = fmaf(f, x.w, o.w);
         }
-        const size_t at = (size_t)blockIdx.x * rows_all + (size_t)(first_head + h) * P.n_rows + in_head;
-        reinterpret_cast<float4 *>(P.part_o)[at * (D / 4) + c] = o;
-        if (c == 0) reinterpret_cast<float2 *>(P.part_ml)[at] = make_float2(M, l);
+        const size_t to = (size_t)blockIdx.x * rows_all + (size_t)(first_head + head) * P.n_rows + block * ROWS + r;
+        reinterpret_cast<float4 *>(P.part_o)[to * (D / 4) + c] = o;
+        if (c == 0) reinterpret_cast<float2 *>(P.part_ml)[to] = make_float2(M, l);
     }
 }
 
@@ -698,10 +753,13 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     const int head_sets = div_up(P.n_kv, 8);
     P.heads = div_up(P.n_kv, head_sets);
     const int n_blocks = div_up(P.n_rows, ROWS);
-    P.block_groups = div_up(n_blocks, MAX_WARPS / P.heads);
-    P.blocks = div_up(n_blocks, P.block_groups);
+    const int block_groups = div_up(n_blocks, MAX_WARPS / P.heads);
+    P.blocks = div_up(n_blocks, block_groups);
+    P.inv_tasks = 65536u / (P.heads * P.blocks) + 1;
+    P.inv_heads = 65536u / P.heads + 1;
+    P.inv_group = 1.f / (float)P.group;
     P.steps0 = div_up(P.n[0], Q4_STEP);
-    P.steps = P.steps0 + div_up(P.n[1], Q4_STEP);
+    const int steps = P.steps0 + div_up(P.n[1], Q4_STEP);
     P.boxes_k = div_up(P.heads * D.head_dim / 2, BOX);
     P.boxes = 2 * P.boxes_k + div_up(P.heads * D.head_dim / 4, BOX);
     P.unit_bytes = P.boxes * BOX_BYTES;
@@ -719,16 +777,18 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.part_ml = w->part_ml;
     P.logits = weigh && P.n[1] > 0 ? w->logits : nullptr;
     // parts of the keys: the count with which the CTAs' waves over the SMs take the fewest steps in all
-    const int rows = P.n_kv * P.n_rows, ctas = head_sets * P.block_groups;
-    const int most = (int)std::min<long long>({(long long)div_up(P.steps, P.subs), (long long)(w->part_rows / rows), (long long)std::max(1, 2 * ctx->sm_count / ctas)});
+    const int rows = P.n_kv * P.n_rows, ctas = head_sets * block_groups;
+    const int most = (int)std::min<long long>({(long long)div_up(steps, P.subs), (long long)(w->part_rows / rows), (long long)std::max(1, 2 * ctx->sm_count / ctas)});
     int splits = 1;
     long long best = -1;
     for (int s = 1; s <= most; ++s) {
-        const long long cost = (long long)div_up(ctas * s, ctx->sm_count) * (div_up(div_up(P.steps, s), P.subs) + 2);
+        const long long cost = (long long)div_up(ctas * s, ctx->sm_count) * (div_up(div_up(steps, s), P.subs) + 2);
         if (best < 0 || cost < best) { best = cost; splits = s; }
     }
+    P.steps_cta = steps / splits;
+    P.steps_more = steps % splits;
     const bool f32 = D.dtype == PC_F32;
-    const dim3 grid(splits, ctas), block(n_warps * 32);
+    const dim3 grid(splits, block_groups, head_sets), block(n_warps * 32);
     static bool attr_set[PC_MAX_DEVICES] = {};
     if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
     if (!attr_set[ctx->device]) {

@@ -49,7 +49,7 @@ def decode(rows, d):
         if kv == 0:
             codes = nib.reshape(n, hkv, 4, ng, 8).transpose(0, 1, 3, 2, 4)                    # word (t, g) = channels 32 g + 8 t ..
         else:
-            codes = nib.reshape(n, hkv, 8, ng, 4).transpose(0, 1, 3, 2, 4)                    # half (n, g) = channels 32 g + 4 n ..
+            codes = nib                                                                       # channel by channel
         out.append((codes.reshape(n, hkv, d).astype(np.float64), sl[:, :, 2 * kv], sl[:, :, 2 * kv + 1]))
     return out
 
