@@ -33,8 +33,8 @@ namespace {
 
 constexpr int ROWS = 8;                // query rows of a warp
 constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
-constexpr int MAX_STAGES = 8;
-constexpr int BAR_BYTES = 256;         // barriers and flags
+constexpr int MAX_SLOTS = 16;
+constexpr int RING_AT = 1024;          // barriers and flags before the ring
 constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
 constexpr int UNIT = 2, UNIT_KEYS = UNIT * Q4_STEP;        // steps that a warp takes together
 constexpr int BOX = 128, BOX_BYTES = UNIT_KEYS * BOX;      // a box of the rows: a unit's tokens x 128 bytes
@@ -43,8 +43,9 @@ constexpr float P_LOG = 2.f;
 constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, so that a masked logit (-infinity) gives probability 0
 
 // Queries as the B operand in shared memory, of a task (KV head, block of 8 rows): words [hi and lo parts 8 NG][sums 2] of 32 lanes, then 8 factors
-constexpr int query_words(int d) { return 8 * (d / Q4_GROUP) + 2; }
-constexpr int query_bytes(int d) { return query_words(d) * 128 + ROWS * 4; }
+// Of up to four rows (a single token of grouped heads) the lo parts are columns of their own, 4 to 7, and one pass multiplies both ("folded").
+constexpr int query_words(int d, bool folded) { return folded ? 4 * (d / Q4_GROUP) + 1 : 8 * (d / Q4_GROUP) + 2; }
+constexpr int query_bytes(int d, bool folded) { return query_words(d, folded) * 128 + ROWS * 4; }
 
 struct Q4Params {
     int n[2], shift[2];                // tokens of anchors, history; what their keys are shifted by
@@ -55,11 +56,11 @@ struct Q4Params {
     int heads, blocks, subs;           // of a CTA: KV heads, blocks of 8 query rows, parts of the keys
     uint32_t inv_tasks, inv_heads;     // 65536 / (heads * blocks) + 1, 65536 / heads + 1: a warp's number (below 16) is divided by multiplying
     float inv_group;
-    int steps0;                        // steps of 16 keys of the anchors
-    int steps_cta, steps_more;         // steps of a CTA, and how many CTAs take one more
+    int ctas0;                         // CTAs that take the anchors; the others take the history
+    int steps[2], more[2];             // of 16 keys: of a CTA of either kind, and how many of these take one more
     int boxes_k, boxes;                // boxes of a unit: of the key codes (as many for the values), all
-    int unit_bytes, stages;            // of the ring; a stage holds a unit for each of `subs`
-    int ring_at, queries_at;           // places in shared memory
+    int unit_bytes, slots;             // of the ring, which holds `slots` units
+    int query_slots;                   // last slots of the ring, in which the queries are made
     float *part_o, *part_ml;           // [split][KV head * n_rows + row]
     float *logits;                     // [history token][n_kv * n_rows] or NULL
     float scale;                       // log2(e) / sqrt(d)
@@ -124,7 +125,7 @@ __device__ __forceinline__ uint32_t place(int box0, int b, int key) {
     return (uint32_t)((box0 + (b >> 7)) * BOX_BYTES + key * BOX + ((((b >> 4) & 7) ^ key) << 4) + (b & 15));
 }
 
-__device__ __forceinline__ int4 ldg_int4(const int32_t *p) {        // in program order, ahead of the copies that are issued behind it
+__device__ __forceinline__ int4 ldg_int4(const int32_t *p) {
     int4 v;
     asm volatile("ld.global.nc.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
@@ -136,13 +137,10 @@ __device__ __forceinline__ float2 ldg_float2(const float2 *p) {
 }
 
 // The queries of a task, rotated at (t + shift, h, w), times log2(e) / sqrt(d), as the B operand of Q K^T in shared memory.  The warps of a task (one for
-// each part of the keys) take its rows in turn, D / 32 consecutive channels a lane; columns without a row are zero.  Positions and queries
-// of up to PER rows are requested first, then the first tile (between()), then the table entries that the positions name, then the
-// other tiles (behind()): these few loads, one behind the other, would take 7,500 cycles behind the whole ring's.
-template <int D, bool F32, typename Between, typename Behind>
-__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int kv_head, int block, int sub, int shift,
-                                             Between between, Behind behind) {
-    constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D), PER = 2;
+// each part of the keys) take its rows in turn, D / 32 consecutive channels a lane, two rows at a time; columns without a row are zero.
+template <int D, bool F32, bool FOLD>
+__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int kv_head, int block, int sub, int shift) {
+    constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D, FOLD), PER = 2;
     const int lane = threadIdx.x & 31;
     const int count = min(P.n_rows - block * ROWS, ROWS);            // none or fewer for a warp that has no head or no rows
     // channel 32 g + 8 t + k of a row: 16-bit half k / 4 of word (2 g + k % 2) * 2 + (k / 2) % 2 of lane 4 row + t.  The code words give
@@ -169,9 +167,7 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
             }
         }
         if (first) {
-            between();
-            __syncthreads();                       // the queries of the segment before are in registers
-            if ((lane >> 2) >= count) {
+            if ((FOLD ? (lane >> 2) & 3 : lane >> 2) >= count) {
                 for (int w = sub; w < WORDS; w += P.subs) reinterpret_cast<uint32_t *>(to)[w * 32 + lane] = 0u;
                 if ((lane & 3) == 0) reinterpret_cast<float *>(to + WORDS * 128)[lane >> 2] = 0.f;
             }
@@ -191,7 +187,6 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 cs[u][c] = ldg_float2(rope.tab + off + (size_t)min(max(at, 0), most - 1) * n);
             }
         }
-        if (first) behind();
         if (bad) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
@@ -220,24 +215,25 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 const int word = (2 * g + (c & 1)) * 2 + ((k >> 1) & 1);
                 __half *at16 = reinterpret_cast<__half *>(to + (word * 32 + col * 4 + t) * 4) + (k >> 2);
                 at16[0] = hi;
-                at16[4 * NG * 64] = __float2half_rn(y - __half2float(hi));
+                at16[FOLD ? 32 : 4 * NG * 64] = __float2half_rn(y - __half2float(hi));
             }
             // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps and
             // are zero), a second fp16 part at the same places of the other eight
 #pragma unroll
             for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            uint32_t *sums = reinterpret_cast<uint32_t *>(to) + 8 * NG * 32 + col * 4;
+            constexpr int SUMS = FOLD ? 4 * NG : 8 * NG, SECOND = FOLD ? 16 : 32;       // the second part: the column's other half, or the next word
+            uint32_t *sums = reinterpret_cast<uint32_t *>(to) + SUMS * 32 + col * 4;
             const float next = __shfl_down_sync(0xffffffffu, total, Q4_GROUP / CH);   // of the group behind
             if (lane < 4) {                        // a word of two groups a lane, zero where the steps are
                 sums[lane] = 0u;
-                sums[32 + lane] = 0u;
+                sums[SECOND + lane] = 0u;
             }
             __syncwarp();
             if (lane % (2 * Q4_GROUP / CH) == 0) {
                 const uint32_t h = pack_half(total, next);
                 const float2 back = halves(h);
                 sums[NG / 2 + g / 2] = h;
-                sums[32 + NG / 2 + g / 2] = pack_half(total - back.x, next - back.y);
+                sums[SECOND + NG / 2 + g / 2] = pack_half(total - back.x, next - back.y);
             }
             if (lane == 0) reinterpret_cast<float *>(to + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
         }
@@ -245,23 +241,23 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
     __syncthreads();
 }
 
-template <int D, bool F32>
+template <int D, bool F32, bool FOLD>
 __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_constant__ CUtensorMap map0, const __grid_constant__ CUtensorMap map1,
                                                                   const __grid_constant__ Q4Params P, const pc_rope_dev rope) {
     constexpr int NG = D / Q4_GROUP;
     extern __shared__ char smem_raw[];
     pc_grid_dep_launch();
-    const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + P.ring_at;
+    const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + RING_AT;
     char *smem = smem_raw + (base - pc_smem_u32(smem_raw));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 16 * MAX_STAGES);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 16 * MAX_SLOTS);
     const auto full = [&](int s) { return base + 8 * s; };
-    const auto empty = [&](int s) { return base + 8 * (MAX_STAGES + s); };
+    const auto empty = [&](int s) { return base + 8 * (MAX_SLOTS + s); };
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int tasks = P.heads * P.blocks, n_warps = tasks * P.subs;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < P.stages; ++s) {
+        for (int s = 0; s < P.slots; ++s) {
             pc_mbar_init(full(s), 1);
-            pc_mbar_init(empty(s), n_warps);
+            pc_mbar_init(empty(s), tasks);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -272,66 +268,38 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const int sub = (int)(warp * P.inv_tasks >> 16), task = warp - sub * tasks;
     const int head = task - (int)(task * P.inv_heads >> 16) * P.heads, block = first_block + (int)(task * P.inv_heads >> 16);
     const bool works = head < n_heads && block * ROWS < P.n_rows;      // else the ring still goes round
-    // This CTA's steps of the two segments; a tile is UNIT * subs steps of one segment
-    const int bx = (int)blockIdx.x, s0 = bx * P.steps_cta + min(bx, P.steps_more), s1 = s0 + P.steps_cta + (bx < P.steps_more ? 1 : 0);
-    const int begin0 = min(s0, P.steps0), end0 = min(s1, P.steps0), begin1 = max(s0 - P.steps0, 0), end1 = max(s1 - P.steps0, 0);
-    const int tile_steps = UNIT * P.subs;
-    const int tiles0 = (end0 - begin0 + tile_steps - 1) / tile_steps, n_tiles = tiles0 + (end1 - begin1 + tile_steps - 1) / tile_steps;
+    // This CTA's steps, of one segment.  A unit is two of them; the parts of the keys take the units in turn.
+    const bool hist = (int)blockIdx.x >= P.ctas0;
+    const int bx = (int)blockIdx.x - (hist ? P.ctas0 : 0), more = hist ? P.more[1] : P.more[0];
+    const int n_steps = (hist ? P.steps[1] : P.steps[0]) + (bx < more ? 1 : 0), step0 = bx * (hist ? P.steps[1] : P.steps[0]) + min(bx, more);
+    const int n_units = (n_steps + UNIT - 1) / UNIT, n_seg = hist ? P.n[1] : P.n[0];
     pc_grid_dep_wait();
 
-    // A tile into stage st, by one warp: boxes of the key codes, of the value codes, of the steps and lows.  One elected lane issues them (about 20
+    // A unit into a slot, by one warp: boxes of the key codes, of the value codes, of the steps and lows.  One elected lane issues them (about 20
     // cycles each; spread over the lanes of a warp they took 90).
     const bool lead = pc_tc::elect_one();
-    const auto fetch = [&](int tile, int st) {
-        const bool hist = tile >= tiles0;
-        const int first = hist ? begin1 + (tile - tiles0) * tile_steps : begin0 + tile * tile_steps;
-        const int units = (min(tile_steps, (hist ? end1 : end0) - first) + UNIT - 1) / UNIT;
-        const CUtensorMap *map = hist ? &map1 : &map0;
-        const uint32_t bar = full(st);
-        uint32_t dst = ring + st * P.subs * P.unit_bytes;
+    const auto fetch = [&](int unit, int slot) {
         if (lead) {
-            pc_mbar_expect_tx(bar, units * P.unit_bytes);
+            const CUtensorMap *map = hist ? &map1 : &map0;
+            const uint32_t bar = full(slot);
+            uint32_t dst = ring + slot * P.unit_bytes;
+            const int y = (step0 + unit * UNIT) * Q4_STEP;
+            int x = first_head * (D / 2);
+            pc_mbar_expect_tx(bar, P.unit_bytes);
 #pragma unroll 1
-            for (int u = 0; u < units; ++u) {
-                const int y = (first + u * UNIT) * Q4_STEP;
-                int x = first_head * (D / 2);
-#pragma unroll 1
-                for (int i = 0; i < P.boxes_k; ++i, x += BOX, dst += BOX_BYTES) {
-                    pc_tc::tma_load_2d(dst, map, x, y, bar);
-                    pc_tc::tma_load_2d(dst + P.boxes_k * BOX_BYTES, map, x + P.n_kv * (D / 2), y, bar);
-                }
-                dst += P.boxes_k * BOX_BYTES;
-                x = P.n_kv * D + first_head * (D / 4);
-#pragma unroll 1
-                for (int i = 2 * P.boxes_k; i < P.boxes; ++i, x += BOX, dst += BOX_BYTES) pc_tc::tma_load_2d(dst, map, x, y, bar);
+            for (int i = 0; i < P.boxes_k; ++i, x += BOX, dst += BOX_BYTES) {
+                pc_tc::tma_load_2d(dst, map, x, y, bar);
+                pc_tc::tma_load_2d(dst + P.boxes_k * BOX_BYTES, map, x + P.n_kv * (D / 2), y, bar);
             }
+            dst += P.boxes_k * BOX_BYTES;
+            x = P.n_kv * D + first_head * (D / 4);
+#pragma unroll 1
+            for (int i = 2 * P.boxes_k; i < P.boxes; ++i, x += BOX, dst += BOX_BYTES) pc_tc::tma_load_2d(dst, map, x, y, bar);
         }
         __syncwarp();
     };
-    // Where the warp is in the ring, and whose turn it is to refill: before a tile one of the warps fetches the tile that follows in
-    // the stage of the tile before it
-    int st = 0, at = 0, turn = 0;
-    uint32_t phase = 0;
-    const auto ready = [&]() {
-        if (at > 0 && at - 1 + P.stages < n_tiles) {
-            if (warp == turn) {
-                const int before = st == 0 ? P.stages - 1 : st - 1;
-                if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(before), st == 0 ? phase ^ 1u : phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) return false;
-                fetch(at - 1 + P.stages, before);
-            }
-            if (++turn == n_warps) turn = 0;
-        }
-        return __all_sync(0xffffffffu, pc_mbar_wait(full(st), phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us)) != 0;
-    };
-    const auto done = [&]() {
-        __syncwarp();
-        if (lane == 0) pc_mbar_arrive(empty(st));
-        ++at;
-        if (++st == P.stages) {
-            st = 0;
-            phase ^= 1u;
-        }
-    };
+    const int slots0 = P.slots - P.query_slots;
+    for (int u = warp; u < min(slots0, n_units); u += n_warps) fetch(u, u);
 
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
@@ -357,32 +325,27 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
 #pragma unroll
     for (int g = 0; g < NG; g += 2) at_v[g / 2] = place(P.boxes_k, head * (D / 2) + (g + (lane >> 4)) * 16, km) + ((lane >> 3) & 1) * EIGHT;
     const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + ((lane >> 3) & 1) * EIGHT;
-    const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;
-    bool alive = true;
-#pragma unroll 1
-    for (int seg = 0; seg < 2; ++seg) {
-        const int seg_begin = seg ? begin1 : begin0, seg_end = seg ? end1 : end0;
-        if (seg_begin == seg_end) continue;
-        char *queries = smem + P.queries_at + task * query_bytes(D);
-        const bool starts = at == 0;
-        take_queries<D, F32>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, seg ? P.shift[1] : P.shift[0],
-                             [&] { if (starts && warp == 0) fetch(0, 0); },
-                             [&] { if (starts) for (int tile = warp; tile < min(P.stages, n_tiles); tile += n_warps) if (tile > 0) fetch(tile, tile); });
-        uint32_t q_hi[2 * NG][2], q_lo[2 * NG][2], q_sum[2];
-        const uint32_t my_q = pc_smem_u32(queries) + lane * 4;
+    const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;        // folded: lanes of the lo parts (t > 1) have no row
+    char *queries = smem + RING_AT + slots0 * P.unit_bytes + task * query_bytes(D, FOLD);
+    take_queries<D, F32, FOLD>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, hist ? P.shift[1] : P.shift[0]);
+    uint32_t q_hi[2 * NG][2], q_lo[FOLD ? 1 : 2 * NG][2], q_sum[2];
+    const uint32_t my_q = pc_smem_u32(queries) + lane * 4;
 #pragma unroll
-        for (int i = 0; i < 4 * NG; ++i) {
-            q_hi[i / 2][i & 1] = lds32(my_q + i * 128);
-            q_lo[i / 2][i & 1] = lds32(my_q + (4 * NG + i) * 128);
-        }
-        q_sum[0] = lds32(my_q + 8 * NG * 128);
-        q_sum[1] = lds32(my_q + (8 * NG + 1) * 128);
-        const float *factor = reinterpret_cast<const float *>(queries + query_words(D) * 128);
-        const float f0 = factor[2 * t], f1 = factor[2 * t + 1];
-        const uint8_t *valid = seg == 1 ? P.valid : nullptr;
-        float *logits = seg == 1 ? P.logits : nullptr;
-        if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
-        const int n_seg = seg ? P.n[1] : P.n[0];
+    for (int i = 0; i < 4 * NG; ++i) {
+        q_hi[i / 2][i & 1] = lds32(my_q + i * 128);
+        if constexpr (!FOLD) q_lo[i / 2][i & 1] = lds32(my_q + (4 * NG + i) * 128);
+    }
+    q_sum[0] = lds32(my_q + (FOLD ? 4 : 8) * NG * 128);
+    q_sum[1] = FOLD ? 0u : lds32(my_q + (8 * NG + 1) * 128);
+    const float *factor = reinterpret_cast<const float *>(queries + query_words(D, FOLD) * 128);
+    const float f0 = factor[FOLD ? (2 * t) & 3 : 2 * t], f1 = factor[FOLD ? (2 * t + 1) & 3 : 2 * t + 1];
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the queries' slots are written by TMA from here on
+    __syncthreads();
+    for (int u = slots0 + warp; u < min(P.slots, n_units); u += n_warps) fetch(u, u);
+
+    const uint8_t *valid = hist ? P.valid : nullptr;
+    float *logits = hist ? P.logits : nullptr;
+    if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
         // Raw logits of a step's keys k0, k0 + 8 against columns 2 t, 2 t + 1: to be multiplied by f0, f1
         const auto logits_of = [&](uint32_t rows, float (&S)[4]) {
             uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la, lb;
@@ -398,12 +361,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    if (h == 0) mma_first(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g][0], q_lo[2 * g][1]);
-                    else mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_lo[2 * g + 1][0], q_lo[2 * g + 1][1]);
+                    const uint32_t a0 = wa[g] & mask, a1 = wb[g] & mask, a2 = (wa[g] >> 8) & mask, a3 = (wb[g] >> 8) & mask;
+                    if (h == 0) mma_first(C[g], a0, a1, a2, a3, q_hi[2 * g][0], q_hi[2 * g][1]);
+                    else mma(C[g], a0, a1, a2, a3, q_hi[2 * g + 1][0], q_hi[2 * g + 1][1]);
+                    if constexpr (!FOLD) mma(C[g], a0, a1, a2, a3, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
                 }
-#pragma unroll
-                for (int g = 0; g < NG; ++g)
-                    mma(C[g], wa[g] & mask, wb[g] & mask, (wa[g] >> 8) & mask, (wb[g] >> 8) & mask, q_hi[2 * g + h][0], q_hi[2 * g + h][1]);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) S[j] = E[j] * (1.f / 16777216.f);
@@ -415,6 +377,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 S[1] = fmaf(fa, C[g][1], S[1]);
                 S[2] = fmaf(fb, C[g][2], S[2]);
                 S[3] = fmaf(fb, C[g][3], S[3]);
+            }
+            if constexpr (FOLD) {                    // both halves of the columns get the sum
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[j] += __shfl_xor_sync(0xffffffffu, S[j], 2);
             }
         };
         // Keys of a step that are there and not masked: a bit per row of the instruction
@@ -498,16 +464,24 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 }
             }
         };
+    // The warp's units: every subs-th, in the ring's slots in turn.  Before a unit one of the warps that share it (they take turns) fetches
+    // what follows in the slot of the unit before it, once all of them have left that.
+    int slot = sub, before = 0, turn = 0;
+    uint32_t phase = 0, phase_before = 0;
 #pragma unroll 1
-        for (int tile_first = seg_begin; alive && tile_first < seg_end; tile_first += tile_steps) {
-            if (!ready()) {
-                alive = false;
-                break;
+    for (int unit = sub; unit < n_units; unit += P.subs) {
+            if (unit >= P.subs && unit - P.subs + P.slots < n_units) {
+                if (task == turn) {
+                    if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(before), phase_before, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) break;
+                    fetch(unit - P.subs + P.slots, before);
+                }
+                if (++turn == tasks) turn = 0;
             }
-            const int s = tile_first + UNIT * sub;
-            if (works && s < seg_end) {
-                const uint32_t rows = ring + (st * P.subs + sub) * P.unit_bytes, rows1 = rows + Q4_STEP * BOX;
-                const bool two = s + 1 < seg_end;
+            if (!__all_sync(0xffffffffu, pc_mbar_wait(full(slot), phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) break;
+            if (works) {
+                const int s = step0 + unit * UNIT;
+                const uint32_t rows = ring + slot * P.unit_bytes, rows1 = rows + Q4_STEP * BOX;
+                const bool two = unit * UNIT + 1 < n_steps;
                 float S0[4], S1[4];
                 logits_of(rows, S0);
                 if (two) logits_of(rows1, S1);
@@ -552,8 +526,15 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 add_values(rows, S0, all, seen0);
                 if (two) add_values(rows1, S1, all, seen1);
             }
-            done();
-        }
+            __syncwarp();
+            if (lane == 0) pc_mbar_arrive(empty(slot));
+            before = slot;
+            phase_before = phase;
+            slot += P.subs;
+            if (slot >= P.slots) {
+                slot -= P.slots;
+                phase ^= 1u;
+            }
     }
     __syncthreads();
     if (*abort_flag) {
@@ -563,7 +544,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
 
     // ---- the parts of the keys that the CTA's warps took, merged in shared memory (the ring is done with)
     constexpr int PITCH = D + 4;
-    float *parts = reinterpret_cast<float *>(smem + P.ring_at);      // [warp][8][PITCH], then [warp][8] maxima, sums
+    float *parts = reinterpret_cast<float *>(smem + RING_AT);      // [warp][8][PITCH], then [warp][8] maxima, sums
     float *ms = parts + n_warps * ROWS * PITCH, *ls = ms + n_warps * ROWS;
     {
 #pragma unroll
@@ -758,48 +739,59 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.inv_tasks = 65536u / (P.heads * P.blocks) + 1;
     P.inv_heads = 65536u / P.heads + 1;
     P.inv_group = 1.f / (float)P.group;
-    P.steps0 = div_up(P.n[0], Q4_STEP);
-    const int steps = P.steps0 + div_up(P.n[1], Q4_STEP);
     P.boxes_k = div_up(P.heads * D.head_dim / 2, BOX);
     P.boxes = 2 * P.boxes_k + div_up(P.heads * D.head_dim / 4, BOX);
     P.unit_bytes = P.boxes * BOX_BYTES;
-    P.queries_at = BAR_BYTES;
-    P.ring_at = div_up(BAR_BYTES + P.heads * P.blocks * query_bytes(D.head_dim), 1024) * 1024;
-    const int room = SMEM_MOST - 1024 - P.ring_at;
-    P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), room / (2 * P.unit_bytes));          // of one or two heads a unit holds more than it needs
+    P.slots = std::min(MAX_SLOTS, (SMEM_MOST - 1024 - RING_AT) / P.unit_bytes);
+    P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), P.slots / 2);              // of one or two heads a unit holds more than it needs
+    const bool fold = P.n_rows <= 4;
+    P.query_slots = div_up(P.heads * P.blocks * query_bytes(D.head_dim, fold), P.unit_bytes);
     const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
-    P.stages = std::min(MAX_STAGES, room / (P.subs * P.unit_bytes));
-    const size_t smem = 1024 + P.ring_at + std::max(P.stages * P.subs * P.unit_bytes, merge_bytes);
+    const size_t smem = 1024 + RING_AT + std::max(P.slots * P.unit_bytes, merge_bytes);
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
     P.part_o = w->part_o;
     P.part_ml = w->part_ml;
     P.logits = weigh && P.n[1] > 0 ? w->logits : nullptr;
-    // parts of the keys: the count with which the CTAs' waves over the SMs take the fewest steps in all
+    // Parts of the keys: with ctas * parts CTAs in up to four waves over the SMs, the count that ends first, a CTA's start and end taken as the time
+    // of eight steps.  Anchors and history have CTAs of their own, with the same number of steps, or fewer where they do not divide.
     const int rows = P.n_kv * P.n_rows, ctas = head_sets * block_groups;
-    const int most = (int)std::min<long long>({(long long)div_up(steps, P.subs), (long long)(w->part_rows / rows), (long long)std::max(1, 2 * ctx->sm_count / ctas)});
-    int splits = 1;
+    const int s0 = div_up(P.n[0], Q4_STEP), s1 = div_up(P.n[1], Q4_STEP), least = (s0 > 0) + (s1 > 0);
+    int splits = 0;
     long long best = -1;
-    for (int s = 1; s <= most; ++s) {
-        const long long cost = (long long)div_up(ctas * s, ctx->sm_count) * (div_up(div_up(steps, s), P.subs) + 2);
-        if (best < 0 || cost < best) { best = cost; splits = s; }
+    for (int wave = 1; wave <= 4; ++wave) {
+        const int want = std::max(least, std::min<int>(wave * ctx->sm_count / ctas, (int)(w->part_rows / rows)));
+        int per = std::max(P.subs, div_up(s0 + s1, want));
+        while (div_up(s0, per) + div_up(s1, per) > want) ++per;
+        const int n = div_up(s0, per) + div_up(s1, per);
+        const long long cost = (long long)div_up(ctas * n, ctx->sm_count) * (div_up(div_up(per, UNIT), P.subs) * UNIT + 8);
+        if (best >= 0 && cost >= best) continue;
+        best = cost;
+        splits = n;
+        P.ctas0 = div_up(s0, per);
     }
-    P.steps_cta = steps / splits;
-    P.steps_more = steps % splits;
+    for (int i = 0; i < 2; ++i) {
+        const int n = i ? splits - P.ctas0 : P.ctas0, s = i ? s1 : s0;
+        if (n == 0) continue;
+        P.steps[i] = s / n;
+        P.more[i] = s % n;
+    }
     const bool f32 = D.dtype == PC_F32;
     const dim3 grid(splits, block_groups, head_sets), block(n_warps * 32);
     static bool attr_set[PC_MAX_DEVICES] = {};
     if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
     if (!attr_set[ctx->device]) {
-        for (const auto kernel : {k_q4_attend<128, false>, k_q4_attend<128, true>, k_q4_attend<64, false>, k_q4_attend<64, true>})
-            PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+        for (const auto kernel : {k_q4_attend<128, false, false>, k_q4_attend<128, false, true>, k_q4_attend<128, true, false>, k_q4_attend<128, true, true>,
+                                  k_q4_attend<64, false, false>, k_q4_attend<64, false, true>, k_q4_attend<64, true, false>, k_q4_attend<64, true, true>})
+            PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST));
         attr_set[ctx->device] = true;
     }
-    if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_attend<128, true>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
-    else if (D.head_dim == 128) PC_LAUNCH((k_q4_attend<128, false>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
-    else if (f32) PC_LAUNCH((k_q4_attend<64, true>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
-    else PC_LAUNCH((k_q4_attend<64, false>), grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
+    const auto kernel = D.head_dim == 128 ? (f32 ? (fold ? k_q4_attend<128, true, true> : k_q4_attend<128, true, false>)
+                                                 : (fold ? k_q4_attend<128, false, true> : k_q4_attend<128, false, false>))
+                                          : (f32 ? (fold ? k_q4_attend<64, true, true> : k_q4_attend<64, true, false>)
+                                                 : (fold ? k_q4_attend<64, false, true> : k_q4_attend<64, false, false>));
+    PC_LAUNCH(kernel, grid, block, smem, stream, maps[0], maps[1], P, ctx->rope);
     JoinParams J{w->part_o, w->part_ml, splits, rows, P.n_rows, P.group, P.n_q_heads, out, lse, P.logits ? w->lse : nullptr};
     if (D.head_dim == 128 && f32) PC_LAUNCH((k_q4_join<128, true>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
     else if (D.head_dim == 128) PC_LAUNCH((k_q4_join<128, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
@@ -846,8 +838,8 @@ extern "C" pc_status pc_q4_create(pc_ctx *ctx, int32_t max_tokens, int32_t parts
     w->max_tokens = max_tokens;
     w->parts = parts;
     const pc_layer_desc &D = ctx->desc;
-    // every row of the largest call once, and what two CTAs an SM leave in any split
-    w->part_rows = std::max((size_t)D.max_q * D.n_q_heads, (size_t)2 * ctx->sm_count * MAX_WARPS * ROWS);
+    // every row of the largest call in two parts (anchors and history), and what two CTAs an SM leave in any split
+    w->part_rows = std::max((size_t)2 * D.max_q * D.n_q_heads, (size_t)2 * ctx->sm_count * MAX_WARPS * ROWS);
     const auto fill = [&]() -> pc_status {
         PC_CUDA_TRY(cudaMalloc(&w->part_o, w->part_rows * D.head_dim * sizeof(float)));
         PC_CUDA_TRY(cudaMalloc(&w->part_ml, w->part_rows * 2 * sizeof(float)));
