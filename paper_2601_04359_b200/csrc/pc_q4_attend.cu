@@ -138,8 +138,9 @@ __device__ __forceinline__ float2 ldg_float2(const float2 *p) {
 
 // The queries of a task, rotated at (t + shift, h, w), times log2(e) / sqrt(d), as the B operand of Q K^T in shared memory.  The warps of a task (one for
 // each part of the keys) take its rows in turn, D / 32 consecutive channels a lane, two rows at a time; columns without a row are zero.
-template <int D, bool F32, bool FOLD>
-__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int kv_head, int block, int sub, int shift) {
+// behind() is called once the first rows' table entries have been requested: what it fetches would hold up these loads, one behind the other.
+template <int D, bool F32, bool FOLD, typename Behind>
+__device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_dev &rope, char *to, int kv_head, int block, int sub, int shift, Behind behind) {
     constexpr int NG = D / Q4_GROUP, CH = D / 32, WORDS = query_words(D, FOLD), PER = 2;
     const int lane = threadIdx.x & 31;
     const int count = min(P.n_rows - block * ROWS, ROWS);            // none or fewer for a warp that has no head or no rows
@@ -187,6 +188,7 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 cs[u][c] = ldg_float2(rope.tab + off + (size_t)min(max(at, 0), most - 1) * n);
             }
         }
+        if (first) behind();
         if (bad) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
@@ -299,7 +301,6 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         __syncwarp();
     };
     const int slots0 = P.slots - P.query_slots;
-    for (int u = warp; u < min(slots0, n_units); u += n_warps) fetch(u, u);
 
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
@@ -327,7 +328,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + ((lane >> 3) & 1) * EIGHT;
     const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;        // folded: lanes of the lo parts (t > 1) have no row
     char *queries = smem + RING_AT + slots0 * P.unit_bytes + task * query_bytes(D, FOLD);
-    take_queries<D, F32, FOLD>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, hist ? P.shift[1] : P.shift[0]);
+    take_queries<D, F32, FOLD>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, hist ? P.shift[1] : P.shift[0], [&] {
+        for (int u = warp; u < min(slots0, n_units); u += n_warps) fetch(u, u);
+    });
     uint32_t q_hi[2 * NG][2], q_lo[FOLD ? 1 : 2 * NG][2], q_sum[2];
     const uint32_t my_q = pc_smem_u32(queries) + lane * 4;
 #pragma unroll
@@ -464,8 +467,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 }
             }
         };
-    // The warp's units: every subs-th, in the ring's slots in turn.  Before a unit one of the warps that share it (they take turns) fetches
-    // what follows in the slot of the unit before it, once all of them have left that.
+    // The warp's units: every subs-th, in the ring's slots in turn.  `slots` is a multiple of `subs`, so a slot only ever holds units of one part of
+    // the keys and its barriers are only waited on by warps that have seen every phase before (a wait by parity cannot tell a phase that
+    // is still to come from the one before it).  Before a unit one of the warps that share it (they take turns) fetches what follows in the slot of the
+    // unit before it, once all of them have left that.
     int slot = sub, before = 0, turn = 0;
     uint32_t phase = 0, phase_before = 0;
 #pragma unroll 1
@@ -744,10 +749,13 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.unit_bytes = P.boxes * BOX_BYTES;
     P.slots = std::min(MAX_SLOTS, (SMEM_MOST - 1024 - RING_AT) / P.unit_bytes);
     P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), P.slots / 2);              // of one or two heads a unit holds more than it needs
+    P.slots -= P.slots % P.subs;
     const bool fold = P.n_rows <= 4;
-    P.query_slots = div_up(P.heads * P.blocks * query_bytes(D.head_dim, fold), P.unit_bytes);
+    // queries: behind the ring if there is room, else in its last slots, which are filled when they have been read
+    const int query_area = P.heads * P.blocks * query_bytes(D.head_dim, fold), room = SMEM_MOST - 1024 - RING_AT - P.slots * P.unit_bytes;
+    P.query_slots = room >= query_area ? 0 : div_up(query_area, P.unit_bytes);
     const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
-    const size_t smem = 1024 + RING_AT + std::max(P.slots * P.unit_bytes, merge_bytes);
+    const size_t smem = 1024 + RING_AT + std::max(P.slots * P.unit_bytes + (P.query_slots ? 0 : query_area), merge_bytes);
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
