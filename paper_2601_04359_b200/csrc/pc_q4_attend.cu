@@ -10,7 +10,7 @@
 // Shape.  m16n8k16 instructions with 16 keys (channels, for the values) as rows and 8 query rows of one KV head as columns: a warp
 // takes one KV head and 8 query rows and goes through the keys 16 at a time; the warps of a CTA cover the KV heads (and several
 // blocks of rows, or several parts of the keys), so a CTA reads whole token rows.  TMA brings them, boxes of 32 tokens x 128 bytes with the 128-byte
-// swizzle, into a ring of tiles that the warps refill in turn.  CTAs split the keys evenly; k_q4_join merges their parts, k_q4_weigh
+// swizzle, into a ring of units of two steps that the warps refill in turn.  CTAs split the keys evenly; k_q4_join merges their parts, k_q4_weigh
 // turns the logits that the history left into weights.
 #include <algorithm>
 #include <new>
@@ -33,11 +33,11 @@ namespace {
 
 constexpr int ROWS = 8;                // query rows of a warp
 constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
-constexpr int MAX_SLOTS = 16;
+constexpr int MAX_SLOTS = 32;
 constexpr int RING_AT = 1024;          // barriers and flags before the ring
 constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
-constexpr int UNIT = 2, UNIT_KEYS = UNIT * Q4_STEP;        // steps that a warp takes together
-constexpr int BOX = 128, BOX_BYTES = UNIT_KEYS * BOX;      // a box of the rows: a unit's tokens x 128 bytes
+constexpr int UNIT = 2;                // steps that a warp takes together
+constexpr int BOX = 128, BOX_BYTES = UNIT * Q4_STEP * BOX; // a box of the rows: a unit's tokens x 128 bytes
 // Probabilities are scaled by 2^P_LOG (the sums with them, so that it cancels): times a step they stay below fp16's largest, 4 * 2 * 65504 / 15
 constexpr float P_LOG = 2.f;
 constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, so that a masked logit (-infinity) gives probability 0
@@ -60,7 +60,8 @@ struct Q4Params {
     int steps[2], more[2];             // of 16 keys: of a CTA of either kind, and how many of these take one more
     int boxes_k, boxes;                // boxes of a unit: of the key codes (as many for the values), all
     int unit_bytes, slots;             // of the ring, which holds `slots` units
-    int query_slots;                   // last slots of the ring, in which the queries are made
+    int whole_rows;                    // 1: a unit comes by one instruction
+    int queries_at;                    // behind the ring
     float *part_o, *part_ml;           // [split][KV head * n_rows + row]
     float *logits;                     // [history token][n_kv * n_rows] or NULL
     float scale;                       // log2(e) / sqrt(d)
@@ -90,13 +91,10 @@ __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// Two 8 x 8 matrices of 16-bit values, a row at the address of each of the first sixteen lanes; TRANS: transposed
-template <bool TRANS> __device__ __forceinline__ void load_matrices(uint32_t a, uint32_t &x, uint32_t &y) {
-    if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
-    else asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a));
-}
-__device__ __forceinline__ void load_codes(uint32_t a, uint32_t &x0, uint32_t &x1, uint32_t &x2, uint32_t &x3) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x0), "=r"(x1), "=r"(x2), "=r"(x3) : "r"(a));
+// Four 8 x 8 matrices of 16-bit values, a row at each lane's address (eight lanes a matrix); TRANS: transposed
+template <bool TRANS> __device__ __forceinline__ void load_matrices(uint32_t a, uint32_t (&x)[4]) {
+    if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(a));
+    else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(a));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {         // an 8 x 8 matrix of 16-bit values, two a lane
     uint32_t y;
@@ -251,15 +249,15 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     pc_grid_dep_launch();
     const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + RING_AT;
     char *smem = smem_raw + (base - pc_smem_u32(smem_raw));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 16 * MAX_SLOTS);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + 12 * MAX_SLOTS);
     const auto full = [&](int s) { return base + 8 * s; };
-    const auto empty = [&](int s) { return base + 8 * (MAX_SLOTS + s); };
+    const auto left = [&](int s) { return base + 8 * MAX_SLOTS + 4 * s; };        // warps that are done with the unit of a slot
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int tasks = P.heads * P.blocks, n_warps = tasks * P.subs;
     if (threadIdx.x == 0) {
         for (int s = 0; s < P.slots; ++s) {
             pc_mbar_init(full(s), 1);
-            pc_mbar_init(empty(s), tasks);
+            *reinterpret_cast<int *>(smem + 8 * MAX_SLOTS + 4 * s) = 0;
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -277,31 +275,35 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const int n_units = (n_steps + UNIT - 1) / UNIT, n_seg = hist ? P.n[1] : P.n[0];
     pc_grid_dep_wait();
 
-    // A unit into a slot, by one warp: boxes of the key codes, of the value codes, of the steps and lows.  One elected lane issues them (about 20
-    // cycles each; spread over the lanes of a warp they took 90).
+    // A unit into a slot, by one elected lane of a warp: all boxes by one instruction where a CTA takes whole rows of whole boxes, else box by box:
+    // of the key codes, of the value codes, of the steps and lows.  (A TMA instruction takes its warp 85 cycles: ten a unit held up the
+    // warp whose turn it was, and with it the ring.)
     const bool lead = pc_tc::elect_one();
+    const CUtensorMap *map = hist ? &map1 : &map0;
     const auto fetch = [&](int unit, int slot) {
         if (lead) {
-            const CUtensorMap *map = hist ? &map1 : &map0;
             const uint32_t bar = full(slot);
             uint32_t dst = ring + slot * P.unit_bytes;
             const int y = (step0 + unit * UNIT) * Q4_STEP;
-            int x = first_head * (D / 2);
             pc_mbar_expect_tx(bar, P.unit_bytes);
+            if (P.whole_rows) {
+                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                             ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(0), "r"(bar) : "memory");
+            } else {
+                int x = first_head * (D / 2);
 #pragma unroll 1
-            for (int i = 0; i < P.boxes_k; ++i, x += BOX, dst += BOX_BYTES) {
-                pc_tc::tma_load_2d(dst, map, x, y, bar);
-                pc_tc::tma_load_2d(dst + P.boxes_k * BOX_BYTES, map, x + P.n_kv * (D / 2), y, bar);
+                for (int i = 0; i < P.boxes_k; ++i, x += BOX, dst += BOX_BYTES) {
+                    pc_tc::tma_load_2d(dst, map, x, y, bar);
+                    pc_tc::tma_load_2d(dst + P.boxes_k * BOX_BYTES, map, x + P.n_kv * (D / 2), y, bar);
+                }
+                dst += P.boxes_k * BOX_BYTES;
+                x = P.n_kv * D + first_head * (D / 4);
+#pragma unroll 1
+                for (int i = 2 * P.boxes_k; i < P.boxes; ++i, x += BOX, dst += BOX_BYTES) pc_tc::tma_load_2d(dst, map, x, y, bar);
             }
-            dst += P.boxes_k * BOX_BYTES;
-            x = P.n_kv * D + first_head * (D / 4);
-#pragma unroll 1
-            for (int i = 2 * P.boxes_k; i < P.boxes; ++i, x += BOX, dst += BOX_BYTES) pc_tc::tma_load_2d(dst, map, x, y, bar);
         }
         __syncwarp();
     };
-    const int slots0 = P.slots - P.query_slots;
-
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
     float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
@@ -318,18 +320,19 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const int box_s = 2 * P.boxes_k;
     const uint32_t at_k = place(0, head * (D / 2) + t * NG * 4, k0), at_ks = place(box_s, head * (D / 4), k0);
     const uint32_t at_vsa = place(box_s, head * (D / 4) + 4 * NG, kva), at_vsb = place(box_s, head * (D / 4) + 4 * NG, kvb);
-    // steps and lows as matrices, eight numbers of a token a row
+    // steps and lows as matrices, eight numbers of a token a row, in the order of an A operand: of the key, tokens as rows (the second half of the
+    // instruction's index sees them again); of the value, transposed
     const int km = key_of_row(lane & 7);
     const uint32_t at_mk = place(box_s, head * (D / 4), km) + ((lane >> 3) & 1) * EIGHT;
     // value codes likewise: a group's 16 bytes of a token a row; lanes 0-15 give the rows of the even group of a pair, lanes 16-31 of the odd
     uint32_t at_v[NG / 2];
 #pragma unroll
     for (int g = 0; g < NG; g += 2) at_v[g / 2] = place(P.boxes_k, head * (D / 2) + (g + (lane >> 4)) * 16, km) + ((lane >> 3) & 1) * EIGHT;
-    const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + ((lane >> 3) & 1) * EIGHT;
+    const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + (lane >> 4) * EIGHT;
     const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;        // folded: lanes of the lo parts (t > 1) have no row
-    char *queries = smem + RING_AT + slots0 * P.unit_bytes + task * query_bytes(D, FOLD);
+    char *queries = smem + P.queries_at + task * query_bytes(D, FOLD);
     take_queries<D, F32, FOLD>(P, rope, queries, first_head + head, head < n_heads ? block : P.n_rows, sub, hist ? P.shift[1] : P.shift[0], [&] {
-        for (int u = warp; u < min(slots0, n_units); u += n_warps) fetch(u, u);
+        for (int u = warp; u < min(P.slots, n_units); u += n_warps) fetch(u, u);
     });
     uint32_t q_hi[2 * NG][2], q_lo[FOLD ? 1 : 2 * NG][2], q_sum[2];
     const uint32_t my_q = pc_smem_u32(queries) + lane * 4;
@@ -342,23 +345,19 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     q_sum[1] = FOLD ? 0u : lds32(my_q + (8 * NG + 1) * 128);
     const float *factor = reinterpret_cast<const float *>(queries + query_words(D, FOLD) * 128);
     const float f0 = factor[FOLD ? (2 * t) & 3 : 2 * t], f1 = factor[FOLD ? (2 * t + 1) & 3 : 2 * t + 1];
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the queries' slots are written by TMA from here on
-    __syncthreads();
-    for (int u = slots0 + warp; u < min(P.slots, n_units); u += n_warps) fetch(u, u);
-
     const uint8_t *valid = hist ? P.valid : nullptr;
     float *logits = hist ? P.logits : nullptr;
     if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
         // Raw logits of a step's keys k0, k0 + 8 against columns 2 t, 2 t + 1: to be multiplied by f0, f1
         const auto logits_of = [&](uint32_t rows, float (&S)[4]) {
-            uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la, lb;
+            uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la[4];
             lds(rows + at_k, wa);
             lds(rows + at_k + EIGHT, wb);
             lds(rows + at_ks, sa);
             lds(rows + at_ks + EIGHT, sb);
-            load_matrices<false>(rows + at_mk, la, lb);
+            load_matrices<false>(rows + at_mk, la);
             float E[4], C[NG][4];
-            mma_first(E, la, lb, la, lb, q_sum[0], q_sum[1]);
+            mma_first(E, la[0], la[1], la[2], la[3], q_sum[0], q_sum[1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {            // channels in the low four bits of the code words' bytes, then in the high four
                 const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
@@ -387,8 +386,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             }
         };
         // Keys of a step that are there and not masked: a bit per row of the instruction
-        const auto look_at_mask = [&](int first, float (&S)[4]) {
-            const int n = n_seg - first;
+        const auto look_at_mask = [&](int first, float (&S)[4], bool there) {
+            const int n = there ? n_seg - first : 0;
             bool ok0 = k0 < n, ok1 = k0 + 8 < n;
             if (valid) {
                 if (ok0) ok0 = __ldg(valid + first + k0) != 0;
@@ -414,17 +413,18 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         };
         // O += P V of a step, p = the probabilities of S's keys and columns
         const auto add_values = [&](uint32_t rows, const float (&p)[4], bool all, uint32_t seen) {
-            uint32_t steps[4][NG / 2], ca[NG], cb[NG], ua, ub;         // codes: a group's four of each key, of two keys a word
+            uint32_t steps[4][NG / 2], codes[NG / 2][4], lows[4];        // codes: a group's four of each key, of two keys a word
 #pragma unroll
             for (int j = 0; j < 4; ++j) lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
 #pragma unroll
-            for (int g = 0; g < NG; g += 2) load_codes(rows + at_v[g / 2], ca[g], cb[g], ca[g + 1], cb[g + 1]);
-            load_matrices<true>(rows + at_mv, ua, ub);
+            for (int g = 0; g < NG / 2; ++g) load_matrices<true>(rows + at_v[g], codes[g]);
+            load_matrices<true>(rows + at_mv, lows);
             if (!all) {                              // what lies in the place of a masked key may be anything
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (!((seen >> (4 * (2 * t + (j & 1)) + (j >> 1))) & 1u)) {
-                        (j < 2 ? ua : ub) &= (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                        lows[j & 2] &= (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                        lows[(j & 2) + 1] = lows[j & 2];
 #pragma unroll
                         for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
                     }
@@ -439,12 +439,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             }
             ph[0] = transpose8(ph[0]);
             ph[1] = transpose8(ph[1]);
-            mma(L, ua, 0u, ub, 0u, ph[0], ph[1]);
-            if constexpr (F32) mma(L, ua, 0u, ub, 0u, pl[0], pl[1]);
+            mma(L, lows[0], lows[1], lows[2], lows[3], ph[0], ph[1]);
+            if constexpr (F32) mma(L, lows[0], lows[1], lows[2], lows[3], pl[0], pl[1]);
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
-                const uint32_t ta = ca[g], tb = cb[g];
+                const uint32_t ta = codes[g / 2][2 * (g & 1)], tb = codes[g / 2][2 * (g & 1) + 1];
                 const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
                 const uint32_t ya = ta >> 8, yb = tb >> 8;
                 const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
@@ -467,39 +467,37 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 }
             }
         };
-    // The warp's units: every subs-th, in the ring's slots in turn.  `slots` is a multiple of `subs`, so a slot only ever holds units of one part of
-    // the keys and its barriers are only waited on by warps that have seen every phase before (a wait by parity cannot tell a phase that
-    // is still to come from the one before it).  Before a unit one of the warps that share it (they take turns) fetches what follows in the slot of the
-    // unit before it, once all of them have left that.
-    int slot = sub, before = 0, turn = 0;
-    uint32_t phase = 0, phase_before = 0;
+    // The warp's units: every subs-th, in the slots of its part of the keys (sub, sub + subs, ...) in turn.  `slots` is a multiple of `subs`, so
+    // the barriers of a slot are only waited on by warps that have seen every phase before (a wait by parity cannot tell a phase from the one
+    // two before or behind it).  The last of the warps that share a unit to leave it fetches what follows in its slot.
+    const auto wait_for = [&](uint32_t bar, uint32_t parity) {
+        return __all_sync(0xffffffffu, pc_mbar_wait(bar, parity, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us)) != 0;
+    };
+    int slot = sub;
+    uint32_t phase = 0;
 #pragma unroll 1
     for (int unit = sub; unit < n_units; unit += P.subs) {
-            if (unit >= P.subs && unit - P.subs + P.slots < n_units) {
-                if (task == turn) {
-                    if (!__all_sync(0xffffffffu, pc_mbar_wait(empty(before), phase_before, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) break;
-                    fetch(unit - P.subs + P.slots, before);
-                }
-                if (++turn == tasks) turn = 0;
-            }
-            if (!__all_sync(0xffffffffu, pc_mbar_wait(full(slot), phase, abort_flag, P.status, PC_WHERE_Q4_WAIT, P.wait_us))) break;
+        if (!wait_for(full(slot), phase)) break;
+            const uint32_t rows = ring + slot * P.unit_bytes;
+            const uint32_t rows1 = rows + Q4_STEP * BOX;
+            // (of one step: the second one's place holds tokens of the next CTA, or zeros; its logits count as masked)
+            const bool two = unit * UNIT + 1 < n_steps;
+            const int first = (step0 + unit * UNIT) * Q4_STEP;
+            float S0[4], S1[4];
             if (works) {
-                const int s = step0 + unit * UNIT;
-                const uint32_t rows = ring + slot * P.unit_bytes, rows1 = rows + Q4_STEP * BOX;
-                const bool two = unit * UNIT + 1 < n_steps;
-                float S0[4], S1[4];
                 logits_of(rows, S0);
-                if (two) logits_of(rows1, S1);
-                else S1[0] = S1[1] = S1[2] = S1[3] = -INFINITY;
+                logits_of(rows1, S1);
+            }
+            if (works) {
                 uint32_t seen0 = 0xffffffffu, seen1 = 0xffffffffu;
-                const bool all = !valid && (s + UNIT) * Q4_STEP <= n_seg;
+                const bool all = !valid && two && first + UNIT * Q4_STEP <= n_seg;
                 if (!all) {
-                    seen0 = look_at_mask(s * Q4_STEP, S0);
-                    if (two) seen1 = look_at_mask((s + 1) * Q4_STEP, S1);
+                    seen0 = look_at_mask(first, S0, true);
+                    seen1 = look_at_mask(first + Q4_STEP, S1, two);
                 }
                 if (logits) {
-                    leave_logits(s * Q4_STEP, S0);
-                    if (two) leave_logits((s + 1) * Q4_STEP, S1);
+                    leave_logits(first, S0);
+                    if (two) leave_logits(first + Q4_STEP, S1);
                 }
                 // ---- softmax: maximum of the keys of each column
                 float x0 = fmaxf(fmaxf(S0[0], S0[2]), fmaxf(S1[0], S1[2])), x1 = fmaxf(fmaxf(S0[1], S0[3]), fmaxf(S1[1], S1[3]));
@@ -529,17 +527,22 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 l0 += (S0[0] + S0[2]) + (S1[0] + S1[2]);
                 l1 += (S0[1] + S0[3]) + (S1[1] + S1[3]);
                 add_values(rows, S0, all, seen0);
-                if (two) add_values(rows1, S1, all, seen1);
+                add_values(rows1, S1, all, seen1);
             }
+        __syncwarp();
+        int n = 0;
+        if (lane == 0) asm volatile("atom.shared.acq_rel.cta.add.u32 %0, [%1], 1;" : "=r"(n) : "r"(left(slot)) : "memory");
+        n = __shfl_sync(0xffffffffu, n, 0);
+        if (n == tasks - 1 && unit + P.slots < n_units) {
+            if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(left(slot)), "r"(0) : "memory");
             __syncwarp();
-            if (lane == 0) pc_mbar_arrive(empty(slot));
-            before = slot;
-            phase_before = phase;
-            slot += P.subs;
-            if (slot >= P.slots) {
-                slot -= P.slots;
-                phase ^= 1u;
-            }
+            fetch(unit + P.slots, slot);
+        }
+        slot += P.subs;
+        if (slot >= P.slots) {
+            slot = sub;
+            phase ^= 1u;
+        }
     }
     __syncthreads();
     if (*abort_flag) {
@@ -699,13 +702,14 @@ __global__ void __launch_bounds__(256) k_accumulate(const float *__restrict__ ma
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// Rows as bytes, boxes of 32 tokens x 128 bytes; what lies outside reads as zero
-bool make_row_map(CUtensorMap *m, const void *rows, uint64_t n, uint64_t row_bytes) {
+// Rows as bytes, boxes of 32 tokens x 128 bytes; what lies outside reads as zero.  whole: as [128-byte piece][token][128] with all pieces of 32 tokens as
+// one box.
+bool make_row_map(CUtensorMap *m, const void *rows, uint64_t n, uint64_t row_bytes, bool whole) {
     const pc_tc::EncodeTiledFn fn = pc_tc::encode_fn();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {row_bytes, n}, strides[1] = {row_bytes};
-    const cuuint32_t box[2] = {BOX, UNIT_KEYS}, estr[2] = {1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(rows), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const cuuint64_t dims[3] = {whole ? BOX : row_bytes, n, row_bytes / BOX}, strides[2] = {row_bytes, BOX};
+    const cuuint32_t box[3] = {BOX, UNIT * Q4_STEP, (cuuint32_t)(row_bytes / BOX)}, estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, whole ? 3 : 2, const_cast<void *>(rows), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -717,11 +721,13 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     Q4Params P{};
     const pc_q4_segment *segs[2] = {&cache->anchors, &cache->history};
     CUtensorMap maps[2];
+    // one set of heads, and sections of whole boxes (4 or 8 KV heads of 128 channels, 8 of 64)
+    P.whole_rows = D.n_kv_heads <= 8 && D.n_kv_heads * D.head_dim / 4 % BOX == 0;
     for (int i = 0; i < 2; ++i) {
         P.n[i] = segs[i]->n_tokens;
         P.shift[i] = segs[i]->t_shift;
         const pc_q4_segment *s = P.n[i] > 0 ? segs[i] : segs[1 - i];          // an empty segment is never asked for
-        if (!make_row_map(&maps[i], s->rows, (uint64_t)s->n_tokens, q4_row(D))) {
+        if (!make_row_map(&maps[i], s->rows, (uint64_t)s->n_tokens, q4_row(D), P.whole_rows)) {
             fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
             return PC_ERR_CUDA;
         }
@@ -747,15 +753,14 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.boxes_k = div_up(P.heads * D.head_dim / 2, BOX);
     P.boxes = 2 * P.boxes_k + div_up(P.heads * D.head_dim / 4, BOX);
     P.unit_bytes = P.boxes * BOX_BYTES;
-    P.slots = std::min(MAX_SLOTS, (SMEM_MOST - 1024 - RING_AT) / P.unit_bytes);
-    P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), P.slots / 2);              // of one or two heads a unit holds more than it needs
-    P.slots -= P.slots % P.subs;
     const bool fold = P.n_rows <= 4;
-    // queries: behind the ring if there is room, else in its last slots, which are filled when they have been read
-    const int query_area = P.heads * P.blocks * query_bytes(D.head_dim, fold), room = SMEM_MOST - 1024 - RING_AT - P.slots * P.unit_bytes;
-    P.query_slots = room >= query_area ? 0 : div_up(query_area, P.unit_bytes);
+    const int query_area = P.heads * P.blocks * query_bytes(D.head_dim, fold);
+    P.slots = std::min(MAX_SLOTS, (SMEM_MOST - 1024 - RING_AT - query_area) / P.unit_bytes);         // three of 40 KB at least
+    P.subs = std::min(MAX_WARPS / (P.heads * P.blocks), P.slots / 2);
+    P.slots -= P.slots % P.subs;
+    P.queries_at = RING_AT + P.slots * P.unit_bytes;
     const int n_warps = P.heads * P.blocks * P.subs, merge_bytes = n_warps * ROWS * (D.head_dim + 4 + 2) * (int)sizeof(float);
-    const size_t smem = 1024 + RING_AT + std::max(P.slots * P.unit_bytes + (P.query_slots ? 0 : query_area), merge_bytes);
+    const size_t smem = 1024 + std::max(P.queries_at + query_area, RING_AT + merge_bytes);
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
@@ -773,7 +778,7 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
         int per = std::max(P.subs, div_up(s0 + s1, want));
         while (div_up(s0, per) + div_up(s1, per) > want) ++per;
         const int n = div_up(s0, per) + div_up(s1, per);
-        const long long cost = (long long)div_up(ctas * n, ctx->sm_count) * (div_up(div_up(per, UNIT), P.subs) * UNIT + 8);
+        const long long cost = (long long)div_up(ctas * n, ctx->sm_count) * (div_up(per, P.subs * UNIT) * UNIT + 8);
         if (best >= 0 && cost >= best) continue;
         best = cost;
         splits = n;
