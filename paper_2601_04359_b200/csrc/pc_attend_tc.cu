@@ -66,9 +66,12 @@ constexpr int SM_BAR = SM_V + KV_STAGES * TILE_BYTES;     // barriers etc.
 constexpr int SM_ML = SM_BAR + 256;                       // (max, sum) of both tiles' rows for the cluster merge: 2 KB
 constexpr int SM_TOTAL = SM_ML + 2 * TILE * 8;
 constexpr int SM_ALLOC = SM_TOTAL + 1024;                 // slack for manual alignment
+// the same with queries in two fp16 parts: both parts of 2 query tiles, one K tile, KV_STAGES V tiles, barriers
+constexpr int FINE_K = SM_Q + 4 * TILE_BYTES, FINE_V = FINE_K + TILE_BYTES, FINE_BAR = FINE_V + KV_STAGES * TILE_BYTES, FINE_ALLOC = FINE_BAR + 256 + 1024;
 
 enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_VFULL = 4 /* [stage] */, BAR_EMPTY = 6 /* [step & 1] */, BAR_SFULL = 8 /* [tile] */,
-       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, BAR_PART = 19, N_BARS = 20 };
+       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, BAR_PART = 19, N_BARS = 20,
+       BAR_KFULL = BAR_PART /* of the form with queries in two parts, which merges nothing */ };
 static_assert(N_BARS * 8 + 12 <= 256, "barriers, abort flag and TMEM address share 256 bytes");
 
 constexpr int SYNC_PARTS = 2, LEFT_PER_ITEM = 8;          // words of TcParams::sync
@@ -88,6 +91,7 @@ struct TcParams {
     int n_seg;
     int cluster;      // 1: the KV ranges of one item form a thread-block cluster and merge through shared memory
     uint32_t wait_us; // limit of every bounded wait in microseconds (0 = about one second)
+    int lo_row0;      // queries in two parts: first row of the second part in the query scratch
     uint32_t extra_tx; // test hook: bytes the first barrier expects beyond what is sent, so that its wait runs out (0 = off)
     int seg_tile_end[PC_MAX_SEGMENTS];
     int seg_n[PC_MAX_SEGMENTS];
@@ -258,19 +262,25 @@ __device__ __noinline__ void merge_left(const TcParams &P, uint32_t call, int w,
 
 // MERGE: items in two parts are merged by the CTA that has the first one.  A kernel of its own: with what that takes in its code, calls
 // that merge nothing took 0.3 us longer.
-template <bool MERGE>
+// FINE: queries, keys, values and probabilities in fp16 instead of bf16 and the queries in two parts, whose products with the keys add up in the same
+// columns (22 bits of a query, so that the lse is good to fp32's accuracy over thousands of keys).  The second part takes the place of the
+// second K stage: K(step + 1) is fetched once both tiles' Q K^T of the step have read K(step), under their softmax.
+template <bool MERGE, bool FINE = false>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
             const __grid_constant__ CUtensorMap map_v0, const __grid_constant__ CUtensorMap map_v1,
             const __grid_constant__ CUtensorMap map_v2, const __grid_constant__ TcParams P) {
+    static_assert(!(MERGE && FINE), "the form with queries in two parts leaves merges to the merge kernel");
+    constexpr int AT_K = FINE ? FINE_K : SM_K, AT_V = FINE ? FINE_V : SM_V, AT_BAR = FINE ? FINE_BAR : SM_BAR;
+    constexpr uint32_t QK = FINE ? IDESC_QK & IDESC_F16 : IDESC_QK, PV = FINE ? IDESC_PV & IDESC_F16 : IDESC_PV;
     pc_grid_dep_launch();
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + SM_BAR + N_BARS * 8);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + AT_BAR + N_BARS * 8);
     volatile int *left_here = abort_flag + 1;            // a warp of this CTA left a merge
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + SM_BAR + N_BARS * 8 + 8);
-    const uint32_t bar0 = base + SM_BAR;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + AT_BAR + N_BARS * 8 + 8);
+    const uint32_t bar0 = base + AT_BAR;
     auto bar = [&](int i) { return bar0 + 8u * i; };
 
     // from one lane, so that the compiler knows a warp's number, and with it barrier and tensor-memory addresses and descriptors, to be
@@ -294,7 +304,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             mbar_init(bar(BAR_PHALF + 2 * t + 1), 4);
         }
         mbar_init(bar(BAR_DONE), 3);
-        mbar_init(bar(BAR_PART), 8);
+        mbar_init(bar(BAR_PART), FINE ? 1 : 8);
         *abort_flag = 0;
         *left_here = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -343,11 +353,14 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     if (un > 0) alive = mbar_wait(bar(BAR_QFREE + t), (un - 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
                     if (!alive) break;
                     const bool first = un == 0 && t == 0;
-                    mbar_expect_tx(bar(BAR_Q + t), (first ? 2 : 1) * TILE_BYTES + (first ? P.extra_tx : 0u));
+                    mbar_expect_tx(bar(BAR_Q + t), (FINE || first ? 2 : 1) * TILE_BYTES + (first ? P.extra_tx : 0u));
                     const int T = 2 * pair + min(t, n_tiles_q - 1), tb = T / P.group, h = kvh * P.group + T % P.group;
                     tma_load_2d(base + SM_Q + t * TILE_BYTES, &map_q, h * TILE, tb * TILE, bar(BAR_Q + t));
                     tma_load_2d(base + SM_Q + t * TILE_BYTES + HALF_BYTES, &map_q, h * TILE + 64, tb * TILE, bar(BAR_Q + t));
-                    if (first) {
+                    if constexpr (FINE) {
+                        tma_load_2d(base + SM_Q + (2 + t) * TILE_BYTES, &map_q, h * TILE, P.lo_row0 + tb * TILE, bar(BAR_Q + t));
+                        tma_load_2d(base + SM_Q + (2 + t) * TILE_BYTES + HALF_BYTES, &map_q, h * TILE + 64, P.lo_row0 + tb * TILE, bar(BAR_Q + t));
+                    } else if (first) {
                         tma_load_2d(base + SM_K, &map_k, kvh * TILE, U.jb * TILE, bar(BAR_Q));
                         tma_load_2d(base + SM_K + HALF_BYTES, &map_k, kvh * TILE + 64, U.jb * TILE, bar(BAR_Q));
                     }
@@ -358,13 +371,21 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     int seg, local, n_valid;
                     kv_tile_info(P, U.jb + j, seg, local, n_valid);
                     const CUtensorMap *mv = seg == 0 ? &map_v0 : (seg == 1 ? &map_v1 : &map_v2);
+                    if constexpr (FINE) {
+                        for (int t = 0; t < 2 && alive && gs > 0; ++t)           // both Q K^T(step - 1) have read the one K tile
+                            alive = mbar_wait(bar(BAR_SFULL + t), (gs - 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
+                        if (!alive) break;
+                        mbar_expect_tx(bar(BAR_KFULL), TILE_BYTES);
+                        tma_load_2d(base + AT_K, &map_k, kvh * TILE, (U.jb + j) * TILE, bar(BAR_KFULL));
+                        tma_load_2d(base + AT_K + HALF_BYTES, &map_k, kvh * TILE + 64, (U.jb + j) * TILE, bar(BAR_KFULL));
+                    }
                     // PV(step - 2) and QK^T(step - 1) have read what lies where V(step) and K(step + 1) go
                     if (gs > 0) alive = mbar_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
                     if (!alive) break;
-                    const bool in_unit = j + 1 < U.n_j, more = in_unit || g < G1;
+                    const bool in_unit = j + 1 < U.n_j, more = !FINE && (in_unit || g < G1);
                     mbar_expect_tx(bar(BAR_VFULL + st), (more ? 2 : 1) * TILE_BYTES);
-                    tma_load_2d(base + SM_V + st * TILE_BYTES, mv, kvh * TILE, local * TILE, bar(BAR_VFULL + st));
-                    tma_load_2d(base + SM_V + st * TILE_BYTES + HALF_BYTES, mv, kvh * TILE + 64, local * TILE, bar(BAR_VFULL + st));
+                    tma_load_2d(base + AT_V + st * TILE_BYTES, mv, kvh * TILE, local * TILE, bar(BAR_VFULL + st));
+                    tma_load_2d(base + AT_V + st * TILE_BYTES + HALF_BYTES, mv, kvh * TILE + 64, local * TILE, bar(BAR_VFULL + st));
                     if (more) {
                         // the next step's keys: the next tile of this item, or the first tile of the next item
                         const int nk = in_unit ? kvh : (U.item + 1) / P.pairs_per_g, nj = in_unit ? U.jb + j + 1 : 0;
@@ -392,7 +413,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         bool alive = true;
         if (warp < 3) {
             const int t = warp - 1;
-            const uint64_t dq0 = desc_kmajor(base + SM_Q + t * TILE_BYTES), dk0 = desc_kmajor(base + SM_K);
+            const uint64_t dq0 = desc_kmajor(base + SM_Q + t * TILE_BYTES), dk0 = desc_kmajor(base + AT_K);
             long long g = G0;
             int un = -1, left = 0;                           // this unit, and its steps left
 #pragma unroll 1
@@ -405,22 +426,27 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     if (!alive) break;
                 }
                 --left;
-                if (gs > 0) alive = wait(BAR_VFULL + (gs - 1) % KV_STAGES, ((gs - 1) / KV_STAGES) & 1);      // K(step) came with V(step - 1)
+                if constexpr (FINE) alive = wait(BAR_KFULL, gs & 1);
+                else if (gs > 0) alive = wait(BAR_VFULL + (gs - 1) % KV_STAGES, ((gs - 1) / KV_STAGES) & 1);      // K(step) came with V(step - 1)
                 if (alive && gs + t > 0) alive = wait(BAR_SFREE + (t ^ 1), (gs + t + 1) & 1);      // the other tile's scores have left the columns
                 if (!alive) break;
-                uint64_t dq = dq0, dk = dk0 + (gs % KV_STAGES) * (TILE_BYTES >> 4);
+                uint64_t dq = dq0, dk = FINE ? dk0 : dk0 + (gs % KV_STAGES) * (TILE_BYTES >> 4);
 #pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
+                for (int half = 0; half < (FINE ? 4 : 2); ++half) {
 #pragma unroll
                     for (int k4 = 0; k4 < 4; ++k4)
-                        if (lead) mma_ss(tm + TM_S, dq + k4 * 2, dk + k4 * 2, IDESC_QK, (half > 0 || k4 > 0));
+                        if (lead) mma_ss(tm + TM_S, dq + k4 * 2, dk + k4 * 2, QK, (half > 0 || k4 > 0));
                     dq += HALF_BYTES >> 4;
                     dk += HALF_BYTES >> 4;
+                    if (FINE && half == 1) {         // the second part of the queries, two tiles on, against the same keys
+                        dq += TILE_BYTES >> 4;
+                        dk = dk0;
+                    }
                 }
                 if (lead) tc_commit(bar(BAR_SFULL + t));
             }
         } else {
-            const uint64_t dv0 = desc_mnmajor(base + SM_V);
+            const uint64_t dv0 = desc_mnmajor(base + AT_V);
             int at = (int)(G0 % P.n_kv_tiles);               // key tile of the step
 #pragma unroll 1
             for (int gs = 0; gs < n_steps && alive; ++gs) {
@@ -441,7 +467,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                         if (!alive) break;
 #pragma unroll
                         for (int k4 = 0; k4 < 4; ++k4)     // 16 keys per step: P columns advance by 8 (two bf16 per column)
-                            if (lead) mma_ts(oa, pa + k4 * 8, dv + k4 * (2048 >> 4), IDESC_PV, (!first || hf > 0 || k4 > 0));
+                            if (lead) mma_ts(oa, pa + k4 * 8, dv + k4 * (2048 >> 4), PV, (!first || hf > 0 || k4 > 0));
                         dv += 8192 >> 4;
                         pa += 32;
                     }
@@ -613,8 +639,8 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                         y.x = fast_exp2(y.x); y.y = fast_exp2(y.y);
                         la = add2(la, x);
                         lb = add2(lb, y);
-                        pk[i] = pc_pack_bf16(x.x, x.y);
-                        pk[i + 1] = pc_pack_bf16(y.x, y.y);
+                        pk[i] = FINE ? pc_pack_f16(x.x, x.y) : pc_pack_bf16(x.x, x.y);
+                        pk[i + 1] = FINE ? pc_pack_f16(y.x, y.y) : pc_pack_bf16(y.x, y.y);
                     }
                     // the sums belong in the gaps of this chunk's exponentials, not behind the hand-over
                     asm volatile("" : "+f"(la.x), "+f"(la.y), "+f"(lb.x), "+f"(lb.y));
@@ -806,7 +832,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         // some of it was given up, and a captured call replays unchanged.  It also merges what was left: every part of the call is
         // stored and fenced ahead of its CTA's ticket (a second part by pass_on, which this thread ran).
         // That something was left travels with the ticket: a look behind it (a fence and a load) made every call 1.2 us longer.
-        volatile uint32_t *last = reinterpret_cast<volatile uint32_t *>(gen + SM_BAR + N_BARS * 8 + 4);   // (left_here and tmem_slot, read already) anything left, number of the call
+        volatile uint32_t *last = reinterpret_cast<volatile uint32_t *>(gen + AT_BAR + N_BARS * 8 + 4);   // (left_here and tmem_slot, read already) anything left, number of the call
         if (threadIdx.x == 0) {
             const uint32_t mine = *left_here ? 0x10000u : 0u;
             uint32_t left = 0;
@@ -1202,5 +1228,69 @@ pc_status pc_launch_attend_tc(pc_ctx *ctx, int n_seg, const pc_segment *segs, co
     ctx->last_n_q = n_q;
     ctx->last_n_seg = n_seg;
     for (int s = 0; s < n_seg; ++s) ctx->last_seg_n[s] = segs[s].n_tokens;
+    return PC_OK;
+}
+
+// The same attention over keys and values that lie in fp16 already, and queries in two fp16 parts (q16: the first parts of n_q rows, from lo_row0 on
+// the second ones): k16 with the segments on tile boundaries as in the context's scratch, v16[s] the rows of segment s.
+pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, const void *const *v16, const void *q16, int lo_row0, int32_t n_q,
+                                void *out, float *lse, cudaStream_t stream) {
+    const pc_layer_desc &D = ctx->desc;
+    if (D.head_dim != TILE || D.dtype != PC_BF16) return PC_ERR_UNSUPPORTED;
+    const uint64_t kv_row = (uint64_t)D.n_kv_heads * TILE, q_row = (uint64_t)D.n_q_heads * TILE;
+    TcParams P{};
+    int tiles = 0;
+    for (int s = 0; s < n_seg; ++s) {
+        tiles += div_up(seg_n[s], TILE);
+        P.seg_tile_end[s] = tiles;
+        P.seg_n[s] = seg_n[s];
+    }
+    P.n_q = n_q;
+    P.n_q_heads = D.n_q_heads;
+    P.group = ctx->group;
+    P.n_tb = div_up(n_q, TILE);
+    P.tiles_per_g = P.group * P.n_tb;
+    P.pairs_per_g = div_up(P.tiles_per_g, 2);
+    P.n_kv_tiles = tiles;
+    P.n_seg = n_seg;
+    P.n_items = D.n_kv_heads * P.pairs_per_g;
+    P.out = static_cast<__nv_bfloat16 *>(out);
+    P.lse = lse;
+    P.part_o = ctx->part_o;
+    P.part_ml = ctx->part_ml;
+    P.status = ctx->status;
+    P.wait_us = ctx->wait_limit_us;
+    P.extra_tx = ctx->test_extra_tx;
+    P.lo_row0 = lo_row0;
+    P.sync = ctx->part_sync;
+    choose_division(ctx, P.n_items, tiles, P);
+    if (P.part_stride > 1 && (size_t)P.n_items * P.part_stride * 2 * TILE * TILE > ctx->part_o_floats) return PC_ERR_CAPACITY;
+    CUtensorMap mq, mk, mv[PC_MAX_SEGMENTS];
+    bool ok = make_map(&mq, q16, (uint64_t)lo_row0 + n_q, q_row) && make_map(&mk, k16, (uint64_t)tiles * TILE, kv_row);
+    for (int s = 0; s < PC_MAX_SEGMENTS; ++s) ok = ok && make_map(&mv[s], v16[s < n_seg ? s : 0], (uint64_t)seg_n[s < n_seg ? s : 0], kv_row);
+    if (!ok) {
+        fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
+        return PC_ERR_CUDA;
+    }
+    const auto kernel = k_attend_tc<false, true>;
+    static bool attr_set[PC_MAX_DEVICES] = {};
+    if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
+    if (!attr_set[ctx->device]) {
+        cudaFuncAttributes a;
+        PC_CUDA_TRY(cudaFuncGetAttributes(&a, kernel));
+        if (a.numRegs * TC_THREADS < REGS_SPLIT) {
+            fprintf(stderr, "packcache: attention kernel built with %d registers a thread, its warps would wait for more\n", a.numRegs);
+            return PC_ERR_CUDA;
+        }
+        PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FINE_ALLOC));
+        attr_set[ctx->device] = true;
+    }
+    PC_LAUNCH(kernel, dim3(P.n_cta), dim3(TC_THREADS), FINE_ALLOC, stream, mq, mk, mv[0], mv[1], mv[2], P);
+    if (P.part_stride > 1) {
+        const dim3 grid(P.n_tb * D.n_q_heads * 4);
+        if (P.part_stride == 2) PC_LAUNCH((k_combine<2, 4>), grid, dim3(256), 0, stream, P);
+        else if (P.part_stride <= 4) PC_LAUNCH((k_combine<4, 3>), grid, dim3(256), 0, stream, P);
+        else PC_LAUNCH((k_combine<MAX_SPLITS, 2>), grid, dim3(256), 0, stream, P);
+    }
     return PC_OK;
 }

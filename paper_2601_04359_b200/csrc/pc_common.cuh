@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <stdint.h>
 #include <stdio.h>
 
@@ -135,6 +136,11 @@ __device__ __forceinline__ float pc_bf16_hi(uint32_t w) { return __uint_as_float
 __device__ __forceinline__ uint32_t pc_pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t *>(&v);
+}
+
+__device__ __forceinline__ uint32_t pc_pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
 }
 
 __device__ __forceinline__ uint4 pc_ldg_stream(const void *p) {
@@ -332,6 +338,9 @@ enum { PC_TC_ROPE_K = 1, PC_TC_ROPE_Q = 2, PC_TC_ATTEND = 4, PC_TC_ALL = 7, PC_T
 // q_row0: first row of the rotated-query scratch that PC_TC_ATTEND reads (q, out and lse are the caller's, already offset)
 pc_status pc_launch_attend_tc(pc_ctx *ctx, int n_seg, const pc_segment *segs, const void *q, const int32_t *q_pos,
                               int32_t n_q, void *out, float *lse, cudaStream_t stream, int what, int q_row0 = 0);
+// keys and values in fp16, queries in two fp16 parts (a frame over the 4-bit cache)
+pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, const void *const *v16, const void *q16, int lo_row0, int32_t n_q,
+                                void *out, float *lse, cudaStream_t stream);
 // query rows of one part of a frame's attention when its output is to leave in parts: enough row tiles per part to fill the GPU
 int pc_attend_part_rows(const pc_ctx *ctx, int n_q);
 // What a frame step driven from host memory adds to pc_frame_step / pc_attend_frame: an event the stream waits for before V or

@@ -25,7 +25,7 @@ struct pc_q4 {
     size_t part_rows;
     float *logits;                     // [history token][rows of a pass]
     size_t logit_floats;
-    void *v;                           // values of the whole cache in bf16 (PC_Q4_FRAMES)
+    void *v, *q16;                     // values of the whole cache in fp16, queries in two fp16 parts (PC_Q4_FRAMES)
     size_t v_rows;
 };
 
@@ -823,20 +823,21 @@ pc_status attend_frame(pc_q4 *w, const pc_q4_cache *cache, const void *q, const 
     ctx->prepared_n_seg = 0;                       // the rotated-key scratch is about to be overwritten
     ctx->anchor_rot_n = 0;
     ctx->last_n_q = 0;
-    pc_segment segs[2];
-    int n_seg = 0;
+    int seg_n[2] = {0, 0}, n_seg = 0;
+    const void *v16[2] = {nullptr, nullptr};
     size_t at = 0;                                 // rows; segments start on tile boundaries
     for (const pc_q4_segment *s : {&cache->anchors, &cache->history}) {
         if (s->n_tokens == 0) continue;
         char *v = static_cast<char *>(w->v) + at * row;
         const pc_status st = pc_q4_launch_thaw(ctx, s, static_cast<char *>(ctx->k_rot) + at * row, v, stream);
         if (st != PC_OK) return st;
-        segs[n_seg++] = pc_segment{nullptr, v, s->pos, s->n_tokens, s->n_tokens};
+        v16[n_seg] = v;
+        seg_n[n_seg++] = s->n_tokens;
         at += (size_t)div_up(s->n_tokens, 128) * 128;
     }
-    const pc_status st = pc_launch_attend_tc(ctx, n_seg, segs, q, q_pos, n_q, out, lse, stream, PC_TC_ROPE_Q | PC_TC_ATTEND);
-    ctx->last_n_q = 0;                             // the masses of this call's queries are not offered
-    return st;
+    const int lo_row0 = div_up(n_q, 128) * 128;
+    const pc_status st = pc_q4_launch_queries(ctx, q, q_pos, n_q, w->q16, lo_row0, stream);
+    return st != PC_OK ? st : pc_launch_attend_fine(ctx, n_seg, seg_n, ctx->k_rot, v16, w->q16, lo_row0, n_q, out, lse, stream);
 }
 
 }  // namespace
@@ -865,7 +866,8 @@ extern "C" pc_status pc_q4_create(pc_ctx *ctx, int32_t max_tokens, int32_t parts
         }
         if ((parts & PC_Q4_FRAMES) && pc_tensor_core_shape(ctx)) {
             w->v_rows = (size_t)(div_up(max_tokens, 128) + 1) * 128;
-            PC_CUDA_TRY(cudaMalloc(&w->v, w->v_rows * D.n_kv_heads * D.head_dim * sizeof(__nv_bfloat16)));
+            PC_CUDA_TRY(cudaMalloc(&w->v, w->v_rows * D.n_kv_heads * D.head_dim * sizeof(__half)));
+            PC_CUDA_TRY(cudaMalloc(&w->q16, ((size_t)div_up(D.max_q, 128) * 128 + D.max_q) * D.n_q_heads * D.head_dim * sizeof(__half)));
         }
         return PC_OK;
     };
@@ -885,6 +887,7 @@ extern "C" pc_status pc_q4_destroy(pc_q4 *w) {
     cudaFree(w->lse);
     cudaFree(w->logits);
     cudaFree(w->v);
+    cudaFree(w->q16);
     delete w;
     return PC_OK;
 }

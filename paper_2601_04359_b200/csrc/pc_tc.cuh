@@ -149,6 +149,7 @@ __device__ __forceinline__ uint64_t desc_mnmajor(uint32_t addr) {
 constexpr uint32_t IDESC_BASE = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 constexpr uint32_t IDESC_QK = IDESC_BASE;               // A, B K-major
 constexpr uint32_t IDESC_PV = IDESC_BASE | (1u << 16);  // B (V) MN-major
+constexpr uint32_t IDESC_F16 = ~((1u << 7) | (1u << 10)); // and-ed: fp16 x fp16 instead of bf16 x bf16
 
 // ------------------------------------------------------------------------------------------------ tensor maps (host)
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,

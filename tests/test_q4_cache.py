@@ -286,13 +286,16 @@ def test_on_another_stream():
 
 @pytest.mark.parametrize("shape,n_q,shift", [("lumos", 100, 0), ("lumos", 130, 40), ("mha", 200, 12), ("gqa4", 40, 8)])
 def test_frames_on_the_tensor_core_kernel(shape, n_q, shift):
-    """Rotated queries and keys in bf16 (2^-9 each, at random over d channels: 2^-8 of sum |q k| / sqrt(d) bounds a logit's error from above),
-    probabilities and values in bf16 (2^-8)."""
+    """Keys, values and probabilities in fp16 (2^-12 of each, at most), queries in two parts: a logit is off by 2^-12 of sum |q k| / sqrt(d) and what fp32
+    sums round, an output by twice that and two more roundings of sum p |v|, and the rounding to bf16."""
     c = Case(shape, 70, 300, n_q, shift=shift, frames=True)
     want, want_lse, _, mag_l, mag_v = ref.attend(_np(c.q), c.q_pos.cpu().numpy(), c.parts())
     out, lse = pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos, want_lse=True)
     assert pc.pc_poll_status(c.ctx) == pc.PC_OK
     assert np.abs(_np(lse) - want_lse).max() <= 2e-2 and np.abs(_np(out) - want).max() <= 2e-2 * max(1.0, np.abs(want).max())
+    delta = (2.0 ** -12 + 48 * 2.0 ** -23) * mag_l
+    assert (np.abs(_np(lse) - want_lse) <= delta + 2.0 ** -20 * (1 + np.abs(want_lse))).all()
+    assert (np.abs(_np(out) - want) <= (2 * delta + 2.0 ** -11)[..., None] * mag_v + 2.0 ** -8 * np.abs(want)).all()
     slow = pc.Q4Work(c.ctx, 370)
     rows = _np(pc.pc_q4_attend(slow, c.cache, c.q, c.q_pos))
     assert np.abs(rows - want).max() <= 2e-2 * max(1.0, np.abs(want).max())
