@@ -66,12 +66,12 @@ constexpr int SM_BAR = SM_V + KV_STAGES * TILE_BYTES;     // barriers etc.
 constexpr int SM_ML = SM_BAR + 256;                       // (max, sum) of both tiles' rows for the cluster merge: 2 KB
 constexpr int SM_TOTAL = SM_ML + 2 * TILE * 8;
 constexpr int SM_ALLOC = SM_TOTAL + 1024;                 // slack for manual alignment
-// the same with queries in two fp16 parts: both parts of 2 query tiles, one K tile, KV_STAGES V tiles, barriers
-constexpr int FINE_K = SM_Q + 4 * TILE_BYTES, FINE_V = FINE_K + TILE_BYTES, FINE_BAR = FINE_V + KV_STAGES * TILE_BYTES, FINE_ALLOC = FINE_BAR + 256 + 1024;
+// the same with queries in two fp16 parts: both parts of 2 query tiles, three tiles that keys and values take in turn, barriers
+constexpr int FINE_KV = SM_Q + 4 * TILE_BYTES, FINE_BAR = FINE_KV + 3 * TILE_BYTES, FINE_ALLOC = FINE_BAR + 256 + 1024;
 
 enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_VFULL = 4 /* [stage] */, BAR_EMPTY = 6 /* [step & 1] */, BAR_SFULL = 8 /* [tile] */,
-       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, BAR_PART = 19, N_BARS = 20,
-       BAR_KFULL = BAR_PART /* of the form with queries in two parts, which merges nothing */ };
+       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, BAR_PART = 19,
+       BAR_KFULL = 20 /* [step & 1], of the form with queries in two parts */, N_BARS = 22 };
 static_assert(N_BARS * 8 + 12 <= 256, "barriers, abort flag and TMEM address share 256 bytes");
 
 constexpr int SYNC_PARTS = 2, LEFT_PER_ITEM = 8;          // words of TcParams::sync
@@ -263,15 +263,19 @@ __device__ __noinline__ void merge_left(const TcParams &P, uint32_t call, int w,
 // MERGE: items in two parts are merged by the CTA that has the first one.  A kernel of its own: with what that takes in its code, calls
 // that merge nothing took 0.3 us longer.
 // FINE: queries, keys, values and probabilities in fp16 instead of bf16 and the queries in two parts, whose products with the keys add up in the same
-// columns (22 bits of a query, so that the lse is good to fp32's accuracy over thousands of keys).  The second part takes the place of the
-// second K stage: K(step + 1) is fetched once both tiles' Q K^T of the step have read K(step), under their softmax.
+// columns (22 bits of a query, so that the lse is good to fp32's accuracy over thousands of keys).  The second part leaves room for three tiles
+// of keys or values, which are fetched in the order K(0) K(1) V(0) K(2) V(1) K(3) V(2) ... into the three places in turn: K(step + 1) lies
+// there a step ahead, and V(step) comes where K(step) has been read, under the step's softmax and the next Q K^T.  (One place for keys and two for
+// values: Q K^T waited for its keys, 4,000 cycles a step instead of the tensor core's 3,072.)
 template <bool MERGE, bool FINE = false>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
             const __grid_constant__ CUtensorMap map_v0, const __grid_constant__ CUtensorMap map_v1,
             const __grid_constant__ CUtensorMap map_v2, const __grid_constant__ TcParams P) {
     static_assert(!(MERGE && FINE), "the form with queries in two parts leaves merges to the merge kernel");
-    constexpr int AT_K = FINE ? FINE_K : SM_K, AT_V = FINE ? FINE_V : SM_V, AT_BAR = FINE ? FINE_BAR : SM_BAR;
+    constexpr int AT_K = FINE ? FINE_KV : SM_K, AT_V = FINE ? FINE_KV : SM_V, AT_BAR = FINE ? FINE_BAR : SM_BAR;
+    const auto fine_k = [](int step) { return step == 0 ? 0 : (2 * step - 1) % 3; };      // places of a step's keys and values
+    const auto fine_v = [](int step) { return (2 * step + 2) % 3; };
     constexpr uint32_t QK = FINE ? IDESC_QK & IDESC_F16 : IDESC_QK, PV = FINE ? IDESC_PV & IDESC_F16 : IDESC_PV;
     pc_grid_dep_launch();
     extern __shared__ uint8_t smem_raw[];
@@ -304,7 +308,9 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             mbar_init(bar(BAR_PHALF + 2 * t + 1), 4);
         }
         mbar_init(bar(BAR_DONE), 3);
-        mbar_init(bar(BAR_PART), FINE ? 1 : 8);
+        mbar_init(bar(BAR_PART), 8);
+        mbar_init(bar(BAR_KFULL), 1);
+        mbar_init(bar(BAR_KFULL + 1), 1);
         *abort_flag = 0;
         *left_here = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -372,17 +378,31 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     kv_tile_info(P, U.jb + j, seg, local, n_valid);
                     const CUtensorMap *mv = seg == 0 ? &map_v0 : (seg == 1 ? &map_v1 : &map_v2);
                     if constexpr (FINE) {
-                        for (int t = 0; t < 2 && alive && gs > 0; ++t)           // both Q K^T(step - 1) have read the one K tile
-                            alive = mbar_wait(bar(BAR_SFULL + t), (gs - 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
+                        const auto load_k = [&](int step, int kv_head, int tile) {
+                            const uint32_t to = base + AT_K + fine_k(step) * TILE_BYTES, b = bar(BAR_KFULL + (step & 1));
+                            mbar_expect_tx(b, TILE_BYTES);
+                            tma_load_2d(to, &map_k, kv_head * TILE, tile * TILE, b);
+                            tma_load_2d(to + HALF_BYTES, &map_k, kv_head * TILE + 64, tile * TILE, b);
+                        };
+                        if (gs == 0) load_k(0, kvh, U.jb);
+                        // QK^T(step - 1) and PV(step - 2) are done: K(step + 1) takes the place of V(step - 2) (of K(0) at step 1)
+                        else alive = mbar_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
                         if (!alive) break;
-                        mbar_expect_tx(bar(BAR_KFULL), TILE_BYTES);
-                        tma_load_2d(base + AT_K, &map_k, kvh * TILE, (U.jb + j) * TILE, bar(BAR_KFULL));
-                        tma_load_2d(base + AT_K + HALF_BYTES, &map_k, kvh * TILE + 64, (U.jb + j) * TILE, bar(BAR_KFULL));
+                        const bool same = j + 1 < U.n_j;
+                        if (same || g < G1) load_k(gs + 1, same ? kvh : (U.item + 1) / P.pairs_per_g, same ? U.jb + j + 1 : 0);
+                        // QK^T(step) is done: V(step) takes the place of K(step)
+                        if (gs > 0) alive = mbar_wait(bar(BAR_EMPTY + (gs & 1)), (gs >> 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
+                        if (!alive) break;
+                        const uint32_t to = base + AT_V + fine_v(gs) * TILE_BYTES;
+                        mbar_expect_tx(bar(BAR_VFULL + st), TILE_BYTES);
+                        tma_load_2d(to, mv, kvh * TILE, local * TILE, bar(BAR_VFULL + st));
+                        tma_load_2d(to + HALF_BYTES, mv, kvh * TILE + 64, local * TILE, bar(BAR_VFULL + st));
+                        continue;
                     }
                     // PV(step - 2) and QK^T(step - 1) have read what lies where V(step) and K(step + 1) go
                     if (gs > 0) alive = mbar_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, P.status, PC_WHERE_ATTN_WAIT, P.wait_us);
                     if (!alive) break;
-                    const bool in_unit = j + 1 < U.n_j, more = !FINE && (in_unit || g < G1);
+                    const bool in_unit = j + 1 < U.n_j, more = in_unit || g < G1;
                     mbar_expect_tx(bar(BAR_VFULL + st), (more ? 2 : 1) * TILE_BYTES);
                     tma_load_2d(base + AT_V + st * TILE_BYTES, mv, kvh * TILE, local * TILE, bar(BAR_VFULL + st));
                     tma_load_2d(base + AT_V + st * TILE_BYTES + HALF_BYTES, mv, kvh * TILE + 64, local * TILE, bar(BAR_VFULL + st));
@@ -426,11 +446,12 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     if (!alive) break;
                 }
                 --left;
-                if constexpr (FINE) alive = wait(BAR_KFULL, gs & 1);
+                if constexpr (FINE) alive = wait(BAR_KFULL + (gs & 1), (gs >> 1) & 1);
                 else if (gs > 0) alive = wait(BAR_VFULL + (gs - 1) % KV_STAGES, ((gs - 1) / KV_STAGES) & 1);      // K(step) came with V(step - 1)
                 if (alive && gs + t > 0) alive = wait(BAR_SFREE + (t ^ 1), (gs + t + 1) & 1);      // the other tile's scores have left the columns
                 if (!alive) break;
-                uint64_t dq = dq0, dk = FINE ? dk0 : dk0 + (gs % KV_STAGES) * (TILE_BYTES >> 4);
+                const uint64_t dk_step = dk0 + (FINE ? fine_k(gs) : gs % KV_STAGES) * (TILE_BYTES >> 4);
+                uint64_t dq = dq0, dk = dk_step;
 #pragma unroll 1
                 for (int half = 0; half < (FINE ? 4 : 2); ++half) {
 #pragma unroll
@@ -440,7 +461,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                     dk += HALF_BYTES >> 4;
                     if (FINE && half == 1) {         // the second part of the queries, two tiles on, against the same keys
                         dq += TILE_BYTES >> 4;
-                        dk = dk0;
+                        dk = dk_step;
                     }
                 }
                 if (lead) tc_commit(bar(BAR_SFULL + t));
@@ -458,7 +479,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
 #pragma unroll 1
                 for (int t = 0; t < 2 && alive; ++t) {
                     // P arrives in two halves of 64 keys: the first PV steps run while the rest is exponentiated
-                    uint64_t dv = dv0 + st * (TILE_BYTES >> 4);
+                    uint64_t dv = dv0 + (FINE ? fine_v(gs) : st) * (TILE_BYTES >> 4);
                     uint32_t pa = tm + TM_P + t * (TILE / 2);
                     const uint32_t oa = tm + TM_O + t * TILE;
 #pragma unroll 1
