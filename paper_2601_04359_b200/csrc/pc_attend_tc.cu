@@ -272,7 +272,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
             const __grid_constant__ CUtensorMap map_v0, const __grid_constant__ CUtensorMap map_v1,
             const __grid_constant__ CUtensorMap map_v2, const __grid_constant__ TcParams P) {
-    static_assert(!(MERGE && FINE), "the form with queries in two parts leaves merges to the merge kernel");
     constexpr int AT_K = FINE ? FINE_KV : SM_K, AT_V = FINE ? FINE_KV : SM_V, AT_BAR = FINE ? FINE_BAR : SM_BAR;
     const auto fine_k = [](int step) { return step == 0 ? 0 : (2 * step - 1) % 3; };      // places of a step's keys and values
     const auto fine_v = [](int step) { return (2 * step + 2) % 3; };
@@ -397,6 +396,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                         mbar_expect_tx(bar(BAR_VFULL + st), TILE_BYTES);
                         tma_load_2d(to, mv, kvh * TILE, local * TILE, bar(BAR_VFULL + st));
                         tma_load_2d(to + HALF_BYTES, mv, kvh * TILE + 64, local * TILE, bar(BAR_VFULL + st));
+                        if (owes && un > 0 && pc_mbar_test(bar(BAR_PART), 0)) pass_on();
                         continue;
                     }
                     // PV(step - 2) and QK^T(step - 1) have read what lies where V(step) and K(step + 1) go
@@ -1254,7 +1254,7 @@ pc_status pc_launch_attend_tc(pc_ctx *ctx, int n_seg, const pc_segment *segs, co
 
 // The same attention over keys and values that lie in fp16 already, and queries in two fp16 parts (q16: the first parts of n_q rows, from lo_row0 on
 // the second ones): k16 with the segments on tile boundaries as in the context's scratch, v16[s] the rows of segment s.
-pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, const void *const *v16, const void *q16, int lo_row0, int32_t n_q,
+pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, void *const *v16, const void *q16, int lo_row0, int32_t n_q,
                                 void *out, float *lse, cudaStream_t stream) {
     const pc_layer_desc &D = ctx->desc;
     if (D.head_dim != TILE || D.dtype != PC_BF16) return PC_ERR_UNSUPPORTED;
@@ -1293,21 +1293,24 @@ pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const 
         fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
         return PC_ERR_CUDA;
     }
-    const auto kernel = k_attend_tc<false, true>;
+    const bool merge = P.persistent && P.part_stride == 2 && P.n_cta % P.n_items != 0;        // as in pc_launch_attend_tc
+    P.leave_parts = ctx->test_leave_parts;
     static bool attr_set[PC_MAX_DEVICES] = {};
     if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
     if (!attr_set[ctx->device]) {
-        cudaFuncAttributes a;
-        PC_CUDA_TRY(cudaFuncGetAttributes(&a, kernel));
-        if (a.numRegs * TC_THREADS < REGS_SPLIT) {
-            fprintf(stderr, "packcache: attention kernel built with %d registers a thread, its warps would wait for more\n", a.numRegs);
-            return PC_ERR_CUDA;
+        for (const auto kernel : {k_attend_tc<false, true>, k_attend_tc<true, true>}) {
+            cudaFuncAttributes a;
+            PC_CUDA_TRY(cudaFuncGetAttributes(&a, kernel));
+            if (a.numRegs * TC_THREADS < REGS_SPLIT) {
+                fprintf(stderr, "packcache: attention kernel built with %d registers a thread, its warps would wait for more\n", a.numRegs);
+                return PC_ERR_CUDA;
+            }
+            PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FINE_ALLOC));
         }
-        PC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FINE_ALLOC));
         attr_set[ctx->device] = true;
     }
-    PC_LAUNCH(kernel, dim3(P.n_cta), dim3(TC_THREADS), FINE_ALLOC, stream, mq, mk, mv[0], mv[1], mv[2], P);
-    if (P.part_stride > 1) {
+    PC_LAUNCH((merge ? k_attend_tc<true, true> : k_attend_tc<false, true>), dim3(P.n_cta), dim3(TC_THREADS), FINE_ALLOC, stream, mq, mk, mv[0], mv[1], mv[2], P);
+    if (P.part_stride > 1 && !merge) {
         const dim3 grid(P.n_tb * D.n_q_heads * 4);
         if (P.part_stride == 2) PC_LAUNCH((k_combine<2, 4>), grid, dim3(256), 0, stream, P);
         else if (P.part_stride <= 4) PC_LAUNCH((k_combine<4, 3>), grid, dim3(256), 0, stream, P);

@@ -339,7 +339,7 @@ enum { PC_TC_ROPE_K = 1, PC_TC_ROPE_Q = 2, PC_TC_ATTEND = 4, PC_TC_ALL = 7, PC_T
 pc_status pc_launch_attend_tc(pc_ctx *ctx, int n_seg, const pc_segment *segs, const void *q, const int32_t *q_pos,
                               int32_t n_q, void *out, float *lse, cudaStream_t stream, int what, int q_row0 = 0);
 // keys and values in fp16, queries in two fp16 parts (a frame over the 4-bit cache)
-pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, const void *const *v16, const void *q16, int lo_row0, int32_t n_q,
+pc_status pc_launch_attend_fine(pc_ctx *ctx, int n_seg, const int *seg_n, const void *k16, void *const *v16, const void *q16, int lo_row0, int32_t n_q,
                                 void *out, float *lse, cudaStream_t stream);
 // query rows of one part of a frame's attention when its output is to leave in parts: enough row tiles per part to fill the GPU
 int pc_attend_part_rows(const pc_ctx *ctx, int n_q);

@@ -25,7 +25,7 @@ inline bool pc_overlaps(const void *a, size_t na, const void *b, size_t nb) {
     return a && b && x < y + nb && y < x + na;
 }
 
-// Rows of a segment in fp16 for the tensor-core attention kernel: keys turned back by t_shift only (they stay rotated at their positions)
-pc_status pc_q4_launch_thaw(pc_ctx *ctx, const pc_q4_segment *src, void *k16, void *v16, cudaStream_t stream);
-// Queries rotated and scaled, in two fp16 parts: q16 rows 0 .. n_q - 1 and, from row lo_row0 on, what they leave
-pc_status pc_q4_launch_queries(pc_ctx *ctx, const void *q, const int32_t *q_pos, int32_t n_q, void *q16, int lo_row0, cudaStream_t stream);
+// What the tensor-core attention kernel needs of a frame over the cache: rows of up to two segments in fp16 (keys turned back by t_shift only: they stay
+// rotated at their positions), queries rotated and scaled in two fp16 parts (q16 rows 0 .. n_q - 1 and, from row lo_row0 on, what they leave)
+pc_status pc_q4_launch_front(pc_ctx *ctx, const pc_q4_segment *const *segs, int n_seg, void *const *k16, void *const *v16, const void *q, const int32_t *q_pos,
+                             int32_t n_q, void *q16, int lo_row0, cudaStream_t stream);

@@ -823,20 +823,20 @@ pc_status attend_frame(pc_q4 *w, const pc_q4_cache *cache, const void *q, const 
     ctx->prepared_n_seg = 0;                       // the rotated-key scratch is about to be overwritten
     ctx->anchor_rot_n = 0;
     ctx->last_n_q = 0;
-    int seg_n[2] = {0, 0}, n_seg = 0;
-    const void *v16[2] = {nullptr, nullptr};
+    const pc_q4_segment *segs[2];
+    void *k16[2], *v16[2];
+    int seg_n[2], n_seg = 0;
     size_t at = 0;                                 // rows; segments start on tile boundaries
     for (const pc_q4_segment *s : {&cache->anchors, &cache->history}) {
         if (s->n_tokens == 0) continue;
-        char *v = static_cast<char *>(w->v) + at * row;
-        const pc_status st = pc_q4_launch_thaw(ctx, s, static_cast<char *>(ctx->k_rot) + at * row, v, stream);
-        if (st != PC_OK) return st;
-        v16[n_seg] = v;
+        segs[n_seg] = s;
+        k16[n_seg] = static_cast<char *>(ctx->k_rot) + at * row;
+        v16[n_seg] = static_cast<char *>(w->v) + at * row;
         seg_n[n_seg++] = s->n_tokens;
         at += (size_t)div_up(s->n_tokens, 128) * 128;
     }
     const int lo_row0 = div_up(n_q, 128) * 128;
-    const pc_status st = pc_q4_launch_queries(ctx, q, q_pos, n_q, w->q16, lo_row0, stream);
+    const pc_status st = pc_q4_launch_front(ctx, segs, n_seg, k16, v16, q, q_pos, n_q, w->q16, lo_row0, stream);
     return st != PC_OK ? st : pc_launch_attend_fine(ctx, n_seg, seg_n, ctx->k_rot, v16, w->q16, lo_row0, n_q, out, lse, stream);
 }
 
