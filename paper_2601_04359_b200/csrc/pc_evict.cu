@@ -36,13 +36,15 @@ __device__ __forceinline__ uint32_t remote(uint32_t addr, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
     return there;
 }
-// Two integers of every CTA's shared memory at the same place, all requested before the first is used (one behind the other, a read
-// took 700 cycles: selection among 24,192 tokens 25 us)
-__device__ __forceinline__ void remote_pairs(uint32_t addr, int2 (&v)[MAX_CLUSTER]) {
-#pragma unroll
-    for (int r = 0; r < MAX_CLUSTER; ++r)
-        asm volatile("ld.shared::cluster.v2.s32 {%0,%1}, [%2];" : "=r"(v[r].x), "=r"(v[r].y) : "r"(remote(addr, r)) : "memory");
+__device__ __forceinline__ int4 remote_load(uint32_t addr, uint32_t rank) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote(addr, rank)) : "memory");
+    return v;
 }
+__device__ __forceinline__ void remote_store(uint32_t addr, uint32_t rank, int4 v) {
+    asm volatile("st.shared::cluster.v4.s32 [%0], {%1,%2,%3,%4};" ::"r"(remote(addr, rank)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ int4 operator+(int4 a, int4 b) { return make_int4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
 // Sum of v over the threads before this one, and over all
 __device__ __forceinline__ int scan_block(int v, int *warp_sums, int &all) {
@@ -63,10 +65,11 @@ __device__ __forceinline__ int scan_block(int v, int *warp_sums, int &all) {
 
 __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectParams P) {
     extern __shared__ uint32_t keys[];             // [min(piece, CACHED)]
-    __shared__ __align__(8) int hist[2][DIGIT_BINS];
+    constexpr int SLICE = DIGIT_BINS / MAX_CLUSTER;                  // bins that a CTA of the cluster adds up for all
+    __shared__ __align__(16) int hist[2][DIGIT_BINS], total[DIGIT_BINS], slice[MAX_CLUSTER][SLICE];
     __shared__ int warp_sums[SEL_WARPS];
     __shared__ int found[3];
-    __shared__ int2 counts;
+    __shared__ int4 counts[MAX_CLUSTER];
     static_assert(SEL_WARPS == 32 && DIGIT_BINS == 2 * SEL_THREADS, "a lane reads a warp's total, a thread owns two bins");
     pc_grid_dep_launch();
     const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
@@ -102,23 +105,27 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
             const uint32_t k = key_at(j);
             if (pass == 0 || ((k ^ prefix) >> above) == 0) atomicAdd(&h[(k >> shift) & mask], 1);
         }
-        if (ctas > 1) cluster_sync();
-        else __syncthreads();
+        if (ctas > 1) {
+            // Every CTA adds up a slice of the bins and gives it to all: 16 KB through distributed shared memory and a barrier more, where every CTA reading all
+            // counts of all takes 64 KB and 5,000 cycles
+            cluster_sync();
+            const int i = 4 * (threadIdx.x % (SLICE / 4)), other = threadIdx.x / (SLICE / 4);
+            if (other < MAX_CLUSTER) *reinterpret_cast<int4 *>(&slice[other][i]) = remote_load(pc_smem_u32(h + rank * SLICE + i), other);
+            __syncthreads();
+            if (other < MAX_CLUSTER) {
+                int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < MAX_CLUSTER; ++r) sum = sum + *reinterpret_cast<const int4 *>(&slice[r][i]);
+                remote_store(pc_smem_u32(total + rank * SLICE + i), other, sum);
+            }
+            cluster_sync();
+        } else {
+            __syncthreads();
+        }
         // thread t owns the bins 2047 - 2 t and 2046 - 2 t: counts from the top bin down
         const int b0 = DIGIT_BINS - 1 - 2 * threadIdx.x;
-        int c0 = 0, c1 = 0;
-        if (ctas > 1) {
-            int2 c[MAX_CLUSTER];
-            remote_pairs(pc_smem_u32(h + b0 - 1), c);
-#pragma unroll
-            for (int r = 0; r < MAX_CLUSTER; ++r) {
-                c0 += c[r].y;
-                c1 += c[r].x;
-            }
-        } else {
-            c0 = h[b0];
-            c1 = h[b0 - 1];
-        }
+        const int *sums = ctas > 1 ? total : h;
+        const int c0 = sums[b0], c1 = sums[b0 - 1];
         int all;
         const int before = scan_block(c0 + c1, warp_sums, all);
         if (before < want && want <= before + c0 + c1) {
@@ -151,18 +158,12 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
     const int gt0 = scan_block(gt, warp_sums, all_gt), eq0 = scan_block(eq, warp_sums, all_eq);
     int gt_before = gt0, eq_before = eq0;
     if (ctas > 1) {
-        if (threadIdx.x == 0) {
-            counts = make_int2(all_gt, all_eq);
-        }
+        if (threadIdx.x < MAX_CLUSTER) remote_store(pc_smem_u32(&counts[rank]), threadIdx.x, make_int4(all_gt, all_eq, 0, 0));
         cluster_sync();
-        int2 c[MAX_CLUSTER];
-        remote_pairs(pc_smem_u32(&counts), c);
-#pragma unroll
-        for (int r = 0; r < MAX_CLUSTER; ++r)
-            if (r < rank) {
-                gt_before += c[r].x;
-                eq_before += c[r].y;
-            }
+        for (int r = 0; r < rank; ++r) {
+            gt_before += counts[r].x;
+            eq_before += counts[r].y;
+        }
     }
     for (int j = j0; j < j1; ++j) {
         const uint32_t k = key_at(j);
@@ -172,7 +173,6 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
         eq_before += k == prefix;
     }
     for (int j = rank * SEL_THREADS + threadIdx.x; j < P.recent; j += ctas * SEL_THREADS) P.sel_idx[P.want + j] = P.n_old + j;
-    if (ctas > 1) cluster_sync();                  // nobody leaves while others read its counts
 }
 
 // Nothing to choose: the tokens from `first` on are kept
