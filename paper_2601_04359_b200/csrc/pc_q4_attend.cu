@@ -386,13 +386,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             }
         };
         // Keys of a step that are there and not masked: a bit per row of the instruction
-        const auto look_at_mask = [&](int first, float (&S)[4], bool there) {
+        const auto look_at_mask = [&](int first, float (&S)[4], bool there, const uint8_t (&mask)[2]) {
             const int n = there ? n_seg - first : 0;
-            bool ok0 = k0 < n, ok1 = k0 + 8 < n;
-            if (valid) {
-                if (ok0) ok0 = __ldg(valid + first + k0) != 0;
-                if (ok1) ok1 = __ldg(valid + first + k0 + 8) != 0;
-            }
+            const bool ok0 = k0 < n && mask[0] != 0, ok1 = k0 + 8 < n && mask[1] != 0;
             if (!ok0) S[0] = S[1] = -INFINITY;
             if (!ok1) S[2] = S[3] = -INFINITY;
             // lane 4 i speaks for row i, lane 4 i + 1 for row i + 8
@@ -477,6 +473,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     uint32_t phase = 0;
 #pragma unroll 1
     for (int unit = sub; unit < n_units; unit += P.subs) {
+        uint8_t mask[2][2] = {{1, 1}, {1, 1}};       // requested ahead of the wait
+        if (valid) {
+            const int at = (step0 + unit * UNIT) * Q4_STEP + k0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + 8 * i < n_seg) mask[i / 2][i & 1] = __ldg(valid + at + 8 * i);
+        }
         if (!wait_for(full(slot), phase)) break;
             const uint32_t rows = ring + slot * P.unit_bytes;
             const uint32_t rows1 = rows + Q4_STEP * BOX;
@@ -492,8 +495,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 uint32_t seen0 = 0xffffffffu, seen1 = 0xffffffffu;
                 const bool all = !valid && two && first + UNIT * Q4_STEP <= n_seg;
                 if (!all) {
-                    seen0 = look_at_mask(first, S0, true);
-                    seen1 = look_at_mask(first + Q4_STEP, S1, two);
+                    seen0 = look_at_mask(first, S0, true, mask[0]);
+                    seen1 = look_at_mask(first + Q4_STEP, S1, two, mask[1]);
                 }
                 if (logits) {
                     leave_logits(first, S0);
@@ -675,21 +678,22 @@ template <int D, bool F32> __global__ void __launch_bounds__(JOIN_THREADS) k_q4_
     }
 }
 
-// weight_j <- decay weight_j + gain sum over rows of 2^(logit - lse): eight lanes a token, which take its rows in turn
-constexpr int WEIGH_THREADS = 256, WEIGH_LANES = 8;
-__global__ void __launch_bounds__(WEIGH_THREADS) k_q4_weigh(const float *__restrict__ logits, const float *__restrict__ lse, int n, int rows,
-                                                            float decay, float gain, float *__restrict__ weight) {
+// weight_j <- decay weight_j + gain sum over rows of 2^(logit - lse): LANES lanes a token, which take its rows in turn
+constexpr int WEIGH_THREADS = 256;
+template <int LANES> __global__ void __launch_bounds__(WEIGH_THREADS) k_q4_weigh(const float *__restrict__ logits, const float *__restrict__ lse, int n, int rows,
+                                                                                 float decay, float gain, float *__restrict__ weight) {
     pc_grid_dep_launch();
-    const int lane = threadIdx.x % WEIGH_LANES, j = (int)(((long long)blockIdx.x * WEIGH_THREADS + threadIdx.x) / WEIGH_LANES);
+    const int lane = threadIdx.x % LANES, j = (int)(((long long)blockIdx.x * WEIGH_THREADS + threadIdx.x) / LANES);
     pc_grid_dep_wait();
     float sum = 0.f;
     if (j < n)
-        for (int r = lane; r < rows; r += WEIGH_LANES) {
-            const float z = lse[r];
-            sum += z == -INFINITY ? 0.f : exp2_fast(logits[(size_t)j * rows + r] - z);
+#pragma unroll 4
+        for (int r = lane; r < rows; r += LANES) {
+            const float z = __ldg(lse + r);
+            sum += z == -INFINITY ? 0.f : exp2_fast(__ldg(logits + (size_t)j * rows + r) - z);
         }
 #pragma unroll
-    for (int o = 1; o < WEIGH_LANES; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (j < n && lane == 0) weight[j] = fmaf(decay, weight[j], gain * sum);
 }
 
@@ -720,9 +724,26 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     const pc_layer_desc &D = ctx->desc;
     Q4Params P{};
     const pc_q4_segment *segs[2] = {&cache->anchors, &cache->history};
+    // KV heads of a CTA (up to eight, shared out evenly) and blocks of query rows: of one, two or four times as few heads that with which the CTAs of
+    // a piece of the keys have the fewest warps' places in all, so that few stay empty (five queries of 32 / 8 heads are three blocks: 2 x 16 places
+    // with eight heads a CTA, 2 x 12 with four).  Warps left over take further parts of the keys.
+    P.n_rows = n_q * ctx->group;
+    const int n_blocks = div_up(P.n_rows, ROWS);
+    int head_sets = 0, block_groups = 0, places = 0;
+    for (int fewer = 1; fewer <= 4; fewer *= 2) {
+        const int sets = div_up(D.n_kv_heads, 8) * fewer, heads = div_up(D.n_kv_heads, sets);
+        if (sets > D.n_kv_heads) break;
+        const int groups = div_up(n_blocks, MAX_WARPS / heads), blocks = div_up(n_blocks, groups);
+        if (places && sets * heads * groups * blocks >= places) continue;
+        places = sets * heads * groups * blocks;
+        head_sets = sets;
+        block_groups = groups;
+        P.heads = heads;
+        P.blocks = blocks;
+    }
     CUtensorMap maps[2];
     // one set of heads, and sections of whole boxes (4 or 8 KV heads of 128 channels, 8 of 64)
-    P.whole_rows = D.n_kv_heads <= 8 && D.n_kv_heads * D.head_dim / 4 % BOX == 0;
+    P.whole_rows = head_sets == 1 && D.n_kv_heads * D.head_dim / 4 % BOX == 0;
     for (int i = 0; i < 2; ++i) {
         P.n[i] = segs[i]->n_tokens;
         P.shift[i] = segs[i]->t_shift;
@@ -739,14 +760,6 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.n_q_heads = D.n_q_heads;
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
-    P.n_rows = n_q * ctx->group;
-    // KV heads of a CTA: up to eight, shared out evenly; then as many blocks of query rows as there are warps for; the warps left over
-    // take further parts of the keys
-    const int head_sets = div_up(P.n_kv, 8);
-    P.heads = div_up(P.n_kv, head_sets);
-    const int n_blocks = div_up(P.n_rows, ROWS);
-    const int block_groups = div_up(n_blocks, MAX_WARPS / P.heads);
-    P.blocks = div_up(n_blocks, block_groups);
     P.inv_tasks = 65536u / (P.heads * P.blocks) + 1;
     P.inv_heads = 65536u / P.heads + 1;
     P.inv_group = 1.f / (float)P.group;
@@ -810,9 +823,14 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     else if (D.head_dim == 128) PC_LAUNCH((k_q4_join<128, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
     else if (f32) PC_LAUNCH((k_q4_join<64, true>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
     else PC_LAUNCH((k_q4_join<64, false>), dim3(rows), dim3(JOIN_THREADS), 0, stream, J);
-    if (P.logits)
-        PC_LAUNCH(k_q4_weigh, dim3((unsigned)(((long long)P.n[1] * WEIGH_LANES + WEIGH_THREADS - 1) / WEIGH_THREADS)), dim3(WEIGH_THREADS), 0, stream,
-                  w->logits, w->lse, P.n[1], rows, weigh->decay, gain, cache->history.weight);
+    if (P.logits) {
+        const auto weigh_with = [&](auto kernel, int lanes) -> pc_status {
+            PC_LAUNCH(kernel, dim3((unsigned)(((long long)P.n[1] * lanes + WEIGH_THREADS - 1) / WEIGH_THREADS)), dim3(WEIGH_THREADS), 0, stream,
+                      w->logits, w->lse, P.n[1], rows, weigh->decay, gain, cache->history.weight);
+            return PC_OK;
+        };
+        return rows <= 48 ? weigh_with(k_q4_weigh<8>, 8) : weigh_with(k_q4_weigh<32>, 32);
+    }
     return PC_OK;
 }
 
@@ -909,9 +927,12 @@ extern "C" pc_status pc_q4_attend(pc_q4 *w, const pc_q4_cache *cache, const uint
     if (keys > w->max_tokens) return PC_ERR_CAPACITY;
     if (weigh && (!(w->parts & PC_Q4_WEIGH) || (!cache->history.weight && cache->history.n_tokens > 0))) return PC_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    // Many queries: the tensor-core kernel's rows of 128 are full, and the pass that turns the cache into 16 bits is paid once for all.
+    // Many query rows of a KV head: the pass that turns the cache into 16 bits is paid once for all, and the tensor-core kernel's tiles of 128 rows are filled.
+    // Frame route / kernels of few queries, us: 24 / 8 heads over 9,200 tokens 72 rows 42 / 41, 96 42 / 45, 126 44 / 57; over 25,328 72 97 / 74, 96 99 / 90,
+    // 126 99 / 110; 8 / 8 heads 64 rows 40 / 36 and 96 / 63, 100 40 / 50 and 95 / 96; over 537 tokens 24 rows 15 / 18, 96 17 / 23, 12 15 / 15.
     const size_t tile_rows = (size_t)(div_up(cache->anchors.n_tokens, 128) + div_up(cache->history.n_tokens, 128)) * 128;
-    if (n_q * ctx->group >= 128 && !valid && !weigh && w->v && ctx->attend_impl != 1 && tile_rows <= w->v_rows && tile_rows <= ctx->k_rot_rows)
+    const int many = keys <= 1024 ? 24 : 96;
+    if (n_q * ctx->group >= many && !valid && !weigh && w->v && ctx->attend_impl != 1 && tile_rows <= w->v_rows && tile_rows <= ctx->k_rot_rows)
         return attend_frame(w, cache, q, q_pos, n_q, out, lse, stream);
     int pass = n_q;
     if (weigh && cache->history.n_tokens > 0) {
