@@ -53,32 +53,45 @@ template <int OUT> __device__ __forceinline__ void store8(void *base, size_t ele
     }
 }
 
-// A pair turned by (cos, sin) with every product and sum rounded by itself, so that the codes follow from plain fp32 arithmetic
+// Two sums by one instruction
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tadd.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+// A pair turned by (cos, sin) with every product and sum rounded by itself, so that the codes follow from plain fp32 arithmetic (products and sums of two
+// at a time came out fused, with other bits)
 __device__ __forceinline__ void turn(float &x0, float &x1, float2 cs) {
     const float a = __fsub_rn(__fmul_rn(x0, cs.x), __fmul_rn(x1, cs.y)), b = __fadd_rn(__fmul_rn(x0, cs.y), __fmul_rn(x1, cs.x));
     x0 = a;
     x1 = b;
 }
 
+// Smallest and largest of three; NaN if one is NaN
+__device__ __forceinline__ float min3_nan(float a, float b, float c) { float d; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+
 // Codes, step and low of this thread's eight channels; all four lanes of a group get the same step and low.
-// Bound by instructions as much as by memory, so: values that fp16 cannot hold are looked for with one comparison a value and put right in a branch
-// that the warp takes together; (x - low) / step is clamped at zero by the multiplication's saturation, in units of 16 steps; and it is rounded and
-// turned into an integer by adding 1.5 * 2^19, whose last place is then a sixteenth (rounding and conversion instructions run at a quarter of the rate:
-// with them 24,193 tokens took 54 us).
+// Bound by instructions as much as by memory, so: smallest and largest by threes, NaN kept, so that one look at the two tells whether every value is one
+// that fp16 can hold (if not, the warp puts its values right in a branch); (x - low) / step is clamped at zero by the multiplication's saturation, in units of
+// 16 steps; it is rounded and turned into an integer by adding 1.5 * 2^19, whose last place is then a sixteenth (rounding and conversion
+// instructions run at a quarter of the rate: with them 24,193 tokens took 54 us); and the codes are put together by multiply-adds on the
+// sums' bits, from which what the eight 1.5 * 2^19 add up to is taken at the end.
 __device__ __forceinline__ uint32_t quantise8(float (&x)[8], __half &step, __half &low, bool &bad) {
-    bool off = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) off |= !(fabsf(x[i]) <= Q4_MAX);
+    const auto range = [&](float &lo, float &hi) {
+        lo = min3_nan(min3_nan(x[0], x[1], x[2]), min3_nan(x[3], x[4], x[5]), min3_nan(x[6], x[7], x[7]));
+        hi = max3_nan(max3_nan(x[0], x[1], x[2]), max3_nan(x[3], x[4], x[5]), max3_nan(x[6], x[7], x[7]));
+    };
+    float lo, hi;
+    range(lo, hi);
+    const bool off = !(lo >= -Q4_MAX && hi <= Q4_MAX);
     if (__any_sync(0xffffffffu, off)) {
         bad |= off;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = x[i] != x[i] ? 0.f : fminf(fmaxf(x[i], -Q4_MAX), Q4_MAX);
-    }
-    float lo = x[0], hi = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
+        range(lo, hi);
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
@@ -89,13 +102,16 @@ __device__ __forceinline__ uint32_t quantise8(float (&x)[8], __half &step, __hal
     const float l = __half2float(low);
     step = __float2half_rn(__fmul_rn(__fsub_rn(hi, l), 1.0f / 15.0f));
     const float s = __half2float(step), inv = s > 0.f ? __frcp_rn(s) * 0.0625f : 0.f;
+    constexpr uint32_t MAGIC = 0x49400000u;        // 1.5 * 2^19
     uint32_t word = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float c = fminf(__saturatef(__fmul_rn(__fsub_rn(x[i], l), inv)), 0.9375f);
-        word |= (__float_as_uint(__fadd_rn(c, 786432.f)) & 15u) << (4 * i);
+    for (int i = 6; i >= 0; i -= 2) {
+        const float2 d = add2(make_float2(x[i], x[i + 1]), make_float2(-l, -l));
+        const float2 c = add2(make_float2(fminf(__saturatef(__fmul_rn(d.x, inv)), 0.9375f), fminf(__saturatef(__fmul_rn(d.y, inv)), 0.9375f)),
+                              make_float2(__uint_as_float(MAGIC), __uint_as_float(MAGIC)));
+        word = (word * 16u + __float_as_uint(c.y)) * 16u + __float_as_uint(c.x);
     }
-    return word;
+    return word - MAGIC * 0x11111111u;
 }
 
 struct RowsArgs {
@@ -111,7 +127,7 @@ struct RowsArgs {
 };
 
 template <int D, bool F32>
-__global__ void __launch_bounds__(ROW_THREADS) k_q4_store(RowsArgs A, pc_rope_dev rope) {
+__global__ void __launch_bounds__(ROW_THREADS, F32 ? 2 : 4) k_q4_store(RowsArgs A, pc_rope_dev rope) {
     constexpr int LANES = D / 8, NG = D / Q4_GROUP;
     pc_grid_dep_launch();
     const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;

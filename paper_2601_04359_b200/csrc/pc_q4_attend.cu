@@ -67,6 +67,7 @@ struct Q4Params {
     float scale;                       // log2(e) / sqrt(d)
     int32_t *status;
     uint32_t wait_us;
+    uint32_t extra_tx;                 // test hook: bytes the first barrier expects beyond what is sent (0 = off)
 };
 
 struct JoinParams {
@@ -107,6 +108,13 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t mul_half(uint32_t a, uint32_t b) {
     const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// ON: two codes less 8, exactly (the codes lie `shift` bits up)
+template <bool ON> __device__ __forceinline__ uint32_t middle(uint32_t codes, int shift) {
+    if constexpr (!ON) return codes;
+    const uint32_t eight = 0x00080008u << shift;
+    const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&codes), *reinterpret_cast<const __half2 *>(&eight));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
@@ -285,7 +293,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             const uint32_t bar = full(slot);
             uint32_t dst = ring + slot * P.unit_bytes;
             const int y = (step0 + unit * UNIT) * Q4_STEP;
-            pc_mbar_expect_tx(bar, P.unit_bytes);
+            pc_mbar_expect_tx(bar, P.unit_bytes + (unit == 0 ? P.extra_tx : 0u));
             if (P.whole_rows) {
                 asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                              ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(0), "r"(bar) : "memory");
@@ -306,7 +314,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     };
     const int t = lane & 3, row = lane >> 2;
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
+    float W[F32 ? NG : 1][2];          // fp32 contexts, in the place of L: of the lane's own keys
     float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < (F32 ? NG : 1); ++i) W[i][0] = W[i][1] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * NG; ++i)
 #pragma unroll
@@ -328,6 +339,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     uint32_t at_v[NG / 2];
 #pragma unroll
     for (int g = 0; g < NG; g += 2) at_v[g / 2] = place(P.boxes_k, head * (D / 2) + (g + (lane >> 4)) * 16, km) + ((lane >> 3) & 1) * EIGHT;
+    const uint32_t at_vk = place(box_s, head * (D / 4) + 4 * NG, k0);              // fp32 contexts: steps and lows of the lane's two values
     const uint32_t at_mv = place(box_s, head * (D / 4) + (NG == 4 ? 16 : 0), km) + (lane >> 4) * EIGHT;
     const int r0 = block * ROWS + 2 * t, R = P.n_kv * P.n_rows;        // folded: lanes of the lo parts (t > 1) have no row
     char *queries = smem + P.queries_at + task * query_bytes(D, FOLD);
@@ -348,121 +360,138 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     const uint8_t *valid = hist ? P.valid : nullptr;
     float *logits = hist ? P.logits : nullptr;
     if (logits) logits += (size_t)(first_head + head) * P.n_rows + r0;
-        // Raw logits of a step's keys k0, k0 + 8 against columns 2 t, 2 t + 1: to be multiplied by f0, f1
-        const auto logits_of = [&](uint32_t rows, float (&S)[4]) {
-            uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la[4];
-            lds(rows + at_k, wa);
-            lds(rows + at_k + EIGHT, wb);
-            lds(rows + at_ks, sa);
-            lds(rows + at_ks + EIGHT, sb);
-            load_matrices<false>(rows + at_mk, la);
-            float E[4], C[NG][4];
-            mma_first(E, la[0], la[1], la[2], la[3], q_sum[0], q_sum[1]);
+    // Raw logits of a step's keys k0, k0 + 8 against columns 2 t, 2 t + 1: to be multiplied by f0, f1
+    const auto logits_of = [&](uint32_t rows, float (&S)[4]) {
+        uint32_t wa[NG], wb[NG], sa[NG / 2], sb[NG / 2], la[4];
+        lds(rows + at_k, wa);
+        lds(rows + at_k + EIGHT, wb);
+        lds(rows + at_ks, sa);
+        lds(rows + at_ks + EIGHT, sb);
+        load_matrices<false>(rows + at_mk, la);
+        float E[4], C[NG][4];
+        mma_first(E, la[0], la[1], la[2], la[3], q_sum[0], q_sum[1]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {            // channels in the low four bits of the code words' bytes, then in the high four
-                const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const uint32_t a0 = wa[g] & mask, a1 = wb[g] & mask, a2 = (wa[g] >> 8) & mask, a3 = (wb[g] >> 8) & mask;
-                    if (h == 0) mma_first(C[g], a0, a1, a2, a3, q_hi[2 * g][0], q_hi[2 * g][1]);
-                    else mma(C[g], a0, a1, a2, a3, q_hi[2 * g + 1][0], q_hi[2 * g + 1][1]);
-                    if constexpr (!FOLD) mma(C[g], a0, a1, a2, a3, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[j] = E[j] * (1.f / 16777216.f);
+        for (int h = 0; h < 2; ++h) {            // channels in the low four bits of the code words' bytes, then in the high four
+            const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
-                const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
-                S[0] = fmaf(fa, C[g][0], S[0]);
-                S[1] = fmaf(fa, C[g][1], S[1]);
-                S[2] = fmaf(fb, C[g][2], S[2]);
-                S[3] = fmaf(fb, C[g][3], S[3]);
+                const uint32_t a0 = wa[g] & mask, a1 = wb[g] & mask, a2 = (wa[g] >> 8) & mask, a3 = (wb[g] >> 8) & mask;
+                if (h == 0) mma_first(C[g], a0, a1, a2, a3, q_hi[2 * g][0], q_hi[2 * g][1]);
+                else mma(C[g], a0, a1, a2, a3, q_hi[2 * g + 1][0], q_hi[2 * g + 1][1]);
+                if constexpr (!FOLD) mma(C[g], a0, a1, a2, a3, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
             }
-            if constexpr (FOLD) {                    // both halves of the columns get the sum
+        }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) S[j] += __shfl_xor_sync(0xffffffffu, S[j], 2);
-            }
-        };
-        // Keys of a step that are there and not masked: a bit per row of the instruction
-        const auto look_at_mask = [&](int first, float (&S)[4], bool there, const uint8_t (&mask)[2]) {
-            const int n = there ? n_seg - first : 0;
-            const bool ok0 = k0 < n && mask[0] != 0, ok1 = k0 + 8 < n && mask[1] != 0;
-            if (!ok0) S[0] = S[1] = -INFINITY;
-            if (!ok1) S[2] = S[3] = -INFINITY;
-            // lane 4 i speaks for row i, lane 4 i + 1 for row i + 8
-            return __ballot_sync(0xffffffffu, t == 0 ? ok0 : ok1);
-        };
-        const auto leave_logits = [&](int first, const float (&S)[4]) {
-            const int n = n_seg - first;
-            float *to = logits + (size_t)(first + k0) * R;
-            if (k0 < n) {
-                if (r0 < P.n_rows) to[0] = S[0] * f0;
-                if (r0 + 1 < P.n_rows) to[1] = S[1] * f1;
-            }
-            if (k0 + 8 < n) {
-                to += (size_t)8 * R;
-                if (r0 < P.n_rows) to[0] = S[2] * f0;
-                if (r0 + 1 < P.n_rows) to[1] = S[3] * f1;
-            }
-        };
-        // O += P V of a step, p = the probabilities of S's keys and columns
-        const auto add_values = [&](uint32_t rows, const float (&p)[4], bool all, uint32_t seen) {
-            uint32_t steps[4][NG / 2], codes[NG / 2][4], lows[4];        // codes: a group's four of each key, of two keys a word
+        for (int j = 0; j < 4; ++j) S[j] = E[j] * (1.f / 16777216.f);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
+        for (int g = 0; g < NG; ++g) {
+            const float2 pa = halves(sa[g / 2]), pb = halves(sb[g / 2]);
+            const float fa = (g & 1) ? pa.y : pa.x, fb = (g & 1) ? pb.y : pb.x;
+            S[0] = fmaf(fa, C[g][0], S[0]);
+            S[1] = fmaf(fa, C[g][1], S[1]);
+            S[2] = fmaf(fb, C[g][2], S[2]);
+            S[3] = fmaf(fb, C[g][3], S[3]);
+        }
+        if constexpr (FOLD) {                    // both halves of the columns get the sum
 #pragma unroll
-            for (int g = 0; g < NG / 2; ++g) load_matrices<true>(rows + at_v[g], codes[g]);
-            load_matrices<true>(rows + at_mv, lows);
-            if (!all) {                              // what lies in the place of a masked key may be anything
+            for (int j = 0; j < 4; ++j) S[j] += __shfl_xor_sync(0xffffffffu, S[j], 2);
+        }
+    };
+    // Keys of a step that are there and not masked: a bit per row of the instruction
+    const auto look_at_mask = [&](int first, float (&S)[4], bool there, const uint8_t (&mask)[2]) {
+        const int n = there ? n_seg - first : 0;
+        const bool ok0 = k0 < n && mask[0] != 0, ok1 = k0 + 8 < n && mask[1] != 0;
+        if (!ok0) S[0] = S[1] = -INFINITY;
+        if (!ok1) S[2] = S[3] = -INFINITY;
+        // lane 4 i speaks for row i, lane 4 i + 1 for row i + 8
+        return __ballot_sync(0xffffffffu, t == 0 ? ok0 : ok1);
+    };
+    const auto leave_logits = [&](int first, const float (&S)[4]) {
+        const int n = n_seg - first;
+        float *to = logits + (size_t)(first + k0) * R;
+        if (k0 < n) {
+            if (r0 < P.n_rows) to[0] = S[0] * f0;
+            if (r0 + 1 < P.n_rows) to[1] = S[1] * f1;
+        }
+        if (k0 + 8 < n) {
+            to += (size_t)8 * R;
+            if (r0 < P.n_rows) to[0] = S[2] * f0;
+            if (r0 + 1 < P.n_rows) to[1] = S[3] * f1;
+        }
+    };
+    // O += P V of a step, p = the probabilities of S's keys and columns
+    const auto add_values = [&](uint32_t rows, const float (&p)[4], bool all, uint32_t seen) {
+        uint32_t steps[4][NG / 2], codes[NG / 2][4], lows[4];        // codes: a group's four of each key, of two keys a word
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!((seen >> (4 * (2 * t + (j & 1)) + (j >> 1))) & 1u)) {
+        for (int j = 0; j < 4; ++j) lds(rows + (j & 1 ? at_vsb : at_vsa) + (j >> 1) * EIGHT, steps[j]);
+#pragma unroll
+        for (int g = 0; g < NG / 2; ++g) load_matrices<true>(rows + at_v[g], codes[g]);
+        if constexpr (!F32) load_matrices<true>(rows + at_mv, lows);
+        if (!all) {                              // what lies in the place of a masked key may be anything
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (!((seen >> (4 * (2 * t + (j & 1)) + (j >> 1))) & 1u)) {
+                    if constexpr (!F32) {
                         lows[j & 2] &= (j & 1) ? 0x0000FFFFu : 0xFFFF0000u;
                         lows[(j & 2) + 1] = lows[j & 2];
-#pragma unroll
-                        for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
                     }
-            }
-            uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
-            ph[0] = pack_half(p[0], p[1]);
-            ph[1] = pack_half(p[2], p[3]);
-            if constexpr (F32) {
-                const float2 a = halves(ph[0]), b = halves(ph[1]);
-                pl[0] = transpose8(pack_half(p[0] - a.x, p[1] - a.y));
-                pl[1] = transpose8(pack_half(p[2] - b.x, p[3] - b.y));
-            }
-            ph[0] = transpose8(ph[0]);
-            ph[1] = transpose8(ph[1]);
-            mma(L, lows[0], lows[1], lows[2], lows[3], ph[0], ph[1]);
-            if constexpr (F32) mma(L, lows[0], lows[1], lows[2], lows[3], pl[0], pl[1]);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
-                const uint32_t ta = codes[g / 2][2 * (g & 1)], tb = codes[g / 2][2 * (g & 1) + 1];
-                const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
-                const uint32_t ya = ta >> 8, yb = tb >> 8;
-                const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
-                const uint32_t c0 = ya & 0x000F000Fu, c1 = ya & 0x00F000F0u, c2 = yb & 0x000F000Fu, c3 = yb & 0x00F000F0u;
-                if constexpr (F32) {
-                    // probability times step in fp32 from the two parts, split again
-                    const float2 sa = halves(qa), sb = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
-                    const float e0 = (xh.x + xl.x) * sa.x, e1 = (xh.y + xl.y) * sa.y, e2 = (yh.x + yl.x) * sb.x, e3 = (yh.y + yl.y) * sb.y;
-                    const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
-                    const float2 g0 = halves(h0), g1 = halves(h1);
-                    const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
-                    mma(O[2 * g], a0, a1, a2, a3, w0, w1);
-                    mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
-                    mma(O[2 * g], a0, a1, a2, a3, h0, h1);
-                    mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
-                } else {
-                    const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
-                    mma(O[2 * g], a0, a1, a2, a3, h0, h1);
-                    mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                    for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
+                }
+        }
+        uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
+        ph[0] = pack_half(p[0], p[1]);
+        ph[1] = pack_half(p[2], p[3]);
+        if constexpr (F32) {
+            const float2 a = halves(ph[0]), b = halves(ph[1]);
+            pl[0] = transpose8(pack_half(p[0] - a.x, p[1] - a.y));
+            pl[1] = transpose8(pack_half(p[2] - b.x, p[3] - b.y));
+            // Values around their group's middle, v = (low + 8 step) + step (code - 8): sums over codes and sums over lows would each be many times
+            // larger than their difference, the output, which an fp32 output shows
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t st[NG / 2], lo[NG / 2];
+                lds(rows + at_vk + i * EIGHT, st);
+                lds(rows + at_vk + i * EIGHT + 2 * NG, lo);
+                if (!((seen >> (4 * row + i)) & 1u)) continue;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float2 s2 = halves(st[g / 2]), l2 = halves(lo[g / 2]);
+                    const float mid = fmaf(8.f, (g & 1) ? s2.y : s2.x, (g & 1) ? l2.y : l2.x);
+                    W[g][0] = fmaf(p[2 * i], mid, W[g][0]);
+                    W[g][1] = fmaf(p[2 * i + 1], mid, W[g][1]);
                 }
             }
-        };
+        }
+        ph[0] = transpose8(ph[0]);
+        ph[1] = transpose8(ph[1]);
+        if constexpr (!F32) mma(L, lows[0], lows[1], lows[2], lows[3], ph[0], ph[1]);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const uint32_t pick = (g & 1) ? 0x7632u : 0x5410u;
+            const uint32_t ta = codes[g / 2][2 * (g & 1)], tb = codes[g / 2][2 * (g & 1) + 1];
+            const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
+            const uint32_t ya = ta >> 8, yb = tb >> 8;
+            const uint32_t a0 = middle<F32>(ta & 0x000F000Fu, 0), a1 = middle<F32>(ta & 0x00F000F0u, 4), a2 = middle<F32>(tb & 0x000F000Fu, 0), a3 = middle<F32>(tb & 0x00F000F0u, 4);
+            const uint32_t c0 = middle<F32>(ya & 0x000F000Fu, 0), c1 = middle<F32>(ya & 0x00F000F0u, 4), c2 = middle<F32>(yb & 0x000F000Fu, 0), c3 = middle<F32>(yb & 0x00F000F0u, 4);
+            if constexpr (F32) {
+                // probability times step in fp32 from the two parts, split again
+                const float2 sa = halves(qa), sb = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
+                const float e0 = (xh.x + xl.x) * sa.x, e1 = (xh.y + xl.y) * sa.y, e2 = (yh.x + yl.x) * sb.x, e3 = (yh.y + yl.y) * sb.y;
+                const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
+                const float2 g0 = halves(h0), g1 = halves(h1);
+                const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
+                mma(O[2 * g], a0, a1, a2, a3, w0, w1);
+                mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
+                mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+            } else {
+                const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
+                mma(O[2 * g], a0, a1, a2, a3, h0, h1);
+                mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+            }
+        }
+    };
     // The warp's units: every subs-th, in the slots of its part of the keys (sub, sub + subs, ...) in turn.  `slots` is a multiple of `subs`, so
     // the barriers of a slot are only waited on by warps that have seen every phase before (a wait by parity cannot tell a phase from the one
     // two before or behind it).  The last of the warps that share a unit to leave it fetches what follows in its slot.
@@ -481,57 +510,56 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 if (at + 8 * i < n_seg) mask[i / 2][i & 1] = __ldg(valid + at + 8 * i);
         }
         if (!wait_for(full(slot), phase)) break;
-            const uint32_t rows = ring + slot * P.unit_bytes;
-            const uint32_t rows1 = rows + Q4_STEP * BOX;
+        if (works) {
+            const uint32_t rows = ring + slot * P.unit_bytes, rows1 = rows + Q4_STEP * BOX;
             // (of one step: the second one's place holds tokens of the next CTA, or zeros; its logits count as masked)
             const bool two = unit * UNIT + 1 < n_steps;
             const int first = (step0 + unit * UNIT) * Q4_STEP;
             float S0[4], S1[4];
-            if (works) {
-                logits_of(rows, S0);
-                logits_of(rows1, S1);
+            logits_of(rows, S0);
+            logits_of(rows1, S1);
+            uint32_t seen0 = 0xffffffffu, seen1 = 0xffffffffu;
+            const bool all = !valid && two && first + UNIT * Q4_STEP <= n_seg;
+            if (!all) {
+                seen0 = look_at_mask(first, S0, true, mask[0]);
+                seen1 = look_at_mask(first + Q4_STEP, S1, two, mask[1]);
             }
-            if (works) {
-                uint32_t seen0 = 0xffffffffu, seen1 = 0xffffffffu;
-                const bool all = !valid && two && first + UNIT * Q4_STEP <= n_seg;
-                if (!all) {
-                    seen0 = look_at_mask(first, S0, true, mask[0]);
-                    seen1 = look_at_mask(first + Q4_STEP, S1, two, mask[1]);
-                }
-                if (logits) {
-                    leave_logits(first, S0);
-                    if (two) leave_logits(first + Q4_STEP, S1);
-                }
-                // ---- softmax: maximum of the keys of each column
-                float x0 = fmaxf(fmaxf(S0[0], S0[2]), fmaxf(S1[0], S1[2])), x1 = fmaxf(fmaxf(S0[1], S0[3]), fmaxf(S1[1], S1[3]));
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
-                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
-                }
-                x0 = fmaf(x0, f0, -P_LOG);
-                x1 = fmaf(x1, f1, -P_LOG);
-                if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
-                    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1), c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1);
-                    m0 = n0;
-                    m1 = n1;
-                    l0 *= c0;
-                    l1 *= c1;
-#pragma unroll
-                    for (int i = 0; i < 2 * NG; ++i) { O[i][0] *= c0; O[i][1] *= c1; O[i][2] *= c0; O[i][3] *= c1; }
-                    L[0] *= c0;
-                    L[1] *= c1;
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    S0[j] = exp2_fast(fmaf(S0[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
-                    S1[j] = exp2_fast(fmaf(S1[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
-                }
-                l0 += (S0[0] + S0[2]) + (S1[0] + S1[2]);
-                l1 += (S0[1] + S0[3]) + (S1[1] + S1[3]);
-                add_values(rows, S0, all, seen0);
-                add_values(rows1, S1, all, seen1);
+            if (logits) {
+                leave_logits(first, S0);
+                if (two) leave_logits(first + Q4_STEP, S1);
             }
+            // ---- softmax: maximum of the keys of each column
+            float x0 = fmaxf(fmaxf(S0[0], S0[2]), fmaxf(S1[0], S1[2])), x1 = fmaxf(fmaxf(S0[1], S0[3]), fmaxf(S1[1], S1[3]));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
+                x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
+            }
+            x0 = fmaf(x0, f0, -P_LOG);
+            x1 = fmaf(x1, f1, -P_LOG);
+            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
+                const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1), c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1);
+                m0 = n0;
+                m1 = n1;
+                l0 *= c0;
+                l1 *= c1;
+#pragma unroll
+                for (int i = 0; i < 2 * NG; ++i) { O[i][0] *= c0; O[i][1] *= c1; O[i][2] *= c0; O[i][3] *= c1; }
+                L[0] *= c0;
+                L[1] *= c1;
+#pragma unroll
+                for (int i = 0; i < (F32 ? NG : 1); ++i) { W[i][0] *= c0; W[i][1] *= c1; }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                S0[j] = exp2_fast(fmaf(S0[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
+                S1[j] = exp2_fast(fmaf(S1[j], j & 1 ? f1 : f0, j & 1 ? -m1 : -m0));
+            }
+            l0 += (S0[0] + S0[2]) + (S1[0] + S1[2]);
+            l1 += (S0[1] + S0[3]) + (S1[1] + S1[3]);
+            add_values(rows, S0, all, seen0);
+            add_values(rows1, S1, all, seen1);
+        }
         __syncwarp();
         int n = 0;
         if (lane == 0) asm volatile("atom.shared.acq_rel.cta.add.u32 %0, [%1], 1;" : "=r"(n) : "r"(left(slot)) : "memory");
@@ -572,7 +600,19 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
         float *mine = parts + (warp * ROWS + 2 * t) * PITCH + 4 * row;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const float w0 = __shfl_sync(0xffffffffu, L[0], (8 - NG + g) * 4 + t), w1 = __shfl_sync(0xffffffffu, L[1], (8 - NG + g) * 4 + t);
+            float w0, w1;
+            if constexpr (F32) {
+                w0 = W[g][0];
+                w1 = W[g][1];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    w0 += __shfl_xor_sync(0xffffffffu, w0, o);
+                    w1 += __shfl_xor_sync(0xffffffffu, w1, o);
+                }
+            } else {
+                w0 = __shfl_sync(0xffffffffu, L[0], (8 - NG + g) * 4 + t);
+                w1 = __shfl_sync(0xffffffffu, L[1], (8 - NG + g) * 4 + t);
+            }
             constexpr float A = 16777216.f, B = 1048576.f;      // the codes' powers of two
             *reinterpret_cast<float4 *>(mine + g * Q4_GROUP) =
                 make_float4(fmaf(O[2 * g][0], A, w0), fmaf(O[2 * g][2], B, w0), fmaf(O[2 * g + 1][0], A, w0), fmaf(O[2 * g + 1][2], B, w0));
@@ -777,6 +817,7 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     P.scale = pc_q_rot_scale(D.head_dim);
     P.status = ctx->status;
     P.wait_us = ctx->wait_limit_us;
+    P.extra_tx = ctx->test_extra_tx;
     P.part_o = w->part_o;
     P.part_ml = w->part_ml;
     P.logits = weigh && P.n[1] > 0 ? w->logits : nullptr;
