@@ -92,6 +92,10 @@ __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // Four 8 x 8 matrices of 16-bit values, a row at each lane's address (eight lanes a matrix); TRANS: transposed
 template <bool TRANS> __device__ __forceinline__ void load_matrices(uint32_t a, uint32_t (&x)[4]) {
     if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(a));
@@ -115,6 +119,12 @@ template <bool ON> __device__ __forceinline__ uint32_t middle(uint32_t codes, in
     if constexpr (!ON) return codes;
     const uint32_t eight = 0x00080008u << shift;
     const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&codes), *reinterpret_cast<const __half2 *>(&eight));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// Two codes less 8 in bf16: in the last places of 128 + code, less 136
+__device__ __forceinline__ uint32_t middle_bf16(uint32_t codes) {
+    const uint32_t x = (codes & 0x000F000Fu) | 0x43004300u, y = 0x43084308u;
+    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
@@ -210,9 +220,9 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 x[c + 1] = y.y * P.scale;
                 most = fmaxf(most, fmaxf(fabsf(x[c]), fabsf(x[c + 1])));
             }
-            // the row's largest value to 2^9 .. 2^10: sums over 32 channels stay in fp16's range
+            // the row's largest value to 2^6 .. 2^7: eight times a sum over 32 channels stays in fp16's range
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-            const int e = min(100, max(-118, 9 - ((int)(__float_as_uint(most) >> 23) - 127)));
+            const int e = min(100, max(-118, 6 - ((int)(__float_as_uint(most) >> 23) - 127)));
             const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -225,8 +235,8 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 at16[0] = hi;
                 at16[FOLD ? 32 : 4 * NG * 64] = __float2half_rn(y - __half2float(hi));
             }
-            // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps and
-            // are zero), a second fp16 part at the same places of the other eight
+            // sums over the groups, which meet the lows: indices NG .. 2 NG - 1 of the instruction's first eight (the others meet the steps: zero, or,
+            // where codes are taken around 8, eight times the sums), a second fp16 part at the same places of the other eight
 #pragma unroll
             for (int o = 1; o < Q4_GROUP / CH; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
             constexpr int SUMS = FOLD ? 4 * NG : 8 * NG, SECOND = FOLD ? 16 : 32;       // the second part: the column's other half, or the next word
@@ -242,6 +252,10 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                 const float2 back = halves(h);
                 sums[NG / 2 + g / 2] = h;
                 sums[SECOND + NG / 2 + g / 2] = pack_half(total - back.x, next - back.y);
+                if constexpr (F32) {
+                    sums[g / 2] = pack_half(8.f * back.x, 8.f * back.y);
+                    sums[SECOND + g / 2] = pack_half(8.f * (total - back.x), 8.f * (next - back.y));
+                }
             }
             if (lane == 0) reinterpret_cast<float *>(to + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
         }
@@ -375,7 +389,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             const uint32_t mask = h ? 0x00F000F0u : 0x000F000Fu;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                const uint32_t a0 = wa[g] & mask, a1 = wb[g] & mask, a2 = (wa[g] >> 8) & mask, a3 = (wb[g] >> 8) & mask;
+                const uint32_t a0 = middle<F32>(wa[g] & mask, 4 * h), a1 = middle<F32>(wb[g] & mask, 4 * h);
+                const uint32_t a2 = middle<F32>((wa[g] >> 8) & mask, 4 * h), a3 = middle<F32>((wb[g] >> 8) & mask, 4 * h);
                 if (h == 0) mma_first(C[g], a0, a1, a2, a3, q_hi[2 * g][0], q_hi[2 * g][1]);
                 else mma(C[g], a0, a1, a2, a3, q_hi[2 * g + 1][0], q_hi[2 * g + 1][1]);
                 if constexpr (!FOLD) mma(C[g], a0, a1, a2, a3, q_lo[2 * g + h][0], q_lo[2 * g + h][1]);
@@ -440,12 +455,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 }
         }
         uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
-        ph[0] = pack_half(p[0], p[1]);
-        ph[1] = pack_half(p[2], p[3]);
+        constexpr float UP = F32 ? 8192.f : 1.f; // the second part of a small probability would be a subnormal number
+        ph[0] = pack_half(p[0] * UP, p[1] * UP);
+        ph[1] = pack_half(p[2] * UP, p[3] * UP);
         if constexpr (F32) {
             const float2 a = halves(ph[0]), b = halves(ph[1]);
-            pl[0] = transpose8(pack_half(p[0] - a.x, p[1] - a.y));
-            pl[1] = transpose8(pack_half(p[2] - b.x, p[3] - b.y));
+            pl[0] = transpose8(pack_half(p[0] * UP - a.x, p[1] * UP - a.y));
+            pl[1] = transpose8(pack_half(p[2] * UP - b.x, p[3] * UP - b.y));
             // Values around their group's middle, v = (low + 8 step) + step (code - 8): sums over codes and sums over lows would each be many times
             // larger than their difference, the output, which an fp32 output shows
 #pragma unroll
@@ -472,20 +488,23 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             const uint32_t ta = codes[g / 2][2 * (g & 1)], tb = codes[g / 2][2 * (g & 1) + 1];
             const uint32_t qa = __byte_perm(steps[0][g / 2], steps[1][g / 2], pick), qb = __byte_perm(steps[2][g / 2], steps[3][g / 2], pick);
             const uint32_t ya = ta >> 8, yb = tb >> 8;
-            const uint32_t a0 = middle<F32>(ta & 0x000F000Fu, 0), a1 = middle<F32>(ta & 0x00F000F0u, 4), a2 = middle<F32>(tb & 0x000F000Fu, 0), a3 = middle<F32>(tb & 0x00F000F0u, 4);
-            const uint32_t c0 = middle<F32>(ya & 0x000F000Fu, 0), c1 = middle<F32>(ya & 0x00F000F0u, 4), c2 = middle<F32>(yb & 0x000F000Fu, 0), c3 = middle<F32>(yb & 0x00F000F0u, 4);
             if constexpr (F32) {
-                // probability times step in fp32 from the two parts, split again
+                // probability times step in fp32 from the two parts, then in three bf16 parts, whose range no step leaves
                 const float2 sa = halves(qa), sb = halves(qb), xh = halves(ph[0]), yh = halves(ph[1]), xl = halves(pl[0]), yl = halves(pl[1]);
-                const float e0 = (xh.x + xl.x) * sa.x, e1 = (xh.y + xl.y) * sa.y, e2 = (yh.x + yl.x) * sb.x, e3 = (yh.y + yl.y) * sb.y;
-                const uint32_t h0 = pack_half(e0, e1), h1 = pack_half(e2, e3);
-                const float2 g0 = halves(h0), g1 = halves(h1);
-                const uint32_t w0 = pack_half(e0 - g0.x, e1 - g0.y), w1 = pack_half(e2 - g1.x, e3 - g1.y);
-                mma(O[2 * g], a0, a1, a2, a3, w0, w1);
-                mma(O[2 * g + 1], c0, c1, c2, c3, w0, w1);
-                mma(O[2 * g], a0, a1, a2, a3, h0, h1);
-                mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
+                float e[4] = {(xh.x + xl.x) * (sa.x / UP), (xh.y + xl.y) * (sa.y / UP), (yh.x + yl.x) * (sb.x / UP), (yh.y + yl.y) * (sb.y / UP)};
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    const uint32_t h0 = pc_pack_bf16(e[0], e[1]), h1 = pc_pack_bf16(e[2], e[3]);
+                    mma_bf16(O[2 * g], middle_bf16(ta), middle_bf16(ta >> 4), middle_bf16(tb), middle_bf16(tb >> 4), h0, h1);
+                    mma_bf16(O[2 * g + 1], middle_bf16(ya), middle_bf16(ya >> 4), middle_bf16(yb), middle_bf16(yb >> 4), h0, h1);
+                    e[0] -= pc_bf16_lo(h0);
+                    e[1] -= pc_bf16_hi(h0);
+                    e[2] -= pc_bf16_lo(h1);
+                    e[3] -= pc_bf16_hi(h1);
+                }
             } else {
+                const uint32_t a0 = ta & 0x000F000Fu, a1 = ta & 0x00F000F0u, a2 = tb & 0x000F000Fu, a3 = tb & 0x00F000F0u;
+                const uint32_t c0 = ya & 0x000F000Fu, c1 = ya & 0x00F000F0u, c2 = yb & 0x000F000Fu, c3 = yb & 0x00F000F0u;
                 const uint32_t h0 = mul_half(ph[0], qa), h1 = mul_half(ph[1], qb);
                 mma(O[2 * g], a0, a1, a2, a3, h0, h1);
                 mma(O[2 * g + 1], c0, c1, c2, c3, h0, h1);
@@ -613,7 +632,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 w0 = __shfl_sync(0xffffffffu, L[0], (8 - NG + g) * 4 + t);
                 w1 = __shfl_sync(0xffffffffu, L[1], (8 - NG + g) * 4 + t);
             }
-            constexpr float A = 16777216.f, B = 1048576.f;      // the codes' powers of two
+            constexpr float A = F32 ? 1.f : 16777216.f, B = F32 ? 1.f : 1048576.f;      // the codes' powers of two
             *reinterpret_cast<float4 *>(mine + g * Q4_GROUP) =
                 make_float4(fmaf(O[2 * g][0], A, w0), fmaf(O[2 * g][2], B, w0), fmaf(O[2 * g + 1][0], A, w0), fmaf(O[2 * g + 1][2], B, w0));
             *reinterpret_cast<float4 *>(mine + PITCH + g * Q4_GROUP) =
@@ -875,7 +894,7 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
     return PC_OK;
 }
 
-// The whole cache in 16 bits, then the context's tensor-core attention
+// The whole cache in fp16, then the tensor-core attention kernel
 pc_status attend_frame(pc_q4 *w, const pc_q4_cache *cache, const void *q, const int32_t *q_pos, int n_q, void *out, float *lse, cudaStream_t stream) {
     pc_ctx *ctx = w->ctx;
     const size_t row = (size_t)ctx->desc.n_kv_heads * ctx->desc.head_dim * sizeof(__nv_bfloat16);

@@ -4,7 +4,7 @@ Tolerances.  A logit of the kernel is off by what its sums round: the query's tw
 exact, and no more than 48 additions in fp32, each 2^-23 of a partial sum that is at most S = sum |q| (step code + |low|) / sqrt(d), so
 delta <= (48 * 2^-23 + 2^-21) S.  Probabilities are then off by 2 delta + 2^-18 relative (exponential, sums, normaliser).  Outputs add the
 roundings of probability times step: two to fp16 in bf16 contexts (2^-10 in all, of sum p (step code + |low|)), 2^-20 in fp32 ones, where the
-probability and the product are each held in two parts; and half a unit of the output's type."""
+probability and the product are each held in parts; and half a unit of the output's type."""
 from __future__ import annotations
 
 import numpy as np
