@@ -431,10 +431,12 @@ pc_status pc_q4_destroy(pc_q4 *w);
  *   weigh host or NULL: the weights of the history are brought up to date in the same call,
  *     weight_j <- decay * weight_j + gain * (mean over queries and heads of the probability of token j).
  *   out device [n_q][Hq][d]; lse device [n_q][Hq] fp32 or NULL.
+ * A query row that holds a NaN or an infinity gives NaN, in its own head alone.
  * Sums and softmax statistics are fp32.  Queries go to the multiply-adds as two fp16 parts (22 bits), probabilities times steps as one fp16
  * number (bf16 contexts) or three bf16 parts (fp32).  Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
  * on a context with tensor-core attention and a workspace with PC_Q4_FRAMES, instead turn the cache into fp16 once and run a tensor-core kernel
- * on it (keys, values and probabilities rounded to fp16, queries in two parts; max_keys of the context bounds the tokens); they use the
+ * on it (keys, values and probabilities rounded to fp16, queries in two parts, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger
+ * ones are held there, with PC_ERR_INVALID_ARG in the status word; max_keys of the context bounds the tokens); they use the
  * context's rotated-key scratch as pc_attend_frame does, and what pc_attend_prepare fixed is dropped; pc_attend_mass cannot follow them.
  * Calls that share a workspace have to be ordered on the GPU; with weights, a call's queries go in passes that the workspace's logits hold.
  * Errors: PC_ERR_INVALID_ARG (no keys at all, weigh without PC_Q4_WEIGH or without weights), PC_ERR_CAPACITY, PC_ERR_CUDA. */

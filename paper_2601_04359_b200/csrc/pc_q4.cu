@@ -36,12 +36,18 @@ template <bool F32> __device__ __forceinline__ void unpack8(const Eight<F32> &e,
         for (int i = 0; i < 4; ++i) { x[2 * i] = pc_bf16_lo(w[i]); x[2 * i + 1] = pc_bf16_hi(w[i]); }
     }
 }
+// Smallest and largest of three; NaN if one is NaN
+__device__ __forceinline__ float min3_nan(float a, float b, float c) { float d; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+// Into fp16's range; NaN stays
+__device__ __forceinline__ float into_f16(float x) { return min3_nan(max3_nan(x, -Q4_MAX, -Q4_MAX), Q4_MAX, Q4_MAX); }
+
 enum { OUT_BF16 = 0, OUT_F32 = 1, OUT_F16 = 2 };
 template <int OUT> __device__ __forceinline__ void store8(void *base, size_t elem, const float (&x)[8]) {
     if constexpr (OUT == OUT_F16) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pc_pack_f16(fminf(fmaxf(x[2 * i], -Q4_MAX), Q4_MAX), fminf(fmaxf(x[2 * i + 1], -Q4_MAX), Q4_MAX));
+        for (int i = 0; i < 4; ++i) w[i] = pc_pack_f16(into_f16(x[2 * i]), into_f16(x[2 * i + 1]));
         *reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2) = make_uint4(w[0], w[1], w[2], w[3]);
     } else if constexpr (OUT == OUT_F32) {
         uint4 *p = reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 4);
@@ -68,10 +74,6 @@ __device__ __forceinline__ void turn(float &x0, float &x1, float2 cs) {
     x0 = a;
     x1 = b;
 }
-
-// Smallest and largest of three; NaN if one is NaN
-__device__ __forceinline__ float min3_nan(float a, float b, float c) { float d; asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
-__device__ __forceinline__ float max3_nan(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 
 // Codes, step and low of this thread's eight channels; all four lanes of a group get the same step and low.
 // Bound by instructions as much as by memory, so: smallest and largest by threes, NaN kept, so that one look at the two tells whether every value is one
@@ -130,8 +132,8 @@ template <int D, bool F32>
 __global__ void __launch_bounds__(ROW_THREADS, F32 ? 2 : 4) k_q4_store(RowsArgs A, pc_rope_dev rope) {
     constexpr int LANES = D / 8, NG = D / Q4_GROUP;
     pc_grid_dep_launch();
-    const int unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
-    const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
+    const unsigned unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES;      // unsigned: 2^32 threads are more rows than memory holds
+    const int u = threadIdx.x % LANES, token = (int)(unit / A.slices), h0 = (int)(unit % A.slices) * HEADS;
     const bool live = token < A.n;                 // lanes of a warp stay together for the shuffles
     const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
     const int g = u >> 2, t = u & 3;
@@ -182,10 +184,10 @@ __global__ void __launch_bounds__(ROW_THREADS, F32 ? 2 : 4) k_q4_store(RowsArgs 
 
 // FROM_POS: keys turned back from (t + t_shift, h, w) to how they came in; else from t_shift alone (they stay rotated at their positions)
 template <int D, int OUT, bool FROM_POS>
-__device__ __forceinline__ void load_rows(const RowsArgs &A, const pc_rope_dev &rope, int block) {
+__device__ __forceinline__ void load_rows(const RowsArgs &A, const pc_rope_dev &rope, unsigned block) {
     constexpr int LANES = D / 8, NG = D / Q4_GROUP;
-    const int unit = (block * ROW_THREADS + threadIdx.x) / LANES, u = threadIdx.x % LANES;
-    const int token = unit / A.slices, h0 = unit % A.slices * HEADS;
+    const unsigned unit = (block * ROW_THREADS + threadIdx.x) / LANES;
+    const int u = threadIdx.x % LANES, token = (int)(unit / A.slices), h0 = (int)(unit % A.slices) * HEADS;
     const bool live = token < A.n;
     const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
     const int g = u >> 2, t = u & 3;
@@ -257,21 +259,28 @@ struct QueryArgs {
     size_t second;              // where the second parts begin
     int32_t *status;
 };
-// Queries of 128 channels, rotated, times log2(e) / sqrt(d), in two fp16 parts: eight channels a thread
+// Queries of 128 channels, rotated, times log2(e) / sqrt(d), in two fp16 parts: eight channels a thread.  Beyond +-65504 after that: held there and
+// recorded; infinities and NaN become NaN.
 __device__ __forceinline__ void make_queries(const QueryArgs &A, const pc_rope_dev &rope, int block) {
     const int c = block * ROW_THREADS + threadIdx.x;
     if (c >= A.chunks) return;
     float x[8], r[8];
     unpack8<false>(load8<false>(A.q, (size_t)c * 8), x);
     const int4 p = __ldg(reinterpret_cast<const int4 *>(A.pos) + c / A.chunks_row);
-    bool bad = false;
+    bool bad = false, off = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 y = pc_rotate(x[2 * i], x[2 * i + 1], pc_rope_cs_clamped(rope, c % 16 * 4 + i, p.x, p.y, p.z, bad));
-        x[2 * i] = fminf(fmaxf(y.x * A.scale, -Q4_MAX), Q4_MAX);
-        x[2 * i + 1] = fminf(fmaxf(y.y * A.scale, -Q4_MAX), Q4_MAX);
+        x[2 * i] = y.x * A.scale;
+        x[2 * i + 1] = y.y * A.scale;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        off |= fabsf(x[i]) > Q4_MAX;
+        x[i] = into_f16(x[i]) + (x[i] - x[i]);     // + 0, or NaN
     }
     if (bad) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_POS);
+    if (off) pc_flag(A.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_RANGE);
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = x[i] - __half2float(__float2half_rn(x[i]));
     store8<OUT_F16>(A.to, (size_t)c * 8, x);

@@ -386,3 +386,28 @@ def test_positions_outside_the_rotary_table_are_recorded():
     c.hist.t_shift = 1                                   # 600 is outside
     pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos)
     assert pc.pc_poll_status(c.ctx) == pc.PC_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("n_q,frames", [(1, False), (5, False), (40, True)])
+def test_queries_that_are_not_finite_stay_so_and_alone(n_q, frames):
+    c = Case("lumos", 96, 384, n_q, shift=8, frames=frames)
+    clean = _np(pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos))
+    c.q[n_q - 1, 2, 7] = float("nan")
+    c.q[n_q // 2, 11, 90] = float("-inf")
+    got = _np(pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos))
+    off = np.zeros(got.shape[:2], bool)
+    off[n_q - 1, 2] = off[n_q // 2, 11] = True
+    assert np.isnan(got[off]).all()
+    # the rows beside them may be scaled at another step: one rounding of the output and of the probabilities
+    assert (np.abs(got - clean)[~off] <= 2.0 ** -7 * np.abs(clean[~off]) + 2.0 ** -9).all()
+    pc.pc_poll_status(c.ctx)
+
+
+def test_frame_queries_beyond_half_precision_are_recorded():
+    c = Case("lumos", 96, 384, 40, frames=True)
+    pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos)
+    assert pc.pc_poll_status(c.ctx) == pc.PC_OK
+    c.q[3, 5, 0] = 1e8
+    out = pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos)
+    assert pc.pc_poll_status(c.ctx) == pc.PC_ERR_INVALID_ARG
+    assert torch.isfinite(out).all()
