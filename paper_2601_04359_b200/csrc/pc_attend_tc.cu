@@ -265,8 +265,9 @@ __device__ __noinline__ void merge_left(const TcParams &P, uint32_t call, int w,
 // FINE: queries, keys, values and probabilities in fp16 instead of bf16 and the queries in two parts, whose products with the keys add up in the same
 // columns (22 bits of a query, so that the lse is good to fp32's accuracy over thousands of keys).  The second part leaves room for three tiles
 // of keys or values, which are fetched in the order K(0) K(1) V(0) K(2) V(1) K(3) V(2) ... into the three places in turn: K(step + 1) lies
-// there a step ahead, and V(step) comes where K(step) has been read, under the step's softmax and the next Q K^T.  (One place for keys and two for
-// values: Q K^T waited for its keys, 4,000 cycles a step instead of the tensor core's 3,072.)
+// there a step ahead, and V(step) comes where K(step) has been read, under the step's softmax and the next Q K^T.  One place for keys and two for
+// values made Q K^T wait for its keys: 4,000 cycles a step of the two tiles, where the tensor core's share (six products of 128 x 128 x 128) is three
+// quarters of that.  1,008 queries of 24 heads over 9,200 keys: 123 to 140 us by box and clock, against 95 with single bf16 queries (1.5 times the products).
 template <bool MERGE, bool FINE = false>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,

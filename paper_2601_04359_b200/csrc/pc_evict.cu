@@ -5,6 +5,10 @@
 // indices of all larger keys and of the first equal ones.  One CTA for short histories; for longer ones a cluster of CTAs that
 // each hold a piece of the history in shared memory, count it, and read one another's counts through distributed shared memory: one
 // barrier of the cluster a pass.  k_evict_move copies the kept rows.
+//
+// The selection is latency: a launch, a fetch, up to three rounds of count, barrier and scan, and the sweep (675 tokens 5.8 us, 24,192 11.7, 47,376 17.2,
+// which are 0.03 us of memory); more CTAs would share out the counts, not the rounds.  The move is bound by memory: 6,048 rows of 4,096 bytes, 49.5 MB read and
+// written, 9.2 us from cold caches (5.4 TB/s).
 #include <algorithm>
 
 #include "pc_q4.cuh"
