@@ -50,8 +50,8 @@ constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, 
 
 // Queries as the B operand in shared memory, of a task (KV head, block of 8 rows): words [hi and lo parts 8 NG][sums 2] of 32 lanes, then 8 factors
 // Of up to four rows (a single token of grouped heads) the lo parts are columns of their own, 4 to 7, and one pass multiplies both ("folded").
-constexpr int query_words(int d, bool folded) { return folded ? 4 * (d / Q4_GROUP) + 1 : 8 * (d / Q4_GROUP) + 2; }
-constexpr int query_bytes(int d, bool folded) { return query_words(d, folded) * 128 + ROWS * 4; }
+__host__ __device__ constexpr int query_words(int d, bool folded) { return folded ? 4 * (d / Q4_GROUP) + 1 : 8 * (d / Q4_GROUP) + 2; }
+__host__ __device__ constexpr int query_bytes(int d, bool folded) { return query_words(d, folded) * 128 + ROWS * 4; }
 
 struct Q4Params {
     int n[2], shift[2];                // tokens of anchors, history; what their keys are shifted by
