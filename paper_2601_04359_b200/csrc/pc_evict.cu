@@ -1,8 +1,8 @@
 // Eviction by accumulated attention weight: of a history's older tokens the ones with the largest weight, behind them the newest tokens.
 //
 // Two launches.  k_evict_select finds the kept tokens: weights become 32-bit keys whose unsigned order is the weights' (score_key); three
-// passes over digits of 11, 11 and 10 bits narrow the range in which the want-th largest key lies, and an ordered sweep writes the
-// indices of all larger keys and of the first equal ones.  One CTA for short histories; for longer ones a cluster of CTAs that
+// passes over digits of 11, 11 and 10 bits narrow the range in which the want-th largest key lies (fewer, once at most 32 keys are left), and an ordered sweep
+// writes the indices of all larger keys and of the first equal ones.  One CTA for short histories; for longer ones a cluster of CTAs that
 // each hold a piece of the history in shared memory, count it, and read one another's counts through distributed shared memory: one
 // barrier of the cluster a pass.  k_evict_move copies the kept rows.
 //
@@ -18,7 +18,8 @@ namespace {
 
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
 constexpr int DIGIT_BINS = 2048;
-constexpr int MAX_CLUSTER = 8;
+constexpr int MAX_CLUSTER = 8;                     // sixteen: 47,376 tokens 31.4 -> 30.5 us, 24,000 19.7 -> 20.0, 8,000 14.4 -> 15.4
+constexpr int FEW = 32;                            // keys that a warp holds at once, a warp for each of them
 constexpr int CACHED = 36 * 1024;                  // keys of a CTA's piece kept in shared memory; the rest is read again
 
 struct SelectParams {
@@ -48,6 +49,9 @@ __device__ __forceinline__ int4 remote_load(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void remote_store(uint32_t addr, uint32_t rank, int4 v) {
     asm volatile("st.shared::cluster.v4.s32 [%0], {%1,%2,%3,%4};" ::"r"(remote(addr, rank)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ void remote_store(uint32_t addr, uint32_t rank, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(addr, rank)), "r"(v) : "memory");
+}
 __device__ __forceinline__ int4 operator+(int4 a, int4 b) { return make_int4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
 // Sum of v over the threads before this one, and over all
@@ -74,11 +78,14 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
     __shared__ int warp_sums[SEL_WARPS];
     __shared__ int found[3];
     __shared__ int4 counts[MAX_CLUSTER];
-    static_assert(SEL_WARPS == 32 && DIGIT_BINS == 2 * SEL_THREADS, "a lane reads a warp's total, a thread owns two bins");
+    __shared__ uint32_t few[MAX_CLUSTER][FEW];     // keys of each CTA that share the digits so far, and how many
+    __shared__ int few_n[MAX_CLUSTER];
+    static_assert(SEL_WARPS == FEW && DIGIT_BINS == 2 * SEL_THREADS, "a lane reads a warp's total, a thread owns two bins");
     pc_grid_dep_launch();
     const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
     const int first = rank * P.piece, n = max(0, min(P.piece, P.n_old - first));
     for (int b = threadIdx.x; b < 2 * DIGIT_BINS; b += SEL_THREADS) (&hist[0][0])[b] = 0;
+    if (threadIdx.x < MAX_CLUSTER) few_n[threadIdx.x] = 0;
     pc_grid_dep_wait();
     const auto key_of = [&](int j) {
         const float w = P.weight[first + j];
@@ -147,6 +154,41 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
         if (want == found[2]) {                    // all keys of the bin stay, whatever their lower digits: no key is compared further
             prefix -= 1;
             want = 0;
+            break;
+        }
+        if (pass < 2 && found[2] <= FEW) {
+            // Few keys left: every CTA gets them all, a lane of each warp holds one, and warp i compares the i-th with all
+            for (int j = threadIdx.x; j < n; j += SEL_THREADS) {
+                const uint32_t k = key_at(j);
+                if (((k ^ prefix) >> shift) == 0) few[rank][atomicAdd(&few_n[rank], 1) % FEW] = k;
+            }
+            __syncthreads();                       // and `found` has been read
+            if (ctas > 1) {
+                const int other = threadIdx.x / FEW, i = threadIdx.x % FEW;
+                if (other < ctas && other != rank) {
+                    if (i < few_n[rank]) remote_store(pc_smem_u32(&few[rank][i]), other, few[rank][i]);
+                    if (i == 0) remote_store(pc_smem_u32(&few_n[rank]), other, (uint32_t)few_n[rank]);
+                }
+                cluster_sync();
+            }
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+            uint32_t key = 0;
+            int all = 0;
+            for (int r = 0; r < ctas; ++r) {
+                const int here = few_n[r];
+                if (lane >= all && lane < all + here) key = few[r][lane - all];
+                all += here;
+            }
+            const uint32_t k = __shfl_sync(0xffffffffu, key, warp);  // a warp's own
+            const int larger = __popc(__ballot_sync(0xffffffffu, lane < all && key > k));
+            const int as_large = __popc(__ballot_sync(0xffffffffu, lane < all && key >= k));
+            if (lane == 0 && warp < all && larger < want && want <= as_large) {
+                found[0] = (int)k;                 // warps whose keys are equal write the same
+                found[1] = want - larger;
+            }
+            __syncthreads();
+            prefix = (uint32_t)found[0];
+            want = found[1];
             break;
         }
     }

@@ -139,3 +139,25 @@ def test_refusals():
     _refused(pc.PC_ERR_CAPACITY, pc.pc_evict, ctx, src, w, 12, 0, to)
     _refused(pc.PC_ERR_INVALID_ARG, pc.pc_evict, ctx, src, w, 10, 0, to, w[20:])
     assert to.n_tokens == 0 and dst.n_tokens == 0 and pc.pc_poll_status(ctx) == pc.PC_OK
+
+
+@pytest.mark.parametrize("n", [300, 9000, 40000])
+@pytest.mark.parametrize("near,same", [(1, 1), (2, 1), (2, 2), (31, 3), (32, 1), (32, 32), (33, 5), (40, 1)])
+def test_few_tokens_around_the_last_that_stays(n, near, same):
+    """`near` weights that share all but their last bits, `same` of them equal, the last that stays among them."""
+    rng = np.random.default_rng(n + near + same)
+    ctx = _ctx("tiny_f32", 1, 64)
+    above = n // 5
+    w = np.concatenate([2 + rng.random(above), 1 + 2.0 ** -23 * np.maximum(np.arange(near), same - 1), 0.5 * rng.random(n - above - near)]).astype(np.float32)
+    w = w[rng.permutation(n)]
+    k = torch.arange(n, device="cuda", dtype=torch.float32)[:, None, None].expand(n, 2, 64).contiguous()
+    src = pc.Segment(k, k, torch.zeros(n, 4, dtype=torch.int32, device="cuda"), n)
+    masked = np.ones(n, bool)
+    masked[rng.permutation(n)[:near]] = False
+    for keep, valid in ((above + 1, None), (above + near // 2, None), (above + near, None), (n - near + near // 2, masked)):
+        dst = pc.Segment(k.new_empty(keep, 2, 64), k.new_empty(keep, 2, 64), torch.empty(keep, 4, dtype=torch.int32, device="cuda"), 0)
+        v = None if valid is None else torch.from_numpy(valid.astype(np.uint8)).cuda()
+        sel = pc.pc_evict(ctx, src, torch.from_numpy(w).cuda(), keep, 0, dst, valid=v)
+        assert pc.pc_poll_status(ctx) == pc.PC_OK
+        want = ref.evict(w, keep, 0, valid)
+        assert np.array_equal(sel.cpu().numpy(), want) and np.array_equal(dst.k[:, 0, 0].cpu().numpy().astype(np.int64), want)
