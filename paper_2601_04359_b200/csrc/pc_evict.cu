@@ -6,9 +6,9 @@
 // each hold a piece of the history in shared memory, count it, and read one another's counts through distributed shared memory: one
 // barrier of the cluster a pass.  k_evict_move copies the kept rows.
 //
-// The selection is latency: a launch, a fetch, up to three rounds of count, barrier and scan, and the sweep (675 tokens 5.8 us, 24,192 11.7, 47,376 17.2,
-// which are 0.03 us of memory); more CTAs would share out the counts, not the rounds.  The move is bound by memory: 6,048 rows of 4,096 bytes, 49.5 MB read and
-// written, 9.2 us from cold caches (5.4 TB/s).
+// The selection is latency: a launch, a fetch, up to three rounds of count, barrier and scan, and the sweep (675 tokens 5.4 us, 24,192 11.6, 47,376 16.3,
+// which are 0.03 us of memory).  Of the 27,000 cycles at 47,376 a round is 7,300: counting 1,600, a barrier 1,300, the exchange of counts 2,300, the scan 1,800.  The move is bound by memory: 6,048 rows of 4,096 bytes, 49.5 MB read and
+// written, 9.6 us from cold caches (5.2 TB/s).
 #include <algorithm>
 
 #include "pc_q4.cuh"
