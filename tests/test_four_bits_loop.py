@@ -1,12 +1,13 @@
 """The generation loop over the 4-bit cache: frames, text tokens, weights and evictions together; and waits that run out in its attention."""
 from __future__ import annotations
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2601_04359_b200 import binding as pc
 from paper_2601_04359_b200 import four_bits
-from tests.test_q4_cache import Case, _np
+from tests.test_q4_cache import Case, _np, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,42 @@ def test_sixteen_bit_calls_after_a_frame_over_four_bits():
     assert pc.pc_poll_status(c.ctx) == pc.PC_OK
     assert torch.equal(again, want)
     assert abs(_np(out) - _np(want)).max() <= 2e-2 * max(1.0, abs(_np(want)).max())
+
+
+@pytest.mark.parametrize("n_q,frames", [(1, False), (40, True)])
+def test_calls_replay_from_a_cuda_graph(n_q, frames):
+    c = Case("lumos", 96, 384, n_q, shift=8, weight=True, frames=frames)
+    raw = _rows(np.random.default_rng(3), "lumos", 64)[0]
+    out, lse = torch.empty_like(c.q), torch.empty(n_q, c.q.shape[1], device="cuda")
+    dst = pc.Q4Segment.empty(c.ctx, 200, weight=True)
+    sel = torch.empty(200, dtype=torch.int32, device="cuda")
+
+    def calls():
+        pc.pc_q4_store(c.ctx, raw, c.hist, at=320)
+        pc.pc_q4_attend(c.work, c.cache, c.q, c.q_pos, weigh=None if frames else (0.5, 1.0), out=out, lse=lse)
+        pc.pc_q4_evict(c.ctx, c.hist, 200, 50, dst, delta_t=4, sel_idx=sel)
+
+    def result():
+        torch.cuda.synchronize()
+        return [x.clone() for x in (out, lse, dst.rows, dst.pos, dst.weight, sel)]
+
+    start = torch.rand(384, device="cuda")
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        calls()
+        with torch.cuda.graph(graph, stream=s):
+            calls()
+    torch.cuda.synchronize()
+    for scale in (1.0, 0.5):                                 # inputs changed in place between replays
+        c.q.mul_(scale)
+        raw.k.mul_(scale)
+        c.hist.weight.copy_(start)
+        calls()
+        want = result()
+        for x in (out, lse, dst.rows, dst.weight, sel):
+            x.zero_()
+        c.hist.weight.copy_(start)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(result(), want))
+    assert pc.pc_poll_status(c.ctx) == pc.PC_OK
