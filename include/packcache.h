@@ -432,8 +432,10 @@ pc_status pc_q4_destroy(pc_q4 *w);
  *     weight_j <- decay * weight_j + gain * (mean over queries and heads of the probability of token j).
  *   out device [n_q][Hq][d]; lse device [n_q][Hq] fp32 or NULL.
  * A query row that holds a NaN or an infinity gives NaN, in its own head alone.
- * Sums and softmax statistics are fp32.  Queries go to the multiply-adds as two fp16 parts (22 bits), probabilities times steps as one fp16
- * number (bf16 contexts) or three bf16 parts (fp32).  Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
+ * Sums and softmax statistics are fp32.  Queries go to the multiply-adds as two fp16 parts (22 bits).  Probabilities and probabilities times steps
+ * are one fp16 number each in bf16 contexts: 11 bits down to 2^-22 of the largest probability and, of the products, 2^-27 of the largest probability times
+ * the largest step of the channel group (or of 2^-8, if that is more), and fixed places of 2^-33 and 2^-38 below; in fp32 contexts products are three bf16 parts.
+ * Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
  * on a context with tensor-core attention and a workspace with PC_Q4_FRAMES, instead turn the cache into fp16 once and run a tensor-core kernel
  * on it (keys, values and probabilities rounded to fp16, queries in two parts, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger
  * ones are held there, with PC_ERR_INVALID_ARG in the status word; max_keys of the context bounds the tokens); they use the

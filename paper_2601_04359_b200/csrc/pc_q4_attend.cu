@@ -44,8 +44,13 @@ constexpr int RING_AT = 1024;          // barriers and flags before the ring
 constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
 constexpr int UNIT = 2;                // steps that a warp takes together
 constexpr int BOX = 128, BOX_BYTES = UNIT * Q4_STEP * BOX; // a box of the rows: a unit's tokens x 128 bytes
-// Probabilities are scaled by 2^P_LOG (the sums with them, so that it cancels): times a step they stay below fp16's largest, 4 * 2 * 65504 / 15
-constexpr float P_LOG = 2.f;
+// fp16's range, where probabilities and their products with steps are fp16 numbers (bf16 contexts): probabilities are scaled by 2^8 (the sums with them, so
+// that it cancels), and the steps of a value's channel group by a power of two that leaves the largest met so far below 2^7, so that products
+// stay below 2^15.  That largest is at 2^5 at least (or the factor 2^15, its most): a product that is 2^-27 of the largest still has all its bits.
+// (Unscaled, products below 2^-25 vanished, always towards the group's low.)  fp32 contexts hold products in bf16 parts, which have the range.
+constexpr float P_LOG_F16 = 8.f, P_LOG_F32 = 2.f;
+constexpr uint32_t SIGNS = 0x80008000u, STEPS_BELOW = 0x58005800u;         // 2^7, twice
+constexpr uint32_t FACTOR_MOST = 0x78007800u;      // 2^15, twice: the factors before any step has been met
 constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, so that a masked logit (-infinity) gives probability 0
 
 // Queries as the B operand in shared memory, of a task (KV head, block of 8 rows): words [hi and lo parts 8 NG][sums 2] of 32 lanes, then 8 factors
@@ -133,6 +138,12 @@ __device__ __forceinline__ uint32_t middle_bf16(uint32_t codes) {
     const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
+// Factors for two groups' steps of which the largest are `top`: 2^(e - 15) <= top < 2^(e - 14) gives 2^(20 - e)
+__device__ __forceinline__ uint32_t factors_for(uint32_t top) {
+    return (0x00230023u - __vmaxu2((top >> 10) & 0x001F001Fu, 0x00050005u)) << 10;
+}
+__device__ __forceinline__ int factor_exponent(uint32_t factors, int upper) { return (int)((factors >> (upper ? 26 : 10)) & 31u); }      // + 15
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
@@ -336,6 +347,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     float O[2 * NG][4], L[4];          // out without the lows, channel 32 g + 4 row + {0, 1} ({2, 3}) of columns 2 t, 2 t + 1; the lows' part of group g in row 8 - NG + g
     float W[F32 ? NG : 1][2];          // fp32 contexts, in the place of L: of the lane's own keys
     float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
+    constexpr float P_LOG = F32 ? P_LOG_F32 : P_LOG_F16;
+    uint32_t factors[NG / 2];          // of the steps of each group, two to a word as the steps are; O has them too
+#pragma unroll
+    for (int w = 0; w < NG / 2; ++w) factors[w] = FACTOR_MOST;
 #pragma unroll
     for (int i = 0; i < (F32 ? NG : 1); ++i) W[i][0] = W[i][1] = 0.f;
 #pragma unroll
@@ -459,6 +474,41 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
 #pragma unroll
                     for (int w = 0; w < NG / 2; ++w) steps[j][w] = 0u;
                 }
+        }
+        if constexpr (!F32) {
+            // (a step is negative, and its codes 0, where a group's low was rounded up past all its values)
+            uint32_t scaled[4][NG / 2], most = 0u;
+            const auto scale_steps = [&] {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int w = 0; w < NG / 2; ++w) scaled[j][w] = mul_half(steps[j][w], factors[w]);
+            };
+            scale_steps();
+#pragma unroll
+            for (int w = 0; w < NG / 2; ++w) most = __vimax3_s16x2(__vimax3_s16x2(most, scaled[0][w], scaled[1][w]), scaled[2][w], scaled[3][w]);
+            if (__any_sync(0xffffffffu, ((most + (SIGNS - STEPS_BELOW)) & SIGNS) != 0u)) {
+                // larger than the factors allow for: once or twice in a warp's run, as a running maximum grows
+#pragma unroll
+                for (int w = 0; w < NG / 2; ++w) {
+                    uint32_t top = __vimax3_s16x2(__vimax3_s16x2(0u, steps[0][w], steps[1][w]), steps[2][w], steps[3][w]);
+                    top = __vmaxs2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = __vmaxs2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const uint32_t now = __vminu2(factors[w], factors_for(top));
+#pragma unroll
+                    for (int g = 2 * w; g < 2 * w + 2; ++g) {
+                        const float c = power_of_two(factor_exponent(now, g & 1) - factor_exponent(factors[w], g & 1));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { O[2 * g][i] *= c; O[2 * g + 1][i] *= c; }
+                    }
+                    factors[w] = now;
+                }
+                scale_steps();
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int w = 0; w < NG / 2; ++w) steps[j][w] = scaled[j][w];
         }
         uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
         constexpr float UP = F32 ? 8192.f : 1.f; // the second part of a small probability would be a subnormal number
@@ -638,7 +688,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 w0 = __shfl_sync(0xffffffffu, L[0], (8 - NG + g) * 4 + t);
                 w1 = __shfl_sync(0xffffffffu, L[1], (8 - NG + g) * 4 + t);
             }
-            constexpr float A = F32 ? 1.f : 16777216.f, B = F32 ? 1.f : 1048576.f;      // the codes' powers of two
+            // the codes' powers of two and the steps' factor come off
+            const float unit = F32 ? 1.f : power_of_two(15 - factor_exponent(factors[g / 2], g & 1));
+            const float A = F32 ? 1.f : 16777216.f * unit, B = F32 ? 1.f : 1048576.f * unit;
             *reinterpret_cast<float4 *>(mine + g * Q4_GROUP) =
                 make_float4(fmaf(O[2 * g][0], A, w0), fmaf(O[2 * g][2], B, w0), fmaf(O[2 * g + 1][0], A, w0), fmaf(O[2 * g + 1][2], B, w0));
             *reinterpret_cast<float4 *>(mine + PITCH + g * Q4_GROUP) =
