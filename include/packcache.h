@@ -437,7 +437,7 @@ pc_status pc_q4_destroy(pc_q4 *w);
  * the largest step of the channel group (or of 2^-8, if that is more), and fixed places of 2^-33 and 2^-38 below; in fp32 contexts products are three bf16 parts.
  * Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
  * on a context with tensor-core attention and a workspace with PC_Q4_FRAMES, instead turn the cache into fp16 once and run a tensor-core kernel
- * on it (keys, values and probabilities rounded to fp16, queries in two parts, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger
+ * on it (keys, values and probabilities rounded to fp16, probabilities below 2^-21 of a row's largest to places of 2^-31 of it, queries in two parts with places of 2^-24, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger
  * ones are held there, with PC_ERR_INVALID_ARG in the status word; max_keys of the context bounds the tokens); they use the
  * context's rotated-key scratch as pc_attend_frame does, and what pc_attend_prepare fixed is dropped; pc_attend_mass cannot follow them.
  * Calls that share a workspace have to be ordered on the GPU; with weights, a call's queries go in passes that the workspace's logits hold.

@@ -57,6 +57,9 @@ constexpr int MAX_SPLITS = 8;             // most parts of an item
 constexpr int BOUNDARY_STEPS = 2;         // what a CTA's crossing into the next item costs, in steps
 constexpr int MAX_FIXED_SPLITS = 4;       // most key ranges a caller can fix, and most of the cluster merge
 constexpr float RESCALE_THRESHOLD = 8.0f;
+// Probabilities in fp16 are held as 2^7 p: up to 2^15 with what the threshold leaves, and the last place of a small one is 2^-31 of the largest (as p it
+// was 2^-24, and keys below half of that counted in the sum but not in the output)
+constexpr float FINE_UP = 7.0f;
 
 // shared memory map (dynamic, 1024-byte aligned)
 constexpr int SM_Q = 0;                                   // 2 tiles
@@ -622,7 +625,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                 }
                 const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
                 // lazy rescale: move the reference maximum only when it grew by more than the threshold
-                const bool grow = mx > m_used + RESCALE_THRESHOLD;
+                const bool grow = mx > m_used + (FINE ? RESCALE_THRESHOLD + FINE_UP : RESCALE_THRESHOLD);
                 if (__builtin_expect(!__all_sync(0xffffffffu, pv_done), 0)) {
                     alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, P.status, P.wait_us);
                     if (!alive) break;
@@ -631,7 +634,7 @@ k_attend_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                 // tile 1 comes last: QK^T(step) and PV(step - 1) have read their keys and values
                 if (t == 1) arrive_if(lead, bar(BAR_EMPTY + (gs & 1)));
                 if (__builtin_expect(__any_sync(0xffffffffu, grow), 0)) {
-                    const float m_new = fmaxf(m_used, mx);
+                    const float m_new = fmaxf(m_used, FINE ? mx - FINE_UP : mx);
                     const float corr = fast_exp2(m_used - m_new);       // 0 on the first tile (m_used = -inf)
                     l *= corr;
                     if (j > 0) {

@@ -149,3 +149,17 @@ def test_a_key_that_leaves_the_others_little(shape, n, n_q, max_q, c, scale, sil
 def test_a_key_that_leaves_the_others_little_fp32(c):
     """fp32 contexts have no last places to reckon with: down to 2^-39 of the largest probability and beyond."""
     _dominant("lumos_f32", 4_000, 2, c, 1.0, True, others=0.05).check()
+
+
+@pytest.mark.parametrize("n,n_q", [(3_000, 40), (300, 130)])
+@pytest.mark.parametrize("c,scale", [(1.2, 1.0), (1.55, 1.0), (1.7, 1.0), (1.7, 1e-2)])
+def test_a_key_that_leaves_the_others_little_in_a_frame(n, n_q, c, scale):
+    """Tolerances as in test_frames_on_the_tensor_core_kernel, and half of fp16's last place of a probability, 2^-25, which is held as 2^7 p / p_max at least."""
+    case = _dominant("lumos", n, n_q, c, scale, True, others=0.05, frames=True)
+    out, lse = case.run()
+    want, want_lse, mag_l, mag_v, p_max, _ = _attend64(case.q, case.seg)
+    delta = (2.0 ** -12 + 48 * 2.0 ** -23) * mag_l
+    assert ((lse - want_lse).abs() <= delta + 2.0 ** -20 * (1 + want_lse.abs())).all()
+    sv = _values(_decoded(case.seg, 128)[1])[1].sum(0).repeat_interleave(3, 0)[None]                  # of the query heads' KV heads
+    tol = (2 * delta + 2.0 ** -11)[..., None] * mag_v + 2.0 ** -8 * want.abs() + 2.0 ** -32 * p_max[..., None] * sv
+    assert ((out - want).abs() <= tol).all(), float(((out - want).abs() / tol).max())
