@@ -431,10 +431,11 @@ pc_status pc_q4_destroy(pc_q4 *w);
  *   weigh host or NULL: the weights of the history are brought up to date in the same call,
  *     weight_j <- decay * weight_j + gain * (mean over queries and heads of the probability of token j).
  *   out device [n_q][Hq][d]; lse device [n_q][Hq] fp32 or NULL.
- * A query row that holds a NaN or an infinity gives NaN, in its own head alone.
+ * A query row that holds a NaN or an infinity gives NaN, in its own head alone.  One of which a channel, rotated and times log2(e) / sqrt(d), reaches
+ * 2^109 is taken smaller by the power of two that it is beyond that, with PC_ERR_INVALID_ARG in the status word.
  * Sums and softmax statistics are fp32.  Queries go to the multiply-adds as two fp16 parts (22 bits).  Probabilities and probabilities times steps
  * are one fp16 number each in bf16 contexts: 11 bits down to 2^-22 of the largest probability and, of the products, 2^-27 of the largest probability times
- * the largest step of the channel group (or of 2^-8, if that is more), and fixed places of 2^-33 and 2^-38 below; in fp32 contexts products are three bf16 parts.
+ * the largest step of the channel group (or 2^-10, if that is more), below that they are off by up to 2^-33 and 2^-38 of the same; in fp32 contexts products are three bf16 parts.
  * Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
  * on a context with tensor-core attention and a workspace with PC_Q4_FRAMES, instead turn the cache into fp16 once and run a tensor-core kernel
  * on it (keys, values and probabilities rounded to fp16, probabilities below 2^-21 of a row's largest to places of 2^-31 of it, queries in two parts with places of 2^-24, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger

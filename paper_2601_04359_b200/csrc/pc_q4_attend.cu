@@ -239,7 +239,7 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
             }
             // the row's largest value to 2^6 .. 2^7: eight times a sum over 32 channels stays in fp16's range
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-            const int e = min(100, max(-118, 6 - ((int)(__float_as_uint(most) >> 23) - 127)));
+            const int e = min(100, max(-121, 6 - ((int)(__float_as_uint(most) >> 23) - 127)));
             const float up = __uint_as_float((uint32_t)(e + 127) << 23);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -274,7 +274,11 @@ __device__ __forceinline__ void take_queries(const Q4Params &P, const pc_rope_de
                     sums[SECOND + g / 2] = pack_half(8.f * (total - back.x), 8.f * (next - back.y));
                 }
             }
-            if (lane == 0) reinterpret_cast<float *>(to + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
+            // (what takes the scale off again is an fp32 number up to 2^127: a row beyond 2^109 counts as a power of two smaller)
+            if (lane == 0) {
+                if (e < -102 && most < INFINITY) pc_flag(P.status, PC_ERR_INVALID_ARG, PC_WHERE_Q4_RANGE);
+                reinterpret_cast<float *>(to + WORDS * 128)[col] = __uint_as_float((uint32_t)(min(126, 24 - e) + 127) << 23);
+            }
         }
     }
     __syncthreads();

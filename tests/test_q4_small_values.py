@@ -163,3 +163,30 @@ def test_a_key_that_leaves_the_others_little_in_a_frame(n, n_q, c, scale):
     sv = _values(_decoded(case.seg, 128)[1])[1].sum(0).repeat_interleave(3, 0)[None]                  # of the query heads' KV heads
     tol = (2 * delta + 2.0 ** -11)[..., None] * mag_v + 2.0 ** -8 * want.abs() + 2.0 ** -32 * p_max[..., None] * sv
     assert ((out - want).abs() <= tol).all(), float(((out - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("shape,n_q", [("lumos", 1), ("lumos", 5), ("tiny_f32", 1), ("tiny_f32", 3)])
+def test_queries_up_to_the_largest(shape, n_q):
+    """Queries that rotation and log2(e) / sqrt(d) leave below 2^109 are taken as they are; beyond it they are scaled down, and that is recorded."""
+    hq, hkv, d, _ = SHAPES[shape]
+    rng = np.random.default_rng(9)
+    q = rng.standard_normal((n_q, hq, d))
+    case = Small(shape, 100, n_q, rng.standard_normal((100, hkv, d)), q=q)
+    clean, clean_lse = case.run()
+    case.q[0, 1] *= 1e31                                  # 2^103 and less
+    _, lse = case.run()
+    _, want, mag_l, _, _, _ = _attend64(case.q, case.seg)
+    assert ((lse - want).abs() <= (48 * 2.0 ** -23 + 2.0 ** -21) * mag_l + 2.0 ** -20 * (1 + want.abs())).all()
+    case.q[0, 1, :] = 0.0
+    case.q[0, 1, 5] = 3e38
+    cache = pc.Q4Cache(pc.Q4Segment.empty(case.ctx, 0), case.seg)
+    out, lse = pc.pc_q4_attend(case.work, cache, case.q, case.q_pos, want_lse=True)
+    assert pc.pc_poll_status(case.ctx) == pc.PC_ERR_INVALID_ARG
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all() and lse[0, 1] > 1e31
+    others = torch.ones(n_q, hq, dtype=torch.bool, device="cuda")
+    others[0, 1] = False
+    assert ((lse.double() - clean_lse).abs()[others] <= 1e-5).all()
+    case.q[0, 1] = 3e38                                   # sums over channels as well
+    out, lse = pc.pc_q4_attend(case.work, cache, case.q, case.q_pos, want_lse=True)
+    assert pc.pc_poll_status(case.ctx) == pc.PC_ERR_INVALID_ARG
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
