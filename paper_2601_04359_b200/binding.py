@@ -624,20 +624,20 @@ def pc_q4_evict(ctx: Context, src: Q4Segment, keep: int, recent: int, dst: Q4Seg
     """Keep the ``recent`` newest tokens and the heaviest of the others, ``keep`` in all, in dst; returns sel_idx."""
     kept = min(keep, src.n_tokens)
     if sel_idx is None:
-        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=src.rows.device)
+        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=src.rows.device if src.rows is not None else "cuda")
     _check(_native().q4_evict(ctx.handle, src, keep, recent, delta_t, valid, dst, sel_idx, _stream(stream)), "pc_q4_evict")
     dst.n_tokens = kept
     dst.t_shift = src.t_shift + delta_t
     return sel_idx
 
 
-def pc_evict(ctx: Context, src: Segment, weight: torch.Tensor, keep: int, recent: int, dst: Segment,
+def pc_evict(ctx: Context, src: Segment, weight: Optional[torch.Tensor], keep: int, recent: int, dst: Segment,
              dst_weight: Optional[torch.Tensor] = None, delta_t: int = 0, valid: Optional[torch.Tensor] = None,
              sel_idx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The same for rows in the context's element type."""
     kept = min(keep, src.n_tokens)
     if sel_idx is None:
-        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=weight.device)
+        sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=weight.device if weight is not None else "cuda")
     _check(_native().evict(ctx.handle, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel_idx, _stream(stream)), "pc_evict")
     dst.n_tokens = kept
     return sel_idx
