@@ -101,6 +101,7 @@ def _native():
         load()
         from . import _packcache_py
         _packcache_py.set_i32_converter(_i32)
+        _packcache_py.set_types(torch.int32, torch.float32, torch.uint8, PackCacheError)
         _native_module = _packcache_py
     return _native_module
 
@@ -236,6 +237,7 @@ class Context:
         self.desc = pc_layer_desc(n_q_heads, n_kv_heads, head_dim, dtype, rope_base, (C.c_int32 * 3)(*max_pos),
                                   max_q, max_keys)
         self.torch_dtype = torch.bfloat16 if dtype == PC_BF16 else torch.float32
+        self.sizes = (n_q_heads, n_kv_heads, head_dim, self.torch_dtype)
         h = C.c_void_p()
         _check(lib.pc_create(C.byref(self.desc), C.byref(h)), "pc_create")
         self.handle = h
@@ -596,13 +598,13 @@ def pc_q4_store(ctx: Context, src: Segment, dst: Q4Segment, at: Optional[int] = 
     """Write src's rows to dst's rows from ``at`` on (default: behind the tokens in use)."""
     if at is None:
         at = dst.n_tokens
-    _check(_native().q4_store(ctx.handle, src, dst, at, _stream(stream)), "pc_q4_store")
+    _check(_native().q4_store(ctx.handle, ctx.sizes, src, dst, at, _stream(stream)), "pc_q4_store")
     dst.n_tokens = max(dst.n_tokens, at + src.n_tokens)
 
 
 def pc_q4_load(ctx: Context, src: Q4Segment, first: int, n: int, dst: Segment, stream=None) -> None:
     """Tokens first .. first + n - 1 of src as dst's rows, keys turned back to how they came in."""
-    _check(_native().q4_load(ctx.handle, src, first, n, dst, _stream(stream)), "pc_q4_load")
+    _check(_native().q4_load(ctx.handle, ctx.sizes, src, first, n, dst, _stream(stream)), "pc_q4_load")
     dst.n_tokens = n
 
 
@@ -615,7 +617,7 @@ def pc_q4_attend(work: Q4Work, cache: Q4Cache, q: torch.Tensor, q_pos: torch.Ten
     if lse is None and want_lse:
         lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
     decay, gain = weigh if weigh is not None else (None, None)
-    _check(_native().q4_attend(work.handle, cache, valid, q, q_pos, out, lse, decay, gain, _stream(stream)), "pc_q4_attend")
+    _check(_native().q4_attend(work.handle, work.ctx.sizes, cache, valid, q, q_pos, out, lse, decay, gain, _stream(stream)), "pc_q4_attend")
     return (out, lse) if want_lse else out
 
 
@@ -625,7 +627,7 @@ def pc_q4_evict(ctx: Context, src: Q4Segment, keep: int, recent: int, dst: Q4Seg
     kept = min(keep, src.n_tokens)
     if sel_idx is None:
         sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=src.rows.device if src.rows is not None else "cuda")
-    _check(_native().q4_evict(ctx.handle, src, keep, recent, delta_t, valid, dst, sel_idx, _stream(stream)), "pc_q4_evict")
+    _check(_native().q4_evict(ctx.handle, ctx.sizes, src, keep, recent, delta_t, valid, dst, sel_idx, _stream(stream)), "pc_q4_evict")
     dst.n_tokens = kept
     dst.t_shift = src.t_shift + delta_t
     return sel_idx
@@ -638,7 +640,7 @@ def pc_evict(ctx: Context, src: Segment, weight: Optional[torch.Tensor], keep: i
     kept = min(keep, src.n_tokens)
     if sel_idx is None:
         sel_idx = torch.empty(max(kept, 1), dtype=torch.int32, device=weight.device if weight is not None else "cuda")
-    _check(_native().evict(ctx.handle, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel_idx, _stream(stream)), "pc_evict")
+    _check(_native().evict(ctx.handle, ctx.sizes, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel_idx, _stream(stream)), "pc_evict")
     dst.n_tokens = kept
     return sel_idx
 
@@ -646,4 +648,5 @@ def pc_evict(ctx: Context, src: Segment, weight: Optional[torch.Tensor], keep: i
 def pc_accumulate(ctx: Context, mass: torch.Tensor, weight: torch.Tensor, decay: float, gain: float, stream=None) -> None:
     """weight <- decay * weight + gain * mass, over mass's tokens."""
     assert weight.numel() >= mass.numel(), "fewer weights than masses"
+    assert mass.dtype == weight.dtype == torch.float32, "masses and weights are fp32"
     _check(load().pc_accumulate(ctx.handle, _ptr(mass), mass.numel(), decay, gain, _ptr(weight), _stream(stream)), "pc_accumulate")

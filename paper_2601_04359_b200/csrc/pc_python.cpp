@@ -10,6 +10,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
+#include <cstdarg>
 #include <cstdint>
 #include <vector>
 
@@ -17,7 +19,9 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift;
+PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift,
+    *s_dtype, *s_itemsize, *s_nbytes;
+PyObject *g_i32, *g_f32, *g_u8, *g_refusal;      // torch.int32, torch.float32, torch.uint8; the binding's error, made of a status and a text
 PyObject *g_as_i32;       // numpy.ascontiguousarray(x, dtype=int32), for anything that is not an int32 array already
 
 bool failed() { return PyErr_Occurred() != nullptr; }
@@ -139,7 +143,80 @@ bool segment_of(PyObject *o, pc_segment *out) {
     return !failed();
 }
 
-bool q4_segment_of(PyObject *o, pc_q4_segment *out) {
+// ---- Calls of the 4-bit cache and of eviction look at the types and lengths of what they are given (the kernels would read and write past it): what does not
+// fit is refused as PC_ERR_INVALID_ARG, with the tensor's name.
+void refuse(const char *format, ...) {
+    va_list args;
+    va_start(args, format);
+    PyObject *text = PyUnicode_FromFormatV(format, args);
+    va_end(args);
+    if (!text) return;
+    PyObject *e = PyObject_CallFunction(g_refusal, "iO", (int)PC_ERR_INVALID_ARG, text);
+    Py_DECREF(text);
+    if (!e) return;
+    PyErr_SetObject(g_refusal, e);
+    Py_DECREF(e);
+}
+
+// heads, head dimension and element type of a context (Context.sizes)
+struct Sizes {
+    long long hq, hkv, d;
+    PyObject *dtype;                                  // borrowed from the tuple
+    int size;                                         // bytes of an element
+    bool take(PyObject *t) {
+        if (!PyArg_ParseTuple(t, "LLLO", &hq, &hkv, &d, &dtype)) return false;
+        size = dtype == g_f32 ? 4 : 2;
+        return true;
+    }
+    int64_t q_row() const { return hq * d; }
+    int64_t kv_row() const { return hkv * d; }
+};
+
+enum { AT_LEAST, EXACTLY };
+// The tensor has elements of this type (null: of one byte) and size, and so many of them; None is left to the library.  (Bytes are a third cheaper to ask
+// for than elements, and a length costs five times as much.)
+bool fits(PyObject *t, PyObject *dtype, int size, int64_t want, int how, const char *what) {
+    if (t == Py_None) return true;
+    PyObject *x = PyObject_GetAttr(t, dtype ? s_dtype : s_itemsize);
+    if (!x) return false;
+    const bool typed = dtype ? x == dtype : PyLong_AsLong(x) == 1;
+    Py_DECREF(x);
+    if (failed()) return false;
+    if (!typed) {
+        if (dtype) refuse("%s has to be %S", what, dtype);
+        else refuse("%s has to be of one byte an element", what);
+        return false;
+    }
+    x = PyObject_GetAttr(t, s_nbytes);
+    if (!x) return false;
+    const int64_t n = PyLong_AsLongLong(x) / size;
+    Py_DECREF(x);
+    if (failed()) return false;
+    if (how == EXACTLY ? n == want : n >= want) return true;
+    refuse("%s has %lld elements, %lld are needed", what, (long long)n, (long long)want);
+    return false;
+}
+
+bool fitting_segment_of(PyObject *o, const Sizes &z, pc_segment *out) {
+    *out = pc_segment{};
+    PyObject *k = PyObject_GetAttr(o, s_k), *v = PyObject_GetAttr(o, s_v), *pos = PyObject_GetAttr(o, s_pos);
+    if (k && v && pos) {
+        out->k = tensor_ptr(k);
+        if (!failed()) out->v = tensor_ptr(v);
+        if (!failed()) out->pos = static_cast<int32_t *>(tensor_ptr(pos));
+        if (!failed()) out->n_tokens = int_attr(o, s_n_tokens);
+        if (!failed() && k != Py_None) out->capacity = rows_of(k);
+        const int64_t n = out->capacity;
+        if (!failed())
+            fits(k, z.dtype, z.size, n * z.kv_row(), EXACTLY, "k") && fits(v, z.dtype, z.size, n * z.kv_row(), AT_LEAST, "v") && fits(pos, g_i32, 4, 4 * n, AT_LEAST, "pos");
+    }
+    Py_XDECREF(k);
+    Py_XDECREF(v);
+    Py_XDECREF(pos);
+    return !failed();
+}
+
+bool q4_segment_of(PyObject *o, const Sizes &z, pc_q4_segment *out) {
     *out = pc_q4_segment{};
     PyObject *rows = PyObject_GetAttr(o, s_rows), *pos = PyObject_GetAttr(o, s_pos), *weight = PyObject_GetAttr(o, s_weight);
     if (rows && pos && weight) {
@@ -149,6 +226,9 @@ bool q4_segment_of(PyObject *o, pc_q4_segment *out) {
         if (!failed()) out->n_tokens = int_attr(o, s_n_tokens);
         if (!failed()) out->t_shift = int_attr(o, s_t_shift);
         if (!failed() && rows != Py_None) out->capacity = rows_of(rows);
+        const int64_t n = out->capacity;
+        if (!failed())
+            fits(rows, g_u8, 1, n * z.kv_row() * 5 / 4, EXACTLY, "rows") && fits(pos, g_i32, 4, 4 * n, AT_LEAST, "pos") && fits(weight, g_f32, 4, n, AT_LEAST, "weight");
     }
     Py_XDECREF(rows);
     Py_XDECREF(pos);
@@ -340,71 +420,83 @@ PyObject *window_step(PyObject *, PyObject *const *a, Py_ssize_t n) {       // w
     return Py_BuildValue("ii", (int)st, (int)regime);
 }
 
-PyObject *q4_store(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, src, dst, at, stream
-    if (!arity(n, 5)) return nullptr;
+PyObject *q4_store(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, sizes, src, dst, at, stream
+    if (!arity(n, 6)) return nullptr;
+    Sizes z;
     pc_segment src{};
     pc_q4_segment dst{};
-    void *ctx = handle_of(a[0]), *stream = stream_of(a[4]);
-    const int32_t at = int_of(a[3]);
-    if (failed() || !segment_of(a[1], &src) || !q4_segment_of(a[2], &dst)) return nullptr;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[5]);
+    const int32_t at = int_of(a[4]);
+    if (failed() || !z.take(a[1]) || !fitting_segment_of(a[2], z, &src) || !q4_segment_of(a[3], z, &dst)) return nullptr;
     return call([&] { return pc_q4_store(static_cast<pc_ctx *>(ctx), &src, &dst, at, stream); });
 }
 
-PyObject *q4_load(PyObject *, PyObject *const *a, Py_ssize_t n) {           // ctx, src, first, n, dst, stream
-    if (!arity(n, 6)) return nullptr;
+PyObject *q4_load(PyObject *, PyObject *const *a, Py_ssize_t n) {           // ctx, sizes, src, first, n, dst, stream
+    if (!arity(n, 7)) return nullptr;
+    Sizes z;
     pc_q4_segment src{};
     pc_segment dst{};
-    void *ctx = handle_of(a[0]), *stream = stream_of(a[5]);
-    const int32_t first = int_of(a[2]), count = int_of(a[3]);
-    if (failed() || !q4_segment_of(a[1], &src) || !segment_of(a[4], &dst)) return nullptr;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[6]);
+    const int32_t first = int_of(a[3]), count = int_of(a[4]);
+    if (failed() || !z.take(a[1]) || !q4_segment_of(a[2], z, &src) || !fitting_segment_of(a[5], z, &dst)) return nullptr;
     return call([&] { return pc_q4_load(static_cast<pc_ctx *>(ctx), &src, first, count, &dst, stream); });
 }
 
-PyObject *q4_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {         // work, cache, valid, q, q_pos, out, lse, decay, gain (None: no weights), stream
-    if (!arity(n, 10)) return nullptr;
+PyObject *q4_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {         // work, sizes, cache, valid, q, q_pos, out, lse, decay, gain (None: no weights), stream
+    if (!arity(n, 11)) return nullptr;
+    Sizes z;
     pc_q4_cache cache{};
     Tensors<5> t;
     pc_q4_weigh weigh{};
-    void *work = handle_of(a[0]), *stream = stream_of(a[9]);
-    const bool weighs = a[7] != Py_None;
+    void *work = handle_of(a[0]), *stream = stream_of(a[10]);
+    const bool weighs = a[8] != Py_None;
     if (weighs) {
-        weigh.decay = (float)PyFloat_AsDouble(a[7]);
-        weigh.gain = (float)PyFloat_AsDouble(a[8]);
+        weigh.decay = (float)PyFloat_AsDouble(a[8]);
+        weigh.gain = (float)PyFloat_AsDouble(a[9]);
     }
-    if (failed()) return nullptr;
-    PyObject *anchors = PyObject_GetAttr(a[1], s_anchors), *history = PyObject_GetAttr(a[1], s_history);
-    const bool ok = anchors && history && q4_segment_of(anchors, &cache.anchors) && q4_segment_of(history, &cache.history);
+    if (failed() || !z.take(a[1])) return nullptr;
+    PyObject *anchors = PyObject_GetAttr(a[2], s_anchors), *history = PyObject_GetAttr(a[2], s_history);
+    const bool ok = anchors && history && q4_segment_of(anchors, z, &cache.anchors) && q4_segment_of(history, z, &cache.history);
     Py_XDECREF(anchors);
     Py_XDECREF(history);
-    if (!ok || !t.take(a + 2)) return nullptr;
-    const int32_t n_q = rows_of(a[3]);
-    if (failed()) return nullptr;
+    if (!ok || !t.take(a + 3)) return nullptr;
+    const int32_t n_q = rows_of(a[4]);
+    if (failed() || !fits(a[3], nullptr, 1, cache.history.n_tokens, AT_LEAST, "valid") || !fits(a[4], z.dtype, z.size, n_q * z.q_row(), EXACTLY, "q") ||
+        !fits(a[5], g_i32, 4, 4 * (int64_t)n_q, AT_LEAST, "q_pos") || !fits(a[6], z.dtype, z.size, n_q * z.q_row(), AT_LEAST, "out") ||
+        !fits(a[7], g_f32, 4, n_q * z.hq, AT_LEAST, "lse")) return nullptr;
     return call([&] {
         return pc_q4_attend(static_cast<pc_q4 *>(work), &cache, static_cast<uint8_t *>(t.p[0]), t.p[1], static_cast<int32_t *>(t.p[2]), n_q, t.p[3],
                             static_cast<float *>(t.p[4]), weighs ? &weigh : nullptr, stream);
     });
 }
 
-PyObject *q4_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, src, keep, recent, delta_t, valid, dst, sel, stream
-    if (!arity(n, 9)) return nullptr;
+PyObject *q4_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {          // ctx, sizes, src, keep, recent, delta_t, valid, dst, sel, stream
+    if (!arity(n, 10)) return nullptr;
+    Sizes z;
     pc_q4_segment src{}, dst{};
     Tensors<1> valid, sel;
-    void *ctx = handle_of(a[0]), *stream = stream_of(a[8]);
-    const pc_evict_params p{int_of(a[2]), int_of(a[3]), int_of(a[4])};
-    if (failed() || !q4_segment_of(a[1], &src) || !valid.take(a + 5) || !q4_segment_of(a[6], &dst) || !sel.take(a + 7)) return nullptr;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[9]);
+    const pc_evict_params p{int_of(a[3]), int_of(a[4]), int_of(a[5])};
+    if (failed() || !z.take(a[1]) || !q4_segment_of(a[2], z, &src) || !valid.take(a + 6) || !q4_segment_of(a[7], z, &dst) || !sel.take(a + 8) ||
+        !fits(a[6], nullptr, 1, src.n_tokens, AT_LEAST, "valid") || !fits(a[8], g_i32, 4, std::min(p.keep, src.n_tokens), AT_LEAST, "sel_idx")) return nullptr;
     return call([&] {
         return pc_q4_evict(static_cast<pc_ctx *>(ctx), &src, &p, static_cast<uint8_t *>(valid.p[0]), &dst, static_cast<int32_t *>(sel.p[0]), stream);
     });
 }
 
-PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {             // ctx, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel, stream
-    if (!arity(n, 11)) return nullptr;
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {             // ctx, sizes, src, weight, keep, recent, delta_t, valid, dst, dst_weight, sel, stream
+    if (!arity(n, 12)) return nullptr;
+    Sizes z;
     pc_segment src{}, dst{};
     Tensors<1> weight, valid;
     Tensors<2> to;
-    void *ctx = handle_of(a[0]), *stream = stream_of(a[10]);
-    const pc_evict_params p{int_of(a[3]), int_of(a[4]), int_of(a[5])};
-    if (failed() || !segment_of(a[1], &src) || !weight.take(a + 2) || !valid.take(a + 6) || !segment_of(a[7], &dst) || !to.take(a + 8)) return nullptr;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[11]);
+    const pc_evict_params p{int_of(a[4]), int_of(a[5]), int_of(a[6])};
+    if (failed() || !z.take(a[1]) || !fitting_segment_of(a[2], z, &src) || !weight.take(a + 3) || !valid.take(a + 7) || !fitting_segment_of(a[8], z, &dst) ||
+        !to.take(a + 9)) return nullptr;
+    const int64_t kept = std::min(p.keep, src.n_tokens);
+    if (!fits(a[3], g_f32, 4, src.n_tokens, AT_LEAST, "weight") || !fits(a[7], nullptr, 1, src.n_tokens, AT_LEAST, "valid") || !fits(a[9], g_f32, 4, kept, AT_LEAST, "dst_weight") ||
+        !fits(a[10], g_i32, 4, kept, AT_LEAST, "sel_idx")) return nullptr;
     return call([&] {
         return pc_evict(static_cast<pc_ctx *>(ctx), &src, static_cast<float *>(weight.p[0]), &p, static_cast<uint8_t *>(valid.p[0]), &dst,
                         static_cast<float *>(to.p[0]), static_cast<int32_t *>(to.p[1]), stream);
@@ -417,10 +509,20 @@ PyObject *set_i32_converter(PyObject *, PyObject *f) {
     Py_RETURN_NONE;
 }
 
+PyObject *set_types(PyObject *, PyObject *const *a, Py_ssize_t n) {        // torch.int32, torch.float32, torch.uint8, the error
+    if (!arity(n, 4)) return nullptr;
+    PyObject **to[] = {&g_i32, &g_f32, &g_u8, &g_refusal};
+    for (int i = 0; i < 4; ++i) {
+        Py_INCREF(a[i]);
+        Py_XSETREF(*to[i], a[i]);
+    }
+    Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(plan_budget), FAST(total), FAST(score), FAST(compact), FAST(attend_frame), FAST(attend_prepare), FAST(attend_prepared),
                          FAST(attend_mass), FAST(frame_step), FAST(window_append), FAST(window_step),
-                         FAST(q4_store), FAST(q4_load), FAST(q4_attend), FAST(q4_evict), FAST(evict),
+                         FAST(q4_store), FAST(q4_load), FAST(q4_attend), FAST(q4_evict), FAST(evict), FAST(set_types),
                          {"set_i32_converter", set_i32_converter, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackcache.so on the binding's objects.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -429,7 +531,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackc
 PyMODINIT_FUNC PyInit__packcache_py(void) {
     struct { PyObject **at; const char *name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_is_contiguous, "is_contiguous"}, {&s_shape, "shape"},
         {&s_k, "k"}, {&s_v, "v"}, {&s_pos, "pos"}, {&s_n_tokens, "n_tokens"}, {&s_anchors, "anchors"}, {&s_history, "history"},
-        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"}};
+        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"},
+        {&s_dtype, "dtype"}, {&s_itemsize, "itemsize"}, {&s_nbytes, "nbytes"}};
     for (auto &x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;
     return PyModule_Create(&module);
