@@ -41,15 +41,17 @@ constexpr int ROWS = 8;                // query rows of a warp
 constexpr int MAX_WARPS = 16;          // of a CTA: 128 registers a thread
 constexpr int MAX_SLOTS = 32;
 constexpr int RING_AT = 1024;          // barriers and flags before the ring
+constexpr int FACTORS_AT = 512;        // of these, steps' factors of each warp
 constexpr int SMEM_MOST = 226 * 1024;  // with 1,024 bytes to align the ring
 constexpr int UNIT = 2;                // steps that a warp takes together
 constexpr int BOX = 128, BOX_BYTES = UNIT * Q4_STEP * BOX; // a box of the rows: a unit's tokens x 128 bytes
 // fp16's range, where probabilities and their products with steps are fp16 numbers (bf16 contexts): probabilities are scaled by 2^8 (the sums with them, so
-// that it cancels), and the steps of a value's channel group by a power of two that leaves the largest met so far below 2^7, so that products
-// stay below 2^15.  That largest is at 2^5 at least (or the factor 2^15, its most): a product that is 2^-27 of the largest still has all its bits.
+// that it cancels), and the steps of a value's channel group by a power of two that leaves the largest met so far at up to 2^7, so that products
+// stay at up to 2^15.  That largest is at 2^5 at least (or the factor 2^15, its most): a product that is 2^-27 of the largest still has all its bits.
 // (Unscaled, products below 2^-25 vanished, always towards the group's low.)  fp32 contexts hold products in bf16 parts, which have the range.
 constexpr float P_LOG_F16 = 8.f, P_LOG_F32 = 2.f;
-constexpr uint32_t SIGNS = 0x80008000u, STEPS_BELOW = 0x58005800u;         // 2^7, twice
+constexpr uint32_t SIGNS = 0x80008000u;
+constexpr uint32_t STEPS_LIMIT = 0x14011400u;      // (0x9400 - a factor) is 2^7 / factor, with the sign set: less a step, it keeps the sign unless the step is larger
 constexpr uint32_t FACTOR_MOST = 0x78007800u;      // 2^15, twice: the factors before any step has been met
 constexpr float NO_MAX = -1e30f;       // of a row that has met no key: finite, so that a masked logit (-infinity) gives probability 0
 
@@ -138,9 +140,9 @@ __device__ __forceinline__ uint32_t middle_bf16(uint32_t codes) {
     const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-// Factors for two groups' steps of which the largest are `top`: 2^(e - 15) <= top < 2^(e - 14) gives 2^(20 - e)
+// Factors for two groups' steps of which the largest are `top`: 2^(e - 15) <= top < 2^(e - 14) gives 2^(20 - e), room for a step twice as large
 __device__ __forceinline__ uint32_t factors_for(uint32_t top) {
-    return (0x00230023u - __vmaxu2((top >> 10) & 0x001F001Fu, 0x00050005u)) << 10;
+    return (0x00230023u - __vminu2(__vmaxu2((top >> 10) & 0x001F001Fu, 0x00050005u), 0x001D001Du)) << 10;
 }
 __device__ __forceinline__ int factor_exponent(uint32_t factors, int upper) { return (int)((factors >> (upper ? 26 : 10)) & 31u); }      // + 15
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -352,9 +354,13 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     float W[F32 ? NG : 1][2];          // fp32 contexts, in the place of L: of the lane's own keys
     float m0 = NO_MAX, m1 = NO_MAX, l0 = 0.f, l1 = 0.f;
     constexpr float P_LOG = F32 ? P_LOG_F32 : P_LOG_F16;
-    uint32_t factors[NG / 2];          // of the steps of each group, two to a word as the steps are; O has them too
+    // Factors of the steps of each group, two to a word as the steps are (O has them too): in shared memory, a warp's own, for want of registers
+    const uint32_t factors_at = base + FACTORS_AT + 8 * warp;
+    const auto set_factor = [&](int w, uint32_t f) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(factors_at + 4 * w), "r"(f) : "memory"); };
+    if constexpr (!F32) {
 #pragma unroll
-    for (int w = 0; w < NG / 2; ++w) factors[w] = FACTOR_MOST;
+        for (int w = 0; w < NG / 2; ++w) set_factor(w, FACTOR_MOST);
+    }
 #pragma unroll
     for (int i = 0; i < (F32 ? NG : 1); ++i) W[i][0] = W[i][1] = 0.f;
 #pragma unroll
@@ -480,39 +486,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
                 }
         }
         if constexpr (!F32) {
-            // (a step is negative, and its codes 0, where a group's low was rounded up past all its values)
-            uint32_t scaled[4][NG / 2], most = 0u;
-            const auto scale_steps = [&] {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int w = 0; w < NG / 2; ++w) scaled[j][w] = mul_half(steps[j][w], factors[w]);
-            };
-            scale_steps();
-#pragma unroll
-            for (int w = 0; w < NG / 2; ++w) most = __vimax3_s16x2(__vimax3_s16x2(most, scaled[0][w], scaled[1][w]), scaled[2][w], scaled[3][w]);
-            if (__any_sync(0xffffffffu, ((most + (SIGNS - STEPS_BELOW)) & SIGNS) != 0u)) {
-                // larger than the factors allow for: once or twice in a warp's run, as a running maximum grows
-#pragma unroll
-                for (int w = 0; w < NG / 2; ++w) {
-                    uint32_t top = __vimax3_s16x2(__vimax3_s16x2(0u, steps[0][w], steps[1][w]), steps[2][w], steps[3][w]);
-                    top = __vmaxs2(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = __vmaxs2(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const uint32_t now = __vminu2(factors[w], factors_for(top));
-#pragma unroll
-                    for (int g = 2 * w; g < 2 * w + 2; ++g) {
-                        const float c = power_of_two(factor_exponent(now, g & 1) - factor_exponent(factors[w], g & 1));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { O[2 * g][i] *= c; O[2 * g + 1][i] *= c; }
-                    }
-                    factors[w] = now;
-                }
-                scale_steps();
-            }
+            uint32_t factors[NG / 2];
+            lds(factors_at, factors);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int w = 0; w < NG / 2; ++w) steps[j][w] = scaled[j][w];
+                for (int w = 0; w < NG / 2; ++w) steps[j][w] = mul_half(steps[j][w], factors[w]);
         }
         uint32_t pl[2], ph[2];                   // probabilities as the B operand: column = query row lane / 4
         constexpr float UP = F32 ? 8192.f : 1.f; // the second part of a small probability would be a subnormal number
@@ -594,6 +573,12 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             // (of one step: the second one's place holds tokens of the next CTA, or zeros; its logits count as masked)
             const bool two = unit * UNIT + 1 < n_steps;
             const int first = (step0 + unit * UNIT) * Q4_STEP;
+            // Steps beyond what the factors leave room for: a token a lane (of step `lane / 8 % 2` of the unit, row `lane % 8` of its half `lane / 16`)
+            uint32_t top[NG / 2], factors[NG / 2];
+            if constexpr (!F32) {
+                lds(factors_at, factors);
+                lds(rows + at_mv + (NG == 4 ? 0 : 8) + ((lane >> 3) & 1) * (Q4_STEP * BOX), top);
+            }
             float S0[4], S1[4];
             logits_of(rows, S0);
             logits_of(rows1, S1);
@@ -616,7 +601,33 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
             }
             x0 = fmaf(x0, f0, -P_LOG);
             x1 = fmaf(x1, f1, -P_LOG);
-            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1)) {
+            uint32_t within = SIGNS;
+            if constexpr (!F32) {
+                const bool there = ((lane & 8 ? seen1 : seen0) >> (4 * (lane & 7) + (lane >> 4))) & 1u;
+#pragma unroll
+                for (int w = 0; w < NG / 2; ++w) {
+                    top[w] = there ? __vmaxs2(top[w], 0u) : 0u;      // (negative, with codes of 0, where a group's low was rounded up past all its values)
+                    within &= STEPS_LIMIT - factors[w] - top[w];
+                }
+            }
+            if (__any_sync(0xffffffffu, x0 > m0 || x1 > m1 || within != SIGNS)) {
+                if constexpr (!F32)
+                    if (__any_sync(0xffffffffu, within != SIGNS)) {
+#pragma unroll
+                        for (int w = 0; w < NG / 2; ++w) {
+#pragma unroll
+                            for (int o = 1; o < 32; o <<= 1) top[w] = __vmaxs2(top[w], __shfl_xor_sync(0xffffffffu, top[w], o));
+                            const uint32_t now = __vminu2(factors[w], factors_for(top[w]));
+#pragma unroll
+                            for (int g = 2 * w; g < 2 * w + 2; ++g) {
+                                const float c = power_of_two(factor_exponent(now, g & 1) - factor_exponent(factors[w], g & 1));
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) { O[2 * g][i] *= c; O[2 * g + 1][i] *= c; }
+                            }
+                            set_factor(w, now);
+                        }
+                        __syncwarp();
+                    }
                 const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1), c0 = exp2_fast(m0 - n0), c1 = exp2_fast(m1 - n1);
                 m0 = n0;
                 m1 = n1;
@@ -665,6 +676,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) k_q4_attend(const __grid_co
     float *parts = reinterpret_cast<float *>(smem + RING_AT);      // [warp][8][PITCH], then [warp][8] maxima, sums
     float *ms = parts + n_warps * ROWS * PITCH, *ls = ms + n_warps * ROWS;
     {
+        uint32_t factors[NG / 2];
+        if constexpr (!F32) lds(factors_at, factors);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, o);

@@ -100,7 +100,7 @@ def test_values_far_below_one(call, scale):
     Small(shape, n, n_q, scale * np.random.default_rng(1).standard_normal((n, hkv, d)), max_q=max_q, masked=masked).check()
 
 
-@pytest.mark.parametrize("call", ["token", "few", "many_masked"])
+@pytest.mark.parametrize("call", ["token", "token64", "few", "many_masked"])
 @pytest.mark.parametrize("kind", ["growing", "shrinking", "one_large", "groups"])
 def test_steps_that_differ(call, kind):
     """Steps over a factor of 4,096: along the tokens, of one token in the middle, and from one group of channels to the next."""
