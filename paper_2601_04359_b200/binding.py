@@ -101,7 +101,7 @@ def _native():
         load()
         from . import _packcache_py
         _packcache_py.set_i32_converter(_i32)
-        _packcache_py.set_types(torch.int32, torch.float32, torch.uint8, PackCacheError)
+        _packcache_py.set_types(torch.float32, torch.Tensor, torch.Tensor.__dlpack_c_exchange_api__, PackCacheError)
         _native_module = _packcache_py
     return _native_module
 

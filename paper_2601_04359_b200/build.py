@@ -1,6 +1,7 @@
 """Build the CUDA library in-tree with nvcc for sm_100a (no JIT cache, no torch extension)."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -44,7 +45,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
     tmp = PYLIB + f".tmp{os.getpid()}"
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
+    torch_include = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin), "include")     # for ATen/dlpack.h, plain C
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", INCLUDE, "-I", torch_include, "-I", sysconfig.get_paths()["include"],
                            "-o", tmp, os.path.join(CSRC, "pc_python.cpp"), "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, PYLIB)
     return LIB

@@ -5,7 +5,7 @@
 // 2.3 us per array pointer), more than the launches of the step.  Host time of a
 // pass, ctypes against this file: frame step 51 -> 27 us (fp32 62 -> 24, with a shorter launch list), attention over a cache
 // 19.8 -> 10.6, mask, score, pack and attend 82 -> 36; the small bf16 step 53.8 -> 37.5 us a pass.
-// Tensors are read through their Python methods (data_ptr, is_contiguous, shape), so nothing here depends on torch's C++ ABI.
+// Tensors are read through their Python methods (data_ptr, is_contiguous, shape) or the C table of their type, so nothing here depends on torch's C++ ABI.
 // Each function returns the pc_status; the Python wrapper raises.  The interpreter lock is released around the library calls.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -15,13 +15,15 @@
 #include <cstdint>
 #include <vector>
 
+#include <ATen/dlpack.h>
+
 #include "packcache.h"
 
 namespace {
 
-PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift,
-    *s_dtype, *s_itemsize, *s_nbytes;
-PyObject *g_i32, *g_f32, *g_u8, *g_refusal;      // torch.int32, torch.float32, torch.uint8; the binding's error, made of a status and a text
+PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift;
+PyObject *g_f32, *g_tensor, *g_refusal;          // torch.float32, torch.Tensor; the binding's error, made of a status and a text
+const DLPackExchangeAPI *g_exchange;              // through which a tensor describes itself in one call
 PyObject *g_as_i32;       // numpy.ascontiguousarray(x, dtype=int32), for anything that is not an int32 array already
 
 bool failed() { return PyErr_Occurred() != nullptr; }
@@ -158,82 +160,104 @@ void refuse(const char *format, ...) {
     Py_DECREF(e);
 }
 
+enum Type { I32, F32, BF16, U8, BYTE /* any of one byte */ };
+
+// Where a tensor lies and what it holds.  Asked for through the table that the tensor's type publishes (DLPack's C exchange table): address, contiguity, shape,
+// type and bytes one attribute after the other are five calls of 0.05 to 0.1 us a tensor, of which a call has six to eleven.
+struct Tensor {
+    void *p = nullptr;                                // null for None
+    int64_t rows = 0, n = 0;                          // first extent, elements
+    DLDataType type{};
+    bool none = true;
+
+    bool take(PyObject *t) {
+        if (t == Py_None) return true;
+        if (!PyObject_TypeCheck(t, reinterpret_cast<PyTypeObject *>(g_tensor))) {
+            PyErr_Format(PyExc_TypeError, "a tensor is expected, not %s", Py_TYPE(t)->tp_name);
+            return false;
+        }
+        DLTensor d;
+        if (g_exchange->dltensor_from_py_object_no_sync(t, &d) != 0) return false;
+        n = 1;
+        bool dense = true;
+        for (int i = d.ndim - 1; i >= 0; --i) {       // strides of extents of one may be anything
+            if (d.strides && d.shape[i] != 1 && d.strides[i] != n) dense = false;
+            n *= d.shape[i];
+        }
+        if (!dense && n > 0) {
+            PyErr_SetString(PyExc_AssertionError, "tensors passed to the library must be contiguous");
+            return false;
+        }
+        p = static_cast<char *>(d.data) + d.byte_offset;
+        rows = d.ndim > 0 ? d.shape[0] : 1;
+        type = d.dtype;
+        none = false;
+        return true;
+    }
+    bool is(Type t) const {
+        if (type.lanes != 1) return false;
+        switch (t) {
+        case I32: return type.code == kDLInt && type.bits == 32;
+        case F32: return type.code == kDLFloat && type.bits == 32;
+        case BF16: return type.code == kDLBfloat && type.bits == 16;
+        case U8: return type.code == kDLUInt && type.bits == 8;
+        case BYTE: return type.bits == 8;
+        }
+        return false;
+    }
+    enum How { AT_LEAST, EXACTLY };
+    // It has elements of this type, and so many of them; None is left to the library
+    bool fits(Type t, int64_t want, How how, const char *what) const {
+        static const char *const names[] = {"torch.int32", "torch.float32", "torch.bfloat16", "torch.uint8", "of one byte an element"};
+        if (none) return true;
+        if (!is(t)) {
+            refuse("%s has to be %s", what, names[t]);
+            return false;
+        }
+        if (how == EXACTLY ? n == want : n >= want) return true;
+        refuse("%s has %lld elements, %lld are needed", what, (long long)n, (long long)want);
+        return false;
+    }
+};
+
 // heads, head dimension and element type of a context (Context.sizes)
 struct Sizes {
     long long hq, hkv, d;
-    PyObject *dtype;                                  // borrowed from the tuple
-    int size;                                         // bytes of an element
+    Type type;
     bool take(PyObject *t) {
+        PyObject *dtype;
         if (!PyArg_ParseTuple(t, "LLLO", &hq, &hkv, &d, &dtype)) return false;
-        size = dtype == g_f32 ? 4 : 2;
+        type = dtype == g_f32 ? F32 : BF16;
         return true;
     }
     int64_t q_row() const { return hq * d; }
     int64_t kv_row() const { return hkv * d; }
 };
 
-enum { AT_LEAST, EXACTLY };
-// The tensor has elements of this type (null: of one byte) and size, and so many of them; None is left to the library.  (Bytes are a third cheaper to ask
-// for than elements, and a length costs five times as much.)
-bool fits(PyObject *t, PyObject *dtype, int size, int64_t want, int how, const char *what) {
-    if (t == Py_None) return true;
-    PyObject *x = PyObject_GetAttr(t, dtype ? s_dtype : s_itemsize);
-    if (!x) return false;
-    const bool typed = dtype ? x == dtype : PyLong_AsLong(x) == 1;
-    Py_DECREF(x);
-    if (failed()) return false;
-    if (!typed) {
-        if (dtype) refuse("%s has to be %S", what, dtype);
-        else refuse("%s has to be of one byte an element", what);
-        return false;
-    }
-    x = PyObject_GetAttr(t, s_nbytes);
-    if (!x) return false;
-    const int64_t n = PyLong_AsLongLong(x) / size;
-    Py_DECREF(x);
-    if (failed()) return false;
-    if (how == EXACTLY ? n == want : n >= want) return true;
-    refuse("%s has %lld elements, %lld are needed", what, (long long)n, (long long)want);
-    return false;
+bool tensor_attr(PyObject *o, PyObject *name, Tensor *out) {
+    PyObject *t = PyObject_GetAttr(o, name);
+    if (!t) return false;
+    const bool ok = out->take(t);
+    Py_DECREF(t);
+    return ok;
 }
 
 bool fitting_segment_of(PyObject *o, const Sizes &z, pc_segment *out) {
-    *out = pc_segment{};
-    PyObject *k = PyObject_GetAttr(o, s_k), *v = PyObject_GetAttr(o, s_v), *pos = PyObject_GetAttr(o, s_pos);
-    if (k && v && pos) {
-        out->k = tensor_ptr(k);
-        if (!failed()) out->v = tensor_ptr(v);
-        if (!failed()) out->pos = static_cast<int32_t *>(tensor_ptr(pos));
-        if (!failed()) out->n_tokens = int_attr(o, s_n_tokens);
-        if (!failed() && k != Py_None) out->capacity = rows_of(k);
-        const int64_t n = out->capacity;
-        if (!failed())
-            fits(k, z.dtype, z.size, n * z.kv_row(), EXACTLY, "k") && fits(v, z.dtype, z.size, n * z.kv_row(), AT_LEAST, "v") && fits(pos, g_i32, 4, 4 * n, AT_LEAST, "pos");
-    }
-    Py_XDECREF(k);
-    Py_XDECREF(v);
-    Py_XDECREF(pos);
-    return !failed();
+    Tensor k, v, pos;
+    if (!tensor_attr(o, s_k, &k) || !tensor_attr(o, s_v, &v) || !tensor_attr(o, s_pos, &pos)) return false;
+    const int64_t n = k.rows;
+    *out = pc_segment{k.p, v.p, static_cast<int32_t *>(pos.p), int_attr(o, s_n_tokens), (int32_t)n};
+    return !failed() && k.fits(z.type, n * z.kv_row(), Tensor::EXACTLY, "k") && v.fits(z.type, n * z.kv_row(), Tensor::AT_LEAST, "v") &&
+           pos.fits(I32, 4 * n, Tensor::AT_LEAST, "pos");
 }
 
 bool q4_segment_of(PyObject *o, const Sizes &z, pc_q4_segment *out) {
-    *out = pc_q4_segment{};
-    PyObject *rows = PyObject_GetAttr(o, s_rows), *pos = PyObject_GetAttr(o, s_pos), *weight = PyObject_GetAttr(o, s_weight);
-    if (rows && pos && weight) {
-        out->rows = tensor_ptr(rows);
-        if (!failed()) out->pos = static_cast<int32_t *>(tensor_ptr(pos));
-        if (!failed()) out->weight = static_cast<float *>(tensor_ptr(weight));
-        if (!failed()) out->n_tokens = int_attr(o, s_n_tokens);
-        if (!failed()) out->t_shift = int_attr(o, s_t_shift);
-        if (!failed() && rows != Py_None) out->capacity = rows_of(rows);
-        const int64_t n = out->capacity;
-        if (!failed())
-            fits(rows, g_u8, 1, n * z.kv_row() * 5 / 4, EXACTLY, "rows") && fits(pos, g_i32, 4, 4 * n, AT_LEAST, "pos") && fits(weight, g_f32, 4, n, AT_LEAST, "weight");
-    }
-    Py_XDECREF(rows);
-    Py_XDECREF(pos);
-    Py_XDECREF(weight);
-    return !failed();
+    Tensor rows, pos, weight;
+    if (!tensor_attr(o, s_rows, &rows) || !tensor_attr(o, s_pos, &pos) || !tensor_attr(o, s_weight, &weight)) return false;
+    const int64_t n = rows.rows;
+    *out = pc_q4_segment{rows.p, static_cast<int32_t *>(pos.p), static_cast<float *>(weight.p), int_attr(o, s_n_tokens), (int32_t)n, int_attr(o, s_t_shift)};
+    return !failed() && rows.fits(U8, n * z.kv_row() * 5 / 4, Tensor::EXACTLY, "rows") && pos.fits(I32, 4 * n, Tensor::AT_LEAST, "pos") &&
+           weight.fits(F32, n, Tensor::AT_LEAST, "weight");
 }
 
 struct CacheArg {
@@ -446,7 +470,7 @@ PyObject *q4_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {         // w
     if (!arity(n, 11)) return nullptr;
     Sizes z;
     pc_q4_cache cache{};
-    Tensors<5> t;
+    Tensor valid, q, q_pos, out, lse;
     pc_q4_weigh weigh{};
     void *work = handle_of(a[0]), *stream = stream_of(a[10]);
     const bool weighs = a[8] != Py_None;
@@ -459,14 +483,14 @@ PyObject *q4_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {         // w
     const bool ok = anchors && history && q4_segment_of(anchors, z, &cache.anchors) && q4_segment_of(history, z, &cache.history);
     Py_XDECREF(anchors);
     Py_XDECREF(history);
-    if (!ok || !t.take(a + 3)) return nullptr;
-    const int32_t n_q = rows_of(a[4]);
-    if (failed() || !fits(a[3], nullptr, 1, cache.history.n_tokens, AT_LEAST, "valid") || !fits(a[4], z.dtype, z.size, n_q * z.q_row(), EXACTLY, "q") ||
-        !fits(a[5], g_i32, 4, 4 * (int64_t)n_q, AT_LEAST, "q_pos") || !fits(a[6], z.dtype, z.size, n_q * z.q_row(), AT_LEAST, "out") ||
-        !fits(a[7], g_f32, 4, n_q * z.hq, AT_LEAST, "lse")) return nullptr;
+    if (!ok || !valid.take(a[3]) || !q.take(a[4]) || !q_pos.take(a[5]) || !out.take(a[6]) || !lse.take(a[7])) return nullptr;
+    const int64_t n_q = q.rows;
+    if (!valid.fits(BYTE, cache.history.n_tokens, Tensor::AT_LEAST, "valid") || !q.fits(z.type, n_q * z.q_row(), Tensor::EXACTLY, "q") ||
+        !q_pos.fits(I32, 4 * n_q, Tensor::AT_LEAST, "q_pos") || !out.fits(z.type, n_q * z.q_row(), Tensor::AT_LEAST, "out") ||
+        !lse.fits(F32, n_q * z.hq, Tensor::AT_LEAST, "lse")) return nullptr;
     return call([&] {
-        return pc_q4_attend(static_cast<pc_q4 *>(work), &cache, static_cast<uint8_t *>(t.p[0]), t.p[1], static_cast<int32_t *>(t.p[2]), n_q, t.p[3],
-                            static_cast<float *>(t.p[4]), weighs ? &weigh : nullptr, stream);
+        return pc_q4_attend(static_cast<pc_q4 *>(work), &cache, static_cast<uint8_t *>(valid.p), q.p, static_cast<int32_t *>(q_pos.p), (int32_t)n_q, out.p,
+                            static_cast<float *>(lse.p), weighs ? &weigh : nullptr, stream);
     });
 }
 
@@ -474,13 +498,13 @@ PyObject *q4_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {          // c
     if (!arity(n, 10)) return nullptr;
     Sizes z;
     pc_q4_segment src{}, dst{};
-    Tensors<1> valid, sel;
+    Tensor valid, sel;
     void *ctx = handle_of(a[0]), *stream = stream_of(a[9]);
     const pc_evict_params p{int_of(a[3]), int_of(a[4]), int_of(a[5])};
-    if (failed() || !z.take(a[1]) || !q4_segment_of(a[2], z, &src) || !valid.take(a + 6) || !q4_segment_of(a[7], z, &dst) || !sel.take(a + 8) ||
-        !fits(a[6], nullptr, 1, src.n_tokens, AT_LEAST, "valid") || !fits(a[8], g_i32, 4, std::min(p.keep, src.n_tokens), AT_LEAST, "sel_idx")) return nullptr;
+    if (failed() || !z.take(a[1]) || !q4_segment_of(a[2], z, &src) || !valid.take(a[6]) || !q4_segment_of(a[7], z, &dst) || !sel.take(a[8]) ||
+        !valid.fits(BYTE, src.n_tokens, Tensor::AT_LEAST, "valid") || !sel.fits(I32, std::min(p.keep, src.n_tokens), Tensor::AT_LEAST, "sel_idx")) return nullptr;
     return call([&] {
-        return pc_q4_evict(static_cast<pc_ctx *>(ctx), &src, &p, static_cast<uint8_t *>(valid.p[0]), &dst, static_cast<int32_t *>(sel.p[0]), stream);
+        return pc_q4_evict(static_cast<pc_ctx *>(ctx), &src, &p, static_cast<uint8_t *>(valid.p), &dst, static_cast<int32_t *>(sel.p), stream);
     });
 }
 
@@ -488,18 +512,17 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {             // c
     if (!arity(n, 12)) return nullptr;
     Sizes z;
     pc_segment src{}, dst{};
-    Tensors<1> weight, valid;
-    Tensors<2> to;
+    Tensor weight, valid, to_weight, sel;
     void *ctx = handle_of(a[0]), *stream = stream_of(a[11]);
     const pc_evict_params p{int_of(a[4]), int_of(a[5]), int_of(a[6])};
-    if (failed() || !z.take(a[1]) || !fitting_segment_of(a[2], z, &src) || !weight.take(a + 3) || !valid.take(a + 7) || !fitting_segment_of(a[8], z, &dst) ||
-        !to.take(a + 9)) return nullptr;
+    if (failed() || !z.take(a[1]) || !fitting_segment_of(a[2], z, &src) || !weight.take(a[3]) || !valid.take(a[7]) || !fitting_segment_of(a[8], z, &dst) ||
+        !to_weight.take(a[9]) || !sel.take(a[10])) return nullptr;
     const int64_t kept = std::min(p.keep, src.n_tokens);
-    if (!fits(a[3], g_f32, 4, src.n_tokens, AT_LEAST, "weight") || !fits(a[7], nullptr, 1, src.n_tokens, AT_LEAST, "valid") || !fits(a[9], g_f32, 4, kept, AT_LEAST, "dst_weight") ||
-        !fits(a[10], g_i32, 4, kept, AT_LEAST, "sel_idx")) return nullptr;
+    if (!weight.fits(F32, src.n_tokens, Tensor::AT_LEAST, "weight") || !valid.fits(BYTE, src.n_tokens, Tensor::AT_LEAST, "valid") ||
+        !to_weight.fits(F32, kept, Tensor::AT_LEAST, "dst_weight") || !sel.fits(I32, kept, Tensor::AT_LEAST, "sel_idx")) return nullptr;
     return call([&] {
-        return pc_evict(static_cast<pc_ctx *>(ctx), &src, static_cast<float *>(weight.p[0]), &p, static_cast<uint8_t *>(valid.p[0]), &dst,
-                        static_cast<float *>(to.p[0]), static_cast<int32_t *>(to.p[1]), stream);
+        return pc_evict(static_cast<pc_ctx *>(ctx), &src, static_cast<float *>(weight.p), &p, static_cast<uint8_t *>(valid.p), &dst,
+                        static_cast<float *>(to_weight.p), static_cast<int32_t *>(sel.p), stream);
     });
 }
 
@@ -509,12 +532,19 @@ PyObject *set_i32_converter(PyObject *, PyObject *f) {
     Py_RETURN_NONE;
 }
 
-PyObject *set_types(PyObject *, PyObject *const *a, Py_ssize_t n) {        // torch.int32, torch.float32, torch.uint8, the error
+PyObject *set_types(PyObject *, PyObject *const *a, Py_ssize_t n) {        // torch.float32, torch.Tensor, its exchange table, the error
     if (!arity(n, 4)) return nullptr;
-    PyObject **to[] = {&g_i32, &g_f32, &g_u8, &g_refusal};
-    for (int i = 0; i < 4; ++i) {
-        Py_INCREF(a[i]);
-        Py_XSETREF(*to[i], a[i]);
+    const auto *table = static_cast<const DLPackExchangeAPI *>(PyCapsule_GetPointer(a[2], "dlpack_exchange_api"));
+    if (!table) return nullptr;
+    if (table->header.version.major != DLPACK_MAJOR_VERSION || !table->dltensor_from_py_object_no_sync) {
+        PyErr_SetString(PyExc_RuntimeError, "tensors do not describe themselves in a form that is known here");
+        return nullptr;
+    }
+    g_exchange = table;
+    PyObject **to[] = {&g_f32, &g_tensor, &g_refusal}, *from[] = {a[0], a[1], a[3]};
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(from[i]);
+        Py_XSETREF(*to[i], from[i]);
     }
     Py_RETURN_NONE;
 }
@@ -531,8 +561,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackc
 PyMODINIT_FUNC PyInit__packcache_py(void) {
     struct { PyObject **at; const char *name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_is_contiguous, "is_contiguous"}, {&s_shape, "shape"},
         {&s_k, "k"}, {&s_v, "v"}, {&s_pos, "pos"}, {&s_n_tokens, "n_tokens"}, {&s_anchors, "anchors"}, {&s_history, "history"},
-        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"},
-        {&s_dtype, "dtype"}, {&s_itemsize, "itemsize"}, {&s_nbytes, "nbytes"}};
+        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"}};
     for (auto &x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;
     return PyModule_Create(&module);
