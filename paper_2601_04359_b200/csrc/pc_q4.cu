@@ -134,13 +134,15 @@ struct RowsArgs {
 template <int D, bool F32>
 __global__ void __launch_bounds__(ROW_THREADS, F32 ? 2 : 4) k_q4_store(RowsArgs A, pc_rope_dev rope) {
     constexpr int LANES = D / 8, NG = D / Q4_GROUP;
-    pc_grid_dep_launch();
     const unsigned unit = (blockIdx.x * ROW_THREADS + threadIdx.x) / LANES;      // unsigned: 2^32 threads are more rows than memory holds
     const int u = threadIdx.x % LANES, token = (int)(unit / A.slices), h0 = (int)(unit % A.slices) * HEADS;
     const bool live = token < A.n;                 // lanes of a warp stay together for the shuffles
     const int heads = live ? min(HEADS, A.n_kv - h0) : 0;
     const int g = u >> 2, t = u & 3;
     pc_grid_dep_wait();
+    // Only now may the next launch come: with calls queued up, launches that each let the next one in before their own wait filled the SMs with waiting
+    // CTAs, and a frame's 126 shared what was left (store and load of 1,008 tokens in a queue of calls 13.3 us, so 8.4; 24,193 tokens 63.3, so 63.5)
+    pc_grid_dep_launch();
     Eight<F32> kr[HEADS], vr[HEADS];
     const size_t at = ((size_t)token * A.n_kv + h0) * D + u * 8;
 #pragma unroll
