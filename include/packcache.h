@@ -438,9 +438,11 @@ pc_status pc_q4_destroy(pc_q4 *w);
  * the largest step of the channel group (or 2^-10, if that is more), below that they are off by up to 2^-33 and 2^-38 of the same; in fp32 contexts products are three bf16 parts.
  * Calls of many query rows (96 of a KV head, 24 over up to 1,024 tokens) without mask and weights,
  * on a context with tensor-core attention and a workspace with PC_Q4_FRAMES, instead turn the cache into fp16 once and run a tensor-core kernel
- * on it (keys, values and probabilities rounded to fp16, probabilities below 2^-21 of a row's largest to places of 2^-31 of it, queries in two parts with places of 2^-24, which take rotated queries times log2(e) / sqrt(d) up to +-65504: larger
- * ones are held there, with PC_ERR_INVALID_ARG in the status word; max_keys of the context bounds the tokens); they use the
+ * on it: keys, values and probabilities rounded to fp16 (probabilities below 2^-21 of a row's largest to places of 2^-31 of it), queries in two parts
+ * with places of 2^-24; these take rotated queries times log2(e) / sqrt(d) up to +-65504: larger ones are held there, with PC_ERR_INVALID_ARG in
+ * the status word; max_keys of the context bounds the tokens.  They use the
  * context's rotated-key scratch as pc_attend_frame does, and what pc_attend_prepare fixed is dropped; pc_attend_mass cannot follow them.
+ * Frames with a mask or weights go through the kernels of few queries, which take about ten times as long.
  * Calls that share a workspace have to be ordered on the GPU; with weights, a call's queries go in passes that the workspace's logits hold.
  * Errors: PC_ERR_INVALID_ARG (no keys at all, weigh without PC_Q4_WEIGH or without weights), PC_ERR_CAPACITY, PC_ERR_CUDA. */
 typedef struct {
@@ -454,9 +456,10 @@ pc_status pc_q4_attend(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid,
  * Keeps `keep` tokens of src (all, if it has no more): the `recent` newest, and of the older ones those with the largest weight, equal
  * weights by lower index (-0 == +0).  A token with valid == 0 is taken only after all others among the older ones.  Kept rows go to dst in
  * their order; K, V or 4-bit rows, (h, w, tag) and weights are bit copies, delta_t is subtracted from t (and added to the 4-bit
- * segment's t_shift, so that its keys stay as they are; delta_t >= -t_shift).  A NaN weight is recorded in the status word.
+ * segment's t_shift, so that its keys stay as they are; delta_t >= -t_shift).  A NaN among the weights that are compared (unmasked older tokens, where some
+ * of them stay and some do not) is recorded in the status word.
  *   weight device [n_tokens]; valid device bytes or NULL; dst and src must not overlap; dst->n_tokens is set;
- *   sel_idx device out [min(keep, n_tokens)]: the source index of every kept token, ascending.
+ *   sel_idx device out [min(keep, n_tokens)], 16-byte aligned as all device memory: the source index of every kept token, ascending.
  * Errors: PC_ERR_INVALID_ARG (recent > keep, overlapping buffers, no weights), PC_ERR_CAPACITY. */
 typedef struct {
     int32_t keep, recent, delta_t;

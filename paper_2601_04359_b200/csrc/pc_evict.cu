@@ -3,8 +3,8 @@
 // Two launches.  k_evict_select finds the kept tokens: weights become 32-bit keys whose unsigned order is the weights' (score_key); three
 // passes over digits of 11, 11 and 10 bits narrow the range in which the want-th largest key lies (fewer, once at most 32 keys are left), and an ordered sweep
 // writes the indices of all larger keys and of the first equal ones.  One CTA for short histories; for longer ones a cluster of CTAs that
-// each hold a piece of the history in shared memory, count it, and read one another's counts through distributed shared memory: one
-// barrier of the cluster a pass.  k_evict_move copies the kept rows.
+// each hold a piece of the history in shared memory and count it; through distributed shared memory each CTA adds up its slice of all counts and gives the sums to
+// all, between two barriers of the cluster a pass (and one more where the last few keys are exchanged).  k_evict_move copies the kept rows.
 //
 // The selection is latency: a launch, a fetch, up to three rounds of count, barrier and scan, and the sweep (675 tokens 5.4 us, 24,192 11.6, 47,376 16.3,
 // which are 0.03 us of memory).  Of the 27,000 cycles at 47,376 a round is 7,300: counting 1,600, a barrier 1,300, the exchange of counts 2,300, the scan 1,800.  The move is bound by memory: 6,048 rows of 4,096 bytes, 49.5 MB read and
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) k_evict_select(const SelectPar
             found[1] = want - before - (second ? c0 : 0);
             found[2] = second ? c1 : c0;
         }
-        // the other buffer was read by all before this pass's barrier of the cluster: cleared for the next pass
+        // All reads of the first pass's counts by other CTAs ended before that pass's second barrier (its own ahead of a barrier of the CTA): cleared for the third
         if (pass == 1)
             for (int b = threadIdx.x; b < DIGIT_BINS; b += SEL_THREADS) hist[0][b] = 0;
         __syncthreads();

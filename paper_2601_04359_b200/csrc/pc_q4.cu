@@ -5,8 +5,9 @@
 // eight channels of a row, so a group of 32 channels is four neighbouring lanes (two shuffles give its range) and the d / 8 lanes of a
 // token go through up to HEADS of its heads: the four rotary table entries of a thread's channels are looked up once for all of them,
 // and the loads of all heads are in flight together.
-// 24,193 tokens, bf16, 131 MB either way, from cold caches: k_q4_store 38 us (3.5 TB/s; instructions issue in 78 % of the cycles), k_q4_load 27 us
-// (4.8 TB/s).  One frame of 1,008 tokens, 5.5 MB: 6.4 and 5.0 us, of which about 4 are the launch.
+// 24,193 tokens, bf16, 131 MB either way, from cold caches: k_q4_store 37 us (3.5 TB/s; instructions issue in 78 % of the cycles, and
+// the bf16 form spills: 20 bytes stored and 68 loaded a thread, at the 64 registers that four blocks an SM leave), k_q4_load 27 us
+// (4.8 TB/s).  One frame of 1,008 tokens, 5.5 MB: 6.9 and 5.0 us, of which about 4 are the launch.
 #include "pc_q4.cuh"
 
 namespace {

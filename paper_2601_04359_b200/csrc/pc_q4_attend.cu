@@ -14,10 +14,11 @@
 // turns the logits that the history left into weights.
 //
 // What bounds it.  A token of 8 KV heads x 128 is 1,280 bytes, so 48,512 tokens are 62 MB, 9.6 us of memory.  Measured with 24 query heads, one token, by
-// kernel from cold caches: 20 us (3.1 TB/s) + 5 us of merging, which overlap in a run of calls (22.4 us a call); 13,232 tokens 11.6 + 5.1 us (11.6 a call).  In
-// the loop a warp step (16 keys of a head) is about 300 instructions and 13 matrix products of eight cycles each: instructions issue in 51 % of all
-// cycles, and of a CTA's 31,000 cycles 21,500 are the loop (18,000 if it only streamed, 17,000 if the keys lay there), 7,000 come ahead of it (queries and
-// their table entries, one dependent fetch behind the other, under which the ring fills) and 2,600 behind it (parts merged and written).
+// kernel from cold caches: 21 us (3.0 TB/s) + 5 us of merging, which overlap in a run of calls (23.0 us a call); 13,232 tokens 12.0 + 4.9 us (12.0 a call).  In
+// the loop a warp step (16 keys of a head) is some 330 instructions and 13 matrix products of eight cycles each: instructions issue in 55 % of all
+// cycles, and of a CTA's 32,000 cycles 22,100 are the loop (18,000 if it only streamed), 6,900 come ahead of it (queries and
+// their table entries, one dependent fetch behind the other, under which the ring fills) and 3,100 behind it (parts merged and written).  The form
+// whose lo parts are no columns of their own has 8 bytes of spills at 128 registers a thread, that of fp32 contexts 52.
 #include <algorithm>
 #include <new>
 
@@ -966,7 +967,7 @@ pc_status attend_rows(pc_q4 *w, const pc_q4_cache *cache, const uint8_t *valid, 
                       w->logits, w->lse, P.n[1], rows, weigh->decay, gain, cache->history.weight);
             return PC_OK;
         };
-        // 8 / 32 lanes, us a whole call over 12,196 keys: 8 rows 13.4 / 14.9, 24 15.2 / 15.6, 48 18.5 / 19.1, 72 24.5 / 25.3, 144 32.0 / 31.5
+        // 8 / 32 lanes, us a whole call over 12,196 keys: 8 rows 14.5 / 15.2, 24 15.8 / 16.5, 48 19.3 / 20.1, 72 25.5 / 26.7, 144 32.6 / 32.6
         return rows <= 96 ? weigh_with(k_q4_weigh<8>, 8) : weigh_with(k_q4_weigh<32>, 32);
     }
     return PC_OK;
@@ -1066,8 +1067,11 @@ extern "C" pc_status pc_q4_attend(pc_q4 *w, const pc_q4_cache *cache, const uint
     if (weigh && (!(w->parts & PC_Q4_WEIGH) || (!cache->history.weight && cache->history.n_tokens > 0))) return PC_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     // Many query rows of a KV head: the pass that turns the cache into 16 bits is paid once for all, and the tensor-core kernel's tiles of 128 rows are filled.
-    // Frame route / kernels of few queries, us: 24 / 8 heads over 9,200 tokens 72 rows 42 / 41, 96 42 / 45, 126 44 / 57; over 25,328 72 97 / 74, 96 99 / 90,
-    // 126 99 / 110; 8 / 8 heads 64 rows 40 / 36 and 96 / 63, 100 40 / 50 and 95 / 96; over 537 tokens 24 rows 15 / 18, 96 17 / 23, 12 15 / 15.
+    // Frame route / kernels of few queries, us: 24 / 8 heads over 9,200 tokens 72 rows 42 / 40, 96 42 / 47, 126 42 / 59; over 25,328 72 97 / 80, 96 97 / 94,
+    // 126 98 / 116; 8 / 8 heads 64 rows 40 / 37 and 96 / 66, 100 39 / 51 and 95 / 100; over 537 tokens 24 rows 16 / 17, 96 17 / 24, 12 15 / 16.
+    // (By rows alone: what turning the cache into 16 bits costs grows with its keys and KV heads, so over 25,328 keys the rule is 3 % off at 96 rows.)
+    // With a mask or weights frames take the kernels of few queries as well: 1,008 queries over 9,200 tokens 1.55 ms masked, 1.7 weighed, where 0.14 to 0.16 is
+    // the frame route's; 48,512 tokens 7.7 and 9.7 against 0.71.
     const size_t tile_rows = (size_t)(div_up(cache->anchors.n_tokens, 128) + div_up(cache->history.n_tokens, 128)) * 128;
     const int many = keys <= 1024 ? 24 : 96;
     if (n_q * ctx->group >= many && !valid && !weigh && w->v && ctx->attend_impl != 1 && tile_rows <= w->v_rows && tile_rows <= ctx->k_rot_rows)
