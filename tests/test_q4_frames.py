@@ -77,10 +77,10 @@ def test_runs_are_long(rt, name):
 class Layer:
     """Queries, and a cache of rows that differ from tile to tile, all at position zero; the history's keys have been rebased."""
 
-    def __init__(self, name):
-        (hq, hkv), self.n_q, n_a, n_h, splits = CASES[name]
-        self.g = hq // hkv
-        rng = np.random.default_rng(len(name) + self.n_q)
+    def __init__(self, heads, n_q, n_a, n_h, splits=0):
+        hq, hkv = heads
+        self.n_q, self.g = n_q, hq // hkv
+        rng = np.random.default_rng(n_h + n_q)
         base = rng.standard_normal((hkv, 128))
         self.ctx = pc.Context(hq, hkv, 128, pc.PC_BF16, 10000.0, (64, 8, 8), self.n_q, n_a + n_h)
         pc.pc_set_kv_splits(self.ctx, splits)
@@ -139,7 +139,7 @@ class Layer:
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", list(CASES))
 def test_frames_of_many_steps(name):
-    layer = Layer(name)
+    layer = Layer(*CASES[name])
     out, lse = pc.pc_q4_attend(layer.work, layer.cache, layer.q, layer.q_pos, want_lse=True)
     assert pc.pc_poll_status(layer.ctx) == pc.PC_OK
     want, want_lse, spread, mag, places, _ = layer.attend64()
@@ -166,11 +166,7 @@ def test_many_keys_without_the_tensor_core_form(n, n_q, masked, weigh):
     """Few queries, and whole frames with a mask or weights: the ring of units goes round many times, all keys in play.  Sums over codes and lows of a key are up to 34 |q o k|_2 (sqrt(128) for
     the sum of absolute values, 3 for step code + |low| of rows like these), of which 48 additions and the queries' parts round 48 * 2^-23 + 2^-21;
     probabilities and their products with steps are two roundings of 2^-11 each, independent from key to key: 8 of their standard deviations."""
-    CASES["few"] = ((24, 8), n_q, 1000, n, 0)
-    try:
-        layer = Layer("few")
-    finally:
-        del CASES["few"]
+    layer = Layer((24, 8), n_q, 1000, n)
     valid = (torch.rand(n, generator=torch.Generator().manual_seed(n_q)) >= masked).to(torch.uint8).cuda() if masked else None
     work = pc.Q4Work(layer.ctx, n + 1000, weigh=weigh)
     start = layer.cache.history.weight = torch.rand(n, device="cuda")
