@@ -473,6 +473,57 @@ pc_status pc_evict(pc_ctx *ctx, const pc_segment *src, const float *weight, cons
  * Both device fp32, 4-byte alignment is enough.  Errors: PC_ERR_INVALID_ARG. */
 pc_status pc_accumulate(pc_ctx *ctx, const float *mass, int32_t n, float decay, float gain, float *weight, void *stream);
 
+/* ---- Paged cache of a batch.
+ *
+ * Several sequences (samples of one prompt, or prompts of their own) hold their keys and values in one pool of pages.  A page has page_tokens token rows as
+ * they are in a pc_segment, keys rotated already (pair i of a head turns with axis i mod 3, as everywhere).  Which pages a sequence has, how many tokens, and which
+ * rows of a call are its own lies in device memory, so that a captured call can be replayed with other numbers.  All of it is read by the kernels of a call;
+ * a number that makes no sense (a sequence with more rows than max_rows, with more tokens than its pages hold or with rows outside the call's, a page that
+ * the pool does not have, a position outside the rotary tables) is recorded in the status word: the sequence is skipped, the page not written (its nearest neighbour read), the
+ * position clamped. */
+#define PC_MAX_SEQS 1024 /* most sequences of a call */
+
+typedef struct {
+    void *k;              /* device [n_pages][page_tokens][Hkv][d], 16-byte aligned */
+    void *v;              /* the same */
+    int32_t n_pages;      /* n_pages * page_tokens < 2^31 */
+    int32_t page_tokens;  /* 16, 32, 64 or 128 */
+} pc_pages;
+
+typedef struct {
+    const int32_t *table;     /* device [n_seqs][max_pages]: a sequence's token j is row j % page_tokens of page table[s][j / page_tokens]; entries behind its tokens are not read */
+    const int32_t *length;    /* device [n_seqs]: tokens of its own that a sequence has, those of the call's rows included */
+    const int32_t *row_start; /* device [n_seqs + 1]: rows row_start[s] .. row_start[s + 1] - 1 of the call belong to sequence s (none is fine); rows behind the last are left alone */
+    const int32_t *prefix;    /* device, pages of the prefix that all sequences share, or NULL; its last page need not be full */
+    int32_t n_seqs;           /* up to PC_MAX_SEQS */
+    int32_t max_pages;        /* entries of a sequence in `table` */
+    int32_t n_prefix;         /* tokens of the prefix; a sequence's own tokens come behind them */
+    int32_t max_rows;         /* no sequence has more rows than this */
+} pc_batch;
+
+/* Keys and values of a call's rows enter the cache: row i of the n_s rows of sequence s becomes its token length[s] - n_s + i, the key rotated at the row's
+ * position.  (A prefix is filled as a sequence of its own.)  No two rows may go to one place.
+ *   k, v device [n_rows][Hkv][d]; pos device [n_rows][4]; n_rows up to the context's max_q.  No workspace is used.
+ * Errors: PC_ERR_INVALID_ARG (also: the context's device is not the current one), PC_ERR_CAPACITY, PC_ERR_UNSUPPORTED (page_tokens). */
+pc_status pc_paged_append(pc_ctx *ctx, const pc_pages *pages, const pc_batch *batch, const void *k, const void *v, const int32_t *pos, int32_t n_rows,
+                          void *stream);
+
+/* Workspaces of pc_paged_attend, sized from the context's max_q.  Calls that share one have to be ordered on the GPU.  Errors: PC_ERR_INVALID_ARG, PC_ERR_CUDA. */
+typedef struct pc_paged pc_paged;
+pc_status pc_paged_create(pc_ctx *ctx, pc_paged **out);
+pc_status pc_paged_destroy(pc_paged *w);
+
+/* Attention of a call's rows over the paged cache, every sequence over its prefix and its own tokens:
+ *   out[i][h] = softmax_j((R q_ih).k_j,g / sqrt(d)) v_j,g,  g = h / (Hq/Hkv).
+ * causal: row i of the n_s rows of sequence s sees the prefix and own tokens 0 .. length[s] - n_s + i (a whole prompt: n_s = length[s]; its next piece; a token); otherwise
+ * all of them (a frame).  A row that sees nothing gives out 0 and lse -infinity.  Infinite or NaN values of tokens that a row does not see do not reach it.
+ *   q device [n_rows][Hq][d], not rotated; q_pos device [n_rows][4]; out device [n_rows][Hq][d]; lse device [n_rows][Hq] fp32 or NULL.
+ * Sums and softmax statistics are fp32.  In bf16 contexts the rotated queries and the probabilities go to the products in bf16, each rounded once.  In
+ * fp32 contexts products are of three bf16 parts a number, their terms below 2^-24 left out; infinite keys and queries give NaN there.
+ * The context's max_keys does not bound these calls.  Errors: as pc_paged_append. */
+pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const pc_batch *batch, const void *q, const int32_t *q_pos, int32_t n_rows, int32_t causal,
+                          void *out, float *lse, void *stream);
+
 /* Wait for the stream, then return and clear the first device-side event
  * recorded since the last poll (PC_OK if none). */
 pc_status pc_poll_status(pc_ctx *ctx, void *stream);

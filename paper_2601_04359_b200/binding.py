@@ -21,6 +21,7 @@ PC_OK, PC_ERR_INVALID_ARG, PC_ERR_BUDGET, PC_ERR_CAPACITY, PC_ERR_UNSUPPORTED, P
 PC_F32, PC_BF16 = 0, 1
 PC_GEOMETRIC, PC_CLOSED_HALF, PC_LINEAR, PC_HALFLIFE = 0, 1, 2, 3
 PC_MAX_FRAMES = 256
+PC_MAX_SEQS = 1024
 
 EXPORTS = ["pc_create", "pc_destroy", "pc_plan_budget", "pc_score", "pc_compact", "pc_attend_frame",
            "pc_poll_status", "pc_set_attend_impl", "pc_set_kv_splits", "pc_set_timing", "pc_get_timing",
@@ -29,7 +30,7 @@ EXPORTS = ["pc_create", "pc_destroy", "pc_plan_budget", "pc_score", "pc_compact"
            "pc_window_state", "pc_attend_prepare", "pc_attend_prepared", "pc_attend_mass", "pc_frame_step",
            "pc_forget_anchors", "pc_set_wait_limit_us", "pc_test_expect_extra_bytes", "pc_test_leave_parts", "pc_window_step", "pc_window_step_host", "pc_set_timing_skip",
            "pc_get_span", "pc_probe_stream_read", "pc_probe_mma_rate", "pc_q4_store", "pc_q4_load", "pc_q4_create", "pc_q4_destroy",
-           "pc_q4_attend", "pc_q4_evict", "pc_evict", "pc_accumulate"]
+           "pc_q4_attend", "pc_q4_evict", "pc_evict", "pc_accumulate", "pc_paged_create", "pc_paged_destroy", "pc_paged_append", "pc_paged_attend"]
 
 
 class pc_layer_desc(C.Structure):
@@ -164,6 +165,8 @@ def load() -> C.CDLL:
                                     C.POINTER(C.c_int32)]
     lib.pc_q4_create.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
     lib.pc_q4_destroy.argtypes = [C.c_void_p]
+    lib.pc_paged_create.argtypes = [C.c_void_p, C.POINTER(C.c_void_p)]
+    lib.pc_paged_destroy.argtypes = [C.c_void_p]
     lib.pc_accumulate.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
     _lib = lib
     return lib
@@ -241,6 +244,7 @@ class Context:
         h = C.c_void_p()
         _check(lib.pc_create(C.byref(self.desc), C.byref(h)), "pc_create")
         self.handle = h
+        self.device = torch.cuda.current_device() if torch.cuda.is_available() else -1      # -1: no GPU at all, and nothing is asked of where tensors lie
 
     def close(self) -> None:
         if getattr(self, "handle", None):
@@ -650,3 +654,67 @@ def pc_accumulate(ctx: Context, mass: torch.Tensor, weight: torch.Tensor, decay:
     assert weight.numel() >= mass.numel(), "fewer weights than masses"
     assert mass.dtype == weight.dtype == torch.float32, "masses and weights are fp32"
     _check(load().pc_accumulate(ctx.handle, _ptr(mass), mass.numel(), decay, gain, _ptr(weight), _stream(stream)), "pc_accumulate")
+
+
+# ---- paged cache of a batch
+@dataclass
+class Pages:
+    """A pool of pages: K/V [n_pages][page_tokens][Hkv][d] in the context's element type, keys rotated; page_tokens 16, 32, 64 or 128."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    @staticmethod
+    def empty(ctx: Context, n_pages: int, page_tokens: int = 64) -> "Pages":
+        d = ctx.desc
+        k, v = (torch.empty(n_pages, page_tokens, d.n_kv_heads, d.head_dim, dtype=ctx.torch_dtype, device="cuda") for _ in range(2))
+        return Pages(k, v)
+
+
+@dataclass
+class Batch:
+    """The sequences of a call, on the device in int32: table [n_seqs][max_pages], length [n_seqs] (own tokens, the call's rows included), row_start
+    [n_seqs + 1]; max_rows: no sequence has more rows; prefix: pages of n_prefix tokens that all sequences share."""
+    table: torch.Tensor
+    length: torch.Tensor
+    row_start: torch.Tensor
+    max_rows: int
+    prefix: Optional[torch.Tensor] = None
+    n_prefix: int = 0
+
+
+class PagedWork:
+    """Workspaces of pc_paged_attend."""
+
+    def __init__(self, ctx: Context):
+        self.ctx = ctx                                   # the context outlives its workspaces
+        h = C.c_void_p()
+        _check(load().pc_paged_create(ctx.handle, C.byref(h)), "pc_paged_create")
+        self.handle = h
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            load().pc_paged_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def pc_paged_append(ctx: Context, pages: Pages, batch: Batch, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, stream=None) -> None:
+    """Keys (rotated on the way) and values of a call's rows become the last tokens of their sequences."""
+    _check(_native().paged_append(ctx.handle, ctx.sizes, ctx.device, pages, batch, k, v, pos, _stream(stream)), "pc_paged_append")
+
+
+def pc_paged_attend(work: PagedWork, pages: Pages, batch: Batch, q: torch.Tensor, q_pos: torch.Tensor, causal: bool = True,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False, stream=None):
+    """Attention of a call's rows over their sequences' prefix and own tokens: prompts, their next pieces and tokens (causal), frames (not)."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+    ctx = work.ctx
+    _check(_native().paged_attend(work.handle, ctx.sizes, ctx.device, pages, batch, q, q_pos, causal, out, lse, _stream(stream)), "pc_paged_attend")
+    return (out, lse) if want_lse else out

@@ -36,6 +36,10 @@ enum {
     PC_WHERE_Q4_POS = 12,
     PC_WHERE_Q4_WAIT = 13,
     PC_WHERE_EVICT_NAN = 14,
+    PC_WHERE_PAGED_ROWS = 15,
+    PC_WHERE_PAGED_TABLE = 16,
+    PC_WHERE_PAGED_POS = 17,
+    PC_WHERE_PAGED_WAIT = 18,
 };
 
 constexpr int PC_MAX_SEGMENTS = 3;

@@ -1,0 +1,60 @@
+// Shared by the kernels of the paged cache: the batch as kernels see it, and how a sequence's rows, tokens and pages are looked up.
+#pragma once
+#include "pc_common.cuh"
+
+// Everything here may have been written by the launch before, so it is read past L1 and never as constant data.
+struct PagedBatch {
+    const int32_t *table, *length, *row_start, *prefix;
+    int n_seqs, max_pages, n_prefix, n_pages, n_rows, max_rows;
+    int page_shift;          // log2 of a page's tokens
+    int causal;
+    int32_t *status;
+};
+
+struct PagedSeq { int r0, n, len; };          // first row, rows, own tokens
+
+// A sequence whose numbers make no sense is recorded and has no rows.
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch &B, int s) {
+    const int r0 = __ldcg(B.row_start + s), r1 = __ldcg(B.row_start + s + 1), len = __ldcg(B.length + s);
+    if (r0 < 0 || r1 < r0 || r1 > B.n_rows || r1 - r0 > B.max_rows || len < 0 || (long long)len > ((long long)B.max_pages << B.page_shift)) {
+        pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_ROWS);
+        return {0, 0, 0};
+    }
+    return {r0, r1 - r0, len};
+}
+// rows of the whole batch
+__device__ __forceinline__ int paged_rows(const PagedBatch &B) { return min(max(__ldcg(B.row_start + B.n_seqs), 0), B.n_rows); }
+// A page from a table; one that the pool does not have is recorded and read as its nearest.
+__device__ __forceinline__ int paged_page(const PagedBatch &B, const int32_t *entry) {
+    int p = __ldcg(entry);
+    if (p < 0 || p >= B.n_pages) {
+        pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_TABLE);
+        p = min(max(p, 0), B.n_pages - 1);
+    }
+    return p;
+}
+
+// Inclusive prefix sums over a block of THREADS threads (a multiple of 32, at most 1024); warps' sums go through `sums` [32].
+template <int THREADS, typename T> __device__ __forceinline__ T paged_scan(T v, T *sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    if (lane == 31) sums[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+        T t = lane < THREADS / 32 ? sums[lane] : T(0);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const T u = __shfl_up_sync(0xffffffffu, t, o);
+            if (lane >= o) t += u;
+        }
+        sums[lane] = t;
+    }
+    __syncthreads();
+    if (warp > 0) v += sums[warp - 1];
+    __syncthreads();
+    return v;
+}

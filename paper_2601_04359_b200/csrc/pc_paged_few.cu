@@ -1,0 +1,717 @@
+// Attention over a paged cache on warp-level matrix instructions: calls of few rows a sequence, whose sequences may share a prefix, and every call of the
+// shapes that the tcgen05 kernel does not take.
+//
+// out_i = sum_j 2^(s_ij - m_i) v_j / sum_j 2^(s_ij - m_i), s = log2(e) / sqrt(d) (R q_i) . k_j, over the keys that row i sees.
+//
+// Keys and values are read once a block of query rows, so with few rows the kernel is bound by memory: scores are taken transposed, S^T = K Q^T, a step of 16 keys by 8
+// packed rows (token-major, the heads of a group side by side), so that one token of three to eight heads fills an instruction, and O^T = V^T P^T the same way.
+// A work item is (run of rows, KV head, block of 8 or 16 packed rows); its steps of 16 keys lie on one line with those of all other items, which the warps of the
+// GPU share evenly.  A warp fetches its own steps by TMA into its own ring (a page holds a whole number of steps, so a step is two boxes of 16 rows a 64 channels) and meets no
+// other warp: an item that several warps share leaves (maximum, sum, output) of each in scratch, and k_paged_join adds them up in the order of the keys.
+// The line follows from lengths that lie on the device: every CTA adds them up for itself.
+#include <algorithm>
+
+#include "pc_paged.cuh"
+#include "pc_paged_host.cuh"
+#include "pc_tc.cuh"
+
+namespace {
+
+constexpr int STEP = 16;                                 // keys of a step
+constexpr int BOX_BYTES = STEP * 128;
+constexpr float GROW = 8.f;                              // a row's reference moves once a score is 2^8 beyond it
+constexpr int MAX_ROWS = PAGED_FEW_ROWS;                 // most packed rows of a block
+
+template <int D, bool F32> struct Form {
+    static constexpr int CH = F32 ? 32 : 64;             // channels of a box (128 bytes)
+    static constexpr int BOXES = D / CH;                 // of a step's keys (and again of its values)
+    static constexpr int STAGE = 2 * BOXES * BOX_BYTES;
+    // Ring of a warp and warps of a CTA: as many bytes in flight as shared memory holds.  fp32's 16 KB stages leave six warps of two.
+    static constexpr int STAGES = STAGE <= 4096 ? 4 : (STAGE <= 8192 ? 3 : 2);
+    static constexpr int WARPS = STAGE <= 8192 ? 8 : 6;
+    static constexpr int PARTS = F32 ? 3 : 1;            // bf16 numbers that a value is held as in a product
+    static constexpr int KK = D / 16, CB = D / 16;
+    static constexpr int PLAN_AT = 1024, RING_AT = PLAN_AT + (PC_MAX_SEQS + 8) * 8 / 1024 * 1024 + 1024;
+    static constexpr int SMEM = RING_AT + WARPS * STAGES * STAGE + 1024;
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ float lds32(uint32_t a) {
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(a) : "memory");
+    return x;
+}
+__device__ __forceinline__ float2 lds64(uint32_t a) {
+    float2 x;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(a) : "memory");
+    return x;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// A pair of fp32 numbers as PARTS pairs of bf16 whose sums they are (to 2^-24 with three)
+template <int PARTS> __device__ __forceinline__ void split(float x, float y, uint32_t (&p)[PARTS]) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        p[i] = pc_pack_bf16(x, y);
+        if (i + 1 < PARTS) {
+            x -= pc_bf16_lo(p[i]);
+            y -= pc_bf16_hi(p[i]);
+            if (!(fabsf(x) <= 3e38f)) x = 0.f;            // what an infinity leaves of itself
+            if (!(fabsf(y) <= 3e38f)) y = 0.f;
+        }
+    }
+}
+// d += the product of two sums of parts, smallest terms first; those below 2^-24 of it left out
+template <int PARTS> __device__ __forceinline__ void mma_parts(float (&d)[4], const uint32_t (&a)[PARTS][4], const uint32_t (&b)[PARTS][2]) {
+#pragma unroll
+    for (int sum = PARTS - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = sum; i >= 0; --i) mma16(d, a[i], b[sum - i]);
+}
+// halves of a word that are infinite or NaN, as a mask of those that are not
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    return ((w & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+}
+
+struct FewParams {
+    PagedBatch B;
+    const void *q;
+    const int32_t *q_pos;
+    int n_q_heads, n_kv, group;
+    int shared;              // the prefix is attended apart from the sequences' own tokens, and k_paged_join adds the two up
+    int prefix_here;         // ... in this kernel
+    int block_own, block_prefix;       // packed rows of a block
+    int workers, least;      // warps of the grid; fewest steps of one
+    float scale;
+    void *out;
+    float *lse;
+    float *part_o;           // [2 workers][MAX_ROWS][D]: a warp's first and last item
+    float2 *part_ml;         // [2 workers][MAX_ROWS]
+    float *home_o;           // [2][rows][query heads][D]: items that one warp has done (own, prefix)
+    float2 *home_ml;
+    size_t home_rows;        // rows x query heads of one of the two
+    long long *plan;         // [sequences + 1] first place of a sequence's items on the line, the line's length
+    uint32_t wait_us, extra_tx;
+};
+
+// The line.  Places 0 .. prefix_end - 1 are the prefix items' (block-major), then come the sequences, KV head by KV head.
+struct Line { long long total, prefix_end; int prefix_len, workers; };
+
+__device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
+__device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (rows * group + block - 1) / block; }
+__device__ __forceinline__ int item_len(const FewParams &P, const PagedSeq &S) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(S.len)); }
+__device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block_prefix) : 0; }
+__device__ __forceinline__ Line line_of(const FewParams &P, long long total) {
+    Line L;
+    L.prefix_len = max(1, steps_of(P.B.n_prefix));
+    L.prefix_end = (long long)prefix_blocks(P) * P.n_kv * L.prefix_len;
+    L.total = total;
+    L.workers = (int)min((long long)P.workers, (total + P.least - 1) / P.least);
+    return L;
+}
+__device__ __forceinline__ long long cut(const Line &L, int w) { return L.total * w / L.workers; }
+__device__ __forceinline__ int worker_of(const Line &L, long long place) { return (int)(((place + 1) * L.workers + L.total - 1) / L.total) - 1; }
+// Blocks of a sequence's rows from both ends in turn: where attention is causal, two neighbours on the line have as much to do as any other two.
+__device__ __forceinline__ int zigzag(int k, int n) { return k & 1 ? n - 1 - k / 2 : k / 2; }
+
+struct Item {
+    int r0, n;               // rows of the run, in the batch
+    int s;                   // sequence, -1: all of them over the prefix
+    int h, block, rows;      // KV head, block, packed rows of a block
+    int len;                 // steps
+    int own, before;         // own tokens, those of them before the run
+};
+
+template <int D, bool F32> struct Warp {
+    uint32_t ring, bar;      // its stages and their barriers
+    int lane, done;          // steps it has taken so far
+    bool alive;
+};
+
+// One item's steps j0 .. j1 - 1, in NB blocks of 8 packed rows; what comes out goes to o and ml (whole and not shared: to the output).
+template <int D, bool F32, int NB>
+__device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev &rope, const CUtensorMap *map_k, const CUtensorMap *map_v, Warp<D, F32> &W, volatile int *abort_flag,
+                                          const Item &I, int j0, int j1, bool direct, float *o, float2 *ml, size_t row_pitch) {
+    using F = Form<D, F32>;
+    constexpr int PARTS = F::PARTS, KK = F::KK, CB = F::CB;
+    const int lane = W.lane, quad = lane & 3, eighth = lane >> 2;
+    const int prefix = I.s < 0 || !P.shared ? P.B.n_prefix : 0, prefix_steps = steps_of(prefix);
+    const int packed = I.n * P.group, p0 = I.block * I.rows;
+    // own tokens that a column's row sees, and the most and fewest of a row of the block
+    const auto sees = [&](int p) { return P.B.causal ? I.before + p / P.group + 1 : I.own; };
+    const int most = I.s < 0 ? 0 : min(I.own, sees(min(packed, p0 + I.rows) - 1));
+    const int fewest = I.s < 0 ? 0 : max(0, sees(p0));
+    int lim[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) lim[nb][e] = I.s < 0 ? 0 : sees(min(p0 + nb * 8 + quad * 2 + e, packed - 1));
+    j1 = min(j1, prefix_steps + steps_of(max(0, most)));
+
+    // pages of 32 steps, one a lane
+    const int32_t *own_table = P.B.table + (size_t)max(I.s, 0) * P.B.max_pages;
+    int page = 0, pages_from = j0;
+    const auto look_up = [&](int from) {
+        pages_from = from;
+        const int j = from + lane;
+        if (j < j1) {
+            const bool in_prefix = j < prefix_steps;
+            const int t = (in_prefix ? j : j - prefix_steps) * STEP;
+            page = (paged_page(P.B, (in_prefix ? P.B.prefix : own_table) + (t >> P.B.page_shift)) << P.B.page_shift) + (t & ((1 << P.B.page_shift) - 1));
+        }
+    };
+    const auto fetch = [&](int j, int at) {                // step j, the at-th of this warp
+        if (j >= pages_from + 32) look_up(j);
+        const int y = __shfl_sync(0xffffffffu, page, j - pages_from);
+        if (lane == 0) {
+            const int stage = at % F::STAGES;
+            const uint32_t to = W.ring + stage * F::STAGE, b = W.bar + 8 * stage;
+            pc_mbar_expect_tx(b, F::STAGE + (at == 0 ? P.extra_tx : 0u));
+#pragma unroll
+            for (int i = 0; i < F::BOXES; ++i) {
+                pc_tc::tma_load_2d(to + i * BOX_BYTES, map_k, I.h * D + i * F::CH, y, b);
+                pc_tc::tma_load_2d(to + (F::BOXES + i) * BOX_BYTES, map_v, I.h * D + i * F::CH, y, b);
+            }
+        }
+    };
+    look_up(j0);
+    const int base = W.done - j0;                          // step j is this warp's (base + j)-th
+#pragma unroll 1
+    for (int j = j0; j < min(j1, j0 + F::STAGES); ++j) fetch(j, base + j);
+
+    // Queries, rotated and scaled, as the instructions want them: a lane's channels are whole rotary pairs.  One rounding to bf16 where the context is bf16 (half a
+    // unit of 2^-8, as the keys have it), three parts where it is fp32.
+    uint32_t qf[KK][NB][PARTS][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int p = p0 + nb * 8 + eighth;
+        const bool there = p < packed;
+        const int i = there ? p / P.group : 0, g = there ? p - i * P.group : 0;
+        const size_t row = (size_t)(I.r0 + i);
+        const size_t at = (row * P.n_q_heads + I.h * P.group + g) * D;
+        const int4 pos = there ? __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + row) : make_int4(0, 0, 0, 0);
+        bool bad = false;
+        float2 x[KK][2];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int c = kk * 16 + u * 8 + quad * 2;
+                if constexpr (F32) {
+                    x[kk][u] = there ? __ldcg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + at + c)) : make_float2(0.f, 0.f);
+                } else {
+                    const uint32_t w = there ? __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + at + c)) : 0u;
+                    x[kk][u] = make_float2(pc_bf16_lo(w), pc_bf16_hi(w));
+                }
+            }
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float2 y = pc_rotate(x[kk][u].x, x[kk][u].y, pc_rope_cs_clamped(rope, kk * 8 + u * 4 + quad, pos.x, pos.y, pos.z, bad));
+                uint32_t parts[PARTS];
+                split<PARTS>(__fmul_rn(y.x, P.scale), __fmul_rn(y.y, P.scale), parts);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) qf[kk][nb][i][u] = parts[i];
+            }
+        if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
+    }
+
+    float acc[CB][NB][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[cb][nb][i] = 0.f;
+        m[nb][0] = m[nb][1] = -INFINITY;
+        l[nb][0] = l[nb][1] = 0.f;
+    }
+    const int lrow = (lane & 7) + ((lane >> 3) & 1) * 8, lchunk = lane >> 4;              // ldmatrix: keys as rows
+    const int trow = (lane & 7) + (lane >> 4) * 8, tchunk = (lane >> 3) & 1;              // values, transposed
+
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+        const int at = base + j, stage = at % F::STAGES;
+        const uint32_t ks = W.ring + stage * F::STAGE, vs = ks + F::BOXES * BOX_BYTES;
+        W.alive = __all_sync(0xffffffffu, pc_mbar_wait(W.bar + 8 * stage, (at / F::STAGES) & 1, abort_flag, P.B.status, PC_WHERE_PAGED_WAIT, P.wait_us));
+        if (!W.alive) return;
+
+        // ---- scores of 16 keys (rows: eighth, eighth + 8) by 8 NB packed rows (columns: 2 quad, 2 quad + 1)
+        float sc[NB][4];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[nb][i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            uint32_t a[PARTS][4];
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = eighth + (i & 1) * 8, c = (kk & 1) * 16 + (i >> 1) * 8 + quad * 2;
+                    const float2 x = lds64(ks + (kk >> 1) * BOX_BYTES + key * 128 + (((c >> 2) ^ (key & 7)) << 4) + (c & 3) * 4);
+                    uint32_t parts[PARTS];
+                    split<PARTS>(x.x, x.y, parts);
+#pragma unroll
+                    for (int u = 0; u < PARTS; ++u) a[u][i] = parts[u];
+                }
+            } else {
+                ldsm4(a[0], ks + (kk >> 2) * BOX_BYTES + lrow * 128 + ((((kk & 3) * 2 + lchunk) ^ (lrow & 7)) << 4));
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_parts<PARTS>(sc[nb], a, qf[kk][nb]);
+        }
+        // ---- keys that are there: all 16 but in a segment's last step and where rows of the block end
+        const bool in_prefix = j < prefix_steps;
+        const int key0 = (in_prefix ? j : j - prefix_steps) * STEP;
+        const int nv_most = min(STEP, (in_prefix ? prefix : most) - key0), nv_fewest = min(STEP, (in_prefix ? prefix : fewest) - key0);
+        if (nv_fewest < STEP) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int nv = in_prefix ? nv_most : min(nv_most, lim[nb][e] - key0);
+                    if (eighth >= nv) sc[nb][e] = -INFINITY;
+                    if (eighth + 8 >= nv) sc[nb][2 + e] = -INFINITY;
+                }
+        }
+        // ---- running maximum: the reference moves only where a score is well beyond it, so most steps take no shuffles
+        bool grow = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) grow |= fmaxf(sc[nb][e], sc[nb][2 + e]) > m[nb][e] + GROW;
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(sc[nb][e], sc[nb][2 + e]);
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+                    x = fmaxf(x, m[nb][e]);
+                    const float f = x == -INFINITY ? 1.f : exp2_fast(m[nb][e] - x);
+                    m[nb][e] = x;
+                    l[nb][e] *= f;
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        acc[cb][nb][e] *= f;
+                        acc[cb][nb][2 + e] *= f;
+                    }
+                }
+        }
+        uint32_t pb[NB][PARTS][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float r0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0], r1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1];
+            sc[nb][0] = exp2_fast(sc[nb][0] - r0);
+            sc[nb][1] = exp2_fast(sc[nb][1] - r1);
+            sc[nb][2] = exp2_fast(sc[nb][2] - r0);
+            sc[nb][3] = exp2_fast(sc[nb][3] - r1);
+            l[nb][0] += sc[nb][0] + sc[nb][2];
+            l[nb][1] += sc[nb][1] + sc[nb][3];
+            uint32_t lo[PARTS], hi[PARTS];
+            split<PARTS>(sc[nb][0], sc[nb][1], lo);
+            split<PARTS>(sc[nb][2], sc[nb][3], hi);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                pb[nb][i][0] = transpose8(lo[i]);
+                pb[nb][i][1] = transpose8(hi[i]);
+            }
+        }
+        // ---- O^T += V^T P^T.  Values of keys that no row of the block sees are taken as zero whatever lies there.  Where some rows see a key and others do not, an infinite
+        // or NaN value would reach all of them (0 times it is NaN): it is taken out of the product and added to those that see it.  (fp32's parts cannot hold one, so there always.)
+        const uint32_t keep0 = (quad * 2 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 1 < nv_most ? 0xFFFF0000u : 0u);
+        const uint32_t keep1 = (quad * 2 + 8 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 9 < nv_most ? 0xFFFF0000u : 0u);
+        const bool check = F32 || nv_fewest < nv_most;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            uint32_t a[PARTS][4];
+            bool odd = false;
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = quad * 2 + (i >> 1) * 8, c = (cb & 1) * 16 + (i & 1) * 8 + eighth;
+                    const uint32_t box = vs + (cb >> 1) * BOX_BYTES + (c & 3) * 4;
+                    float x = lds32(box + key * 128 + (((c >> 2) ^ (key & 7)) << 4));
+                    float y = lds32(box + (key + 1) * 128 + (((c >> 2) ^ ((key + 1) & 7)) << 4));
+                    if (key >= nv_most) x = 0.f;
+                    if (key + 1 >= nv_most) y = 0.f;
+                    if (!(fabsf(x) <= 3.3e38f)) { odd = true; x = 0.f; }
+                    if (!(fabsf(y) <= 3.3e38f)) { odd = true; y = 0.f; }
+                    uint32_t parts[PARTS];
+                    split<PARTS>(x, y, parts);
+#pragma unroll
+                    for (int u = 0; u < PARTS; ++u) a[u][i] = parts[u];
+                }
+            } else {
+                ldsm4t(a[0], vs + (cb >> 2) * BOX_BYTES + trow * 128 + ((((cb & 3) * 2 + tchunk) ^ (trow & 7)) << 4));
+                if (nv_most < STEP) {
+                    a[0][0] &= keep0;
+                    a[0][1] &= keep0;
+                    a[0][2] &= keep1;
+                    a[0][3] &= keep1;
+                }
+                if (check) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t f = finite_halves(a[0][i]);
+                        odd |= f != 0xFFFFFFFFu;
+                        a[0][i] &= f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_parts<PARTS>(acc[cb][nb], a, pb[nb]);
+            if (check && __any_sync(0xffffffffu, odd)) {
+#pragma unroll 1
+                for (int key = 0; key < nv_most; ++key)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float v;
+                        if constexpr (F32) {
+                            const int c = (cb & 1) * 16 + u * 8 + eighth;
+                            v = lds32(vs + (cb >> 1) * BOX_BYTES + key * 128 + (((c >> 2) ^ (key & 7)) << 4) + (c & 3) * 4);
+                        } else {
+                            const uint32_t w = __float_as_uint(lds32(vs + (cb >> 2) * BOX_BYTES + key * 128 + ((((cb & 3) * 2 + u) ^ (key & 7)) << 4) + (eighth >> 1) * 4));
+                            v = eighth & 1 ? pc_bf16_hi(w) : pc_bf16_lo(w);
+                        }
+                        if (fabsf(v) <= 3.3e38f || (!F32 && fabsf(v) < INFINITY)) continue;
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (in_prefix || key < lim[nb][e] - key0) acc[cb][nb][2 * u + e] += v;
+                    }
+            }
+        }
+        __syncwarp();
+        if (j + F::STAGES < j1) fetch(j + F::STAGES, at + F::STAGES);
+    }
+    W.done += max(0, j1 - j0);
+
+    // ---- out
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        float inv[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) inv[e] = !direct ? 1.f : (l[nb][e] > 0.f ? 1.f / l[nb][e] : (l[nb][e] != l[nb][e] ? l[nb][e] : 0.f));       // nothing seen: 0
+        const auto place = [&](int p) {                    // where a packed row goes, in rows of D
+            if (!row_pitch) return (size_t)(p - p0);
+            const int i = p / P.group;
+            return (size_t)(I.r0 + i) * P.n_q_heads + I.h * P.group + (p - i * P.group);
+        };
+        if (!F32 && direct) {
+            const int p = p0 + nb * 8 + eighth;
+            __nv_bfloat16 *row = static_cast<__nv_bfloat16 *>(P.out) + place(min(p, packed - 1)) * D + quad * 2;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t w = transpose8(pc_pack_bf16(acc[cb][nb][2 * u] * inv[0], acc[cb][nb][2 * u + 1] * inv[1]));
+                    if (p < packed) *reinterpret_cast<uint32_t *>(row + cb * 16 + u * 8) = w;
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int p = p0 + nb * 8 + quad * 2 + e;
+                if (p >= packed) continue;
+                float *row = (direct ? static_cast<float *>(P.out) : o) + place(p) * D + eighth;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    row[cb * 16] = acc[cb][nb][e] * inv[e];
+                    row[cb * 16 + 8] = acc[cb][nb][2 + e] * inv[e];
+                }
+            }
+        }
+        if (eighth == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int p = p0 + nb * 8 + quad * 2 + e;
+                if (p >= packed) continue;
+                if (!direct) ml[place(p)] = make_float2(m[nb][e], l[nb][e]);
+                else if (P.lse) P.lse[place(p)] = (m[nb][e] + log2f(l[nb][e])) * 0.6931471805599453f;
+            }
+        }
+    }
+}
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(Form<D, F32>::WARPS * 32, 1)
+k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FewParams P, const pc_rope_dev rope) {
+    using F = Form<D, F32>;
+    pc_grid_dep_launch();
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *gen = smem_raw + (base - pc_smem_u32(smem_raw));
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 512);
+    long long *sums = reinterpret_cast<long long *>(gen + 640), *plan = reinterpret_cast<long long *>(gen + F::PLAN_AT);
+    const int warp = threadIdx.x >> 5;
+    Warp<D, F32> W;
+    W.lane = threadIdx.x & 31;
+    W.bar = base + warp * F::STAGES * 8;
+    W.ring = base + F::RING_AT + warp * F::STAGES * F::STAGE;
+    W.done = 0;
+    W.alive = true;
+    if (threadIdx.x == 0) *abort_flag = 0;
+    if (W.lane == 0) {
+        for (int i = 0; i < F::STAGES; ++i) pc_mbar_init(W.bar + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    pc_grid_dep_wait();
+
+    // ---- the line
+    constexpr int THREADS = F::WARPS * 32;
+    const int pblocks = prefix_blocks(P);
+    const long long prefix_end = (long long)pblocks * P.n_kv * max(1, steps_of(P.B.n_prefix));
+    long long at = prefix_end;
+    for (int s0 = 0; s0 < P.B.n_seqs; s0 += THREADS) {
+        const int s = s0 + threadIdx.x;
+        long long v = 0;
+        if (s < P.B.n_seqs) {
+            const PagedSeq S = paged_seq(P.B, s);
+            v = (long long)blocks_of(S.n, P.group, P.block_own) * P.n_kv * item_len(P, S);
+        }
+        const long long end = paged_scan<THREADS>(v, sums);
+        if (s < P.B.n_seqs) plan[s] = at + end - v;
+        at += sums[F::WARPS - 1];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) plan[P.B.n_seqs] = at;
+    __syncthreads();
+    if (P.plan && blockIdx.x == 0)
+        for (int s = threadIdx.x; s <= P.B.n_seqs; s += THREADS) P.plan[s] = plan[s];
+    const Line L = line_of(P, at);
+
+    // ---- this warp's part of it; neighbours on the line are on different SMs
+    const int w = warp * gridDim.x + blockIdx.x;
+    if (at == 0 || w >= L.workers) return;
+    long long g = cut(L, w);
+    const long long g1 = cut(L, w + 1);
+    while (g < g1 && W.alive) {
+        Item I;
+        int off;
+        if (g < L.prefix_end) {
+            const int item = (int)(g / L.prefix_len);
+            off = (int)(g - (long long)item * L.prefix_len);
+            I = {0, paged_rows(P.B), -1, item % P.n_kv, item / P.n_kv, P.block_prefix, L.prefix_len, 0, 0};
+        } else {
+            int lo = 0, hi = P.B.n_seqs - 1;               // the last sequence that begins at or before g (one without rows has no places)
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (plan[mid] <= g) lo = mid; else hi = mid - 1;
+            }
+            const PagedSeq S = paged_seq(P.B, lo);
+            const int len = item_len(P, S), blocks = blocks_of(S.n, P.group, P.block_own);
+            const long long y = g - plan[lo], item = y / len;
+            off = (int)(y - item * len);
+            I = {S.r0, S.n, lo, (int)(item / blocks), zigzag((int)(item % blocks), blocks), P.block_own, len, S.len, S.len - S.n};
+        }
+        const int take = (int)min((long long)(I.len - off), g1 - g);
+        const bool whole = off == 0 && take == I.len, direct = whole && !P.shared;
+        float *o = P.part_o + (size_t)(2 * w + (off == 0)) * MAX_ROWS * D;
+        float2 *ml = P.part_ml + (size_t)(2 * w + (off == 0)) * MAX_ROWS;
+        if (whole && P.shared) {
+            o = P.home_o + (I.s < 0 ? P.home_rows * D : 0);
+            ml = P.home_ml + (I.s < 0 ? P.home_rows : 0);
+        }
+        if (I.rows == 8) take_unit<D, F32, 1>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, direct, o, ml, whole);
+        else take_unit<D, F32, 2>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, direct, o, ml, whole);
+        g += take;
+    }
+    if (!W.alive) pc_let_copies_land();
+}
+
+// ------------------------------------------------------------------------------------------------ the parts of an item added up
+// A CTA has one block of a sequence's packed rows of one KV head: JOIN_WARPS warps in as many sets as its rows leave, each set every so-many-th part of every row; then the sets, in their
+// order.  The order is that of the keys, so a call gives the same bits every time.
+constexpr int JOIN_WARPS = 16;
+
+struct JoinParams {
+    FewParams F;
+    PagedTcParts T;          // what the tcgen05 kernel has left of the prefix
+};
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_constant__ JoinParams J) {
+    constexpr int E = D / 32;                              // channels of a lane
+    __shared__ float so[JOIN_WARPS][D];
+    __shared__ float2 sml[JOIN_WARPS];
+    const FewParams &P = J.F;
+    pc_grid_dep_launch();
+    const int s = blockIdx.x % P.B.n_seqs, k = blockIdx.x / P.B.n_seqs, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pc_grid_dep_wait();
+    const PagedSeq S = paged_seq(P.B, s);
+    const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block_own);
+    if (k >= blocks) return;
+    const int block = zigzag(k, blocks), p0 = block * P.block_own, n = min(P.block_own, packed - p0);
+    const Line L = line_of(P, __ldcg(P.plan + P.B.n_seqs));
+    const int len = item_len(P, S);
+    const long long first = __ldcg(P.plan + s) + ((long long)h * blocks + k) * len;
+    const int w0 = worker_of(L, first), w1 = worker_of(L, first + len - 1);
+    if (!P.shared && w0 == w1) return;                     // its warp has written the output
+    const int sets = JOIN_WARPS / n, r = warp % n, set = warp / n;
+    float o[E] = {}, M = -INFINITY, l = 0.f;
+    if (set < sets) {
+        const int p = p0 + r, i = p / P.group;
+        const size_t home = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
+        const auto add = [&](const float *po, float2 y, size_t pitch) {
+            float x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = __ldcg(po + e * pitch);
+            const float m = fmaxf(M, y.x), f = m == -INFINITY ? 1.f : exp2_fast(M - m), g = m == -INFINITY ? 1.f : exp2_fast(y.x - m);
+            M = m;
+            l = l * f + y.y * g;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * g;
+        };
+        // own parts: worker w0's last item, the others' first
+        const int own = w1 - w0 + 1;
+#pragma unroll 4
+        for (int c = set; c < own; c += sets) {
+            const size_t slot = own == 1 ? 0 : (size_t)(2 * (w0 + c) + (c == 0)) * MAX_ROWS + r;
+            const float *po = own == 1 ? P.home_o + home * D : P.part_o + slot * D;
+            add(po + lane, own == 1 ? __ldcg(P.home_ml + home) : __ldcg(P.part_ml + slot), 32);
+        }
+        if (P.shared) {
+            const long long row = (long long)S.r0 * P.group + p;          // packed row of the batch
+            if (P.prefix_here) {
+                const long long item = row / P.block_prefix * P.n_kv + h;
+                const int v0 = worker_of(L, item * L.prefix_len), v1 = worker_of(L, (item + 1) * L.prefix_len - 1), parts = v1 - v0 + 1;
+                const int rr = (int)(row % P.block_prefix);
+#pragma unroll 4
+                for (int c = set; c < parts; c += sets) {
+                    const size_t slot = parts == 1 ? 0 : (size_t)(2 * (v0 + c) + (c == 0)) * MAX_ROWS + rr;
+                    const float *po = parts == 1 ? P.home_o + (P.home_rows + home) * D : P.part_o + slot * D;
+                    add(po + lane, parts == 1 ? __ldcg(P.home_ml + P.home_rows + home) : __ldcg(P.part_ml + slot), 32);
+                }
+            } else if (P.B.n_prefix > 0) {
+                const PagedTcRow T = paged_tc_row(J.T, h, row);
+#pragma unroll 4
+                for (int c = set; c < T.parts; c += sets)
+                    add(J.T.part_o + ((T.first + c) * PAGED_TC_TILE + T.row) * D + lane, __ldcg(J.T.part_ml + (T.first + c) * PAGED_TC_TILE + T.row), 32);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) so[warp][e * 32 + lane] = o[e];
+        if (lane == 0) sml[warp] = make_float2(M, l);
+    }
+    __syncthreads();
+    if (warp >= n) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    M = -INFINITY;
+    for (int c = 0; c < sets; ++c) M = fmaxf(M, sml[c * n + warp].x);
+    l = 0.f;
+    for (int c = 0; c < sets; ++c) {
+        const float2 y = sml[c * n + warp];
+        const float g = M == -INFINITY ? 1.f : exp2_fast(y.x - M);
+        l = fmaf(y.y, g, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(so[c * n + warp][e * 32 + lane], g, o[e]);
+    }
+    const int p = p0 + warp, i = p / P.group;
+    const size_t to = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
+    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if constexpr (F32) static_cast<float *>(P.out)[to * D + e * 32 + lane] = o[e] * inv;
+        else static_cast<__nv_bfloat16 *>(P.out)[to * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
+    }
+    if (P.lse && lane == 0) P.lse[to] = (M + log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D, bool F32> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, int max_blocks, cudaStream_t stream) {
+    using F = Form<D, F32>;
+    static bool attr_set[PC_MAX_DEVICES] = {};
+    if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
+    if (!attr_set[ctx->device]) {
+        PC_CUDA_TRY(cudaFuncSetAttribute(k_paged_few<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM));
+        attr_set[ctx->device] = true;
+    }
+    JoinParams j = J;
+    j.F.workers = ctx->sm_count * F::WARPS;
+    PC_LAUNCH((k_paged_few<D, F32>), dim3(ctx->sm_count), dim3(F::WARPS * 32), F::SMEM, stream, mk, mv, j.F, ctx->rope);
+    PC_LAUNCH((k_paged_join<D, F32>), dim3((unsigned)(J.F.B.n_seqs * max_blocks), J.F.n_kv), dim3(JOIN_WARPS * 32), 0, stream, j);
+    return PC_OK;
+}
+
+}  // namespace
+
+// Rows as [page x token][KV head x channel], boxes of 16 tokens by 128 bytes
+static bool few_map(CUtensorMap *m, const void *p, const pc_paged_args &A) {
+    const pc_tc::EncodeTiledFn fn = pc_tc::encode_fn();
+    if (!fn) return false;
+    const pc_layer_desc &D = A.ctx->desc;
+    const bool f32 = D.dtype == PC_F32;
+    const cuuint64_t dims[2] = {(cuuint64_t)D.n_kv_heads * D.head_dim, (cuuint64_t)A.batch.n_pages << A.batch.page_shift}, strides[1] = {dims[0] * (f32 ? 4 : 2)};
+    const cuuint32_t box[2] = {f32 ? 32u : 64u, STEP}, estr[2] = {1, 1};
+    return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t pc_paged_few_parts(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count * 8 * MAX_ROWS; }
+
+pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream) {
+    const pc_ctx *ctx = A.ctx;
+    const pc_layer_desc &D = ctx->desc;
+    CUtensorMap mk, mv;
+    if (!few_map(&mk, A.pages->k, A) || !few_map(&mv, A.pages->v, A)) {
+        fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
+        return PC_ERR_CUDA;
+    }
+    JoinParams J{};
+    FewParams &P = J.F;
+    P.B = A.batch;
+    P.q = A.q;
+    P.q_pos = A.q_pos;
+    P.n_q_heads = D.n_q_heads;
+    P.n_kv = D.n_kv_heads;
+    P.group = ctx->group;
+    P.shared = shared;
+    P.prefix_here = shared && !tc && A.batch.n_prefix > 0;
+    P.block_own = A.batch.max_rows * ctx->group <= 8 ? 8 : MAX_ROWS;
+    P.block_prefix = (long long)A.batch.n_rows * ctx->group <= 8 ? 8 : MAX_ROWS;
+    P.least = 2;
+    P.scale = pc_q_rot_scale(D.head_dim);
+    P.out = A.out;
+    P.lse = A.lse;
+    P.part_o = w->few_o;
+    P.part_ml = w->few_ml;
+    P.home_o = w->home_o;
+    P.home_ml = w->home_ml;
+    P.home_rows = w->home_rows * D.n_q_heads;
+    P.plan = w->plan;
+    P.wait_us = ctx->wait_limit_us;
+    P.extra_tx = ctx->test_extra_tx;
+    if (tc) J.T = *tc;
+    const int max_blocks = (int)(((long long)A.batch.max_rows * ctx->group + P.block_own - 1) / P.block_own);
+    const bool f32 = D.dtype == PC_F32;
+    if (D.head_dim == 128) return f32 ? launch<128, true>(mk, mv, J, ctx, max_blocks, stream) : launch<128, false>(mk, mv, J, ctx, max_blocks, stream);
+    return f32 ? launch<64, true>(mk, mv, J, ctx, max_blocks, stream) : launch<64, false>(mk, mv, J, ctx, max_blocks, stream);
+}

@@ -1,0 +1,41 @@
+// Host side shared by the paged cache's entry points and launchers.
+#pragma once
+#include "pc_paged.cuh"
+
+constexpr int PAGED_FEW_ROWS = 16;           // most packed rows of a block of the few-row kernel
+constexpr int PAGED_HOME_ROWS = 1024;        // most rows of a call whose prefix is attended apart
+constexpr int PAGED_TC_TILE = 128;           // packed rows of a tile of the tcgen05 kernel
+
+struct pc_paged {
+    pc_ctx *ctx;
+    float *few_o, *home_o;
+    float2 *few_ml, *home_ml;
+    size_t home_rows;
+    long long *plan;
+};
+
+struct pc_paged_args {
+    pc_ctx *ctx;
+    PagedBatch batch;
+    const pc_pages *pages;
+    const void *q;
+    const int32_t *q_pos;
+    void *out;
+    float *lse;
+};
+
+// What the tcgen05 kernel leaves of a shared prefix: `parts` pieces of its keys for every tile of packed rows of every KV head, each a tile of rows of d fp32
+// values and their (maximum, sum)
+struct PagedTcParts {
+    const float *part_o;
+    const float2 *part_ml;
+    int tiles, parts;
+};
+struct PagedTcRow { size_t first; int row, parts; };
+__device__ __forceinline__ PagedTcRow paged_tc_row(const PagedTcParts &T, int h, long long packed_row) {
+    return {((size_t)h * T.tiles + (size_t)(packed_row / PAGED_TC_TILE)) * T.parts, (int)(packed_row % PAGED_TC_TILE), T.parts};
+}
+
+size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kernel's scratch
+// shared: the prefix is attended apart from the sequences' own tokens, here or (tc given) by the tcgen05 kernel before
+pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream);

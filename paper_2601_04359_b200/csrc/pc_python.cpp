@@ -21,7 +21,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift;
+PyObject *s_data_ptr, *s_is_contiguous, *s_shape, *s_k, *s_v, *s_pos, *s_n_tokens, *s_anchors, *s_history, *s_frame_count, *s_value, *s_rows, *s_weight, *s_t_shift, *s_table, *s_length, *s_row_start, *s_prefix, *s_n_prefix, *s_max_rows;
 PyObject *g_f32, *g_tensor, *g_refusal;          // torch.float32, torch.Tensor; the binding's error, made of a status and a text
 const DLPackExchangeAPI *g_exchange;              // through which a tensor describes itself in one call
 PyObject *g_as_i32;       // numpy.ascontiguousarray(x, dtype=int32), for anything that is not an int32 array already
@@ -166,8 +166,9 @@ enum Type { I32, F32, BF16, U8, BYTE /* any of one byte */ };
 // type and bytes one attribute after the other are five calls of 0.05 to 0.1 us a tensor, of which a call has six to eleven.
 struct Tensor {
     void *p = nullptr;                                // null for None
-    int64_t rows = 0, n = 0;                          // first extent, elements
+    int64_t rows = 0, second = 0, n = 0;              // first and second extent, elements
     DLDataType type{};
+    DLDevice device{};
     bool none = true;
 
     bool take(PyObject *t) {
@@ -190,7 +191,9 @@ struct Tensor {
         }
         p = static_cast<char *>(d.data) + d.byte_offset;
         rows = d.ndim > 0 ? d.shape[0] : 1;
+        second = d.ndim > 1 ? d.shape[1] : 1;
         type = d.dtype;
+        device = d.device;
         none = false;
         return true;
     }
@@ -216,6 +219,12 @@ struct Tensor {
         }
         if (how == EXACTLY ? n == want : n >= want) return true;
         refuse("%s has %lld elements, %lld are needed", what, (long long)n, (long long)want);
+        return false;
+    }
+    // It lies on this GPU (any, if negative); None and tensors without elements are left to the library
+    bool on(int gpu, const char *what) const {
+        if (gpu < 0 || none || n == 0 || (device.device_type == kDLCUDA && device.device_id == gpu)) return true;
+        refuse("%s is not on the context's device", what);
         return false;
     }
 };
@@ -526,6 +535,67 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {             // c
     });
 }
 
+// Pages and Batch as the library takes them.  Table, lengths and row starts are read to the ends that the kernels trust, so they have to be as long as that.
+struct PagedArg {
+    pc_pages pages{};
+    pc_batch batch{};
+    bool take(PyObject *p, PyObject *b, const Sizes &z, int gpu) {
+        Tensor k, v, table, length, row_start, prefix;
+        if (!tensor_attr(p, s_k, &k) || !tensor_attr(p, s_v, &v) || !tensor_attr(b, s_table, &table) || !tensor_attr(b, s_length, &length) ||
+            !tensor_attr(b, s_row_start, &row_start) || !tensor_attr(b, s_prefix, &prefix)) return false;
+        const int64_t n = length.rows, n_prefix = int_attr(b, s_n_prefix), max_rows = int_attr(b, s_max_rows);
+        if (failed()) return false;
+        if (n > PC_MAX_SEQS || k.rows > INT32_MAX || k.second > INT32_MAX || table.second > INT32_MAX) {
+            refuse("more than a call takes: %lld sequences, %lld pages of %lld tokens, %lld pages a sequence", (long long)n, (long long)k.rows, (long long)k.second, (long long)table.second);
+            return false;
+        }
+        const int64_t page = k.second > 0 ? k.second : 1;
+        if (k.none || v.none || length.none || row_start.none || table.none) {
+            refuse("pages, table, length and row_start are needed");
+            return false;
+        }
+        pages = pc_pages{k.p, v.p, (int32_t)k.rows, (int32_t)k.second};
+        batch = pc_batch{static_cast<int32_t *>(table.p), static_cast<int32_t *>(length.p), static_cast<int32_t *>(row_start.p), static_cast<int32_t *>(prefix.p),
+                         (int32_t)n, (int32_t)table.second, (int32_t)n_prefix, (int32_t)max_rows};
+        return k.fits(z.type, k.rows * k.second * z.kv_row(), Tensor::EXACTLY, "pages.k") && v.fits(z.type, k.n, Tensor::EXACTLY, "pages.v") &&
+               length.fits(I32, n, Tensor::EXACTLY, "length") && table.fits(I32, n * table.second, Tensor::EXACTLY, "table") &&
+               row_start.fits(I32, n + 1, Tensor::AT_LEAST, "row_start") && prefix.fits(I32, (n_prefix + page - 1) / page, Tensor::AT_LEAST, "prefix") &&
+               k.on(gpu, "pages.k") && v.on(gpu, "pages.v") && length.on(gpu, "length") && table.on(gpu, "table") && row_start.on(gpu, "row_start") && prefix.on(gpu, "prefix");
+    }
+};
+
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {      // ctx, sizes, device, pages, batch, k, v, pos, stream
+    if (!arity(n, 9)) return nullptr;
+    Sizes z;
+    PagedArg g;
+    Tensor k, v, pos;
+    void *ctx = handle_of(a[0]), *stream = stream_of(a[8]);
+    const int gpu = int_of(a[2]);
+    if (failed() || !z.take(a[1]) || !g.take(a[3], a[4], z, gpu) || !k.take(a[5]) || !v.take(a[6]) || !pos.take(a[7])) return nullptr;
+    const int64_t rows = k.rows;
+    if (!k.fits(z.type, rows * z.kv_row(), Tensor::EXACTLY, "k") || !v.fits(z.type, rows * z.kv_row(), Tensor::EXACTLY, "v") ||
+        !pos.fits(I32, 4 * rows, Tensor::AT_LEAST, "pos") || !k.on(gpu, "k") || !v.on(gpu, "v") || !pos.on(gpu, "pos")) return nullptr;
+    return call([&] { return pc_paged_append(static_cast<pc_ctx *>(ctx), &g.pages, &g.batch, k.p, v.p, static_cast<int32_t *>(pos.p), (int32_t)rows, stream); });
+}
+
+PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {      // work, sizes, device, pages, batch, q, q_pos, causal, out, lse, stream
+    if (!arity(n, 11)) return nullptr;
+    Sizes z;
+    PagedArg g;
+    Tensor q, q_pos, out, lse;
+    void *work = handle_of(a[0]), *stream = stream_of(a[10]);
+    const int gpu = int_of(a[2]), causal = PyObject_IsTrue(a[7]);
+    if (failed() || !z.take(a[1]) || !g.take(a[3], a[4], z, gpu) || !q.take(a[5]) || !q_pos.take(a[6]) || !out.take(a[8]) || !lse.take(a[9])) return nullptr;
+    const int64_t rows = q.rows;
+    if (!q.fits(z.type, rows * z.q_row(), Tensor::EXACTLY, "q") || !q_pos.fits(I32, 4 * rows, Tensor::AT_LEAST, "q_pos") ||
+        !out.fits(z.type, rows * z.q_row(), Tensor::AT_LEAST, "out") || !lse.fits(F32, rows * z.hq, Tensor::AT_LEAST, "lse") || !q.on(gpu, "q") || !q_pos.on(gpu, "q_pos") ||
+        !out.on(gpu, "out") || !lse.on(gpu, "lse")) return nullptr;
+    return call([&] {
+        return pc_paged_attend(static_cast<pc_paged *>(work), &g.pages, &g.batch, q.p, static_cast<int32_t *>(q_pos.p), (int32_t)rows, causal, out.p,
+                               static_cast<float *>(lse.p), stream);
+    });
+}
+
 PyObject *set_i32_converter(PyObject *, PyObject *f) {
     Py_INCREF(f);
     Py_XSETREF(g_as_i32, f);
@@ -552,7 +622,7 @@ PyObject *set_types(PyObject *, PyObject *const *a, Py_ssize_t n) {        // to
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(plan_budget), FAST(total), FAST(score), FAST(compact), FAST(attend_frame), FAST(attend_prepare), FAST(attend_prepared),
                          FAST(attend_mass), FAST(frame_step), FAST(window_append), FAST(window_step),
-                         FAST(q4_store), FAST(q4_load), FAST(q4_attend), FAST(q4_evict), FAST(evict), FAST(set_types),
+                         FAST(q4_store), FAST(q4_load), FAST(q4_attend), FAST(q4_evict), FAST(evict), FAST(paged_append), FAST(paged_attend), FAST(set_types),
                          {"set_i32_converter", set_i32_converter, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackcache.so on the binding's objects.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -561,7 +631,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_packcache_py", "Calls of libpackc
 PyMODINIT_FUNC PyInit__packcache_py(void) {
     struct { PyObject **at; const char *name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_is_contiguous, "is_contiguous"}, {&s_shape, "shape"},
         {&s_k, "k"}, {&s_v, "v"}, {&s_pos, "pos"}, {&s_n_tokens, "n_tokens"}, {&s_anchors, "anchors"}, {&s_history, "history"},
-        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"}};
+        {&s_frame_count, "frame_count"}, {&s_value, "value"}, {&s_rows, "rows"}, {&s_weight, "weight"}, {&s_t_shift, "t_shift"},
+        {&s_table, "table"}, {&s_length, "length"}, {&s_row_start, "row_start"}, {&s_prefix, "prefix"}, {&s_n_prefix, "n_prefix"}, {&s_max_rows, "max_rows"}};
     for (auto &x : names)
         if (!(*x.at = PyUnicode_InternFromString(x.name))) return nullptr;
     return PyModule_Create(&module);
