@@ -481,7 +481,7 @@ pc_status pc_accumulate(pc_ctx *ctx, const float *mass, int32_t n, float decay, 
  * a number that makes no sense (a sequence with more rows than max_rows, with more tokens than its pages hold or with rows outside the call's, a page that
  * the pool does not have, a position outside the rotary tables) is recorded in the status word: the sequence is skipped, the page not written (its nearest neighbour read), the
  * position clamped. */
-#define PC_MAX_SEQS 1024 /* most sequences of a call */
+#define PC_MAX_SEQS 512 /* most sequences of a call */
 
 typedef struct {
     void *k;              /* device [n_pages][page_tokens][Hkv][d], 16-byte aligned */

@@ -8,7 +8,7 @@ namespace {
 
 // A warp per row and up to 8 chunks a lane: a chunk is eight channels (16 bytes, 32 in fp32), whole rotary pairs, and all chunks of a lane lie at the same place
 // of a head (256 is a multiple of d), so four table entries serve them.  Keys and values are requested first; what they wait for behind that is where they go: the
-// row's sequence (a search by all lanes at once, two looks for up to 1,024 sequences), its length, its page.
+// row's sequence (a search by all lanes at once, two looks at most), its length, its page.
 constexpr int APPEND_THREADS = 256;
 
 struct AppendParams {
@@ -176,7 +176,7 @@ extern "C" pc_status pc_paged_create(pc_ctx *ctx, pc_paged **out) {
         PC_CUDA_TRY(cudaMalloc(&w->few_ml, few * sizeof(float2)));
         PC_CUDA_TRY(cudaMalloc(&w->home_o, home * D.head_dim * sizeof(float)));
         PC_CUDA_TRY(cudaMalloc(&w->home_ml, home * sizeof(float2)));
-        PC_CUDA_TRY(cudaMalloc(&w->plan, (PC_MAX_SEQS + 1) * sizeof(long long)));
+        PC_CUDA_TRY(cudaMalloc(&w->plan, (PC_MAX_SEQS + PAGED_PLAN_HEAD) * sizeof(long long)));
         return PC_OK;
     };
     const pc_status st = fill();

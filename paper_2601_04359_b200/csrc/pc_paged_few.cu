@@ -31,8 +31,11 @@ template <int D, bool F32> struct Form {
     static constexpr int WARPS = STAGE <= 8192 ? 8 : 6;
     static constexpr int PARTS = F32 ? 3 : 1;            // bf16 numbers that a value is held as in a product
     static constexpr int KK = D / 16, CB = D / 16;
-    static constexpr int PLAN_AT = 1024, RING_AT = PLAN_AT + (PC_MAX_SEQS + 8) * 8 / 1024 * 1024 + 1024;
-    static constexpr int SMEM = RING_AT + WARPS * STAGES * STAGE + 1024;
+    static constexpr int Q_BYTES = 8 * D * (F32 ? 4 : 2);          // eight rotated query rows of a warp on their way into registers
+    static constexpr bool INFO = !F32 || D == 64;        // there is room for the sequences' rows and lengths
+    static constexpr int PLAN_AT = 768, INFO_AT = PLAN_AT + PC_MAX_SEQS * 8, RING_AT = (INFO_AT + (INFO ? PC_MAX_SEQS * 12 : 0) + 1023) / 1024 * 1024, Q_AT = RING_AT + WARPS * STAGES * STAGE;
+    static constexpr int SMEM = Q_AT + WARPS * Q_BYTES + 1024;
+    static_assert(SMEM <= 232448 && MAX_ROWS * D * 4 <= STAGES * STAGE, "shared memory; an item's output is staged in the ring");
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
@@ -60,6 +63,8 @@ __device__ __forceinline__ float2 lds64(uint32_t a) {
     asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(a) : "memory");
     return x;
 }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -97,7 +102,7 @@ struct FewParams {
     int n_q_heads, n_kv, group;
     int shared;              // the prefix is attended apart from the sequences' own tokens, and k_paged_join adds the two up
     int prefix_here;         // ... in this kernel
-    int block_own, block_prefix;       // packed rows of a block
+    int block;               // packed rows of a block
     int workers, least;      // warps of the grid; fewest steps of one
     float scale;
     void *out;
@@ -107,78 +112,90 @@ struct FewParams {
     float *home_o;           // [2][rows][query heads][D]: items that one warp has done (own, prefix)
     float2 *home_ml;
     size_t home_rows;        // rows x query heads of one of the two
-    long long *plan;         // [sequences + 1] first place of a sequence's items on the line, the line's length
+    long long *plan;         // Line, then the first place of every sequence's items on it
     uint32_t wait_us, extra_tx;
 };
 
 // The line.  Places 0 .. prefix_end - 1 are the prefix items' (block-major), then come the sequences, KV head by KV head.
-struct Line { long long total, prefix_end; int prefix_len, workers; };
+// Where warps are plenty (at least two an item) an item's length on the line is its steps made up to a multiple of `unit`, and a warp takes one unit: part of one item.  Otherwise
+// `unit` is 1 and warps take runs of even length, which go from item to item.
+struct Line { long long total, prefix_end, per; int prefix_len, workers, rest, unit; };
+static_assert(sizeof(Line) <= PAGED_PLAN_HEAD * 8, "the plan's head");
+
+// (kept out of line: the code of a call of a few steps is fetched as it runs, and its length is what such a call waits for)
+__device__ __noinline__ long long divide(long long a, int b) { return ((a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
 __device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
-__device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (rows * group + block - 1) / block; }
-__device__ __forceinline__ int item_len(const FewParams &P, const PagedSeq &S) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(S.len)); }
-__device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block_prefix) : 0; }
-__device__ __forceinline__ Line line_of(const FewParams &P, long long total) {
-    Line L;
-    L.prefix_len = max(1, steps_of(P.B.n_prefix));
-    L.prefix_end = (long long)prefix_blocks(P) * P.n_kv * L.prefix_len;
-    L.total = total;
-    L.workers = (int)min((long long)P.workers, (total + P.least - 1) / P.least);
-    return L;
+__device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (rows * group + block - 1) / block; }      // block: 8 or 16
+__device__ __forceinline__ int made_up(int len, int unit) { return unit == 1 ? len : (len + unit - 1) / unit * unit; }
+__device__ __forceinline__ int item_steps(const FewParams &P, int own) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(own)); }
+__device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block) : 0; }
+// first place of warp w; the warp that has a place
+__device__ __forceinline__ long long cut(const Line &L, int w) { return L.per * w + (L.rest ? (uint32_t)(L.rest * w) / (uint32_t)L.workers : 0u); }
+__device__ __forceinline__ int worker_of(const Line &L, long long place) {
+    if (L.rest == 0) return (int)divide(place, (int)min(L.per, (long long)INT32_MAX));
+    int w = min(L.workers - 1, (int)((double)place * L.workers / (double)L.total));
+    while (w > 0 && cut(L, w) > place) --w;
+    while (w + 1 < L.workers && cut(L, w + 1) <= place) ++w;
+    return w;
 }
-__device__ __forceinline__ long long cut(const Line &L, int w) { return L.total * w / L.workers; }
-__device__ __forceinline__ int worker_of(const Line &L, long long place) { return (int)(((place + 1) * L.workers + L.total - 1) / L.total) - 1; }
 // Blocks of a sequence's rows from both ends in turn: where attention is causal, two neighbours on the line have as much to do as any other two.
 __device__ __forceinline__ int zigzag(int k, int n) { return k & 1 ? n - 1 - k / 2 : k / 2; }
 
 struct Item {
     int r0, n;               // rows of the run, in the batch
     int s;                   // sequence, -1: all of them over the prefix
-    int h, block, rows;      // KV head, block, packed rows of a block
+    int h, block;            // KV head, block
     int len;                 // steps
     int own, before;         // own tokens, those of them before the run
 };
 
 template <int D, bool F32> struct Warp {
-    uint32_t ring, bar;      // its stages and their barriers
+    uint32_t ring, bar, q;   // its stages, their barriers, its place for queries
     int lane, done;          // steps it has taken so far
     bool alive;
 };
 
-// One item's steps j0 .. j1 - 1, in NB blocks of 8 packed rows; what comes out goes to o and ml (whole and not shared: to the output).
-template <int D, bool F32, int NB>
+// One item's steps j0 .. j1 - 1, in NB blocks of 8 packed rows; what comes out goes to the output (direct), or to o and ml, there where the output would have it (whole) or
+// row by row.  CHECK: rows of a block may see different keys.
+template <int D, bool F32, int NB, bool CHECK>
 __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev &rope, const CUtensorMap *map_k, const CUtensorMap *map_v, Warp<D, F32> &W, volatile int *abort_flag,
-                                          const Item &I, int j0, int j1, bool direct, float *o, float2 *ml, size_t row_pitch) {
+                                          const Item &I, int j0, int j1, bool direct, float *o, float2 *ml, bool whole) {
     using F = Form<D, F32>;
-    constexpr int PARTS = F::PARTS, KK = F::KK, CB = F::CB;
+    constexpr int PARTS = F::PARTS, KK = F::KK, CB = F::CB, ROWS = 8 * NB;
     const int lane = W.lane, quad = lane & 3, eighth = lane >> 2;
     const int prefix = I.s < 0 || !P.shared ? P.B.n_prefix : 0, prefix_steps = steps_of(prefix);
-    const int packed = I.n * P.group, p0 = I.block * I.rows;
-    // own tokens that a column's row sees, and the most and fewest of a row of the block
+    const int packed = I.n * P.group, p0 = I.block * ROWS, n_rows = min(ROWS, packed - p0);
+    // own tokens that a packed row sees, and the most and fewest of a row of the block
     const auto sees = [&](int p) { return P.B.causal ? I.before + p / P.group + 1 : I.own; };
-    const int most = I.s < 0 ? 0 : min(I.own, sees(min(packed, p0 + I.rows) - 1));
-    const int fewest = I.s < 0 ? 0 : max(0, sees(p0));
+    const int most = I.s < 0 ? 0 : min(I.own, sees(p0 + n_rows - 1));
+    const int fewest = I.s < 0 ? 0 : (CHECK ? max(0, sees(p0)) : most);
     int lim[NB][2];
+    if constexpr (CHECK) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) lim[nb][e] = I.s < 0 ? 0 : sees(min(p0 + nb * 8 + quad * 2 + e, packed - 1));
+            for (int e = 0; e < 2; ++e) lim[nb][e] = I.s < 0 ? 0 : sees(min(p0 + nb * 8 + quad * 2 + e, packed - 1));
+    }
     j1 = min(j1, prefix_steps + steps_of(max(0, most)));
 
+    // positions of the block's rows, one a lane: asked for first, as the table entries wait for them
+    int4 pos_of = make_int4(0, 0, 0, 0);
+    if (lane < n_rows) pos_of = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + I.r0 + (p0 + lane) / P.group);
     // pages of 32 steps, one a lane
     const int32_t *own_table = P.B.table + (size_t)max(I.s, 0) * P.B.max_pages;
-    int page = 0, pages_from = j0;
-    const auto look_up = [&](int from) {
-        pages_from = from;
-        const int j = from + lane;
-        if (j < j1) {
-            const bool in_prefix = j < prefix_steps;
-            const int t = (in_prefix ? j : j - prefix_steps) * STEP;
-            page = (paged_page(P.B, (in_prefix ? P.B.prefix : own_table) + (t >> P.B.page_shift)) << P.B.page_shift) + (t & ((1 << P.B.page_shift) - 1));
+    int page = 0, pages_from = j0 - 32;
+    int at = W.done;                                       // steps fetched, of all that this warp fetches
+    const auto fetch = [&](int j) {
+        if (j >= pages_from + 32) {
+            pages_from = j;
+            const int jj = j + lane;
+            if (jj < j1) {
+                const bool in_prefix = jj < prefix_steps;
+                const int t = (in_prefix ? jj : jj - prefix_steps) * STEP;
+                page = (paged_page(P.B, (in_prefix ? P.B.prefix : own_table) + (t >> P.B.page_shift)) << P.B.page_shift) + (t & ((1 << P.B.page_shift) - 1));
+            }
         }
-    };
-    const auto fetch = [&](int j, int at) {                // step j, the at-th of this warp
-        if (j >= pages_from + 32) look_up(j);
         const int y = __shfl_sync(0xffffffffu, page, j - pages_from);
         if (lane == 0) {
             const int stage = at % F::STAGES;
@@ -190,48 +207,76 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
                 pc_tc::tma_load_2d(to + (F::BOXES + i) * BOX_BYTES, map_v, I.h * D + i * F::CH, y, b);
             }
         }
+        ++at;
     };
-    look_up(j0);
-    const int base = W.done - j0;                          // step j is this warp's (base + j)-th
 #pragma unroll 1
-    for (int j = j0; j < min(j1, j0 + F::STAGES); ++j) fetch(j, base + j);
+    for (int j = j0; j < min(j1, j0 + F::STAGES); ++j) fetch(j);
 
-    // Queries, rotated and scaled, as the instructions want them: a lane's channels are whole rotary pairs.  One rounding to bf16 where the context is bf16 (half a
-    // unit of 2^-8, as the keys have it), three parts where it is fp32.
+    // Queries, rotated and scaled, eight rows at a time through shared memory into the form that the instructions want.  One rounding to bf16 where the context is bf16 (half a
+    // step of eight bits, as the keys have it), three parts where it is fp32.
     uint32_t qf[KK][NB][PARTS][2];
+    constexpr int E = D / 32;                              // channels of a lane, whole rotary pairs
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int p = p0 + nb * 8 + eighth;
-        const bool there = p < packed;
-        const int i = there ? p / P.group : 0, g = there ? p - i * P.group : 0;
-        const size_t row = (size_t)(I.r0 + i);
-        const size_t at = (row * P.n_q_heads + I.h * P.group + g) * D;
-        const int4 pos = there ? __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + row) : make_int4(0, 0, 0, 0);
-        bool bad = false;
-        float2 x[KK][2];
+        __syncwarp();
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
+        for (int r = 0; r < 8; ++r) {
+            const int p = p0 + nb * 8 + r;
+            const int px = __shfl_sync(0xffffffffu, pos_of.x, nb * 8 + r), py = __shfl_sync(0xffffffffu, pos_of.y, nb * 8 + r), pz = __shfl_sync(0xffffffffu, pos_of.z, nb * 8 + r);
+            const bool there = p < packed;
+            const int i = there ? p / P.group : 0, g = there ? p - i * P.group : 0;
+            const size_t row = (size_t)(I.r0 + i), from = (row * P.n_q_heads + I.h * P.group + g) * D + lane * E;
+            float x[E];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int c = kk * 16 + u * 8 + quad * 2;
-                if constexpr (F32) {
-                    x[kk][u] = there ? __ldcg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + at + c)) : make_float2(0.f, 0.f);
-                } else {
-                    const uint32_t w = there ? __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + at + c)) : 0u;
-                    x[kk][u] = make_float2(pc_bf16_lo(w), pc_bf16_hi(w));
+            for (int e = 0; e < E; ++e) x[e] = 0.f;
+            if (there) {
+                bool bad = false;
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    float2 y;
+                    if constexpr (F32) y = __ldcg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + from + e));
+                    else {
+                        const uint32_t w = __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + from + e));
+                        y = make_float2(pc_bf16_lo(w), pc_bf16_hi(w));
+                    }
+                    y = pc_rotate(y.x, y.y, pc_rope_cs_clamped(rope, (lane * E + e) / 2, px, py, pz, bad));
+                    x[e] = __fmul_rn(y.x, P.scale);
+                    x[e + 1] = __fmul_rn(y.y, P.scale);
                 }
+                if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
             }
+            // row r: D values, 16-byte pieces at their number ^ r
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const float2 y = pc_rotate(x[kk][u].x, x[kk][u].y, pc_rope_cs_clamped(rope, kk * 8 + u * 4 + quad, pos.x, pos.y, pos.z, bad));
-                uint32_t parts[PARTS];
-                split<PARTS>(__fmul_rn(y.x, P.scale), __fmul_rn(y.y, P.scale), parts);
-#pragma unroll
-                for (int i = 0; i < PARTS; ++i) qf[kk][nb][i][u] = parts[i];
+            for (int e = 0; e < E; e += 2) {
+                const int c = lane * E + e;
+                if constexpr (F32) sts64(W.q + r * D * 4 + (((c >> 2) ^ r) << 4) + (c & 3) * 4, __float_as_uint(x[e]), __float_as_uint(x[e + 1]));
+                else sts32(W.q + r * D * 2 + (((c >> 3) ^ r) << 4) + (c & 7) * 2, pc_pack_bf16(x[e], x[e + 1]));
             }
-        if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
+        }
+        __syncwarp();
+        if constexpr (F32) {
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int c = kk * 16 + u * 8 + quad * 2;
+                    const float2 y = lds64(W.q + eighth * D * 4 + (((c >> 2) ^ eighth) << 4) + (c & 3) * 4);
+                    uint32_t parts[PARTS];
+                    split<PARTS>(y.x, y.y, parts);
+#pragma unroll
+                    for (int i = 0; i < PARTS; ++i) qf[kk][nb][i][u] = parts[i];
+                }
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < KK; kk += 2) {
+                uint32_t r4[4];
+                ldsm4(r4, W.q + (lane & 7) * D * 2 + (((kk * 2 + (lane >> 3)) ^ (lane & 7)) << 4));
+                qf[kk][nb][0][0] = r4[0];
+                qf[kk][nb][0][1] = r4[1];
+                qf[kk + 1][nb][0][0] = r4[2];
+                qf[kk + 1][nb][0][1] = r4[3];
+            }
+        }
     }
 
     float acc[CB][NB][4], m[NB][2], l[NB][2];
@@ -249,9 +294,9 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
 
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
-        const int at = base + j, stage = at % F::STAGES;
+        const int now = W.done, stage = now % F::STAGES;
         const uint32_t ks = W.ring + stage * F::STAGE, vs = ks + F::BOXES * BOX_BYTES;
-        W.alive = __all_sync(0xffffffffu, pc_mbar_wait(W.bar + 8 * stage, (at / F::STAGES) & 1, abort_flag, P.B.status, PC_WHERE_PAGED_WAIT, P.wait_us));
+        W.alive = __all_sync(0xffffffffu, pc_mbar_wait(W.bar + 8 * stage, (now / F::STAGES) & 1, abort_flag, P.B.status, PC_WHERE_PAGED_WAIT, P.wait_us));
         if (!W.alive) return;
 
         // ---- scores of 16 keys (rows: eighth, eighth + 8) by 8 NB packed rows (columns: 2 quad, 2 quad + 1)
@@ -288,7 +333,7 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int nv = in_prefix ? nv_most : min(nv_most, lim[nb][e] - key0);
+                    const int nv = in_prefix || !CHECK ? nv_most : min(nv_most, lim[nb][e] - key0);
                     if (eighth >= nv) sc[nb][e] = -INFINITY;
                     if (eighth + 8 >= nv) sc[nb][2 + e] = -INFINITY;
                 }
@@ -341,7 +386,7 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
         // or NaN value would reach all of them (0 times it is NaN): it is taken out of the product and added to those that see it.  (fp32's parts cannot hold one, so there always.)
         const uint32_t keep0 = (quad * 2 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 1 < nv_most ? 0xFFFF0000u : 0u);
         const uint32_t keep1 = (quad * 2 + 8 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 9 < nv_most ? 0xFFFF0000u : 0u);
-        const bool check = F32 || nv_fewest < nv_most;
+        const bool check = F32 || (CHECK && nv_fewest < nv_most);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             uint32_t a[PARTS][4];
@@ -399,82 +444,81 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
                         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
-                                if (in_prefix || key < lim[nb][e] - key0) acc[cb][nb][2 * u + e] += v;
+                                if (!CHECK || in_prefix || key < lim[nb][e] - key0) acc[cb][nb][2 * u + e] += v;
                     }
             }
         }
         __syncwarp();
-        if (j + F::STAGES < j1) fetch(j + F::STAGES, at + F::STAGES);
+        ++W.done;
+        if (j + F::STAGES < j1) fetch(j + F::STAGES);
     }
-    W.done += max(0, j1 - j0);
 
-    // ---- out
+    // ---- out, by way of the ring (nothing is in flight): row p0 + r at r D floats, channel c at c ^ 8 (r / 2 % 4)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) l[nb][e] += __shfl_xor_sync(0xffffffffu, l[nb][e], w);
+            const uint32_t row = W.ring + (nb * 8 + quad * 2 + e) * D * 4;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        float inv[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) inv[e] = !direct ? 1.f : (l[nb][e] > 0.f ? 1.f / l[nb][e] : (l[nb][e] != l[nb][e] ? l[nb][e] : 0.f));       // nothing seen: 0
-        const auto place = [&](int p) {                    // where a packed row goes, in rows of D
-            if (!row_pitch) return (size_t)(p - p0);
-            const int i = p / P.group;
-            return (size_t)(I.r0 + i) * P.n_q_heads + I.h * P.group + (p - i * P.group);
-        };
-        if (!F32 && direct) {
-            const int p = p0 + nb * 8 + eighth;
-            __nv_bfloat16 *row = static_cast<__nv_bfloat16 *>(P.out) + place(min(p, packed - 1)) * D + quad * 2;
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t w = transpose8(pc_pack_bf16(acc[cb][nb][2 * u] * inv[0], acc[cb][nb][2 * u + 1] * inv[1]));
-                    if (p < packed) *reinterpret_cast<uint32_t *>(row + cb * 16 + u * 8) = w;
-                }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int p = p0 + nb * 8 + quad * 2 + e;
-                if (p >= packed) continue;
-                float *row = (direct ? static_cast<float *>(P.out) : o) + place(p) * D + eighth;
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    row[cb * 16] = acc[cb][nb][e] * inv[e];
-                    row[cb * 16 + 8] = acc[cb][nb][2 + e] * inv[e];
-                }
+            for (int cb = 0; cb < CB; ++cb) {
+                sts32(row + ((cb * 16 + eighth) ^ (quad * 8)) * 4, __float_as_uint(acc[cb][nb][e]));
+                sts32(row + ((cb * 16 + 8 + eighth) ^ (quad * 8)) * 4, __float_as_uint(acc[cb][nb][2 + e]));
             }
+            if (eighth == 0) sts64(W.q + (nb * 8 + quad * 2 + e) * 8, __float_as_uint(m[nb][e]), __float_as_uint(l[nb][e]));
         }
-        if (eighth == 0) {
+    __syncwarp();
+#pragma unroll 1
+    for (int r = 0; r < n_rows; ++r) {
+        const float2 y = lds64(W.q + r * 8);
+        const float mr = y.x, lr = y.y;
+        const int p = p0 + r, i = p / P.group;
+        const size_t to = direct || whole ? (size_t)(I.r0 + i) * P.n_q_heads + I.h * P.group + (p - i * P.group) : (size_t)r;
+        const float inv = !direct ? 1.f : (lr > 0.f ? 1.f / lr : (lr != lr ? lr : 0.f));       // nothing seen: 0
+        const uint32_t from = W.ring + r * D * 4 + (((lane * E) ^ (((r >> 1) & 3) * 8)) * 4);
+        float x[E];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int p = p0 + nb * 8 + quad * 2 + e;
-                if (p >= packed) continue;
-                if (!direct) ml[place(p)] = make_float2(m[nb][e], l[nb][e]);
-                else if (P.lse) P.lse[place(p)] = (m[nb][e] + log2f(l[nb][e])) * 0.6931471805599453f;
-            }
+        for (int e = 0; e < E; e += 2) {
+            const float2 y = lds64(from + e * 4);
+            x[e] = y.x * inv;
+            x[e + 1] = y.y * inv;
+        }
+        float *row = (F32 && direct ? static_cast<float *>(P.out) : o) + to * D + lane * E;
+        if (!F32 && direct) {
+            __nv_bfloat16 *b = static_cast<__nv_bfloat16 *>(P.out) + to * D + lane * E;
+            if constexpr (E == 4) *reinterpret_cast<uint2 *>(b) = make_uint2(pc_pack_bf16(x[0], x[1]), pc_pack_bf16(x[2], x[3]));
+            else *reinterpret_cast<uint32_t *>(b) = pc_pack_bf16(x[0], x[1]);
+        } else {
+            if constexpr (E == 4) *reinterpret_cast<float4 *>(row) = make_float4(x[0], x[1], x[2], x[3]);
+            else *reinterpret_cast<float2 *>(row) = make_float2(x[0], x[1]);
+        }
+        if (lane == 0) {
+            if (!direct) ml[to] = make_float2(mr, lr);
+            else if (P.lse) P.lse[to] = (mr + log2f(lr)) * 0.6931471805599453f;
         }
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the ring is the copies' again
+    __syncwarp();
 }
 
-template <int D, bool F32>
+template <int D, bool F32, int NB, bool CHECK>
 __global__ void __launch_bounds__(Form<D, F32>::WARPS * 32, 1)
-k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FewParams P, const pc_rope_dev rope) {
+k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FewParams P, const __grid_constant__ pc_rope_dev rope) {
     using F = Form<D, F32>;
     pc_grid_dep_launch();
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - pc_smem_u32(smem_raw));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 512);
-    long long *sums = reinterpret_cast<long long *>(gen + 640), *plan = reinterpret_cast<long long *>(gen + F::PLAN_AT);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 256);
+    long long *sums = reinterpret_cast<long long *>(gen + 512), *plan = reinterpret_cast<long long *>(gen + F::PLAN_AT);
+    int *info = reinterpret_cast<int *>(gen + F::INFO_AT);             // rows' start, rows, length of every sequence
     const int warp = threadIdx.x >> 5;
     Warp<D, F32> W;
     W.lane = threadIdx.x & 31;
     W.bar = base + warp * F::STAGES * 8;
     W.ring = base + F::RING_AT + warp * F::STAGES * F::STAGE;
+    W.q = base + F::Q_AT + warp * F::Q_BYTES;
     W.done = 0;
     W.alive = true;
     if (threadIdx.x == 0) *abort_flag = 0;
@@ -485,63 +529,94 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
     pc_grid_dep_wait();
 
-    // ---- the line
+    // ---- the line: steps and items of the whole call, the unit that follows from them, then the sequences' places
     constexpr int THREADS = F::WARPS * 32;
-    const int pblocks = prefix_blocks(P);
-    const long long prefix_end = (long long)pblocks * P.n_kv * max(1, steps_of(P.B.n_prefix));
-    long long at = prefix_end;
-    for (int s0 = 0; s0 < P.B.n_seqs; s0 += THREADS) {
-        const int s = s0 + threadIdx.x;
-        long long v = 0;
-        if (s < P.B.n_seqs) {
+    const auto seq_of = [&](int s) {
+        if constexpr (F::INFO) return PagedSeq{info[3 * s], info[3 * s + 1], info[3 * s + 2]};
+        else return paged_seq(P.B, s);
+    };
+    Line L;
+    {
+        const int pitems = prefix_blocks(P) * P.n_kv, psteps = max(1, steps_of(P.B.n_prefix));
+        long long steps = 0, items = 0;
+#pragma unroll 1
+        for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) {
             const PagedSeq S = paged_seq(P.B, s);
-            v = (long long)blocks_of(S.n, P.group, P.block_own) * P.n_kv * item_len(P, S);
+            const int n = blocks_of(S.n, P.group, 8 * NB) * P.n_kv;
+            items += n;
+            steps += (long long)n * item_steps(P, S.len);
+            if constexpr (F::INFO) {
+                info[3 * s] = S.r0;
+                info[3 * s + 1] = S.n;
+                info[3 * s + 2] = S.len;
+            }
         }
-        const long long end = paged_scan<THREADS>(v, sums);
-        if (s < P.B.n_seqs) plan[s] = at + end - v;
-        at += sums[F::WARPS - 1];
+        paged_scan<THREADS>(steps, sums);
+        steps = sums[F::WARPS - 1] + (long long)pitems * psteps;
         __syncthreads();
+        paged_scan<THREADS>(items, sums);
+        items = sums[F::WARPS - 1] + pitems;
+        __syncthreads();
+        const int spare = items * 2 <= P.workers ? P.workers - (int)items : 0;
+        L.unit = spare ? max(P.least, (int)divide(steps + spare - 1, spare)) : 1;
+        L.prefix_len = made_up(psteps, L.unit);
+        L.prefix_end = (long long)pitems * L.prefix_len;
+        long long at = L.prefix_end;
+#pragma unroll 1
+        for (int s0 = 0; s0 < P.B.n_seqs; s0 += THREADS) {
+            const int s = s0 + threadIdx.x;
+            long long v = 0;
+            if (s < P.B.n_seqs) {
+                const PagedSeq S = seq_of(s);
+                v = (long long)blocks_of(S.n, P.group, 8 * NB) * P.n_kv * made_up(item_steps(P, S.len), L.unit);
+            }
+            const long long end = paged_scan<THREADS>(v, sums);
+            if (s < P.B.n_seqs) plan[s] = at + end - v;
+            at += sums[F::WARPS - 1];
+            __syncthreads();
+        }
+        L.total = at;
+        L.workers = spare ? (int)divide(at, L.unit) : (int)min((long long)P.workers, divide(at + P.least - 1, P.least));
+        L.per = divide(at, max(1, L.workers));
+        L.rest = (int)(at - L.per * L.workers);
     }
-    if (threadIdx.x == 0) plan[P.B.n_seqs] = at;
     __syncthreads();
-    if (P.plan && blockIdx.x == 0)
-        for (int s = threadIdx.x; s <= P.B.n_seqs; s += THREADS) P.plan[s] = plan[s];
-    const Line L = line_of(P, at);
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) *reinterpret_cast<Line *>(P.plan) = L;
+        for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) P.plan[PAGED_PLAN_HEAD + s] = plan[s];
+    }
 
     // ---- this warp's part of it; neighbours on the line are on different SMs
     const int w = warp * gridDim.x + blockIdx.x;
-    if (at == 0 || w >= L.workers) return;
+    if (w >= L.workers) return;
     long long g = cut(L, w);
     const long long g1 = cut(L, w + 1);
+#pragma unroll 1
     while (g < g1 && W.alive) {
         Item I;
         int off;
         if (g < L.prefix_end) {
-            const int item = (int)(g / L.prefix_len);
+            const int item = (int)divide(g, L.prefix_len);
             off = (int)(g - (long long)item * L.prefix_len);
-            I = {0, paged_rows(P.B), -1, item % P.n_kv, item / P.n_kv, P.block_prefix, L.prefix_len, 0, 0};
+            I = {0, paged_rows(P.B), -1, item % P.n_kv, item / P.n_kv, L.prefix_len, 0, 0};
         } else {
             int lo = 0, hi = P.B.n_seqs - 1;               // the last sequence that begins at or before g (one without rows has no places)
+#pragma unroll 1
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (plan[mid] <= g) lo = mid; else hi = mid - 1;
             }
-            const PagedSeq S = paged_seq(P.B, lo);
-            const int len = item_len(P, S), blocks = blocks_of(S.n, P.group, P.block_own);
-            const long long y = g - plan[lo], item = y / len;
+            const PagedSeq S = seq_of(lo);
+            const int len = made_up(item_steps(P, S.len), L.unit), blocks = blocks_of(S.n, P.group, 8 * NB);
+            const long long y = g - plan[lo], item = divide(y, len), h = divide(item, blocks);
             off = (int)(y - item * len);
-            I = {S.r0, S.n, lo, (int)(item / blocks), zigzag((int)(item % blocks), blocks), P.block_own, len, S.len, S.len - S.n};
+            I = {S.r0, S.n, lo, (int)h, zigzag((int)(item - h * blocks), blocks), len, S.len, S.len - S.n};
         }
         const int take = (int)min((long long)(I.len - off), g1 - g);
-        const bool whole = off == 0 && take == I.len, direct = whole && !P.shared;
-        float *o = P.part_o + (size_t)(2 * w + (off == 0)) * MAX_ROWS * D;
-        float2 *ml = P.part_ml + (size_t)(2 * w + (off == 0)) * MAX_ROWS;
-        if (whole && P.shared) {
-            o = P.home_o + (I.s < 0 ? P.home_rows * D : 0);
-            ml = P.home_ml + (I.s < 0 ? P.home_rows : 0);
-        }
-        if (I.rows == 8) take_unit<D, F32, 1>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, direct, o, ml, whole);
-        else take_unit<D, F32, 2>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, direct, o, ml, whole);
+        const bool whole = off == 0 && take == I.len, home = whole && P.shared;
+        float *o = home ? P.home_o + (I.s < 0 ? P.home_rows * D : 0) : P.part_o + (size_t)(2 * w + (off == 0)) * MAX_ROWS * D;
+        float2 *ml = home ? P.home_ml + (I.s < 0 ? P.home_rows : 0) : P.part_ml + (size_t)(2 * w + (off == 0)) * MAX_ROWS;
+        take_unit<D, F32, NB, CHECK>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, whole && !P.shared, o, ml, whole);
         g += take;
     }
     if (!W.alive) pc_let_copies_land();
@@ -566,13 +641,21 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     pc_grid_dep_launch();
     const int s = blockIdx.x % P.B.n_seqs, k = blockIdx.x / P.B.n_seqs, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pc_grid_dep_wait();
+    Line L;
+    {
+        longlong2 x[4];
+        static_assert(sizeof(Line) == 40 && PAGED_PLAN_HEAD * 8 == sizeof(x), "the line, as it lies in memory");
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] = __ldcg(reinterpret_cast<const longlong2 *>(P.plan) + i);
+        L = {x[0].x, x[0].y, x[1].x, (int)x[1].y, (int)(x[1].y >> 32), (int)x[2].x, (int)(x[2].x >> 32)};
+    }
+    const long long place = __ldcg(P.plan + PAGED_PLAN_HEAD + s);
     const PagedSeq S = paged_seq(P.B, s);
-    const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block_own);
+    const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block);
     if (k >= blocks) return;
-    const int block = zigzag(k, blocks), p0 = block * P.block_own, n = min(P.block_own, packed - p0);
-    const Line L = line_of(P, __ldcg(P.plan + P.B.n_seqs));
-    const int len = item_len(P, S);
-    const long long first = __ldcg(P.plan + s) + ((long long)h * blocks + k) * len;
+    const int block = zigzag(k, blocks), p0 = block * P.block, n = min(P.block, packed - p0);
+    const int len = made_up(item_steps(P, S.len), L.unit);
+    const long long first = place + ((long long)h * blocks + k) * len;
     const int w0 = worker_of(L, first), w1 = worker_of(L, first + len - 1);
     if (!P.shared && w0 == w1) return;                     // its warp has written the output
     const int sets = JOIN_WARPS / n, r = warp % n, set = warp / n;
@@ -580,42 +663,40 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     if (set < sets) {
         const int p = p0 + r, i = p / P.group;
         const size_t home = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
-        const auto add = [&](const float *po, float2 y, size_t pitch) {
+        // Parts, own ones first: of this kernel's warps, each its last item for the first one and its first for the others; or of one warp at home; or the tcgen05 kernel's
+        struct From { const float *o; const float2 *ml; int parts; size_t pitch, later; } own{}, pre{};
+        const auto from = [&](int v0, int v1, int row, size_t home_at) {
+            if (v0 == v1) return From{P.home_o + home_at * D, P.home_ml + home_at, 1, 0, 0};
+            const size_t slot = (size_t)(2 * v0 + 1) * MAX_ROWS + row;
+            return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * MAX_ROWS, MAX_ROWS};
+        };
+        own = from(w0, w1, r, home);
+        if (P.shared && P.B.n_prefix > 0) {
+            const long long row = (long long)S.r0 * P.group + p;          // packed row of the batch
+            if (P.prefix_here) {
+                const long long item = row / P.block * P.n_kv + h;
+                pre = from(worker_of(L, item * L.prefix_len), worker_of(L, (item + 1) * L.prefix_len - 1), (int)(row % P.block), P.home_rows + home);
+            } else {
+                const PagedTcRow T = paged_tc_row(J.T, h, row);
+                const size_t slot = T.first * PAGED_TC_TILE + T.row;
+                pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, T.parts, PAGED_TC_TILE, 0};
+            }
+        }
+#pragma unroll 4
+        for (int c = set; c < own.parts + pre.parts; c += sets) {
+            const bool is_own = c < own.parts;
+            const int u = is_own ? c : c - own.parts;
+            const size_t at = (is_own ? own.pitch : pre.pitch) * u - (u ? (is_own ? own.later : pre.later) : 0);
+            const float *po = (is_own ? own.o : pre.o) + at * D + lane;
+            const float2 y = __ldcg((is_own ? own.ml : pre.ml) + at);
             float x[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = __ldcg(po + e * pitch);
+            for (int e = 0; e < E; ++e) x[e] = __ldcg(po + e * 32);
             const float m = fmaxf(M, y.x), f = m == -INFINITY ? 1.f : exp2_fast(M - m), g = m == -INFINITY ? 1.f : exp2_fast(y.x - m);
             M = m;
             l = l * f + y.y * g;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * g;
-        };
-        // own parts: worker w0's last item, the others' first
-        const int own = w1 - w0 + 1;
-#pragma unroll 4
-        for (int c = set; c < own; c += sets) {
-            const size_t slot = own == 1 ? 0 : (size_t)(2 * (w0 + c) + (c == 0)) * MAX_ROWS + r;
-            const float *po = own == 1 ? P.home_o + home * D : P.part_o + slot * D;
-            add(po + lane, own == 1 ? __ldcg(P.home_ml + home) : __ldcg(P.part_ml + slot), 32);
-        }
-        if (P.shared) {
-            const long long row = (long long)S.r0 * P.group + p;          // packed row of the batch
-            if (P.prefix_here) {
-                const long long item = row / P.block_prefix * P.n_kv + h;
-                const int v0 = worker_of(L, item * L.prefix_len), v1 = worker_of(L, (item + 1) * L.prefix_len - 1), parts = v1 - v0 + 1;
-                const int rr = (int)(row % P.block_prefix);
-#pragma unroll 4
-                for (int c = set; c < parts; c += sets) {
-                    const size_t slot = parts == 1 ? 0 : (size_t)(2 * (v0 + c) + (c == 0)) * MAX_ROWS + rr;
-                    const float *po = parts == 1 ? P.home_o + (P.home_rows + home) * D : P.part_o + slot * D;
-                    add(po + lane, parts == 1 ? __ldcg(P.home_ml + P.home_rows + home) : __ldcg(P.part_ml + slot), 32);
-                }
-            } else if (P.B.n_prefix > 0) {
-                const PagedTcRow T = paged_tc_row(J.T, h, row);
-#pragma unroll 4
-                for (int c = set; c < T.parts; c += sets)
-                    add(J.T.part_o + ((T.first + c) * PAGED_TC_TILE + T.row) * D + lane, __ldcg(J.T.part_ml + (T.first + c) * PAGED_TC_TILE + T.row), 32);
-            }
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) so[warp][e * 32 + lane] = o[e];
@@ -646,19 +727,25 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     if (P.lse && lane == 0) P.lse[to] = (M + log2f(l)) * 0.6931471805599453f;
 }
 
-template <int D, bool F32> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, int max_blocks, cudaStream_t stream) {
+template <int D, bool F32, int NB, bool CHECK> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, cudaStream_t stream) {
     using F = Form<D, F32>;
     static bool attr_set[PC_MAX_DEVICES] = {};
     if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
     if (!attr_set[ctx->device]) {
-        PC_CUDA_TRY(cudaFuncSetAttribute(k_paged_few<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM));
+        PC_CUDA_TRY(cudaFuncSetAttribute(k_paged_few<D, F32, NB, CHECK>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM));
         attr_set[ctx->device] = true;
     }
     JoinParams j = J;
     j.F.workers = ctx->sm_count * F::WARPS;
-    PC_LAUNCH((k_paged_few<D, F32>), dim3(ctx->sm_count), dim3(F::WARPS * 32), F::SMEM, stream, mk, mv, j.F, ctx->rope);
-    PC_LAUNCH((k_paged_join<D, F32>), dim3((unsigned)(J.F.B.n_seqs * max_blocks), J.F.n_kv), dim3(JOIN_WARPS * 32), 0, stream, j);
+    const long long blocks = ((long long)j.F.B.max_rows * j.F.group + 8 * NB - 1) / (8 * NB);
+    PC_LAUNCH((k_paged_few<D, F32, NB, CHECK>), dim3(ctx->sm_count), dim3(F::WARPS * 32), F::SMEM, stream, mk, mv, j.F, ctx->rope);
+    PC_LAUNCH((k_paged_join<D, F32>), dim3((unsigned)(j.F.B.n_seqs * blocks), j.F.n_kv), dim3(JOIN_WARPS * 32), 0, stream, j);
     return PC_OK;
+}
+template <int D, bool F32> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, cudaStream_t stream) {
+    const bool check = J.F.B.causal && J.F.B.max_rows > 1;        // rows of a sequence see different keys
+    if (J.F.block == 8) return check ? launch<D, F32, 1, true>(mk, mv, J, ctx, stream) : launch<D, F32, 1, false>(mk, mv, J, ctx, stream);
+    return check ? launch<D, F32, 2, true>(mk, mv, J, ctx, stream) : launch<D, F32, 2, false>(mk, mv, J, ctx, stream);
 }
 
 }  // namespace
@@ -695,9 +782,8 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.group = ctx->group;
     P.shared = shared;
     P.prefix_here = shared && !tc && A.batch.n_prefix > 0;
-    P.block_own = A.batch.max_rows * ctx->group <= 8 ? 8 : MAX_ROWS;
-    P.block_prefix = (long long)A.batch.n_rows * ctx->group <= 8 ? 8 : MAX_ROWS;
-    P.least = 2;
+    P.block = (long long)(P.prefix_here ? A.batch.n_rows : A.batch.max_rows) * ctx->group <= 8 ? 8 : MAX_ROWS;
+    P.least = 4;
     P.scale = pc_q_rot_scale(D.head_dim);
     P.out = A.out;
     P.lse = A.lse;
@@ -710,8 +796,7 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
     if (tc) J.T = *tc;
-    const int max_blocks = (int)(((long long)A.batch.max_rows * ctx->group + P.block_own - 1) / P.block_own);
     const bool f32 = D.dtype == PC_F32;
-    if (D.head_dim == 128) return f32 ? launch<128, true>(mk, mv, J, ctx, max_blocks, stream) : launch<128, false>(mk, mv, J, ctx, max_blocks, stream);
-    return f32 ? launch<64, true>(mk, mv, J, ctx, max_blocks, stream) : launch<64, false>(mk, mv, J, ctx, max_blocks, stream);
+    if (D.head_dim == 128) return f32 ? launch<128, true>(mk, mv, J, ctx, stream) : launch<128, false>(mk, mv, J, ctx, stream);
+    return f32 ? launch<64, true>(mk, mv, J, ctx, stream) : launch<64, false>(mk, mv, J, ctx, stream);
 }

@@ -4,6 +4,7 @@
 
 constexpr int PAGED_FEW_ROWS = 16;           // most packed rows of a block of the few-row kernel
 constexpr int PAGED_HOME_ROWS = 1024;        // most rows of a call whose prefix is attended apart
+constexpr int PAGED_PLAN_HEAD = 8;         // words of the few-row kernel's plan ahead of the sequences' places
 constexpr int PAGED_TC_TILE = 128;           // packed rows of a tile of the tcgen05 kernel
 
 struct pc_paged {
