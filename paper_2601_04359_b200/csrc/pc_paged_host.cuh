@@ -13,6 +13,11 @@ struct pc_paged {
     float2 *few_ml, *home_ml;
     size_t home_rows;
     long long *plan;
+    // bf16: rotated queries, units, parts and their counters of the tcgen05 kernel
+    void *q_rot;
+    int *tc_plan, *tc_tickets;
+    float *tc_o;
+    float2 *tc_ml;
 };
 
 struct pc_paged_args {
@@ -40,3 +45,8 @@ __device__ __forceinline__ PagedTcRow paged_tc_row(const PagedTcParts &T, int h,
 size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kernel's scratch
 // shared: the prefix is attended apart from the sequences' own tokens, here or (tc given) by the tcgen05 kernel before
 pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream);
+bool pc_paged_tc_shape(const pc_ctx *ctx);           // whether the tcgen05 kernel takes the context's type
+size_t pc_paged_tc_slots(const pc_ctx *ctx), pc_paged_tc_plan_bytes(const pc_ctx *ctx);
+int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B);
+// prefix_parts 0: every sequence over prefix and own tokens, into the output; otherwise the shared prefix alone, in so many parts, into scratch (left)
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream);

@@ -1,0 +1,739 @@
+// Attention over a paged cache on tcgen05 tensor cores (bf16): prompts, their pieces and frames, and a prefix that many rows share.
+//
+// Two launches.
+//   k_paged_front  rotates the queries, with log2(e) / sqrt(d) folded in, into rows of KV head x (token, head of the group): the rows that share keys and values lie side by side,
+//                  so a tile of 128 rows is full whatever the group's size, and a causal tile of G heads spans 128 / G tokens only.  Its first CTA plans the call from
+//                  the lengths on the device: units (sequence, pair of query tiles, run of key tiles), longest first.
+//   k_paged_tc     persistent CTAs take units in snake order (CTA c the c-th, the c-th from the end of the next round, ...): with the longest first that leaves them within
+//                  about a unit of each other.  Pairs with more key tiles than an even share are cut into parts; the last of a pair's CTAs adds the parts up, in the order of the keys.
+// A CTA: warp 0 fetches keys and values by TMA, a lane a page's box (a tile of 128 keys is 1 to 8 pages), two stages each; warps 1 and 2 issue S = Q_t K^T of the two query
+// tiles, warp 3 O_t += P_t V; warps 4-7 and 8-11 are the softmax of tile 0 and 1: the score row in registers, running maximum and sum in fp32, probabilities as bf16 into tensor
+// memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame kernel, k_attend_tc.)
+// Rows behind a segment's end: scores are replaced by -infinity whatever they are, and the values' rows are cleared in shared memory, since 0 times what lies
+// there may be NaN.
+#include <algorithm>
+
+#include "pc_paged_host.cuh"
+#include "pc_tc.cuh"
+
+namespace {
+
+using namespace pc_tc;
+
+constexpr int TC_THREADS = 384;
+constexpr int REGS_LAUNCH = 65536 / TC_THREADS / 8 * 8, REGS_ISSUE = 72, REGS_SOFTMAX = 216;
+static_assert(128 * REGS_ISSUE + 256 * REGS_SOFTMAX <= TC_THREADS * REGS_LAUNCH, "more registers than the block has");
+constexpr float GROW = 8.f;
+constexpr int PAIR = 2 * TILE;                     // packed rows of a unit
+constexpr int LEAST_TILES = 4;                     // a part of a pair has as many key tiles at least
+
+// What a unit's roles need to know of it
+struct Unit {
+    int s;                   // sequence; -1: rows of all sequences over the shared prefix
+    int q0;                  // first row of the pair among the rotated queries of a KV head
+    int rows;                // packed rows of the pair
+    int p0;                  // their first, counted from the sequence's first
+    int r0;                  // the sequence's first row in the batch
+    int before, own;         // own tokens before the rows, and in all
+    int j0, nj;              // key tiles: those of the prefix first
+    int part, parts;         // of the pair
+    int slot;                // place of the pair's first part in scratch, in pairs of tiles of one KV head; the KV head and part follow
+};
+static_assert(sizeof(Unit) == 48, "three 16-byte pieces");
+constexpr int PLAN_HEAD = 4;                       // words ahead of the units: their number
+
+template <int D> struct Map {
+    static constexpr int HALVES = D / 64, TILE_B = HALVES * HALF_BYTES;
+    static constexpr int Q = 0, K = Q + 2 * TILE_B, V = K + 2 * TILE_B, BAR = V + 2 * TILE_B, ALLOC = BAR + 256 + 1024;
+};
+enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_KV = 4 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 6 /* [step & 1] */, BAR_SFULL = 8 /* [tile] */,
+       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, N_BARS = 19 };
+constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
+
+struct TcParams {
+    PagedBatch B;
+    int n_q_heads, n_kv, group;
+    int shared;              // the prefix alone, rows of all sequences; parts go to scratch row by row for k_paged_join
+    long long head_rows;     // rows of a KV head among the rotated queries
+    __nv_bfloat16 *out;
+    float *lse;
+    const int4 *units;
+    const int *head;
+    float *part_o;
+    float2 *part_ml;
+    int *tickets;            // [slots][tile][warp] parts that have arrived; zero at first
+    uint32_t wait_us, extra_tx;
+};
+
+__device__ __forceinline__ Unit unit_at(const int4 *units, int i) {
+    const int4 a = __ldcg(units + 3 * i), b = __ldcg(units + 3 * i + 1), c = __ldcg(units + 3 * i + 2);
+    return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w};
+}
+// The k-th unit of a CTA, -1 behind the last
+__device__ __forceinline__ int unit_of(int k, int n) {
+    const long long i = k & 1 ? (long long)(k + 1) * gridDim.x - 1 - blockIdx.x : (long long)k * gridDim.x + blockIdx.x;
+    return i < n ? (int)i : -1;
+}
+__device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
+
+// ------------------------------------------------------------------------------------------------ queries and plan
+constexpr int FRONT_THREADS = 512;
+constexpr int LEVELS = 512;
+
+struct FrontParams {
+    PagedBatch B;
+    const char *q;
+    const int32_t *q_pos;
+    char *q_rot;
+    int chunks, group, n_kv, d;
+    long long head_rows;
+    float scale;
+    int shared, shared_parts, sms, max_units, n_tickets;
+    int4 *units;
+    int *head, *tickets;
+};
+
+__device__ __forceinline__ void put_unit(int4 *units, int i, const Unit &U) {
+    units[3 * i] = make_int4(U.s, U.q0, U.rows, U.p0);
+    units[3 * i + 1] = make_int4(U.r0, U.before, U.own, U.j0);
+    units[3 * i + 2] = make_int4(U.nj, U.part, U.parts, U.slot);
+}
+
+// Key tiles of a pair: up to the last key that one of its rows sees, one at least
+__device__ __forceinline__ int pair_tiles(const FrontParams &P, int n, int len, int pair) {
+    const int last = (min((pair + 1) * PAIR, n * P.group) - 1) / P.group;
+    const int sees = P.B.causal ? min(len, max(0, len - n + last + 1)) : len;
+    return max(1, tiles_of(P.B.n_prefix) + tiles_of(sees));
+}
+
+__device__ void plan(const FrontParams &P) {
+    __shared__ int pair0[PC_MAX_SEQS + 1], seq_r0[PC_MAX_SEQS], seq_n[PC_MAX_SEQS], seq_len[PC_MAX_SEQS], level[LEVELS];
+    __shared__ long long sums[32];
+    __shared__ int counts[2];
+    const int tid = threadIdx.x;
+    static_assert(PC_MAX_SEQS <= FRONT_THREADS && LEVELS == FRONT_THREADS, "a thread a sequence, and a level");
+    if (P.shared) {
+        const int packed = paged_rows(P.B) * P.group, tiles = tiles_of(P.B.n_prefix), parts = P.shared_parts, pairs = (packed + PAIR - 1) / PAIR;
+        for (int i = tid; i < pairs * parts; i += FRONT_THREADS) {
+            const int pair = i / parts, part = i - pair * parts;
+            const int j0 = (int)((long long)tiles * part / parts), j1 = (int)((long long)tiles * (part + 1) / parts);
+            put_unit(P.units, i, Unit{-1, pair * PAIR, min(PAIR, packed - pair * PAIR), pair * PAIR, 0, 0, 0, j0, j1 - j0, part, parts, pair});
+        }
+        if (tid == 0) P.head[0] = pairs * parts;
+        return;
+    }
+    int mine = 0;
+    if (tid < P.B.n_seqs) {
+        const PagedSeq S = paged_seq(P.B, tid);
+        seq_r0[tid] = S.r0;
+        seq_n[tid] = S.n;
+        seq_len[tid] = S.len;
+        mine = (S.n * P.group + PAIR - 1) / PAIR;
+    }
+    level[tid] = 0;
+    for (int i = tid; i < P.n_tickets; i += FRONT_THREADS) P.tickets[i] = 0;
+    if (tid < 2) counts[tid] = 0;
+    const long long end = paged_scan<FRONT_THREADS>((long long)mine, sums);
+    if (tid < P.B.n_seqs) pair0[tid] = (int)end - mine;
+    const int pairs = (int)sums[FRONT_THREADS / 32 - 1];
+    if (tid == 0) pair0[P.B.n_seqs] = pairs;
+    __syncthreads();
+    const auto seq_of = [&](int pair) {
+        int lo = 0, hi = P.B.n_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pair0[mid] <= pair) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    };
+    long long tiles = 0;
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i);
+        tiles += pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]);
+    }
+    paged_scan<FRONT_THREADS>(tiles, sums);
+    tiles = sums[FRONT_THREADS / 32 - 1];
+    // An even share of all key tiles; a pair with more than a quarter above it is cut, into parts that are over 5/9 of a share each: fewer than two an SM, which the scratch holds.
+    const int share = (int)min((long long)INT32_MAX / 2, max((long long)LEAST_TILES, (tiles * P.n_kv + P.sms - 1) / P.sms));
+    const auto parts_of = [&](int t) { return t <= share + share / 4 ? 1 : (t + share - 1) / share; };
+    const auto level_of = [&](int size) { return LEVELS - 1 - min(size, LEVELS - 1); };
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i), t = pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]), parts = parts_of(t);
+        atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
+    }
+    __syncthreads();
+    const int n_level = level[tid];
+    __syncthreads();
+    const long long upto = paged_scan<FRONT_THREADS>((long long)n_level, sums);
+    level[tid] = (int)upto - n_level;
+    if (tid == 0) P.head[0] = min((int)sums[FRONT_THREADS / 32 - 1], P.max_units);
+    __syncthreads();
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i), pair = i - pair0[s], n = seq_n[s], len = seq_len[s], t = pair_tiles(P, n, len, pair);
+        const int parts = parts_of(t);
+        const int at = atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
+        const int slot = parts > 1 ? atomicAdd(&counts[0], parts) : 0;
+        for (int part = 0; part < parts; ++part) {
+            const int j0 = (int)((long long)t * part / parts), j1 = (int)((long long)t * (part + 1) / parts);
+            if (at + part < P.max_units)                      // (row ranges that overlap can make more units than there are rows for)
+                put_unit(P.units, at + part, Unit{s, seq_r0[s] * P.group + pair * PAIR, min(PAIR, n * P.group - pair * PAIR), pair * PAIR, seq_r0[s], len - n, len, j0, j1 - j0, part, parts, slot});
+        }
+    }
+}
+
+__global__ void __launch_bounds__(FRONT_THREADS) k_paged_front(const __grid_constant__ FrontParams P, const __grid_constant__ pc_rope_dev rope) {
+    pc_grid_dep_launch();
+    pc_grid_dep_wait();
+    if (blockIdx.x == 0) {
+        plan(P);
+        return;
+    }
+    // a warp a row of the batch, lane's chunks of eight channels 32 apart: all at one place of a head
+    const int lane = threadIdx.x & 31, row = (int)(((blockIdx.x - 1) * FRONT_THREADS + threadIdx.x) >> 5);
+    if (row >= paged_rows(P.B)) return;
+    const int4 pos = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + row);
+    const char *q = P.q + (size_t)row * P.chunks * 16;
+    constexpr int CPL = 8;
+    float2 cs[4];
+    bool bad = false;
+    for (int c0 = 0; c0 < P.chunks; c0 += CPL * 32) {
+        uint4 v[CPL];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            const int c = c0 + i * 32 + lane;
+            if (c < P.chunks) v[i] = __ldcg(reinterpret_cast<const uint4 *>(q) + c);
+        }
+        if (c0 == 0) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) cs[u] = pc_rope_cs_clamped(rope, ((lane * 8) % P.d) / 2 + u, pos.x, pos.y, pos.z, bad);
+        }
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            const int c = c0 + i * 32 + lane;
+            if (c >= P.chunks) break;
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float2 y = pc_rotate(pc_bf16_lo(w[u]), pc_bf16_hi(w[u]), cs[u]);
+                o[u] = pc_pack_bf16(__fmul_rn(y.x, P.scale), __fmul_rn(y.y, P.scale));
+            }
+            const int head = c * 8 / P.d, h = head / P.group, g = head - h * P.group;
+            const size_t to = ((size_t)h * P.head_rows + (size_t)row * P.group + g) * P.d + c * 8 % P.d;
+            *reinterpret_cast<uint4 *>(P.q_rot + to * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+    if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+__device__ __forceinline__ void arrive_if(bool who, uint32_t bar) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((uint32_t)who) : "memory");
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, uint32_t limit_us) {
+    if (__builtin_expect(__all_sync(0xffffffffu, pc_mbar_try(bar, parity)), 1)) return true;
+    return __all_sync(0xffffffffu, pc_mbar_wait(bar, parity, abort_flag, status, PC_WHERE_PAGED_WAIT, limit_us));
+}
+
+// Keys of tile j of a unit that are there, of 128
+__device__ __forceinline__ int tile_keys(const PagedBatch &B, const Unit &U, int j, int prefix_tiles) {
+    return min(TILE, j < prefix_tiles ? B.n_prefix - j * TILE : max(0, U.own - (j - prefix_tiles) * TILE));
+}
+
+template <int D>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TcParams P) {
+    using M = Map<D>;
+    constexpr uint32_t QK = IDESC_QK, PV = (IDESC_PV & ~(0x3Fu << 17)) | ((D >> 3) << 17);
+    pc_grid_dep_launch();
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + M::BAR + N_BARS * 8);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + M::BAR + N_BARS * 8 + 4);
+    const uint32_t bar0 = base + M::BAR;
+    auto bar = [&](int i) { return bar0 + 8u * i; };
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(BAR_KV + s), 1);
+            mbar_init(bar(BAR_EMPTY + s), 4);
+        }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(bar(BAR_Q + t), 1);
+            mbar_init(bar(BAR_QFREE + t), 4);
+            mbar_init(bar(BAR_SFULL + t), 1);
+            mbar_init(bar(BAR_SFREE + t), 4);
+            mbar_init(bar(BAR_PVDONE + t), 1);
+            mbar_init(bar(BAR_PHALF + 2 * t), 4);
+            mbar_init(bar(BAR_PHALF + 2 * t + 1), 4);
+        }
+        mbar_init(bar(BAR_DONE), 3);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pc_grid_dep_wait();
+
+    const PagedBatch &B = P.B;
+    const int prefix_tiles = tiles_of(B.n_prefix);
+    const int n_units = __ldcg(P.head) * P.n_kv;         // a unit of the list times the KV heads, heads side by side
+    const bool some = unit_of(0, n_units) >= 0;          // this CTA has work
+
+    // Steps are counted through all units (gs), units by un.
+    if (warp == 0) {
+        // ---------------------------------------------------------------- TMA producer: all lanes
+        reg_dealloc<REGS_ISSUE>();
+        // Tiles of keys in the order of the steps.  A lane has a page of the tile: lane 8 half + page of the keys' boxes, 16 + 8 half + page of the values', which are at the same place.
+        struct TileRef { int y, n, h, first, unit; };       // row of the lane's page, keys, KV head, first of its unit
+        Unit U{};
+        int k = -1, j = 0, uh = 0, uidx = 0;
+        const int page_rows = 1 << B.page_shift, pg = lane & 7;
+        const auto next = [&]() -> TileRef {
+            bool first = false;
+            if (k < 0 || j == U.j0 + U.nj) {
+                uidx = unit_of(++k, n_units);
+                if (uidx < 0) {
+                    k = 1 << 29;
+                    j = U.j0 + U.nj;
+                    return {0, -1, 0, 0, 0};
+                }
+                U = unit_at(P.units, uidx / P.n_kv);
+                uh = uidx % P.n_kv;
+                j = U.j0;
+                first = true;
+            }
+            const int n = tile_keys(B, U, j, prefix_tiles);
+            int y = 0;
+            if (pg * page_rows < n) {
+                const int t = (j < prefix_tiles ? j : j - prefix_tiles) * TILE + pg * page_rows;
+                const int32_t *table = j < prefix_tiles ? B.prefix : B.table + (size_t)U.s * B.max_pages;
+                y = paged_page(B, table + (t >> B.page_shift)) << B.page_shift;
+            }
+            ++j;
+            return {y, n, uh, first, uidx};
+        };
+        const int half = (lane >> 3) & 1;
+        const auto bytes = [&](int n) { return (uint32_t)(((n + page_rows - 1) >> B.page_shift) << B.page_shift) * 128u * M::HALVES; };
+        const auto load = [&](const CUtensorMap *map, uint32_t to, const TileRef &T, uint32_t b) {
+            if (half < M::HALVES && pg * page_rows < T.n) tma_load_2d(to + half * HALF_BYTES + pg * page_rows * 128, map, T.h * D + half * 64, T.y, b);
+        };
+        TileRef A = next(), C = A.n >= 0 ? next() : A;
+        bool alive = some;
+        int un = 0;
+        for (int gs = 0; alive && A.n >= 0; ++gs) {
+            TileRef E = C.n >= 0 ? next() : C;               // its page is on the way while this step's copies are issued
+            if (A.first) {                                    // queries of a new unit, once the last products with the old ones have been read
+                const Unit Q = unit_at(P.units, A.unit / P.n_kv);
+                for (int t = 0; t < 2 && alive; ++t) {
+                    if (un > 0) alive = warp_wait(bar(BAR_QFREE + t), (un - 1) & 1, abort_flag, B.status, P.wait_us);
+                    if (!alive) break;
+                    const bool with_k = un == 0 && t == 0;    // the very first keys ride with the very first queries
+                    if (lane == 0) mbar_expect_tx(bar(BAR_Q + t), M::TILE_B + (with_k ? bytes(A.n) + P.extra_tx : 0u));
+                    __syncwarp();
+                    const int y = (int)((long long)A.h * P.head_rows) + Q.q0 + (t * TILE < Q.rows ? t : 0) * TILE;       // a pair of one tile: the same one twice
+                    if (lane < M::HALVES) tma_load_2d(base + M::Q + t * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, y, bar(BAR_Q + t));
+                    if (with_k && lane < 16) load(&map_k, base + M::K, A, bar(BAR_Q));
+                }
+                ++un;
+                if (!alive) break;
+            }
+            // PV(step - 2) and QK(step - 1) have read what lies where V(step) and K(step + 1) go
+            if (gs > 0) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
+            if (!alive) break;
+            const int st = gs & 1;
+            if (lane == 0) mbar_expect_tx(bar(BAR_KV + st), bytes(A.n) + (C.n >= 0 ? bytes(C.n) : 0u));
+            __syncwarp();
+            if (lane >= 16) load(&map_v, base + M::V + st * M::TILE_B, A, bar(BAR_KV + st));
+            else if (C.n >= 0) load(&map_k, base + M::K + (st ^ 1) * M::TILE_B, C, bar(BAR_KV + st));
+            A = C;
+            C = E;
+        }
+    } else if (warp < 4) {
+        // ---------------------------------------------------------------- warps 1 and 2: S = Q_t K^T; warp 3: O += P V.  All lanes wait, one issues.
+        reg_dealloc<REGS_ISSUE>();
+        const bool lead = elect_one();
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        auto wait = [&](int b, int parity) {
+            const bool ok = warp_wait(bar(b), parity, abort_flag, B.status, P.wait_us);
+            tc_fence_after();
+            return ok;
+        };
+        bool alive = true;
+        int gs = 0;
+        for (int k = 0; alive; ++k) {
+            const int idx = unit_of(k, n_units);
+            if (idx < 0) break;
+            const Unit U = unit_at(P.units, idx / P.n_kv);
+            if (warp < 3) {
+                const int t = warp - 1;
+                const uint64_t dq0 = desc_kmajor(base + M::Q + t * M::TILE_B), dk0 = desc_kmajor(base + M::K);
+                alive = wait(BAR_Q + t, k & 1);
+#pragma unroll 1
+                for (int i = 0; i < U.nj && alive; ++i, ++gs) {
+                    if (gs > 0) alive = wait(BAR_KV + ((gs - 1) & 1), ((gs - 1) >> 1) & 1);
+                    if (alive && gs + t > 0) alive = wait(BAR_SFREE + (t ^ 1), (gs + t + 1) & 1);      // the other tile's scores have left the columns
+                    if (!alive) break;
+                    uint64_t dq = dq0, dk = dk0 + (gs & 1) * (M::TILE_B >> 4);
+#pragma unroll 1
+                    for (int half = 0; half < M::HALVES; ++half) {
+#pragma unroll
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            if (lead) mma_ss(tm + TM_S, dq + k4 * 2, dk + k4 * 2, QK, (half > 0 || k4 > 0));
+                        dq += HALF_BYTES >> 4;
+                        dk += HALF_BYTES >> 4;
+                    }
+                    if (lead) tc_commit(bar(BAR_SFULL + t));
+                }
+            } else {
+                const uint64_t dv0 = desc_mnmajor(base + M::V);
+#pragma unroll 1
+                for (int i = 0; i < U.nj && alive; ++i, ++gs) {
+                    const int st = gs & 1;
+                    alive = wait(BAR_KV + st, (gs >> 1) & 1);
+                    if (!alive) break;
+                    const int n = tile_keys(B, U, U.j0 + i, prefix_tiles);
+                    if (n < TILE) {                               // values behind the segment's end are whatever the pool holds there
+                        for (int hf = 0; hf < M::HALVES; ++hf)
+                            for (int c = n * 8 + lane; c < TILE * 8; c += 32) sts128(base + M::V + st * M::TILE_B + hf * HALF_BYTES + c * 16, 0u, 0u, 0u, 0u);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+#pragma unroll 1
+                    for (int t = 0; t < 2 && alive; ++t) {
+                        uint64_t dv = dv0 + st * (M::TILE_B >> 4);
+                        uint32_t pa = tm + TM_P + t * (TILE / 2);
+                        const uint32_t oa = tm + TM_O + t * TILE;
+#pragma unroll 1
+                        for (int hf = 0; hf < 2; ++hf) {
+                            alive = wait(BAR_PHALF + 2 * t + hf, gs & 1);
+                            if (!alive) break;
+#pragma unroll
+                            for (int k4 = 0; k4 < 4; ++k4)
+                                if (lead) mma_ts(oa, pa + k4 * 8, dv + k4 * (2048 >> 4), PV, (i > 0 || hf > 0 || k4 > 0));
+                            dv += 8192 >> 4;
+                            pa += 32;
+                        }
+                        if (alive && lead) tc_commit(bar(BAR_PVDONE + t));
+                    }
+                }
+            }
+        }
+        // nothing of ours still runs on the tensor core when its memory is freed
+        if (lead) tc_commit(bar(BAR_DONE));
+        __syncwarp();
+        pc_mbar_drain(bar(BAR_DONE), 0, B.status, PC_WHERE_PAGED_WAIT);
+    } else if (some) {
+        // ---------------------------------------------------------------- softmax, correction, output
+        reg_alloc<REGS_SOFTMAX>();
+        const int t = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+        const uint32_t s_addr = tmem + lane_addr + TM_S, p_addr = tmem + lane_addr + TM_P + t * (TILE / 2), o_addr = tmem + lane_addr + TM_O + t * TILE;
+        const bool lead = elect_one();
+        bool alive = true;
+        int k = 0, idx = unit_of(0, n_units), j = 0, lim;
+        Unit U = unit_at(P.units, idx / P.n_kv);
+        // own tokens that this thread's row sees (one behind the last row sees what the last one sees; its output is dropped)
+        const auto limit = [&]() { return B.causal ? U.before + (U.p0 + min(t * TILE + r, U.rows - 1)) / P.group + 1 : U.own; };
+        lim = limit();
+        float m_used = -INFINITY, l = 0.f;
+        for (int gs = 0; alive; ++gs) {
+            const bool flush = j == U.nj;
+            const Unit V = U;                                 // the unit to flush
+            const int v_idx = idx;
+            const float m_e = m_used, l_e = l;
+            bool end = false;
+            if (flush) {
+                idx = unit_of(++k, n_units);
+                end = idx < 0;
+                if (!end) {
+                    U = unit_at(P.units, idx / P.n_kv);
+                    lim = limit();
+                }
+                j = 0;
+                m_used = -INFINITY;
+                l = 0.f;
+            }
+            if (!end) {
+                alive = warp_wait(bar(BAR_SFULL + t), gs & 1, abort_flag, B.status, P.wait_us);
+                if (!alive) break;
+                tc_fence_after();
+                uint32_t sv[128];
+                tmem_ld32(s_addr, sv);
+                tmem_ld32(s_addr + 32, sv + 32);
+                tmem_ld32(s_addr + 64, sv + 64);
+                tmem_ld32(s_addr + 96, sv + 96);
+                tmem_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                arrive_if(lead, bar(BAR_SFREE + t));
+                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QFREE + t));
+                const bool pv_done = gs == 0 || pc_mbar_test(bar(BAR_PVDONE + t), (gs - 1) & 1);
+                const int jt = U.j0 + j;
+                const int seen = jt < prefix_tiles ? B.n_prefix - jt * TILE : min(lim, U.own) - (jt - prefix_tiles) * TILE;
+                if (__any_sync(0xffffffffu, seen < TILE)) {
+#pragma unroll
+                    for (int i = 0; i < TILE; ++i) sv[i] = i < seen ? sv[i] : 0xFF800000u;
+                }
+                float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < TILE; i += 4) {
+                    mx0 = fmaxf(mx0, __uint_as_float(sv[i]));
+                    mx1 = fmaxf(mx1, __uint_as_float(sv[i + 1]));
+                    mx2 = fmaxf(mx2, __uint_as_float(sv[i + 2]));
+                    mx3 = fmaxf(mx3, __uint_as_float(sv[i + 3]));
+                }
+                const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+                const bool grow = mx > m_used + GROW;
+                if (__builtin_expect(!__all_sync(0xffffffffu, pv_done), 0)) {
+                    alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
+                    if (!alive) break;
+                }
+                tc_fence_after();
+                if (t == 1) arrive_if(lead, bar(BAR_EMPTY + (gs & 1)));
+                if (__builtin_expect(__any_sync(0xffffffffu, grow), 0)) {
+                    const float m_new = fmaxf(m_used, mx);
+                    const float corr = m_new == -INFINITY ? 1.f : fast_exp2(m_used - m_new);
+                    l *= corr;
+                    if (j > 0) {
+                        uint32_t v[32];
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            tmem_ld32(o_addr + c * 32, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * corr);
+                            tmem_st32(o_addr + c * 32, v);
+                        }
+                    }
+                    m_used = m_new;
+                }
+                const float neg = m_used == -INFINITY ? 0.f : -m_used;
+                const float2 neg_m = make_float2(neg, neg);
+                float2 la = make_float2(0.f, 0.f), lb = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float2 x = add2(make_float2(__uint_as_float(sv[c * 32 + 2 * i]), __uint_as_float(sv[c * 32 + 2 * i + 1])), neg_m);
+                        float2 y = add2(make_float2(__uint_as_float(sv[c * 32 + 2 * i + 2]), __uint_as_float(sv[c * 32 + 2 * i + 3])), neg_m);
+                        x.x = fast_exp2(x.x); x.y = fast_exp2(x.y);
+                        y.x = fast_exp2(y.x); y.y = fast_exp2(y.y);
+                        la = add2(la, x);
+                        lb = add2(lb, y);
+                        pk[i] = pc_pack_bf16(x.x, x.y);
+                        pk[i + 1] = pc_pack_bf16(y.x, y.y);
+                    }
+                    asm volatile("" : "+f"(la.x), "+f"(la.y), "+f"(lb.x), "+f"(lb.y));
+                    tmem_st16(p_addr + c * 16, pk);
+                    if (c & 1) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        arrive_if(lead && !flush, bar(BAR_PHALF + 2 * t + (c >> 1)));
+                    }
+                }
+                l += (la.x + la.y) + (lb.x + lb.y);
+            } else {
+                alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
+                if (!alive) break;
+                tc_fence_after();
+            }
+            if (__builtin_expect(flush, 0)) {
+                uint32_t v[D];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
+                tmem_wait_ld();
+                if (!end) {
+                    tc_fence_before();
+                    __syncwarp();
+                    arrive_if(lead, bar(BAR_PHALF + 2 * t));
+                    arrive_if(lead, bar(BAR_PHALF + 2 * t + 1));
+                }
+                const int h = v_idx % P.n_kv, at = t * TILE + r, p = V.p0 + at, i = p / P.group;
+                const bool there = at < V.rows;
+                const size_t row = (size_t)(V.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
+                __nv_bfloat16 *orow = P.out + row * D;
+                if (P.shared) {
+                    const size_t slot = (((size_t)h * tiles_of((int)P.head_rows) + 2 * V.slot + t) * V.parts + V.part) * TILE + r;
+                    if (there) {
+#pragma unroll
+                        for (int c = 0; c < D / 4; ++c) *reinterpret_cast<uint4 *>(P.part_o + slot * D + c * 4) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                        P.part_ml[slot] = make_float2(m_e, l_e);
+                    }
+                } else if (V.parts == 1) {
+                    const float inv = l_e > 0.f ? 1.f / l_e : (l_e != l_e ? l_e : 0.f);
+                    if (there) {
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) {
+                            uint4 w;
+                            w.x = pc_pack_bf16(__uint_as_float(v[8 * c + 0]) * inv, __uint_as_float(v[8 * c + 1]) * inv);
+                            w.y = pc_pack_bf16(__uint_as_float(v[8 * c + 2]) * inv, __uint_as_float(v[8 * c + 3]) * inv);
+                            w.z = pc_pack_bf16(__uint_as_float(v[8 * c + 4]) * inv, __uint_as_float(v[8 * c + 5]) * inv);
+                            w.w = pc_pack_bf16(__uint_as_float(v[8 * c + 6]) * inv, __uint_as_float(v[8 * c + 7]) * inv);
+                            *reinterpret_cast<uint4 *>(orow + c * 8) = w;
+                        }
+                        if (P.lse) P.lse[row] = (m_e + log2f(l_e)) * 0.6931471805599453f;
+                    }
+                } else {
+                    // Parts lie as 16-byte unit (c, row) at c * 128 + row: a warp's stores and loads are 512 bytes in a row.  The last of a pair's CTAs to come (of their warps with the same rows) adds them up, its
+                    // own among them, by number: the same bits whoever comes last.
+                    const size_t first = ((size_t)V.slot * P.n_kv + (size_t)h * V.parts) * 2 + t;
+                    {
+                        uint4 *po = reinterpret_cast<uint4 *>(P.part_o) + (first + 2 * V.part) * (TILE * D / 4) + r;
+#pragma unroll
+                        for (int c = 0; c < D / 4; ++c) po[c * TILE] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                        P.part_ml[(first + 2 * V.part) * TILE + r] = make_float2(m_e, l_e);
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    int come = 0;                             // every warp for its own 32 rows
+                    if (lane == 0) come = atomicAdd(P.tickets + first * 4 + quad, 1);
+                    come = __shfl_sync(0xffffffffu, come, 0);
+                    if (come == V.parts - 1) {
+                        __threadfence();
+                        float m = -INFINITY, sum = 0.f;
+                        for (int q = 0; q < V.parts; ++q) m = fmaxf(m, __ldcg(P.part_ml + (first + 2 * q) * TILE + r).x);
+                        for (int q = 0; q < V.parts; ++q) {
+                            const float2 ml = __ldcg(P.part_ml + (first + 2 * q) * TILE + r);
+                            sum = fmaf(ml.y, m == -INFINITY ? 1.f : fast_exp2(ml.x - m), sum);
+                        }
+                        const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
+#pragma unroll 1
+                        for (int c0 = 0; c0 < D / 4; c0 += 8) {
+                            float4 a[8];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) a[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            for (int q = 0; q < V.parts; ++q) {
+                                const float f = m == -INFINITY ? 1.f : fast_exp2(__ldcg(P.part_ml + (first + 2 * q) * TILE + r).x - m);
+                                const float4 *po = reinterpret_cast<const float4 *>(P.part_o) + (first + 2 * q) * (TILE * D / 4) + r;
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) {
+                                    const float4 x = __ldcg(po + (c0 + c) * TILE);
+                                    a[c].x = fmaf(x.x, f, a[c].x);
+                                    a[c].y = fmaf(x.y, f, a[c].y);
+                                    a[c].z = fmaf(x.z, f, a[c].z);
+                                    a[c].w = fmaf(x.w, f, a[c].w);
+                                }
+                            }
+                            if (there)
+#pragma unroll
+                                for (int c = 0; c < 8; c += 2)
+                                    *reinterpret_cast<uint4 *>(orow + (c0 + c) * 4) = make_uint4(pc_pack_bf16(a[c].x * inv, a[c].y * inv), pc_pack_bf16(a[c].z * inv, a[c].w * inv),
+                                                                                                 pc_pack_bf16(a[c + 1].x * inv, a[c + 1].y * inv), pc_pack_bf16(a[c + 1].z * inv, a[c + 1].w * inv));
+                        }
+                        if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
+                    }
+                }
+            }
+            if (end) break;
+            ++j;
+        }
+    } else {
+        reg_alloc<REGS_SOFTMAX>();
+    }
+    __syncwarp();
+    if (*abort_flag) pc_let_copies_land();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// Rows as [page x token][KV head x channel], boxes of a page by 64 channels; queries as [KV head x row][channel], boxes of 128 rows
+bool map_rows(CUtensorMap *m, const void *p, uint64_t rows, uint64_t cols, uint32_t box_rows) { return make_map(m, p, rows, cols, box_rows); }
+
+template <int D> pc_status launch_tc(const pc_ctx *ctx, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const TcParams &P, cudaStream_t stream) {
+    static bool ready[PC_MAX_DEVICES] = {};
+    if (ctx->device < 0 || ctx->device >= PC_MAX_DEVICES) return PC_ERR_UNSUPPORTED;
+    if (!ready[ctx->device]) {
+        PC_CUDA_TRY(cudaFuncSetAttribute(k_paged_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Map<D>::ALLOC));
+        cudaFuncAttributes a;
+        PC_CUDA_TRY(cudaFuncGetAttributes(&a, k_paged_tc<D>));
+        if (a.numRegs < REGS_LAUNCH) {                     // setmaxnreg would wait for registers that the block does not have
+            fprintf(stderr, "packcache: k_paged_tc has %d registers a thread, %d are shared out\n", a.numRegs, REGS_LAUNCH);
+            return PC_ERR_UNSUPPORTED;
+        }
+        ready[ctx->device] = true;
+    }
+    PC_LAUNCH(k_paged_tc<D>, dim3(ctx->sm_count), dim3(TC_THREADS), Map<D>::ALLOC, stream, mq, mk, mv, P);
+    return PC_OK;
+}
+
+}  // namespace
+
+bool pc_paged_tc_shape(const pc_ctx *ctx) { return ctx->desc.dtype == PC_BF16; }
+size_t pc_paged_tc_units(const pc_ctx *ctx) { return ((size_t)ctx->desc.max_q * ctx->group + PAIR - 1) / PAIR + PC_MAX_SEQS + (size_t)4 * ctx->sm_count; }
+size_t pc_paged_tc_slots(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count; }
+size_t pc_paged_tc_plan_bytes(const pc_ctx *ctx) { return PLAN_HEAD * sizeof(int) + pc_paged_tc_units(ctx) * sizeof(Unit); }
+
+// Parts of the shared prefix's keys for a call's rows, 0 where the scratch does not hold them
+int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B) {
+    const long long pairs = ((long long)B.n_rows * ctx->group + PAIR - 1) / PAIR, items = pairs * ctx->desc.n_kv_heads;
+    if (items == 0 || items > (long long)pc_paged_tc_slots(ctx)) return 0;
+    return (int)std::max(1LL, std::min<long long>(ctx->sm_count / items, (B.n_prefix + TILE - 1) / TILE));
+}
+
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream) {
+    const pc_ctx *ctx = A.ctx;
+    const pc_layer_desc &D = ctx->desc;
+    const long long head_rows = (long long)A.batch.n_rows * ctx->group;
+    if (head_rows * D.n_kv_heads > INT32_MAX) return PC_ERR_CAPACITY;
+    CUtensorMap mq, mk, mv;
+    const uint64_t rows = (uint64_t)A.batch.n_pages << A.batch.page_shift, cols = (uint64_t)D.n_kv_heads * D.head_dim;
+    if (!map_rows(&mq, w->q_rot, (uint64_t)head_rows * D.n_kv_heads, D.head_dim, TILE) || !map_rows(&mk, A.pages->k, rows, cols, 1u << A.batch.page_shift) ||
+        !map_rows(&mv, A.pages->v, rows, cols, 1u << A.batch.page_shift)) {
+        fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
+        return PC_ERR_CUDA;
+    }
+    FrontParams F{};
+    F.B = A.batch;
+    F.q = static_cast<const char *>(A.q);
+    F.q_pos = A.q_pos;
+    F.q_rot = static_cast<char *>(w->q_rot);
+    F.chunks = D.n_q_heads * D.head_dim / 8;
+    F.group = ctx->group;
+    F.n_kv = D.n_kv_heads;
+    F.d = D.head_dim;
+    F.head_rows = head_rows;
+    F.scale = pc_q_rot_scale(D.head_dim);
+    F.shared = prefix_parts > 0;
+    F.shared_parts = prefix_parts;
+    F.sms = ctx->sm_count;
+    F.max_units = (int)pc_paged_tc_units(ctx);
+    F.n_tickets = (int)pc_paged_tc_slots(ctx) * 8;
+    F.tickets = w->tc_tickets;
+    F.head = w->tc_plan;
+    F.units = reinterpret_cast<int4 *>(w->tc_plan + PLAN_HEAD);
+    const long long blocks = 1 + ((long long)A.batch.n_rows * 32 + FRONT_THREADS - 1) / FRONT_THREADS;
+    PC_LAUNCH(k_paged_front, dim3((unsigned)blocks), dim3(FRONT_THREADS), 0, stream, F, ctx->rope);
+    TcParams P{};
+    P.B = A.batch;
+    P.n_q_heads = D.n_q_heads;
+    P.n_kv = D.n_kv_heads;
+    P.group = ctx->group;
+    P.shared = prefix_parts > 0;
+    P.head_rows = head_rows;
+    P.out = static_cast<__nv_bfloat16 *>(A.out);
+    P.lse = A.lse;
+    P.units = F.units;
+    P.head = F.head;
+    P.part_o = w->tc_o;
+    P.part_ml = w->tc_ml;
+    P.tickets = w->tc_tickets;
+    P.wait_us = ctx->wait_limit_us;
+    P.extra_tx = ctx->test_extra_tx;
+    if (left) *left = PagedTcParts{w->tc_o, w->tc_ml, (int)((head_rows + TILE - 1) / TILE), prefix_parts};
+    return D.head_dim == 128 ? launch_tc<128>(ctx, mq, mk, mv, P, stream) : launch_tc<64>(ctx, mq, mk, mv, P, stream);
+}
