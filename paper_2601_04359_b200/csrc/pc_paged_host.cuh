@@ -13,9 +13,9 @@ struct pc_paged {
     float2 *few_ml, *home_ml;
     size_t home_rows;
     long long *plan;
-    // bf16: rotated queries, units, parts and their counters of the tcgen05 kernel
+    // bf16: rotated queries, parts of the tcgen05 kernel and their counters
     void *q_rot;
-    int *tc_plan, *tc_tickets;
+    uint32_t *tc_sync;
     float *tc_o;
     float2 *tc_ml;
 };
@@ -30,23 +30,22 @@ struct pc_paged_args {
     float *lse;
 };
 
-// What the tcgen05 kernel leaves of a shared prefix: `parts` pieces of its keys for every tile of packed rows of every KV head, each a tile of rows of d fp32
-// values and their (maximum, sum)
-struct PagedTcParts {
+// How the tcgen05 kernel shares out a prefix that all rows of a call see: items (pair of tiles of packed rows, KV head) of `tiles` key tiles and `gap` empty places on a line that `ctas` CTAs share evenly.  An
+// item of one CTA is at home in scratch, row by row; of an item of several the first CTA's part lies in that CTA's second place, the others' in their first, a place being two tiles of rows.
+constexpr int PAGED_TC_LEAST = 4;            // fewest places of a CTA's run
+__device__ __forceinline__ int paged_tc_ctas(long long total, int ctas) { return (int)min((long long)ctas, max(1LL, total / PAGED_TC_LEAST)); }
+__device__ __forceinline__ int paged_tc_cta(long long total, int ctas, long long place) { return (int)(((place + 1) * ctas + total - 1) / total) - 1; }      // the CTA that has a place
+struct PagedTcLine {
     const float *part_o;
     const float2 *part_ml;
-    int tiles, parts;
+    int tiles, gap, ctas;
 };
-struct PagedTcRow { size_t first; int row, parts; };
-__device__ __forceinline__ PagedTcRow paged_tc_row(const PagedTcParts &T, int h, long long packed_row) {
-    return {((size_t)h * T.tiles + (size_t)(packed_row / PAGED_TC_TILE)) * T.parts, (int)(packed_row % PAGED_TC_TILE), T.parts};
-}
 
 size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kernel's scratch
 // shared: the prefix is attended apart from the sequences' own tokens, here or (tc given) by the tcgen05 kernel before
-pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream);
+pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcLine *tc, cudaStream_t stream);
 bool pc_paged_tc_shape(const pc_ctx *ctx);           // whether the tcgen05 kernel takes the context's type
-size_t pc_paged_tc_slots(const pc_ctx *ctx), pc_paged_tc_plan_bytes(const pc_ctx *ctx);
-int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B);
-// prefix_parts 0: every sequence over prefix and own tokens, into the output; otherwise the shared prefix alone, in so many parts, into scratch (left)
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream);
+size_t pc_paged_tc_tiles(const pc_ctx *ctx), pc_paged_tc_sync_words(const pc_ctx *ctx);
+// every sequence over prefix and own tokens, into the output; or (shared) the prefix alone for all rows, into scratch
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, cudaStream_t stream);
+PagedTcLine pc_paged_tc_line(const pc_paged *w, const pc_paged_args &A);

@@ -1,16 +1,16 @@
 // Attention over a paged cache on tcgen05 tensor cores (bf16): prompts, their pieces and frames, and a prefix that many rows share.
 //
-// Two launches.
-//   k_paged_front  rotates the queries, with log2(e) / sqrt(d) folded in, into rows of KV head x (token, head of the group): the rows that share keys and values lie side by side,
-//                  so a tile of 128 rows is full whatever the group's size, and a causal tile of G heads spans 128 / G tokens only.  Its first CTA plans the call from
-//                  the lengths on the device: units (sequence, pair of query tiles, run of key tiles), longest first.
-//   k_paged_tc     persistent CTAs take units in snake order (CTA c the c-th, the c-th from the end of the next round, ...): with the longest first that leaves them within
-//                  about a unit of each other.  Pairs with more key tiles than an even share are cut into parts; the last of a pair's CTAs adds the parts up, in the order of the keys.
-// A CTA: warp 0 fetches keys and values by TMA, a lane a page's box (a tile of 128 keys is 1 to 8 pages), two stages each; warps 1 and 2 issue S = Q_t K^T of the two query
-// tiles, warp 3 O_t += P_t V; warps 4-7 and 8-11 are the softmax of tile 0 and 1: the score row in registers, running maximum and sum in fp32, probabilities as bf16 into tensor
-// memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame kernel, k_attend_tc.)
+// Two launches.  k_paged_front rotates the queries, with log2(e) / sqrt(d) folded in, into rows of KV head x (token, head of the group): rows that share keys and values lie side by side,
+// so a tile of 128 rows is full whatever the group's size, and a causal tile of G heads spans 128 / G tokens only.
+// k_paged_tc: an item is (sequence, pair of such tiles, KV head); its key tiles lie on one line with those of all other items, which the CTAs (one an SM) share evenly.  Where the line is cut follows from
+// lengths that lie on the device: every CTA adds them up for itself.  An item that several CTAs share is added up by the last of them, in the order of the keys.
+// A CTA: warp 0 walks the line, tells the others of its units by way of a ring of four in shared memory, and fetches by TMA, a lane a page's box (a tile of 128 keys is 1 to 8 pages), two stages of keys and
+// of values; warps 1 and 2 issue S = Q_t K^T of the two query tiles, warp 3 O_t += P_t V; warps 4-7 and 8-11 are the softmax of tile 0 and 1: the score row in registers, running
+// maximum and sum in fp32, probabilities as bf16 into tensor memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame kernel, k_attend_tc.)
 // Rows behind a segment's end: scores are replaced by -infinity whatever they are, and the values' rows are cleared in shared memory, since 0 times what lies
 // there may be NaN.
+// Tried: queries rotated in this kernel, by four warps more, into three places in turn.  Their chains of shuffles, addresses and products are 1,000 instructions a tile at five to ten cycles, 7 us, where
+// a unit of three key tiles takes 4.6: packed prompts 227 us a call instead of 89.
 #include <algorithm>
 
 #include "pc_paged_host.cuh"
@@ -24,61 +24,51 @@ constexpr int TC_THREADS = 384;
 constexpr int REGS_LAUNCH = 65536 / TC_THREADS / 8 * 8, REGS_ISSUE = 72, REGS_SOFTMAX = 216;
 static_assert(128 * REGS_ISSUE + 256 * REGS_SOFTMAX <= TC_THREADS * REGS_LAUNCH, "more registers than the block has");
 constexpr float GROW = 8.f;
-constexpr int PAIR = 2 * TILE;                     // packed rows of a unit
-constexpr int LEAST_TILES = 4;                     // a part of a pair has as many key tiles at least
+constexpr int PAIR = 2 * TILE;                     // packed rows of an item
+constexpr int GAP = 2;                             // what crossing into the next item costs, in key tiles: so many empty places lie behind each item on the line
+constexpr int UNITS = 4;                           // units that are told ahead
 
-// What a unit's roles need to know of it
+// What a CTA does of an item, and what its warps need to know of that
 struct Unit {
-    int s;                   // sequence; -1: rows of all sequences over the shared prefix
-    int q0;                  // first row of the pair among the rotated queries of a KV head
-    int rows;                // packed rows of the pair
-    int p0;                  // their first, counted from the sequence's first
     int r0;                  // the sequence's first row in the batch
-    int before, own;         // own tokens before the rows, and in all
-    int j0, nj;              // key tiles: those of the prefix first
-    int part, parts;         // of the pair
-    int slot;                // place of the pair's first part in scratch, in pairs of tiles of one KV head; the KV head and part follow
+    int p0, rows;            // first of the pair's packed rows in the sequence, and how many
+    int before, own;         // own tokens before the sequence's rows, and in all
+    int j0, nj;              // key tiles: those of the prefix first; nj 0: no more units
+    int h;
+    int c0, parts, part;     // first CTA of the item, CTAs of it, which of them this is
+    int pad;
 };
 static_assert(sizeof(Unit) == 48, "three 16-byte pieces");
-constexpr int PLAN_HEAD = 4;                       // words ahead of the units: their number
 
 template <int D> struct Map {
     static constexpr int HALVES = D / 64, TILE_B = HALVES * HALF_BYTES;
-    static constexpr int Q = 0, K = Q + 2 * TILE_B, V = K + 2 * TILE_B, BAR = V + 2 * TILE_B, ALLOC = BAR + 256 + 1024;
+    static constexpr int Q = 0, K = Q + 2 * TILE_B, V = K + 2 * TILE_B, BAR = V + 2 * TILE_B, FLAGS = BAR + 256, UNIT = FLAGS + 64, ALLOC = UNIT + UNITS * 48 + 1024;
+    static constexpr int SEQS = 0, ENDS = PC_MAX_SEQS * 16;       // while the line is made, where the queries will be: a sequence's numbers, the line's place behind it
+    static_assert(ALLOC <= 232448 && ENDS + PC_MAX_SEQS * 8 <= 2 * TILE_B, "shared memory");
 };
-enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_KV = 4 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 6 /* [step & 1] */, BAR_SFULL = 8 /* [tile] */,
-       BAR_SFREE = 10 /* [tile] */, BAR_PHALF = 12 /* [tile][half] */, BAR_PVDONE = 16 /* [tile] */, BAR_DONE = 18, N_BARS = 19 };
+enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_K0 = 4, BAR_KV = 5 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 7 /* [step & 1] */, BAR_SFULL = 9 /* [tile] */,
+       BAR_SFREE = 11 /* [tile] */, BAR_PHALF = 13 /* [tile][half] */, BAR_PVDONE = 17 /* [tile] */, BAR_DONE = 19, BAR_UF = 20 /* [unit & 3]: told */, BAR_UE = 24 /* [unit & 3]: taken by all */, N_BARS = 28 };
+static_assert(N_BARS * 8 <= 256, "barriers");
+constexpr int UNIT_READERS = 11;                   // warps 1 to 11
 constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
 
 struct TcParams {
     PagedBatch B;
     int n_q_heads, n_kv, group;
-    int shared;              // the prefix alone, rows of all sequences; parts go to scratch row by row for k_paged_join
-    long long head_rows;     // rows of a KV head among the rotated queries
+    int head_rows;           // rows of a KV head among the rotated queries
+    int shared;              // the prefix alone, rows of all sequences; what comes out goes to scratch row by row for k_paged_join
     __nv_bfloat16 *out;
     float *lse;
-    const int4 *units;
-    const int *head;
-    float *part_o;
+    float *part_o;           // [2 CTAs][tile][128][D]: a CTA's first and last item
     float2 *part_ml;
-    int *tickets;            // [slots][tile][warp] parts that have arrived; zero at first
+    float *home_o;           // shared: items of one CTA, [rows][query heads][D]
+    float2 *home_ml;
+    uint32_t *sync;          // [0] number of the call, [1] CTAs that are done, then [CTA][tile][warp] tickets: number of the call and parts that have come
     uint32_t wait_us, extra_tx;
 };
+constexpr int SYNC_HEAD = 2;
 
-__device__ __forceinline__ Unit unit_at(const int4 *units, int i) {
-    const int4 a = __ldcg(units + 3 * i), b = __ldcg(units + 3 * i + 1), c = __ldcg(units + 3 * i + 2);
-    return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w};
-}
-// The k-th unit of a CTA, -1 behind the last
-__device__ __forceinline__ int unit_of(int k, int n) {
-    const long long i = k & 1 ? (long long)(k + 1) * gridDim.x - 1 - blockIdx.x : (long long)k * gridDim.x + blockIdx.x;
-    return i < n ? (int)i : -1;
-}
-__device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
-
-// ------------------------------------------------------------------------------------------------ queries and plan
-constexpr int FRONT_THREADS = 512;
-constexpr int LEVELS = 512;
+constexpr int FRONT_THREADS = 256;
 
 struct FrontParams {
     PagedBatch B;
@@ -88,108 +78,13 @@ struct FrontParams {
     int chunks, group, n_kv, d;
     long long head_rows;
     float scale;
-    int shared, shared_parts, sms, max_units, n_tickets;
-    int4 *units;
-    int *head, *tickets;
 };
 
-__device__ __forceinline__ void put_unit(int4 *units, int i, const Unit &U) {
-    units[3 * i] = make_int4(U.s, U.q0, U.rows, U.p0);
-    units[3 * i + 1] = make_int4(U.r0, U.before, U.own, U.j0);
-    units[3 * i + 2] = make_int4(U.nj, U.part, U.parts, U.slot);
-}
-
-// Key tiles of a pair: up to the last key that one of its rows sees, one at least
-__device__ __forceinline__ int pair_tiles(const FrontParams &P, int n, int len, int pair) {
-    const int last = (min((pair + 1) * PAIR, n * P.group) - 1) / P.group;
-    const int sees = P.B.causal ? min(len, max(0, len - n + last + 1)) : len;
-    return max(1, tiles_of(P.B.n_prefix) + tiles_of(sees));
-}
-
-__device__ void plan(const FrontParams &P) {
-    __shared__ int pair0[PC_MAX_SEQS + 1], seq_r0[PC_MAX_SEQS], seq_n[PC_MAX_SEQS], seq_len[PC_MAX_SEQS], level[LEVELS];
-    __shared__ long long sums[32];
-    __shared__ int counts[2];
-    const int tid = threadIdx.x;
-    static_assert(PC_MAX_SEQS <= FRONT_THREADS && LEVELS == FRONT_THREADS, "a thread a sequence, and a level");
-    if (P.shared) {
-        const int packed = paged_rows(P.B) * P.group, tiles = tiles_of(P.B.n_prefix), parts = P.shared_parts, pairs = (packed + PAIR - 1) / PAIR;
-        for (int i = tid; i < pairs * parts; i += FRONT_THREADS) {
-            const int pair = i / parts, part = i - pair * parts;
-            const int j0 = (int)((long long)tiles * part / parts), j1 = (int)((long long)tiles * (part + 1) / parts);
-            put_unit(P.units, i, Unit{-1, pair * PAIR, min(PAIR, packed - pair * PAIR), pair * PAIR, 0, 0, 0, j0, j1 - j0, part, parts, pair});
-        }
-        if (tid == 0) P.head[0] = pairs * parts;
-        return;
-    }
-    int mine = 0;
-    if (tid < P.B.n_seqs) {
-        const PagedSeq S = paged_seq(P.B, tid);
-        seq_r0[tid] = S.r0;
-        seq_n[tid] = S.n;
-        seq_len[tid] = S.len;
-        mine = (S.n * P.group + PAIR - 1) / PAIR;
-    }
-    level[tid] = 0;
-    for (int i = tid; i < P.n_tickets; i += FRONT_THREADS) P.tickets[i] = 0;
-    if (tid < 2) counts[tid] = 0;
-    const long long end = paged_scan<FRONT_THREADS>((long long)mine, sums);
-    if (tid < P.B.n_seqs) pair0[tid] = (int)end - mine;
-    const int pairs = (int)sums[FRONT_THREADS / 32 - 1];
-    if (tid == 0) pair0[P.B.n_seqs] = pairs;
-    __syncthreads();
-    const auto seq_of = [&](int pair) {
-        int lo = 0, hi = P.B.n_seqs - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (pair0[mid] <= pair) lo = mid; else hi = mid - 1;
-        }
-        return lo;
-    };
-    long long tiles = 0;
-    for (int i = tid; i < pairs; i += FRONT_THREADS) {
-        const int s = seq_of(i);
-        tiles += pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]);
-    }
-    paged_scan<FRONT_THREADS>(tiles, sums);
-    tiles = sums[FRONT_THREADS / 32 - 1];
-    // An even share of all key tiles; a pair with more than a quarter above it is cut, into parts that are over 5/9 of a share each: fewer than two an SM, which the scratch holds.
-    const int share = (int)min((long long)INT32_MAX / 2, max((long long)LEAST_TILES, (tiles * P.n_kv + P.sms - 1) / P.sms));
-    const auto parts_of = [&](int t) { return t <= share + share / 4 ? 1 : (t + share - 1) / share; };
-    const auto level_of = [&](int size) { return LEVELS - 1 - min(size, LEVELS - 1); };
-    for (int i = tid; i < pairs; i += FRONT_THREADS) {
-        const int s = seq_of(i), t = pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]), parts = parts_of(t);
-        atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
-    }
-    __syncthreads();
-    const int n_level = level[tid];
-    __syncthreads();
-    const long long upto = paged_scan<FRONT_THREADS>((long long)n_level, sums);
-    level[tid] = (int)upto - n_level;
-    if (tid == 0) P.head[0] = min((int)sums[FRONT_THREADS / 32 - 1], P.max_units);
-    __syncthreads();
-    for (int i = tid; i < pairs; i += FRONT_THREADS) {
-        const int s = seq_of(i), pair = i - pair0[s], n = seq_n[s], len = seq_len[s], t = pair_tiles(P, n, len, pair);
-        const int parts = parts_of(t);
-        const int at = atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
-        const int slot = parts > 1 ? atomicAdd(&counts[0], parts) : 0;
-        for (int part = 0; part < parts; ++part) {
-            const int j0 = (int)((long long)t * part / parts), j1 = (int)((long long)t * (part + 1) / parts);
-            if (at + part < P.max_units)                      // (row ranges that overlap can make more units than there are rows for)
-                put_unit(P.units, at + part, Unit{s, seq_r0[s] * P.group + pair * PAIR, min(PAIR, n * P.group - pair * PAIR), pair * PAIR, seq_r0[s], len - n, len, j0, j1 - j0, part, parts, slot});
-        }
-    }
-}
-
 __global__ void __launch_bounds__(FRONT_THREADS) k_paged_front(const __grid_constant__ FrontParams P, const __grid_constant__ pc_rope_dev rope) {
-    pc_grid_dep_launch();
     pc_grid_dep_wait();
-    if (blockIdx.x == 0) {
-        plan(P);
-        return;
-    }
+    pc_grid_dep_launch();              // behind the wait: what came before is complete when the attention kernel starts, which looks at lengths and tables ahead of its own
     // a warp a row of the batch, lane's chunks of eight channels 32 apart: all at one place of a head
-    const int lane = threadIdx.x & 31, row = (int)(((blockIdx.x - 1) * FRONT_THREADS + threadIdx.x) >> 5);
+    const int lane = threadIdx.x & 31, row = (int)((blockIdx.x * FRONT_THREADS + threadIdx.x) >> 5);
     if (row >= paged_rows(P.B)) return;
     const int4 pos = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + row);
     const char *q = P.q + (size_t)row * P.chunks * 16;
@@ -226,18 +121,22 @@ __global__ void __launch_bounds__(FRONT_THREADS) k_paged_front(const __grid_cons
     if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
 }
 
-// ------------------------------------------------------------------------------------------------ attention
+__device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
+// Key tiles of a pair: up to the last key that one of its rows sees, one at least
+__device__ __forceinline__ int pair_tiles(const TcParams &P, int n, int len, int pair) {
+    if (P.shared) return max(1, tiles_of(P.B.n_prefix));
+    const int last = (min((pair + 1) * PAIR, n * P.group) - 1) / P.group;
+    const int sees = P.B.causal ? min(len, max(0, len - n + last + 1)) : len;
+    return max(1, tiles_of(P.B.n_prefix) + tiles_of(sees));
+}
+__device__ __forceinline__ long long cta_cut(long long total, int ctas, int c) { return total * min(c, ctas) / ctas; }
+
 __device__ __forceinline__ void arrive_if(bool who, uint32_t bar) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((uint32_t)who) : "memory");
 }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, uint32_t limit_us) {
     if (__builtin_expect(__all_sync(0xffffffffu, pc_mbar_try(bar, parity)), 1)) return true;
     return __all_sync(0xffffffffu, pc_mbar_wait(bar, parity, abort_flag, status, PC_WHERE_PAGED_WAIT, limit_us));
-}
-
-// Keys of tile j of a unit that are there, of 128
-__device__ __forceinline__ int tile_keys(const PagedBatch &B, const Unit &U, int j, int prefix_tiles) {
-    return min(TILE, j < prefix_tiles ? B.n_prefix - j * TILE : max(0, U.own - (j - prefix_tiles) * TILE));
 }
 
 template <int D>
@@ -249,26 +148,17 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + M::BAR + N_BARS * 8);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + M::BAR + N_BARS * 8 + 4);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + M::FLAGS);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + M::FLAGS + 4);
+    int4 *told = reinterpret_cast<int4 *>(gen + M::UNIT);
     const uint32_t bar0 = base + M::BAR;
     auto bar = [&](int i) { return bar0 + 8u * i; };
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(bar(BAR_KV + s), 1);
-            mbar_init(bar(BAR_EMPTY + s), 4);
+        for (int i = 0; i < N_BARS; ++i) {
+            const bool by_warps = (i >= BAR_QFREE && i < BAR_K0) || (i >= BAR_EMPTY && i < BAR_SFULL) || (i >= BAR_SFREE && i < BAR_PVDONE);        // of the four of one tile's softmax
+            mbar_init(bar(i), by_warps ? 4 : (i == BAR_DONE ? 3 : (i >= BAR_UE ? UNIT_READERS : 1)));
         }
-        for (int t = 0; t < 2; ++t) {
-            mbar_init(bar(BAR_Q + t), 1);
-            mbar_init(bar(BAR_QFREE + t), 4);
-            mbar_init(bar(BAR_SFULL + t), 1);
-            mbar_init(bar(BAR_SFREE + t), 4);
-            mbar_init(bar(BAR_PVDONE + t), 1);
-            mbar_init(bar(BAR_PHALF + 2 * t), 4);
-            mbar_init(bar(BAR_PHALF + 2 * t + 1), 4);
-        }
-        mbar_init(bar(BAR_DONE), 3);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -277,77 +167,214 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    const PagedBatch &B = P.B;
+    const int prefix_tiles = tiles_of(B.n_prefix);
+
+    // ---- the line (of what was there before the rotation began, so ahead of the wait for that): every sequence's places, then where this CTA's run begins
+    int4 *seqs = reinterpret_cast<int4 *>(gen + M::SEQS);
+    long long *ends = reinterpret_cast<long long *>(gen + M::ENDS);
+    const int n_seqs = P.shared ? 1 : B.n_seqs;
+    for (int s = threadIdx.x; s < n_seqs; s += TC_THREADS) {
+        PagedSeq S = {0, 0, 0};
+        if (P.shared) S.n = paged_rows(B); else S = paged_seq(B, s);
+        seqs[s] = make_int4(S.r0, S.n, S.len, 0);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    pc_grid_dep_wait();
-
-    const PagedBatch &B = P.B;
-    const int prefix_tiles = tiles_of(B.n_prefix);
-    const int n_units = __ldcg(P.head) * P.n_kv;         // a unit of the list times the KV heads, heads side by side
-    const bool some = unit_of(0, n_units) >= 0;          // this CTA has work
-
-    // Steps are counted through all units (gs), units by un.
+    for (int s = warp; s < n_seqs; s += TC_THREADS / 32) {
+        const int4 S = seqs[s];
+        const int pairs = (S.y * P.group + PAIR - 1) / PAIR;
+        long long v = 0;
+        for (int i = lane; i < pairs; i += 32) v += pair_tiles(P, S.y, S.z, i) + GAP;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) ends[s] = v * P.n_kv;
+    }
+    __syncthreads();
+    // warp 0's walk: sequence, pair, KV head, places of the item that lie behind; places left of the run
+    struct { int s, r0, n, len, pair, h, off, tiles, ctas; long long left, item, total; } W{};
     if (warp == 0) {
-        // ---------------------------------------------------------------- TMA producer: all lanes
-        reg_dealloc<REGS_ISSUE>();
-        // Tiles of keys in the order of the steps.  A lane has a page of the tile: lane 8 half + page of the keys' boxes, 16 + 8 half + page of the values', which are at the same place.
-        struct TileRef { int y, n, h, first, unit; };       // row of the lane's page, keys, KV head, first of its unit
-        Unit U{};
-        int k = -1, j = 0, uh = 0, uidx = 0;
-        const int page_rows = 1 << B.page_shift, pg = lane & 7;
-        const auto next = [&]() -> TileRef {
-            bool first = false;
-            if (k < 0 || j == U.j0 + U.nj) {
-                uidx = unit_of(++k, n_units);
-                if (uidx < 0) {
-                    k = 1 << 29;
-                    j = U.j0 + U.nj;
-                    return {0, -1, 0, 0, 0};
-                }
-                U = unit_at(P.units, uidx / P.n_kv);
-                uh = uidx % P.n_kv;
-                j = U.j0;
-                first = true;
+        const auto scan = [&](long long v) {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
             }
-            const int n = tile_keys(B, U, j, prefix_tiles);
+            return v;
+        };
+        long long total = 0;
+        for (int s0 = 0; s0 < n_seqs; s0 += 32) {
+            const long long v = scan(s0 + lane < n_seqs ? ends[s0 + lane] : 0) + total;
+            if (s0 + lane < n_seqs) ends[s0 + lane] = v;
+            total = __shfl_sync(0xffffffffu, v, 31);
+        }
+        __syncwarp();
+        W.total = total;
+        W.ctas = paged_tc_ctas(total, gridDim.x);
+        const long long g0 = cta_cut(total, W.ctas, blockIdx.x);
+        W.left = cta_cut(total, W.ctas, blockIdx.x + 1) - g0;
+        if (W.left > 0) {
+            for (int s0 = 0;; s0 += 32) {
+                const unsigned later = __ballot_sync(0xffffffffu, s0 + lane >= n_seqs || ends[s0 + lane] > g0);
+                if (later) {
+                    W.s = s0 + __ffs(later) - 1;
+                    break;
+                }
+            }
+            const int4 S = seqs[W.s];
+            W.r0 = S.x;
+            W.n = S.y;
+            W.len = S.z;
+            long long rest = g0 - (W.s > 0 ? ends[W.s - 1] : 0);
+            const int pairs = (W.n * P.group + PAIR - 1) / PAIR;
+            for (int i0 = 0;; i0 += 32) {
+                const int t = i0 + lane < pairs ? pair_tiles(P, W.n, W.len, i0 + lane) + GAP : 0;
+                const long long v = scan((long long)t * P.n_kv);
+                const unsigned later = __ballot_sync(0xffffffffu, i0 + lane >= pairs || v > rest);
+                if (later) {
+                    const int i = __ffs(later) - 1;
+                    rest -= __shfl_sync(0xffffffffu, v - (long long)t * P.n_kv, i);
+                    W.pair = i0 + i;
+                    W.tiles = __shfl_sync(0xffffffffu, t, i) - GAP;
+                    break;
+                }
+                rest -= __shfl_sync(0xffffffffu, v, 31);
+            }
+            W.h = (int)(rest / (W.tiles + GAP));
+            W.off = (int)(rest - (long long)W.h * (W.tiles + GAP));
+            W.item = g0 - W.off;
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the scratch is the queries' from here on
+    __syncthreads();
+
+    // Steps are counted through all units (gs), units by un.  A warp's look at unit un:
+    const auto look = [&](int un, bool &alive) {
+        alive = warp_wait(bar(BAR_UF + (un & (UNITS - 1))), (un / UNITS) & 1, abort_flag, B.status, P.wait_us);
+        const int4 *u = told + 3 * (un & (UNITS - 1));
+        const int4 a = u[0], b = u[1], c = u[2];
+        __syncwarp();
+        arrive_if(lane == 0 && alive, bar(BAR_UE + (un & (UNITS - 1))));
+        return Unit{a.x, a.y, a.z, a.w, b.x, alive ? b.y : 0, alive ? b.z : 0, b.w, c.x, c.y, c.z, c.w};
+    };
+    if (warp == 0) {
+        // ---------------------------------------------------------------- the walk and the TMA producer: all lanes
+        reg_dealloc<REGS_ISSUE>();
+        bool alive = true;
+        int un = 0;
+        // The next unit is told to the others, and its first tile is this warp's next
+        int j = 0, j_end = 0, uh = 0, us = 0, uown = 0, uq = 0, urows = 0;
+        const auto next_unit = [&]() {
+            Unit U{};
+            while (W.left > 0) {
+                const int all = W.tiles + GAP, take = (int)min((long long)(all - W.off), W.left);
+                U.j0 = W.off;
+                U.nj = min(W.tiles, W.off + take) - W.off;
+                if (U.nj > 0) {
+                    U.r0 = W.r0;
+                    U.p0 = W.pair * PAIR;
+                    U.rows = min(PAIR, W.n * P.group - U.p0);
+                    U.before = W.len - W.n;
+                    U.own = W.len;
+                    U.h = W.h;
+                    U.c0 = blockIdx.x;
+                    U.parts = 1;
+                    if (W.off > 0 || U.nj < W.tiles) {
+                        U.c0 = paged_tc_cta(W.total, W.ctas, W.item);
+                        U.parts = paged_tc_cta(W.total, W.ctas, W.item + W.tiles - 1) - U.c0 + 1;
+                    }
+                    U.part = blockIdx.x - U.c0;
+                    us = W.s;
+                }
+                W.left -= take;
+                W.off += take;
+                if (W.off == all) {                           // the next item
+                    W.off = 0;
+                    W.item += all;
+                    if (++W.h == P.n_kv) {
+                        W.h = 0;
+                        ++W.pair;
+                        if (W.pair * PAIR >= W.n * P.group) {
+                            W.pair = 0;
+                            while (W.left > 0 && ++W.s < B.n_seqs) {
+                                const PagedSeq S = paged_seq(B, W.s);
+                                W.r0 = S.r0;
+                                W.n = S.n;
+                                W.len = S.len;
+                                if (W.n > 0) break;
+                            }
+                            if (W.s >= B.n_seqs) W.left = 0;
+                        }
+                        W.tiles = pair_tiles(P, W.n, W.len, W.pair);
+                    }
+                }
+                if (U.nj > 0) break;
+                U.nj = 0;
+            }
+            if (un >= UNITS) alive = alive && warp_wait(bar(BAR_UE + (un & (UNITS - 1))), (un / UNITS - 1) & 1, abort_flag, B.status, P.wait_us);
+            if (lane == 0 && alive) {
+                int4 *u = told + 3 * (un & (UNITS - 1));
+                u[0] = make_int4(U.r0, U.p0, U.rows, U.before);
+                u[1] = make_int4(U.own, U.j0, U.nj, U.h);
+                u[2] = make_int4(U.c0, U.parts, U.part, 0);
+                mbar_arrive(bar(BAR_UF + (un & (UNITS - 1))));
+            }
+            ++un;
+            j = U.j0;
+            j_end = U.j0 + U.nj;
+            uh = U.h;
+            uown = U.own;
+            uq = U.h * P.head_rows + U.r0 * P.group + U.p0;
+            urows = U.rows;
+            return U.nj > 0;
+        };
+        // Tiles in the order of the steps.  A lane has a page of the tile: lane 8 half + page of the keys' boxes, 16 + 8 half + page of the values', which are at the same place.
+        struct TileRef { int y, n, h, q, rows; };             // row of the lane's page, keys (-1: no tile), KV head; of a unit's first tile: the pair's first query row, its rows
+        const int page_rows = 1 << B.page_shift, pg = lane & 7, half = (lane >> 3) & 1;
+        bool more = true;
+        const auto next = [&]() -> TileRef {
+            const bool first = j == j_end;
+            if (first) more = more && next_unit();
+            if (!more) return {0, -1, 0, 0, 0};
+            const int in = j - prefix_tiles;
+            const int n = min(TILE, in < 0 ? B.n_prefix - j * TILE : max(0, uown - in * TILE));
             int y = 0;
             if (pg * page_rows < n) {
-                const int t = (j < prefix_tiles ? j : j - prefix_tiles) * TILE + pg * page_rows;
-                const int32_t *table = j < prefix_tiles ? B.prefix : B.table + (size_t)U.s * B.max_pages;
+                const int t = (in < 0 ? j : in) * TILE + pg * page_rows;
+                const int32_t *table = in < 0 ? B.prefix : B.table + (size_t)us * B.max_pages;
                 y = paged_page(B, table + (t >> B.page_shift)) << B.page_shift;
             }
             ++j;
-            return {y, n, uh, first, uidx};
+            return {y, n, uh, uq, first ? urows : 0};
         };
-        const int half = (lane >> 3) & 1;
         const auto bytes = [&](int n) { return (uint32_t)(((n + page_rows - 1) >> B.page_shift) << B.page_shift) * 128u * M::HALVES; };
         const auto load = [&](const CUtensorMap *map, uint32_t to, const TileRef &T, uint32_t b) {
             if (half < M::HALVES && pg * page_rows < T.n) tma_load_2d(to + half * HALF_BYTES + pg * page_rows * 128, map, T.h * D + half * 64, T.y, b);
         };
-        TileRef A = next(), C = A.n >= 0 ? next() : A;
-        bool alive = some;
-        int un = 0;
+        TileRef A = next(), C = next();
+        if (A.n >= 0) {
+            if (lane == 0) mbar_expect_tx(bar(BAR_K0), bytes(A.n) + P.extra_tx);
+            __syncwarp();
+            if (lane < 16) load(&map_k, base + M::K, A, bar(BAR_K0));
+        }
+        pc_grid_dep_wait();                                   // the rotated queries are there
+        int queries = 0;                                      // units whose queries have been fetched
         for (int gs = 0; alive && A.n >= 0; ++gs) {
-            TileRef E = C.n >= 0 ? next() : C;               // its page is on the way while this step's copies are issued
-            if (A.first) {                                    // queries of a new unit, once the last products with the old ones have been read
-                const Unit Q = unit_at(P.units, A.unit / P.n_kv);
+            if (A.rows) {                                     // a new unit: once the last products with the old queries have been read
                 for (int t = 0; t < 2 && alive; ++t) {
-                    if (un > 0) alive = warp_wait(bar(BAR_QFREE + t), (un - 1) & 1, abort_flag, B.status, P.wait_us);
+                    if (queries > 0) alive = warp_wait(bar(BAR_QFREE + t), (queries - 1) & 1, abort_flag, B.status, P.wait_us);
                     if (!alive) break;
-                    const bool with_k = un == 0 && t == 0;    // the very first keys ride with the very first queries
-                    if (lane == 0) mbar_expect_tx(bar(BAR_Q + t), M::TILE_B + (with_k ? bytes(A.n) + P.extra_tx : 0u));
+                    if (lane == 0) mbar_expect_tx(bar(BAR_Q + t), M::TILE_B);
                     __syncwarp();
-                    const int y = (int)((long long)A.h * P.head_rows) + Q.q0 + (t * TILE < Q.rows ? t : 0) * TILE;       // a pair of one tile: the same one twice
-                    if (lane < M::HALVES) tma_load_2d(base + M::Q + t * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, y, bar(BAR_Q + t));
-                    if (with_k && lane < 16) load(&map_k, base + M::K, A, bar(BAR_Q));
+                    if (lane < M::HALVES) tma_load_2d(base + M::Q + t * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, A.q + (t * TILE < A.rows ? t : 0) * TILE, bar(BAR_Q + t));     // a pair of one tile: the same one twice
                 }
-                ++un;
-                if (!alive) break;
+                ++queries;
             }
+            const TileRef E = next();                         // its page is on the way while this step's copies are issued
             // PV(step - 2) and QK(step - 1) have read what lies where V(step) and K(step + 1) go
-            if (gs > 0) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
+            if (gs > 0 && alive) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
             if (!alive) break;
             const int st = gs & 1;
             if (lane == 0) mbar_expect_tx(bar(BAR_KV + st), bytes(A.n) + (C.n >= 0 ? bytes(C.n) : 0u));
@@ -369,18 +396,18 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         };
         bool alive = true;
         int gs = 0;
-        for (int k = 0; alive; ++k) {
-            const int idx = unit_of(k, n_units);
-            if (idx < 0) break;
-            const Unit U = unit_at(P.units, idx / P.n_kv);
+        for (int un = 0;; ++un) {
+            const Unit U = look(un, alive);
+            if (U.nj == 0) break;
             if (warp < 3) {
                 const int t = warp - 1;
                 const uint64_t dq0 = desc_kmajor(base + M::Q + t * M::TILE_B), dk0 = desc_kmajor(base + M::K);
-                alive = wait(BAR_Q + t, k & 1);
+                alive = wait(BAR_Q + t, un & 1);
 #pragma unroll 1
                 for (int i = 0; i < U.nj && alive; ++i, ++gs) {
-                    if (gs > 0) alive = wait(BAR_KV + ((gs - 1) & 1), ((gs - 1) >> 1) & 1);
-                    if (alive && gs + t > 0) alive = wait(BAR_SFREE + (t ^ 1), (gs + t + 1) & 1);      // the other tile's scores have left the columns
+                    // the other tile's scores have left the columns (tile 1's first step: so tile 0 has seen the first keys)
+                    alive = gs > 0 ? wait(BAR_KV + ((gs - 1) & 1), ((gs - 1) >> 1) & 1) : (t > 0 || wait(BAR_K0, 0));
+                    if (alive && gs + t > 0) alive = wait(BAR_SFREE + (t ^ 1), (gs + t + 1) & 1);
                     if (!alive) break;
                     uint64_t dq = dq0, dk = dk0 + (gs & 1) * (M::TILE_B >> 4);
 #pragma unroll 1
@@ -397,10 +424,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 const uint64_t dv0 = desc_mnmajor(base + M::V);
 #pragma unroll 1
                 for (int i = 0; i < U.nj && alive; ++i, ++gs) {
-                    const int st = gs & 1;
+                    const int st = gs & 1, in = U.j0 + i - prefix_tiles;
                     alive = wait(BAR_KV + st, (gs >> 1) & 1);
                     if (!alive) break;
-                    const int n = tile_keys(B, U, U.j0 + i, prefix_tiles);
+                    const int n = in < 0 ? B.n_prefix - (U.j0 + i) * TILE : max(0, U.own - in * TILE);
                     if (n < TILE) {                               // values behind the segment's end are whatever the pool holds there
                         for (int hf = 0; hf < M::HALVES; ++hf)
                             for (int c = n * 8 + lane; c < TILE * 8; c += 32) sts128(base + M::V + st * M::TILE_B + hf * HALF_BYTES + c * 16, 0u, 0u, 0u, 0u);
@@ -426,12 +453,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                     }
                 }
             }
+            if (!alive) break;
         }
         // nothing of ours still runs on the tensor core when its memory is freed
         if (lead) tc_commit(bar(BAR_DONE));
         __syncwarp();
         pc_mbar_drain(bar(BAR_DONE), 0, B.status, PC_WHERE_PAGED_WAIT);
-    } else if (some) {
+    } else {
         // ---------------------------------------------------------------- softmax, correction, output
         reg_alloc<REGS_SOFTMAX>();
         const int t = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
@@ -439,25 +467,22 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         const uint32_t s_addr = tmem + lane_addr + TM_S, p_addr = tmem + lane_addr + TM_P + t * (TILE / 2), o_addr = tmem + lane_addr + TM_O + t * TILE;
         const bool lead = elect_one();
         bool alive = true;
-        int k = 0, idx = unit_of(0, n_units), j = 0, lim;
-        Unit U = unit_at(P.units, idx / P.n_kv);
+        int un = 0, j = 0, lim;
+        Unit U = look(0, alive);
         // own tokens that this thread's row sees (one behind the last row sees what the last one sees; its output is dropped)
-        const auto limit = [&]() { return B.causal ? U.before + (U.p0 + min(t * TILE + r, U.rows - 1)) / P.group + 1 : U.own; };
+        const auto limit = [&]() { return B.causal ? min(U.own, U.before + (U.p0 + min(t * TILE + r, U.rows - 1)) / P.group + 1) : U.own; };
         lim = limit();
         float m_used = -INFINITY, l = 0.f;
-        for (int gs = 0; alive; ++gs) {
+        for (int gs = 0; alive && (U.nj > 0 || gs > 0); ++gs) {
             const bool flush = j == U.nj;
             const Unit V = U;                                 // the unit to flush
-            const int v_idx = idx;
             const float m_e = m_used, l_e = l;
             bool end = false;
             if (flush) {
-                idx = unit_of(++k, n_units);
-                end = idx < 0;
-                if (!end) {
-                    U = unit_at(P.units, idx / P.n_kv);
-                    lim = limit();
-                }
+                U = look(++un, alive);
+                if (!alive) break;
+                end = U.nj == 0;
+                lim = limit();
                 j = 0;
                 m_used = -INFINITY;
                 l = 0.f;
@@ -475,10 +500,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 tc_fence_before();
                 __syncwarp();
                 arrive_if(lead, bar(BAR_SFREE + t));
-                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QFREE + t));
+                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QFREE + t));                     // that was the unit's last product with this tile's queries
                 const bool pv_done = gs == 0 || pc_mbar_test(bar(BAR_PVDONE + t), (gs - 1) & 1);
                 const int jt = U.j0 + j;
-                const int seen = jt < prefix_tiles ? B.n_prefix - jt * TILE : min(lim, U.own) - (jt - prefix_tiles) * TILE;
+                const int seen = jt < prefix_tiles ? B.n_prefix - jt * TILE : lim - (jt - prefix_tiles) * TILE;
                 if (__any_sync(0xffffffffu, seen < TILE)) {
 #pragma unroll
                     for (int i = 0; i < TILE; ++i) sv[i] = i < seen ? sv[i] : 0xFF800000u;
@@ -549,110 +574,153 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 tc_fence_after();
             }
             if (__builtin_expect(flush, 0)) {
-                uint32_t v[D];
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
-                tmem_wait_ld();
-                if (!end) {
-                    tc_fence_before();
-                    __syncwarp();
-                    arrive_if(lead, bar(BAR_PHALF + 2 * t));
-                    arrive_if(lead, bar(BAR_PHALF + 2 * t + 1));
-                }
-                const int h = v_idx % P.n_kv, at = t * TILE + r, p = V.p0 + at, i = p / P.group;
+                const int h = V.h, at = t * TILE + r, p = V.p0 + at, i = p / P.group;
                 const bool there = at < V.rows;
                 const size_t row = (size_t)(V.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
                 __nv_bfloat16 *orow = P.out + row * D;
-                if (P.shared) {
-                    const size_t slot = (((size_t)h * tiles_of((int)P.head_rows) + 2 * V.slot + t) * V.parts + V.part) * TILE + r;
-                    if (there) {
-#pragma unroll
-                        for (int c = 0; c < D / 4; ++c) *reinterpret_cast<uint4 *>(P.part_o + slot * D + c * 4) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                        P.part_ml[slot] = make_float2(m_e, l_e);
+                // Places of a CTA in scratch: its last item's (the first part of it), its first item's.  Parts of an item that is added up here lie as 16-byte unit (c, row) at c * 128 + row: a warp's
+                // stores and loads are 512 bytes in a row.
+                const auto slot_of = [&](int part) { return (size_t)(2 * (V.c0 + part) + (part == 0)) * 2 + t; };
+                // The parts in the order of the keys, so the same bits whoever adds them up; this CTA's own from tensor memory (own = its number) or from scratch like the others (own = -1)
+                const auto add_up = [&](int own) {
+                    const auto ml_of = [&](int q) { return q == own ? make_float2(m_e, l_e) : __ldcg(P.part_ml + slot_of(q) * TILE + r); };
+                    float m = -INFINITY, sum = 0.f;
+                    for (int q = 0; q < V.parts; ++q) m = fmaxf(m, ml_of(q).x);
+                    const auto weight = [&](float x) { return m == -INFINITY ? 1.f : fast_exp2(x - m); };
+                    for (int q = 0; q < V.parts; ++q) {
+                        const float2 ml = ml_of(q);
+                        sum = fmaf(ml.y, weight(ml.x), sum);
                     }
-                } else if (V.parts == 1) {
-                    const float inv = l_e > 0.f ? 1.f / l_e : (l_e != l_e ? l_e : 0.f);
-                    if (there) {
-#pragma unroll
-                        for (int c = 0; c < D / 8; ++c) {
-                            uint4 w;
-                            w.x = pc_pack_bf16(__uint_as_float(v[8 * c + 0]) * inv, __uint_as_float(v[8 * c + 1]) * inv);
-                            w.y = pc_pack_bf16(__uint_as_float(v[8 * c + 2]) * inv, __uint_as_float(v[8 * c + 3]) * inv);
-                            w.z = pc_pack_bf16(__uint_as_float(v[8 * c + 4]) * inv, __uint_as_float(v[8 * c + 5]) * inv);
-                            w.w = pc_pack_bf16(__uint_as_float(v[8 * c + 6]) * inv, __uint_as_float(v[8 * c + 7]) * inv);
-                            *reinterpret_cast<uint4 *>(orow + c * 8) = w;
-                        }
-                        if (P.lse) P.lse[row] = (m_e + log2f(l_e)) * 0.6931471805599453f;
-                    }
-                } else {
-                    // Parts lie as 16-byte unit (c, row) at c * 128 + row: a warp's stores and loads are 512 bytes in a row.  The last of a pair's CTAs to come (of their warps with the same rows) adds them up, its
-                    // own among them, by number: the same bits whoever comes last.
-                    const size_t first = ((size_t)V.slot * P.n_kv + (size_t)h * V.parts) * 2 + t;
-                    {
-                        uint4 *po = reinterpret_cast<uint4 *>(P.part_o) + (first + 2 * V.part) * (TILE * D / 4) + r;
-#pragma unroll
-                        for (int c = 0; c < D / 4; ++c) po[c * TILE] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                        P.part_ml[(first + 2 * V.part) * TILE + r] = make_float2(m_e, l_e);
-                    }
-                    __threadfence();
-                    __syncwarp();
-                    int come = 0;                             // every warp for its own 32 rows
-                    if (lane == 0) come = atomicAdd(P.tickets + first * 4 + quad, 1);
-                    come = __shfl_sync(0xffffffffu, come, 0);
-                    if (come == V.parts - 1) {
-                        __threadfence();
-                        float m = -INFINITY, sum = 0.f;
-                        for (int q = 0; q < V.parts; ++q) m = fmaxf(m, __ldcg(P.part_ml + (first + 2 * q) * TILE + r).x);
-                        for (int q = 0; q < V.parts; ++q) {
-                            const float2 ml = __ldcg(P.part_ml + (first + 2 * q) * TILE + r);
-                            sum = fmaf(ml.y, m == -INFINITY ? 1.f : fast_exp2(ml.x - m), sum);
-                        }
-                        const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
+                    const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
 #pragma unroll 1
-                        for (int c0 = 0; c0 < D / 4; c0 += 8) {
-                            float4 a[8];
+                    for (int c0 = 0; c0 < D; c0 += 64) {
+                        float a[64];
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) a[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            for (int q = 0; q < V.parts; ++q) {
-                                const float f = m == -INFINITY ? 1.f : fast_exp2(__ldcg(P.part_ml + (first + 2 * q) * TILE + r).x - m);
-                                const float4 *po = reinterpret_cast<const float4 *>(P.part_o) + (first + 2 * q) * (TILE * D / 4) + r;
+                        for (int c = 0; c < 64; ++c) a[c] = 0.f;
+#pragma unroll 1
+                        for (int q = 0; q < V.parts; ++q) {
+                            const float f = weight(ml_of(q).x);
+                            if (q == own) {
+                                uint32_t y[64];
+                                tmem_ld32(o_addr + c0, y);
+                                tmem_ld32(o_addr + c0 + 32, y + 32);
+                                tmem_wait_ld();
 #pragma unroll
-                                for (int c = 0; c < 8; ++c) {
-                                    const float4 x = __ldcg(po + (c0 + c) * TILE);
-                                    a[c].x = fmaf(x.x, f, a[c].x);
-                                    a[c].y = fmaf(x.y, f, a[c].y);
-                                    a[c].z = fmaf(x.z, f, a[c].z);
-                                    a[c].w = fmaf(x.w, f, a[c].w);
+                                for (int c = 0; c < 64; ++c) a[c] = fmaf(__uint_as_float(y[c]), f, a[c]);
+                            } else {
+                                const float4 *po = reinterpret_cast<const float4 *>(P.part_o) + slot_of(q) * (TILE * D / 4) + r + c0 / 4 * TILE;
+                                float4 x[16];
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) x[c] = __ldcg(po + c * TILE);
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) {
+                                    a[4 * c] = fmaf(x[c].x, f, a[4 * c]);
+                                    a[4 * c + 1] = fmaf(x[c].y, f, a[4 * c + 1]);
+                                    a[4 * c + 2] = fmaf(x[c].z, f, a[4 * c + 2]);
+                                    a[4 * c + 3] = fmaf(x[c].w, f, a[4 * c + 3]);
                                 }
                             }
-                            if (there)
-#pragma unroll
-                                for (int c = 0; c < 8; c += 2)
-                                    *reinterpret_cast<uint4 *>(orow + (c0 + c) * 4) = make_uint4(pc_pack_bf16(a[c].x * inv, a[c].y * inv), pc_pack_bf16(a[c].z * inv, a[c].w * inv),
-                                                                                                 pc_pack_bf16(a[c + 1].x * inv, a[c + 1].y * inv), pc_pack_bf16(a[c + 1].z * inv, a[c + 1].w * inv));
                         }
-                        if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
+                        if (there)
+#pragma unroll
+                            for (int c = 0; c < 64; c += 8)
+                                *reinterpret_cast<uint4 *>(orow + c0 + c) = make_uint4(pc_pack_bf16(a[c] * inv, a[c + 1] * inv), pc_pack_bf16(a[c + 2] * inv, a[c + 3] * inv),
+                                                                                       pc_pack_bf16(a[c + 4] * inv, a[c + 5] * inv), pc_pack_bf16(a[c + 6] * inv, a[c + 7] * inv));
+                    }
+                    if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
+                };
+                uint32_t *ticket = P.sync + SYNC_HEAD + (V.c0 * 2 + t) * 4 + quad;       // every warp for its own 32 rows
+                const uint32_t call = __ldcg(P.sync) << 12;
+                const bool split = !P.shared && V.parts > 1;
+                bool added = false;
+                if (end && split) {                           // the run's last item, whose other parts are mostly there by now: they are added to what lies in tensor memory
+                    uint32_t seen;
+                    asm volatile("ld.acquire.gpu.u32 %0, [%1];" : "=r"(seen) : "l"(ticket) : "memory");
+                    added = __all_sync(0xffffffffu, seen == call + V.parts - 1);
+                    if (added) {
+                        add_up(V.part);
+                        if (lane == 0) *ticket = 0;
+                    }
+                }
+                if (!added) {
+                    uint32_t v[D];
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
+                    tmem_wait_ld();
+                    if (!end) {
+                        tc_fence_before();
+                        __syncwarp();
+                        arrive_if(lead, bar(BAR_PHALF + 2 * t));
+                        arrive_if(lead, bar(BAR_PHALF + 2 * t + 1));
+                    }
+                    if (P.shared) {
+                        const size_t slot = slot_of(V.part) * TILE + r;
+                        float *to = V.parts == 1 ? P.home_o + row * D : P.part_o + slot * D;
+                        if (there) {
+#pragma unroll
+                            for (int c = 0; c < D / 4; ++c) *reinterpret_cast<uint4 *>(to + c * 4) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                            *(V.parts == 1 ? P.home_ml + row : P.part_ml + slot) = make_float2(m_e, l_e);
+                        }
+                    } else if (!split) {
+                        const float inv = l_e > 0.f ? 1.f / l_e : (l_e != l_e ? l_e : 0.f);
+                        if (there) {
+#pragma unroll
+                            for (int c = 0; c < D / 8; ++c) {
+                                uint4 w;
+                                w.x = pc_pack_bf16(__uint_as_float(v[8 * c + 0]) * inv, __uint_as_float(v[8 * c + 1]) * inv);
+                                w.y = pc_pack_bf16(__uint_as_float(v[8 * c + 2]) * inv, __uint_as_float(v[8 * c + 3]) * inv);
+                                w.z = pc_pack_bf16(__uint_as_float(v[8 * c + 4]) * inv, __uint_as_float(v[8 * c + 5]) * inv);
+                                w.w = pc_pack_bf16(__uint_as_float(v[8 * c + 6]) * inv, __uint_as_float(v[8 * c + 7]) * inv);
+                                *reinterpret_cast<uint4 *>(orow + c * 8) = w;
+                            }
+                            if (P.lse) P.lse[row] = (m_e + log2f(l_e)) * 0.6931471805599453f;
+                        }
+                    } else {
+                        uint4 *po = reinterpret_cast<uint4 *>(P.part_o) + slot_of(V.part) * (TILE * D / 4) + r;
+#pragma unroll
+                        for (int c = 0; c < D / 4; ++c) po[c * TILE] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+                        P.part_ml[slot_of(V.part) * TILE + r] = make_float2(m_e, l_e);
+                        __threadfence();
+                        __syncwarp();
+                        // A ticket is worth what this call has put there: one that a call before has left (a wait of it ran out) counts from nothing.
+                        uint32_t come = 0;
+                        if (lane == 0) {
+                            uint32_t seen = __ldcg(ticket);
+                            for (;;) {
+                                const uint32_t want = (seen & ~4095u) == call ? seen + 1 : call + 1, was = atomicCAS(ticket, seen, want);
+                                if (was == seen) {
+                                    come = want & 4095u;
+                                    break;
+                                }
+                                seen = was;
+                            }
+                        }
+                        come = __shfl_sync(0xffffffffu, come, 0);
+                        if (come == (uint32_t)V.parts) {      // the last to come
+                            __threadfence();
+                            add_up(-1);
+                            if (lane == 0) *ticket = 0;
+                        }
                     }
                 }
             }
             if (end) break;
             ++j;
         }
-    } else {
-        reg_alloc<REGS_SOFTMAX>();
     }
     __syncwarp();
     if (*abort_flag) pc_let_copies_land();
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && atomicAdd(P.sync + 1, 1u) == gridDim.x - 1) {        // the last CTA of the call: the next one has another number
+        P.sync[1] = 0;
+        P.sync[0] = (__ldcg(P.sync) + 1) & 0xFFFFFu;
+    }
     if (warp == 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
 }
-
-// Rows as [page x token][KV head x channel], boxes of a page by 64 channels; queries as [KV head x row][channel], boxes of 128 rows
-bool map_rows(CUtensorMap *m, const void *p, uint64_t rows, uint64_t cols, uint32_t box_rows) { return make_map(m, p, rows, cols, box_rows); }
 
 template <int D> pc_status launch_tc(const pc_ctx *ctx, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const TcParams &P, cudaStream_t stream) {
     static bool ready[PC_MAX_DEVICES] = {};
@@ -674,66 +742,44 @@ template <int D> pc_status launch_tc(const pc_ctx *ctx, const CUtensorMap &mq, c
 }  // namespace
 
 bool pc_paged_tc_shape(const pc_ctx *ctx) { return ctx->desc.dtype == PC_BF16; }
-size_t pc_paged_tc_units(const pc_ctx *ctx) { return ((size_t)ctx->desc.max_q * ctx->group + PAIR - 1) / PAIR + PC_MAX_SEQS + (size_t)4 * ctx->sm_count; }
-size_t pc_paged_tc_slots(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count; }
-size_t pc_paged_tc_plan_bytes(const pc_ctx *ctx) { return PLAN_HEAD * sizeof(int) + pc_paged_tc_units(ctx) * sizeof(Unit); }
+size_t pc_paged_tc_tiles(const pc_ctx *ctx) { return (size_t)4 * ctx->sm_count; }
+size_t pc_paged_tc_sync_words(const pc_ctx *ctx) { return SYNC_HEAD + (size_t)8 * ctx->sm_count; }
 
-// Parts of the shared prefix's keys for a call's rows, 0 where the scratch does not hold them
-int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B) {
-    const long long pairs = ((long long)B.n_rows * ctx->group + PAIR - 1) / PAIR, items = pairs * ctx->desc.n_kv_heads;
-    if (items == 0 || items > (long long)pc_paged_tc_slots(ctx)) return 0;
-    return (int)std::max(1LL, std::min<long long>(ctx->sm_count / items, (B.n_prefix + TILE - 1) / TILE));
-}
-
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream) {
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, cudaStream_t stream) {
     const pc_ctx *ctx = A.ctx;
     const pc_layer_desc &D = ctx->desc;
     const long long head_rows = (long long)A.batch.n_rows * ctx->group;
     if (head_rows * D.n_kv_heads > INT32_MAX) return PC_ERR_CAPACITY;
+    // keys and values as [page x token][KV head x channel], boxes of a page by 64 channels; queries as [KV head x row][channel], boxes of 128 rows
     CUtensorMap mq, mk, mv;
     const uint64_t rows = (uint64_t)A.batch.n_pages << A.batch.page_shift, cols = (uint64_t)D.n_kv_heads * D.head_dim;
-    if (!map_rows(&mq, w->q_rot, (uint64_t)head_rows * D.n_kv_heads, D.head_dim, TILE) || !map_rows(&mk, A.pages->k, rows, cols, 1u << A.batch.page_shift) ||
-        !map_rows(&mv, A.pages->v, rows, cols, 1u << A.batch.page_shift)) {
+    if (!make_map(&mq, w->q_rot, (uint64_t)head_rows * D.n_kv_heads, D.head_dim) || !make_map(&mk, A.pages->k, rows, cols, 1u << A.batch.page_shift) ||
+        !make_map(&mv, A.pages->v, rows, cols, 1u << A.batch.page_shift)) {
         fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
         return PC_ERR_CUDA;
     }
-    FrontParams F{};
-    F.B = A.batch;
-    F.q = static_cast<const char *>(A.q);
-    F.q_pos = A.q_pos;
-    F.q_rot = static_cast<char *>(w->q_rot);
-    F.chunks = D.n_q_heads * D.head_dim / 8;
-    F.group = ctx->group;
-    F.n_kv = D.n_kv_heads;
-    F.d = D.head_dim;
-    F.head_rows = head_rows;
-    F.scale = pc_q_rot_scale(D.head_dim);
-    F.shared = prefix_parts > 0;
-    F.shared_parts = prefix_parts;
-    F.sms = ctx->sm_count;
-    F.max_units = (int)pc_paged_tc_units(ctx);
-    F.n_tickets = (int)pc_paged_tc_slots(ctx) * 8;
-    F.tickets = w->tc_tickets;
-    F.head = w->tc_plan;
-    F.units = reinterpret_cast<int4 *>(w->tc_plan + PLAN_HEAD);
-    const long long blocks = 1 + ((long long)A.batch.n_rows * 32 + FRONT_THREADS - 1) / FRONT_THREADS;
-    PC_LAUNCH(k_paged_front, dim3((unsigned)blocks), dim3(FRONT_THREADS), 0, stream, F, ctx->rope);
+    const FrontParams F{A.batch, static_cast<const char *>(A.q), A.q_pos, static_cast<char *>(w->q_rot), D.n_q_heads * D.head_dim / 8, ctx->group, D.n_kv_heads, D.head_dim, head_rows,
+                        pc_q_rot_scale(D.head_dim)};
+    PC_LAUNCH(k_paged_front, dim3((unsigned)(((long long)A.batch.n_rows * 32 + FRONT_THREADS - 1) / FRONT_THREADS)), dim3(FRONT_THREADS), 0, stream, F, ctx->rope);
     TcParams P{};
     P.B = A.batch;
+    P.head_rows = (int)head_rows;
     P.n_q_heads = D.n_q_heads;
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
-    P.shared = prefix_parts > 0;
-    P.head_rows = head_rows;
+    P.shared = shared;
     P.out = static_cast<__nv_bfloat16 *>(A.out);
     P.lse = A.lse;
-    P.units = F.units;
-    P.head = F.head;
     P.part_o = w->tc_o;
     P.part_ml = w->tc_ml;
-    P.tickets = w->tc_tickets;
+    P.home_o = w->home_o + w->home_rows * D.n_q_heads * D.head_dim;          // (the second half: the few-row kernel has the first one for the sequences' own tokens)
+    P.home_ml = w->home_ml + w->home_rows * D.n_q_heads;
+    P.sync = w->tc_sync;
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
-    if (left) *left = PagedTcParts{w->tc_o, w->tc_ml, (int)((head_rows + TILE - 1) / TILE), prefix_parts};
     return D.head_dim == 128 ? launch_tc<128>(ctx, mq, mk, mv, P, stream) : launch_tc<64>(ctx, mq, mk, mv, P, stream);
+}
+
+PagedTcLine pc_paged_tc_line(const pc_paged *w, const pc_paged_args &A) {
+    return PagedTcLine{w->tc_o, w->tc_ml, std::max(1, (A.batch.n_prefix + TILE - 1) / TILE), GAP, A.ctx->sm_count};
 }
