@@ -178,12 +178,10 @@ extern "C" pc_status pc_paged_create(pc_ctx *ctx, pc_paged **out) {
         PC_CUDA_TRY(cudaMalloc(&w->home_ml, home * sizeof(float2)));
         PC_CUDA_TRY(cudaMalloc(&w->plan, (PC_MAX_SEQS + PAGED_PLAN_HEAD) * sizeof(long long)));
         if (pc_paged_tc_shape(ctx)) {
-            const size_t tiles = pc_paged_tc_tiles(ctx), words = pc_paged_tc_sync_words(ctx);
-            const uint32_t first_call = 1;
+            const size_t tiles = 2 * pc_paged_tc_slots(ctx);
             PC_CUDA_TRY(cudaMalloc(&w->q_rot, (size_t)D.max_q * D.n_q_heads * D.head_dim * sizeof(__nv_bfloat16)));
-            PC_CUDA_TRY(cudaMalloc(&w->tc_sync, words * sizeof(uint32_t)));
-            PC_CUDA_TRY(cudaMemset(w->tc_sync, 0, words * sizeof(uint32_t)));
-            PC_CUDA_TRY(cudaMemcpy(w->tc_sync, &first_call, sizeof(first_call), cudaMemcpyHostToDevice));
+            PC_CUDA_TRY(cudaMalloc(&w->tc_plan, pc_paged_tc_plan_bytes(ctx)));
+            PC_CUDA_TRY(cudaMalloc(&w->tc_tickets, tiles * 4 * sizeof(int)));
             PC_CUDA_TRY(cudaMalloc(&w->tc_o, tiles * PAGED_TC_TILE * D.head_dim * sizeof(float)));
             PC_CUDA_TRY(cudaMalloc(&w->tc_ml, tiles * PAGED_TC_TILE * sizeof(float2)));
         }
@@ -206,7 +204,8 @@ extern "C" pc_status pc_paged_destroy(pc_paged *w) {
     cudaFree(w->home_ml);
     cudaFree(w->plan);
     cudaFree(w->q_rot);
-    cudaFree(w->tc_sync);
+    cudaFree(w->tc_plan);
+    cudaFree(w->tc_tickets);
     cudaFree(w->tc_o);
     cudaFree(w->tc_ml);
     delete w;
@@ -234,11 +233,15 @@ extern "C" pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const p
     // sequences share is attended once for all their rows.
     const long long rows = (long long)batch->max_rows * w->ctx->group;
     const bool tc = pc_paged_tc_shape(w->ctx) && w->ctx->attend_impl != 1;
-    if (tc && rows > 64) return pc_launch_paged_tc(w, A, false, stream);
+    if (tc && rows > 64) return pc_launch_paged_tc(w, A, 0, nullptr, stream);
     const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows;
-    if (!tc || !shared || (long long)n_rows * w->ctx->group <= PAGED_FEW_ROWS) return pc_launch_paged_few(w, A, shared, nullptr, stream);
-    const pc_status ps = pc_launch_paged_tc(w, A, true, stream);
-    if (ps != PC_OK) return ps;
-    const PagedTcLine line = pc_paged_tc_line(w, A);
-    return pc_launch_paged_few(w, A, true, &line, stream);
+    PagedTcParts left{};
+    if (tc && shared && (long long)n_rows * w->ctx->group > PAGED_FEW_ROWS) {
+        const int parts = pc_paged_tc_prefix_parts(w->ctx, A.batch);
+        if (parts > 0) {
+            const pc_status ps = pc_launch_paged_tc(w, A, parts, &left, stream);
+            return ps != PC_OK ? ps : pc_launch_paged_few(w, A, true, &left, stream);
+        }
+    }
+    return pc_launch_paged_few(w, A, shared, nullptr, stream);
 }

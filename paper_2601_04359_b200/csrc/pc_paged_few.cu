@@ -629,7 +629,7 @@ constexpr int JOIN_WARPS = 16;
 
 struct JoinParams {
     FewParams F;
-    PagedTcLine T;           // of the tcgen05 kernel, where it has attended the prefix
+    PagedTcParts T;          // what the tcgen05 kernel has left of the prefix
 };
 
 template <int D, bool F32>
@@ -677,15 +677,9 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
                 const long long item = row / P.block * P.n_kv + h;
                 pre = from(worker_of(L, item * L.prefix_len), worker_of(L, (item + 1) * L.prefix_len - 1), (int)(row % P.block), P.home_rows + home);
             } else {
-                // an item is two tiles of rows; its first CTA's part is in that CTA's second place, the others' in their first
-                const int pairs = (int)(((long long)paged_rows(P.B) * P.group + 2 * PAGED_TC_TILE - 1) / (2 * PAGED_TC_TILE)), all = J.T.tiles + J.T.gap;
-                const long long item = row / (2 * PAGED_TC_TILE) * P.n_kv + h, total = (long long)pairs * P.n_kv * all, at = item * all;
-                const int ctas = paged_tc_ctas(total, J.T.ctas), c0 = paged_tc_cta(total, ctas, at), c1 = paged_tc_cta(total, ctas, at + J.T.tiles - 1);
-                if (c0 == c1) pre = From{P.home_o + (P.home_rows + home) * D, P.home_ml + P.home_rows + home, 1, 0, 0};
-                else {
-                    const size_t slot = ((size_t)(2 * c0 + 1) * 2 + (row / PAGED_TC_TILE & 1)) * PAGED_TC_TILE + row % PAGED_TC_TILE;
-                    pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, c1 - c0 + 1, 4 * PAGED_TC_TILE, 2 * PAGED_TC_TILE};
-                }
+                const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
+                const size_t slot = T.first * PAGED_TC_TILE + T.row;
+                pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, J.T.parts, 2 * PAGED_TC_TILE, 0};
             }
         }
 #pragma unroll 4
@@ -770,7 +764,7 @@ static bool few_map(CUtensorMap *m, const void *p, const pc_paged_args &A) {
 
 size_t pc_paged_few_parts(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count * 8 * MAX_ROWS; }
 
-pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcLine *tc, cudaStream_t stream) {
+pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream) {
     const pc_ctx *ctx = A.ctx;
     const pc_layer_desc &D = ctx->desc;
     CUtensorMap mk, mv;

@@ -13,9 +13,9 @@ struct pc_paged {
     float2 *few_ml, *home_ml;
     size_t home_rows;
     long long *plan;
-    // bf16: rotated queries, parts of the tcgen05 kernel and their counters
+    // bf16: rotated queries, units, parts and their counters of the tcgen05 kernel
     void *q_rot;
-    uint32_t *tc_sync;
+    int *tc_plan, *tc_tickets;
     float *tc_o;
     float2 *tc_ml;
 };
@@ -30,22 +30,25 @@ struct pc_paged_args {
     float *lse;
 };
 
-// How the tcgen05 kernel shares out a prefix that all rows of a call see: items (pair of tiles of packed rows, KV head) of `tiles` key tiles and `gap` empty places on a line that `ctas` CTAs share evenly.  An
-// item of one CTA is at home in scratch, row by row; of an item of several the first CTA's part lies in that CTA's second place, the others' in their first, a place being two tiles of rows.
-constexpr int PAGED_TC_LEAST = 4;            // fewest places of a CTA's run
-__device__ __forceinline__ int paged_tc_ctas(long long total, int ctas) { return (int)min((long long)ctas, max(1LL, total / PAGED_TC_LEAST)); }
-__device__ __forceinline__ int paged_tc_cta(long long total, int ctas, long long place) { return (int)(((place + 1) * ctas + total - 1) / total) - 1; }      // the CTA that has a place
-struct PagedTcLine {
+// What the tcgen05 kernel leaves of a shared prefix: its keys in `parts` pieces, for every pair of tiles of packed rows and every KV head; a piece is two tiles of rows of d fp32 values and their (maximum,
+// sum)
+struct PagedTcParts {
     const float *part_o;
     const float2 *part_ml;
-    int tiles, gap, ctas;
+    int parts;
 };
+// first tile of a packed row's pieces (the next one's is two further), and the row in it
+struct PagedTcRow { size_t first; int row; };
+__device__ __forceinline__ PagedTcRow paged_tc_row(const PagedTcParts &T, int n_kv, int h, long long packed_row) {
+    const size_t pair = (size_t)(packed_row / (2 * PAGED_TC_TILE));
+    return {((pair * n_kv + h) * T.parts) * 2 + (size_t)(packed_row / PAGED_TC_TILE & 1), (int)(packed_row % PAGED_TC_TILE)};
+}
 
 size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kernel's scratch
 // shared: the prefix is attended apart from the sequences' own tokens, here or (tc given) by the tcgen05 kernel before
-pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcLine *tc, cudaStream_t stream);
+pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream);
 bool pc_paged_tc_shape(const pc_ctx *ctx);           // whether the tcgen05 kernel takes the context's type
-size_t pc_paged_tc_tiles(const pc_ctx *ctx), pc_paged_tc_sync_words(const pc_ctx *ctx);
-// every sequence over prefix and own tokens, into the output; or (shared) the prefix alone for all rows, into scratch
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, cudaStream_t stream);
-PagedTcLine pc_paged_tc_line(const pc_paged *w, const pc_paged_args &A);
+size_t pc_paged_tc_slots(const pc_ctx *ctx), pc_paged_tc_plan_bytes(const pc_ctx *ctx);
+int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B);
+// prefix_parts 0: every sequence over prefix and own tokens, into the output; otherwise the shared prefix alone, in so many parts, into scratch (left)
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream);

@@ -1,16 +1,19 @@
 // Attention over a paged cache on tcgen05 tensor cores (bf16): prompts, their pieces and frames, and a prefix that many rows share.
 //
-// Two launches.  k_paged_front rotates the queries, with log2(e) / sqrt(d) folded in, into rows of KV head x (token, head of the group): rows that share keys and values lie side by side,
-// so a tile of 128 rows is full whatever the group's size, and a causal tile of G heads spans 128 / G tokens only.
-// k_paged_tc: an item is (sequence, pair of such tiles, KV head); its key tiles lie on one line with those of all other items, which the CTAs (one an SM) share evenly.  Where the line is cut follows from
-// lengths that lie on the device: every CTA adds them up for itself.  An item that several CTAs share is added up by the last of them, in the order of the keys.
-// A CTA: warp 0 walks the line, tells the others of its units by way of a ring of four in shared memory, and fetches by TMA, a lane a page's box (a tile of 128 keys is 1 to 8 pages), two stages of keys and
-// of values; warps 1 and 2 issue S = Q_t K^T of the two query tiles, warp 3 O_t += P_t V; warps 4-7 and 8-11 are the softmax of tile 0 and 1: the score row in registers, running
-// maximum and sum in fp32, probabilities as bf16 into tensor memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame kernel, k_attend_tc.)
+// Two launches.
+//   k_paged_front  rotates the queries, with log2(e) / sqrt(d) folded in, into rows of KV head x (token, head of the group): rows that share keys and values lie side by side, so a tile of 128 rows
+//                  is full whatever the group's size, and a causal tile of G heads spans 128 / G tokens only.  Its first CTA plans the call from the lengths on the device: units (sequence, pair of
+//                  query tiles, run of key tiles), longest first.
+//   k_paged_tc     persistent CTAs take units in snake order (CTA c the c-th, the c-th from the end of the next round, ...): with the longest first that leaves them within about a unit of each
+//                  other.  Pairs with more key tiles than an even share are cut into parts; the last of a pair's CTAs adds the parts up, in the order of the keys.
+// A CTA: warp 0 reads the list, tells the others of its units by way of a ring of four in shared memory, and fetches by TMA, a lane a page's box (a tile of 128 keys is 1 to 8 pages), two stages of keys
+// and of values, query tiles into three places in turn; warps 1 and 2 issue S = Q_t K^T of the two query tiles, warp 3 O_t += P_t V; warps 4-7 and 8-11 are the softmax of tile 0 and 1: the score row
+// in registers, running maximum and sum in fp32, probabilities as bf16 into tensor memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame
+// kernel, k_attend_tc.)
 // Rows behind a segment's end: scores are replaced by -infinity whatever they are, and the values' rows are cleared in shared memory, since 0 times what lies
 // there may be NaN.
-// Tried: queries rotated in this kernel, by four warps more, into three places in turn.  Their chains of shuffles, addresses and products are 1,000 instructions a tile at five to ten cycles, 7 us, where
-// a unit of three key tiles takes 4.6: packed prompts 227 us a call instead of 89.
+// Tried: queries rotated in this kernel, by four warps more.  Their chains of shuffles, addresses and products are 1,000 instructions a tile at five to ten cycles, 7 us, where a unit of three key tiles takes 4.6:
+// packed prompts 227 us a call instead of 89.  And key tiles shared out evenly along one line, with items of two CTAs added up by one of them: 98 us, since every CTA ends with such an item.
 #include <algorithm>
 
 #include "pc_paged_host.cuh"
@@ -25,29 +28,31 @@ constexpr int REGS_LAUNCH = 65536 / TC_THREADS / 8 * 8, REGS_ISSUE = 72, REGS_SO
 static_assert(128 * REGS_ISSUE + 256 * REGS_SOFTMAX <= TC_THREADS * REGS_LAUNCH, "more registers than the block has");
 constexpr float GROW = 8.f;
 constexpr int PAIR = 2 * TILE;                     // packed rows of an item
-constexpr int GAP = 2;                             // what crossing into the next item costs, in key tiles: so many empty places lie behind each item on the line
+constexpr int LEAST_TILES = 4;                     // a part of a pair has as many key tiles at least
 constexpr int UNITS = 4;                           // units that are told ahead
 
-// What a CTA does of an item, and what its warps need to know of that
+// What a unit's warps need to know of it
 struct Unit {
+    int s;                   // sequence; -1: rows of all sequences over the shared prefix
     int r0;                  // the sequence's first row in the batch
     int p0, rows;            // first of the pair's packed rows in the sequence, and how many
     int before, own;         // own tokens before the sequence's rows, and in all
     int j0, nj;              // key tiles: those of the prefix first; nj 0: no more units
-    int h;
-    int c0, parts, part;     // first CTA of the item, CTAs of it, which of them this is
-    int pad;
+    int h;                   // KV head (in the list: none, every unit stands for all heads)
+    int slot;                // place of the pair's first part in scratch, in pairs of tiles of one KV head; KV head and part follow
+    int parts, part;         // of the pair
 };
 static_assert(sizeof(Unit) == 48, "three 16-byte pieces");
+constexpr int PLAN_HEAD = 4;                       // words ahead of the units: their number
 
 template <int D> struct Map {
     static constexpr int HALVES = D / 64, TILE_B = HALVES * HALF_BYTES;
-    static constexpr int Q = 0, K = Q + 2 * TILE_B, V = K + 2 * TILE_B, BAR = V + 2 * TILE_B, FLAGS = BAR + 256, UNIT = FLAGS + 64, ALLOC = UNIT + UNITS * 48 + 1024;
-    static constexpr int SEQS = 0, ENDS = PC_MAX_SEQS * 16;       // while the line is made, where the queries will be: a sequence's numbers, the line's place behind it
-    static_assert(ALLOC <= 232448 && ENDS + PC_MAX_SEQS * 8 <= 2 * TILE_B, "shared memory");
+    static constexpr int Q = 0, K = Q + 3 * TILE_B, V = K + 2 * TILE_B, BAR = V + 2 * TILE_B, FLAGS = BAR + 256, UNIT = FLAGS + 64, ALLOC = UNIT + UNITS * 48 + 1024;
+    static_assert(ALLOC <= 232448, "shared memory");
 };
-enum { BAR_Q = 0 /* [tile] */, BAR_QFREE = 2 /* [tile] */, BAR_K0 = 4, BAR_KV = 5 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 7 /* [step & 1] */, BAR_SFULL = 9 /* [tile] */,
-       BAR_SFREE = 11 /* [tile] */, BAR_PHALF = 13 /* [tile][half] */, BAR_PVDONE = 17 /* [tile] */, BAR_DONE = 19, BAR_UF = 20 /* [unit & 3]: told */, BAR_UE = 24 /* [unit & 3]: taken by all */, N_BARS = 28 };
+enum { BAR_QF = 0 /* [place]: queries are there */, BAR_QE = 3 /* [place]: and have been read */, BAR_K0 = 6, BAR_KV = 7 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 9 /* [step & 1] */,
+       BAR_SFULL = 11 /* [tile] */, BAR_SFREE = 13 /* [tile] */, BAR_PHALF = 15 /* [tile][half] */, BAR_PVDONE = 19 /* [tile] */, BAR_DONE = 21, BAR_UF = 22 /* [unit & 3]: told */,
+       BAR_UE = 26 /* [unit & 3]: taken by all */, N_BARS = 30 };
 static_assert(N_BARS * 8 <= 256, "barriers");
 constexpr int UNIT_READERS = 11;                   // warps 1 to 11
 constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
@@ -59,16 +64,24 @@ struct TcParams {
     int shared;              // the prefix alone, rows of all sequences; what comes out goes to scratch row by row for k_paged_join
     __nv_bfloat16 *out;
     float *lse;
-    float *part_o;           // [2 CTAs][tile][128][D]: a CTA's first and last item
+    const int4 *units;
+    const int *head;
+    float *part_o;           // [slots][tile][128][D]
     float2 *part_ml;
-    float *home_o;           // shared: items of one CTA, [rows][query heads][D]
-    float2 *home_ml;
-    uint32_t *sync;          // [0] number of the call, [1] CTAs that are done, then [CTA][tile][warp] tickets: number of the call and parts that have come
+    int *tickets;            // [slots][tile][warp] parts that have come; zero at first
     uint32_t wait_us, extra_tx;
 };
-constexpr int SYNC_HEAD = 2;
 
-constexpr int FRONT_THREADS = 256;
+__device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
+// The k-th unit of a CTA, -1 behind the last
+__device__ __forceinline__ int unit_of(int k, int n) {
+    const long long i = k & 1 ? (long long)(k + 1) * gridDim.x - 1 - blockIdx.x : (long long)k * gridDim.x + blockIdx.x;
+    return i < n ? (int)i : -1;
+}
+
+// ------------------------------------------------------------------------------------------------ queries and plan
+constexpr int FRONT_THREADS = 512;
+constexpr int LEVELS = 512;
 
 struct FrontParams {
     PagedBatch B;
@@ -78,13 +91,108 @@ struct FrontParams {
     int chunks, group, n_kv, d;
     long long head_rows;
     float scale;
+    int shared, shared_parts, sms, max_units, n_tickets;
+    int4 *units;
+    int *head, *tickets;
 };
 
+__device__ __forceinline__ void put_unit(int4 *units, int i, const Unit &U) {
+    units[3 * i] = make_int4(U.s, U.r0, U.p0, U.rows);
+    units[3 * i + 1] = make_int4(U.before, U.own, U.j0, U.nj);
+    units[3 * i + 2] = make_int4(U.h, U.slot, U.parts, U.part);
+}
+
+// Key tiles of a pair: up to the last key that one of its rows sees, one at least
+__device__ __forceinline__ int pair_tiles(const FrontParams &P, int n, int len, int pair) {
+    const int last = (min((pair + 1) * PAIR, n * P.group) - 1) / P.group;
+    const int sees = P.B.causal ? min(len, max(0, len - n + last + 1)) : len;
+    return max(1, tiles_of(P.B.n_prefix) + tiles_of(sees));
+}
+
+__device__ void plan(const FrontParams &P) {
+    __shared__ int pair0[PC_MAX_SEQS + 1], seq_r0[PC_MAX_SEQS], seq_n[PC_MAX_SEQS], seq_len[PC_MAX_SEQS], level[LEVELS];
+    __shared__ long long sums[32];
+    __shared__ int counts[2];
+    const int tid = threadIdx.x;
+    static_assert(PC_MAX_SEQS <= FRONT_THREADS && LEVELS == FRONT_THREADS, "a thread a sequence, and a level");
+    if (P.shared) {
+        const int packed = paged_rows(P.B) * P.group, tiles = tiles_of(P.B.n_prefix), parts = P.shared_parts, pairs = (packed + PAIR - 1) / PAIR;
+        for (int i = tid; i < pairs * parts; i += FRONT_THREADS) {
+            const int pair = i / parts, part = i - pair * parts;
+            const int j0 = (int)((long long)tiles * part / parts), j1 = (int)((long long)tiles * (part + 1) / parts);
+            put_unit(P.units, i, Unit{-1, 0, pair * PAIR, min(PAIR, packed - pair * PAIR), 0, 0, j0, j1 - j0, 0, pair * parts, parts, part});
+        }
+        if (tid == 0) P.head[0] = pairs * parts;
+        return;
+    }
+    int mine = 0;
+    if (tid < P.B.n_seqs) {
+        const PagedSeq S = paged_seq(P.B, tid);
+        seq_r0[tid] = S.r0;
+        seq_n[tid] = S.n;
+        seq_len[tid] = S.len;
+        mine = (S.n * P.group + PAIR - 1) / PAIR;
+    }
+    level[tid] = 0;
+    for (int i = tid; i < P.n_tickets; i += FRONT_THREADS) P.tickets[i] = 0;
+    if (tid < 2) counts[tid] = 0;
+    const long long end = paged_scan<FRONT_THREADS>((long long)mine, sums);
+    if (tid < P.B.n_seqs) pair0[tid] = (int)end - mine;
+    const int pairs = (int)sums[FRONT_THREADS / 32 - 1];
+    if (tid == 0) pair0[P.B.n_seqs] = pairs;
+    __syncthreads();
+    const auto seq_of = [&](int pair) {
+        int lo = 0, hi = P.B.n_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pair0[mid] <= pair) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    };
+    long long tiles = 0;
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i);
+        tiles += pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]);
+    }
+    paged_scan<FRONT_THREADS>(tiles, sums);
+    tiles = sums[FRONT_THREADS / 32 - 1];
+    // An even share of all key tiles; a pair with more than a quarter above it is cut, into parts that are over 5/9 of a share each: fewer than two an SM, which the scratch holds.
+    const int share = (int)min((long long)INT32_MAX / 2, max((long long)LEAST_TILES, (tiles * P.n_kv + P.sms - 1) / P.sms));
+    const auto parts_of = [&](int t) { return t <= share + share / 4 ? 1 : (t + share - 1) / share; };
+    const auto level_of = [&](int size) { return LEVELS - 1 - min(size, LEVELS - 1); };
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i), t = pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]), parts = parts_of(t);
+        atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
+    }
+    __syncthreads();
+    const int n_level = level[tid];
+    __syncthreads();
+    const long long upto = paged_scan<FRONT_THREADS>((long long)n_level, sums);
+    level[tid] = (int)upto - n_level;
+    if (tid == 0) P.head[0] = min((int)sums[FRONT_THREADS / 32 - 1], P.max_units);
+    __syncthreads();
+    for (int i = tid; i < pairs; i += FRONT_THREADS) {
+        const int s = seq_of(i), pair = i - pair0[s], n = seq_n[s], len = seq_len[s], t = pair_tiles(P, n, len, pair);
+        const int parts = parts_of(t);
+        const int at = atomicAdd(&level[level_of((t + parts - 1) / parts)], parts);
+        const int slot = parts > 1 ? atomicAdd(&counts[0], parts) : 0;
+        for (int part = 0; part < parts; ++part) {
+            const int j0 = (int)((long long)t * part / parts), j1 = (int)((long long)t * (part + 1) / parts);
+            if (at + part < P.max_units)                      // (row ranges that overlap can make more units than there are rows for)
+                put_unit(P.units, at + part, Unit{s, seq_r0[s], pair * PAIR, min(PAIR, n * P.group - pair * PAIR), len - n, len, j0, j1 - j0, 0, slot, parts, part});
+        }
+    }
+}
+
 __global__ void __launch_bounds__(FRONT_THREADS) k_paged_front(const __grid_constant__ FrontParams P, const __grid_constant__ pc_rope_dev rope) {
+    pc_grid_dep_launch();
     pc_grid_dep_wait();
-    pc_grid_dep_launch();              // behind the wait: what came before is complete when the attention kernel starts, which looks at lengths and tables ahead of its own
+    if (blockIdx.x == 0) {
+        plan(P);
+        return;
+    }
     // a warp a row of the batch, lane's chunks of eight channels 32 apart: all at one place of a head
-    const int lane = threadIdx.x & 31, row = (int)((blockIdx.x * FRONT_THREADS + threadIdx.x) >> 5);
+    const int lane = threadIdx.x & 31, row = (int)(((blockIdx.x - 1) * FRONT_THREADS + threadIdx.x) >> 5);
     if (row >= paged_rows(P.B)) return;
     const int4 pos = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + row);
     const char *q = P.q + (size_t)row * P.chunks * 16;
@@ -121,22 +229,105 @@ __global__ void __launch_bounds__(FRONT_THREADS) k_paged_front(const __grid_cons
     if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
 }
 
-__device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
-// Key tiles of a pair: up to the last key that one of its rows sees, one at least
-__device__ __forceinline__ int pair_tiles(const TcParams &P, int n, int len, int pair) {
-    if (P.shared) return max(1, tiles_of(P.B.n_prefix));
-    const int last = (min((pair + 1) * PAIR, n * P.group) - 1) / P.group;
-    const int sees = P.B.causal ? min(len, max(0, len - n + last + 1)) : len;
-    return max(1, tiles_of(P.B.n_prefix) + tiles_of(sees));
-}
-__device__ __forceinline__ long long cta_cut(long long total, int ctas, int c) { return total * min(c, ctas) / ctas; }
-
+// ------------------------------------------------------------------------------------------------ attention
 __device__ __forceinline__ void arrive_if(bool who, uint32_t bar) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((uint32_t)who) : "memory");
 }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status, uint32_t limit_us) {
     if (__builtin_expect(__all_sync(0xffffffffu, pc_mbar_try(bar, parity)), 1)) return true;
     return __all_sync(0xffffffffu, pc_mbar_wait(bar, parity, abort_flag, status, PC_WHERE_PAGED_WAIT, limit_us));
+}
+
+// 32 bytes of a lane at once: a warp's store to 32 rows takes a request for every row, whatever it stores there
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+template <int WORDS> __device__ __forceinline__ void store_words(void *to, const uint32_t (&w)[WORDS]) {
+#pragma unroll
+    for (int n = 0; n < WORDS; n += 8) store32(static_cast<char *>(to) + n * 4, reinterpret_cast<const uint32_t (&)[8]>(w[n]));
+}
+// D fp32 values of a row, times inv, as bf16
+template <int D> __device__ __forceinline__ void store_bf16(__nv_bfloat16 *to, const uint32_t *v, float inv) {
+    uint32_t w[D / 2];
+#pragma unroll
+    for (int e = 0; e < D / 2; ++e) w[e] = pc_pack_bf16(__uint_as_float(v[2 * e]) * inv, __uint_as_float(v[2 * e + 1]) * inv);
+    store_words(to, w);
+}
+
+// ---- where things of a unit are.  Parts that are added up here lie as 16-byte unit (c, row) at c * 128 + row: a warp's stores and loads are 512 bytes in a row; the shared prefix's row by row.
+__device__ __forceinline__ size_t slot_of(const TcParams &P, const Unit &U, int part, int t) { return ((size_t)U.slot * P.n_kv + U.h * U.parts + part) * 2 + t; }
+__device__ __forceinline__ size_t row_of(const TcParams &P, const Unit &U, int at) {
+    const int p = U.p0 + at, i = p / P.group;
+    return (size_t)(U.r0 + i) * P.n_q_heads + U.h * P.group + (p - i * P.group);
+}
+
+// The parts of an item from scratch, in the order of the keys, so the same bits whoever adds them up.  Out of line: it is rare, and its registers would be the loop's.
+template <int D> __device__ __noinline__ void add_up(const TcParams &P, Unit U, int t, int r) {
+    const auto ml_of = [&](int q) { return __ldcg(P.part_ml + slot_of(P, U, q, t) * TILE + r); };
+    float m = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int q = 0; q < U.parts; ++q) m = fmaxf(m, ml_of(q).x);
+    const auto weight = [&](float x) { return m == -INFINITY ? 1.f : fast_exp2(x - m); };
+#pragma unroll 4
+    for (int q = 0; q < U.parts; ++q) {
+        const float2 ml = ml_of(q);
+        sum = fmaf(ml.y, weight(ml.x), sum);
+    }
+    const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
+    const size_t row = row_of(P, U, t * TILE + r);
+    const bool there = t * TILE + r < U.rows;
+#pragma unroll 1
+    for (int c0 = 0; c0 < D; c0 += 64) {
+        float a[64];
+#pragma unroll
+        for (int c = 0; c < 64; ++c) a[c] = 0.f;
+#pragma unroll 1
+        for (int q = 0; q < U.parts; ++q) {
+            const float f = weight(ml_of(q).x);
+            const float4 *po = reinterpret_cast<const float4 *>(P.part_o) + slot_of(P, U, q, t) * (TILE * D / 4) + r + c0 / 4 * TILE;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+                const float4 x = __ldcg(po + c * TILE);
+                a[4 * c] = fmaf(x.x, f, a[4 * c]);
+                a[4 * c + 1] = fmaf(x.y, f, a[4 * c + 1]);
+                a[4 * c + 2] = fmaf(x.z, f, a[4 * c + 2]);
+                a[4 * c + 3] = fmaf(x.w, f, a[4 * c + 3]);
+            }
+        }
+        if (there) store_bf16<64>(P.out + row * D + c0, reinterpret_cast<const uint32_t *>(a), inv);
+    }
+    if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
+}
+
+// A thread's row of a unit (v: D fp32 values, not yet divided by their sum) leaves: whole items to the output, parts to scratch, and the last part to come adds them up
+template <int D> __device__ __forceinline__ void put_out(const TcParams &P, const Unit &U, const uint32_t (&v)[D], float m, float l, int t, int quad, int lane) {
+    const int r = quad * 32 + lane;
+    const bool there = t * TILE + r < U.rows;
+    const size_t row = row_of(P, U, t * TILE + r);
+    if (P.shared) {
+        const size_t slot = slot_of(P, U, U.part, t) * TILE + r;
+        if (there) {
+            store_words(P.part_o + slot * D, v);
+            P.part_ml[slot] = make_float2(m, l);
+        }
+    } else if (U.parts == 1) {
+        if (there) store_bf16<D>(P.out + row * D, v, l > 0.f ? 1.f / l : (l != l ? l : 0.f));       // nothing seen: 0
+        if (there && P.lse) P.lse[row] = (m + log2f(l)) * 0.6931471805599453f;
+    } else {
+        uint4 *po = reinterpret_cast<uint4 *>(P.part_o) + slot_of(P, U, U.part, t) * (TILE * D / 4) + r;
+#pragma unroll
+        for (int c = 0; c < D / 4; ++c) po[c * TILE] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        P.part_ml[slot_of(P, U, U.part, t) * TILE + r] = make_float2(m, l);
+        __threadfence();
+        __syncwarp();
+        int come = 0;                                         // every warp for its own 32 rows
+        if (lane == 0) come = atomicAdd(P.tickets + slot_of(P, U, 0, t) * 4 + quad, 1);
+        come = __shfl_sync(0xffffffffu, come, 0);
+        if (come == U.parts - 1) {                            // the last to come
+            __threadfence();
+            add_up<D>(P, U, t, r);
+        }
+    }
 }
 
 template <int D>
@@ -156,7 +347,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < N_BARS; ++i) {
-            const bool by_warps = (i >= BAR_QFREE && i < BAR_K0) || (i >= BAR_EMPTY && i < BAR_SFULL) || (i >= BAR_SFREE && i < BAR_PVDONE);        // of the four of one tile's softmax
+            const bool by_warps = (i >= BAR_QE && i < BAR_K0) || (i >= BAR_EMPTY && i < BAR_SFULL) || (i >= BAR_SFREE && i < BAR_PVDONE);        // of the four of one tile's softmax
             mbar_init(bar(i), by_warps ? 4 : (i == BAR_DONE ? 3 : (i >= BAR_UE ? UNIT_READERS : 1)));
         }
         *abort_flag = 0;
@@ -170,85 +361,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     const PagedBatch &B = P.B;
     const int prefix_tiles = tiles_of(B.n_prefix);
 
-    // ---- the line (of what was there before the rotation began, so ahead of the wait for that): every sequence's places, then where this CTA's run begins
-    int4 *seqs = reinterpret_cast<int4 *>(gen + M::SEQS);
-    long long *ends = reinterpret_cast<long long *>(gen + M::ENDS);
-    const int n_seqs = P.shared ? 1 : B.n_seqs;
-    for (int s = threadIdx.x; s < n_seqs; s += TC_THREADS) {
-        PagedSeq S = {0, 0, 0};
-        if (P.shared) S.n = paged_rows(B); else S = paged_seq(B, s);
-        seqs[s] = make_int4(S.r0, S.n, S.len, 0);
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    for (int s = warp; s < n_seqs; s += TC_THREADS / 32) {
-        const int4 S = seqs[s];
-        const int pairs = (S.y * P.group + PAIR - 1) / PAIR;
-        long long v = 0;
-        for (int i = lane; i < pairs; i += 32) v += pair_tiles(P, S.y, S.z, i) + GAP;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) ends[s] = v * P.n_kv;
-    }
-    __syncthreads();
-    // warp 0's walk: sequence, pair, KV head, places of the item that lie behind; places left of the run
-    struct { int s, r0, n, len, pair, h, off, tiles, ctas; long long left, item, total; } W{};
-    if (warp == 0) {
-        const auto scan = [&](long long v) {
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long u = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v += u;
-            }
-            return v;
-        };
-        long long total = 0;
-        for (int s0 = 0; s0 < n_seqs; s0 += 32) {
-            const long long v = scan(s0 + lane < n_seqs ? ends[s0 + lane] : 0) + total;
-            if (s0 + lane < n_seqs) ends[s0 + lane] = v;
-            total = __shfl_sync(0xffffffffu, v, 31);
-        }
-        __syncwarp();
-        W.total = total;
-        W.ctas = paged_tc_ctas(total, gridDim.x);
-        const long long g0 = cta_cut(total, W.ctas, blockIdx.x);
-        W.left = cta_cut(total, W.ctas, blockIdx.x + 1) - g0;
-        if (W.left > 0) {
-            for (int s0 = 0;; s0 += 32) {
-                const unsigned later = __ballot_sync(0xffffffffu, s0 + lane >= n_seqs || ends[s0 + lane] > g0);
-                if (later) {
-                    W.s = s0 + __ffs(later) - 1;
-                    break;
-                }
-            }
-            const int4 S = seqs[W.s];
-            W.r0 = S.x;
-            W.n = S.y;
-            W.len = S.z;
-            long long rest = g0 - (W.s > 0 ? ends[W.s - 1] : 0);
-            const int pairs = (W.n * P.group + PAIR - 1) / PAIR;
-            for (int i0 = 0;; i0 += 32) {
-                const int t = i0 + lane < pairs ? pair_tiles(P, W.n, W.len, i0 + lane) + GAP : 0;
-                const long long v = scan((long long)t * P.n_kv);
-                const unsigned later = __ballot_sync(0xffffffffu, i0 + lane >= pairs || v > rest);
-                if (later) {
-                    const int i = __ffs(later) - 1;
-                    rest -= __shfl_sync(0xffffffffu, v - (long long)t * P.n_kv, i);
-                    W.pair = i0 + i;
-                    W.tiles = __shfl_sync(0xffffffffu, t, i) - GAP;
-                    break;
-                }
-                rest -= __shfl_sync(0xffffffffu, v, 31);
-            }
-            W.h = (int)(rest / (W.tiles + GAP));
-            W.off = (int)(rest - (long long)W.h * (W.tiles + GAP));
-            W.item = g0 - W.off;
-        }
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // the scratch is the queries' from here on
-    __syncthreads();
+    if (warp == 0) pc_grid_dep_wait();                        // warp 0 alone reads what the launch before has left: the units, and by TMA the queries
 
     // Steps are counted through all units (gs), units by un.  A warp's look at unit un:
     const auto look = [&](int un, bool &alive) {
@@ -257,78 +374,42 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         const int4 a = u[0], b = u[1], c = u[2];
         __syncwarp();
         arrive_if(lane == 0 && alive, bar(BAR_UE + (un & (UNITS - 1))));
-        return Unit{a.x, a.y, a.z, a.w, b.x, alive ? b.y : 0, alive ? b.z : 0, b.w, c.x, c.y, c.z, c.w};
+        return Unit{a.x, a.y, a.z, a.w, b.x, b.y, b.z, alive ? b.w : 0, c.x, c.y, c.z, c.w};
     };
     if (warp == 0) {
         // ---------------------------------------------------------------- the walk and the TMA producer: all lanes
         reg_dealloc<REGS_ISSUE>();
         bool alive = true;
         int un = 0;
-        // The next unit is told to the others, and its first tile is this warp's next
+        // The next unit of the list is told to the others, and its first tile is this warp's next
         int j = 0, j_end = 0, uh = 0, us = 0, uown = 0, uq = 0, urows = 0;
+        const int n_units = __ldcg(P.head) * P.n_kv;          // a unit of the list times the KV heads, heads side by side
         const auto next_unit = [&]() {
-            Unit U{};
-            while (W.left > 0) {
-                const int all = W.tiles + GAP, take = (int)min((long long)(all - W.off), W.left);
-                U.j0 = W.off;
-                U.nj = min(W.tiles, W.off + take) - W.off;
-                if (U.nj > 0) {
-                    U.r0 = W.r0;
-                    U.p0 = W.pair * PAIR;
-                    U.rows = min(PAIR, W.n * P.group - U.p0);
-                    U.before = W.len - W.n;
-                    U.own = W.len;
-                    U.h = W.h;
-                    U.c0 = blockIdx.x;
-                    U.parts = 1;
-                    if (W.off > 0 || U.nj < W.tiles) {
-                        U.c0 = paged_tc_cta(W.total, W.ctas, W.item);
-                        U.parts = paged_tc_cta(W.total, W.ctas, W.item + W.tiles - 1) - U.c0 + 1;
-                    }
-                    U.part = blockIdx.x - U.c0;
-                    us = W.s;
-                }
-                W.left -= take;
-                W.off += take;
-                if (W.off == all) {                           // the next item
-                    W.off = 0;
-                    W.item += all;
-                    if (++W.h == P.n_kv) {
-                        W.h = 0;
-                        ++W.pair;
-                        if (W.pair * PAIR >= W.n * P.group) {
-                            W.pair = 0;
-                            while (W.left > 0 && ++W.s < B.n_seqs) {
-                                const PagedSeq S = paged_seq(B, W.s);
-                                W.r0 = S.r0;
-                                W.n = S.n;
-                                W.len = S.len;
-                                if (W.n > 0) break;
-                            }
-                            if (W.s >= B.n_seqs) W.left = 0;
-                        }
-                        W.tiles = pair_tiles(P, W.n, W.len, W.pair);
-                    }
-                }
-                if (U.nj > 0) break;
-                U.nj = 0;
+            const int idx = unit_of(un, n_units), i = max(idx, 0) / P.n_kv;
+            int4 a = make_int4(0, 0, 0, 0), b = a, c = a;
+            if (idx >= 0) {
+                a = __ldcg(P.units + 3 * i);
+                b = __ldcg(P.units + 3 * i + 1);
+                c = __ldcg(P.units + 3 * i + 2);
+                c.x = idx - i * P.n_kv;
             }
             if (un >= UNITS) alive = alive && warp_wait(bar(BAR_UE + (un & (UNITS - 1))), (un / UNITS - 1) & 1, abort_flag, B.status, P.wait_us);
             if (lane == 0 && alive) {
                 int4 *u = told + 3 * (un & (UNITS - 1));
-                u[0] = make_int4(U.r0, U.p0, U.rows, U.before);
-                u[1] = make_int4(U.own, U.j0, U.nj, U.h);
-                u[2] = make_int4(U.c0, U.parts, U.part, 0);
+                u[0] = a;
+                u[1] = b;
+                u[2] = c;
                 mbar_arrive(bar(BAR_UF + (un & (UNITS - 1))));
             }
             ++un;
-            j = U.j0;
-            j_end = U.j0 + U.nj;
-            uh = U.h;
-            uown = U.own;
-            uq = U.h * P.head_rows + U.r0 * P.group + U.p0;
-            urows = U.rows;
-            return U.nj > 0;
+            us = a.x;
+            uown = b.y;
+            j = b.z;
+            j_end = b.z + b.w;
+            uh = c.x;
+            uq = c.x * P.head_rows + a.y * P.group + a.z;
+            urows = a.w;
+            return b.w > 0;
         };
         // Tiles in the order of the steps.  A lane has a page of the tile: lane 8 half + page of the keys' boxes, 16 + 8 half + page of the values', which are at the same place.
         struct TileRef { int y, n, h, q, rows; };             // row of the lane's page, keys (-1: no tile), KV head; of a unit's first tile: the pair's first query row, its rows
@@ -359,20 +440,34 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             __syncwarp();
             if (lane < 16) load(&map_k, base + M::K, A, bar(BAR_K0));
         }
-        pc_grid_dep_wait();                                   // the rotated queries are there
-        int queries = 0;                                      // units whose queries have been fetched
+        // Query tiles (two a unit) go to three places in turn, tile n where tile n - 3 was.  A unit's first tile is fetched two steps ahead of it, its second one once the unit before it has
+        // no more use for its first.
+        int fetched = 0;
+        const auto fetch_queries = [&](const TileRef &T, int t) {
+            const int place = fetched % 3;
+            if (fetched >= 3) alive = alive && warp_wait(bar(BAR_QE + place), (fetched / 3 - 1) & 1, abort_flag, B.status, P.wait_us);
+            if (!alive) return;
+            if (lane == 0) mbar_expect_tx(bar(BAR_QF + place), M::TILE_B);
+            __syncwarp();
+            if (lane < M::HALVES) tma_load_2d(base + M::Q + place * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, T.q + (t * TILE < T.rows ? t : 0) * TILE, bar(BAR_QF + place));    // a pair of one tile: the same one twice
+            ++fetched;
+        };
+        if (A.n >= 0) {
+            fetch_queries(A, 0);
+            fetch_queries(A, 1);
+        }
+        const auto begins = [](const TileRef &T) { return T.n >= 0 && T.rows > 0; };
+        bool c_waits = begins(C);                             // the first query tile of the unit that begins with C is still to be fetched
         for (int gs = 0; alive && A.n >= 0; ++gs) {
-            if (A.rows) {                                     // a new unit: once the last products with the old queries have been read
-                for (int t = 0; t < 2 && alive; ++t) {
-                    if (queries > 0) alive = warp_wait(bar(BAR_QFREE + t), (queries - 1) & 1, abort_flag, B.status, P.wait_us);
-                    if (!alive) break;
-                    if (lane == 0) mbar_expect_tx(bar(BAR_Q + t), M::TILE_B);
-                    __syncwarp();
-                    if (lane < M::HALVES) tma_load_2d(base + M::Q + t * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, A.q + (t * TILE < A.rows ? t : 0) * TILE, bar(BAR_Q + t));     // a pair of one tile: the same one twice
-                }
-                ++queries;
-            }
             const TileRef E = next();                         // its page is on the way while this step's copies are issued
+            if (gs > 0 && begins(A)) fetch_queries(A, 1);
+            if (c_waits) fetch_queries(C, 0);
+            bool e_waits = begins(E);
+            if (e_waits && !begins(C)) {                      // (a unit that begins with C has its second tile first)
+                fetch_queries(E, 0);
+                e_waits = false;
+            }
+            if (!alive) break;
             // PV(step - 2) and QK(step - 1) have read what lies where V(step) and K(step + 1) go
             if (gs > 0 && alive) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
             if (!alive) break;
@@ -383,6 +478,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             else if (C.n >= 0) load(&map_k, base + M::K + (st ^ 1) * M::TILE_B, C, bar(BAR_KV + st));
             A = C;
             C = E;
+            c_waits = e_waits;
         }
     } else if (warp < 4) {
         // ---------------------------------------------------------------- warps 1 and 2: S = Q_t K^T; warp 3: O += P V.  All lanes wait, one issues.
@@ -400,9 +496,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             const Unit U = look(un, alive);
             if (U.nj == 0) break;
             if (warp < 3) {
-                const int t = warp - 1;
-                const uint64_t dq0 = desc_kmajor(base + M::Q + t * M::TILE_B), dk0 = desc_kmajor(base + M::K);
-                alive = wait(BAR_Q + t, un & 1);
+                const int t = warp - 1, tile = 2 * un + t, place = tile % 3;
+                const uint64_t dq0 = desc_kmajor(base + M::Q + place * M::TILE_B), dk0 = desc_kmajor(base + M::K);
+                alive = wait(BAR_QF + place, (tile / 3) & 1);
 #pragma unroll 1
                 for (int i = 0; i < U.nj && alive; ++i, ++gs) {
                     // the other tile's scores have left the columns (tile 1's first step: so tile 0 has seen the first keys)
@@ -473,21 +569,24 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         const auto limit = [&]() { return B.causal ? min(U.own, U.before + (U.p0 + min(t * TILE + r, U.rows - 1)) / P.group + 1) : U.own; };
         lim = limit();
         float m_used = -INFINITY, l = 0.f;
-        for (int gs = 0; alive && (U.nj > 0 || gs > 0); ++gs) {
+        int gs = 0;
+        for (; alive && U.nj > 0; ++gs) {
             const bool flush = j == U.nj;
             const Unit V = U;                                 // the unit to flush
             const float m_e = m_used, l_e = l;
-            bool end = false;
             if (flush) {
                 U = look(++un, alive);
                 if (!alive) break;
-                end = U.nj == 0;
+                if (U.nj == 0) {                              // that was the last one: it leaves behind the loop
+                    U = V;
+                    break;
+                }
                 lim = limit();
                 j = 0;
                 m_used = -INFINITY;
                 l = 0.f;
             }
-            if (!end) {
+            {
                 alive = warp_wait(bar(BAR_SFULL + t), gs & 1, abort_flag, B.status, P.wait_us);
                 if (!alive) break;
                 tc_fence_after();
@@ -500,7 +599,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 tc_fence_before();
                 __syncwarp();
                 arrive_if(lead, bar(BAR_SFREE + t));
-                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QFREE + t));                     // that was the unit's last product with this tile's queries
+                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QE + (2 * un + t) % 3));         // that was the unit's last product with this tile's queries
                 const bool pv_done = gs == 0 || pc_mbar_test(bar(BAR_PVDONE + t), (gs - 1) & 1);
                 const int jt = U.j0 + j;
                 const int seen = jt < prefix_tiles ? B.n_prefix - jt * TILE : lim - (jt - prefix_tiles) * TILE;
@@ -568,154 +667,36 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                     }
                 }
                 l += (la.x + la.y) + (lb.x + lb.y);
-            } else {
-                alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
-                if (!alive) break;
-                tc_fence_after();
             }
             if (__builtin_expect(flush, 0)) {
-                const int h = V.h, at = t * TILE + r, p = V.p0 + at, i = p / P.group;
-                const bool there = at < V.rows;
-                const size_t row = (size_t)(V.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
-                __nv_bfloat16 *orow = P.out + row * D;
-                // Places of a CTA in scratch: its last item's (the first part of it), its first item's.  Parts of an item that is added up here lie as 16-byte unit (c, row) at c * 128 + row: a warp's
-                // stores and loads are 512 bytes in a row.
-                const auto slot_of = [&](int part) { return (size_t)(2 * (V.c0 + part) + (part == 0)) * 2 + t; };
-                // The parts in the order of the keys, so the same bits whoever adds them up; this CTA's own from tensor memory (own = its number) or from scratch like the others (own = -1)
-                const auto add_up = [&](int own) {
-                    const auto ml_of = [&](int q) { return q == own ? make_float2(m_e, l_e) : __ldcg(P.part_ml + slot_of(q) * TILE + r); };
-                    float m = -INFINITY, sum = 0.f;
-                    for (int q = 0; q < V.parts; ++q) m = fmaxf(m, ml_of(q).x);
-                    const auto weight = [&](float x) { return m == -INFINITY ? 1.f : fast_exp2(x - m); };
-                    for (int q = 0; q < V.parts; ++q) {
-                        const float2 ml = ml_of(q);
-                        sum = fmaf(ml.y, weight(ml.x), sum);
-                    }
-                    const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
-#pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 64) {
-                        float a[64];
+                uint32_t v[D];
 #pragma unroll
-                        for (int c = 0; c < 64; ++c) a[c] = 0.f;
-#pragma unroll 1
-                        for (int q = 0; q < V.parts; ++q) {
-                            const float f = weight(ml_of(q).x);
-                            if (q == own) {
-                                uint32_t y[64];
-                                tmem_ld32(o_addr + c0, y);
-                                tmem_ld32(o_addr + c0 + 32, y + 32);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int c = 0; c < 64; ++c) a[c] = fmaf(__uint_as_float(y[c]), f, a[c]);
-                            } else {
-                                const float4 *po = reinterpret_cast<const float4 *>(P.part_o) + slot_of(q) * (TILE * D / 4) + r + c0 / 4 * TILE;
-                                float4 x[16];
-#pragma unroll
-                                for (int c = 0; c < 16; ++c) x[c] = __ldcg(po + c * TILE);
-#pragma unroll
-                                for (int c = 0; c < 16; ++c) {
-                                    a[4 * c] = fmaf(x[c].x, f, a[4 * c]);
-                                    a[4 * c + 1] = fmaf(x[c].y, f, a[4 * c + 1]);
-                                    a[4 * c + 2] = fmaf(x[c].z, f, a[4 * c + 2]);
-                                    a[4 * c + 3] = fmaf(x[c].w, f, a[4 * c + 3]);
-                                }
-                            }
-                        }
-                        if (there)
-#pragma unroll
-                            for (int c = 0; c < 64; c += 8)
-                                *reinterpret_cast<uint4 *>(orow + c0 + c) = make_uint4(pc_pack_bf16(a[c] * inv, a[c + 1] * inv), pc_pack_bf16(a[c + 2] * inv, a[c + 3] * inv),
-                                                                                       pc_pack_bf16(a[c + 4] * inv, a[c + 5] * inv), pc_pack_bf16(a[c + 6] * inv, a[c + 7] * inv));
-                    }
-                    if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
-                };
-                uint32_t *ticket = P.sync + SYNC_HEAD + (V.c0 * 2 + t) * 4 + quad;       // every warp for its own 32 rows
-                const uint32_t call = __ldcg(P.sync) << 12;
-                const bool split = !P.shared && V.parts > 1;
-                bool added = false;
-                if (end && split) {                           // the run's last item, whose other parts are mostly there by now: they are added to what lies in tensor memory
-                    uint32_t seen;
-                    asm volatile("ld.acquire.gpu.u32 %0, [%1];" : "=r"(seen) : "l"(ticket) : "memory");
-                    added = __all_sync(0xffffffffu, seen == call + V.parts - 1);
-                    if (added) {
-                        add_up(V.part);
-                        if (lane == 0) *ticket = 0;
-                    }
-                }
-                if (!added) {
-                    uint32_t v[D];
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
-                    tmem_wait_ld();
-                    if (!end) {
-                        tc_fence_before();
-                        __syncwarp();
-                        arrive_if(lead, bar(BAR_PHALF + 2 * t));
-                        arrive_if(lead, bar(BAR_PHALF + 2 * t + 1));
-                    }
-                    if (P.shared) {
-                        const size_t slot = slot_of(V.part) * TILE + r;
-                        float *to = V.parts == 1 ? P.home_o + row * D : P.part_o + slot * D;
-                        if (there) {
-#pragma unroll
-                            for (int c = 0; c < D / 4; ++c) *reinterpret_cast<uint4 *>(to + c * 4) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                            *(V.parts == 1 ? P.home_ml + row : P.part_ml + slot) = make_float2(m_e, l_e);
-                        }
-                    } else if (!split) {
-                        const float inv = l_e > 0.f ? 1.f / l_e : (l_e != l_e ? l_e : 0.f);
-                        if (there) {
-#pragma unroll
-                            for (int c = 0; c < D / 8; ++c) {
-                                uint4 w;
-                                w.x = pc_pack_bf16(__uint_as_float(v[8 * c + 0]) * inv, __uint_as_float(v[8 * c + 1]) * inv);
-                                w.y = pc_pack_bf16(__uint_as_float(v[8 * c + 2]) * inv, __uint_as_float(v[8 * c + 3]) * inv);
-                                w.z = pc_pack_bf16(__uint_as_float(v[8 * c + 4]) * inv, __uint_as_float(v[8 * c + 5]) * inv);
-                                w.w = pc_pack_bf16(__uint_as_float(v[8 * c + 6]) * inv, __uint_as_float(v[8 * c + 7]) * inv);
-                                *reinterpret_cast<uint4 *>(orow + c * 8) = w;
-                            }
-                            if (P.lse) P.lse[row] = (m_e + log2f(l_e)) * 0.6931471805599453f;
-                        }
-                    } else {
-                        uint4 *po = reinterpret_cast<uint4 *>(P.part_o) + slot_of(V.part) * (TILE * D / 4) + r;
-#pragma unroll
-                        for (int c = 0; c < D / 4; ++c) po[c * TILE] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-                        P.part_ml[slot_of(V.part) * TILE + r] = make_float2(m_e, l_e);
-                        __threadfence();
-                        __syncwarp();
-                        // A ticket is worth what this call has put there: one that a call before has left (a wait of it ran out) counts from nothing.
-                        uint32_t come = 0;
-                        if (lane == 0) {
-                            uint32_t seen = __ldcg(ticket);
-                            for (;;) {
-                                const uint32_t want = (seen & ~4095u) == call ? seen + 1 : call + 1, was = atomicCAS(ticket, seen, want);
-                                if (was == seen) {
-                                    come = want & 4095u;
-                                    break;
-                                }
-                                seen = was;
-                            }
-                        }
-                        come = __shfl_sync(0xffffffffu, come, 0);
-                        if (come == (uint32_t)V.parts) {      // the last to come
-                            __threadfence();
-                            add_up(-1);
-                            if (lane == 0) *ticket = 0;
-                        }
-                    }
-                }
+                for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
+                tmem_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                arrive_if(lead, bar(BAR_PHALF + 2 * t));
+                arrive_if(lead, bar(BAR_PHALF + 2 * t + 1));
+                put_out<D>(P, V, v, m_e, l_e, t, quad, lane);
             }
-            if (end) break;
             ++j;
+        }
+        if (alive && U.nj > 0) {                              // the last unit
+            alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
+            if (alive) {
+                tc_fence_after();
+                uint32_t v[D];
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
+                tmem_wait_ld();
+                put_out<D>(P, U, v, m_used, l, t, quad, lane);
+            }
         }
     }
     __syncwarp();
     if (*abort_flag) pc_let_copies_land();
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && atomicAdd(P.sync + 1, 1u) == gridDim.x - 1) {        // the last CTA of the call: the next one has another number
-        P.sync[1] = 0;
-        P.sync[0] = (__ldcg(P.sync) + 1) & 0xFFFFFu;
-    }
     if (warp == 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -742,44 +723,66 @@ template <int D> pc_status launch_tc(const pc_ctx *ctx, const CUtensorMap &mq, c
 }  // namespace
 
 bool pc_paged_tc_shape(const pc_ctx *ctx) { return ctx->desc.dtype == PC_BF16; }
-size_t pc_paged_tc_tiles(const pc_ctx *ctx) { return (size_t)4 * ctx->sm_count; }
-size_t pc_paged_tc_sync_words(const pc_ctx *ctx) { return SYNC_HEAD + (size_t)8 * ctx->sm_count; }
+size_t pc_paged_tc_units(const pc_ctx *ctx) { return ((size_t)ctx->desc.max_q * ctx->group + PAIR - 1) / PAIR + PC_MAX_SEQS + (size_t)4 * ctx->sm_count; }
+size_t pc_paged_tc_slots(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count; }
+size_t pc_paged_tc_plan_bytes(const pc_ctx *ctx) { return PLAN_HEAD * sizeof(int) + pc_paged_tc_units(ctx) * sizeof(Unit); }
 
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, cudaStream_t stream) {
+// Parts of the shared prefix's keys for a call's rows, 0 where the scratch does not hold them
+int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B) {
+    const long long pairs = ((long long)B.n_rows * ctx->group + PAIR - 1) / PAIR, items = pairs * ctx->desc.n_kv_heads;
+    if (items == 0 || items > (long long)pc_paged_tc_slots(ctx)) return 0;
+    return (int)std::max(1LL, std::min<long long>(ctx->sm_count / items, (B.n_prefix + TILE - 1) / TILE));
+}
+
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream) {
     const pc_ctx *ctx = A.ctx;
     const pc_layer_desc &D = ctx->desc;
     const long long head_rows = (long long)A.batch.n_rows * ctx->group;
     if (head_rows * D.n_kv_heads > INT32_MAX) return PC_ERR_CAPACITY;
-    // keys and values as [page x token][KV head x channel], boxes of a page by 64 channels; queries as [KV head x row][channel], boxes of 128 rows
     CUtensorMap mq, mk, mv;
     const uint64_t rows = (uint64_t)A.batch.n_pages << A.batch.page_shift, cols = (uint64_t)D.n_kv_heads * D.head_dim;
-    if (!make_map(&mq, w->q_rot, (uint64_t)head_rows * D.n_kv_heads, D.head_dim) || !make_map(&mk, A.pages->k, rows, cols, 1u << A.batch.page_shift) ||
+    if (!make_map(&mq, w->q_rot, (uint64_t)head_rows * D.n_kv_heads, D.head_dim, TILE) || !make_map(&mk, A.pages->k, rows, cols, 1u << A.batch.page_shift) ||
         !make_map(&mv, A.pages->v, rows, cols, 1u << A.batch.page_shift)) {
         fprintf(stderr, "packcache: cuTensorMapEncodeTiled failed\n");
         return PC_ERR_CUDA;
     }
-    const FrontParams F{A.batch, static_cast<const char *>(A.q), A.q_pos, static_cast<char *>(w->q_rot), D.n_q_heads * D.head_dim / 8, ctx->group, D.n_kv_heads, D.head_dim, head_rows,
-                        pc_q_rot_scale(D.head_dim)};
-    PC_LAUNCH(k_paged_front, dim3((unsigned)(((long long)A.batch.n_rows * 32 + FRONT_THREADS - 1) / FRONT_THREADS)), dim3(FRONT_THREADS), 0, stream, F, ctx->rope);
+    FrontParams F{};
+    F.B = A.batch;
+    F.q = static_cast<const char *>(A.q);
+    F.q_pos = A.q_pos;
+    F.q_rot = static_cast<char *>(w->q_rot);
+    F.chunks = D.n_q_heads * D.head_dim / 8;
+    F.group = ctx->group;
+    F.n_kv = D.n_kv_heads;
+    F.d = D.head_dim;
+    F.head_rows = head_rows;
+    F.scale = pc_q_rot_scale(D.head_dim);
+    F.shared = prefix_parts > 0;
+    F.shared_parts = prefix_parts;
+    F.sms = ctx->sm_count;
+    F.max_units = (int)pc_paged_tc_units(ctx);
+    F.n_tickets = (int)pc_paged_tc_slots(ctx) * 8;
+    F.tickets = w->tc_tickets;
+    F.head = w->tc_plan;
+    F.units = reinterpret_cast<int4 *>(w->tc_plan + PLAN_HEAD);
+    const long long blocks = 1 + ((long long)A.batch.n_rows * 32 + FRONT_THREADS - 1) / FRONT_THREADS;
+    PC_LAUNCH(k_paged_front, dim3((unsigned)blocks), dim3(FRONT_THREADS), 0, stream, F, ctx->rope);
     TcParams P{};
     P.B = A.batch;
-    P.head_rows = (int)head_rows;
     P.n_q_heads = D.n_q_heads;
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
-    P.shared = shared;
+    P.shared = prefix_parts > 0;
+    P.head_rows = (int)head_rows;
     P.out = static_cast<__nv_bfloat16 *>(A.out);
     P.lse = A.lse;
+    P.units = F.units;
+    P.head = F.head;
     P.part_o = w->tc_o;
     P.part_ml = w->tc_ml;
-    P.home_o = w->home_o + w->home_rows * D.n_q_heads * D.head_dim;          // (the second half: the few-row kernel has the first one for the sequences' own tokens)
-    P.home_ml = w->home_ml + w->home_rows * D.n_q_heads;
-    P.sync = w->tc_sync;
+    P.tickets = w->tc_tickets;
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
+    if (left) *left = PagedTcParts{w->tc_o, w->tc_ml, prefix_parts};
     return D.head_dim == 128 ? launch_tc<128>(ctx, mq, mk, mv, P, stream) : launch_tc<64>(ctx, mq, mk, mv, P, stream);
-}
-
-PagedTcLine pc_paged_tc_line(const pc_paged *w, const pc_paged_args &A) {
-    return PagedTcLine{w->tc_o, w->tc_ml, std::max(1, (A.batch.n_prefix + TILE - 1) / TILE), GAP, A.ctx->sm_count};
 }
