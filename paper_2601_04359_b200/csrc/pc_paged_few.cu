@@ -5,9 +5,10 @@
 //
 // Keys and values are read once a block of query rows, so with few rows the kernel is bound by memory: scores are taken transposed, S^T = K Q^T, a step of 16 keys by 8
 // packed rows (token-major, the heads of a group side by side), so that one token of three to eight heads fills an instruction, and O^T = V^T P^T the same way.
-// A work item is (run of rows, KV head, block of 8 or 16 packed rows); its steps of 16 keys lie on one line with those of all other items, which the warps of the
-// GPU share evenly.  A warp fetches its own steps by TMA into its own ring (a page holds a whole number of steps, so a step is two boxes of 16 rows a 64 channels) and meets no
-// other warp: an item that several warps share leaves (maximum, sum, output) of each in scratch, and k_paged_join adds them up in the order of the keys.
+// A work item is (run of rows, block of 8 or 16 packed rows); its steps of 16 keys lie on one line with those of all other items.  The line is shared out evenly among groups of as many warps as there are
+// KV heads, a warp a head: a group's warps read the same tokens at the same time, whose rows lie side by side (with the heads one after the other on the line, each at its own place of a
+// sequence, 549 MB of 128 sequences came at 4.3 TB/s).  A warp fetches its own steps by TMA into its own ring (a page holds a whole number of steps, so a step is two boxes of 16 rows a 64 channels)
+// and meets no other warp: an item that several groups share leaves (maximum, sum, output) of each in scratch, and k_paged_join adds them up in the order of the keys.
 // The line follows from lengths that lie on the device: every CTA adds them up for itself.
 #include <algorithm>
 
@@ -21,6 +22,7 @@ constexpr int STEP = 16;                                 // keys of a step
 constexpr int BOX_BYTES = STEP * 128;
 constexpr float GROW = 8.f;                              // a row's reference moves once a score is 2^8 beyond it
 constexpr int MAX_ROWS = PAGED_FEW_ROWS;                 // most packed rows of a block
+constexpr int GAP = 4;                                   // what an item costs besides its steps, in steps: so many empty places lie behind each on the line
 
 template <int D, bool F32> struct Form {
     static constexpr int CH = F32 ? 32 : 64;             // channels of a box (128 bytes)
@@ -103,12 +105,13 @@ struct FewParams {
     int shared;              // the prefix is attended apart from the sequences' own tokens, and k_paged_join adds the two up
     int prefix_here;         // ... in this kernel
     int block;               // packed rows of a block
-    int workers, least;      // warps of the grid; fewest steps of one
+    int groups, least;       // groups of warps; fewest steps of one
+    const void *pool_v;
     float scale;
     void *out;
     float *lse;
-    float *part_o;           // [2 workers][MAX_ROWS][D]: a warp's first and last item
-    float2 *part_ml;         // [2 workers][MAX_ROWS]
+    float *part_o;           // [2 groups][KV heads][MAX_ROWS][D]: a warp's first and last item
+    float2 *part_ml;
     float *home_o;           // [2][rows][query heads][D]: items that one warp has done (own, prefix)
     float2 *home_ml;
     size_t home_rows;        // rows x query heads of one of the two
@@ -116,10 +119,10 @@ struct FewParams {
     uint32_t wait_us, extra_tx;
 };
 
-// The line.  Places 0 .. prefix_end - 1 are the prefix items' (block-major), then come the sequences, KV head by KV head.
-// Where warps are plenty (at least two an item) an item's length on the line is its steps made up to a multiple of `unit`, and a warp takes one unit: part of one item.  Otherwise
-// `unit` is 1 and warps take runs of even length, which go from item to item.
-struct Line { long long total, prefix_end, per; int prefix_len, workers, rest, unit; };
+// The line.  Places 0 .. prefix_end - 1 are the prefix items', then come the sequences'.
+// Where groups are plenty (at least two an item) an item's length on the line is its steps made up to a multiple of `unit`, and a group takes one unit: part of one item.  Otherwise
+// `unit` is 1, a gap lies behind each item, and groups take runs of even length, which go from item to item.
+struct Line { long long total, prefix_end, per; int prefix_len, groups, rest, unit; };
 static_assert(sizeof(Line) <= PAGED_PLAN_HEAD * 8, "the plan's head");
 
 // (kept out of line: the code of a call of a few steps is fetched as it runs, and its length is what such a call waits for)
@@ -127,16 +130,16 @@ __device__ __noinline__ long long divide(long long a, int b) { return ((a | b) >
 
 __device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
 __device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (rows * group + block - 1) / block; }      // block: 8 or 16
-__device__ __forceinline__ int made_up(int len, int unit) { return unit == 1 ? len : (len + unit - 1) / unit * unit; }
+__device__ __forceinline__ int made_up(int len, int unit) { return unit == 1 ? len + GAP : (len + unit - 1) / unit * unit; }
 __device__ __forceinline__ int item_steps(const FewParams &P, int own) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(own)); }
 __device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block) : 0; }
-// first place of warp w; the warp that has a place
-__device__ __forceinline__ long long cut(const Line &L, int w) { return L.per * w + (L.rest ? (uint32_t)(L.rest * w) / (uint32_t)L.workers : 0u); }
-__device__ __forceinline__ int worker_of(const Line &L, long long place) {
+// first place of a group; the group that has a place
+__device__ __forceinline__ long long cut(const Line &L, int w) { return L.per * w + (L.rest ? (uint32_t)(L.rest * w) / (uint32_t)L.groups : 0u); }
+__device__ __forceinline__ int group_of(const Line &L, long long place) {
     if (L.rest == 0) return (int)divide(place, (int)min(L.per, (long long)INT32_MAX));
-    int w = min(L.workers - 1, (int)((double)place * L.workers / (double)L.total));
+    int w = min(L.groups - 1, (int)((double)place * L.groups / (double)L.total));
     while (w > 0 && cut(L, w) > place) --w;
-    while (w + 1 < L.workers && cut(L, w + 1) <= place) ++w;
+    while (w + 1 < L.groups && cut(L, w + 1) <= place) ++w;
     return w;
 }
 // Blocks of a sequence's rows from both ends in turn: where attention is causal, two neighbours on the line have as much to do as any other two.
@@ -155,6 +158,24 @@ template <int D, bool F32> struct Warp {
     int lane, done;          // steps it has taken so far
     bool alive;
 };
+
+// Infinite and NaN values that the products of steps max(j0, first) .. j1 - 1 left out, added to a row that sees `own` of its sequence's own tokens.  They are looked for in the pool: this is rare.
+template <int D, bool F32> __device__ __noinline__ void add_odd(const FewParams &P, const Item &I, int j0, int j1, int first, int own, float (&x)[D / 32]) {
+    constexpr int E = D / 32;
+    const int lane = threadIdx.x & 31, prefix = I.s < 0 || !P.shared ? P.B.n_prefix : 0, prefix_steps = steps_of(prefix);
+    for (int j = max(j0, first); j < j1; ++j) {
+        const bool in_prefix = j < prefix_steps;
+        const int t = (in_prefix ? j : j - prefix_steps) * STEP, n = min(STEP, (in_prefix ? prefix : own) - t);
+        const int page = paged_page(P.B, (in_prefix ? P.B.prefix : P.B.table + (size_t)I.s * P.B.max_pages) + (t >> P.B.page_shift));
+        const size_t row = ((size_t)page << P.B.page_shift) + (t & ((1 << P.B.page_shift) - 1));
+        for (int key = 0; key < n; ++key)
+            for (int e = 0; e < E; ++e) {
+                const size_t at = ((row + key) * P.n_kv + I.h) * D + lane * E + e;
+                const float v = F32 ? __ldcg(static_cast<const float *>(P.pool_v) + at) : __bfloat162float(static_cast<const __nv_bfloat16 *>(P.pool_v)[at]);
+                if (F32 ? !(fabsf(v) <= 3.3e38f) : !(fabsf(v) < INFINITY)) x[e] += v;
+            }
+    }
+}
 
 // One item's steps j0 .. j1 - 1, in NB blocks of 8 packed rows; what comes out goes to the output (direct), or to o and ml, there where the output would have it (whole) or
 // row by row.  CHECK: rows of a block may see different keys.
@@ -279,6 +300,7 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
         }
     }
 
+    bool odd_seen = false;
     float acc[CB][NB][4], m[NB][2], l[NB][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -383,14 +405,15 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             }
         }
         // ---- O^T += V^T P^T.  Values of keys that no row of the block sees are taken as zero whatever lies there.  Where some rows see a key and others do not, an infinite
-        // or NaN value would reach all of them (0 times it is NaN): it is taken out of the product and added to those that see it.  (fp32's parts cannot hold one, so there always.)
+        // or NaN value would reach all of them (0 times it is NaN): it is taken out of the product here
+        // and added at the end to those that see it.  (fp32's parts cannot hold one, so there always.)
         const uint32_t keep0 = (quad * 2 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 1 < nv_most ? 0xFFFF0000u : 0u);
         const uint32_t keep1 = (quad * 2 + 8 < nv_most ? 0xFFFFu : 0u) | (quad * 2 + 9 < nv_most ? 0xFFFF0000u : 0u);
         const bool check = F32 || (CHECK && nv_fewest < nv_most);
+        bool odd = false;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             uint32_t a[PARTS][4];
-            bool odd = false;
             if constexpr (F32) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -426,33 +449,14 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) mma_parts<PARTS>(acc[cb][nb], a, pb[nb]);
-            if (check && __any_sync(0xffffffffu, odd)) {
-#pragma unroll 1
-                for (int key = 0; key < nv_most; ++key)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        float v;
-                        if constexpr (F32) {
-                            const int c = (cb & 1) * 16 + u * 8 + eighth;
-                            v = lds32(vs + (cb >> 1) * BOX_BYTES + key * 128 + (((c >> 2) ^ (key & 7)) << 4) + (c & 3) * 4);
-                        } else {
-                            const uint32_t w = __float_as_uint(lds32(vs + (cb >> 2) * BOX_BYTES + key * 128 + ((((cb & 3) * 2 + u) ^ (key & 7)) << 4) + (eighth >> 1) * 4));
-                            v = eighth & 1 ? pc_bf16_hi(w) : pc_bf16_lo(w);
-                        }
-                        if (fabsf(v) <= 3.3e38f || (!F32 && fabsf(v) < INFINITY)) continue;
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                if (!CHECK || in_prefix || key < lim[nb][e] - key0) acc[cb][nb][2 * u + e] += v;
-                    }
-            }
         }
+        odd_seen |= odd;
         __syncwarp();
         ++W.done;
         if (j + F::STAGES < j1) fetch(j + F::STAGES);
     }
 
+    if constexpr (F32 || CHECK) odd_seen = __any_sync(0xffffffffu, odd_seen);
     // ---- out, by way of the ring (nothing is in flight): row p0 + r at r D floats, channel c at c ^ 8 (r / 2 % 4)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -484,6 +488,8 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             x[e] = y.x * inv;
             x[e + 1] = y.y * inv;
         }
+        if constexpr (F32 || CHECK)
+            if (odd_seen) add_odd<D, F32>(P, I, j0, j1, F32 ? 0 : prefix_steps + (fewest & ~(STEP - 1)) / STEP, I.s < 0 ? 0 : sees(p), x);
         float *row = (F32 && direct ? static_cast<float *>(P.out) : o) + to * D + lane * E;
         if (!F32 && direct) {
             __nv_bfloat16 *b = static_cast<__nv_bfloat16 *>(P.out) + to * D + lane * E;
@@ -537,27 +543,25 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     };
     Line L;
     {
-        const int pitems = prefix_blocks(P) * P.n_kv, psteps = max(1, steps_of(P.B.n_prefix));
-        long long steps = 0, items = 0;
+        const int pitems = prefix_blocks(P), psteps = max(1, steps_of(P.B.n_prefix));
+        long long both = 0;                                // steps, and items in the lower 24 bits
 #pragma unroll 1
         for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) {
             const PagedSeq S = paged_seq(P.B, s);
-            const int n = blocks_of(S.n, P.group, 8 * NB) * P.n_kv;
-            items += n;
-            steps += (long long)n * item_steps(P, S.len);
+            const int n = blocks_of(S.n, P.group, 8 * NB);
+            both += ((long long)n * item_steps(P, S.len) << 24) + n;
             if constexpr (F::INFO) {
                 info[3 * s] = S.r0;
                 info[3 * s + 1] = S.n;
                 info[3 * s + 2] = S.len;
             }
         }
-        paged_scan<THREADS>(steps, sums);
-        steps = sums[F::WARPS - 1] + (long long)pitems * psteps;
+        paged_scan<THREADS>(both, sums);
+        both = sums[F::WARPS - 1];
+        const int items = (int)(both & 0xFFFFFF) + pitems;
+        const long long steps = (both >> 24) + (long long)pitems * psteps;
         __syncthreads();
-        paged_scan<THREADS>(items, sums);
-        items = sums[F::WARPS - 1] + pitems;
-        __syncthreads();
-        const int spare = items * 2 <= P.workers ? P.workers - (int)items : 0;
+        const int spare = items * 2 <= P.groups ? P.groups - items : 0;
         L.unit = spare ? max(P.least, (int)divide(steps + spare - 1, spare)) : 1;
         L.prefix_len = made_up(psteps, L.unit);
         L.prefix_end = (long long)pitems * L.prefix_len;
@@ -568,7 +572,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             long long v = 0;
             if (s < P.B.n_seqs) {
                 const PagedSeq S = seq_of(s);
-                v = (long long)blocks_of(S.n, P.group, 8 * NB) * P.n_kv * made_up(item_steps(P, S.len), L.unit);
+                v = (long long)blocks_of(S.n, P.group, 8 * NB) * made_up(item_steps(P, S.len), L.unit);
             }
             const long long end = paged_scan<THREADS>(v, sums);
             if (s < P.B.n_seqs) plan[s] = at + end - v;
@@ -576,9 +580,9 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             __syncthreads();
         }
         L.total = at;
-        L.workers = spare ? (int)divide(at, L.unit) : (int)min((long long)P.workers, divide(at + P.least - 1, P.least));
-        L.per = divide(at, max(1, L.workers));
-        L.rest = (int)(at - L.per * L.workers);
+        L.groups = spare ? (int)divide(at, L.unit) : (int)min((long long)P.groups, divide(at + P.least - 1, P.least));
+        L.per = divide(at, max(1, L.groups));
+        L.rest = (int)(at - L.per * L.groups);
     }
     __syncthreads();
     if (blockIdx.x == 0) {
@@ -586,19 +590,20 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) P.plan[PAGED_PLAN_HEAD + s] = plan[s];
     }
 
-    // ---- this warp's part of it; neighbours on the line are on different SMs
-    const int w = warp * gridDim.x + blockIdx.x;
-    if (w >= L.workers) return;
-    long long g = cut(L, w);
-    const long long g1 = cut(L, w + 1);
+    // ---- this warp's part of it
+    const int w = blockIdx.x * F::WARPS + warp, group = w / P.n_kv, h = w - group * P.n_kv;
+    if (group >= L.groups) return;
+    long long g = cut(L, group);
+    const long long g1 = cut(L, group + 1);
 #pragma unroll 1
     while (g < g1 && W.alive) {
         Item I;
-        int off;
+        int off, all;                                      // place in the item, places of it
         if (g < L.prefix_end) {
             const int item = (int)divide(g, L.prefix_len);
+            all = L.prefix_len;
             off = (int)(g - (long long)item * L.prefix_len);
-            I = {0, paged_rows(P.B), -1, item % P.n_kv, item / P.n_kv, L.prefix_len, 0, 0};
+            I = {0, paged_rows(P.B), -1, h, item, max(1, steps_of(P.B.n_prefix)), 0, 0};
         } else {
             int lo = 0, hi = P.B.n_seqs - 1;               // the last sequence that begins at or before g (one without rows has no places)
 #pragma unroll 1
@@ -607,17 +612,20 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
                 if (plan[mid] <= g) lo = mid; else hi = mid - 1;
             }
             const PagedSeq S = seq_of(lo);
-            const int len = made_up(item_steps(P, S.len), L.unit), blocks = blocks_of(S.n, P.group, 8 * NB);
-            const long long y = g - plan[lo], item = divide(y, len), h = divide(item, blocks);
-            off = (int)(y - item * len);
-            I = {S.r0, S.n, lo, (int)h, zigzag((int)(item - h * blocks), blocks), len, S.len, S.len - S.n};
+            const int len = item_steps(P, S.len), blocks = blocks_of(S.n, P.group, 8 * NB);
+            all = made_up(len, L.unit);
+            const long long y = g - plan[lo], item = divide(y, all);
+            off = (int)(y - item * all);
+            I = {S.r0, S.n, lo, h, zigzag((int)item, blocks), len, S.len, S.len - S.n};
         }
-        const int take = (int)min((long long)(I.len - off), g1 - g);
-        const bool whole = off == 0 && take == I.len, home = whole && P.shared;
-        float *o = home ? P.home_o + (I.s < 0 ? P.home_rows * D : 0) : P.part_o + (size_t)(2 * w + (off == 0)) * MAX_ROWS * D;
-        float2 *ml = home ? P.home_ml + (I.s < 0 ? P.home_rows : 0) : P.part_ml + (size_t)(2 * w + (off == 0)) * MAX_ROWS;
-        take_unit<D, F32, NB, CHECK>(P, rope, &map_k, &map_v, W, abort_flag, I, off, off + take, whole && !P.shared, o, ml, whole);
+        const int take = (int)min((long long)(all - off), g1 - g), end = min(I.len, off + take);
         g += take;
+        if (off >= end) continue;                          // empty places
+        const bool whole = off == 0 && end == I.len, home = whole && P.shared;
+        const size_t slot = ((size_t)(2 * group + (off == 0)) * P.n_kv + h) * MAX_ROWS;
+        float *o = home ? P.home_o + (I.s < 0 ? P.home_rows * D : 0) : P.part_o + slot * D;
+        float2 *ml = home ? P.home_ml + (I.s < 0 ? P.home_rows : 0) : P.part_ml + slot;
+        take_unit<D, F32, NB, CHECK>(P, rope, &map_k, &map_v, W, abort_flag, I, off, end, whole && !P.shared, o, ml, whole);
     }
     if (!W.alive) pc_let_copies_land();
 }
@@ -654,28 +662,28 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block);
     if (k >= blocks) return;
     const int block = zigzag(k, blocks), p0 = block * P.block, n = min(P.block, packed - p0);
-    const int len = made_up(item_steps(P, S.len), L.unit);
-    const long long first = place + ((long long)h * blocks + k) * len;
-    const int w0 = worker_of(L, first), w1 = worker_of(L, first + len - 1);
+    const int len = item_steps(P, S.len);
+    const long long first = place + (long long)k * made_up(len, L.unit);
+    const int w0 = group_of(L, first), w1 = group_of(L, first + len - 1);
     if (!P.shared && w0 == w1) return;                     // its warp has written the output
     const int sets = JOIN_WARPS / n, r = warp % n, set = warp / n;
     float o[E] = {}, M = -INFINITY, l = 0.f;
     if (set < sets) {
         const int p = p0 + r, i = p / P.group;
         const size_t home = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
-        // Parts, own ones first: of this kernel's warps, each its last item for the first one and its first for the others; or of one warp at home; or the tcgen05 kernel's
+        // Parts, own ones first: of the groups, each its last item for the first one and its first for the others; or of one group at home; or the tcgen05 kernel's
         struct From { const float *o; const float2 *ml; int parts; size_t pitch, later; } own{}, pre{};
         const auto from = [&](int v0, int v1, int row, size_t home_at) {
             if (v0 == v1) return From{P.home_o + home_at * D, P.home_ml + home_at, 1, 0, 0};
-            const size_t slot = (size_t)(2 * v0 + 1) * MAX_ROWS + row;
-            return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * MAX_ROWS, MAX_ROWS};
+            const size_t step = (size_t)P.n_kv * MAX_ROWS, slot = ((size_t)(2 * v0 + 1) * P.n_kv + h) * MAX_ROWS + row;
+            return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * step, step};
         };
         own = from(w0, w1, r, home);
         if (P.shared && P.B.n_prefix > 0) {
             const long long row = (long long)S.r0 * P.group + p;          // packed row of the batch
             if (P.prefix_here) {
-                const long long item = row / P.block * P.n_kv + h;
-                pre = from(worker_of(L, item * L.prefix_len), worker_of(L, (item + 1) * L.prefix_len - 1), (int)(row % P.block), P.home_rows + home);
+                const long long at = row / P.block * L.prefix_len;
+                pre = from(group_of(L, at), group_of(L, at + max(1, steps_of(P.B.n_prefix)) - 1), (int)(row % P.block), P.home_rows + home);
             } else {
                 const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
                 const size_t slot = T.first * PAGED_TC_TILE + T.row;
@@ -736,7 +744,7 @@ template <int D, bool F32, int NB, bool CHECK> pc_status launch(const CUtensorMa
         attr_set[ctx->device] = true;
     }
     JoinParams j = J;
-    j.F.workers = ctx->sm_count * F::WARPS;
+    j.F.groups = ctx->sm_count * F::WARPS / j.F.n_kv;
     const long long blocks = ((long long)j.F.B.max_rows * j.F.group + 8 * NB - 1) / (8 * NB);
     PC_LAUNCH((k_paged_few<D, F32, NB, CHECK>), dim3(ctx->sm_count), dim3(F::WARPS * 32), F::SMEM, stream, mk, mv, j.F, ctx->rope);
     PC_LAUNCH((k_paged_join<D, F32>), dim3((unsigned)(j.F.B.n_seqs * blocks), j.F.n_kv), dim3(JOIN_WARPS * 32), 0, stream, j);
@@ -784,6 +792,7 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.prefix_here = shared && !tc && A.batch.n_prefix > 0;
     P.block = (long long)(P.prefix_here ? A.batch.n_rows : A.batch.max_rows) * ctx->group <= 8 ? 8 : MAX_ROWS;
     P.least = 4;
+    P.pool_v = A.pages->v;
     P.scale = pc_q_rot_scale(D.head_dim);
     P.out = A.out;
     P.lse = A.lse;

@@ -28,7 +28,7 @@ constexpr int REGS_LAUNCH = 65536 / TC_THREADS / 8 * 8, REGS_ISSUE = 72, REGS_SO
 static_assert(128 * REGS_ISSUE + 256 * REGS_SOFTMAX <= TC_THREADS * REGS_LAUNCH, "more registers than the block has");
 constexpr float GROW = 8.f;
 constexpr int PAIR = 2 * TILE;                     // packed rows of an item
-constexpr int LEAST_TILES = 4;                     // a part of a pair has as many key tiles at least
+constexpr int LEAST_TILES = 16;                    // a part of a pair has as many key tiles at least (with 4 and parts of three tiles a prompt of 1,136 tokens took 37 us, so 27.5)
 constexpr int UNITS = 4;                           // units that are told ahead
 
 // What a unit's warps need to know of it
