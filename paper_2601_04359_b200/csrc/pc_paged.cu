@@ -176,7 +176,7 @@ extern "C" pc_status pc_paged_create(pc_ctx *ctx, pc_paged **out) {
         PC_CUDA_TRY(cudaMalloc(&w->few_ml, few * sizeof(float2)));
         PC_CUDA_TRY(cudaMalloc(&w->home_o, home * D.head_dim * sizeof(float)));
         PC_CUDA_TRY(cudaMalloc(&w->home_ml, home * sizeof(float2)));
-        PC_CUDA_TRY(cudaMalloc(&w->plan, (PC_MAX_SEQS + PAGED_PLAN_HEAD) * sizeof(long long)));
+        PC_CUDA_TRY(cudaMalloc(&w->groups_of, ((w->home_rows * ctx->group + 7) / 8 + (size_t)D.max_q * ctx->group / 8 + PC_MAX_SEQS + 1) * sizeof(int2)));
         if (pc_paged_tc_shape(ctx)) {
             const size_t tiles = 2 * pc_paged_tc_slots(ctx);
             PC_CUDA_TRY(cudaMalloc(&w->q_rot, (size_t)D.max_q * D.n_q_heads * D.head_dim * sizeof(__nv_bfloat16)));
@@ -202,7 +202,7 @@ extern "C" pc_status pc_paged_destroy(pc_paged *w) {
     cudaFree(w->few_ml);
     cudaFree(w->home_o);
     cudaFree(w->home_ml);
-    cudaFree(w->plan);
+    cudaFree(w->groups_of);
     cudaFree(w->q_rot);
     cudaFree(w->tc_plan);
     cudaFree(w->tc_tickets);

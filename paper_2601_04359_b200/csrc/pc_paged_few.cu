@@ -115,7 +115,8 @@ struct FewParams {
     float *home_o;           // [2][rows][query heads][D]: items that one warp has done (own, prefix)
     float2 *home_ml;
     size_t home_rows;        // rows x query heads of one of the two
-    long long *plan;         // Line, then the first place of every sequence's items on it
+    int2 *groups_of;         // the first and the last group of every item (item_index), for k_paged_join
+    int own_items;           // where the sequences' items begin there
     uint32_t wait_us, extra_tx;
 };
 
@@ -123,7 +124,6 @@ struct FewParams {
 // Where groups are plenty (at least two an item) an item's length on the line is its steps made up to a multiple of `unit`, and a group takes one unit: part of one item.  Otherwise
 // `unit` is 1, a gap lies behind each item, and groups take runs of even length, which go from item to item.
 struct Line { long long total, prefix_end, per; int prefix_len, groups, rest, unit; };
-static_assert(sizeof(Line) <= PAGED_PLAN_HEAD * 8, "the plan's head");
 
 // (kept out of line: the code of a call of a few steps is fetched as it runs, and its length is what such a call waits for)
 __device__ __noinline__ long long divide(long long a, int b) { return ((a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
@@ -133,15 +133,10 @@ __device__ __forceinline__ int blocks_of(int rows, int group, int block) { retur
 __device__ __forceinline__ int made_up(int len, int unit) { return unit == 1 ? len + GAP : (len + unit - 1) / unit * unit; }
 __device__ __forceinline__ int item_steps(const FewParams &P, int own) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(own)); }
 __device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block) : 0; }
-// first place of a group; the group that has a place
+// first place of a group
 __device__ __forceinline__ long long cut(const Line &L, int w) { return L.per * w + (L.rest ? (uint32_t)(L.rest * w) / (uint32_t)L.groups : 0u); }
-__device__ __forceinline__ int group_of(const Line &L, long long place) {
-    if (L.rest == 0) return (int)divide(place, (int)min(L.per, (long long)INT32_MAX));
-    int w = min(L.groups - 1, (int)((double)place * L.groups / (double)L.total));
-    while (w > 0 && cut(L, w) > place) --w;
-    while (w + 1 < L.groups && cut(L, w + 1) <= place) ++w;
-    return w;
-}
+// Number of block k of sequence s, the first of whose rows is r0: no two blocks have one, whatever the sequences' rows, and none is beyond rows * group / block + sequences.
+__device__ __forceinline__ int item_index(const FewParams &P, int block, int r0, int s, int k) { return P.own_items + (int)((long long)r0 * P.group / block) + s + k; }
 // Blocks of a sequence's rows from both ends in turn: where attention is causal, two neighbours on the line have as much to do as any other two.
 __device__ __forceinline__ int zigzag(int k, int n) { return k & 1 ? n - 1 - k / 2 : k / 2; }
 
@@ -200,9 +195,10 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
     }
     j1 = min(j1, prefix_steps + steps_of(max(0, most)));
 
-    // positions of the block's rows, one a lane: asked for first, as the table entries wait for them
-    int4 pos_of = make_int4(0, 0, 0, 0);
-    if (lane < n_rows) pos_of = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + I.r0 + (p0 + lane) / P.group);
+    // the block's rows, one a lane: where a row lies among queries and outputs, and its position, asked for first, as the table entries wait for it
+    const int my_p = p0 + min(lane, n_rows - 1), my_i = my_p / P.group;
+    const uint32_t my_row = (uint32_t)(I.r0 + my_i) * P.n_q_heads + I.h * P.group + (my_p - my_i * P.group);
+    const int4 my_pos = __ldcg(reinterpret_cast<const int4 *>(P.q_pos) + I.r0 + my_i);
     // pages of 32 steps, one a lane
     const int32_t *own_table = P.B.table + (size_t)max(I.s, 0) * P.B.max_pages;
     int page = 0, pages_from = j0 - 32;
@@ -236,44 +232,57 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
     // Queries, rotated and scaled, eight rows at a time through shared memory into the form that the instructions want.  One rounding to bf16 where the context is bf16 (half a
     // step of eight bits, as the keys have it), three parts where it is fp32.
     uint32_t qf[KK][NB][PARTS][2];
-    constexpr int E = D / 32;                              // channels of a lane, whole rotary pairs
+    constexpr int E = D / 32, PAIRS = E / 2;               // channels of a lane, whole rotary pairs
+    if (my_pos.x < 0 || my_pos.x >= rope.max_pos[0] || my_pos.y < 0 || my_pos.y >= rope.max_pos[1] || my_pos.z < 0 || my_pos.z >= rope.max_pos[2])
+        pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
+    const int my_t = min(max(my_pos.x, 0), rope.max_pos[0] - 1), my_h = min(max(my_pos.y, 0), rope.max_pos[1] - 1), my_w = min(max(my_pos.z, 0), rope.max_pos[2] - 1);
+    const auto axis = [](int a, int t, int h, int w) { return a == 0 ? t : (a == 1 ? h : w); };
+    int pair_axis[PAIRS], pair_n[PAIRS], pair_at[PAIRS];   // a pair's axis, entries a position of it, and where the pair's column begins
+#pragma unroll
+    for (int e = 0; e < PAIRS; ++e) {
+        const int pair = lane * PAIRS + e, a = pair % 3;
+        pair_axis[e] = a;
+        pair_n[e] = axis(a, rope.n_axis[0], rope.n_axis[1], rope.n_axis[2]);
+        pair_at[e] = axis(a, rope.off[0], rope.off[1], rope.off[2]) + pair / 3;
+    }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         __syncwarp();
+        // all eight rows (the last one again where there are fewer) and their table entries are asked for at once: what this takes is their latency
+        uint32_t raw[8][F32 ? E : E / 2];
+        float2 cs[8][PAIRS];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            const int p = p0 + nb * 8 + r;
-            const int px = __shfl_sync(0xffffffffu, pos_of.x, nb * 8 + r), py = __shfl_sync(0xffffffffu, pos_of.y, nb * 8 + r), pz = __shfl_sync(0xffffffffu, pos_of.z, nb * 8 + r);
-            const bool there = p < packed;
-            const int i = there ? p / P.group : 0, g = there ? p - i * P.group : 0;
-            const size_t row = (size_t)(I.r0 + i), from = (row * P.n_q_heads + I.h * P.group + g) * D + lane * E;
-            float x[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = 0.f;
-            if (there) {
-                bool bad = false;
+            const int from = nb * 8 + r;
+            const size_t row = (size_t)__shfl_sync(0xffffffffu, my_row, from) * D + lane * E;
+            const int pt = __shfl_sync(0xffffffffu, my_t, from), ph = __shfl_sync(0xffffffffu, my_h, from), pw = __shfl_sync(0xffffffffu, my_w, from);
+            if constexpr (F32) {
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
-                    float2 y;
-                    if constexpr (F32) y = __ldcg(reinterpret_cast<const float2 *>(static_cast<const float *>(P.q) + from + e));
-                    else {
-                        const uint32_t w = __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + from + e));
-                        y = make_float2(pc_bf16_lo(w), pc_bf16_hi(w));
-                    }
-                    y = pc_rotate(y.x, y.y, pc_rope_cs_clamped(rope, (lane * E + e) / 2, px, py, pz, bad));
-                    x[e] = __fmul_rn(y.x, P.scale);
-                    x[e + 1] = __fmul_rn(y.y, P.scale);
+                    const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const float *>(P.q) + row + e));
+                    raw[r][e] = y.x;
+                    raw[r][e + 1] = y.y;
                 }
-                if (bad) pc_flag(P.B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
+            } else if constexpr (E == 4) {
+                const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
+                raw[r][0] = y.x;
+                raw[r][1] = y.y;
+            } else {
+                raw[r][0] = __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
             }
-            // row r: D values, 16-byte pieces at their number ^ r
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                const int c = lane * E + e;
-                if constexpr (F32) sts64(W.q + r * D * 4 + (((c >> 2) ^ r) << 4) + (c & 3) * 4, __float_as_uint(x[e]), __float_as_uint(x[e + 1]));
-                else sts32(W.q + r * D * 2 + (((c >> 3) ^ r) << 4) + (c & 7) * 2, pc_pack_bf16(x[e], x[e + 1]));
-            }
+            for (int e = 0; e < PAIRS; ++e) cs[r][e] = __ldg(rope.tab + (pair_at[e] + axis(pair_axis[e], pt, ph, pw) * pair_n[e]));
         }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int e = 0; e < PAIRS; ++e) {              // row r: D values, 16-byte pieces at their number ^ r
+                float2 y = F32 ? make_float2(__uint_as_float(raw[r][2 * e]), __uint_as_float(raw[r][F32 ? 2 * e + 1 : 0])) : make_float2(pc_bf16_lo(raw[r][e]), pc_bf16_hi(raw[r][e]));
+                y = pc_rotate(y.x, y.y, cs[r][e]);
+                const int c = lane * E + 2 * e;
+                if constexpr (F32) sts64(W.q + r * D * 4 + (((c >> 2) ^ r) << 4) + (c & 3) * 4, __float_as_uint(__fmul_rn(y.x, P.scale)), __float_as_uint(__fmul_rn(y.y, P.scale)));
+                else sts32(W.q + r * D * 2 + (((c >> 3) ^ r) << 4) + (c & 7) * 2, pc_pack_bf16(__fmul_rn(y.x, P.scale), __fmul_rn(y.y, P.scale)));
+            }
         __syncwarp();
         if constexpr (F32) {
 #pragma unroll
@@ -473,12 +482,12 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             if (eighth == 0) sts64(W.q + (nb * 8 + quad * 2 + e) * 8, __float_as_uint(m[nb][e]), __float_as_uint(l[nb][e]));
         }
     __syncwarp();
-#pragma unroll 1
+#pragma unroll 2
     for (int r = 0; r < n_rows; ++r) {
         const float2 y = lds64(W.q + r * 8);
         const float mr = y.x, lr = y.y;
-        const int p = p0 + r, i = p / P.group;
-        const size_t to = direct || whole ? (size_t)(I.r0 + i) * P.n_q_heads + I.h * P.group + (p - i * P.group) : (size_t)r;
+        const uint32_t row_at = __shfl_sync(0xffffffffu, my_row, r);
+        const size_t to = direct || whole ? (size_t)row_at : (size_t)r;
         const float inv = !direct ? 1.f : (lr > 0.f ? 1.f / lr : (lr != lr ? lr : 0.f));       // nothing seen: 0
         const uint32_t from = W.ring + r * D * 4 + (((lane * E) ^ (((r >> 1) & 3) * 8)) * 4);
         float x[E];
@@ -489,7 +498,7 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             x[e + 1] = y.y * inv;
         }
         if constexpr (F32 || CHECK)
-            if (odd_seen) add_odd<D, F32>(P, I, j0, j1, F32 ? 0 : prefix_steps + (fewest & ~(STEP - 1)) / STEP, I.s < 0 ? 0 : sees(p), x);
+            if (odd_seen) add_odd<D, F32>(P, I, j0, j1, F32 ? 0 : prefix_steps + (fewest & ~(STEP - 1)) / STEP, I.s < 0 ? 0 : sees(p0 + r), x);
         float *row = (F32 && direct ? static_cast<float *>(P.out) : o) + to * D + lane * E;
         if (!F32 && direct) {
             __nv_bfloat16 *b = static_cast<__nv_bfloat16 *>(P.out) + to * D + lane * E;
@@ -517,7 +526,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - pc_smem_u32(smem_raw));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 256);
-    long long *sums = reinterpret_cast<long long *>(gen + 512), *plan = reinterpret_cast<long long *>(gen + F::PLAN_AT);
+    long long *plan = reinterpret_cast<long long *>(gen + F::PLAN_AT);
     int *info = reinterpret_cast<int *>(gen + F::INFO_AT);             // rows' start, rows, length of every sequence
     const int warp = threadIdx.x >> 5;
     Warp<D, F32> W;
@@ -541,55 +550,63 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         if constexpr (F::INFO) return PagedSeq{info[3 * s], info[3 * s + 1], info[3 * s + 2]};
         else return paged_seq(P.B, s);
     };
-    Line L;
-    {
+    for (int s = threadIdx.x; F::INFO && s < P.B.n_seqs; s += THREADS) {
+        const PagedSeq S = paged_seq(P.B, s);
+        info[3 * s] = S.r0;
+        info[3 * s + 1] = S.n;
+        info[3 * s + 2] = S.len;
+    }
+    __syncthreads();
+    Line *line = reinterpret_cast<Line *>(gen + 512);
+    if (warp == 0) {
         const int pitems = prefix_blocks(P), psteps = max(1, steps_of(P.B.n_prefix));
-        long long both = 0;                                // steps, and items in the lower 24 bits
+        long long steps = 0;
+        int items = 0;
 #pragma unroll 1
-        for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) {
-            const PagedSeq S = paged_seq(P.B, s);
+        for (int s = W.lane; s < P.B.n_seqs; s += 32) {
+            const PagedSeq S = seq_of(s);
             const int n = blocks_of(S.n, P.group, 8 * NB);
-            both += ((long long)n * item_steps(P, S.len) << 24) + n;
-            if constexpr (F::INFO) {
-                info[3 * s] = S.r0;
-                info[3 * s + 1] = S.n;
-                info[3 * s + 2] = S.len;
-            }
+            items += n;
+            steps += (long long)n * item_steps(P, S.len);
         }
-        paged_scan<THREADS>(both, sums);
-        both = sums[F::WARPS - 1];
-        const int items = (int)(both & 0xFFFFFF) + pitems;
-        const long long steps = (both >> 24) + (long long)pitems * psteps;
-        __syncthreads();
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            items += __shfl_xor_sync(0xffffffffu, items, o);
+            steps += __shfl_xor_sync(0xffffffffu, steps, o);
+        }
+        items += pitems;
+        steps += (long long)pitems * psteps;
+        Line L;
         const int spare = items * 2 <= P.groups ? P.groups - items : 0;
         L.unit = spare ? max(P.least, (int)divide(steps + spare - 1, spare)) : 1;
         L.prefix_len = made_up(psteps, L.unit);
         L.prefix_end = (long long)pitems * L.prefix_len;
         long long at = L.prefix_end;
 #pragma unroll 1
-        for (int s0 = 0; s0 < P.B.n_seqs; s0 += THREADS) {
-            const int s = s0 + threadIdx.x;
+        for (int s0 = 0; s0 < P.B.n_seqs; s0 += 32) {
+            const int s = s0 + W.lane;
             long long v = 0;
             if (s < P.B.n_seqs) {
                 const PagedSeq S = seq_of(s);
                 v = (long long)blocks_of(S.n, P.group, 8 * NB) * made_up(item_steps(P, S.len), L.unit);
             }
-            const long long end = paged_scan<THREADS>(v, sums);
+            long long end = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, end, o);
+                if (W.lane >= o) end += u;
+            }
             if (s < P.B.n_seqs) plan[s] = at + end - v;
-            at += sums[F::WARPS - 1];
-            __syncthreads();
+            at += __shfl_sync(0xffffffffu, end, 31);
         }
         L.total = at;
         L.groups = spare ? (int)divide(at, L.unit) : (int)min((long long)P.groups, divide(at + P.least - 1, P.least));
         L.per = divide(at, max(1, L.groups));
         L.rest = (int)(at - L.per * L.groups);
+        if (W.lane == 0) *line = L;
     }
     __syncthreads();
-    if (blockIdx.x == 0) {
-        if (threadIdx.x == 0) *reinterpret_cast<Line *>(P.plan) = L;
-        for (int s = threadIdx.x; s < P.B.n_seqs; s += THREADS) P.plan[PAGED_PLAN_HEAD + s] = plan[s];
-    }
-
+    const Line L = *line;
     // ---- this warp's part of it
     const int w = blockIdx.x * F::WARPS + warp, group = w / P.n_kv, h = w - group * P.n_kv;
     if (group >= L.groups) return;
@@ -598,12 +615,13 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 #pragma unroll 1
     while (g < g1 && W.alive) {
         Item I;
-        int off, all;                                      // place in the item, places of it
+        int off, all, number;                              // place in the item, places of it, its number
         if (g < L.prefix_end) {
             const int item = (int)divide(g, L.prefix_len);
             all = L.prefix_len;
             off = (int)(g - (long long)item * L.prefix_len);
             I = {0, paged_rows(P.B), -1, h, item, max(1, steps_of(P.B.n_prefix)), 0, 0};
+            number = item;
         } else {
             int lo = 0, hi = P.B.n_seqs - 1;               // the last sequence that begins at or before g (one without rows has no places)
 #pragma unroll 1
@@ -617,10 +635,15 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             const long long y = g - plan[lo], item = divide(y, all);
             off = (int)(y - item * all);
             I = {S.r0, S.n, lo, h, zigzag((int)item, blocks), len, S.len, S.len - S.n};
+            number = item_index(P, 8 * NB, S.r0, lo, (int)item);
         }
         const int take = (int)min((long long)(all - off), g1 - g), end = min(I.len, off + take);
         g += take;
         if (off >= end) continue;                          // empty places
+        if (h == 0 && W.lane == 0) {
+            if (off == 0) P.groups_of[number].x = group;
+            if (end == I.len) P.groups_of[number].y = group;
+        }
         const bool whole = off == 0 && end == I.len, home = whole && P.shared;
         const size_t slot = ((size_t)(2 * group + (off == 0)) * P.n_kv + h) * MAX_ROWS;
         float *o = home ? P.home_o + (I.s < 0 ? P.home_rows * D : 0) : P.part_o + slot * D;
@@ -631,16 +654,15 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
 }
 
 // ------------------------------------------------------------------------------------------------ the parts of an item added up
-// A CTA has one block of a sequence's packed rows of one KV head: JOIN_WARPS warps in as many sets as its rows leave, each set every so-many-th part of every row; then the sets, in their
-// order.  The order is that of the keys, so a call gives the same bits every time.
-constexpr int JOIN_WARPS = 16;
-
+// A CTA has one block of a sequence's packed rows of one KV head: WARPS warps in as many sets as its rows leave, each set every so-many-th part of every row; then the sets, in their
+// order.  The order is that of the keys, so a call gives the same bits every time.  Sixteen warps while their CTAs are resident at once, for most of the time is the latency of a set's parts; eight beyond
+// that.
 struct JoinParams {
     FewParams F;
     PagedTcParts T;          // what the tcgen05 kernel has left of the prefix
 };
 
-template <int D, bool F32>
+template <int D, bool F32, int JOIN_WARPS>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_constant__ JoinParams J) {
     constexpr int E = D / 32;                              // channels of a lane
     __shared__ float so[JOIN_WARPS][D];
@@ -649,90 +671,92 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     pc_grid_dep_launch();
     const int s = blockIdx.x % P.B.n_seqs, k = blockIdx.x / P.B.n_seqs, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pc_grid_dep_wait();
-    Line L;
-    {
-        longlong2 x[4];
-        static_assert(sizeof(Line) == 40 && PAGED_PLAN_HEAD * 8 == sizeof(x), "the line, as it lies in memory");
-#pragma unroll
-        for (int i = 0; i < 3; ++i) x[i] = __ldcg(reinterpret_cast<const longlong2 *>(P.plan) + i);
-        L = {x[0].x, x[0].y, x[1].x, (int)x[1].y, (int)(x[1].y >> 32), (int)x[2].x, (int)(x[2].x >> 32)};
-    }
-    const long long place = __ldcg(P.plan + PAGED_PLAN_HEAD + s);
     const PagedSeq S = paged_seq(P.B, s);
     const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block);
     if (k >= blocks) return;
     const int block = zigzag(k, blocks), p0 = block * P.block, n = min(P.block, packed - p0);
-    const int len = item_steps(P, S.len);
-    const long long first = place + (long long)k * made_up(len, L.unit);
-    const int w0 = group_of(L, first), w1 = group_of(L, first + len - 1);
-    if (!P.shared && w0 == w1) return;                     // its warp has written the output
-    const int sets = JOIN_WARPS / n, r = warp % n, set = warp / n;
-    float o[E] = {}, M = -INFINITY, l = 0.f;
-    if (set < sets) {
-        const int p = p0 + r, i = p / P.group;
+    const int2 w = __ldcg(P.groups_of + item_index(P, P.block, S.r0, s, k));
+    if (!P.shared && w.x == w.y) return;                   // its warp has written the output
+    const int sets = max(1, JOIN_WARPS / n);
+    // Parts of a row, own ones first: of the groups, each its last item for the first one and its first for the others; or of one group at home; or the tcgen05 kernel's
+    struct From { const float *o; const float2 *ml; int parts; size_t pitch, later; };
+    const auto from = [&](int v0, int v1, int row, size_t home_at) {
+        if (v0 == v1) return From{P.home_o + home_at * D, P.home_ml + home_at, 1, 0, 0};
+        const size_t step = (size_t)P.n_kv * MAX_ROWS, slot = ((size_t)(2 * v0 + 1) * P.n_kv + h) * MAX_ROWS + row;
+        return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * step, step};
+    };
+    for (int r0 = 0; r0 < n; r0 += JOIN_WARPS) {           // (more than one turn where there are more rows than warps: one set)
+        const int r = r0 + warp % min(n, JOIN_WARPS), set = warp / min(n, JOIN_WARPS);
+        const int p = p0 + min(r, n - 1), i = p / P.group;
         const size_t home = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
-        // Parts, own ones first: of the groups, each its last item for the first one and its first for the others; or of one group at home; or the tcgen05 kernel's
-        struct From { const float *o; const float2 *ml; int parts; size_t pitch, later; } own{}, pre{};
-        const auto from = [&](int v0, int v1, int row, size_t home_at) {
-            if (v0 == v1) return From{P.home_o + home_at * D, P.home_ml + home_at, 1, 0, 0};
-            const size_t step = (size_t)P.n_kv * MAX_ROWS, slot = ((size_t)(2 * v0 + 1) * P.n_kv + h) * MAX_ROWS + row;
-            return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * step, step};
-        };
-        own = from(w0, w1, r, home);
-        if (P.shared && P.B.n_prefix > 0) {
-            const long long row = (long long)S.r0 * P.group + p;          // packed row of the batch
-            if (P.prefix_here) {
-                const long long at = row / P.block * L.prefix_len;
-                pre = from(group_of(L, at), group_of(L, at + max(1, steps_of(P.B.n_prefix)) - 1), (int)(row % P.block), P.home_rows + home);
-            } else {
-                const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
-                const size_t slot = T.first * PAGED_TC_TILE + T.row;
-                pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, J.T.parts, 2 * PAGED_TC_TILE, 0};
+        float o[E] = {}, M = -INFINITY, l = 0.f;
+        if (set < sets && r < n) {
+            const From own = from(w.x, w.y, r, home);
+            From pre{};
+            if (P.shared && P.B.n_prefix > 0) {
+                const long long row = (long long)S.r0 * P.group + p;      // packed row of the batch
+                if (P.prefix_here) {
+                    const int2 v = __ldcg(P.groups_of + row / P.block);
+                    pre = from(v.x, v.y, (int)(row % P.block), P.home_rows + home);
+                } else {
+                    const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
+                    const size_t slot = T.first * PAGED_TC_TILE + T.row;
+                    pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, J.T.parts, 2 * PAGED_TC_TILE, 0};
+                }
+            }
+#pragma unroll 4
+            for (int c = set; c < own.parts + pre.parts; c += sets) {
+                const bool is_own = c < own.parts;
+                const int u = is_own ? c : c - own.parts;
+                const size_t at = (is_own ? own.pitch : pre.pitch) * u - (u ? (is_own ? own.later : pre.later) : 0);
+                const float *po = (is_own ? own.o : pre.o) + at * D + lane * E;
+                const float2 y = __ldcg((is_own ? own.ml : pre.ml) + at);
+                float x[E];
+                if constexpr (E == 4) {
+                    const float4 z = __ldcg(reinterpret_cast<const float4 *>(po));
+                    x[0] = z.x; x[1] = z.y; x[2] = z.z; x[3] = z.w;
+                } else {
+                    const float2 z = __ldcg(reinterpret_cast<const float2 *>(po));
+                    x[0] = z.x; x[1] = z.y;
+                }
+                const float m = fmaxf(M, y.x), f = m == -INFINITY ? 1.f : exp2_fast(M - m), g = m == -INFINITY ? 1.f : exp2_fast(y.x - m);
+                M = m;
+                l = l * f + y.y * g;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * g;
             }
         }
-#pragma unroll 4
-        for (int c = set; c < own.parts + pre.parts; c += sets) {
-            const bool is_own = c < own.parts;
-            const int u = is_own ? c : c - own.parts;
-            const size_t at = (is_own ? own.pitch : pre.pitch) * u - (u ? (is_own ? own.later : pre.later) : 0);
-            const float *po = (is_own ? own.o : pre.o) + at * D + lane;
-            const float2 y = __ldcg((is_own ? own.ml : pre.ml) + at);
-            float x[E];
+        if (sets > 1) {
+            __syncthreads();
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = __ldcg(po + e * 32);
-            const float m = fmaxf(M, y.x), f = m == -INFINITY ? 1.f : exp2_fast(M - m), g = m == -INFINITY ? 1.f : exp2_fast(y.x - m);
-            M = m;
-            l = l * f + y.y * g;
+            for (int e = 0; e < E; ++e) so[warp][e * 32 + lane] = o[e];
+            if (lane == 0) sml[warp] = make_float2(M, l);
+            __syncthreads();
+            if (warp >= n) return;                         // (one turn)
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * g;
+            for (int e = 0; e < E; ++e) o[e] = 0.f;
+            M = -INFINITY;
+            for (int c = 0; c < sets; ++c) M = fmaxf(M, sml[c * n + warp].x);
+            l = 0.f;
+            for (int c = 0; c < sets; ++c) {
+                const float2 y = sml[c * n + warp];
+                const float g = M == -INFINITY ? 1.f : exp2_fast(y.x - M);
+                l = fmaf(y.y, g, l);
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = fmaf(so[c * n + warp][e * 32 + lane], g, o[e]);
+            }
         }
+        if (r >= n) return;
+        const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+        if constexpr (F32) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) so[warp][e * 32 + lane] = o[e];
-        if (lane == 0) sml[warp] = make_float2(M, l);
+            for (int e = 0; e < E; ++e) static_cast<float *>(P.out)[home * D + lane * E + e] = o[e] * inv;
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(static_cast<__nv_bfloat16 *>(P.out) + home * D + lane * E + e) = pc_pack_bf16(o[e] * inv, o[e + 1] * inv);
+        }
+        if (P.lse && lane == 0) P.lse[home] = (M + log2f(l)) * 0.6931471805599453f;
     }
-    __syncthreads();
-    if (warp >= n) return;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    M = -INFINITY;
-    for (int c = 0; c < sets; ++c) M = fmaxf(M, sml[c * n + warp].x);
-    l = 0.f;
-    for (int c = 0; c < sets; ++c) {
-        const float2 y = sml[c * n + warp];
-        const float g = M == -INFINITY ? 1.f : exp2_fast(y.x - M);
-        l = fmaf(y.y, g, l);
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(so[c * n + warp][e * 32 + lane], g, o[e]);
-    }
-    const int p = p0 + warp, i = p / P.group;
-    const size_t to = (size_t)(S.r0 + i) * P.n_q_heads + h * P.group + (p - i * P.group);
-    const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        if constexpr (F32) static_cast<float *>(P.out)[to * D + e * 32 + lane] = o[e] * inv;
-        else static_cast<__nv_bfloat16 *>(P.out)[to * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
-    }
-    if (P.lse && lane == 0) P.lse[to] = (M + log2f(l)) * 0.6931471805599453f;
 }
 
 template <int D, bool F32, int NB, bool CHECK> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, cudaStream_t stream) {
@@ -747,7 +771,9 @@ template <int D, bool F32, int NB, bool CHECK> pc_status launch(const CUtensorMa
     j.F.groups = ctx->sm_count * F::WARPS / j.F.n_kv;
     const long long blocks = ((long long)j.F.B.max_rows * j.F.group + 8 * NB - 1) / (8 * NB);
     PC_LAUNCH((k_paged_few<D, F32, NB, CHECK>), dim3(ctx->sm_count), dim3(F::WARPS * 32), F::SMEM, stream, mk, mv, j.F, ctx->rope);
-    PC_LAUNCH((k_paged_join<D, F32>), dim3((unsigned)(j.F.B.n_seqs * blocks), j.F.n_kv), dim3(JOIN_WARPS * 32), 0, stream, j);
+    const dim3 grid((unsigned)(j.F.B.n_seqs * blocks), j.F.n_kv);
+    if ((long long)grid.x * grid.y <= 4ll * ctx->sm_count) PC_LAUNCH((k_paged_join<D, F32, 16>), grid, dim3(16 * 32), 0, stream, j);
+    else PC_LAUNCH((k_paged_join<D, F32, 8>), grid, dim3(8 * 32), 0, stream, j);
     return PC_OK;
 }
 template <int D, bool F32> pc_status launch(const CUtensorMap &mk, const CUtensorMap &mv, const JoinParams &J, const pc_ctx *ctx, cudaStream_t stream) {
@@ -801,7 +827,8 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.home_o = w->home_o;
     P.home_ml = w->home_ml;
     P.home_rows = w->home_rows * D.n_q_heads;
-    P.plan = w->plan;
+    P.groups_of = w->groups_of;
+    P.own_items = (int)((w->home_rows * ctx->group + 7) / 8);
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
     if (tc) J.T = *tc;

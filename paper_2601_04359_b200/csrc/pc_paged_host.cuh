@@ -4,7 +4,6 @@
 
 constexpr int PAGED_FEW_ROWS = 16;           // most packed rows of a block of the few-row kernel
 constexpr int PAGED_HOME_ROWS = 1024;        // most rows of a call whose prefix is attended apart
-constexpr int PAGED_PLAN_HEAD = 8;         // words of the few-row kernel's plan ahead of the sequences' places
 constexpr int PAGED_TC_TILE = 128;           // packed rows of a tile of the tcgen05 kernel
 
 struct pc_paged {
@@ -12,7 +11,7 @@ struct pc_paged {
     float *few_o, *home_o;
     float2 *few_ml, *home_ml;
     size_t home_rows;
-    long long *plan;
+    int2 *groups_of;                         // the few-row kernel's items: prefix blocks of home_rows rows, then blocks of max_q rows and one a sequence
     // bf16: rotated queries, units, parts and their counters of the tcgen05 kernel
     void *q_rot;
     int *tc_plan, *tc_tickets;
