@@ -233,15 +233,12 @@ extern "C" pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const p
     // sequences share is attended once for all their rows.
     const long long rows = (long long)batch->max_rows * w->ctx->group;
     const bool tc = pc_paged_tc_shape(w->ctx) && w->ctx->attend_impl != 1;
-    if (tc && rows > 64) return pc_launch_paged_tc(w, A, 0, nullptr, stream);
+    if (tc && rows > 64) return pc_launch_paged_tc(w, A, false, 0, nullptr, stream);
     const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows;
     PagedTcParts left{};
-    if (tc && shared && (long long)n_rows * w->ctx->group > PAGED_FEW_ROWS) {
-        const int parts = pc_paged_tc_prefix_parts(w->ctx, A.batch);
-        if (parts > 0) {
-            const pc_status ps = pc_launch_paged_tc(w, A, parts, &left, stream);
-            return ps != PC_OK ? ps : pc_launch_paged_few(w, A, true, &left, stream);
-        }
+    if (tc && shared && (long long)n_rows * w->ctx->group > PAGED_FEW_ROWS && pc_paged_tc_holds(w->ctx, A.batch)) {
+        const pc_status ps = pc_launch_paged_tc(w, A, true, pc_paged_few_block(A, false), &left, stream);
+        return ps != PC_OK ? ps : pc_launch_paged_few(w, A, true, &left, stream);
     }
     return pc_launch_paged_few(w, A, shared, nullptr, stream);
 }

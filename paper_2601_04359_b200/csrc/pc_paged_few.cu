@@ -106,6 +106,7 @@ struct FewParams {
     int prefix_here;         // ... in this kernel
     int block;               // packed rows of a block
     int groups, least;       // groups of warps; fewest steps of one
+    const int *share;        // beside the tcgen05 kernel: [2] CTAs for this one
     const void *pool_v;
     float scale;
     void *out;
@@ -542,7 +543,9 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    pc_grid_dep_wait();
+    // Beside the tcgen05 kernel: that one's wait has been over before this one began, so what it found is there; this one ends behind it, for k_paged_join waits for this one alone.
+    if (!P.share) pc_grid_dep_wait();
+    const int ctas = P.share ? min(max(__ldcg(P.share + 2), 1), (int)gridDim.x) : (int)gridDim.x, groups = min(P.groups, ctas * F::WARPS / P.n_kv);
 
     // ---- the line: steps and items of the whole call, the unit that follows from them, then the sequences' places
     constexpr int THREADS = F::WARPS * 32;
@@ -577,7 +580,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         items += pitems;
         steps += (long long)pitems * psteps;
         Line L;
-        const int spare = items * 2 <= P.groups ? P.groups - items : 0;
+        const int spare = items * 2 <= groups ? groups - items : 0;
         L.unit = spare ? max(P.least, (int)divide(steps + spare - 1, spare)) : 1;
         L.prefix_len = made_up(psteps, L.unit);
         L.prefix_end = (long long)pitems * L.prefix_len;
@@ -600,7 +603,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
             at += __shfl_sync(0xffffffffu, end, 31);
         }
         L.total = at;
-        L.groups = spare ? (int)divide(at, L.unit) : (int)min((long long)P.groups, divide(at + P.least - 1, P.least));
+        L.groups = spare ? (int)divide(at, L.unit) : (int)min((long long)groups, divide(at + P.least - 1, P.least));
         L.per = divide(at, max(1, L.groups));
         L.rest = (int)(at - L.per * L.groups);
         if (W.lane == 0) *line = L;
@@ -609,9 +612,11 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     const Line L = *line;
     // ---- this warp's part of it
     const int w = blockIdx.x * F::WARPS + warp, group = w / P.n_kv, h = w - group * P.n_kv;
-    if (group >= L.groups) return;
-    long long g = cut(L, group);
-    const long long g1 = cut(L, group + 1);
+    long long g = 0, g1 = 0;
+    if (group < L.groups) {
+        g = cut(L, group);
+        g1 = cut(L, group + 1);
+    }
 #pragma unroll 1
     while (g < g1 && W.alive) {
         Item I;
@@ -651,6 +656,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         take_unit<D, F32, NB, CHECK>(P, rope, &map_k, &map_v, W, abort_flag, I, off, end, whole && !P.shared, o, ml, whole);
     }
     if (!W.alive) pc_let_copies_land();
+    if (P.share) pc_grid_dep_wait();
 }
 
 // ------------------------------------------------------------------------------------------------ the parts of an item added up
@@ -681,6 +687,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     // Parts of a row, own ones first: of the groups, each its last item for the first one and its first for the others; or of one group at home; or the tcgen05 kernel's
     struct From { const float *o; const float2 *ml; int parts; size_t pitch, later; };
     const auto from = [&](int v0, int v1, int row, size_t home_at) {
+        v0 = min(max(v0, 0), P.groups - 1);                // (whatever a call whose waits ran out has left)
+        v1 = min(max(v1, v0), P.groups - 1);
         if (v0 == v1) return From{P.home_o + home_at * D, P.home_ml + home_at, 1, 0, 0};
         const size_t step = (size_t)P.n_kv * MAX_ROWS, slot = ((size_t)(2 * v0 + 1) * P.n_kv + h) * MAX_ROWS + row;
         return From{P.part_o + slot * D, P.part_ml + slot, v1 - v0 + 1, 2 * step, step};
@@ -701,7 +709,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
                 } else {
                     const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
                     const size_t slot = T.first * PAGED_TC_TILE + T.row;
-                    pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, J.T.parts, 2 * PAGED_TC_TILE, 0};
+                    pre = From{J.T.part_o + slot * D, J.T.part_ml + slot, T.parts, 2 * PAGED_TC_TILE, 0};
                 }
             }
 #pragma unroll 4
@@ -798,6 +806,10 @@ static bool few_map(CUtensorMap *m, const void *p, const pc_paged_args &A) {
 
 size_t pc_paged_few_parts(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count * 8 * MAX_ROWS; }
 
+int pc_paged_few_block(const pc_paged_args &A, bool prefix_here) {
+    return (long long)(prefix_here ? A.batch.n_rows : A.batch.max_rows) * A.ctx->group <= 8 ? 8 : MAX_ROWS;
+}
+
 pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream) {
     const pc_ctx *ctx = A.ctx;
     const pc_layer_desc &D = ctx->desc;
@@ -816,7 +828,7 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.group = ctx->group;
     P.shared = shared;
     P.prefix_here = shared && !tc && A.batch.n_prefix > 0;
-    P.block = (long long)(P.prefix_here ? A.batch.n_rows : A.batch.max_rows) * ctx->group <= 8 ? 8 : MAX_ROWS;
+    P.block = pc_paged_few_block(A, P.prefix_here);
     P.least = 4;
     P.pool_v = A.pages->v;
     P.scale = pc_q_rot_scale(D.head_dim);
@@ -831,7 +843,10 @@ pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool sh
     P.own_items = (int)((w->home_rows * ctx->group + 7) / 8);
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
-    if (tc) J.T = *tc;
+    if (tc) {
+        J.T = *tc;
+        P.share = tc->head;
+    }
     const bool f32 = D.dtype == PC_F32;
     if (D.head_dim == 128) return f32 ? launch<128, true>(mk, mv, J, ctx, stream) : launch<128, false>(mk, mv, J, ctx, stream);
     return f32 ? launch<64, true>(mk, mv, J, ctx, stream) : launch<64, false>(mk, mv, J, ctx, stream);

@@ -34,13 +34,14 @@ struct pc_paged_args {
 struct PagedTcParts {
     const float *part_o;
     const float2 *part_ml;
-    int parts;
+    const int *head;                         // [1] parts, [2] CTAs that are left for the sequences' own tokens
 };
 // first tile of a packed row's pieces (the next one's is two further), and the row in it
-struct PagedTcRow { size_t first; int row; };
+struct PagedTcRow { size_t first; int row, parts; };
 __device__ __forceinline__ PagedTcRow paged_tc_row(const PagedTcParts &T, int n_kv, int h, long long packed_row) {
     const size_t pair = (size_t)(packed_row / (2 * PAGED_TC_TILE));
-    return {((pair * n_kv + h) * T.parts) * 2 + (size_t)(packed_row / PAGED_TC_TILE & 1), (int)(packed_row % PAGED_TC_TILE)};
+    const int parts = __ldcg(T.head + 1);
+    return {((pair * n_kv + h) * parts) * 2 + (size_t)(packed_row / PAGED_TC_TILE & 1), (int)(packed_row % PAGED_TC_TILE), parts};
 }
 
 size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kernel's scratch
@@ -48,6 +49,7 @@ size_t pc_paged_few_parts(const pc_ctx *ctx);        // rows of the few-row kern
 pc_status pc_launch_paged_few(const pc_paged *w, const pc_paged_args &A, bool shared, const PagedTcParts *tc, cudaStream_t stream);
 bool pc_paged_tc_shape(const pc_ctx *ctx);           // whether the tcgen05 kernel takes the context's type
 size_t pc_paged_tc_slots(const pc_ctx *ctx), pc_paged_tc_plan_bytes(const pc_ctx *ctx);
-int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B);
-// prefix_parts 0: every sequence over prefix and own tokens, into the output; otherwise the shared prefix alone, in so many parts, into scratch (left)
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream);
+bool pc_paged_tc_holds(const pc_ctx *ctx, const PagedBatch &B);
+int pc_paged_few_block(const pc_paged_args &A, bool prefix_here);          // packed rows of a block of the few-row kernel
+// every sequence over prefix and own tokens, into the output; or (shared) the prefix alone for all rows, into scratch (left), beside the few-row kernel with blocks of few_block rows
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, int few_block, PagedTcParts *left, cudaStream_t stream);

@@ -43,7 +43,7 @@ struct Unit {
     int parts, part;         // of the pair
 };
 static_assert(sizeof(Unit) == 48, "three 16-byte pieces");
-constexpr int PLAN_HEAD = 4;                       // words ahead of the units: their number
+constexpr int PLAN_HEAD = 4;                       // words ahead of the units: their number, parts of a pair (shared prefix), CTAs of k_paged_few beside this kernel's, this kernel's
 
 template <int D> struct Map {
     static constexpr int HALVES = D / 64, TILE_B = HALVES * HALF_BYTES;
@@ -74,9 +74,9 @@ struct TcParams {
 
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + TILE - 1) / TILE; }
 // The k-th unit of a CTA, -1 behind the last
-__device__ __forceinline__ int unit_of(int k, int n) {
-    const long long i = k & 1 ? (long long)(k + 1) * gridDim.x - 1 - blockIdx.x : (long long)k * gridDim.x + blockIdx.x;
-    return i < n ? (int)i : -1;
+__device__ __forceinline__ int unit_of(int k, int ctas, int n) {
+    const long long i = k & 1 ? (long long)(k + 1) * ctas - 1 - blockIdx.x : (long long)k * ctas + blockIdx.x;
+    return i < n && blockIdx.x < ctas ? (int)i : -1;
 }
 
 // ------------------------------------------------------------------------------------------------ queries and plan
@@ -91,7 +91,7 @@ struct FrontParams {
     int chunks, group, n_kv, d;
     long long head_rows;
     float scale;
-    int shared, shared_parts, sms, max_units, n_tickets;
+    int shared, few_block, sms, max_units, n_tickets;
     int4 *units;
     int *head, *tickets;
 };
@@ -116,13 +116,32 @@ __device__ void plan(const FrontParams &P) {
     const int tid = threadIdx.x;
     static_assert(PC_MAX_SEQS <= FRONT_THREADS && LEVELS == FRONT_THREADS, "a thread a sequence, and a level");
     if (P.shared) {
-        const int packed = paged_rows(P.B) * P.group, tiles = tiles_of(P.B.n_prefix), parts = P.shared_parts, pairs = (packed + PAIR - 1) / PAIR;
+        // This kernel, which is bound by the tensor cores and the exponentials, and the one that attends the sequences' own tokens, bound by memory, run side by side on SMs of their own, shared out
+        // by what each has to do: a pair's key tile takes an SM 1.6 us, a block's step of 16 keys and one KV head about 0.1 (0.15 with 16 rows); with more than half of the SMs the few-row
+        // kernel is bound by memory and gains nothing.
+        long long steps = 0;
+        if (tid < P.B.n_seqs) {
+            const PagedSeq S = paged_seq(P.B, tid);
+            steps = (long long)((S.n * P.group + P.few_block - 1) / P.few_block) * ((S.len + 15) / 16 + 4);
+        }
+        paged_scan<FRONT_THREADS>(steps, sums);
+        steps = sums[FRONT_THREADS / 32 - 1];
+        const int packed = paged_rows(P.B) * P.group, tiles = tiles_of(P.B.n_prefix), pairs = (packed + PAIR - 1) / PAIR, items = max(1, pairs * P.n_kv);
+        const float tc = 1.6f * (float)items * (float)(tiles + 3), few = (P.few_block > 8 ? 0.15f : 0.1f) * (float)steps * (float)P.n_kv;
+        const int least = (P.n_kv + 7) / 8;               // CTAs of eight warps that have a warp for every KV head
+        const int for_few = min(max(least, (int)((float)P.sms * few / (tc + few) + 0.5f)), P.sms * 9 / 16);
+        const int parts = max(1, min((P.sms - for_few) / items, tiles)), ctas = min(items * parts, P.sms - for_few);
         for (int i = tid; i < pairs * parts; i += FRONT_THREADS) {
             const int pair = i / parts, part = i - pair * parts;
             const int j0 = (int)((long long)tiles * part / parts), j1 = (int)((long long)tiles * (part + 1) / parts);
             put_unit(P.units, i, Unit{-1, 0, pair * PAIR, min(PAIR, packed - pair * PAIR), 0, 0, j0, j1 - j0, 0, pair * parts, parts, part});
         }
-        if (tid == 0) P.head[0] = pairs * parts;
+        if (tid == 0) {
+            P.head[0] = pairs * parts;
+            P.head[1] = parts;
+            P.head[2] = P.sms - ctas;
+            P.head[3] = ctas;
+        }
         return;
     }
     int mine = 0;
@@ -169,7 +188,10 @@ __device__ void plan(const FrontParams &P) {
     __syncthreads();
     const long long upto = paged_scan<FRONT_THREADS>((long long)n_level, sums);
     level[tid] = (int)upto - n_level;
-    if (tid == 0) P.head[0] = min((int)sums[FRONT_THREADS / 32 - 1], P.max_units);
+    if (tid == 0) {
+        P.head[0] = min((int)sums[FRONT_THREADS / 32 - 1], P.max_units);
+        P.head[3] = P.sms;
+    }
     __syncthreads();
     for (int i = tid; i < pairs; i += FRONT_THREADS) {
         const int s = seq_of(i), pair = i - pair0[s], n = seq_n[s], len = seq_len[s], t = pair_tiles(P, n, len, pair);
@@ -335,7 +357,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TcParams P) {
     using M = Map<D>;
     constexpr uint32_t QK = IDESC_QK, PV = (IDESC_PV & ~(0x3Fu << 17)) | ((D >> 3) << 17);
-    pc_grid_dep_launch();
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - smem_u32(smem_raw));
@@ -365,7 +386,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    if (warp == 0) pc_grid_dep_wait();                        // warp 0 alone reads what the launch before has left: the units, and by TMA the queries
+    if (warp == 0) {                                          // it alone reads what the launch before has left: the units, and by TMA the queries
+        pc_grid_dep_wait();
+        pc_grid_dep_launch();                                 // behind the wait: the few-row kernel that runs beside this one looks at the plan without a wait of its own
+    }
 
     // Steps are counted through all units (gs), units by un.  A warp's look at unit un:
     const auto look = [&](int un, bool &alive) {
@@ -383,9 +407,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         int un = 0;
         // The next unit of the list is told to the others, and its first tile is this warp's next
         int j = 0, j_end = 0, uh = 0, us = 0, uown = 0, uq = 0, urows = 0;
-        const int n_units = __ldcg(P.head) * P.n_kv;          // a unit of the list times the KV heads, heads side by side
+        const int n_units = __ldcg(P.head) * P.n_kv, ctas = __ldcg(P.head + 3);          // a unit of the list times the KV heads, heads side by side
         const auto next_unit = [&]() {
-            const int idx = unit_of(un, n_units), i = max(idx, 0) / P.n_kv;
+            const int idx = unit_of(un, ctas, n_units), i = max(idx, 0) / P.n_kv;
             int4 a = make_int4(0, 0, 0, 0), b = a, c = a;
             if (idx >= 0) {
                 a = __ldcg(P.units + 3 * i);
@@ -727,14 +751,12 @@ size_t pc_paged_tc_units(const pc_ctx *ctx) { return ((size_t)ctx->desc.max_q * 
 size_t pc_paged_tc_slots(const pc_ctx *ctx) { return (size_t)2 * ctx->sm_count; }
 size_t pc_paged_tc_plan_bytes(const pc_ctx *ctx) { return PLAN_HEAD * sizeof(int) + pc_paged_tc_units(ctx) * sizeof(Unit); }
 
-// Parts of the shared prefix's keys for a call's rows, 0 where the scratch does not hold them
-int pc_paged_tc_prefix_parts(const pc_ctx *ctx, const PagedBatch &B) {
-    const long long pairs = ((long long)B.n_rows * ctx->group + PAIR - 1) / PAIR, items = pairs * ctx->desc.n_kv_heads;
-    if (items == 0 || items > (long long)pc_paged_tc_slots(ctx)) return 0;
-    return (int)std::max(1LL, std::min<long long>(ctx->sm_count / items, (B.n_prefix + TILE - 1) / TILE));
+// Whether the scratch holds the pieces of a shared prefix for a call's rows
+bool pc_paged_tc_holds(const pc_ctx *ctx, const PagedBatch &B) {
+    return ((long long)B.n_rows * ctx->group + PAIR - 1) / PAIR * ctx->desc.n_kv_heads <= (long long)pc_paged_tc_slots(ctx);
 }
 
-pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int prefix_parts, PagedTcParts *left, cudaStream_t stream) {
+pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool shared, int few_block, PagedTcParts *left, cudaStream_t stream) {
     const pc_ctx *ctx = A.ctx;
     const pc_layer_desc &D = ctx->desc;
     const long long head_rows = (long long)A.batch.n_rows * ctx->group;
@@ -757,8 +779,8 @@ pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int pref
     F.d = D.head_dim;
     F.head_rows = head_rows;
     F.scale = pc_q_rot_scale(D.head_dim);
-    F.shared = prefix_parts > 0;
-    F.shared_parts = prefix_parts;
+    F.shared = shared;
+    F.few_block = few_block;
     F.sms = ctx->sm_count;
     F.max_units = (int)pc_paged_tc_units(ctx);
     F.n_tickets = (int)pc_paged_tc_slots(ctx) * 8;
@@ -772,7 +794,7 @@ pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int pref
     P.n_q_heads = D.n_q_heads;
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
-    P.shared = prefix_parts > 0;
+    P.shared = shared;
     P.head_rows = (int)head_rows;
     P.out = static_cast<__nv_bfloat16 *>(A.out);
     P.lse = A.lse;
@@ -783,6 +805,6 @@ pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, int pref
     P.tickets = w->tc_tickets;
     P.wait_us = ctx->wait_limit_us;
     P.extra_tx = ctx->test_extra_tx;
-    if (left) *left = PagedTcParts{w->tc_o, w->tc_ml, prefix_parts};
+    if (left) *left = PagedTcParts{w->tc_o, w->tc_ml, F.head};
     return D.head_dim == 128 ? launch_tc<128>(ctx, mq, mk, mv, P, stream) : launch_tc<64>(ctx, mq, mk, mv, P, stream);
 }
