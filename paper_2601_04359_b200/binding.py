@@ -78,6 +78,15 @@ class pc_device_workspace(C.Structure):
                 ("sel_idx", C.c_void_p), ("out", C.c_void_p)]
 
 
+class pc_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_tokens", C.c_int32)]
+
+
+class pc_batch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("length", C.c_void_p), ("row_start", C.c_void_p), ("prefix", C.c_void_p), ("n_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("n_prefix", C.c_int32), ("max_rows", C.c_int32)]
+
+
 STAGES = ["qpool", "score", "select", "pack", "rope", "attend", "combine", "mass"]
 
 
@@ -167,6 +176,8 @@ def load() -> C.CDLL:
     lib.pc_q4_destroy.argtypes = [C.c_void_p]
     lib.pc_paged_create.argtypes = [C.c_void_p, C.POINTER(C.c_void_p)]
     lib.pc_paged_destroy.argtypes = [C.c_void_p]
+    lib.pc_paged_append.argtypes = [C.c_void_p, C.POINTER(pc_pages), C.POINTER(pc_batch), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+    lib.pc_paged_attend.argtypes = [C.c_void_p, C.POINTER(pc_pages), C.POINTER(pc_batch), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.pc_accumulate.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
     _lib = lib
     return lib

@@ -6,10 +6,11 @@
 
 namespace {
 
-// A warp per row and up to 8 chunks a lane: a chunk is eight channels (16 bytes, 32 in fp32), whole rotary pairs, and all chunks of a lane lie at the same place
-// of a head (256 is a multiple of d), so four table entries serve them.  Keys and values are requested first; what they wait for behind that is where they go: the
-// row's sequence (a search by all lanes at once, two looks at most), its length, its page.
-constexpr int APPEND_THREADS = 256;
+// Bound by memory: 4,096 bytes a token of 8 KV heads x 128 channels in bf16 come in and as many go out.  What stands between the two is where a row goes: its sequence, whose length and page.  So a
+// CTA has the sequences' row starts and lengths in shared memory, a warp looks its rows up there, a lane a row, and asks for their pages and positions together; the first row's keys and values are
+// asked for ahead of all that, the next row's while a row is turned and stored.  (8,064 tokens 14.5 us, 4.6 TB/s with the launch, 16,965 26.3, 5.3 TB/s; with rows that looked for everything themselves, one thing after the other, 14.9 and 31.8.)
+// A chunk is eight channels (16 bytes, 32 in fp32), whole rotary pairs; all chunks of a lane lie at the same place of a head (256 is a multiple of d), so four table entries serve them.
+constexpr int APPEND_THREADS = 128, APPEND_WARPS = APPEND_THREADS / 32;
 
 struct AppendParams {
     PagedBatch B;
@@ -17,6 +18,8 @@ struct AppendParams {
     const int32_t *pos;
     char *pool_k, *pool_v;
     int chunks;              // of a row
+    int passes;              // of 32 CPL chunks that a row takes
+    int per;                 // rows of a warp, up to 32
 };
 
 template <bool F32> struct Chunk { uint4 a[F32 ? 2 : 1]; };
@@ -48,69 +51,90 @@ template <bool F32> __device__ __forceinline__ void store_chunk(char *p, const C
 }
 
 template <bool F32, int CPL /* chunks of a lane at a time */>
-__global__ void __launch_bounds__(APPEND_THREADS) k_paged_append(const __grid_constant__ AppendParams P, const pc_rope_dev rope, int d) {
+__global__ void __launch_bounds__(APPEND_THREADS) k_paged_append(const __grid_constant__ AppendParams P, const __grid_constant__ pc_rope_dev rope, int d) {
     constexpr int BYTES = F32 ? 32 : 16;
+    __shared__ int starts[PC_MAX_SEQS + 1], lengths[PC_MAX_SEQS];
     pc_grid_dep_launch();
-    const int lane = threadIdx.x & 31, row = (blockIdx.x * APPEND_THREADS + threadIdx.x) >> 5;
-    pc_grid_dep_wait();
     const PagedBatch &B = P.B;
-    if (row >= B.n_rows) return;
+    const int lane = threadIdx.x & 31, row0 = (blockIdx.x * APPEND_WARPS + (threadIdx.x >> 5)) * P.per, n = min(P.per, B.n_rows - row0);
     const size_t width = (size_t)P.chunks * BYTES;
-    const char *k = P.k + row * width, *v = P.v + row * width;
-    Chunk<F32> ck[CPL], cv[CPL];
-    const auto load = [&](int c0) {
+    pc_grid_dep_wait();
+    struct Piece { Chunk<F32> k[CPL], v[CPL]; };           // what a warp moves at once: a row, or a part of a wide one
+    const auto load = [&](Piece &x, int item) {
+        const int i = item / P.passes, c0 = (item - i * P.passes) * CPL * 32 + lane;
+        const size_t at = (size_t)(row0 + i) * width;
 #pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-            const int c = c0 + i * 32 + lane;
+        for (int u = 0; u < CPL; ++u) {
+            const int c = c0 + u * 32;
             if (c < P.chunks) {
-                ck[i] = load_chunk<F32>(k + (size_t)c * BYTES);
-                cv[i] = load_chunk<F32>(v + (size_t)c * BYTES);
+                x.k[u] = load_chunk<F32>(P.k + at + (size_t)c * BYTES);
+                x.v[u] = load_chunk<F32>(P.v + at + (size_t)c * BYTES);
             }
         }
     };
-    load(0);
-    // the row's sequence: the last that begins at or before it
-    const int stride = (B.n_seqs + 31) / 32;
-    const int at0 = lane * stride;
-    int s = __popc(__ballot_sync(0xffffffffu, at0 < B.n_seqs && __ldcg(B.row_start + at0) <= row)) - 1;
-    if (s >= 0 && stride > 1) {
-        const int at1 = s * stride + lane;
-        s = s * stride + __popc(__ballot_sync(0xffffffffu, lane < stride && at1 < B.n_seqs && __ldcg(B.row_start + at1) <= row)) - 1;
+    const int items = max(0, n) * P.passes;
+    Piece x, y;
+    if (items > 0) load(x, 0);
+    int4 pos = make_int4(0, 0, 0, 0);
+    if (lane < n) pos = __ldcg(reinterpret_cast<const int4 *>(P.pos) + row0 + lane);
+    for (int s = threadIdx.x; s <= B.n_seqs; s += APPEND_THREADS) {
+        starts[s] = __ldcg(B.row_start + s);
+        if (s < B.n_seqs) lengths[s] = __ldcg(B.length + s);
     }
-    if (s < 0) return;                                     // ahead of the first sequence: nobody's
-    const PagedSeq S = paged_seq(B, s);
-    if (row - S.r0 >= S.n) return;                         // behind the last
-    const int slot = S.len - S.n + (row - S.r0);
-    if (slot < 0) {                                        // more rows than tokens
-        if (lane == 0) pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_ROWS);
-        return;
-    }
-    const int page = __ldcg(B.table + (size_t)s * B.max_pages + (slot >> B.page_shift));
-    if (page < 0 || page >= B.n_pages) {
-        if (lane == 0) pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_TABLE);
-        return;
-    }
-    const size_t to = (((size_t)page << B.page_shift) + (slot & ((1 << B.page_shift) - 1))) * width;
-    const int4 pos = __ldcg(reinterpret_cast<const int4 *>(P.pos) + row);
-    float2 cs[4];
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) cs[i] = pc_rope_cs_clamped(rope, ((lane * 8) % d) / 2 + i, pos.x, pos.y, pos.z, bad);
-    if (bad) pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
-    for (int c0 = 0;;) {
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-            const int c = c0 + i * 32 + lane;
-            if (c < P.chunks) {
-                turn_chunk<F32>(ck[i], cs);
-                store_chunk<F32>(P.pool_k + to + (size_t)c * BYTES, ck[i]);
-                store_chunk<F32>(P.pool_v + to + (size_t)c * BYTES, cv[i]);
+    __syncthreads();
+    // a lane's row: its sequence is the last that begins at or before it; -1: the row goes nowhere
+    long long to = -1;
+    if (lane < n) {
+        const int row = row0 + lane;
+        int lo = -1, hi = B.n_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (starts[mid] <= row) lo = mid; else hi = mid - 1;
+        }
+        if (lo >= 0) {                                     // (ahead of the first sequence: nobody's)
+            const PagedSeq S = paged_seq_of(B, starts[lo], starts[lo + 1], lengths[lo]);
+            const int slot = S.len - S.n + (row - S.r0);
+            if (row - S.r0 >= S.n) {                       // behind the last
+            } else if (slot < 0) {                         // more rows than tokens
+                pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_ROWS);
+            } else {
+                const int page = __ldcg(B.table + (size_t)lo * B.max_pages + (slot >> B.page_shift));
+                if (page < 0 || page >= B.n_pages) pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_TABLE);
+                else to = ((long long)page << B.page_shift) + (slot & ((1 << B.page_shift) - 1));
             }
         }
-        c0 += CPL * 32;
-        if (c0 >= P.chunks) break;
-        load(c0);
     }
+    float2 cs[4];
+    bool bad = false;
+    const auto move = [&](Piece &x, int item) {
+        const int i = item / P.passes, pass = item - i * P.passes;
+        const long long place = __shfl_sync(0xffffffffu, to, i);
+        if (place < 0) return;
+        if (pass == 0) {
+            const int pt = __shfl_sync(0xffffffffu, pos.x, i), ph = __shfl_sync(0xffffffffu, pos.y, i), pw = __shfl_sync(0xffffffffu, pos.z, i);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) cs[u] = pc_rope_cs_clamped(rope, ((lane * 8) % d) / 2 + u, pt, ph, pw, bad);
+        }
+        const size_t at = (size_t)place * width;
+#pragma unroll
+        for (int u = 0; u < CPL; ++u) {
+            const int c = pass * CPL * 32 + u * 32 + lane;
+            if (c < P.chunks) {
+                turn_chunk<F32>(x.k[u], cs);
+                store_chunk<F32>(P.pool_k + at + (size_t)c * BYTES, x.k[u]);
+                store_chunk<F32>(P.pool_v + at + (size_t)c * BYTES, x.v[u]);
+            }
+        }
+    };
+#pragma unroll 1
+    for (int item = 0; item < items; item += 2) {
+        if (item + 1 < items) load(y, item + 1);
+        move(x, item);
+        if (item + 1 >= items) break;
+        if (item + 2 < items) load(x, item + 2);
+        move(y, item + 1);
+    }
+    if (bad) pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_POS);
 }
 
 int log2_of(int x) {
@@ -156,7 +180,12 @@ extern "C" pc_status pc_paged_append(pc_ctx *ctx, const pc_pages *pages, const p
     P.pool_v = static_cast<char *>(pages->v);
     P.chunks = D.n_kv_heads * D.head_dim / 8;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const dim3 grid((unsigned)(((long long)n_rows * 32 + APPEND_THREADS - 1) / APPEND_THREADS)), block(APPEND_THREADS);
+    P.passes = (P.chunks + 32 * (D.dtype == PC_F32 ? 2 : 4) - 1) / (32 * (D.dtype == PC_F32 ? 2 : 4));
+    // Rows of a warp: as many as let the call run in one wave of sixteen warps an SM, four at most (8,064 rows: one 18.0 us, two 14.3, three in two waves 16.8, four 14.5; 16,965: one 34, four
+    // 26.3, eight 27.2).
+    P.per = (int)std::min<long long>(4, std::max<long long>(1, (n_rows + 16ll * ctx->sm_count - 1) / (16ll * ctx->sm_count)));
+    const int rows = APPEND_WARPS * P.per;
+    const dim3 grid((unsigned)((n_rows + (long long)rows - 1) / rows)), block(APPEND_THREADS);
     if (D.dtype == PC_F32) PC_LAUNCH((k_paged_append<true, 2>), grid, block, 0, stream, P, ctx->rope, D.head_dim);
     else PC_LAUNCH((k_paged_append<false, 4>), grid, block, 0, stream, P, ctx->rope, D.head_dim);
     return PC_OK;

@@ -14,14 +14,14 @@ struct PagedBatch {
 struct PagedSeq { int r0, n, len; };          // first row, rows, own tokens
 
 // A sequence whose numbers make no sense is recorded and has no rows.
-__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch &B, int s) {
-    const int r0 = __ldcg(B.row_start + s), r1 = __ldcg(B.row_start + s + 1), len = __ldcg(B.length + s);
+__device__ __forceinline__ PagedSeq paged_seq_of(const PagedBatch &B, int r0, int r1, int len) {
     if (r0 < 0 || r1 < r0 || r1 > B.n_rows || r1 - r0 > B.max_rows || len < 0 || (long long)len > ((long long)B.max_pages << B.page_shift)) {
         pc_flag(B.status, PC_ERR_INVALID_ARG, PC_WHERE_PAGED_ROWS);
         return {0, 0, 0};
     }
     return {r0, r1 - r0, len};
 }
+__device__ __forceinline__ PagedSeq paged_seq(const PagedBatch &B, int s) { return paged_seq_of(B, __ldcg(B.row_start + s), __ldcg(B.row_start + s + 1), __ldcg(B.length + s)); }
 // rows of the whole batch
 __device__ __forceinline__ int paged_rows(const PagedBatch &B) { return min(max(__ldcg(B.row_start + B.n_seqs), 0), B.n_rows); }
 // A page from a table; one that the pool does not have is recorded and read as its nearest.

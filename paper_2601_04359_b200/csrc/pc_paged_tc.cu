@@ -11,7 +11,8 @@
 // in registers, running maximum and sum in fp32, probabilities as bf16 into tensor memory in two halves, O rescaled only where the maximum grew by more than 2^8.  (The division of labour is that of the frame
 // kernel, k_attend_tc.)
 // Rows behind a segment's end: scores are replaced by -infinity whatever they are, and the values' rows are cleared in shared memory, since 0 times what lies
-// there may be NaN.
+// there may be NaN.  Values of a causal tile that some rows see and others do not are looked through by warp 3 while the softmax works: infinite and NaN ones are taken out of the product and added, in tensor
+// memory, to the rows that see them.
 // Tried: queries rotated in this kernel, by four warps more.  Their chains of shuffles, addresses and products are 1,000 instructions a tile at five to ten cycles, 7 us, where a unit of three key tiles takes 4.6:
 // packed prompts 227 us a call instead of 89.  And key tiles shared out evenly along one line, with items of two CTAs added up by one of them: 98 us, since every CTA ends with such an item.
 #include <algorithm>
@@ -52,7 +53,7 @@ template <int D> struct Map {
 };
 enum { BAR_QF = 0 /* [place]: queries are there */, BAR_QE = 3 /* [place]: and have been read */, BAR_K0 = 6, BAR_KV = 7 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 9 /* [step & 1] */,
        BAR_SFULL = 11 /* [tile] */, BAR_SFREE = 13 /* [tile] */, BAR_PHALF = 15 /* [tile][half] */, BAR_PVDONE = 19 /* [tile] */, BAR_DONE = 21, BAR_UF = 22 /* [unit & 3]: told */,
-       BAR_UE = 26 /* [unit & 3]: taken by all */, N_BARS = 30 };
+       BAR_UE = 26 /* [unit & 3]: taken by all */, BAR_SCAN = 30 /* a unit's values have been looked through */, N_BARS = 31 };
 static_assert(N_BARS * 8 <= 256, "barriers");
 constexpr int UNIT_READERS = 11;                   // warps 1 to 11
 constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
@@ -60,6 +61,7 @@ constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
 struct TcParams {
     PagedBatch B;
     int n_q_heads, n_kv, group;
+    const __nv_bfloat16 *pool_v;
     int head_rows;           // rows of a KV head among the rotated queries
     int shared;              // the prefix alone, rows of all sequences; what comes out goes to scratch row by row for k_paged_join
     __nv_bfloat16 *out;
@@ -321,6 +323,57 @@ template <int D> __device__ __noinline__ void add_up(const TcParams &P, Unit U, 
     if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
 }
 
+// Infinite and NaN values of rows first .. last - 1 of a tile in shared memory become zero; whether there were any
+template <int HALVES> __device__ __forceinline__ bool take_out_odd(uint32_t tile, int first, int last, int lane) {
+    bool odd = false;
+#pragma unroll 1
+    for (int half = 0; half < HALVES; ++half)
+#pragma unroll 1
+        for (int c0 = first * 8 + lane; c0 < last * 8; c0 += 8 * 32) {
+            uint4 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = pc_lds128(tile + half * HALF_BYTES + min(c0 + 32 * u, last * 8 - 1) * 16);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                bool some = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) some |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
+                if (__builtin_expect(some && c0 + 32 * u < last * 8, 0)) {
+                    odd = true;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+                    sts128(tile + half * HALF_BYTES + (c0 + 32 * u) * 16, w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+    odd = __any_sync(0xffffffffu, odd);
+    if (odd) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+    }
+    return odd;
+}
+// What take_out_odd has left out of a unit's products, added to the rows of a warp that see it (a whole warp calls; the unit's products are done).  The values are looked for in the pool: this is rare.
+template <int D> __device__ __noinline__ void add_odd(const TcParams &P, Unit U, int t, int r, uint32_t o_addr) {
+    const PagedBatch &B = P.B;
+    const int prefix_tiles = tiles_of(B.n_prefix), row = U.p0 + min(t * TILE + r, U.rows - 1), sees = min(U.own, U.before + row / P.group + 1);
+    const int first = max(0, max(U.before + U.p0 / P.group + 1, (U.j0 - prefix_tiles) * TILE)), last = min(U.own, (U.j0 + U.nj - prefix_tiles) * TILE);
+    for (int key = first; key < last; ++key) {
+        const size_t at = (((size_t)paged_page(B, B.table + (size_t)U.s * B.max_pages + (key >> B.page_shift)) << B.page_shift) + (key & ((1 << B.page_shift) - 1))) * P.n_kv + U.h;
+        for (int c = 0; c < D; ++c) {
+            const float v = __bfloat162float(P.pool_v[at * D + c]);
+            if (fabsf(v) < INFINITY) continue;
+            uint32_t o;
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_addr + c));
+            tmem_wait_ld();
+            if (key < sees) o = __float_as_uint(__uint_as_float(o) + v);
+            tmem_st1(o_addr + c, o);
+            tmem_wait_st();
+        }
+    }
+}
+
 // A thread's row of a unit (v: D fp32 values, not yet divided by their sum) leaves: whole items to the output, parts to scratch, and the last part to come adds them up
 template <int D> __device__ __forceinline__ void put_out(const TcParams &P, const Unit &U, const uint32_t (&v)[D], float m, float l, int t, int quad, int lane) {
     const int r = quad * 32 + lane;
@@ -363,13 +416,14 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + M::FLAGS);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(gen + M::FLAGS + 4);
     int4 *told = reinterpret_cast<int4 *>(gen + M::UNIT);
+    volatile int *odd_units = reinterpret_cast<volatile int *>(gen + M::FLAGS + 16);         // [unit & 3]: values were taken out of its products
     const uint32_t bar0 = base + M::BAR;
     auto bar = [&](int i) { return bar0 + 8u * i; };
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < N_BARS; ++i) {
             const bool by_warps = (i >= BAR_QE && i < BAR_K0) || (i >= BAR_EMPTY && i < BAR_SFULL) || (i >= BAR_SFREE && i < BAR_PVDONE);        // of the four of one tile's softmax
-            mbar_init(bar(i), by_warps ? 4 : (i == BAR_DONE ? 3 : (i >= BAR_UE ? UNIT_READERS : 1)));
+            mbar_init(bar(i), by_warps ? 4 : (i == BAR_DONE ? 3 : (i >= BAR_UE && i < BAR_SCAN ? UNIT_READERS : 1)));
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -542,16 +596,26 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 }
             } else {
                 const uint64_t dv0 = desc_mnmajor(base + M::V);
+                bool odd = false;
 #pragma unroll 1
                 for (int i = 0; i < U.nj && alive; ++i, ++gs) {
                     const int st = gs & 1, in = U.j0 + i - prefix_tiles;
                     alive = wait(BAR_KV + st, (gs >> 1) & 1);
                     if (!alive) break;
                     const int n = in < 0 ? B.n_prefix - (U.j0 + i) * TILE : max(0, U.own - in * TILE);
+                    const int hidden = B.causal && in >= 0 ? max(0, U.before + U.p0 / P.group + 1 - in * TILE) : TILE;           // first key that not every row sees
+                    if (hidden < min(n, TILE)) odd |= take_out_odd<M::HALVES>(base + M::V + st * M::TILE_B, hidden, min(n, TILE), lane);
                     if (n < TILE) {                               // values behind the segment's end are whatever the pool holds there
                         for (int hf = 0; hf < M::HALVES; ++hf)
                             for (int c = n * 8 + lane; c < TILE * 8; c += 32) sts128(base + M::V + st * M::TILE_B + hf * HALF_BYTES + c * 16, 0u, 0u, 0u, 0u);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (i + 1 == U.nj) {
+                        if (lane == 0) {
+                            odd_units[un & (UNITS - 1)] = odd;
+                            mbar_arrive(bar(BAR_SCAN));
+                        }
                         __syncwarp();
                     }
 #pragma unroll 1
@@ -693,6 +757,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 l += (la.x + la.y) + (lb.x + lb.y);
             }
             if (__builtin_expect(flush, 0)) {
+                alive = warp_wait(bar(BAR_SCAN), (un - 1) & 1, abort_flag, B.status, P.wait_us);
+                if (!alive) break;
+                if (__builtin_expect(odd_units[(un - 1) & (UNITS - 1)], 0)) add_odd<D>(P, V, t, r, o_addr);
                 uint32_t v[D];
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
@@ -707,8 +774,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         }
         if (alive && U.nj > 0) {                              // the last unit
             alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
+            alive = alive && warp_wait(bar(BAR_SCAN), (un - 1) & 1, abort_flag, B.status, P.wait_us);
             if (alive) {
                 tc_fence_after();
+                if (__builtin_expect(odd_units[(un - 1) & (UNITS - 1)], 0)) add_odd<D>(P, U, t, r, o_addr);
                 uint32_t v[D];
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) tmem_ld32(o_addr + c * 32, v + c * 32);
@@ -795,6 +864,7 @@ pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool sha
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
     P.shared = shared;
+    P.pool_v = static_cast<const __nv_bfloat16 *>(A.pages->v);
     P.head_rows = (int)head_rows;
     P.out = static_cast<__nv_bfloat16 *>(A.out);
     P.lse = A.lse;

@@ -115,17 +115,19 @@ class Paged:
             spread = seen_v(vs.abs()) * (torch.expm1(2 * delta).T[..., None] + 2.0 ** -18 + (2.0 ** -8 if bf else 0.0) + (len(at) / 16 + 8) * (1 if bf else 6) * 2.0 ** -22)
             out[i0:i0 + r], lse[i0:i0 + r] = o, z.T
             tol[i0:i0 + r] = spread * 1.01 + o.abs() * (2.0 ** -8 if bf else 2.0 ** -24)
-            tol_lse[i0:i0 + r] = delta.T + 2.0 ** -18 * (1 + z.T.abs().nan_to_num(posinf=0.0))
+            tol_lse[i0:i0 + r] = (delta.T + 2.0 ** -18 * (1 + z.T.abs().nan_to_num(posinf=0.0))).nan_to_num()
         return out, lse, tol, tol_lse
 
 
 def compare(got, want):
-    """(out, lse) of a call against Paged.want(): infinities and zeros exactly, the rest within the tolerance; rows that are nobody's are not looked at"""
+    """(out, lse) of a call against Paged.want(): what is infinite, NaN or empty exactly, the rest within the tolerance; rows that are nobody's are not looked at"""
     (out, lse), (o, z, tol, tol_lse) = got, want
     out, lse = out.double().cpu(), lse.double().cpu()
-    mine = ~z.isnan().all(-1)
+    mine = ~tol_lse.isnan().all(-1)
     out, lse, o, z, tol, tol_lse = (x[mine] for x in (out, lse, o, z, tol, tol_lse))
     empty = z == float("-inf")
     assert (out[empty] == 0).all() and (lse[empty] == float("-inf")).all()
-    assert ((out - o).abs() <= tol)[~empty].all(), float(((out - o).abs() / tol)[~empty].max())
-    assert ((lse - z).abs() <= tol_lse)[~empty].all(), float(((lse - z).abs() / tol_lse)[~empty].max())
+    for x, w, t in ((out, o, tol), (lse, z, tol_lse)):
+        fine = w.isfinite()
+        assert torch.equal(x.isnan(), w.isnan()) and torch.equal(x[~fine & ~w.isnan()], w[~fine & ~w.isnan()])
+        assert ((x - w).abs() <= t)[fine].all(), float(((x - w).abs() / t)[fine].max())
