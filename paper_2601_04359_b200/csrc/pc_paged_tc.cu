@@ -53,7 +53,7 @@ template <int D> struct Map {
 };
 enum { BAR_QF = 0 /* [place]: queries are there */, BAR_QE = 3 /* [place]: and have been read */, BAR_K0 = 6, BAR_KV = 7 /* [stage]: values of a step and keys of the next */, BAR_EMPTY = 9 /* [step & 1] */,
        BAR_SFULL = 11 /* [tile] */, BAR_SFREE = 13 /* [tile] */, BAR_PHALF = 15 /* [tile][half] */, BAR_PVDONE = 19 /* [tile] */, BAR_DONE = 21, BAR_UF = 22 /* [unit & 3]: told */,
-       BAR_UE = 26 /* [unit & 3]: taken by all */, BAR_SCAN = 30 /* a unit's values have been looked through */, N_BARS = 31 };
+       BAR_UE = 26 /* [unit & 3]: taken by all */, BAR_SCAN = 30 /* [unit & 1]: its values have been looked through (warp 3 is up to one unit ahead of the softmax) */, N_BARS = 32 };
 static_assert(N_BARS * 8 <= 256, "barriers");
 constexpr int UNIT_READERS = 11;                   // warps 1 to 11
 constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
@@ -323,9 +323,9 @@ template <int D> __device__ __noinline__ void add_up(const TcParams &P, Unit U, 
     if (there && P.lse) P.lse[row] = (m + log2f(sum)) * 0.6931471805599453f;
 }
 
-// Infinite and NaN values of rows first .. last - 1 of a tile in shared memory become zero; whether there were any
+// Infinite and NaN values of rows first .. last - 1 of a tile in shared memory become zero; whether there were any.  They are looked for by the largest magnitude, two numbers at a time.
 template <int HALVES> __device__ __forceinline__ bool take_out_odd(uint32_t tile, int first, int last, int lane) {
-    bool odd = false;
+    uint32_t most = 0;
 #pragma unroll 1
     for (int half = 0; half < HALVES; ++half)
 #pragma unroll 1
@@ -335,24 +335,26 @@ template <int HALVES> __device__ __forceinline__ bool take_out_odd(uint32_t tile
             for (int u = 0; u < 8; ++u) x[u] = pc_lds128(tile + half * HALF_BYTES + min(c0 + 32 * u, last * 8 - 1) * 16);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-                bool some = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) some |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
-                if (__builtin_expect(some && c0 + 32 * u < last * 8, 0)) {
-                    odd = true;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
-                    sts128(tile + half * HALF_BYTES + (c0 + 32 * u) * 16, w[0], w[1], w[2], w[3]);
-                }
+                most = __vmaxu2(most, x[u].x & 0x7FFF7FFFu);
+                most = __vmaxu2(most, x[u].y & 0x7FFF7FFFu);
+                most = __vmaxu2(most, x[u].z & 0x7FFF7FFFu);
+                most = __vmaxu2(most, x[u].w & 0x7FFF7FFFu);
             }
         }
-    odd = __any_sync(0xffffffffu, odd);
-    if (odd) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+    if (__builtin_expect(!__any_sync(0xffffffffu, (most & 0xFFFFu) >= 0x7F80u || most >= 0x7F800000u), 1)) return false;
+#pragma unroll 1
+    for (int c = lane; c < HALVES * (last - first) * 8; c += 32) {
+        const int half = c / ((last - first) * 8);
+        const uint32_t at = tile + half * HALF_BYTES + (first * 8 + c - half * (last - first) * 8) * 16;
+        const uint4 x = pc_lds128(at);
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+        sts128(at, w[0], w[1], w[2], w[3]);
     }
-    return odd;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    return true;
 }
 // What take_out_odd has left out of a unit's products, added to the rows of a warp that see it (a whole warp calls; the unit's products are done).  The values are looked for in the pool: this is rare.
 template <int D> __device__ __noinline__ void add_odd(const TcParams &P, Unit U, int t, int r, uint32_t o_addr) {
@@ -602,10 +604,15 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                     const int st = gs & 1, in = U.j0 + i - prefix_tiles;
                     alive = wait(BAR_KV + st, (gs >> 1) & 1);
                     if (!alive) break;
-                    const int n = in < 0 ? B.n_prefix - (U.j0 + i) * TILE : max(0, U.own - in * TILE);
-                    const int hidden = B.causal && in >= 0 ? max(0, U.before + U.p0 / P.group + 1 - in * TILE) : TILE;           // first key that not every row sees
-                    if (hidden < min(n, TILE)) odd |= take_out_odd<M::HALVES>(base + M::V + st * M::TILE_B, hidden, min(n, TILE), lane);
-                    if (n < TILE) {                               // values behind the segment's end are whatever the pool holds there
+                    // Values that no row of the pair sees (behind the segment's end, or the last row's sight) are whatever the pool holds there, and become zero; those that some rows see and
+                    // others do not are looked through.
+                    int n = in < 0 ? B.n_prefix - (U.j0 + i) * TILE : max(0, U.own - in * TILE);
+                    if (B.causal && in >= 0) {
+                        const int all_see = max(0, U.before + U.p0 / P.group + 1 - in * TILE);
+                        n = min(n, max(0, U.before + (U.p0 + U.rows - 1) / P.group + 1 - in * TILE));
+                        if (all_see < min(n, TILE)) odd |= take_out_odd<M::HALVES>(base + M::V + st * M::TILE_B, all_see, min(n, TILE), lane);
+                    }
+                    if (n < TILE) {
                         for (int hf = 0; hf < M::HALVES; ++hf)
                             for (int c = n * 8 + lane; c < TILE * 8; c += 32) sts128(base + M::V + st * M::TILE_B + hf * HALF_BYTES + c * 16, 0u, 0u, 0u, 0u);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -614,7 +621,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                     if (i + 1 == U.nj) {
                         if (lane == 0) {
                             odd_units[un & (UNITS - 1)] = odd;
-                            mbar_arrive(bar(BAR_SCAN));
+                            mbar_arrive(bar(BAR_SCAN + (un & 1)));
                         }
                         __syncwarp();
                     }
@@ -757,7 +764,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 l += (la.x + la.y) + (lb.x + lb.y);
             }
             if (__builtin_expect(flush, 0)) {
-                alive = warp_wait(bar(BAR_SCAN), (un - 1) & 1, abort_flag, B.status, P.wait_us);
+                alive = warp_wait(bar(BAR_SCAN + ((un - 1) & 1)), ((un - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
                 if (!alive) break;
                 if (__builtin_expect(odd_units[(un - 1) & (UNITS - 1)], 0)) add_odd<D>(P, V, t, r, o_addr);
                 uint32_t v[D];
@@ -774,7 +781,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         }
         if (alive && U.nj > 0) {                              // the last unit
             alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
-            alive = alive && warp_wait(bar(BAR_SCAN), (un - 1) & 1, abort_flag, B.status, P.wait_us);
+            alive = alive && warp_wait(bar(BAR_SCAN + ((un - 1) & 1)), ((un - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
             if (alive) {
                 tc_fence_after();
                 if (__builtin_expect(odd_units[(un - 1) & (UNITS - 1)], 0)) add_odd<D>(P, U, t, r, o_addr);
