@@ -246,40 +246,40 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
         pair_n[e] = axis(a, rope.n_axis[0], rope.n_axis[1], rope.n_axis[2]);
         pair_at[e] = axis(a, rope.off[0], rope.off[1], rope.off[2]) + pair / 3;
     }
+    // all rows (the last one again where there are fewer) and their table entries are asked for at once: what this takes is their latency
+    uint32_t raw[NB * 8][F32 ? E : E / 2];
+    float2 cs[NB * 8][PAIRS];
+#pragma unroll
+    for (int r = 0; r < NB * 8; ++r) {
+        const size_t row = (size_t)__shfl_sync(0xffffffffu, my_row, r) * D + lane * E;
+        const int pt = __shfl_sync(0xffffffffu, my_t, r), ph = __shfl_sync(0xffffffffu, my_h, r), pw = __shfl_sync(0xffffffffu, my_w, r);
+        if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const float *>(P.q) + row + e));
+                raw[r][e] = y.x;
+                raw[r][e + 1] = y.y;
+            }
+        } else if constexpr (E == 4) {
+            const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
+            raw[r][0] = y.x;
+            raw[r][1] = y.y;
+        } else {
+            raw[r][0] = __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
+        }
+#pragma unroll
+        for (int e = 0; e < PAIRS; ++e) cs[r][e] = __ldg(rope.tab + (pair_at[e] + axis(pair_axis[e], pt, ph, pw) * pair_n[e]));
+    }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         __syncwarp();
-        // all eight rows (the last one again where there are fewer) and their table entries are asked for at once: what this takes is their latency
-        uint32_t raw[8][F32 ? E : E / 2];
-        float2 cs[8][PAIRS];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const int from = nb * 8 + r;
-            const size_t row = (size_t)__shfl_sync(0xffffffffu, my_row, from) * D + lane * E;
-            const int pt = __shfl_sync(0xffffffffu, my_t, from), ph = __shfl_sync(0xffffffffu, my_h, from), pw = __shfl_sync(0xffffffffu, my_w, from);
-            if constexpr (F32) {
-#pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const float *>(P.q) + row + e));
-                    raw[r][e] = y.x;
-                    raw[r][e + 1] = y.y;
-                }
-            } else if constexpr (E == 4) {
-                const uint2 y = __ldcg(reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
-                raw[r][0] = y.x;
-                raw[r][1] = y.y;
-            } else {
-                raw[r][0] = __ldcg(reinterpret_cast<const uint32_t *>(static_cast<const __nv_bfloat16 *>(P.q) + row));
-            }
-#pragma unroll
-            for (int e = 0; e < PAIRS; ++e) cs[r][e] = __ldg(rope.tab + (pair_at[e] + axis(pair_axis[e], pt, ph, pw) * pair_n[e]));
-        }
 #pragma unroll
         for (int r = 0; r < 8; ++r)
 #pragma unroll
             for (int e = 0; e < PAIRS; ++e) {              // row r: D values, 16-byte pieces at their number ^ r
-                float2 y = F32 ? make_float2(__uint_as_float(raw[r][2 * e]), __uint_as_float(raw[r][F32 ? 2 * e + 1 : 0])) : make_float2(pc_bf16_lo(raw[r][e]), pc_bf16_hi(raw[r][e]));
-                y = pc_rotate(y.x, y.y, cs[r][e]);
+                const uint32_t(&w)[F32 ? E : E / 2] = raw[nb * 8 + r];
+                float2 y = F32 ? make_float2(__uint_as_float(w[F32 ? 2 * e : e]), __uint_as_float(w[F32 ? 2 * e + 1 : 0])) : make_float2(pc_bf16_lo(w[e]), pc_bf16_hi(w[e]));
+                y = pc_rotate(y.x, y.y, cs[nb * 8 + r][e]);
                 const int c = lane * E + 2 * e;
                 if constexpr (F32) sts64(W.q + r * D * 4 + (((c >> 2) ^ r) << 4) + (c & 3) * 4, __float_as_uint(__fmul_rn(y.x, P.scale)), __float_as_uint(__fmul_rn(y.y, P.scale)));
                 else sts32(W.q + r * D * 2 + (((c >> 3) ^ r) << 4) + (c & 7) * 2, pc_pack_bf16(__fmul_rn(y.x, P.scale), __fmul_rn(y.y, P.scale)));
@@ -483,7 +483,7 @@ __device__ __forceinline__ void take_unit(const FewParams &P, const pc_rope_dev 
             if (eighth == 0) sts64(W.q + (nb * 8 + quad * 2 + e) * 8, __float_as_uint(m[nb][e]), __float_as_uint(l[nb][e]));
         }
     __syncwarp();
-#pragma unroll 2
+#pragma unroll 4
     for (int r = 0; r < n_rows; ++r) {
         const float2 y = lds64(W.q + r * 8);
         const float mr = y.x, lr = y.y;
