@@ -1,0 +1,120 @@
+"""Several samples of one prompt generated together over a paged cache (synthetic lumos-shaped layer).
+
+    python -m paper_2601_04359_b200.samples [--samples 8] [--frames 3] [--tokens 4] [--grid 24 42] [--heads 24 8] [--page 64] [--reps 10]
+
+The prompt (text and a conditioning image) enters the cache once and attends to itself (pc_paged_append, pc_paged_attend, causal).  Then all samples go on
+together over that prefix, each in pages of its own that it is given as it grows: per frame, the frame's keys and values are appended and its queries see everything their sample has (not causal); then a few
+text tokens are generated one at a time.  One JSON line: times of a prompt, a frame step, a token (append and attention, CUDA events over repeated calls), bytes of the cache and
+what the samples would hold without the shared prefix, and how far the last token's output of one sample is from pc_attend_frame over the same tokens."""
+from __future__ import annotations
+
+import argparse
+import json
+
+import torch
+
+from . import binding as pc
+from .four_bits import T_STEP, _positions, _time
+
+
+class Growing:
+    """Lengths and pages of the samples: pages are handed out as tokens come.  Kept on the host, and brought to the GPU where a step changes them."""
+
+    def __init__(self, samples, most, page, free):
+        self.page, self.free, self.length = page, free, [0] * samples
+        self.table = torch.zeros(samples, -(-most // page), dtype=torch.int32)
+        self.on_gpu = self.table.cuda()
+
+    def grow(self, rows):
+        """Every sample gets `rows` more tokens; the batch that brings them"""
+        n = len(self.length)
+        for s in range(n):
+            for p in range(-(-self.length[s] // self.page), -(-(self.length[s] + rows) // self.page)):
+                self.table[s, p] = self.free.pop()
+            self.length[s] += rows
+        self.on_gpu.copy_(self.table)
+        return pc.Batch(self.on_gpu, torch.tensor(self.length, dtype=torch.int32, device="cuda"), torch.arange(n + 1, dtype=torch.int32, device="cuda") * rows, rows)
+
+
+def generate(samples=8, frames=3, tokens=4, grid=(24, 42), heads=(24, 8), page=64, n_text=128, reps=10, seed=0):
+    """Runs the loop; returns what the command prints."""
+    hq, hkv = heads
+    d, n = 128, grid[0] * grid[1]
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n_prompt, most = n_text + n, frames * (n + tokens)
+    ctx = pc.Context(hq, hkv, d, pc.PC_BF16, 10000.0, (n_text + T_STEP * (frames + 2), max(n_text, 8 * grid[0]), max(n_text, 8 * grid[1])), max(n_prompt, samples * n), n_prompt + most)
+    work = pc.PagedWork(ctx)
+    n_pages = -(-n_prompt // page) + samples * -(-most // page)
+    pool = pc.Pages.empty(ctx, n_pages, page)
+    free = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).tolist()
+    prefix = torch.tensor([free.pop() for _ in range(-(-n_prompt // page))], dtype=torch.int32, device="cuda")
+
+    def rows(count):
+        q = torch.randn(count, hq, d, generator=gen, device="cuda").bfloat16()
+        k, v = (torch.randn(count, hkv, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+        return q, k, v
+
+    text = torch.arange(n_text, dtype=torch.int32, device="cuda")[:, None].expand(n_text, 4).contiguous()
+    pos = torch.cat([text, _positions(n_text, 0, *grid, n_text)]).contiguous()
+    q, k, v = rows(n_prompt)
+    prompt = pc.Batch(prefix[None].contiguous(), torch.tensor([n_prompt], dtype=torch.int32, device="cuda"), torch.tensor([0, n_prompt], dtype=torch.int32, device="cuda"), n_prompt)
+
+    def enter():
+        pc.pc_paged_append(ctx, pool, prompt, k, v, pos)
+        return pc.pc_paged_attend(work, pool, prompt, q, pos)
+
+    enter()
+    us_prompt = _time(enter, reps)
+    first = [(k, v, pos)]                                # everything that sample 0 has, as it came
+    held = Growing(samples, most, page, free)
+
+    def step(batch, q, k, v, pos, causal):
+        batch.prefix, batch.n_prefix = prefix, n_prompt
+        pc.pc_paged_append(ctx, pool, batch, k, v, pos)
+        return pc.pc_paged_attend(work, pool, batch, q, pos, causal=causal)
+
+    for f in range(1, frames + 1):
+        at = _positions(n_text, f, *grid, n_prompt + (f - 1) * (n + tokens)).repeat(samples, 1)
+        q, k, v = rows(samples * n)
+        frame = (held.grow(n), q, k, v, at, False)
+        step(*frame)
+        first.append((k[:n], v[:n], at[:n]))
+        if f == frames:
+            us_frame = _time(lambda: step(*frame), reps)
+        for i in range(tokens):
+            at = torch.tensor([[n_text + T_STEP * f, 0, 0, n_prompt + (f - 1) * (n + tokens) + n + i]], dtype=torch.int32, device="cuda").repeat(samples, 1)
+            q, k, v = rows(samples)
+            token = (held.grow(1), q, k, v, at, True)
+            out = step(*token)
+            first.append((k[:1], v[:1], at[:1]))
+    us_token = _time(lambda: step(*token), reps)
+    status = pc.pc_poll_status(ctx)
+    assert status == pc.PC_OK, f"device status {status}"
+    keys, values, places = (torch.cat(x).contiguous() for x in zip(*first))
+    want = pc.pc_attend_frame(ctx, pc.Cache(pc.Segment(keys, values, places, len(keys)), pc.Segment.empty(), []), None, q[:1].contiguous(), at[:1].contiguous())
+    token_bytes = 2 * hkv * d * 2
+    report = {"samples": samples, "prompt": n_prompt, "own": held.length[0], "us_prompt": us_prompt, "us_frame": us_frame, "us_token": us_token,
+              "bytes": (n_prompt + sum(held.length)) * token_bytes, "bytes_apart": (samples * n_prompt + sum(held.length)) * token_bytes,
+              "off_frame_kernel": float((out[:1].float() - want.float()).abs().max())}
+    work.close()
+    ctx.close()
+    return report
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--samples", type=int, default=8)
+    ap.add_argument("--frames", type=int, default=3)
+    ap.add_argument("--tokens", type=int, default=4)
+    ap.add_argument("--grid", type=int, nargs=2, default=(24, 42))
+    ap.add_argument("--heads", type=int, nargs=2, default=(24, 8))
+    ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--reps", type=int, default=10)
+    args = ap.parse_args()
+    if not torch.cuda.is_available():
+        raise RuntimeError("the loop needs a CUDA device; there is no CPU fallback")
+    print(json.dumps(generate(args.samples, args.frames, args.tokens, tuple(args.grid), tuple(args.heads), args.page, reps=args.reps)))
+
+
+if __name__ == "__main__":
+    main()
