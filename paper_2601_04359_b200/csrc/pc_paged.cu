@@ -258,12 +258,18 @@ extern "C" pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const p
     A.lse = lse;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (batch->max_rows == 0) return PC_OK;
-    // Rows of a sequence and KV head that fill little of a tile of 128 go to the few-row kernel, which reads as many keys and values for a sixteenth of the rows; a prefix that several such
-    // sequences share is attended once for all their rows.
+    // Rows of a sequence and KV head that fill little of a tile of 128 go to the few-row kernel, which reads as many keys and values for a sixteenth of the rows.  A prefix that several such
+    // sequences share is attended once for all their rows, by the tcgen05 kernel where they are many: two launches more (a wait for their results in any case), which a short prefix is not worth.  Every
+    // sequence's blocks reading it by themselves / once for all, us, one row of 24 / 8 heads: 8 sequences over 1,136 tokens (31 MB more) 17.8 / 23.7, over 4,000 (109) 26.0 / 25.9; 16 over
+    // 1,136 (67) 21.4 / 25.9; 32 over 1,136 (138) 33.3 / 34.2; 64 over 300 (74) 38.4 / 41.8, over 1,136 (280) 66.7 / 44.5; five rows of 32 / 8 heads, two blocks: 8 over 1,136 (62) 32.9 / 38.6, 16 (128) 48.0 /
+    // 46.4.  In fp32 the few-row kernel is bound by its instructions and a third of that is the limit.
     const long long rows = (long long)batch->max_rows * w->ctx->group;
     const bool tc = pc_paged_tc_shape(w->ctx) && w->ctx->attend_impl != 1;
     if (tc && rows > 64) return pc_launch_paged_tc(w, A, false, 0, nullptr, stream);
-    const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows;
+    const pc_layer_desc &D = w->ctx->desc;
+    const long long blocks = (rows + pc_paged_few_block(A, false) - 1) / pc_paged_few_block(A, false);
+    const double again = (double)(batch->n_seqs * blocks - 1) * batch->n_prefix * 2 * D.n_kv_heads * D.head_dim * w->ctx->elem_size;
+    const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows && again > (D.dtype == PC_F32 ? 32e6 : 1e8);
     PagedTcParts left{};
     if (tc && shared && (long long)n_rows * w->ctx->group > PAGED_FEW_ROWS && pc_paged_tc_holds(w->ctx, A.batch)) {
         const pc_status ps = pc_launch_paged_tc(w, A, true, pc_paged_few_block(A, false), &left, stream);

@@ -51,6 +51,7 @@ CASES = {
     "tokens_shared": ([1] * 5, [1, 15, 16, 17, 300], 37, True),
     "tokens_shared_long": ([1] * 33, [1 + 13 * i for i in range(33)], 1025, True),
     "few_shared": ([5, 0, 3, 1], [5, 4, 77, 130], 129, True),
+    "many_tokens_shared": ([1 + (i == 7) for i in range(150)], [1 + i % 40 for i in range(150)], 700, True),
     "few_seeing_all": ([2, 1], [40, 3], 50, False),
     "prompts": ([1, 50, 129, 2, 257], [1, 50, 129, 2, 257], 0, True),
     "pieces": ([33, 100], [200, 101], 0, True),
@@ -76,3 +77,20 @@ def test_attend(shape, case, page):
     compare(got, c.want(causal))
     again = c.attend(work, causal)
     assert torch.equal(_bits(again[0][:-3]), _bits(out[:-3]))
+
+
+@pytest.mark.parametrize("shape,rows,length,prefix", [
+    ("lumos", [1, 1], [3, 40], 25001),                 # six packed rows over a prefix that is read once
+    ("lumos", [1, 1, 1, 1], [3, 1, 40, 17], 9001),     # twelve
+    ("small", [1] * 150, [1 + i % 30 for i in range(150)], 2001),
+    ("odd64", [2] * 100, [2 + i % 30 for i in range(100)], 1501),
+    ("lumos", [5] * 40, [5 + i % 30 for i in range(40)], 1001),
+    ("gqa4", [9] * 12, [9 + i for i in range(12)], 1001),
+])
+def test_a_prefix_read_once(shape, rows, length, prefix):
+    c = Paged(shape, rows, length, prefix=prefix, page=128, behind=3)
+    work = pc.PagedWork(c.ctx)
+    got = c.attend(work)
+    compare(got, c.want())
+    again = c.attend(work)
+    assert torch.equal(_bits(again[0][:-3]), _bits(got[0][:-3])) and pc.pc_poll_status(c.ctx) == pc.PC_OK

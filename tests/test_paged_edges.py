@@ -17,7 +17,7 @@ def _bits(t):
 
 
 # the few-row kernel, the tcgen05 kernel, and both with a prefix
-ROUTES = {"few": ([5, 3, 1], [21, 3, 40], 0), "few_shared": ([5, 3, 1], [21, 3, 40], 37), "many": ([140, 60], [200, 60], 0), "many_prefix": ([140, 60], [200, 60], 50)}
+ROUTES = {"shared": ([5, 3, 1] + [1] * 60, [21, 3, 40] + [9] * 60, 1000), "few": ([5, 3, 1], [21, 3, 40], 0), "few_shared": ([5, 3, 1], [21, 3, 40], 37), "many": ([140, 60], [200, 60], 0), "many_prefix": ([140, 60], [200, 60], 50)}
 
 
 @pytest.mark.parametrize("route", list(ROUTES))
@@ -121,7 +121,7 @@ def test_senseless_numbers_are_recorded(kind, rows, prefix):
     assert pc.pc_poll_status(c.ctx) == pc.PC_OK
 
 
-@pytest.mark.parametrize("rows,prefix,length", [((1, 1, 1, 1), 70, (5, 30, 1, 64)), ((40, 100, 3, 1), 33, (40, 120, 60, 1))])
+@pytest.mark.parametrize("rows,prefix,length", [((1, 1, 1, 1), 70, (5, 30, 1, 64)), ((40, 100, 3, 1), 33, (40, 120, 60, 1)), ((1,) * 50, 1000, tuple(1 + i % 60 for i in range(50)))])
 def test_a_captured_step_replays_with_other_numbers(rows, prefix, length):
     c = Paged("lumos", rows, length, prefix=prefix, page=16, free=0.0)
     work = pc.PagedWork(c.ctx)
@@ -177,7 +177,7 @@ def test_another_stream():
     compare(got, want)
 
 
-@pytest.mark.parametrize("rows,prefix", [((1, 1), 0), ((1,) * 12, 200), ((90, 40), 0)])
+@pytest.mark.parametrize("rows,prefix", [((1, 1), 0), ((1,) * 40, 1000), ((90, 40), 0)])
 def test_waits_that_run_out(rows, prefix):
     c = Paged("lumos", rows, [r + 30 for r in rows], prefix=prefix)
     work = pc.PagedWork(c.ctx)
