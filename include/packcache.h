@@ -498,7 +498,7 @@ typedef struct {
     int32_t n_seqs;           /* up to PC_MAX_SEQS */
     int32_t max_pages;        /* entries of a sequence in `table` */
     int32_t n_prefix;         /* tokens of the prefix; a sequence's own tokens come behind them */
-    int32_t max_rows;         /* no sequence has more rows than this */
+    int32_t max_rows;         /* no sequence has more rows than this.  Kernels are chosen by it, so a loose bound may cost time */
 } pc_batch;
 
 /* Keys and values of a call's rows enter the cache: row i of the n_s rows of sequence s becomes its token length[s] - n_s + i, the key rotated at the row's
@@ -519,7 +519,8 @@ pc_status pc_paged_destroy(pc_paged *w);
  * all of them (a frame).  A row that sees nothing gives out 0 and lse -infinity.  Infinite or NaN values of tokens that a row does not see do not reach it.
  *   q device [n_rows][Hq][d], not rotated; q_pos device [n_rows][4]; out device [n_rows][Hq][d]; lse device [n_rows][Hq] fp32 or NULL.
  * Sums and softmax statistics are fp32.  In bf16 contexts the rotated queries and the probabilities go to the products in bf16, each rounded once.  In
- * fp32 contexts products are of three bf16 parts a number, their terms below 2^-24 left out; infinite keys and queries give NaN there.
+ * fp32 contexts products are of three bf16 parts a number, their terms below 2^-24 left out; infinite keys and queries give NaN there, and values
+ * beyond 3.3e38 are treated as infinite ones are.
  * The context's max_keys does not bound these calls.  Errors: as pc_paged_append. */
 pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const pc_batch *batch, const void *q, const int32_t *q_pos, int32_t n_rows, int32_t causal,
                           void *out, float *lse, void *stream);
@@ -529,7 +530,7 @@ pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const pc_batch *ba
 pc_status pc_poll_status(pc_ctx *ctx, void *stream);
 
 /* Choose the bf16 attention kernel: 0 = tcgen05 tensor-core kernel (default), 1 = CUDA-core kernel (a slow second
- * opinion).  Returns PC_ERR_INVALID_ARG otherwise. */
+ * opinion).  Over a paged cache 1 = the kernel for few rows, whatever their number.  Returns PC_ERR_INVALID_ARG otherwise. */
 pc_status pc_set_attend_impl(pc_ctx *ctx, int32_t impl);
 
 /* Fix the number of key ranges the tensor-core attention kernel splits the keys into (1..4); 0 lets each call
@@ -543,14 +544,14 @@ pc_status pc_set_kv_splits(pc_ctx *ctx, int32_t n);
  * number of work items fits that; results agree up to fp32 rounding order. */
 pc_status pc_set_cluster_merge(pc_ctx *ctx, int32_t on);
 
-/* Limit of every bounded device-side wait of the context's kernels (scoring, tensor-core attention, attention over 4-bit caches, attention mass), in
+/* Limit of every bounded device-side wait of the context's kernels (scoring, tensor-core attention, attention over 4-bit and paged caches, attention mass), in
  * microseconds, to within some ten (0 = the default of about one second; pc_score_tokens_static, which has no context, always
  * waits by the default).  A wait that runs out records PC_ERR_TIMEOUT in the status word, the CTA gives up its remaining work, lets its
  * copies land, frees its tensor memory and exits; the outputs that depended on it are undefined (scores keep what their buffer
  * held) and the context stays usable. */
 pc_status pc_set_wait_limit_us(pc_ctx *ctx, uint32_t limit_us);
 /* Test hook for that path: the first barrier of every CTA of the attention (4-bit caches' too) and mass kernels, and of every warp of the scoring
- * kernel, is told to expect n_bytes more than are ever sent, so its wait runs out after the limit above and pc_poll_status
+ * kernel and of the paged cache's kernel for few rows, is told to expect n_bytes more than are ever sent, so its wait runs out after the limit above and pc_poll_status
  * returns PC_ERR_TIMEOUT; the call's output is then undefined.  0 switches the hook off.  Nothing traps and nothing waits without a limit. */
 pc_status pc_test_expect_extra_bytes(pc_ctx *ctx, uint32_t n_bytes);
 /* Test hook for the merge in the attention kernel.  A CTA with the first part of an item that two CTAs share looks for the other's part

@@ -160,7 +160,7 @@ pc_status check_batch(const pc_ctx *ctx, const pc_pages *pages, const pc_batch *
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess) return PC_ERR_CUDA;
     if (device != ctx->device) return PC_ERR_INVALID_ARG;
-    *out = PagedBatch{b->table, b->length, b->row_start, b->prefix, b->n_seqs, b->max_pages, b->n_prefix, pages->n_pages, n_rows, b->max_rows, log2_of(p), 0, ctx->status};
+    *out = PagedBatch{b->table, b->length, b->row_start, b->prefix, b->n_seqs, b->max_pages, b->n_prefix, pages->n_pages, n_rows, std::min(b->max_rows, n_rows), log2_of(p), 0, ctx->status};
     return PC_OK;
 }
 

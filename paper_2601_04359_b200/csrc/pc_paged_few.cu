@@ -167,7 +167,7 @@ template <int D, bool F32> __device__ __noinline__ void add_odd(const FewParams 
         for (int key = 0; key < n; ++key)
             for (int e = 0; e < E; ++e) {
                 const size_t at = ((row + key) * P.n_kv + I.h) * D + lane * E + e;
-                const float v = F32 ? __ldcg(static_cast<const float *>(P.pool_v) + at) : __bfloat162float(static_cast<const __nv_bfloat16 *>(P.pool_v)[at]);
+                const float v = F32 ? __ldcg(static_cast<const float *>(P.pool_v) + at) : __uint_as_float((uint32_t)__ldcg(static_cast<const unsigned short *>(P.pool_v) + at) << 16);
                 if (F32 ? !(fabsf(v) <= 3.3e38f) : !(fabsf(v) < INFINITY)) x[e] += v;
             }
     }

@@ -61,7 +61,7 @@ constexpr int TM_S = 0, TM_P = TILE, TM_O = 2 * TILE;
 struct TcParams {
     PagedBatch B;
     int n_q_heads, n_kv, group;
-    const __nv_bfloat16 *pool_v;
+    const unsigned short *pool_v;
     int head_rows;           // rows of a KV head among the rotated queries
     int shared;              // the prefix alone, rows of all sequences; what comes out goes to scratch row by row for k_paged_join
     __nv_bfloat16 *out;
@@ -364,7 +364,7 @@ template <int D> __device__ __noinline__ void add_odd(const TcParams &P, Unit U,
     for (int key = first; key < last; ++key) {
         const size_t at = (((size_t)paged_page(B, B.table + (size_t)U.s * B.max_pages + (key >> B.page_shift)) << B.page_shift) + (key & ((1 << B.page_shift) - 1))) * P.n_kv + U.h;
         for (int c = 0; c < D; ++c) {
-            const float v = __bfloat162float(P.pool_v[at * D + c]);
+            const float v = __uint_as_float((uint32_t)__ldcg(P.pool_v + at * D + c) << 16);
             if (fabsf(v) < INFINITY) continue;
             uint32_t o;
             asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(o) : "r"(o_addr + c));
@@ -871,7 +871,7 @@ pc_status pc_launch_paged_tc(const pc_paged *w, const pc_paged_args &A, bool sha
     P.n_kv = D.n_kv_heads;
     P.group = ctx->group;
     P.shared = shared;
-    P.pool_v = static_cast<const __nv_bfloat16 *>(A.pages->v);
+    P.pool_v = static_cast<const unsigned short *>(A.pages->v);
     P.head_rows = (int)head_rows;
     P.out = static_cast<__nv_bfloat16 *>(A.out);
     P.lse = A.lse;

@@ -254,3 +254,13 @@ def test_samples_of_a_prompt(shape):
     step([40, 40, 40, 40], False, n_prompt, table)
     step([2, 0, 1, 5], True, n_prompt, table)
     assert pc.pc_poll_status(prompt.ctx) == pc.PC_OK
+
+
+@pytest.mark.parametrize("shape,most", [("tiny_f32", 2**31 - 1), ("tiny_f32", 6), ("lumos", 2**31 - 1), ("lumos", 6)])
+def test_a_loose_bound_of_rows(shape, most):
+    c = Paged(shape, [5, 1, 3], [21, 40, 3], prefix=37)
+    want = c.want()
+    c.batch.max_rows = most
+    work = pc.PagedWork(c.ctx)
+    compare(c.attend(work), want)
+    assert pc.pc_poll_status(c.ctx) == pc.PC_OK
