@@ -85,12 +85,20 @@ template <int PARTS> __device__ __forceinline__ void split(float x, float y, uin
         }
     }
 }
-// d += the product of two sums of parts, smallest terms first; those below 2^-24 of it left out
+// d += the product of two sums of parts, smallest terms first; those below 2^-24 of it left out.  The instruction's own sums are cut off, not rounded, so a product's terms are summed
+// apart and enter the long sum by an addition that rounds.
 template <int PARTS> __device__ __forceinline__ void mma_parts(float (&d)[4], const uint32_t (&a)[PARTS][4], const uint32_t (&b)[PARTS][2]) {
+    if constexpr (PARTS == 1) {
+        mma16(d, a[0], b[0]);
+    } else {
+        float t[4] = {};
 #pragma unroll
-    for (int sum = PARTS - 1; sum >= 0; --sum)
+        for (int sum = PARTS - 1; sum >= 0; --sum)
 #pragma unroll
-        for (int i = sum; i >= 0; --i) mma16(d, a[i], b[sum - i]);
+            for (int i = sum; i >= 0; --i) mma16(t, a[i], b[sum - i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] += t[i];
+    }
 }
 // halves of a word that are infinite or NaN, as a mask of those that are not
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {

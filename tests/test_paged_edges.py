@@ -264,3 +264,13 @@ def test_a_loose_bound_of_rows(shape, most):
     work = pc.PagedWork(c.ctx)
     compare(c.attend(work), want)
     assert pc.pc_poll_status(c.ctx) == pc.PC_OK
+
+
+@pytest.mark.parametrize("prefix,rows", [(20011, [8]), (3001, [1, 1, 1, 1]), (0, [500, 90])])
+def test_fp32_sums_do_not_drift(prefix, rows):
+    """The error's norm over the output's.  Scores are a few units and sums of 8 rounded terms of 16 channels: 2^-24 x 4 x 3 (root of 8) / 2 on the way; exponential 2^-22, its argument
+    2^-24 x 4; long sums of at most 50 rounded terms, errors of either sign: 2^-24 x 7.  Their root of squares is below 2^-20.8; sums that are cut off, six times a step, pass it."""
+    c = Paged("lumos_f32", rows, [r + 40 if prefix else r for r in rows], prefix=prefix, page=64)
+    out, _ = c.attend(pc.PagedWork(c.ctx))
+    want = c.want()[0]
+    assert (out.double().cpu() - want).norm() <= 2.0 ** -20 * want.norm()
