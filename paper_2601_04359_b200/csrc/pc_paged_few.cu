@@ -554,6 +554,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     // Beside the tcgen05 kernel: that one's wait has been over before this one began, so what it found is there; this one ends behind it, for k_paged_join waits for this one alone.
     if (!P.share) pc_grid_dep_wait();
     const int ctas = P.share ? min(max(__ldcg(P.share + 2), 1), (int)gridDim.x) : (int)gridDim.x, groups = min(P.groups, ctas * F::WARPS / P.n_kv);
+    if ((int)blockIdx.x >= ctas) return;                   // it gets an SM once others are done, and the call would end with its line (3 us later); the others wait below
 
     // ---- the line: steps and items of the whole call, the unit that follows from them, then the sequences' places
     constexpr int THREADS = F::WARPS * 32;
@@ -589,7 +590,23 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
         steps += (long long)pitems * psteps;
         Line L;
         const int spare = items * 2 <= groups ? groups - items : 0;
-        L.unit = spare ? max(P.least, (int)divide(steps + spare - 1, spare)) : 1;
+        L.unit = 1;
+        if (spare) {                                       // the shortest unit with which the items make no more units than there are groups (an even share at least; `steps / spare` is always enough)
+            int lo = max(P.least, (int)divide(steps + groups - 1, groups));
+            L.unit = max(P.least, (int)divide(steps + spare - 1, spare));
+#pragma unroll 1
+            while (lo < L.unit) {
+                const int mid = (lo + L.unit) >> 1;
+                int units = W.lane == 0 ? pitems * ((psteps + mid - 1) / mid) : 0;
+#pragma unroll 1
+                for (int s = W.lane; s < P.B.n_seqs; s += 32) {
+                    const PagedSeq S = seq_of(s);
+                    units += blocks_of(S.n, P.group, 8 * NB) * ((item_steps(P, S.len) + mid - 1) / mid);
+                }
+                units = __reduce_add_sync(0xffffffffu, units);
+                if (units <= groups) L.unit = mid; else lo = mid + 1;
+            }
+        }
         L.prefix_len = made_up(psteps, L.unit);
         L.prefix_end = (long long)pitems * L.prefix_len;
         long long at = L.prefix_end;

@@ -15,6 +15,8 @@
 // memory, to the rows that see them.
 // Tried: queries rotated in this kernel, by four warps more.  Their chains of shuffles, addresses and products are 1,000 instructions a tile at five to ten cycles, 7 us, where a unit of three key tiles takes 4.6:
 // packed prompts 227 us a call instead of 89.  And key tiles shared out evenly along one line, with items of two CTAs added up by one of them: 98 us, since every CTA ends with such an item.
+// A polynomial on the FMA pipes for an eighth to a quarter of the exponentials: a frame of four samples 207 to 220 us instead of 203, as the softmax warps are bound by issue.  Units of one query tile that skip the second
+// one's work: prompts 5 % slower by the loop's code, single tokens no faster.  A unit's words asked for a unit ahead: warp 0 runs out of its 72 registers, packed prompts 92 -> 97 us.
 #include <algorithm>
 
 #include "pc_paged_host.cuh"
@@ -514,13 +516,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         const auto load = [&](const CUtensorMap *map, uint32_t to, const TileRef &T, uint32_t b) {
             if (half < M::HALVES && pg * page_rows < T.n) tma_load_2d(to + half * HALF_BYTES + pg * page_rows * 128, map, T.h * D + half * 64, T.y, b);
         };
-        TileRef A = next(), C = next();
+        TileRef A = next();
         if (A.n >= 0) {
             if (lane == 0) mbar_expect_tx(bar(BAR_K0), bytes(A.n) + P.extra_tx);
             __syncwarp();
             if (lane < 16) load(&map_k, base + M::K, A, bar(BAR_K0));
         }
-        // Query tiles (two a unit) go to three places in turn, tile n where tile n - 3 was.  A unit's first tile is fetched two steps ahead of it, its second one once the unit before it has
+        // Query tiles (two a unit) go to three places in turn, tile n where tile n - 3 was.  A unit's first tile is fetched a step ahead of it, its second one once the unit before it has
         // no more use for its first.
         int fetched = 0;
         const auto fetch_queries = [&](const TileRef &T, int t) {
@@ -532,33 +534,26 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             if (lane < M::HALVES) tma_load_2d(base + M::Q + place * M::TILE_B + lane * HALF_BYTES, &map_q, lane * 64, T.q + (t * TILE < T.rows ? t : 0) * TILE, bar(BAR_QF + place));    // a pair of one tile: the same one twice
             ++fetched;
         };
-        if (A.n >= 0) {
-            fetch_queries(A, 0);
-            fetch_queries(A, 1);
-        }
         const auto begins = [](const TileRef &T) { return T.n >= 0 && T.rows > 0; };
-        bool c_waits = begins(C);                             // the first query tile of the unit that begins with C is still to be fetched
-        for (int gs = 0; alive && A.n >= 0; ++gs) {
-            const TileRef E = next();                         // its page is on the way while this step's copies are issued
-            if (gs > 0 && begins(A)) fetch_queries(A, 1);
-            if (c_waits) fetch_queries(C, 0);
-            bool e_waits = begins(E);
-            if (e_waits && !begins(C)) {                      // (a unit that begins with C has its second tile first)
-                fetch_queries(E, 0);
-                e_waits = false;
+        TileRef C = {0, -1, 0, 0, 0};
+        for (int gs = -1; alive && A.n >= 0; ++gs) {
+            if (gs >= 0) {
+                // PV(step - 2) and QK(step - 1) have read what lies where V(step) and K(step + 1) go
+                if (gs > 0) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
+                if (!alive) break;
+                const int st = gs & 1;
+                if (lane == 0) mbar_expect_tx(bar(BAR_KV + st), bytes(A.n) + (C.n >= 0 ? bytes(C.n) : 0u));
+                __syncwarp();
+                if (lane >= 16) load(&map_v, base + M::V + st * M::TILE_B, A, bar(BAR_KV + st));
+                else if (C.n >= 0) load(&map_k, base + M::K + (st ^ 1) * M::TILE_B, C, bar(BAR_KV + st));
+                A = C;
+                if (begins(A)) fetch_queries(A, 1);
+            } else {
+                fetch_queries(A, 0);
+                fetch_queries(A, 1);
             }
-            if (!alive) break;
-            // PV(step - 2) and QK(step - 1) have read what lies where V(step) and K(step + 1) go
-            if (gs > 0 && alive) alive = warp_wait(bar(BAR_EMPTY + ((gs - 1) & 1)), ((gs - 1) >> 1) & 1, abort_flag, B.status, P.wait_us);
-            if (!alive) break;
-            const int st = gs & 1;
-            if (lane == 0) mbar_expect_tx(bar(BAR_KV + st), bytes(A.n) + (C.n >= 0 ? bytes(C.n) : 0u));
-            __syncwarp();
-            if (lane >= 16) load(&map_v, base + M::V + st * M::TILE_B, A, bar(BAR_KV + st));
-            else if (C.n >= 0) load(&map_k, base + M::K + (st ^ 1) * M::TILE_B, C, bar(BAR_KV + st));
-            A = C;
-            C = E;
-            c_waits = e_waits;
+            C = next();
+            if (begins(C)) fetch_queries(C, 0);
         }
     } else if (warp < 4) {
         // ---------------------------------------------------------------- warps 1 and 2: S = Q_t K^T; warp 3: O += P V.  All lanes wait, one issues.
@@ -658,15 +653,17 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         const uint32_t s_addr = tmem + lane_addr + TM_S, p_addr = tmem + lane_addr + TM_P + t * (TILE / 2), o_addr = tmem + lane_addr + TM_O + t * TILE;
         const bool lead = elect_one();
         bool alive = true;
-        int un = 0, j = 0, lim;
-        Unit U = look(0, alive);
+        // The loop's first pass is a dry one, over whatever tensor memory holds and without its barriers: its instructions are fetched while the first tile is on its way.  (Where they came with
+        // the first step, that one took 4.2 to 5.7 us instead of 1.4.)
+        int un = 0, j = 0, lim = 0;
+        Unit U{};
+        U.nj = 1;
         // own tokens that this thread's row sees (one behind the last row sees what the last one sees; its output is dropped)
         const auto limit = [&]() { return B.causal ? min(U.own, U.before + (U.p0 + min(t * TILE + r, U.rows - 1)) / P.group + 1) : U.own; };
-        lim = limit();
         float m_used = -INFINITY, l = 0.f;
-        int gs = 0;
+        int gs = -1;
         for (; alive && U.nj > 0; ++gs) {
-            const bool flush = j == U.nj;
+            const bool dry = gs < 0, flush = j == U.nj;
             const Unit V = U;                                 // the unit to flush
             const float m_e = m_used, l_e = l;
             if (flush) {
@@ -682,7 +679,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 l = 0.f;
             }
             {
-                alive = warp_wait(bar(BAR_SFULL + t), gs & 1, abort_flag, B.status, P.wait_us);
+                alive = dry || warp_wait(bar(BAR_SFULL + t), gs & 1, abort_flag, B.status, P.wait_us);
                 if (!alive) break;
                 tc_fence_after();
                 uint32_t sv[128];
@@ -693,9 +690,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 tmem_wait_ld();
                 tc_fence_before();
                 __syncwarp();
-                arrive_if(lead, bar(BAR_SFREE + t));
-                if (j + 1 == U.nj) arrive_if(lead, bar(BAR_QE + (2 * un + t) % 3));         // that was the unit's last product with this tile's queries
-                const bool pv_done = gs == 0 || pc_mbar_test(bar(BAR_PVDONE + t), (gs - 1) & 1);
+                arrive_if(lead && !dry, bar(BAR_SFREE + t));
+                if (j + 1 == U.nj) arrive_if(lead && !dry, bar(BAR_QE + (2 * un + t) % 3));         // that was the unit's last product with this tile's queries
+                const bool pv_done = gs <= 0 || pc_mbar_test(bar(BAR_PVDONE + t), (gs - 1) & 1);
                 const int jt = U.j0 + j;
                 const int seen = jt < prefix_tiles ? B.n_prefix - jt * TILE : lim - (jt - prefix_tiles) * TILE;
                 if (__any_sync(0xffffffffu, seen < TILE)) {
@@ -717,7 +714,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                     if (!alive) break;
                 }
                 tc_fence_after();
-                if (t == 1) arrive_if(lead, bar(BAR_EMPTY + (gs & 1)));
+                if (t == 1) arrive_if(lead && !dry, bar(BAR_EMPTY + (gs & 1)));
                 if (__builtin_expect(__any_sync(0xffffffffu, grow), 0)) {
                     const float m_new = fmaxf(m_used, mx);
                     const float corr = m_new == -INFINITY ? 1.f : fast_exp2(m_used - m_new);
@@ -758,7 +755,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                         tmem_wait_st();
                         tc_fence_before();
                         __syncwarp();
-                        arrive_if(lead && !flush, bar(BAR_PHALF + 2 * t + (c >> 1)));
+                        arrive_if(lead && !flush && !dry, bar(BAR_PHALF + 2 * t + (c >> 1)));
                     }
                 }
                 l += (la.x + la.y) + (lb.x + lb.y);
@@ -778,6 +775,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 put_out<D>(P, V, v, m_e, l_e, t, quad, lane);
             }
             ++j;
+            if (__builtin_expect(dry, 0)) {
+                U = look(0, alive);
+                lim = limit();
+                j = 0;
+                m_used = -INFINITY;
+                l = 0.f;
+            }
         }
         if (alive && U.nj > 0) {                              // the last unit
             alive = warp_wait(bar(BAR_PVDONE + t), (gs - 1) & 1, abort_flag, B.status, P.wait_us);
