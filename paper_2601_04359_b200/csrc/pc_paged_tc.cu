@@ -32,6 +32,7 @@ static_assert(128 * REGS_ISSUE + 256 * REGS_SOFTMAX <= TC_THREADS * REGS_LAUNCH,
 constexpr float GROW = 8.f;
 constexpr int PAIR = 2 * TILE;                     // packed rows of an item
 constexpr int LEAST_TILES = 16;                    // a part of a pair has as many key tiles at least (with 4 and parts of three tiles a prompt of 1,136 tokens took 37 us, so 27.5)
+constexpr int LEAST_TILES_FEW = 8;                 // ... where all parts run at once
 constexpr int UNITS = 4;                           // units that are told ahead
 
 // What a unit's warps need to know of it
@@ -114,7 +115,7 @@ __device__ __forceinline__ int pair_tiles(const FrontParams &P, int n, int len, 
 }
 
 __device__ void plan(const FrontParams &P) {
-    __shared__ int pair0[PC_MAX_SEQS + 1], seq_r0[PC_MAX_SEQS], seq_n[PC_MAX_SEQS], seq_len[PC_MAX_SEQS], level[LEVELS];
+    __shared__ int pair0[PC_MAX_SEQS + 1], seq_r0[PC_MAX_SEQS], seq_n[PC_MAX_SEQS], seq_len[PC_MAX_SEQS], level[LEVELS], size[FRONT_THREADS];
     __shared__ long long sums[32];
     __shared__ int counts[2];
     const int tid = threadIdx.x;
@@ -180,8 +181,26 @@ __device__ void plan(const FrontParams &P) {
     paged_scan<FRONT_THREADS>(tiles, sums);
     tiles = sums[FRONT_THREADS / 32 - 1];
     // An even share of all key tiles; a pair with more than a quarter above it is cut, into parts that are over 5/9 of a share each: fewer than two an SM, which the scratch holds.
-    const int share = (int)min((long long)INT32_MAX / 2, max((long long)LEAST_TILES, (tiles * P.n_kv + P.sms - 1) / P.sms));
-    const auto parts_of = [&](int t) { return t <= share + share / 4 ? 1 : (t + share - 1) / share; };
+    int share = (int)min((long long)INT32_MAX / 2, max((long long)LEAST_TILES, (tiles * P.n_kv + P.sms - 1) / P.sms));
+    const auto cut = [](int t, int share) { return t <= share + share / 4 ? 1 : (t + share - 1) / share; };
+    // Where the pairs leave SMs idle: the smallest of sixteen shares with which the parts still run all at once, a warp a share.  (A piece of 128 tokens, three rows each, over 2,000 tokens 37 us uncut, 32 in three
+    // parts; over 8,000 47.5 in parts of sixteen tiles, 58 in ten parts of 6.4, which are more than SMs, 45 in eight of eight; parts of four to six tiles, over 1,000: 26 uncut, 28 to 29 in two or three.)
+    if (pairs * P.n_kv <= P.sms && pairs <= FRONT_THREADS) {
+        if (tid < pairs) {
+            const int s = seq_of(tid);
+            size[tid] = pair_tiles(P, seq_n[s], seq_len[s], tid - pair0[s]);
+        }
+        if (tid == 0) counts[1] = INT32_MAX;
+        __syncthreads();
+        const int even = max(LEAST_TILES_FEW, (int)((tiles * P.n_kv + P.sms - 1) / P.sms)), mine = even + (int)((long long)even * (tid >> 5) / 8);
+        int units = 0;
+        for (int i = tid & 31; i < pairs; i += 32) units += cut(size[i], mine);
+        units = __reduce_add_sync(0xffffffffu, units);
+        if ((tid & 31) == 0 && units * P.n_kv <= P.sms) atomicMin(&counts[1], mine);
+        __syncthreads();
+        if (counts[1] != INT32_MAX) share = counts[1];
+    }
+    const auto parts_of = [&](int t) { return cut(t, share); };
     const auto level_of = [&](int size) { return LEVELS - 1 - min(size, LEVELS - 1); };
     for (int i = tid; i < pairs; i += FRONT_THREADS) {
         const int s = seq_of(i), t = pair_tiles(P, seq_n[s], seq_len[s], i - pair0[s]), parts = parts_of(t);

@@ -274,3 +274,16 @@ def test_fp32_sums_do_not_drift(prefix, rows):
     out, _ = c.attend(pc.PagedWork(c.ctx))
     want = c.want()[0]
     assert (out.double().cpu() - want).norm() <= 2.0 ** -20 * want.norm()
+
+
+@pytest.mark.parametrize("shape,rows,prefix", [("lumos", [128], 2001), ("lumos", [100], 9000), ("gqa4", [50, 200, 1, 90], 2500), ("one", [60, 700], 1500), ("small", [40] * 9, 3000),
+                                               ("lumos", [1400], 300)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_pairs_over_many_tokens(shape, rows, prefix, causal):
+    """Pairs of query tiles that leave SMs idle are cut along the keys, into parts that run at once"""
+    c = Paged(shape, rows, [r + 70 for r in rows], prefix=prefix, page=32, behind=2)
+    work = pc.PagedWork(c.ctx)
+    got = c.attend(work, causal)
+    compare(got, c.want(causal))
+    again = c.attend(work, causal)
+    assert torch.equal(_bits(again[0][:-2]), _bits(got[0][:-2])) and pc.pc_poll_status(c.ctx) == pc.PC_OK
