@@ -138,14 +138,16 @@ struct Line { long long total, prefix_end, per; int prefix_len, groups, rest, un
 __device__ __noinline__ long long divide(long long a, int b) { return ((a | b) >> 32) ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
 
 __device__ __forceinline__ int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
-__device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (rows * group + block - 1) / block; }      // block: 8 or 16
+// (a block is 8 or 16 rows, so that its number is a shift)
+__device__ __forceinline__ long long block_at(long long packed_row, int block) { return packed_row >> (block == 8 ? 3 : 4); }
+__device__ __forceinline__ int blocks_of(int rows, int group, int block) { return (int)block_at(rows * group + block - 1, block); }
 __device__ __forceinline__ int made_up(int len, int unit) { return unit == 1 ? len + GAP : (len + unit - 1) / unit * unit; }
 __device__ __forceinline__ int item_steps(const FewParams &P, int own) { return max(1, (P.shared ? 0 : steps_of(P.B.n_prefix)) + steps_of(own)); }
 __device__ __forceinline__ int prefix_blocks(const FewParams &P) { return P.prefix_here ? blocks_of(paged_rows(P.B), P.group, P.block) : 0; }
 // first place of a group
 __device__ __forceinline__ long long cut(const Line &L, int w) { return L.per * w + (L.rest ? (uint32_t)(L.rest * w) / (uint32_t)L.groups : 0u); }
 // Number of block k of sequence s, the first of whose rows is r0: no two blocks have one, whatever the sequences' rows, and none is beyond rows * group / block + sequences.
-__device__ __forceinline__ int item_index(const FewParams &P, int block, int r0, int s, int k) { return P.own_items + (int)((long long)r0 * P.group / block) + s + k; }
+__device__ __forceinline__ int item_index(const FewParams &P, int block, int r0, int s, int k) { return P.own_items + (int)block_at((long long)r0 * P.group, block) + s + k; }
 // Blocks of a sequence's rows from both ends in turn: where attention is causal, two neighbours on the line have as much to do as any other two.
 __device__ __forceinline__ int zigzag(int k, int n) { return k & 1 ? n - 1 - k / 2 : k / 2; }
 
@@ -530,7 +532,6 @@ template <int D, bool F32, int NB, bool CHECK>
 __global__ void __launch_bounds__(Form<D, F32>::WARPS * 32, 1)
 k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ FewParams P, const __grid_constant__ pc_rope_dev rope) {
     using F = Form<D, F32>;
-    pc_grid_dep_launch();
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (pc_smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gen = smem_raw + (base - pc_smem_u32(smem_raw));
@@ -553,6 +554,7 @@ k_paged_few(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     }
     // Beside the tcgen05 kernel: that one's wait has been over before this one began, so what it found is there; this one ends behind it, for k_paged_join waits for this one alone.
     if (!P.share) pc_grid_dep_wait();
+    pc_grid_dep_launch();                                  // behind the wait: k_paged_join looks at the batch without a wait of its own
     const int ctas = P.share ? min(max(__ldcg(P.share + 2), 1), (int)gridDim.x) : (int)gridDim.x, groups = min(P.groups, ctas * F::WARPS / P.n_kv);
     if ((int)blockIdx.x >= ctas) return;                   // it gets an SM once others are done, and the call would end with its line (3 us later); the others wait below
 
@@ -701,11 +703,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
     const FewParams &P = J.F;
     pc_grid_dep_launch();
     const int s = blockIdx.x % P.B.n_seqs, k = blockIdx.x / P.B.n_seqs, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    pc_grid_dep_wait();
+    // ahead of the wait: the launch before has begun behind its own, so the batch is what it will find
     const PagedSeq S = paged_seq(P.B, s);
-    const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block);
+    const int packed = S.n * P.group, blocks = blocks_of(S.n, P.group, P.block), block = zigzag(k, blocks), p0 = block * P.block, n = min(P.block, packed - p0);
+    pc_grid_dep_wait();
     if (k >= blocks) return;
-    const int block = zigzag(k, blocks), p0 = block * P.block, n = min(P.block, packed - p0);
     const int2 w = __ldcg(P.groups_of + item_index(P, P.block, S.r0, s, k));
     if (!P.shared && w.x == w.y) return;                   // its warp has written the output
     const int sets = max(1, JOIN_WARPS / n);
@@ -729,8 +731,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) k_paged_join(const __grid_con
             if (P.shared && P.B.n_prefix > 0) {
                 const long long row = (long long)S.r0 * P.group + p;      // packed row of the batch
                 if (P.prefix_here) {
-                    const int2 v = __ldcg(P.groups_of + row / P.block);
-                    pre = from(v.x, v.y, (int)(row % P.block), P.home_rows + home);
+                    const int2 v = __ldcg(P.groups_of + block_at(row, P.block));
+                    pre = from(v.x, v.y, (int)(row & (P.block - 1)), P.home_rows + home);
                 } else {
                     const PagedTcRow T = paged_tc_row(J.T, P.n_kv, h, row);
                     const size_t slot = T.first * PAGED_TC_TILE + T.row;
