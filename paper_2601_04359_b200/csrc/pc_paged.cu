@@ -260,16 +260,17 @@ extern "C" pc_status pc_paged_attend(pc_paged *w, const pc_pages *pages, const p
     if (batch->max_rows == 0) return PC_OK;
     // Rows of a sequence and KV head that fill little of a tile of 128 go to the few-row kernel, which reads as many keys and values for a sixteenth of the rows.  A prefix that several such
     // sequences share is attended once for all their rows, by the tcgen05 kernel where they are many: two launches more (a wait for their results in any case), which a short prefix is not worth.  Every
-    // sequence's blocks reading it by themselves / once for all, us, one row of 24 / 8 heads: 8 sequences over 1,136 tokens (31 MB more) 17.8 / 23.7, over 4,000 (109) 26.0 / 25.9; 16 over
-    // 1,136 (67) 21.4 / 25.9; 32 over 1,136 (138) 33.3 / 34.2; 64 over 300 (74) 38.4 / 41.8, over 1,136 (280) 66.7 / 44.5; five rows of 32 / 8 heads, two blocks: 8 over 1,136 (62) 32.9 / 38.6, 16 (128) 48.0 /
-    // 46.4.  In fp32 the few-row kernel is bound by its instructions and a third of that is the limit.
+    // sequence's blocks reading it by themselves / once for all, us, one row of 24 / 8 heads: 8 sequences over 1,136 tokens (32 MB more) 16.3 / 23.0, over 4,000 (114) 23.2 / 25.1; 16 over
+    // 1,136 (69) 20.6 / 25.5; 32 over 1,136 (144) 28.3 / 27.1; 64 over 300 (77) 27.6 / 31.0, over 1,136 (293) 46.6 / 34.7; five rows of 32 / 8 heads, two blocks: 8 over 1,136 (69) 29.1 / 34.9, 16 (144) 39.1 /
+    // 34.9; one row of 4 / 2 heads of 64 channels: 200 over 1,136 (115) 36.1 / 27.6.  In fp32 the few-row kernel is bound by its instructions and the limit is lower: 24 / 8 heads, 8 over 500 (28) 28.1 / 34.8, over 1,136
+    // (65) 39.7 / 36.0; 4 / 2 heads of 64, 64 over 500 (32) 22.8 / 23.9, over 2,000 (129) 44.7 / 25.1.
     const long long rows = (long long)batch->max_rows * w->ctx->group;
     const bool tc = pc_paged_tc_shape(w->ctx) && w->ctx->attend_impl != 1;
     if (tc && rows > 64) return pc_launch_paged_tc(w, A, false, 0, nullptr, stream);
     const pc_layer_desc &D = w->ctx->desc;
     const long long blocks = (rows + pc_paged_few_block(A, false) - 1) / pc_paged_few_block(A, false);
     const double again = (double)(batch->n_seqs * blocks - 1) * batch->n_prefix * 2 * D.n_kv_heads * D.head_dim * w->ctx->elem_size;
-    const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows && again > (D.dtype == PC_F32 ? 32e6 : 1e8);
+    const bool shared = batch->n_prefix > 0 && batch->n_seqs > 1 && (size_t)n_rows <= w->home_rows && again > (D.dtype == PC_F32 ? 4e7 : 1e8);
     PagedTcParts left{};
     if (tc && shared && (long long)n_rows * w->ctx->group > PAGED_FEW_ROWS && pc_paged_tc_holds(w->ctx, A.batch)) {
         const pc_status ps = pc_launch_paged_tc(w, A, true, pc_paged_few_block(A, false), &left, stream);

@@ -10,6 +10,8 @@
 // sequence, 549 MB of 128 sequences came at 4.3 TB/s).  A warp fetches its own steps by TMA into its own ring (a page holds a whole number of steps, so a step is two boxes of 16 rows a 64 channels)
 // and meets no other warp: an item that several groups share leaves (maximum, sum, output) of each in scratch, and k_paged_join adds them up in the order of the keys.
 // The line follows from lengths that lie on the device: every CTA adds them up for itself.
+// Measured (24 / 8 heads, 128 channels, bf16; a call with its join): a row of 4 sequences over 1,136 tokens shared and up to 300 own 15.4 us, all of it latency; of 128 over 24,320 and up to 2,016, beside the tcgen05 kernel,
+// 131 us, 5.0 TB/s.  A step of 16 keys takes a warp 0.78 us with 8 rows and 1.4 with 16, eight warps an SM.
 #include <algorithm>
 
 #include "pc_paged.cuh"

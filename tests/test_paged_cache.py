@@ -86,6 +86,9 @@ def test_attend(shape, case, page):
     ("odd64", [2] * 100, [2 + i % 30 for i in range(100)], 1501),
     ("lumos", [5] * 40, [5 + i % 30 for i in range(40)], 1001),
     ("gqa4", [9] * 12, [9 + i for i in range(12)], 1001),
+    ("tiny_f32", [1] * 80, [1 + i % 30 for i in range(80)], 1501),
+    ("lumos_f32", [1] * 9, [1 + 7 * i for i in range(9)], 2001),
+    ("lumos_f32", [3, 1, 4, 1, 5], [40, 3, 4, 50, 21], 2501),
 ])
 def test_a_prefix_read_once(shape, rows, length, prefix):
     c = Paged(shape, rows, length, prefix=prefix, page=128, behind=3)
