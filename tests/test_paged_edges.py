@@ -287,3 +287,23 @@ def test_few_pairs_over_many_tokens(shape, rows, prefix, causal):
     compare(got, c.want(causal))
     again = c.attend(work, causal)
     assert torch.equal(_bits(again[0][:-2]), _bits(got[0][:-2])) and pc.pc_poll_status(c.ctx) == pc.PC_OK
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, one context: the same bits as one after the other"""
+    a = Paged("lumos", [1] * 40, [1 + i % 30 for i in range(40)], prefix=1500, page=64, max_q=400)
+    b = Paged("lumos", [140, 60], [200, 90], prefix=70, page=16, seed=5, ctx=a.ctx)
+    calls = [(a, pc.PagedWork(a.ctx)), (b, pc.PagedWork(a.ctx))]
+    alone = [c.attend(w)[0].clone() for c, w in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    got = [[], []]
+    for _ in range(20):
+        for i, (c, w) in enumerate(calls):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(c.attend(w)[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for x in got[i]:
+            assert torch.equal(_bits(x), _bits(alone[i]))
+    assert pc.pc_poll_status(a.ctx) == pc.PC_OK
